@@ -1,7 +1,7 @@
 """Python names for the C ABI of libsignsgd.so -- argument marshalling only.
 
 Each function below has the name and the argument order of its C entry point (see
-``include/signsgd.h``) and does nothing but check tensor types, take ``data_ptr()`` and the
+``include/signsgd.h`` and ``include/signsgd_train.h``) and does nothing but check tensor types, take ``data_ptr()`` and the
 current CUDA stream, call into the library and raise on a non-zero status. All arithmetic
 of Algorithm 1 happens in the CUDA kernels. There is no CPU fallback: if the library has
 not been built (``python -m paper_1810_05291_b200.build``), the first call raises.
@@ -27,6 +27,10 @@ SS_MAX_WORKERS = 64
 SS_STATIC_STAGING_BYTES = 64 << 20
 SS_FLAGS_MAX_TIMEOUT_NS = 2_000_000_000
 
+SS_ACT8_GROUP = 32
+SS_ACT_GELU, SS_ACT_SILU = 0, 1
+SS_PREF_SIGMOID, SS_PREF_HINGE, SS_PREF_SQUARED = 0, 1, 2
+
 SS_OK = 0
 SS_ERR_INVALID_ARG = -1
 SS_ERR_MISALIGNED = -2
@@ -39,7 +43,10 @@ EXPORTS = ("ss_packed_words", "ss_status_string", "ss_last_cuda_error", "ss_sign
            "ss_vote_apply", "ss_vote_apply_segments", "ss_signum_update_push", "ss_vote_tally", "ss_fused_step_host", "ss_fused_step_host_static", "ss_set_launch_option",
            "ss_ternary_words", "ss_absmax", "ss_ternary_pack", "ss_ternary_unpack",
            "ss_flags_signal", "ss_flags_wait", "ss_flags_signal_wait", "ss_vote_apply_guarded",
-           "ss_vote_apply_guarded_segments")
+           "ss_vote_apply_guarded_segments",
+           "ss_act8_bytes", "ss_act8_pack", "ss_act8_unpack", "ss_act8_forward", "ss_act8_backward",
+           "ss_weight_grad8", "ss_weight_grad8_workspace", "ss_loss_workspace", "ss_policy_loss",
+           "ss_preference_loss")
 
 
 class ss_segment(ctypes.Structure):
@@ -104,6 +111,23 @@ def lib() -> ctypes.CDLL:
     L.ss_vote_apply_guarded.argtypes = [vp, i32, i64, u64, vp, f32, f32, vp, vp, vp]
     L.ss_vote_apply_guarded_segments.argtypes = [vp, i32, i64, u64, vp, vp, i32, vp, vp, vp]
     L.ss_flags_signal_wait.argtypes = [vp, i32, i32, vp, i32, ctypes.c_uint32, u64, vp, vp]
+    L.ss_act8_bytes.argtypes = [i64, i64]
+    L.ss_act8_pack.argtypes = [vp, i64, i32, i64, i64, vp, vp]
+    L.ss_act8_unpack.argtypes = [vp, i64, i64, vp, i64, i32, vp]
+    L.ss_act8_forward.argtypes = [vp, i64, vp, i64, i32, i32, i64, i64, vp, i64, vp, vp, vp, vp]
+    L.ss_act8_backward.argtypes = [vp, i64, vp, vp, i32, i32, i64, i64, vp, i64, vp, i64, vp]
+    L.ss_weight_grad8_workspace.argtypes = [vp, i64, i32, i64, i64, i64]
+    L.ss_weight_grad8.argtypes = [vp, i64, i32, vp, i64, i64, i64, vp, i64, i32, vp, i64, vp]
+    L.ss_loss_workspace.argtypes = [i64, i64]
+    L.ss_policy_loss.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, vp, i64,
+                                 vp, i64, vp]
+    L.ss_preference_loss.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, i64, vp, f32, i32, f32, f32, f32, vp, vp, vp,
+                                     vp, vp, vp, i64, vp, i64, vp]
+    for name in ("ss_act8_bytes", "ss_weight_grad8_workspace", "ss_loss_workspace"):
+        getattr(L, name).restype = i64
+    for name in ("ss_act8_pack", "ss_act8_unpack", "ss_act8_forward", "ss_act8_backward", "ss_weight_grad8",
+                 "ss_policy_loss", "ss_preference_loss"):
+        getattr(L, name).restype = i32
     for name in ("ss_flags_signal", "ss_flags_wait", "ss_flags_signal_wait", "ss_vote_apply_guarded",
                  "ss_vote_apply_guarded_segments"):
         getattr(L, name).restype = i32
@@ -460,3 +484,160 @@ def ss_vote_apply_guarded_segments(packed: Sequence[torch.Tensor], param: torch.
                                                 _segments(segments_dev, n_segments), int(n_segments), w_ptr,
                                                 _dev(skip_if_nonzero_dev, torch.int32, "skip_if_nonzero_dev", 1),
                                                 _stream(stream)), "ss_vote_apply_guarded_segments")
+
+
+# ---- training operators (include/signsgd_train.h) -----------------------------------------------
+
+def _mat(t: torch.Tensor, dtype, name: str, shape=None):
+    """(address, row stride) of a 2-D CUDA tensor with unit column stride."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError("%s must have shape %s, has %s" % (name, "[rows, cols]" if shape is None else list(shape), list(t.shape)))
+    stride, unit = t.stride()
+    if unit != 1 and t.shape[1] > 1:
+        raise ValueError("%s must have unit column stride" % name)
+    return t.data_ptr(), stride
+
+
+def _vec(t: torch.Tensor, dtype, name: str, n: int) -> int:
+    if t.dtype != dtype or not t.is_cuda or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise (TypeError if t.dtype != dtype else ValueError)("%s must be a contiguous CUDA tensor of %d %s" % (name, n, dtype))
+    return t.data_ptr()
+
+
+def _opt_vec(t: Optional[torch.Tensor], dtype, name: str, n: int) -> Optional[int]:
+    return None if t is None else _vec(t, dtype, name, n)
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor):
+    """The caller's workspace, or one of the size asked for from PyTorch's allocator."""
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif not workspace.is_cuda or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA uint8 tensor")
+    return workspace
+
+
+def ss_act8_bytes(rows: int, cols: int) -> int:
+    return int(lib().ss_act8_bytes(int(rows), int(cols)))
+
+
+def act8_checkpoint(rows: int, cols: int, device) -> torch.Tensor:
+    """Storage for the 8-bit checkpoint of a [rows, cols] matrix."""
+    return torch.empty(ss_act8_bytes(rows, cols), dtype=torch.uint8, device=device)
+
+
+def _ckpt(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
+    return _vec(t, torch.uint8, name, rows * (SS_ACT8_GROUP + 1) * -(-cols // SS_ACT8_GROUP))
+
+
+def ss_act8_pack(x: torch.Tensor, ckpt: torch.Tensor, stream=None) -> None:
+    code, (ptr, stride) = _dtype_code(x), _mat(x, x.dtype, "x")
+    rows, cols = x.shape
+    _check(lib().ss_act8_pack(ptr, stride, code, rows, cols, _ckpt(ckpt, rows, cols, "ckpt"), _stream(stream)),
+           "ss_act8_pack")
+
+
+def ss_act8_unpack(ckpt: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    code, (ptr, stride) = _dtype_code(out), _mat(out, out.dtype, "out")
+    rows, cols = out.shape
+    _check(lib().ss_act8_unpack(_ckpt(ckpt, rows, cols, "ckpt"), rows, cols, ptr, stride, code, _stream(stream)),
+           "ss_act8_unpack")
+
+
+def ss_act8_forward(x: torch.Tensor, up: Optional[torch.Tensor], act: int, y: torch.Tensor, ckpt_x: torch.Tensor,
+                    ckpt_up: Optional[torch.Tensor] = None, ckpt_y: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    code, dt, shape = _dtype_code(x), x.dtype, x.shape
+    x_ptr, x_stride = _mat(x, dt, "x")
+    rows, cols = shape
+    u_ptr, u_stride = (None, 0) if up is None else _mat(up, dt, "up", shape)
+    y_ptr, y_stride = _mat(y, dt, "y", shape)
+    _check(lib().ss_act8_forward(x_ptr, x_stride, u_ptr, u_stride, code, act, rows, cols, y_ptr, y_stride,
+                                 _ckpt(ckpt_x, rows, cols, "ckpt_x"),
+                                 None if ckpt_up is None else _ckpt(ckpt_up, rows, cols, "ckpt_up"),
+                                 None if ckpt_y is None else _ckpt(ckpt_y, rows, cols, "ckpt_y"), _stream(stream)),
+           "ss_act8_forward")
+
+
+def ss_act8_backward(dy: torch.Tensor, ckpt_x: torch.Tensor, ckpt_up: Optional[torch.Tensor], act: int,
+                     dx: torch.Tensor, dup: Optional[torch.Tensor] = None, stream=None) -> None:
+    code, dt, shape = _dtype_code(dy), dy.dtype, dy.shape
+    dy_ptr, dy_stride = _mat(dy, dt, "dy")
+    rows, cols = shape
+    dx_ptr, dx_stride = _mat(dx, dt, "dx", shape)
+    du_ptr, du_stride = (None, 0) if dup is None else _mat(dup, dt, "dup", shape)
+    _check(lib().ss_act8_backward(dy_ptr, dy_stride, _ckpt(ckpt_x, rows, cols, "ckpt_x"),
+                                  None if ckpt_up is None else _ckpt(ckpt_up, rows, cols, "ckpt_up"), code, act, rows,
+                                  cols, dx_ptr, dx_stride, du_ptr, du_stride, _stream(stream)), "ss_act8_backward")
+
+
+def ss_weight_grad8_workspace(dy: torch.Tensor, n_in: int) -> int:
+    ptr, stride = _mat(dy, dy.dtype, "dy")
+    return int(lib().ss_weight_grad8_workspace(ptr, stride, _dtype_code(dy), dy.shape[0], dy.shape[1], int(n_in)))
+
+
+def ss_weight_grad8(dy: torch.Tensor, ckpt_x: torch.Tensor, dw: torch.Tensor, accumulate: bool = False,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    code, (dy_ptr, dy_stride) = _dtype_code(dy), _mat(dy, dy.dtype, "dy")
+    rows, n_out = dy.shape
+    dw_ptr, dw_stride = _mat(dw, torch.float32, "dw")
+    if dw.shape[0] != n_out:
+        raise ValueError("dw must have one row for each of dy's %d columns" % n_out)
+    n_in = dw.shape[1]
+    L = lib()
+    if workspace is None:
+        need = L.ss_weight_grad8_workspace(dy_ptr, dy_stride, code, rows, n_out, n_in)
+        workspace = _scratch(None, max(need, 0), dy) if need else None
+    w_ptr, w_bytes = (None, 0) if workspace is None else (_scratch(workspace, 0, dy).data_ptr(), workspace.numel())
+    _check(L.ss_weight_grad8(dy_ptr, dy_stride, code, _ckpt(ckpt_x, rows, n_in, "ckpt_x"), rows, n_out, n_in, dw_ptr,
+                             dw_stride, int(bool(accumulate)), w_ptr, w_bytes, _stream(stream)), "ss_weight_grad8")
+
+
+def ss_loss_workspace(rows: int, n_pairs: int = 0) -> int:
+    return int(lib().ss_loss_workspace(int(rows), int(n_pairs)))
+
+
+def ss_policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Tensor,
+                   ref_logp: Optional[torch.Tensor], advantages: torch.Tensor, weights: torch.Tensor,
+                   totals: torch.Tensor, logp: torch.Tensor, dlogits: Optional[torch.Tensor] = None,
+                   inv_temperature: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                   grad_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    f32, code = torch.float32, _dtype_code(logits)
+    z_ptr, z_stride = _mat(logits, logits.dtype, "logits")
+    rows, vocab = logits.shape
+    d_ptr, d_stride = (None, 0) if dlogits is None else _mat(dlogits, logits.dtype, "dlogits", logits.shape)
+    L = lib()
+    ws = _scratch(workspace, 0 if workspace is not None else L.ss_loss_workspace(rows, 0), logits)
+    _check(L.ss_policy_loss(z_ptr, z_stride, code, rows, vocab, _vec(targets, torch.int64, "targets", rows),
+                            _vec(old_logp, f32, "old_logp", rows), _opt_vec(ref_logp, f32, "ref_logp", rows),
+                            _vec(advantages, f32, "advantages", rows), _vec(weights, f32, "weights", rows),
+                            inv_temperature, clip_low, clip_high, kl_coef, _opt_vec(grad_scale, f32, "grad_scale", 1),
+                            _vec(totals, f32, "totals", 3), _vec(logp, f32, "logp", rows), d_ptr, d_stride,
+                            ws.data_ptr(), ws.numel(), _stream(stream)), "ss_policy_loss")
+
+
+def ss_preference_loss(logits: torch.Tensor, targets: torch.Tensor, weights: torch.Tensor, seq_begin: torch.Tensor,
+                       ref_seq_logp: torch.Tensor, loss: torch.Tensor, margins: torch.Tensor, seq_logp: torch.Tensor,
+                       logp: torch.Tensor, dlogits: Optional[torch.Tensor] = None, inv_temperature: float = 1.0,
+                       kind: int = SS_PREF_SIGMOID, beta: float = 0.1, label_smoothing: float = 0.0,
+                       scale: float = 1.0, grad_scale: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    f32, i64, code = torch.float32, torch.int64, _dtype_code(logits)
+    z_ptr, z_stride = _mat(logits, logits.dtype, "logits")
+    rows, vocab = logits.shape
+    pairs = margins.shape[0]
+    d_ptr, d_stride = (None, 0) if dlogits is None else _mat(dlogits, logits.dtype, "dlogits", logits.shape)
+    L = lib()
+    ws = _scratch(workspace, 0 if workspace is not None else L.ss_loss_workspace(rows, pairs), logits)
+    _check(L.ss_preference_loss(z_ptr, z_stride, code, rows, vocab, _vec(targets, i64, "targets", rows),
+                                _vec(weights, f32, "weights", rows), _vec(seq_begin, i64, "seq_begin", 2 * pairs + 1),
+                                pairs, _vec(ref_seq_logp, f32, "ref_seq_logp", 2 * pairs), inv_temperature, kind, beta,
+                                label_smoothing, scale, _opt_vec(grad_scale, f32, "grad_scale", 1),
+                                _vec(loss, f32, "loss", 1), _vec(margins, f32, "margins", pairs),
+                                _vec(seq_logp, f32, "seq_logp", 2 * pairs), _vec(logp, f32, "logp", rows), d_ptr,
+                                d_stride, ws.data_ptr(), ws.numel(), _stream(stream)), "ss_preference_loss")

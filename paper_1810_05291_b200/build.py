@@ -21,13 +21,17 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsignsgd.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "signsgd")
 
-SOURCES = ["abi.cu", "step_f32.cu", "step_bf16.cu", "vote_apply.cu", "noalloc.cu", "ternary.cu", "exchange_flags.cu"]
-HEADERS = ["bitslice.cuh", "common.cuh", "step_kernel.cuh", "step_oct_kernel.cuh", "exchange.cuh", os.path.join("..", "..", "include", "signsgd.h")]
+SOURCES = ["abi.cu", "step_f32.cu", "step_bf16.cu", "vote_apply.cu", "noalloc.cu", "ternary.cu", "exchange_flags.cu",
+           "act8.cu", "weight_grad8.cu", "losses.cu"]
+HEADERS = ["bitslice.cuh", "common.cuh", "step_kernel.cuh", "step_oct_kernel.cuh", "exchange.cuh", "train.cuh", "act8.cuh",
+           os.path.join("..", "..", "include", "signsgd.h"), os.path.join("..", "..", "include", "signsgd_train.h")]
 
 # -fmad=false: no multiply-add contraction anywhere (the arithmetic also uses explicitly
-# rounded intrinsics); no -use_fast_math, denormals kept.
+# rounded intrinsics); no -use_fast_math, denormals kept. The training operators are compared with
+# a tolerance, not bit for bit, and may contract.
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-fmad=false", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
+              "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
+CONTRACTED = ("act8.cu", "weight_grad8.cu", "losses.cu")
 
 
 def _nvcc() -> str:
@@ -54,7 +58,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
     def compile_one(src: str) -> str:
         obj = os.path.join(OBJ_DIR, os.path.splitext(src)[0] + ".o")
-        cmd = [nvcc] + NVCC_FLAGS + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
+        contract = [] if src in CONTRACTED else ["-fmad=false"]
+        cmd = [nvcc] + NVCC_FLAGS + contract + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if verbose or r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
