@@ -23,7 +23,7 @@ OBJ_DIR = os.path.join(ROOT, "_build", "signsgd")
 
 SOURCES = ["abi.cu", "step_f32.cu", "step_bf16.cu", "vote_apply.cu", "noalloc.cu", "ternary.cu", "exchange_flags.cu",
            "act8.cu", "weight_grad8.cu", "losses.cu"]
-HEADERS = ["bitslice.cuh", "common.cuh", "step_kernel.cuh", "step_oct_kernel.cuh", "exchange.cuh", "train.cuh", "act8.cuh",
+HEADERS = ["bitslice.cuh", "common.cuh", "step_kernel.cuh", "step_oct_kernel.cuh", "exchange.cuh", "train.cuh", "act8.cuh", "tcgen05.cuh",
            os.path.join("..", "..", "include", "signsgd.h"), os.path.join("..", "..", "include", "signsgd_train.h")]
 
 # -fmad=false: no multiply-add contraction anywhere (the arithmetic also uses explicitly

@@ -1,68 +1,520 @@
 // Weight gradient of a linear layer from its input kept in 8 bits: dW[n, k] (+)= sum_t dY[t, n] x^[t, k].
+//
+// The contraction runs over the rows t, so both operands lie in memory with the contraction index
+// slow, and go to the matrix unit that way, without a transpose: tiles of dY by TMA, tiles of x^
+// decoded by eight warps from the 8-bit codes straight into the swizzled operand layout. A decoded
+// value has 7 significant bits and is exact in bf16; no operand is rounded.
+//
+// Sums. The matrix unit adds into fp32 with truncation: measured with inputs of mean 0, its sums
+// come out low by 1e-9 of their size for each row (1.9e-5 for 16384 rows). So a tile is summed
+// there over 512 rows at a time, in one half of the tensor memory, and the eight warps add that
+// to fp32 registers, rounding to nearest, while the matrix unit fills the other half: 5e-7.
+#include <cuda.h>
+
+#include <atomic>
+
 #include "act8.cuh"
+#include "tcgen05.cuh"
 
 namespace ss {
 namespace {
 
-struct WeightGrad {
-    const void* dy;
-    Ckpt x;
-    float* dw;
-    int64_t dy_stride, dw_stride, rows, n_out, n_in;
-    int accumulate;
+constexpr int kTileN = 128, kTileK = 256;  // of dW: n from dY, k from x^
+constexpr int kRows = 64;                  // rows of a stage
+constexpr int kStages = 4;
+constexpr int kChunk = 8;                  // stages summed in the matrix unit
+constexpr int kWorkers = 512;              // threads that decode and add
+constexpr int kThreads = kWorkers + 128;   // and a warp each for the copies and the matrix unit (two more idle)
+// A worker holds 64 sums and its share of a stage's codes. The block is launched with 96 registers
+// a thread (what 640 threads leave of an SM's 65536); the other warps give some of theirs up:
+// 512 * 112 + 128 * 32 = 640 * 96 = 61440.
+constexpr int kWorkerRegs = 112, kOtherRegs = 32;
+constexpr int kSums = kTileK / (kWorkers / 128);  // columns of a worker
+constexpr uint32_t kPanel = kRows * 128;   // bytes of 64 columns of a stage
+constexpr uint32_t kBytesA = kTileN / 64 * kPanel, kBytesB = kTileK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
+constexpr uint32_t kSquareBytes = 32 * 16 * 4;  // a worker warp's way out
+constexpr size_t kSmem = 1024 + kStages * kStageBytes + kWorkers / 32 * kSquareBytes;
+
+struct Plan {
+    int tiles_n, tiles_k;   // tiles of dW; tile i: n index i % tiles_n
+    int planes;             // bf16 terms of dY: 1, or 3 for fp32
+    int stages_per_plane;   // stages of one plane
+    int whole;              // tiles formed by one block from all rows
+    int parts;              // parts that each of the other tiles' rows are split in
+    int part_stages;
+    int units;              // whole + others * parts
 };
 
-// Rows summed before a partial sum is added to the whole: a sum of 16384 rows one after the other
-// would be off by a few 1e-6 of its size, in chunks of 512 by a few 1e-7.
-constexpr int64_t kChunkRows = 512;
+struct WeightGrad {
+    Ckpt x;
+    float* dw;
+    float* partial;  // one tile for each part
+    int64_t dw_stride, rows, n_out, n_in;
+    int accumulate;
+    Plan plan;
+};
 
-// A block forms a 64 x 64 tile of dW in fp32 from slices of 16 rows staged in shared memory, a
-// thread 4 x 4 of it.
-template <typename T>
-__global__ void __launch_bounds__(256) weight_grad8_kernel(const __grid_constant__ WeightGrad a) {
-    __shared__ float s_dy[16][64], s_x[16][64];
-    const int tid = threadIdx.x, tn = (tid >> 4) * 4, tk = (tid & 15) * 4;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.y) * 64, k0 = static_cast<int64_t>(blockIdx.x) * 64;
-    const T* dy = static_cast<const T*>(a.dy);
-    float acc[4][4] = {}, whole[4][4] = {};
-    for (int64_t t0 = 0; t0 < a.rows; t0 += 16) {
+struct Unit {
+    int tile, first, stages;
+    bool whole;
+};
+
+__device__ __forceinline__ Unit unit_of(const Plan& p, int u) {
+    if (u < p.whole) return Unit{u, 0, p.planes * p.stages_per_plane, true};
+    const int v = u - p.whole, part = v % p.parts, all = p.planes * p.stages_per_plane;
+    const int first = part * p.part_stages;
+    return Unit{p.whole + v / p.parts, first, min(p.part_stages, all - first), p.parts == 1};
+}
+
+struct Shared {
+    uint64_t full_a[kStages], full_b[kStages], empty[kStages], summed[2], last;
+    uint32_t tmem;
+    int abort;
+};
+
+// Two codes of a word (its bytes 2 i, 2 i + 1) as two bf16. With E the exponent field of 2^(e+7),
+// E | magnitude is 2^e (128 + magnitude) and E alone 2^e 128, both with the code's sign; their
+// difference is exact. A marked group has E of an infinity: inf - inf and NaN - inf are NaN.
+template <int PAIR>
+__device__ __forceinline__ uint32_t decode_pair(uint32_t w, uint32_t e2) {
+    const uint32_t r = __byte_perm(w, 0, PAIR == 0 ? 0x1100 : 0x3322);
+    const uint32_t a = (r & 0x807F807Fu) | e2, b = (r & 0x80008000u) | e2;
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+__device__ __forceinline__ uint32_t exponent_pair(uint32_t exp_byte) {
+    const uint32_t e = exp_byte == 255u ? 255u : exp_byte + 7u;
+    return (e << 7) | (e << 23);
+}
+
+// The worker's share of a stage of codes: 16 columns of two rows, 32 rows apart.
+struct Codes {
+    uint4 q[2];
+    uint32_t e[2];
+};
+
+// Where they are: of the row t, in steps of a stage.
+struct Walk {
+    const uint8_t *values, *exps;
+    int t, left;  // rows from t to the plane's end; negative: columns that do not exist
+
+    __device__ __forceinline__ void start(const WeightGrad& a, int stage, int k0, int tid) {
+        const int64_t k = static_cast<int64_t>(k0) + 16 * (tid & 15);
+        t = stage * kRows + (tid >> 4);
+        left = k < a.x.groups * SS_ACT8_GROUP ? static_cast<int>(a.rows) : 0;
+        values = a.x.values + t * a.x.groups * SS_ACT8_GROUP + k;
+        exps = a.x.exps + t * a.x.groups + (k >> 5);
+    }
+    __device__ __forceinline__ void next(const WeightGrad& a) {
+        t += kRows;
+        values += a.x.groups * (SS_ACT8_GROUP * kRows);
+        exps += a.x.groups * kRows;
+    }
+    __device__ __forceinline__ void load(const WeightGrad& a, Codes* c) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = (tid >> 6) + 4 * i, c = tid & 63;
-            const int64_t t = t0 + r, n = n0 + c, k = k0 + c;
-            s_dy[r][c] = t < a.rows && n < a.n_out ? Elem<T>::load(dy + t * a.dy_stride + n) : 0.0f;
-            float v = 0.0f;
-            if (t < a.rows && k < a.n_in) {
-                const int64_t g = t * a.x.groups + k / SS_ACT8_GROUP;
-                v = act8_value(a.x.values[t * a.x.groups * SS_ACT8_GROUP + k], act8_unit(a.x.exps[g]));
+        for (int i = 0; i < 2; ++i) {
+            c->q[i] = make_uint4(0u, 0u, 0u, 0u);
+            c->e[i] = 1u;
+            if (t + 32 * i < left) {
+                c->q[i] = *reinterpret_cast<const uint4*>(values + i * 32 * a.x.groups * SS_ACT8_GROUP);
+                c->e[i] = exps[i * 32 * a.x.groups];
             }
-            s_x[r][c] = v;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(s_dy[r][tn + i], s_x[r][tk + j], acc[i][j]);
-        __syncthreads();
-        if ((t0 + 16) % kChunkRows == 0 || t0 + 16 >= a.rows) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) whole[i][j] += acc[i][j], acc[i][j] = 0.0f;
         }
     }
+};
+
+// Decodes them into the stage's operand: column chunk c (8 columns, 16 bytes) of row t sits at
+// chunk c ^ (t & 7) of the row. Lanes 8 apart in a row address the same banks in another panel;
+// half of them store their second chunk first, so that eight lanes always cover all banks.
+__device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const Codes& c) {
+    const int piece = tid & 15, t0 = tid >> 4;
+    const uint32_t panel = stage_b + (piece >> 2) * kPanel;
+    const uint32_t chunk = 2 * (piece & 3), swap = (piece >> 2) & 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = t0 + 32 * i;
+        const uint32_t e2 = exponent_pair(c.e[i]);
+        const uint32_t w[4] = {c.q[i].x, c.q[i].y, c.q[i].z, c.q[i].w};
+        uint32_t d[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[2 * j] = decode_pair<0>(w[j], e2), d[2 * j + 1] = decode_pair<1>(w[j], e2);
+        const uint32_t row = panel + t * 128;
+        const uint32_t first = row + (((chunk + swap) ^ (t & 7)) << 4), second = row + (((chunk + 1 - swap) ^ (t & 7)) << 4);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(first), "r"(swap ? d[4] : d[0]), "r"(swap ? d[5] : d[1]),
+                     "r"(swap ? d[6] : d[2]), "r"(swap ? d[7] : d[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(second), "r"(swap ? d[0] : d[4]), "r"(swap ? d[1] : d[5]),
+                     "r"(swap ? d[2] : d[6]), "r"(swap ? d[3] : d[7]) : "memory");
+    }
+}
+
+// Where 32 rows of a tile go: dW, or the part's own tile.
+struct Dest {
+    float* p;
+    int64_t stride;
+    int rows, cols;  // that exist, from p on
+    bool add;
+};
+
+__device__ __forceinline__ Dest dest_of(const WeightGrad& a, int unit, int n_local, int k_local) {
+    const Unit u = unit_of(a.plan, unit);
+    if (!u.whole) {
+        float* t = a.partial + static_cast<int64_t>(unit - a.plan.whole) * kTileN * kTileK;
+        return Dest{t + n_local * kTileK + k_local, kTileK, kTileN - n_local, kTileK - k_local, false};
+    }
+    const int64_t n = static_cast<int64_t>(u.tile % a.plan.tiles_n) * kTileN + n_local;
+    const int64_t k = static_cast<int64_t>(u.tile / a.plan.tiles_n) * kTileK + k_local;
+    return Dest{a.dw + n * a.dw_stride + k, a.dw_stride, static_cast<int>(min(a.n_out - n, static_cast<int64_t>(kTileN))),
+                static_cast<int>(min(a.n_in - k, static_cast<int64_t>(kTileK))), a.accumulate != 0};
+}
+
+// 32 x 16 sums, a row a lane, through the warp's own shared memory so that each row is written by
+// neighbouring lanes. 16-byte chunk c of row r is kept at chunk c ^ (r / 2 mod 4).
+__device__ __forceinline__ void stage_square(uint32_t buf, int lane, const float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)), "f"(v[4 * i]),
+                     "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
+}
+
+__device__ __forceinline__ void store_square(uint32_t buf, int lane, const Dest& d, int col) {
+    if (col + 16 <= d.cols && (reinterpret_cast<uintptr_t>(d.p) & 15) == 0 && (d.stride & 3) == 0) {
+        const int chunk = lane & 3;
+#pragma unroll 2
+        for (int r = lane >> 2; r < 32; r += 8) {
+            if (r >= d.rows) break;
+            float4 v;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                         : "r"(buf + r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4)) : "memory");
+            float4* p = reinterpret_cast<float4*>(d.p + r * d.stride + col + 4 * chunk);
+            if (d.add) {
+                const float4 o = *p;
+                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+            }
+            *p = v;
+        }
+    } else {
+        const int c = lane & 15;
+        if (col + c >= d.cols) return;
+#pragma unroll 2
+        for (int r = lane >> 4; r < min(32, d.rows); r += 2) {
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(buf + r * 64 + (((c >> 2) ^ ((r >> 1) & 3)) << 4) + (c & 3) * 4) : "memory");
+            float* p = d.p + r * d.stride + col + c;
+            *p = d.add ? *p + v : v;
+        }
+    }
+}
+
+// A wait ran out: nothing of this block's tiles can be trusted, and that shows.
+__device__ __noinline__ void spoil(const WeightGrad& a, int tid) {
+    for (int unit = blockIdx.x; unit < a.plan.units; unit += gridDim.x) {
+        const int tile = unit_of(a.plan, unit).tile;
+        const int64_t n0 = static_cast<int64_t>(tile % a.plan.tiles_n) * kTileN, k0 = static_cast<int64_t>(tile / a.plan.tiles_n) * kTileK;
+        for (int i = tid; i < kTileN * kTileK; i += kWorkers) {
+            const int64_t n = n0 + i / kTileK, k = k0 + i % kTileK;
+            if (n < a.n_out && k < a.n_in) a.dw[n * a.dw_stride + k] = __uint_as_float(0x7FC00000u);
+            if (unit >= a.plan.whole && a.plan.parts > 1)
+                a.partial[static_cast<int64_t>(unit - a.plan.whole) * kTileN * kTileK + i] = __uint_as_float(0x7FC00000u);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ WeightGrad a) {
+    extern __shared__ uint8_t dynamic[];
+    __shared__ Shared sh;
+    const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    const Plan& p = a.plan;
+    volatile int* abort = &sh.abort;
+
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_addr(&sh.full_a[s]), 1);
+            mbar_init(smem_addr(&sh.full_b[s]), kWorkers / 32);
+            mbar_init(smem_addr(&sh.empty[s]), 1);
+        }
+        mbar_init(smem_addr(&sh.summed[0]), 1);
+        mbar_init(smem_addr(&sh.summed[1]), 1);
+        mbar_init(smem_addr(&sh.last), 1);
+        sh.abort = 0;
+        mbar_init_visible();
+    }
+    if (warp == 0) tmem_alloc(smem_addr(&sh.tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+
+    if (warp < kWorkers / 32) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWorkerRegs));
+        // ---- decoding, and sums of the chunks. A chunk is added while the next one is decoded, after
+        // its first four stages: the last of them goes to the slot of the chunk's last stage, so the
+        // matrix unit has finished the chunk by then, and has four stages ready to work on meanwhile.
+        const int lane = tid & 31, n_local = (warp & 3) * 32, k_local = (warp >> 2) * kSums;
+        const uint32_t out = stages + kStages * kStageBytes + warp * kSquareBytes;
+        const uint32_t tmem_at = tmem + (static_cast<uint32_t>(n_local) << 16) + k_local;
+        float acc[kSums];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t n = n0 + tn + i, k = k0 + tk + j;
-            if (n < a.n_out && k < a.n_in) {
-                float* p = a.dw + n * a.dw_stride + k;
-                *p = a.accumulate ? *p + whole[i][j] : whole[i][j];
+        for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
+        int it = 0, added = 0;                   // stages decoded, chunks added
+        int unit = blockIdx.x, at = 0, left = 0; // where the next chunk begins: its first stage, stages left of the unit
+        int prev_unit = -1;                      // the chunk to add: its unit, and whether it ends it
+        bool prev_ends = false;
+        int k0 = 0;
+        Walk walk{};
+        Codes codes{};
+        bool ok = true;
+        while (ok) {
+            if (left == 0 && unit < p.units) {
+                const Unit u = unit_of(p, unit);
+                at = u.first % p.stages_per_plane, left = u.stages;
+                k0 = u.tile / p.tiles_n * kTileK;
+                walk.start(a, at, k0, tid);
+                walk.load(a, &codes);
+            }
+            const int len = min(kChunk, left);
+#pragma unroll 1
+            for (int s = 0;; ++s) {
+                if (s == min(kStages, len) && prev_unit >= 0) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[added & 1]), (added >> 1) & 1, abort));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t src = tmem_at + (added & 1) * kTileK;
+#pragma unroll
+                    for (int j = 0; j < kSums; j += 16) {
+                        uint32_t r[16];
+                        tmem_load16(src + j, r);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[j + i] += __uint_as_float(r[i]);
+                    }
+                    tc_fence_before();
+                    ++added;
+                    if (prev_ends) {
+                        const Dest d = dest_of(a, prev_unit, n_local, k_local);
+#pragma unroll
+                        for (int j = 0; j < kSums; j += 16) {
+                            stage_square(out, lane, acc + j);
+                            __syncwarp();
+                            store_square(out, lane, d, j);
+                            __syncwarp();
+                        }
+#pragma unroll
+                        for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
+                    }
+                    prev_unit = -1;
+                }
+                if (s >= len) break;
+                const int slot = it % kStages;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.empty[slot]), ((it / kStages) & 1) ^ 1, abort));
+                if (!ok) break;
+                store_codes(stages + slot * kStageBytes + kBytesA, tid, codes);
+                smem_to_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.full_b[slot]));
+                ++it;
+                if (++at == p.stages_per_plane) {  // the next plane goes over the same codes again
+                    at = 0;
+                    walk.start(a, 0, k0, tid);
+                } else {
+                    walk.next(a);
+                }
+                if (s + 1 < left) walk.load(a, &codes);  // on their way while the slot is waited for
+            }
+            if (!ok || len == 0) break;
+            prev_unit = unit;
+            left -= len;
+            prev_ends = left == 0;
+            if (prev_ends) unit += gridDim.x;
+        }
+        if (!ok) spoil(a, tid);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == kWorkers / 32) {
+            // ---- copies of dY
+            if ((tid & 31) == 0) {
+                int it = 0;
+                bool ok = true;
+                for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+                    const Unit u = unit_of(p, unit);
+                    const int n0 = (u.tile % p.tiles_n) * kTileN;
+#pragma unroll 1
+                    for (int s = 0; s < u.stages; ++s, ++it) {
+                        const int slot = it % kStages;
+                        ok = mbar_wait(smem_addr(&sh.empty[slot]), ((it / kStages) & 1) ^ 1, abort);
+                        if (!ok) break;
+                        const uint32_t bar = smem_addr(&sh.full_a[slot]), dst = stages + slot * kStageBytes;
+                        const int at = u.first + s, plane = at / p.stages_per_plane, t0 = (at - plane * p.stages_per_plane) * kRows;
+                        mbar_expect(bar, kBytesA);
+                        tma_load_3d(dst, &dy_map, bar, n0, t0, plane);
+                        tma_load_3d(dst + kPanel, &dy_map, bar, n0 + 64, t0, plane);
+                    }
+                }
+                if (!ok) {  // the copies under way end in this block's memory: not before they have
+                    int own = 0;
+                    for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
+                        mbar_wait(smem_addr(&sh.full_a[i % kStages]), (i / kStages) & 1, &own);
+                }
+            }
+        } else if (warp == kWorkers / 32 + 1) {
+            // ---- matrix unit
+            if ((tid & 31) == 0) {
+                constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK);
+                int it = 0, chunk = 0;
+                bool ok = true;
+                for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+                    const Unit u = unit_of(p, unit);
+#pragma unroll 1
+                    for (int s = 0; s < u.stages; ++s, ++it) {
+                        const int slot = it % kStages;
+                        ok = mbar_wait(smem_addr(&sh.full_a[slot]), (it / kStages) & 1, abort) &&
+                             mbar_wait(smem_addr(&sh.full_b[slot]), (it / kStages) & 1, abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t at = stages + slot * kStageBytes, d = tmem + (chunk & 1) * kTileK;
+#pragma unroll
+                        for (int k = 0; k < kRows / 16; ++k)
+                            tc_mma_bf16(d, tc_desc_rows(at + k * 2048, kPanel), tc_desc_rows(at + kBytesA + k * 2048, kPanel), idesc,
+                                        (s % kChunk) != 0 || k != 0);
+                        tc_commit(smem_addr(&sh.empty[slot]));
+                        if (s % kChunk == kChunk - 1 || s + 1 == u.stages) {
+                            tc_commit(smem_addr(&sh.summed[chunk & 1]));
+                            ++chunk;
+                        }
+                    }
+                }
+                if (!ok) {  // nothing may still be running when the tensor memory is given back
+                    int own = 0;
+                    tc_commit(smem_addr(&sh.last));
+                    mbar_wait(smem_addr(&sh.last), 0, &own);
+                }
+                for (int i = it > kStages ? it - kStages : 0; ok && i < it; ++i)  // its signals arrive in this block's memory
+                    ok = mbar_wait(smem_addr(&sh.empty[i % kStages]), (i / kStages) & 1, abort);
             }
         }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_free(tmem, 512);
+}
+
+// dW of the tiles whose rows were split: the parts added in their order.
+__global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ WeightGrad a) {
+    const Plan& p = a.plan;
+    const int other = blockIdx.x, tile = p.whole + other;
+    const int64_t n0 = static_cast<int64_t>(tile % p.tiles_n) * kTileN, k0 = static_cast<int64_t>(tile / p.tiles_n) * kTileK;
+    const float* src = a.partial + static_cast<int64_t>(other) * p.parts * kTileN * kTileK;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < kTileN * kTileK; i += gridDim.y * 256) {
+        const int64_t n = n0 + i / kTileK, k = k0 + i % kTileK;
+        if (n >= a.n_out || k >= a.n_in) continue;
+        float v = src[i];
+        for (int s = 1; s < p.parts; ++s) v += src[static_cast<int64_t>(s) * kTileN * kTileK + i];
+        float* d = a.dw + n * a.dw_stride + k;
+        *d = a.accumulate ? *d + v : v;
+    }
+}
+
+__global__ void __launch_bounds__(256) zero_kernel(float* dw, int64_t stride, int64_t n_out, int64_t n_in) {
+    const int64_t total = n_out * n_in;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256)
+        dw[i / n_in * stride + i % n_in] = 0.0f;
+}
+
+// dY as the copies want it: bf16, rows at multiples of 16 bytes. An fp32 value is the sum of three
+// bf16: its leading 8 bits, the next 8 and the last 8, cut off, so that the sum is exact and
+// nothing overflows; an infinity or NaN is carried by the first alone.
+template <typename T>
+__global__ void __launch_bounds__(256) stage_dy_kernel(const T* dy, int64_t stride, int64_t rows, int64_t n_out, uint16_t* out, int64_t out_stride) {
+    const int64_t total = rows * out_stride, plane = total;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t t = i / out_stride, n = i - t * out_stride;
+        if constexpr (sizeof(T) == 2) {
+            out[i] = n < n_out ? dy[t * stride + n] : uint16_t(0);
+        } else {
+            const float v = n < n_out ? dy[t * stride + n] : 0.0f;
+            uint32_t hi = __float_as_uint(v) & 0xFFFF0000u, mid = 0, lo = 0;
+            if ((hi & 0x7F800000u) == 0x7F800000u) {
+                if (v != v) hi = 0x7FC00000u;
+            } else {
+                const float rest = v - __uint_as_float(hi);
+                mid = __float_as_uint(rest) & 0xFFFF0000u;
+                lo = __float_as_uint(rest - __uint_as_float(mid));
+            }
+            out[i] = static_cast<uint16_t>(hi >> 16);
+            out[plane + i] = static_cast<uint16_t>(mid >> 16);
+            out[2 * plane + i] = static_cast<uint16_t>(lo >> 16);
+        }
+    }
+}
+
+constexpr int64_t kMaxUnits = 1 << 24;  // tiles, and stages: rows and their products with kRows stay in 32 bits
+
+// How dY reaches the matrix unit, and how the work is cut. The blocks take whole tiles as long as
+// every SM gets one; the tiles that are left over (all, if there are fewer than SMs) have their
+// rows split so that they too keep most SMs busy.
+struct Layout {
+    bool staged;
+    int64_t stride, planes;  // of the staged copy
+    int64_t staged_bytes, partial_bytes;
+    Plan plan;
+};
+
+int layout_of(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int64_t n_out, int64_t n_in, int sms, Layout* out) {
+    const Mat m = mat(dy, rows, n_out, dy_stride, dtype_bytes(dt));
+    out->staged = dt == SS_F32 || !m.row_aligned(16) || m.stride * 2 % 16 != 0 || m.stride * 2 >= (int64_t(1) << 40);
+    out->planes = dt == SS_F32 ? 3 : 1;
+    out->stride = out->staged ? (n_out + 7) / 8 * 8 : m.stride;
+    out->staged_bytes = out->staged ? (out->planes * rows * out->stride * 2 + 255) / 256 * 256 : 0;
+    const int64_t tn = (n_out + kTileN - 1) / kTileN, tk = (n_in + kTileK - 1) / kTileK, per = (rows + kRows - 1) / kRows;
+    if (tn * tk > kMaxUnits || per * out->planes > kMaxUnits) return SS_ERR_UNSUPPORTED;
+    Plan& p = out->plan;
+    p.tiles_n = static_cast<int>(tn), p.tiles_k = static_cast<int>(tk);
+    p.planes = static_cast<int>(out->planes), p.stages_per_plane = static_cast<int>(per);
+    const int tiles = static_cast<int>(tn * tk), all = p.planes * p.stages_per_plane, others = tiles % sms;
+    p.whole = tiles - others;
+    p.parts = 1;
+    p.part_stages = all;
+    if (others > 0) {
+        int parts = sms / others;
+        if (parts > all / kChunk) parts = all / kChunk;  // a part is at least one chunk
+        if (parts > 1) {
+            const int chunks = (all + kChunk - 1) / kChunk;
+            p.part_stages = (chunks + parts - 1) / parts * kChunk;
+            p.parts = (all + p.part_stages - 1) / p.part_stages;
+        }
+    }
+    p.units = p.whole + others * p.parts;
+    out->partial_bytes = p.parts > 1 ? static_cast<int64_t>(others) * p.parts * kTileN * kTileK * 4 : 0;
+    return SS_OK;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled(cudaError_t* err) {
+    static std::atomic<void*> known{nullptr};
+    void* f = known.load(std::memory_order_relaxed);
+    *err = cudaSuccess;
+    if (f == nullptr) {
+        cudaDriverEntryPointQueryResult found;
+        *err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+        if (*err == cudaSuccess && (found != cudaDriverEntryPointSuccess || f == nullptr)) *err = cudaErrorSymbolNotFound;
+        if (*err != cudaSuccess) return nullptr;
+        known.store(f, std::memory_order_relaxed);
+    }
+    return reinterpret_cast<EncodeTiled>(f);
+}
+
+// SMs that the plan is made for. Without a device (sizes asked for on a host without one) the B200's.
+int plan_sms() {
+    cudaError_t err = cudaSuccess;
+    const int sms = device_sm_count(&err);
+    return err == cudaSuccess && sms > 0 ? sms : 148;
 }
 
 }  // namespace
@@ -73,9 +525,12 @@ using namespace ss;
 extern "C" {
 #pragma GCC visibility push(default)
 
-int64_t ss_weight_grad8_workspace(const void*, int64_t, ss_dtype dt, int64_t rows, int64_t n_out, int64_t n_in) {
-    if (!dtype_known(dt) || !sides_ok(rows, n_out) || !sides_ok(rows, n_in)) return -1;
-    return 0;
+int64_t ss_weight_grad8_workspace(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int64_t n_out, int64_t n_in) {
+    if (!dtype_known(dt) || !sides_ok(rows, n_out) || !sides_ok(rows, n_in) || !stride_ok(rows, n_out, dy_stride)) return -1;
+    if (rows == 0 || n_out == 0 || n_in == 0) return 0;
+    Layout l;
+    if (layout_of(dy, dy_stride, dt, rows, n_out, n_in, plan_sms(), &l) != SS_OK) return -1;
+    return l.staged_bytes + l.partial_bytes;
 }
 
 int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_t* ckpt_x, int64_t rows,
@@ -88,19 +543,57 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     const Mat mw = mat(dw, n_out, n_in, dw_stride, 4), my = mat(dy, rows, n_out, dy_stride, eb);
     if (dw == nullptr || (rows > 0 && (dy == nullptr || ckpt_x == nullptr))) return SS_ERR_INVALID_ARG;
     if (!addr_aligned(dw, 4)) return SS_ERR_MISALIGNED;
-    if (rows > 0) {
-        if (!addr_aligned(dy, eb) || !addr_aligned(ckpt_x, 16)) return SS_ERR_MISALIGNED;
-        const size_t kept = ss_act8_bytes(rows, n_in);
-        if (mats_overlap(mw, my) || mat_overlaps(mw, ckpt_x, kept)) return SS_ERR_INVALID_ARG;
-    }
-    const int64_t need = ss_weight_grad8_workspace(dy, dy_stride, dt, rows, n_out, n_in);
-    if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return SS_ERR_INVALID_ARG;
-    const WeightGrad a{dy, ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, n_in), dw, my.stride, mw.stride, rows, n_out, n_in, accumulate};
-    const dim3 grid(static_cast<unsigned>((n_in + 63) / 64), static_cast<unsigned>((n_out + 63) / 64));
-    if (grid.y > 65535u) return SS_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SS_F32) weight_grad8_kernel<float><<<grid, 256, 0, st>>>(a);
-    else weight_grad8_kernel<uint16_t><<<grid, 256, 0, st>>>(a);
+    if (rows == 0) {
+        if (accumulate) return SS_OK;
+        const int64_t blocks = (n_out * n_in + 255) / 256;
+        zero_kernel<<<static_cast<unsigned>(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(dw, mw.stride, n_out, n_in);
+        return cuda_status_public(cudaGetLastError());
+    }
+    if (!addr_aligned(dy, eb) || !addr_aligned(ckpt_x, 16)) return SS_ERR_MISALIGNED;
+    const size_t kept = ss_act8_bytes(rows, n_in);
+    if (mats_overlap(mw, my) || mat_overlaps(mw, ckpt_x, kept)) return SS_ERR_INVALID_ARG;
+    Layout l;
+    const int status = layout_of(dy, dy_stride, dt, rows, n_out, n_in, plan_sms(), &l);
+    if (status != SS_OK) return status;
+    const int64_t need = l.staged_bytes + l.partial_bytes;
+    if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return SS_ERR_INVALID_ARG;
+    if (need > 0) {
+        if (!addr_aligned(workspace, 256)) return SS_ERR_MISALIGNED;
+        if (mat_overlaps(mw, workspace, need) || mat_overlaps(my, workspace, need) || bytes_overlap(ckpt_x, kept, workspace, need))
+            return SS_ERR_INVALID_ARG;
+    }
+    cudaError_t e;
+    const EncodeTiled encode = encode_tiled(&e);
+    if (encode == nullptr) return cuda_status_public(e);
+    const int sms = device_sm_count(&e);
+    if (e != cudaSuccess) return cuda_status_public(e);
+
+    CUtensorMap map;
+    const cuuint64_t row_bytes = static_cast<cuuint64_t>(l.stride) * 2;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(n_out), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(l.planes)};
+    const cuuint64_t strides[2] = {row_bytes, l.planes > 1 ? row_bytes * rows : row_bytes};
+    const cuuint32_t box[3] = {64, kRows, 1}, ones[3] = {1, 1, 1};
+    void* src = l.staged ? workspace : const_cast<void*>(dy);
+    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, src, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return SS_ERR_UNSUPPORTED;
+    e = cudaFuncSetAttribute(weight_grad8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+    if (e != cudaSuccess) return cuda_status_public(e);
+
+    if (l.staged) {
+        const int64_t want = (rows * l.stride + 255) / 256, most = static_cast<int64_t>(sms) * 16;
+        const unsigned grid = static_cast<unsigned>(want < most ? want : most);
+        if (dt == SS_F32) stage_dy_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
+        else stage_dy_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
+    }
+    float* partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.staged_bytes);
+    const WeightGrad a{ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, n_in), dw, partial, mw.stride, rows, n_out, n_in, accumulate, l.plan};
+    weight_grad8_kernel<<<static_cast<unsigned>(l.plan.units < sms ? l.plan.units : sms), kThreads, kSmem, st>>>(map, a);
+    if (l.plan.parts > 1) {
+        const unsigned others = static_cast<unsigned>(l.plan.tiles_n * l.plan.tiles_k - l.plan.whole);
+        join_parts_kernel<<<dim3(others, 16), 256, 0, st>>>(a);
+    }
     return cuda_status_public(cudaGetLastError());
 }
 
