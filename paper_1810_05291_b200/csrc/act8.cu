@@ -1,134 +1,387 @@
 // Activations kept in 8 bits: packing, unpacking, and the (gated) activation's two passes.
+#include <type_traits>
+
 #include "act8.cuh"
 
 namespace ss {
 namespace {
 
-// f and f' in fp32.
+// f and f' in fp32, with the hardware's exponential and reciprocal (each within two units in the
+// last place; the results are held to 1e-6 of |x|, and stored in 8 or 24 bits).
 //   silu: s = 1 / (1 + exp(-x)), f = x s, f' = s (1 + x (1 - s))
 //   gelu: f = x Phi(x), f' = Phi(x) + x phi(x), Phi(x) = (1 + erf(x / sqrt 2)) / 2
+__device__ __forceinline__ float sigmoid_fast(float x) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_value(float x) {
-    if constexpr (ACT == SS_ACT_SILU) return x / (1.0f + expf(-x));
+    if constexpr (ACT == SS_ACT_SILU) return x * sigmoid_fast(x);
     else return x * (0.5f + 0.5f * erff(x * 0.70710678118654752f));
 }
 
 template <int ACT>
 __device__ __forceinline__ void act_value_slope(float x, float* f, float* slope) {
     if constexpr (ACT == SS_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-x));
+        const float s = sigmoid_fast(x);
         *f = x * s;
         *slope = s * (1.0f + x * (1.0f - s));
     } else {
         const float cdf = 0.5f + 0.5f * erff(x * 0.70710678118654752f);
+        float phi;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(phi) : "f"(x * x * -0.72134752044448170f));
         *f = x * cdf;
-        *slope = cdf + x * 0.39894228040143268f * expf(-0.5f * x * x);
+        *slope = cdf + x * 0.39894228040143268f * phi;
     }
 }
 
-// One lane holds one column of a group, a warp the group.
-__device__ __forceinline__ void keep_lane(const Ckpt& c, int64_t row, int64_t group, int lane, float x) {
-    const uint32_t a = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & 0x7FFFFFFFu);
+// ---- pieces of 8 columns ---------------------------------------------------------------------------
+// A thread takes 8 columns of a row, four neighbouring lanes a group of 32. Pieces are numbered in
+// the checkpoint's order, so its values and exponents are read and written in one run; row and
+// column follow by a division.
+constexpr int kPiece = 8;
+constexpr int kBlock = 256;
+
+struct Pieces {
+    int64_t groups;      // of one row
+    int64_t total;       // pieces: rows * groups * 4
+    int64_t cols;
+    uint32_t mul;        // n / groups = (n * mul) >> (32 + shift) for n < 2^31
+    int shift;           // -1: groups == 1, -2: too many for 32 bits
+
+    __device__ __forceinline__ int64_t row_of(int64_t g) const {
+        if (shift >= 0) return __umulhi(static_cast<uint32_t>(g), mul) >> shift;
+        return shift == -1 ? g : g / groups;
+    }
+};
+
+// With l = ceil(log2 d) and m = ceil(2^(31+l) / d) < 2^32: n m = n 2^(31+l) / d + n r with r < 1, and
+// n r < 2^31 does not reach the next multiple of 2^(31+l) / d for n < 2^31.
+Pieces pieces_of(int64_t rows, int64_t cols) {
+    Pieces p{act8_groups(cols), 0, cols, 0, -2};
+    p.total = rows * p.groups * 4;
+    if (p.groups == 1) {
+        p.shift = -1;
+    } else if (rows * p.groups < (int64_t(1) << 31)) {
+        int l = 1;
+        while ((int64_t(1) << l) < p.groups) ++l;
+        p.mul = static_cast<uint32_t>(((uint64_t(1) << (31 + l)) + p.groups - 1) / p.groups);
+        p.shift = l - 1;
+    }
+    return p;
+}
+
+// One matrix of a call. In a kernel for aligned rows every row starts on 16 bytes.
+struct Side {
+    void* p;
+    int64_t stride;  // elements
+    int64_t bytes;   // extent
+};
+
+// Words s .. of a run of words, and half a word further if `half`.
+template <int N, int KEEP>
+__device__ __forceinline__ void shift_words(uint32_t (&w)[N], uint32_t s, bool half) {
+#pragma unroll
+    for (int i = 0; i + 2 < N; ++i) w[i] = (s & 2) ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i + 1 < N; ++i) w[i] = (s & 1) ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) w[i] = half ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+}
+
+template <typename T>
+struct Eight {
+    static constexpr int kWords = kPiece * sizeof(T) / 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+    }
+    __device__ __forceinline__ void set(const float (&v)[kPiece]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) w[i] = __float_as_uint(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPiece; i += 2) w[i >> 1] = bf16_pair(v[i], v[i + 1]);
+        }
+    }
+
+    // `n` columns that exist (0 .. 8) from p on; the others are 0. Rows that do not start on 16
+    // bytes are read as the aligned vectors around the piece, shifted into place, where all of
+    // those lie within the matrix.
+    template <bool ALIGNED>
+    __device__ __forceinline__ void load(const Side& m, const T* p, int n) {
+        if (ALIGNED && n == kPiece) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
+                w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+            }
+            return;
+        }
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), begin = reinterpret_cast<uintptr_t>(m.p);
+        const uintptr_t base = at & ~static_cast<uintptr_t>(15);
+        if (!ALIGNED && n == kPiece && base >= begin && base + 4 * kWords + 16 <= begin + m.bytes) {
+            uint32_t x[kWords + 4];
+#pragma unroll
+            for (int i = 0; i < kWords + 4; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(base + 4 * i);
+                x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+            }
+            shift_words<kWords + 4, kWords>(x, (at & 15) >> 2, sizeof(T) == 2 && (at & 2) != 0);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = x[i];
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            if (i >= n) break;
+            if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+            else w[i >> 1] |= static_cast<uint32_t>(p[i]) << (16 * (i & 1));
+        }
+    }
+
+    __device__ __forceinline__ void store_some(T* p, int from, int to) const {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            if (i < from || i >= to) continue;
+            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+            else p[i] = static_cast<T>(w[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+
+    // Where rows do not start on 16 bytes, the aligned vectors that begin in the previous piece
+    // are put together from the lane before, so that all but a run's ends are whole vectors.
+    // Every lane of the warp calls it; `joined`: the lane before holds the piece before, whole.
+    template <bool ALIGNED>
+    __device__ __forceinline__ void store(T* p, int n, bool joined) const {
+        if (ALIGNED) {
+            if (n == kPiece) {
+#pragma unroll
+                for (int i = 0; i < kWords; i += 4)
+                    *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p) + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+            } else {
+                store_some(p, 0, n);
+            }
+            return;
+        }
+        uint32_t x[kWords + 4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __shfl_up_sync(0xFFFFFFFFu, w[kWords - 4 + i], 1);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) x[4 + i] = w[i];
+        const uint32_t m = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u;
+        const bool vector = joined && n == kPiece;                                   // writes from its aligned address on
+        const bool follows = __shfl_down_sync(0xFFFFFFFFu, vector, 1) && (threadIdx.x & 31) != 31;  // the next lane writes this one's end
+        const int end = follows ? kPiece - static_cast<int>(m / sizeof(T)) : n;
+        if (vector) {
+            const uint32_t o = 16u - m;  // of the run, from where the vectors are taken
+            if (o < 16u) {
+                shift_words<kWords + 4, kWords>(x, o >> 2, sizeof(T) == 2 && (o & 2) != 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) x[i] = w[i];
+            }
+            uint4* q = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) & ~static_cast<uintptr_t>(15));
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) q[i / 4] = make_uint4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            store_some(p, kPiece - static_cast<int>(m / sizeof(T)), follows ? 0 : kPiece);
+        } else {
+            store_some(p, 0, end);
+        }
+    }
+};
+
+// A piece to the checkpoint; every lane of the warp calls it.
+template <typename T>
+__device__ __forceinline__ void keep(const Ckpt& c, int64_t i, bool in, const Eight<T>& v) {
+    uint32_t a = 0;
+#pragma unroll
+    for (int j = 0; j < kPiece; ++j) a = max(a, __float_as_uint(v.get(j)) & 0x7FFFFFFFu);
+    a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+    a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
     const uint32_t e = act8_exp_byte(a);
-    const int64_t g = row * c.groups + group;
-    c.values[g * SS_ACT8_GROUP + lane] = static_cast<uint8_t>(act8_code(x, act8_inverse(e)));
-    if (lane == 0) c.exps[g] = static_cast<uint8_t>(e);
+    const float inverse = act8_inverse(e);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < kPiece; ++j) w[j >> 2] |= act8_code(v.get(j), inverse) << (8 * (j & 3));
+    if (!in) return;
+    *reinterpret_cast<uint2*>(c.values + i * kPiece) = make_uint2(w[0], w[1]);
+    if ((i & 3) == 0) c.exps[i >> 2] = static_cast<uint8_t>(e);
 }
 
-__device__ __forceinline__ float kept_lane(const Ckpt& c, int64_t g, int lane) {
-    return act8_value(c.values[g * SS_ACT8_GROUP + lane], act8_unit(c.exps[g]));
-}
-
-// ---- one warp per group, one lane per column: any stride, any alignment -----------------------------
-template <typename T>
-__global__ void __launch_bounds__(256) act8_pack_kernel(const T* x, int64_t stride, int64_t rows, int64_t cols, Ckpt c) {
-    const int lane = threadIdx.x & 31;
-    const int64_t total = rows * c.groups, step = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 5;
-    for (int64_t g = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5; g < total; g += step) {
-        const int64_t row = g / c.groups, group = g - row * c.groups, col = group * SS_ACT8_GROUP + lane;
-        const float v = col < cols ? Elem<T>::load(x + row * stride + col) : 0.0f;
-        keep_lane(c, row, group, lane, v);
+struct Kept {
+    uint2 w;
+    uint32_t e;
+    __device__ __forceinline__ void load(const Ckpt& c, int64_t i) {
+        w = *reinterpret_cast<const uint2*>(c.values + i * kPiece);
+        e = c.exps[i >> 2];
     }
+    __device__ __forceinline__ float get(int j, float unit) const { return act8_value((j < 4 ? w.x : w.y) >> (8 * (j & 3)), unit); }
+};
+
+// Where a thread's piece lies.
+struct At {
+    int64_t i, row, col;
+    int n;  // columns that exist; 0 beyond the last piece
+    bool in, joined;
+
+    __device__ __forceinline__ At(const Pieces& p, int u) {
+        i = (static_cast<int64_t>(blockIdx.x) * 2 + u) * kBlock + threadIdx.x;
+        in = i < p.total;
+        const int64_t g = (in ? i : 0) >> 2;
+        row = p.row_of(g);
+        const int64_t piece = (i & 3) + (g - row * p.groups) * 4;
+        col = piece * kPiece;
+        const int64_t left = p.cols - col;
+        n = !in || left <= 0 ? 0 : (left >= kPiece ? kPiece : static_cast<int>(left));
+        joined = in && piece > 0 && (threadIdx.x & 31) != 0;
+    }
+    template <typename T>
+    __device__ __forceinline__ T* of(const Side& m) const {
+        return static_cast<T*>(m.p) + row * m.stride + col;
+    }
+};
+
+// A block takes 2 * 256 pieces, both loads of a thread under way before the first is used.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kBlock) act8_pack_kernel(const __grid_constant__ Pieces p, const __grid_constant__ Side x, const __grid_constant__ Ckpt c) {
+    const At at[2] = {At(p, 0), At(p, 1)};
+    Eight<T> v[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) v[u].template load<ALIGNED>(x, at[u].of<T>(x), at[u].n);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) keep(c, at[u].i, at[u].in, v[u]);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) act8_unpack_kernel(Ckpt c, int64_t rows, int64_t cols, T* out, int64_t stride) {
-    const int lane = threadIdx.x & 31;
-    const int64_t total = rows * c.groups, step = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 5;
-    for (int64_t g = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5; g < total; g += step) {
-        const int64_t row = g / c.groups, col = (g - row * c.groups) * SS_ACT8_GROUP + lane;
-        if (col < cols) Elem<T>::store(out + row * stride + col, kept_lane(c, g, lane));
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kBlock) act8_unpack_kernel(const __grid_constant__ Pieces p, const __grid_constant__ Ckpt c, const __grid_constant__ Side out) {
+    const At at[2] = {At(p, 0), At(p, 1)};
+    Kept k[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+        if (at[u].in) k[u].load(c, at[u].i);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const float unit = act8_unit(k[u].e);
+        float f[kPiece];
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) f[j] = k[u].get(j, unit);
+        Eight<T> v;
+        v.set(f);
+        v.template store<ALIGNED>(at[u].of<T>(out), at[u].n, at[u].joined);
     }
 }
 
 struct Forward {
-    const void *x, *up;
-    void* y;
-    int64_t x_stride, up_stride, y_stride, rows, cols;
+    Pieces p;
+    Side x, up, y;
     Ckpt cx, cu, cy;
 };
 
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) act8_forward_kernel(const __grid_constant__ Forward a) {
-    const int lane = threadIdx.x & 31;
-    const int64_t total = a.rows * a.cx.groups, step = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 5;
-    const T* x = static_cast<const T*>(a.x);
-    const T* up = static_cast<const T*>(a.up);
-    T* y = static_cast<T*>(a.y);
-    for (int64_t g = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5; g < total; g += step) {
-        const int64_t row = g / a.cx.groups, group = g - row * a.cx.groups, col = group * SS_ACT8_GROUP + lane;
-        const bool in = col < a.cols;
-        const float v = in ? Elem<T>::load(x + row * a.x_stride + col) : 0.0f;
-        float f = act_value<ACT>(v);
-        keep_lane(a.cx, row, group, lane, v);
-        if (up != nullptr) {
-            const float u = in ? Elem<T>::load(up + row * a.up_stride + col) : 0.0f;
-            f *= u;
-            keep_lane(a.cu, row, group, lane, u);
+template <typename T, int ACT, bool GATED, bool ALIGNED>
+__global__ void __launch_bounds__(kBlock) act8_forward_kernel(const __grid_constant__ Forward a) {
+    const At at[2] = {At(a.p, 0), At(a.p, 1)};
+    Eight<T> x[2], up[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        x[u].template load<ALIGNED>(a.x, at[u].of<T>(a.x), at[u].n);
+        if constexpr (GATED) up[u].template load<ALIGNED>(a.up, at[u].of<T>(a.up), at[u].n);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        float f[kPiece];
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) {
+            f[j] = act_value<ACT>(x[u].get(j));
+            if constexpr (GATED) f[j] *= up[u].get(j);
         }
-        if (a.cy.values != nullptr) {
-            T stored;  // the checkpoint is of what the next layer reads
-            Elem<T>::store(&stored, f);
-            keep_lane(a.cy, row, group, lane, in ? Elem<T>::load(&stored) : 0.0f);
-        }
-        if (in) Elem<T>::store(y + row * a.y_stride + col, f);
+        Eight<T> y;  // columns that do not exist: f(0) = 0
+        y.set(f);
+        keep(a.cx, at[u].i, at[u].in, x[u]);
+        if constexpr (GATED) keep(a.cu, at[u].i, at[u].in, up[u]);
+        if (a.cy.values != nullptr) keep(a.cy, at[u].i, at[u].in, y);  // of what the next layer reads
+        y.template store<ALIGNED>(at[u].of<T>(a.y), at[u].n, at[u].joined);
     }
 }
 
 struct Backward {
-    const void* dy;
-    void *dx, *dup;
-    int64_t dy_stride, dx_stride, dup_stride, rows, cols;
+    Pieces p;
+    Side dy, dx, dup;
     Ckpt cx, cu;
 };
 
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) act8_backward_kernel(const __grid_constant__ Backward a) {
-    const int lane = threadIdx.x & 31;
-    const int64_t total = a.rows * a.cx.groups, step = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 5;
-    for (int64_t g = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5; g < total; g += step) {
-        const int64_t row = g / a.cx.groups, col = (g - row * a.cx.groups) * SS_ACT8_GROUP + lane;
-        if (col >= a.cols) continue;
-        const float dy = Elem<T>::load(static_cast<const T*>(a.dy) + row * a.dy_stride + col);
-        float f, slope;
-        act_value_slope<ACT>(kept_lane(a.cx, g, lane), &f, &slope);
-        float dx = dy * slope;
-        if (a.dup != nullptr) {
-            dx = dy * kept_lane(a.cu, g, lane) * slope;
-            Elem<T>::store(static_cast<T*>(a.dup) + row * a.dup_stride + col, dy * f);
+template <typename T, int ACT, bool GATED, bool ALIGNED>
+__global__ void __launch_bounds__(kBlock) act8_backward_kernel(const __grid_constant__ Backward a) {
+    const At at[2] = {At(a.p, 0), At(a.p, 1)};
+    Eight<T> dy[2];
+    Kept kx[2], ku[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        dy[u].template load<ALIGNED>(a.dy, at[u].of<T>(a.dy), at[u].n);
+        if (at[u].in) {
+            kx[u].load(a.cx, at[u].i);
+            if constexpr (GATED) ku[u].load(a.cu, at[u].i);
         }
-        Elem<T>::store(static_cast<T*>(a.dx) + row * a.dx_stride + col, dx);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const float unit = act8_unit(kx[u].e), unit_up = GATED ? act8_unit(ku[u].e) : 0.0f;
+        float dx[kPiece], dup[kPiece];
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) {
+            float f, slope;
+            act_value_slope<ACT>(kx[u].get(j, unit), &f, &slope);
+            const float d = dy[u].get(j);
+            if constexpr (GATED) {
+                dx[j] = d * ku[u].get(j, unit_up) * slope;
+                dup[j] = d * f;
+            } else {
+                dx[j] = d * slope;
+            }
+        }
+        Eight<T> v;
+        v.set(dx);
+        v.template store<ALIGNED>(at[u].of<T>(a.dx), at[u].n, at[u].joined);
+        if constexpr (GATED) {
+            v.set(dup);
+            v.template store<ALIGNED>(at[u].of<T>(a.dup), at[u].n, at[u].joined);
+        }
     }
 }
 
-// Grid of a kernel that strides over `warps` items, one to a warp of a 256-thread block.
-cudaError_t warp_grid(int64_t warps, int* grid) {
-    cudaError_t err = cudaSuccess;
-    const int64_t sms = device_sm_count(&err);
-    int64_t blocks = (warps + 7) / 8;
-    if (blocks > sms * 8) blocks = sms * 8;
-    *grid = static_cast<int>(blocks < 1 ? 1 : blocks);
-    return err;
+inline unsigned piece_grid(const Pieces& p) { return static_cast<unsigned>((p.total + 2 * kBlock - 1) / (2 * kBlock)); }
+
+inline Side side_of(const Mat& m) { return Side{const_cast<void*>(m.p), m.stride, static_cast<int64_t>(m.extent())}; }
+
+// The kernel variant of a call: element type, aligned rows, activation, gate.
+template <typename F>
+void pick(ss_dtype dt, bool aligned, F&& launch) {
+    if (dt == SS_F32) {
+        if (aligned) launch(float{}, std::true_type{}); else launch(float{}, std::false_type{});
+    } else {
+        if (aligned) launch(uint16_t{}, std::true_type{}); else launch(uint16_t{}, std::false_type{});
+    }
+}
+
+template <typename F>
+void pick(ss_dtype dt, bool aligned, ss_act act, bool gated, F&& launch) {
+    pick(dt, aligned, [&](auto t, auto al) {
+        if (act == SS_ACT_GELU) {
+            const std::integral_constant<int, SS_ACT_GELU> f;
+            if (gated) launch(t, al, f, std::true_type{}); else launch(t, al, f, std::false_type{});
+        } else {
+            const std::integral_constant<int, SS_ACT_SILU> f;
+            if (gated) launch(t, al, f, std::true_type{}); else launch(t, al, f, std::false_type{});
+        }
+    });
 }
 
 // A checkpoint argument: present, aligned.
@@ -170,12 +423,10 @@ int ss_act8_pack(const void* x, int64_t x_stride, ss_dtype dt, int64_t rows, int
     SS_TRY(ckpt_check(ckpt));
     if (mat_overlaps(mx, ckpt, ss_act8_bytes(rows, cols))) return SS_ERR_INVALID_ARG;
     const Ckpt c = ckpt_of(ckpt, rows, cols);
-    int grid = 1;
-    const cudaError_t e = warp_grid(rows * c.groups, &grid);
-    if (e != cudaSuccess) return cuda_status_public(e);
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SS_F32) act8_pack_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(x), mx.stride, rows, cols, c);
-    else act8_pack_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(x), mx.stride, rows, cols, c);
+    const Pieces p = pieces_of(rows, cols);
+    pick(dt, mx.row_aligned(16), [&](auto t, auto al) {
+        act8_pack_kernel<decltype(t), al.value><<<piece_grid(p), kBlock, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, side_of(mx), c);
+    });
     return cuda_status_public(cudaGetLastError());
 }
 
@@ -188,12 +439,10 @@ int ss_act8_unpack(const uint8_t* ckpt, int64_t rows, int64_t cols, void* out, i
     SS_TRY(ckpt_check(ckpt));
     if (mat_overlaps(mo, ckpt, ss_act8_bytes(rows, cols))) return SS_ERR_INVALID_ARG;
     const Ckpt c = ckpt_of(const_cast<uint8_t*>(ckpt), rows, cols);
-    int grid = 1;
-    const cudaError_t e = warp_grid(rows * c.groups, &grid);
-    if (e != cudaSuccess) return cuda_status_public(e);
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SS_F32) act8_unpack_kernel<float><<<grid, 256, 0, st>>>(c, rows, cols, static_cast<float*>(out), mo.stride);
-    else act8_unpack_kernel<uint16_t><<<grid, 256, 0, st>>>(c, rows, cols, static_cast<uint16_t*>(out), mo.stride);
+    const Pieces p = pieces_of(rows, cols);
+    pick(dt, mo.row_aligned(16), [&](auto t, auto al) {
+        act8_unpack_kernel<decltype(t), al.value><<<piece_grid(p), kBlock, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, c, side_of(mo));
+    });
     return cuda_status_public(cudaGetLastError());
 }
 
@@ -223,19 +472,13 @@ int ss_act8_forward(const void* x, int64_t x_stride, const void* up, int64_t up_
         for (int j = 0; j < i; ++j)
             if (cks[j] != nullptr && bytes_overlap(cks[i], kept, cks[j], kept)) return SS_ERR_INVALID_ARG;
     }
-    const Forward a{x, up, y, mx.stride, mu.stride, my.stride, rows, cols, ckpt_of(ckpt_x, rows, cols),
+    const Forward a{pieces_of(rows, cols), side_of(mx), side_of(mu), side_of(my), ckpt_of(ckpt_x, rows, cols),
                     ckpt_of(ckpt_up, rows, cols), ckpt_of(ckpt_y, rows, cols)};
-    int grid = 1;
-    const cudaError_t e = warp_grid(rows * a.cx.groups, &grid);
-    if (e != cudaSuccess) return cuda_status_public(e);
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SS_F32) {
-        if (act == SS_ACT_GELU) act8_forward_kernel<float, SS_ACT_GELU><<<grid, 256, 0, st>>>(a);
-        else act8_forward_kernel<float, SS_ACT_SILU><<<grid, 256, 0, st>>>(a);
-    } else {
-        if (act == SS_ACT_GELU) act8_forward_kernel<uint16_t, SS_ACT_GELU><<<grid, 256, 0, st>>>(a);
-        else act8_forward_kernel<uint16_t, SS_ACT_SILU><<<grid, 256, 0, st>>>(a);
-    }
+    const bool aligned = mx.row_aligned(16) && my.row_aligned(16) && (up == nullptr || mu.row_aligned(16));
+    pick(dt, aligned, act, up != nullptr, [&](auto t, auto al, auto f, auto gated) {
+        act8_forward_kernel<decltype(t), f.value, gated.value, al.value>
+            <<<piece_grid(a.p), kBlock, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
+    });
     return cuda_status_public(cudaGetLastError());
 }
 
@@ -261,19 +504,13 @@ int ss_act8_backward(const void* dy, int64_t dy_stride, const uint8_t* ckpt_x, c
         if (c == nullptr) continue;
         if (mat_overlaps(mx, c, kept) || (dup != nullptr && mat_overlaps(mu, c, kept))) return SS_ERR_INVALID_ARG;
     }
-    const Backward a{dy, dx, dup, my.stride, mx.stride, mu.stride, rows, cols,
+    const Backward a{pieces_of(rows, cols), side_of(my), side_of(mx), side_of(mu),
                      ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, cols), ckpt_of(const_cast<uint8_t*>(ckpt_up), rows, cols)};
-    int grid = 1;
-    const cudaError_t e = warp_grid(rows * a.cx.groups, &grid);
-    if (e != cudaSuccess) return cuda_status_public(e);
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == SS_F32) {
-        if (act == SS_ACT_GELU) act8_backward_kernel<float, SS_ACT_GELU><<<grid, 256, 0, st>>>(a);
-        else act8_backward_kernel<float, SS_ACT_SILU><<<grid, 256, 0, st>>>(a);
-    } else {
-        if (act == SS_ACT_GELU) act8_backward_kernel<uint16_t, SS_ACT_GELU><<<grid, 256, 0, st>>>(a);
-        else act8_backward_kernel<uint16_t, SS_ACT_SILU><<<grid, 256, 0, st>>>(a);
-    }
+    const bool aligned = my.row_aligned(16) && mx.row_aligned(16) && (dup == nullptr || mu.row_aligned(16));
+    pick(dt, aligned, act, dup != nullptr, [&](auto t, auto al, auto f, auto gated) {
+        act8_backward_kernel<decltype(t), f.value, gated.value, al.value>
+            <<<piece_grid(a.p), kBlock, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
+    });
     return cuda_status_public(cudaGetLastError());
 }
 
