@@ -9,18 +9,46 @@ namespace {
 // f and f' in fp32, with the hardware's exponential and reciprocal (each within two units in the
 // last place; the results are held to 1e-6 of |x|, and stored in 8 or 24 bits).
 //   silu: s = 1 / (1 + exp(-x)), f = x s, f' = s (1 + x (1 - s))
-//   gelu: f = x Phi(x), f' = Phi(x) + x phi(x), Phi(x) = (1 + erf(x / sqrt 2)) / 2
-__device__ __forceinline__ float sigmoid_fast(float x) {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+//   gelu: f = x Phi(x), f' = Phi(x) + x phi(x), phi(x) = exp(-x^2 / 2) / sqrt(2 pi)
+// Phi(-|x|) = exp(-x^2 / 2) P(u), u = 1 / (1 + p |x|), the form of Hastings' approximations of erfc
+// (Approximations for Digital Computers, 1955). p and the coefficients of P, of degree 6 without a
+// constant, were fitted for this kernel to erfcx on [0, 10]: Phi is within 1e-8. It shares the
+// exponential with f' and costs half of erff: with erff the bf16 kernels were bound by
+// instructions (285 us instead of 197 us at 16384 x 8192, gated).
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+__device__ __forceinline__ float reciprocal_fast(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ float sigmoid_fast(float x) { return reciprocal_fast(1.0f + exp2_fast(x * -1.4426950408889634f)); }
+
+__device__ __forceinline__ float normal_cdf(float x, float* exp_half_square) {
+    const float e = exp2_fast(x * x * -0.72134752044448170f), u = reciprocal_fast(fmaf(0.275771645f, fabsf(x), 1.0f));
+    float q = fmaf(-0.113644886f, u, 0.442823028f);
+    q = fmaf(q, u, -0.316866405f);
+    q = fmaf(q, u, 0.324101073f);
+    q = fmaf(q, u, 0.0459687229f);
+    q = fmaf(q, u, 0.11761847f);
+    q *= u * e;
+    *exp_half_square = e;
+    return x < 0.0f ? q : 1.0f - q;
 }
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float x) {
-    if constexpr (ACT == SS_ACT_SILU) return x * sigmoid_fast(x);
-    else return x * (0.5f + 0.5f * erff(x * 0.70710678118654752f));
+    if constexpr (ACT == SS_ACT_SILU) {
+        return x * sigmoid_fast(x);
+    } else {
+        float e;
+        return x * normal_cdf(x, &e);
+    }
 }
 
 template <int ACT>
@@ -28,13 +56,12 @@ __device__ __forceinline__ void act_value_slope(float x, float* f, float* slope)
     if constexpr (ACT == SS_ACT_SILU) {
         const float s = sigmoid_fast(x);
         *f = x * s;
-        *slope = s * (1.0f + x * (1.0f - s));
+        *slope = s * fmaf(x, 1.0f - s, 1.0f);
     } else {
-        const float cdf = 0.5f + 0.5f * erff(x * 0.70710678118654752f);
-        float phi;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(phi) : "f"(x * x * -0.72134752044448170f));
+        float e;
+        const float cdf = normal_cdf(x, &e);
         *f = x * cdf;
-        *slope = cdf + x * 0.39894228040143268f * phi;
+        *slope = fmaf(x * 0.39894228040143268f, e, cdf);
     }
 }
 
@@ -199,21 +226,49 @@ struct Eight {
     }
 };
 
+// Largest magnitude of a piece, as the bits of an fp32.
+__device__ __forceinline__ uint32_t largest(const Eight<float>& v) {
+    uint32_t a = 0;
+#pragma unroll
+    for (int j = 0; j < kPiece; ++j) a = max(a, v.w[j] & 0x7FFFFFFFu);
+    return a;
+}
+
+__device__ __forceinline__ uint32_t largest(const Eight<uint16_t>& v) {
+    uint32_t a = v.w[0] & 0x7FFF7FFFu;
+#pragma unroll
+    for (int j = 1; j < 4; ++j) a = __vmaxu2(a, v.w[j] & 0x7FFF7FFFu);
+    return max(a & 0xFFFF0000u, a << 16);
+}
+
+// Codes of columns 4 h .. 4 h + 3: magnitudes from the low bytes, signs from the top bits.
+__device__ __forceinline__ uint32_t codes(const Eight<float>& v, int h, uint32_t exp_byte) {
+    const float inverse = act8_inverse(exp_byte);
+    const uint32_t* w = v.w + 4 * h;
+    uint32_t m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = act8_magnitude(__uint_as_float(w[j]), inverse);
+    const uint32_t q = __byte_perm(__byte_perm(m[0], m[1], 0x0040), __byte_perm(m[2], m[3], 0x0040), 0x5410);
+    const uint32_t s = __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
+    return (q & 0x7F7F7F7Fu) | (s & 0x80808080u);
+}
+
+__device__ __forceinline__ uint32_t codes(const Eight<uint16_t>& v, int h, uint32_t exp_byte) {
+    const uint32_t inverse = __float_as_uint(act8_inverse(exp_byte)), pair = inverse | (inverse >> 16);
+    const uint32_t* w = v.w + 2 * h;
+    const uint32_t lo = act8_magnitude_pair(w[0] & 0x7FFF7FFFu, pair), hi = act8_magnitude_pair(w[1] & 0x7FFF7FFFu, pair);
+    return (__byte_perm(lo, hi, 0x6420) & 0x7F7F7F7Fu) | (__byte_perm(w[0], w[1], 0x7531) & 0x80808080u);
+}
+
 // A piece to the checkpoint; every lane of the warp calls it.
 template <typename T>
 __device__ __forceinline__ void keep(const Ckpt& c, int64_t i, bool in, const Eight<T>& v) {
-    uint32_t a = 0;
-#pragma unroll
-    for (int j = 0; j < kPiece; ++j) a = max(a, __float_as_uint(v.get(j)) & 0x7FFFFFFFu);
+    uint32_t a = largest(v);
     a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
     a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
     const uint32_t e = act8_exp_byte(a);
-    const float inverse = act8_inverse(e);
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < kPiece; ++j) w[j >> 2] |= act8_code(v.get(j), inverse) << (8 * (j & 3));
     if (!in) return;
-    *reinterpret_cast<uint2*>(c.values + i * kPiece) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint2*>(c.values + i * kPiece) = make_uint2(codes(v, 0, e), codes(v, 1, e));
     if ((i & 3) == 0) c.exps[i >> 2] = static_cast<uint8_t>(e);
 }
 
@@ -224,7 +279,14 @@ struct Kept {
         w = *reinterpret_cast<const uint2*>(c.values + i * kPiece);
         e = c.exps[i >> 2];
     }
-    __device__ __forceinline__ float get(int j, float unit) const { return act8_value((j < 4 ? w.x : w.y) >> (8 * (j & 3)), unit); }
+    // The eight values, exact in bf16.
+    __device__ __forceinline__ Eight<uint16_t> values() const {
+        const uint32_t e2 = act8_exponent_pair(e);
+        Eight<uint16_t> v;
+        v.w[0] = act8_value_pair<0>(w.x, e2), v.w[1] = act8_value_pair<1>(w.x, e2);
+        v.w[2] = act8_value_pair<0>(w.y, e2), v.w[3] = act8_value_pair<1>(w.y, e2);
+        return v;
+    }
 };
 
 // Where a thread's piece lies.
@@ -270,12 +332,14 @@ __global__ void __launch_bounds__(kBlock) act8_unpack_kernel(const __grid_consta
         if (at[u].in) k[u].load(c, at[u].i);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const float unit = act8_unit(k[u].e);
-        float f[kPiece];
-#pragma unroll
-        for (int j = 0; j < kPiece; ++j) f[j] = k[u].get(j, unit);
+        const Eight<uint16_t> kept = k[u].values();
         Eight<T> v;
-        v.set(f);
+        if constexpr (sizeof(T) == 2) {
+            v = kept;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPiece; ++j) v.w[j] = __float_as_uint(kept.get(j));
+        }
         v.template store<ALIGNED>(at[u].of<T>(out), at[u].n, at[u].joined);
     }
 }
@@ -333,15 +397,15 @@ __global__ void __launch_bounds__(kBlock) act8_backward_kernel(const __grid_cons
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const float unit = act8_unit(kx[u].e), unit_up = GATED ? act8_unit(ku[u].e) : 0.0f;
+        const Eight<uint16_t> x = kx[u].values(), up = GATED ? ku[u].values() : Eight<uint16_t>{};
         float dx[kPiece], dup[kPiece];
 #pragma unroll
         for (int j = 0; j < kPiece; ++j) {
             float f, slope;
-            act_value_slope<ACT>(kx[u].get(j, unit), &f, &slope);
+            act_value_slope<ACT>(x.get(j), &f, &slope);
             const float d = dy[u].get(j);
             if constexpr (GATED) {
-                dx[j] = d * ku[u].get(j, unit_up) * slope;
+                dx[j] = d * up.get(j) * slope;
                 dup[j] = d * f;
             } else {
                 dx[j] = d * slope;

@@ -33,22 +33,36 @@ __device__ __forceinline__ float act8_inverse(uint32_t exp_byte) {
     return exp_byte == 255u ? 0.0f : __uint_as_float((254u - exp_byte) << 23);
 }
 
-// Sign and magnitude of x * 2^-e rounded to the nearest integer, ties to even: the product is
-// exact (a power of two), and adding 2^23 rounds it at the unit.
-__device__ __forceinline__ uint32_t act8_code(float x, float inverse) {
-    const float t = __fmaf_rn(fabsf(x), inverse, 8388608.0f);
-    return (__float_as_uint(t) & 0x7Fu) | ((__float_as_uint(x) >> 24) & 0x80u);
+// Magnitude of x * 2^-e rounded to the nearest integer, ties to even, in the low byte (bit 7 is 0):
+// the product is exact (a power of two), and adding 2^23 rounds it at the unit.
+__device__ __forceinline__ uint32_t act8_magnitude(float x, float inverse) {
+    return __float_as_uint(__fmaf_rn(fabsf(x), inverse, 8388608.0f));
 }
 
-// 2^e, or NaN for a marked group.
-__device__ __forceinline__ float act8_unit(uint32_t exp_byte) {
-    return __uint_as_float(exp_byte == 255u ? 0x7FC00000u : exp_byte << 23);
+// The same for two bf16 (|x| given): numbers from 128 to 255 have their unit in the last place of
+// a bf16, so one fused multiply-add rounds both where they belong.
+__device__ __forceinline__ uint32_t act8_magnitude_pair(uint32_t abs_pair, uint32_t inverse_pair) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(abs_pair), "r"(inverse_pair), "r"(0x43004300u));
+    return r;
 }
 
-// Value of a code: exact. `code` may carry other bits above its eight.
-__device__ __forceinline__ float act8_value(uint32_t code, float unit) {
-    const float m = __uint_as_float(0x4B000000u | (code & 0x7Fu)) - 8388608.0f;
-    return (code & 0x80u) ? -(m * unit) : m * unit;
+// The exponent field of 2^(e+7), twice, for act8_value_pair; all ones for a marked group.
+__device__ __forceinline__ uint32_t act8_exponent_pair(uint32_t exp_byte) {
+    const uint32_t e = exp_byte == 255u ? 255u : exp_byte + 7u;
+    return (e << 7) | (e << 23);
+}
+
+// Codes 2 PAIR and 2 PAIR + 1 of a word's four as two bf16, exactly. With E the exponent field of
+// 2^(e+7), E | magnitude is 2^e (128 + magnitude) and E alone 2^e 128, both with the code's sign;
+// their difference is exact. A marked group has the E of an infinity: inf - inf and NaN - inf are NaN.
+template <int PAIR>
+__device__ __forceinline__ uint32_t act8_value_pair(uint32_t codes, uint32_t exponent_pair) {
+    const uint32_t r = __byte_perm(codes, 0, PAIR == 0 ? 0x1100 : 0x3322);
+    const uint32_t a = (r & 0x807F807Fu) | exponent_pair, b = (r & 0x80008000u) | exponent_pair;
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
 }
 
 }  // namespace ss

@@ -72,23 +72,6 @@ struct Shared {
     int abort;
 };
 
-// Two codes of a word (its bytes 2 i, 2 i + 1) as two bf16. With E the exponent field of 2^(e+7),
-// E | magnitude is 2^e (128 + magnitude) and E alone 2^e 128, both with the code's sign; their
-// difference is exact. A marked group has E of an infinity: inf - inf and NaN - inf are NaN.
-template <int PAIR>
-__device__ __forceinline__ uint32_t decode_pair(uint32_t w, uint32_t e2) {
-    const uint32_t r = __byte_perm(w, 0, PAIR == 0 ? 0x1100 : 0x3322);
-    const uint32_t a = (r & 0x807F807Fu) | e2, b = (r & 0x80008000u) | e2;
-    uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
-__device__ __forceinline__ uint32_t exponent_pair(uint32_t exp_byte) {
-    const uint32_t e = exp_byte == 255u ? 255u : exp_byte + 7u;
-    return (e << 7) | (e << 23);
-}
-
 // The worker's share of a stage of codes: 16 columns of two rows, 32 rows apart.
 struct Codes {
     uint4 q[2];
@@ -135,11 +118,11 @@ __device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const Cod
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int t = t0 + 32 * i;
-        const uint32_t e2 = exponent_pair(c.e[i]);
+        const uint32_t e2 = act8_exponent_pair(c.e[i]);
         const uint32_t w[4] = {c.q[i].x, c.q[i].y, c.q[i].z, c.q[i].w};
         uint32_t d[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) d[2 * j] = decode_pair<0>(w[j], e2), d[2 * j + 1] = decode_pair<1>(w[j], e2);
+        for (int j = 0; j < 4; ++j) d[2 * j] = act8_value_pair<0>(w[j], e2), d[2 * j + 1] = act8_value_pair<1>(w[j], e2);
         const uint32_t row = panel + t * 128;
         const uint32_t first = row + (((chunk + swap) ^ (t & 7)) << 4), second = row + (((chunk + 1 - swap) ^ (t & 7)) << 4);
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(first), "r"(swap ? d[4] : d[0]), "r"(swap ? d[5] : d[1]),
