@@ -1,13 +1,21 @@
 // Losses over a language model's logits, with their gradient: the clipped policy loss and the
 // paired preference loss.
 #include <cmath>
+#include <type_traits>
 
+#include "tcgen05.cuh"
 #include "train.cuh"
 
 namespace ss {
+
+template <>
+struct Elem<uint32_t> {  // fp32 by its bits
+    static __device__ __forceinline__ float load(const uint32_t* p) { return __uint_as_float(*p); }
+    static __device__ __forceinline__ void store(uint32_t* p, float v) { *p = __float_as_uint(v); }
+};
+
 namespace {
 
-constexpr int kRowThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Softmax statistics: s = sum of 2^(k (z - m)) over what was seen, m the largest z, k = c log2 e. The
@@ -29,13 +37,19 @@ __device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float k) {
     return Stat{m, a.s * fa + b.s * fb};
 }
 
-__device__ __forceinline__ Stat block_join(Stat v, Stat* shared, float k) {
+// Joined over the THREADS threads that share a row, in a fixed order; every one of them gets the result.
+template <int THREADS>
+__device__ __forceinline__ Stat row_join(Stat v, Stat* shared, float k) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = join(v, Stat{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)}, k);
-    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = shared[0];
-    for (int w = 1; w < kRowThreads / 32; ++w) v = join(v, shared[w], k);
+    if constexpr (THREADS > 32) {
+        if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+        __syncthreads();
+        const int lane = threadIdx.x & 31;
+        v = lane < THREADS / 32 ? shared[lane] : Stat{-INFINITY, 0.0f};
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v = join(v, Stat{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)}, k);
+    }
     return v;
 }
 
@@ -56,33 +70,192 @@ __device__ __forceinline__ bool row_live(const Logits& a, int64_t row, int64_t* 
     return *w != 0.0f && *target >= 0 && *target < a.vocab;
 }
 
+// ---- a row as vectors of 16 bytes -------------------------------------------------------------------
+// The vectors are those of memory, so a row that starts off their grid has a first (and a last)
+// one with elements that are not its own: those are never touched, and read as -inf.
 template <typename T>
-__device__ __forceinline__ Stat row_stat(const T* z, int64_t vocab, float k) {
-    Stat v{-INFINITY, 0.0f};
-    for (int64_t i = threadIdx.x; i < vocab; i += kRowThreads) {
-        const float x = Elem<T>::load(z + i);
-        if (x > v.m) {
-            v.s *= exp2_fast((v.m - x) * k);
-            v.m = x;
+struct Row {
+    static constexpr int kPer = 16 / sizeof(T);
+    uintptr_t base;  // of vector 0
+    int head;        // elements of vector 0 before the row
+    int64_t end;     // head + vocab
+    int64_t vectors;
+
+    __device__ __forceinline__ Row(const void* p, int64_t vocab) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        base = at & ~static_cast<uintptr_t>(15);
+        head = static_cast<int>((at & 15) / sizeof(T));
+        end = head + vocab;
+        vectors = (end + kPer - 1) / kPer;
+    }
+    __device__ __forceinline__ bool whole(int64_t j) const { return (j > 0 || head == 0) && (j + 1) * kPer <= end; }
+    __device__ __forceinline__ bool own(int64_t i) const { return i >= head && i < end; }  // element i of the vectors
+    __device__ __forceinline__ T* element(int64_t i) const { return reinterpret_cast<T*>(base) + i; }
+    __device__ __forceinline__ uint4* vector(int64_t j) const { return reinterpret_cast<uint4*>(base) + j; }
+};
+
+template <typename T>
+struct Vec {
+    static constexpr int kPer = Row<T>::kPer;
+    uint4 v;
+
+    __device__ __forceinline__ const uint32_t* words() const { return &v.x; }
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t* w = &v.x;
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+    }
+    __device__ __forceinline__ void load(const Row<T>& r, int64_t j) {
+        if (r.whole(j)) {
+            v = *r.vector(j);
+            return;
         }
-        v.s += x == -INFINITY ? 0.0f : exp2_fast((x - v.m) * k);
+        uint32_t w[4];
+        constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = none;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (!r.own(j * kPer + i)) continue;
+            const uint32_t x = *r.element(j * kPer + i);
+            if constexpr (sizeof(T) == 4) w[i] = x;
+            else w[i >> 1] = (i & 1) ? (w[i >> 1] & 0x0000FFFFu) | (x << 16) : (w[i >> 1] & 0xFFFF0000u) | x;
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void store(const Row<T>& r, int64_t j) const {
+        if (r.whole(j)) {
+            __stcs(r.vector(j), v);
+            return;
+        }
+        const uint32_t* w = &v.x;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (!r.own(j * kPer + i)) continue;
+            if constexpr (sizeof(T) == 4) *r.element(j * kPer + i) = w[i];
+            else *r.element(j * kPer + i) = static_cast<T>(w[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+};
+
+// Two fp32 operations at once.
+__device__ __forceinline__ float2 sub_mul2(float a, float b, float minus, float k) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, m, k;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 m, {%4, %4};\n\tmov.b64 k, {%5, %5};\n\t"
+        "add.rn.f32x2 x, x, m;\n\tmul.rn.f32x2 x, x, k;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a), "f"(b), "f"(minus), "f"(k));
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void add_vector(Stat& v, const Vec<T>& x, float k) {
+    constexpr int n = Vec<T>::kPer;
+    float top = x.get(0);
+#pragma unroll
+    for (int i = 1; i < n; ++i) top = fmaxf(top, x.get(i));
+    if (top > v.m) {
+        v.s *= exp2_fast((v.m - top) * k);  // 0 where nothing was seen: m is -inf
+        v.m = top;
+    }
+    const float minus = v.m == -INFINITY ? 0.0f : -v.m;  // nothing but -inf so far: their terms are 0
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < n; i += 2) {
+        const float2 t = sub_mul2(x.get(i), x.get(i + 1), minus, k);
+        sum[0] += exp2_fast(t.x), sum[1] += exp2_fast(t.y);
+    }
+    v.s += sum[0] + sum[1];
+}
+
+// coef ([v = y] - softmax_v) for the elements of vector j, `f` = -coef / s; target counted in the vectors' elements.
+template <typename T>
+__device__ __forceinline__ Vec<T> grad_vector(const Vec<T>& x, int64_t j, int64_t target, float m, float k, float f, float coef) {
+    constexpr int n = Vec<T>::kPer;
+    float g[n];
+#pragma unroll
+    for (int i = 0; i < n; i += 2) {
+        const float2 t = sub_mul2(x.get(i), x.get(i + 1), -m, k);
+        g[i] = f * exp2_fast(t.x), g[i + 1] = f * exp2_fast(t.y);
+    }
+    if (target / n == j) {
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            if (target % n == i) g[i] += coef;
+    }
+    Vec<T> r;
+    uint32_t* w = &r.v.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(g[i]);
+        else w[i] = bf16_pair(g[2 * i], g[2 * i + 1]);
+    }
+    return r;
+}
+
+// Stores vector j of z's grid to dz, whose rows may lie differently against 16 bytes.
+template <typename T>
+__device__ __forceinline__ void store_vector(const Vec<T>& v, const Row<T>& z, const Row<T>& dz, int64_t j) {
+    if (z.head == dz.head) {
+        v.store(dz, j);
+        return;
+    }
+    const uint32_t* w = v.words();
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kPer; ++i) {
+        const int64_t at = j * Vec<T>::kPer + i;
+        if (!z.own(at)) continue;
+        T* p = dz.element(at - z.head + dz.head);
+        if constexpr (sizeof(T) == 4) *p = w[i];
+        else *p = static_cast<T>(w[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
+// Vectors first, first + step, ... below last.
+template <typename T>
+__device__ __forceinline__ Stat stat_of(const Row<T>& r, int64_t first, int64_t last, int step, float k) {
+    constexpr int kAhead = 4;  // loads of a thread under way at a time
+    Stat v{-INFINITY, 0.0f};
+    int64_t j = first;
+    for (; j + (kAhead - 1) * step < last; j += kAhead * step) {
+        Vec<T> x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u].load(r, j + u * step);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) add_vector(v, x[u], k);
+    }
+    for (; j < last; j += step) {
+        Vec<T> x;
+        x.load(r, j);
+        add_vector(v, x, k);
     }
     return v;
 }
 
-// dz = coef c ([v = y] - softmax_v)
 template <typename T>
-__device__ __forceinline__ void row_grad(const T* z, T* dz, int64_t vocab, int64_t target, float k, const Stat& v, float coef) {
-    const float f = -coef / v.s;
-    for (int64_t i = threadIdx.x; i < vocab; i += kRowThreads) {
-        const float p = f * exp2_fast((Elem<T>::load(z + i) - v.m) * k);
-        Elem<T>::store(dz + i, i == target ? coef + p : p);
+__device__ __forceinline__ void grad_of(const Row<T>& z, const Row<T>& dz, int64_t first, int64_t last, int step, int64_t target,
+                                        const Stat& s, float k, float coef) {
+    constexpr int kAhead = 4;
+    const float f = -coef / s.s;
+    int64_t j = first;
+    for (; j + (kAhead - 1) * step < last; j += kAhead * step) {
+        Vec<T> x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u].load(z, j + u * step);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) store_vector(grad_vector(x[u], j + u * step, target + z.head, s.m, k, f, coef), z, dz, j + u * step);
+    }
+    for (; j < last; j += step) {
+        Vec<T> x;
+        x.load(z, j);
+        store_vector(grad_vector(x, j, target + z.head, s.m, k, f, coef), z, dz, j);
     }
 }
 
 template <typename T>
-__device__ __forceinline__ void row_zero(T* dz, int64_t vocab) {
-    for (int64_t i = threadIdx.x; i < vocab; i += kRowThreads) dz[i] = T(0);
+__device__ __forceinline__ void zero_of(const Row<T>& dz, int64_t first, int64_t last, int step) {
+    Vec<T> zero;
+    zero.v = make_uint4(0u, 0u, 0u, 0u);
+    for (int64_t j = first; j < last; j += step) zero.store(dz, j);
 }
 
 struct Policy {
@@ -109,50 +282,147 @@ __device__ __forceinline__ PolicyTerm policy_term(const Policy& p, int64_t row, 
                       w * ((clipped ? 0.0f : -gain) + p.beta * dkl)};
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) policy_row_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, int64_t rows) {
-    __shared__ Stat shared[kRowThreads / 32];
-    const int64_t row = blockIdx.x;
-    const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
-    T* dz = a.dz == nullptr ? nullptr : static_cast<T*>(a.dz) + row * a.dz_stride;
+__device__ __forceinline__ void store_term(const Logits& a, const Policy& p, int64_t rows, int64_t row, float logp, const PolicyTerm& t) {
+    a.logp[row] = logp;
+    p.terms[row] = t.loss, p.terms[rows + row] = t.kl, p.terms[2 * rows + row] = t.clipped;
+}
+
+__device__ __forceinline__ float scale_of(const Logits& a) { return a.c * (a.grad_scale == nullptr ? 1.0f : *a.grad_scale); }
+
+// ---- rows read straight from memory, THREADS threads (a warp or a block) to a row. With a
+// gradient the row is read twice, the second time from the caches. ------------------------------------
+template <int THREADS>
+constexpr int block_of() { return THREADS > 256 ? THREADS : 256; }
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(block_of<THREADS>()) policy_stream_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, int64_t rows) {
+    __shared__ Stat shared[THREADS / 32];
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS;
+    const int t = threadIdx.x % THREADS;
+    if (row >= rows) return;  // whole warps, or none of the block
+    const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
+    const Row<T> dz(a.dz == nullptr ? nullptr : static_cast<T*>(a.dz) + row * a.dz_stride, a.vocab);
     int64_t target;
     float w;
     if (!row_live(a, row, &target, &w)) {
-        if (dz != nullptr) row_zero(dz, a.vocab);
-        if (threadIdx.x == 0) {
-            a.logp[row] = 0.0f;
-            for (int i = 0; i < 3; ++i) p.terms[i * rows + row] = 0.0f;
-        }
+        if (a.dz != nullptr) zero_of(dz, t, dz.vectors, THREADS);
+        if (t == 0) store_term(a, p, rows, row, 0.0f, PolicyTerm{0.0f, 0.0f, 0.0f, 0.0f});
         return;
     }
-    const float k = a.c * kLog2e, picked = Elem<T>::load(z + target);
-    const Stat v = block_join(row_stat(z, a.vocab, k), shared, k);
-    const float logp = (picked - v.m) * a.c - logf(v.s);
-    const PolicyTerm t = policy_term(p, row, logp, w);
-    if (dz != nullptr) row_grad(z, dz, a.vocab, target, k, v, t.slope * a.c * (a.grad_scale == nullptr ? 1.0f : *a.grad_scale));
-    if (threadIdx.x == 0) {
-        a.logp[row] = logp;
-        p.terms[row] = t.loss, p.terms[rows + row] = t.kl, p.terms[2 * rows + row] = t.clipped;
+    const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(target + z.head));
+    const Stat s = row_join<THREADS>(stat_of(z, t, z.vectors, THREADS, k), shared, k);
+    const float logp = (picked - s.m) * a.c - logf(s.s);
+    const PolicyTerm term = policy_term(p, row, logp, w);
+    if (t == 0) store_term(a, p, rows, row, logp, term);
+    if (a.dz != nullptr) grad_of(z, dz, t, z.vectors, THREADS, target, s, k, term.slope * scale_of(a));
+}
+
+// ---- rows held in shared memory between the sum and the gradient: one block to a row, or a cluster
+// of up to 8 whose blocks hold a slice each and exchange their statistics. ------------------------------
+constexpr int kSliceThreads = 256;
+constexpr int kParts = 4;  // of a slice, so that summing starts when the first has arrived
+
+template <typename T>
+__global__ void __launch_bounds__(kSliceThreads) policy_slice_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, int64_t rows, int slice) {
+    extern __shared__ __align__(128) uint8_t dynamic[];
+    __shared__ Stat shared[kSliceThreads / 32], joined[8];
+    __shared__ uint64_t arrived[kParts];
+    __shared__ int abort;
+    uint4* const held = reinterpret_cast<uint4*>(dynamic);
+    uint32_t rank, size;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+    const int64_t row = blockIdx.x / size;
+    const int t = threadIdx.x;
+    const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
+    const Row<T> dz(static_cast<T*>(a.dz) + row * a.dz_stride, a.vocab);
+    const int64_t first = static_cast<int64_t>(rank) * slice;
+    int64_t target;
+    float w;
+    if (!row_live(a, row, &target, &w)) {  // for every block of the cluster
+        const int64_t most = dz.vectors > z.vectors ? dz.vectors : z.vectors;
+        zero_of(dz, first + t, min(rank + 1 == size ? most : first + slice, dz.vectors), kSliceThreads);
+        if (rank == 0 && t == 0) store_term(a, p, rows, row, 0.0f, PolicyTerm{0.0f, 0.0f, 0.0f, 0.0f});
+        return;
+    }
+    // every block of the cluster must have begun before another writes to its memory
+    if (size > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    const int n = static_cast<int>(max(min(z.vectors - first, static_cast<int64_t>(slice)), static_cast<int64_t>(0)));
+    const int part = (n + kParts - 1) / kParts;
+    if (t == 0) {
+        for (int i = 0; i < kParts; ++i) mbar_init(smem_addr(&arrived[i]), 1);
+        abort = 0;
+        mbar_init_visible();
+        // whole vectors by bulk copies; the first and the last of the row, if they are not, below
+        const int lo = n > 0 && !z.whole(first) ? 1 : 0, hi = n > 0 && !z.whole(first + n - 1) ? n - 1 : n;
+        for (int i = 0; i < kParts; ++i) {
+            const int from = max(i * part, lo), to = min((i + 1) * part, hi);
+            const uint32_t bytes = to > from ? (to - from) * 16 : 0;
+            mbar_expect(smem_addr(&arrived[i]), bytes);
+            if (bytes > 0) bulk_load(smem_addr(held + from), z.vector(first + from), smem_addr(&arrived[i]), bytes);
+        }
+    }
+    if (t == 32 && n > 0) {
+        Vec<T> x;
+        if (!z.whole(first)) x.load(z, first), held[0] = x.v;
+        if (!z.whole(first + n - 1)) x.load(z, first + n - 1), held[n - 1] = x.v;
+    }
+    const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(target + z.head));
+    __syncthreads();
+    Stat s{-INFINITY, 0.0f};
+    bool ok = true;
+    for (int i = 0; i < kParts; ++i) {
+        ok = mbar_wait(smem_addr(&arrived[i]), 0, &abort) && ok;
+        for (int j = i * part + t; j < min((i + 1) * part, n); j += kSliceThreads) {
+            Vec<T> x;
+            x.v = held[j];
+            add_vector(s, x, k);
+        }
+    }
+    if (!ok) s.s = __uint_as_float(0x7FC00000u);  // a copy that did not arrive shows
+    s = row_join<kSliceThreads>(s, shared, k);
+    if (size > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        if (t < static_cast<int>(size)) {
+            uint32_t at;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(&joined[rank])), "r"(t));
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(s.m), "f"(s.s) : "memory");
+        }
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        s = joined[0];
+        for (uint32_t i = 1; i < size; ++i) s = join(s, joined[i], k);
+    }
+    const float logp = (picked - s.m) * a.c - logf(s.s);
+    const PolicyTerm term = policy_term(p, row, logp, w);
+    if (rank == 0 && t == 0) store_term(a, p, rows, row, logp, term);
+    const float coef = term.slope * scale_of(a), f = -coef / s.s;
+    for (int j = t; j < n; j += kSliceThreads) {
+        Vec<T> x;
+        x.v = held[j];
+        store_vector(grad_vector(x, first + j, target + z.head, s.m, k, f, coef), z, dz, first + j);
     }
 }
 
-// Sum over a block of 256 threads in a fixed order.
+constexpr int kSumThreads = 1024;
+
+// Sum over a block of 1024 threads in a fixed order.
 __device__ __forceinline__ double block_sum(double v, double* shared) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = 0.0;
-    for (int w = 0; w < kRowThreads / 32; ++w) v += shared[w];
+    v = shared[threadIdx.x & 31];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
 
-__global__ void __launch_bounds__(kRowThreads) totals_kernel(const float* terms, int64_t n, double scale, float* out) {
-    __shared__ double shared[kRowThreads / 32];
+__global__ void __launch_bounds__(kSumThreads) totals_kernel(const float* terms, int64_t n, double scale, float* out) {
+    __shared__ double shared[32];
     const float* x = terms + blockIdx.x * n;
     double v = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kRowThreads) v += x[i];
+    for (int64_t i = threadIdx.x; i < n; i += kSumThreads) v += x[i];
     v = block_sum(v, shared);
     if (threadIdx.x == 0) out[blockIdx.x] = static_cast<float>(scale * v);
 }
@@ -163,24 +433,25 @@ struct Rows {
     float* coef;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) row_stat_kernel(const __grid_constant__ Logits a, Rows r) {
-    __shared__ Stat shared[kRowThreads / 32];
-    const int64_t row = blockIdx.x;
-    const T* z = static_cast<const T*>(a.z) + row * a.z_stride;
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(block_of<THREADS>()) row_stat_kernel(const __grid_constant__ Logits a, Rows r, int64_t rows) {
+    __shared__ Stat shared[THREADS / 32];
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS;
+    const int t = threadIdx.x % THREADS;
+    if (row >= rows) return;
     int64_t target;
     float w;
-    const bool live = row_live(a, row, &target, &w);
-    Stat v{0.0f, 1.0f};
+    Stat s{0.0f, 1.0f};
     float logp = 0.0f;
-    if (live) {
-        const float k = a.c * kLog2e, picked = Elem<T>::load(z + target);
-        v = block_join(row_stat(z, a.vocab, k), shared, k);
-        logp = (picked - v.m) * a.c - logf(v.s);
+    if (row_live(a, row, &target, &w)) {
+        const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
+        const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(target + z.head));
+        s = row_join<THREADS>(stat_of(z, t, z.vectors, THREADS, k), shared, k);
+        logp = (picked - s.m) * a.c - logf(s.s);
     }
-    if (threadIdx.x == 0) {
+    if (t == 0) {
         a.logp[row] = logp;
-        r.stat[row] = v;
+        r.stat[row] = s;
         r.coef[row] = 0.0f;  // of rows that belong to no sequence
     }
 }
@@ -194,8 +465,8 @@ struct Preference {
     float *margins, *seq_logp, *pair_loss;
 };
 
-__global__ void __launch_bounds__(kRowThreads) pair_kernel(const __grid_constant__ Logits a, const __grid_constant__ Preference p, Rows r) {
-    __shared__ double shared[kRowThreads / 32];
+__global__ void __launch_bounds__(kSumThreads) pair_kernel(const __grid_constant__ Logits a, const __grid_constant__ Preference p, Rows r) {
+    __shared__ double shared[32];
     const int64_t pair = blockIdx.x;
     int64_t at[3];
     for (int i = 0; i < 3; ++i) {
@@ -205,7 +476,7 @@ __global__ void __launch_bounds__(kRowThreads) pair_kernel(const __grid_constant
     double sum[2];
     for (int i = 0; i < 2; ++i) {
         double v = 0.0;
-        for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kRowThreads) {
+        for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kSumThreads) {
             int64_t target;
             float w;
             if (row_live(a, t, &target, &w)) v += static_cast<double>(w) * a.logp[t];
@@ -235,23 +506,74 @@ __global__ void __launch_bounds__(kRowThreads) pair_kernel(const __grid_constant
     }
     slope *= p.scale * (a.grad_scale == nullptr ? 1.0f : *a.grad_scale);
     for (int i = 0; i < 2; ++i)
-        for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kRowThreads) {
+        for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kSumThreads) {
             int64_t target;
             float w;
             if (row_live(a, t, &target, &w)) r.coef[t] = (i == 0 ? slope : -slope) * w * a.c;
         }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) row_grad_kernel(const __grid_constant__ Logits a, Rows r) {
-    const int64_t row = blockIdx.x;
-    T* dz = static_cast<T*>(a.dz) + row * a.dz_stride;
+// In the order opposite to the statistics', so that it begins with the rows that the caches still hold.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(block_of<THREADS>()) row_grad_kernel(const __grid_constant__ Logits a, Rows r, int64_t rows) {
+    const int64_t row = rows - 1 - (static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS);
+    const int t = threadIdx.x % THREADS;
+    if (row < 0) return;
+    const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
+    const Row<T> dz(static_cast<T*>(a.dz) + row * a.dz_stride, a.vocab);
     const float coef = r.coef[row];
-    if (coef == 0.0f) {
-        row_zero(dz, a.vocab);
-        return;
-    }
-    row_grad(static_cast<const T*>(a.z) + row * a.z_stride, dz, a.vocab, a.targets[row], a.c * kLog2e, r.stat[row], coef);
+    if (coef == 0.0f) zero_of(dz, t, dz.vectors, THREADS);
+    else grad_of(z, dz, t, z.vectors, THREADS, a.targets[row], r.stat[row], a.c * kLog2e, coef);
+}
+
+// ---- choices of a launch ------------------------------------------------------------------------------
+constexpr int64_t kWarpRowBytes = 8192;     // rows up to this size: a warp each
+constexpr int kFewRows = 296;               // fewer rows than two for each SM: a large block each
+constexpr int64_t kSliceBytes = 72 * 1024;  // three such blocks on an SM
+constexpr int64_t kMostSliceBytes = 208 * 1024;
+
+template <typename F>
+void pick_threads(int64_t rows, int64_t vocab, ss_dtype dt, F&& launch) {
+    auto by_type = [&](auto t) {
+        if (vocab * static_cast<int64_t>(sizeof(t)) <= kWarpRowBytes) launch(t, std::integral_constant<int, 32>{});
+        else if (rows < kFewRows) launch(t, std::integral_constant<int, 1024>{});
+        else launch(t, std::integral_constant<int, 256>{});
+    };
+    if (dt == SS_F32) by_type(uint32_t{}); else by_type(uint16_t{});
+}
+
+template <int THREADS>
+unsigned rows_grid(int64_t rows) {
+    constexpr int per = block_of<THREADS>() / THREADS;
+    return static_cast<unsigned>((rows + per - 1) / per);
+}
+
+// Blocks that share a row in policy_slice_kernel, 0 if it does not fit (or is small): the fewest with which
+// three blocks fit on an SM, more where there are not enough rows for all SMs.
+int cluster_of(int64_t rows, int64_t vocab, size_t eb) {
+    const int64_t bytes = vocab * static_cast<int64_t>(eb) + 16;
+    if (bytes <= kWarpRowBytes || bytes > 8 * kMostSliceBytes) return 0;
+    int size = 1;
+    while (size < 8 && (bytes > size * kSliceBytes || (rows * size < 148 && bytes > size * 8192))) size *= 2;
+    return size;
+}
+
+template <typename T>
+cudaError_t launch_slices(const Logits& a, const Policy& p, int64_t rows, int size, cudaStream_t st) {
+    const int64_t vectors = (a.vocab * static_cast<int64_t>(sizeof(T)) + 15 + 15) / 16;  // wherever the row starts
+    const int slice = static_cast<int>((vectors + size - 1) / size);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * size));
+    cfg.blockDim = dim3(kSliceThreads);
+    cfg.dynamicSmemBytes = static_cast<size_t>(slice) * 16;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = size, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaFuncSetAttribute(policy_slice_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(cfg.dynamicSmemBytes));
+    return e != cudaSuccess ? e : cudaLaunchKernelEx(&cfg, policy_slice_kernel<T>, a, p, rows, slice);
 }
 
 // ---- checks shared by the two losses ------------------------------------------------------------------
@@ -328,10 +650,17 @@ int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64
     const Logits a{logits, dlogits, z.stride, dz.stride, vocab, targets, weights, grad_scale, inv_temperature, logp};
     const Policy p{old_logp, ref_logp, advantages, 1.0f - clip_low, 1.0f + clip_high, kl_coef, static_cast<float*>(workspace)};
     if (rows > 0) {
-        if (dt == SS_F32) policy_row_kernel<float><<<static_cast<unsigned>(rows), kRowThreads, 0, st>>>(a, p, rows);
-        else policy_row_kernel<uint16_t><<<static_cast<unsigned>(rows), kRowThreads, 0, st>>>(a, p, rows);
+        const int size = dlogits == nullptr ? 0 : cluster_of(rows, vocab, dtype_bytes(dt));
+        if (size > 0 && rows * size <= kMaxSide) {
+            const cudaError_t e = dt == SS_F32 ? launch_slices<uint32_t>(a, p, rows, size, st) : launch_slices<uint16_t>(a, p, rows, size, st);
+            if (e != cudaSuccess) return cuda_status_public(e);
+        } else {
+            pick_threads(rows, vocab, dt, [&](auto t, auto threads) {
+                policy_stream_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, p, rows);
+            });
+        }
     }
-    totals_kernel<<<3, kRowThreads, 0, st>>>(p.terms, rows, 1.0, totals);
+    totals_kernel<<<3, kSumThreads, 0, st>>>(p.terms, rows, 1.0, totals);
     return cuda_status_public(cudaGetLastError());
 }
 
@@ -365,16 +694,17 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
     const Rows r{static_cast<Stat*>(workspace), static_cast<float*>(workspace) + 2 * rows};
     float* pair_loss = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up(rows * 12, 256));
     const Preference p{seq_begin, ref_seq_logp, n_pairs, rows, kind, beta, label_smoothing, scale, margins, seq_logp, pair_loss};
-    const unsigned grid = static_cast<unsigned>(rows);
     if (rows > 0) {
-        if (dt == SS_F32) row_stat_kernel<float><<<grid, kRowThreads, 0, st>>>(a, r);
-        else row_stat_kernel<uint16_t><<<grid, kRowThreads, 0, st>>>(a, r);
+        pick_threads(rows, vocab, dt, [&](auto t, auto threads) {
+            row_stat_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, r, rows);
+        });
     }
-    if (n_pairs > 0) pair_kernel<<<static_cast<unsigned>(n_pairs), kRowThreads, 0, st>>>(a, p, r);
-    totals_kernel<<<1, kRowThreads, 0, st>>>(pair_loss, n_pairs, scale, loss);
+    if (n_pairs > 0) pair_kernel<<<static_cast<unsigned>(n_pairs), kSumThreads, 0, st>>>(a, p, r);
+    totals_kernel<<<1, kSumThreads, 0, st>>>(pair_loss, n_pairs, scale, loss);
     if (rows > 0 && dlogits != nullptr) {
-        if (dt == SS_F32) row_grad_kernel<float><<<grid, kRowThreads, 0, st>>>(a, r);
-        else row_grad_kernel<uint16_t><<<grid, kRowThreads, 0, st>>>(a, r);
+        pick_threads(rows, vocab, dt, [&](auto t, auto threads) {
+            row_grad_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, r, rows);
+        });
     }
     return cuda_status_public(cudaGetLastError());
 }
