@@ -31,24 +31,33 @@ __device__ __forceinline__ float exp2_fast(float x) {  // 2^x to about 2 units i
 }
 
 // A maximum of -inf means that nothing but -inf was seen: its sum is 0, and 2^(-inf - -inf) must not be formed.
-__device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float k) {
-    const float m = fmaxf(a.m, b.m);
-    const float fa = a.m == -INFINITY ? 0.0f : exp2_fast((a.m - m) * k), fb = b.m == -INFINITY ? 0.0f : exp2_fast((b.m - m) * k);
-    return Stat{m, a.s * fa + b.s * fb};
+__device__ __forceinline__ float warp_max(float x) {  // NaNs are passed over
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
 }
 
-// Joined over the THREADS threads that share a row, in a fixed order; every one of them gets the result.
+// Joined over a warp's first N lanes (a power of two; the others hold nothing), in a fixed order;
+// every lane gets the result. One maximum, one rescaling, then plain sums.
+template <int N>
+__device__ __forceinline__ Stat warp_join(Stat v, float k) {
+    const float m = warp_max(v.m);
+    float s = v.s * (v.m == -INFINITY ? 0.0f : exp2_fast((v.m - m) * k));  // a NaN stays one
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if constexpr (N < 32) s = __shfl_sync(0xFFFFFFFFu, s, 0);
+    return Stat{m, s};
+}
+
+// Joined over the THREADS threads that share a row; every one of them gets the result.
 template <int THREADS>
 __device__ __forceinline__ Stat row_join(Stat v, Stat* shared, float k) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = join(v, Stat{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)}, k);
+    v = warp_join<32>(v, k);
     if constexpr (THREADS > 32) {
         if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
         __syncthreads();
         const int lane = threadIdx.x & 31;
-        v = lane < THREADS / 32 ? shared[lane] : Stat{-INFINITY, 0.0f};
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v = join(v, Stat{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)}, k);
+        v = warp_join<THREADS / 32>(lane < THREADS / 32 ? shared[lane] : Stat{-INFINITY, 0.0f}, k);
     }
     return v;
 }
@@ -72,26 +81,30 @@ __device__ __forceinline__ bool row_live(const Logits& a, int64_t row, int64_t* 
 
 // ---- a row as vectors of 16 bytes -------------------------------------------------------------------
 // The vectors are those of memory, so a row that starts off their grid has a first (and a last)
-// one with elements that are not its own: those are never touched, and read as -inf.
+// one with elements that are not its own: those are never touched, and read as -inf. Whole vectors
+// are lo .. hi - 1; the loops run over them alone, and one thread each takes the partial ones.
 template <typename T>
 struct Row {
     static constexpr int kPer = 16 / sizeof(T);
-    uintptr_t base;  // of vector 0
-    int head;        // elements of vector 0 before the row
-    int64_t end;     // head + vocab
-    int64_t vectors;
+    uintptr_t base;           // of vector 0
+    uint32_t head, end;       // the row's elements, counted from there
+    uint32_t lo, hi;
+    bool first, last;         // partial vectors 0 and hi
 
     __device__ __forceinline__ Row(const void* p, int64_t vocab) {
         const uintptr_t at = reinterpret_cast<uintptr_t>(p);
         base = at & ~static_cast<uintptr_t>(15);
-        head = static_cast<int>((at & 15) / sizeof(T));
-        end = head + vocab;
-        vectors = (end + kPer - 1) / kPer;
+        head = static_cast<uint32_t>(at & 15) / sizeof(T);
+        end = head + static_cast<uint32_t>(vocab);
+        lo = head > 0 ? 1 : 0;
+        hi = max(end / kPer, lo);
+        first = head > 0 && vocab > 0;
+        last = end > hi * kPer;
     }
-    __device__ __forceinline__ bool whole(int64_t j) const { return (j > 0 || head == 0) && (j + 1) * kPer <= end; }
-    __device__ __forceinline__ bool own(int64_t i) const { return i >= head && i < end; }  // element i of the vectors
-    __device__ __forceinline__ T* element(int64_t i) const { return reinterpret_cast<T*>(base) + i; }
-    __device__ __forceinline__ uint4* vector(int64_t j) const { return reinterpret_cast<uint4*>(base) + j; }
+    __device__ __forceinline__ uint32_t vectors() const { return hi + (last ? 1 : 0); }
+    __device__ __forceinline__ T* element(uint32_t i) const { return reinterpret_cast<T*>(base) + i; }
+    __device__ __forceinline__ uint4* vector(uint32_t j) const { return reinterpret_cast<uint4*>(base) + j; }
+    __device__ __forceinline__ bool own(uint32_t i) const { return i >= head && i < end; }
 };
 
 template <typename T>
@@ -99,21 +112,24 @@ struct Vec {
     static constexpr int kPer = Row<T>::kPer;
     uint4 v;
 
-    __device__ __forceinline__ const uint32_t* words() const { return &v.x; }
+    __device__ __forceinline__ uint32_t word(int i) const { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
     __device__ __forceinline__ float get(int i) const {
-        const uint32_t* w = &v.x;
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-        else return __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+        if constexpr (sizeof(T) == 4) return __uint_as_float(word(i));
+        else return __uint_as_float((i & 1) ? word(i >> 1) & 0xFFFF0000u : word(i >> 1) << 16);
     }
-    __device__ __forceinline__ void load(const Row<T>& r, int64_t j) {
-        if (r.whole(j)) {
-            v = *r.vector(j);
-            return;
-        }
+    __device__ __forceinline__ void set(const float (&g)[kPer]) {
+        if constexpr (sizeof(T) == 4) v = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+        else v = make_uint4(bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3]), bf16_pair(g[4 % kPer], g[5 % kPer]), bf16_pair(g[6 % kPer], g[7 % kPer]));
+    }
+    __device__ __forceinline__ void none() {  // nothing but -inf
+        constexpr uint32_t w = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+        v = make_uint4(w, w, w, w);
+    }
+    __device__ __forceinline__ void load_partial(const Row<T>& r, uint32_t j) {
         uint32_t w[4];
-        constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf
+        none();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = none;
+        for (int i = 0; i < 4; ++i) w[i] = v.x;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (!r.own(j * kPer + i)) continue;
@@ -123,17 +139,14 @@ struct Vec {
         }
         v = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ __forceinline__ void store(const Row<T>& r, int64_t j) const {
-        if (r.whole(j)) {
-            __stcs(r.vector(j), v);
-            return;
-        }
-        const uint32_t* w = &v.x;
+    // The elements that vector j of z's grid has of the row, to the same elements of dz.
+    __device__ __forceinline__ void store_partial(const Row<T>& z, const Row<T>& dz, uint32_t j) const {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            if (!r.own(j * kPer + i)) continue;
-            if constexpr (sizeof(T) == 4) *r.element(j * kPer + i) = w[i];
-            else *r.element(j * kPer + i) = static_cast<T>(w[i >> 1] >> (16 * (i & 1)));
+            if (!z.own(j * kPer + i)) continue;
+            T* p = dz.element(j * kPer + i - z.head + dz.head);
+            if constexpr (sizeof(T) == 4) *p = word(i);
+            else *p = static_cast<T>(word(i >> 1) >> (16 * (i & 1)));
         }
     }
 };
@@ -147,115 +160,146 @@ __device__ __forceinline__ float2 sub_mul2(float a, float b, float minus, float 
     return r;
 }
 
-template <typename T>
-__device__ __forceinline__ void add_vector(Stat& v, const Vec<T>& x, float k) {
-    constexpr int n = Vec<T>::kPer;
-    float top = x.get(0);
+__device__ __forceinline__ float2 mul2(float a, float b, float k) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, k;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 k, {%4, %4};\n\tmul.rn.f32x2 x, x, k;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a), "f"(b), "f"(k));
+    return r;
+}
+
+// Largest element of N vectors; NaNs are passed over (they reach the sum).
+template <int N>
+__device__ __forceinline__ float top_of(const Vec<uint32_t> (&x)[N]) {
+    float top = -INFINITY;
 #pragma unroll
-    for (int i = 1; i < n; ++i) top = fmaxf(top, x.get(i));
+    for (int u = 0; u < N; ++u) top = fmaxf(top, fmaxf(fmaxf(x[u].get(0), x[u].get(1)), fmaxf(x[u].get(2), x[u].get(3))));
+    return top;
+}
+
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ float top_of(const Vec<uint16_t> (&x)[N]) {
+    uint32_t top = 0xFF80FF80u;
+#pragma unroll
+    for (int u = 0; u < N; ++u) top = max_pair(top, max_pair(max_pair(x[u].v.x, x[u].v.y), max_pair(x[u].v.z, x[u].v.w)));
+    return fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u));
+}
+
+// N vectors at once: one look at the maximum for all of them, and enough independent terms to keep
+// the exponential unit busy.
+template <typename T, int N>
+__device__ __forceinline__ void add_vectors(Stat& v, const Vec<T> (&x)[N], float k) {
+    const float top = top_of(x);
     if (top > v.m) {
         v.s *= exp2_fast((v.m - top) * k);  // 0 where nothing was seen: m is -inf
         v.m = top;
     }
     const float minus = v.m == -INFINITY ? 0.0f : -v.m;  // nothing but -inf so far: their terms are 0
-    float sum[2] = {0.0f, 0.0f};
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < n; i += 2) {
-        const float2 t = sub_mul2(x.get(i), x.get(i + 1), minus, k);
-        sum[0] += exp2_fast(t.x), sum[1] += exp2_fast(t.y);
-    }
-    v.s += sum[0] + sum[1];
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < Vec<T>::kPer; i += 2) {
+            const float2 t = sub_mul2(x[u].get(i), x[u].get(i + 1), minus, k);
+            sum[i & 2] += exp2_fast(t.x), sum[(i & 2) + 1] += exp2_fast(t.y);
+        }
+    v.s += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
-// coef ([v = y] - softmax_v) for the elements of vector j, `f` = -coef / s; target counted in the vectors' elements.
+// f * 2^(k (z - m)): with f = -coef / s the gradient of a row, but for its target.
 template <typename T>
-__device__ __forceinline__ Vec<T> grad_vector(const Vec<T>& x, int64_t j, int64_t target, float m, float k, float f, float coef) {
-    constexpr int n = Vec<T>::kPer;
-    float g[n];
+__device__ __forceinline__ Vec<T> grad_vector(const Vec<T>& x, float m, float k, float f) {
+    float g[Vec<T>::kPer];
 #pragma unroll
-    for (int i = 0; i < n; i += 2) {
-        const float2 t = sub_mul2(x.get(i), x.get(i + 1), -m, k);
-        g[i] = f * exp2_fast(t.x), g[i + 1] = f * exp2_fast(t.y);
+    for (int i = 0; i < Vec<T>::kPer; i += 2) {
+        const float2 t = sub_mul2(x.get(i), x.get(i + 1), -m, k), r = mul2(exp2_fast(t.x), exp2_fast(t.y), f);
+        g[i] = r.x, g[i + 1] = r.y;
     }
-    if (target / n == j) {
-#pragma unroll
-        for (int i = 0; i < n; ++i)
-            if (target % n == i) g[i] += coef;
-    }
-    Vec<T> r;
-    uint32_t* w = &r.v.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(g[i]);
-        else w[i] = bf16_pair(g[2 * i], g[2 * i + 1]);
-    }
-    return r;
+    Vec<T> v;
+    v.set(g);
+    return v;
 }
 
-// Stores vector j of z's grid to dz, whose rows may lie differently against 16 bytes.
-template <typename T>
-__device__ __forceinline__ void store_vector(const Vec<T>& v, const Row<T>& z, const Row<T>& dz, int64_t j) {
-    if (z.head == dz.head) {
-        v.store(dz, j);
-        return;
-    }
-    const uint32_t* w = v.words();
-#pragma unroll
-    for (int i = 0; i < Vec<T>::kPer; ++i) {
-        const int64_t at = j * Vec<T>::kPer + i;
-        if (!z.own(at)) continue;
-        T* p = dz.element(at - z.head + dz.head);
-        if constexpr (sizeof(T) == 4) *p = w[i];
-        else *p = static_cast<T>(w[i >> 1] >> (16 * (i & 1)));
-    }
-}
+constexpr int kAhead = 4;  // vectors that a thread works on at a time
 
-// Vectors first, first + step, ... below last.
-template <typename T>
-__device__ __forceinline__ Stat stat_of(const Row<T>& r, int64_t first, int64_t last, int step, float k) {
-    constexpr int kAhead = 4;  // loads of a thread under way at a time
+// Whole vectors lo + t, lo + t + THREADS, ...; the first partial vector by thread 0, the last by the last.
+template <typename T, int THREADS>
+__device__ __forceinline__ Stat stat_of(const Row<T>& r, uint32_t t, float k) {
     Stat v{-INFINITY, 0.0f};
-    int64_t j = first;
-    for (; j + (kAhead - 1) * step < last; j += kAhead * step) {
+    const uint32_t n = r.hi - r.lo;
+    const uint4* p = r.vector(r.lo + t);
+    uint32_t j = t;
+    for (; j + (kAhead - 1) * THREADS < n; j += kAhead * THREADS, p += kAhead * THREADS) {
         Vec<T> x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) x[u].load(r, j + u * step);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) add_vector(v, x[u], k);
+        for (int u = 0; u < kAhead; ++u) x[u].v = p[u * THREADS];
+        add_vectors(v, x, k);
     }
-    for (; j < last; j += step) {
-        Vec<T> x;
-        x.load(r, j);
-        add_vector(v, x, k);
+    for (; j < n; j += THREADS, p += THREADS) {
+        Vec<T> x[1];
+        x[0].v = *p;
+        add_vectors(v, x, k);
+    }
+    if ((r.first && t == 0) || (r.last && t == THREADS - 1)) {
+        Vec<T> x[1];
+        if (r.first && t == 0) x[0].load_partial(r, 0), add_vectors(v, x, k);
+        if (r.last && t == THREADS - 1) x[0].load_partial(r, r.hi), add_vectors(v, x, k);
     }
     return v;
 }
 
-template <typename T>
-__device__ __forceinline__ void grad_of(const Row<T>& z, const Row<T>& dz, int64_t first, int64_t last, int step, int64_t target,
-                                        const Stat& s, float k, float coef) {
-    constexpr int kAhead = 4;
+// dz = coef ([v = y] - softmax_v). The target's element is written once more by the thread that
+// wrote it (`picked`: its logit, read before anything is written: dz may be z).
+template <typename T, int THREADS>
+__device__ __forceinline__ void grad_of(const Row<T>& z, const Row<T>& dz, uint32_t t, uint32_t target, float picked, const Stat& s,
+                                        float k, float coef) {
     const float f = -coef / s.s;
-    int64_t j = first;
-    for (; j + (kAhead - 1) * step < last; j += kAhead * step) {
-        Vec<T> x[kAhead];
+    const uint32_t n = z.hi - z.lo;
+    const uint4* p = z.vector(z.lo + t);
+    uint32_t j = t;
+    if (z.head == dz.head) {
+        uint4* q = dz.vector(z.lo + t);
+        for (; j + (kAhead - 1) * THREADS < n; j += kAhead * THREADS, p += kAhead * THREADS, q += kAhead * THREADS) {
+            Vec<T> x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) x[u].load(z, j + u * step);
+            for (int u = 0; u < kAhead; ++u) x[u].v = p[u * THREADS];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) store_vector(grad_vector(x[u], j + u * step, target + z.head, s.m, k, f, coef), z, dz, j + u * step);
+            for (int u = 0; u < kAhead; ++u) __stcs(q + u * THREADS, grad_vector(x[u], s.m, k, f).v);
+        }
+        for (; j < n; j += THREADS, p += THREADS, q += THREADS) {
+            Vec<T> x;
+            x.v = *p;
+            __stcs(q, grad_vector(x, s.m, k, f).v);
+        }
+    } else {  // rows of dz lie otherwise against 16 bytes: element by element
+        for (; j < n; j += THREADS, p += THREADS) {
+            Vec<T> x;
+            x.v = *p;
+            grad_vector(x, s.m, k, f).store_partial(z, dz, z.lo + j);
+        }
     }
-    for (; j < last; j += step) {
+    if ((z.first && t == 0) || (z.last && t == THREADS - 1)) {
         Vec<T> x;
-        x.load(z, j);
-        store_vector(grad_vector(x, j, target + z.head, s.m, k, f, coef), z, dz, j);
+        if (z.first && t == 0) x.load_partial(z, 0), grad_vector(x, s.m, k, f).store_partial(z, dz, 0);
+        if (z.last && t == THREADS - 1) x.load_partial(z, z.hi), grad_vector(x, s.m, k, f).store_partial(z, dz, z.hi);
     }
+    const uint32_t at = (target + z.head) / Row<T>::kPer;  // the target's vector
+    const uint32_t owner = at < z.lo ? 0 : (at >= z.hi ? THREADS - 1 : (at - z.lo) % THREADS);
+    if (t == owner) Elem<T>::store(dz.element(target + dz.head), fmaf(f, exp2_fast((picked - s.m) * k), coef));
 }
 
 template <typename T>
-__device__ __forceinline__ void zero_of(const Row<T>& dz, int64_t first, int64_t last, int step) {
+__device__ __forceinline__ void zero_of(const Row<T>& dz, uint32_t from, uint32_t to, uint32_t t, uint32_t threads) {  // vectors
+    for (uint32_t j = max(from, dz.lo) + t; j < min(to, dz.hi); j += threads) __stcs(dz.vector(j), make_uint4(0u, 0u, 0u, 0u));
     Vec<T> zero;
     zero.v = make_uint4(0u, 0u, 0u, 0u);
-    for (int64_t j = first; j < last; j += step) zero.store(dz, j);
+    if (dz.first && from == 0 && t == 0) zero.store_partial(dz, dz, 0);
+    if (dz.last && from <= dz.hi && dz.hi < to && t == threads - 1) zero.store_partial(dz, dz, dz.hi);
 }
 
 struct Policy {
@@ -268,13 +312,19 @@ struct PolicyTerm {
     float loss, kl, clipped, slope;
 };
 
-__device__ __forceinline__ PolicyTerm policy_term(const Policy& p, int64_t row, float logp, float w) {
-    const float adv = p.advantages[row], r = expf(logp - p.old_logp[row]);
+struct PolicyRow {
+    float adv, old_logp, ref_logp;
+    __device__ __forceinline__ PolicyRow(const Policy& p, int64_t row)
+        : adv(p.advantages[row]), old_logp(p.old_logp[row]), ref_logp(p.ref_logp == nullptr ? 0.0f : p.ref_logp[row]) {}
+};
+
+__device__ __forceinline__ PolicyTerm policy_term(const Policy& p, const PolicyRow& g, float logp, float w) {
+    const float adv = g.adv, r = expf(logp - g.old_logp);
     const float gain = r * adv, held = fminf(fmaxf(r, p.lo), p.hi) * adv;
     const bool clipped = gain > held;
     float kl = 0.0f, dkl = 0.0f;
     if (p.ref_logp != nullptr) {
-        const float back = p.ref_logp[row] - logp, u = expf(back);
+        const float back = g.ref_logp - logp, u = expf(back);
         kl = u - back - 1.0f;
         dkl = 1.0f - u;
     }
@@ -305,101 +355,206 @@ __global__ void __launch_bounds__(block_of<THREADS>()) policy_stream_kernel(cons
     int64_t target;
     float w;
     if (!row_live(a, row, &target, &w)) {
-        if (a.dz != nullptr) zero_of(dz, t, dz.vectors, THREADS);
+        if (a.dz != nullptr) zero_of(dz, 0, dz.vectors(), t, THREADS);
         if (t == 0) store_term(a, p, rows, row, 0.0f, PolicyTerm{0.0f, 0.0f, 0.0f, 0.0f});
         return;
     }
-    const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(target + z.head));
-    const Stat s = row_join<THREADS>(stat_of(z, t, z.vectors, THREADS, k), shared, k);
+    const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(static_cast<uint32_t>(target) + z.head));
+    const PolicyRow given(p, row);
+    const Stat s = row_join<THREADS>(stat_of<T, THREADS>(z, t, k), shared, k);
     const float logp = (picked - s.m) * a.c - logf(s.s);
-    const PolicyTerm term = policy_term(p, row, logp, w);
+    const PolicyTerm term = policy_term(p, given, logp, w);
     if (t == 0) store_term(a, p, rows, row, logp, term);
-    if (a.dz != nullptr) grad_of(z, dz, t, z.vectors, THREADS, target, s, k, term.slope * scale_of(a));
+    if (a.dz != nullptr) grad_of<T, THREADS>(z, dz, t, static_cast<uint32_t>(target), picked, s, k, term.slope * scale_of(a));
 }
 
-// ---- rows held in shared memory between the sum and the gradient: one block to a row, or a cluster
-// of up to 8 whose blocks hold a slice each and exchange their statistics. ------------------------------
-constexpr int kSliceThreads = 256;
-constexpr int kParts = 4;  // of a slice, so that summing starts when the first has arrived
+// 16 bytes to the same place of block `to` of the cluster, and their arrival to its barrier.
+__device__ __forceinline__ void tell(uint32_t at, uint32_t bar, int to, const float4& v) {
+    asm volatile("{\n\t.reg .b32 x, y;\n\tmapa.shared::cluster.u32 x, %0, %2;\n\tmapa.shared::cluster.u32 y, %1, %2;\n\t"
+                 "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [x], {%3, %4, %5, %6}, [y];\n\t}"
+                 ::"r"(at), "r"(bar), "r"(to), "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)),
+                 "r"(__float_as_uint(v.w)) : "memory");
+}
 
+// ---- rows read once: one block to a row, or a cluster of up to 8 whose blocks take a slice each. Slices
+// come by bulk copies, a row or two ahead; a thread turns its 32 logits of a row into exponentials
+// relative to its own maximum, which stay in registers while the block, and the cluster, join their
+// statistics. So the gradient needs one more factor and no second exponential: with two of them for
+// each bf16 logit the exponential unit alone would take as long as the memory (8192 x 131072: 986 us).
+constexpr int kSliceThreads = 128;
+template <int HELD>
+constexpr int kSliceBlocks = HELD == 64 ? 5 : 3;  // on an SM
+
+template <typename T, int HELD>
+constexpr int kSliceVectors = kSliceThreads * HELD / Row<T>::kPer;
 template <typename T>
-__global__ void __launch_bounds__(kSliceThreads) policy_slice_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, int64_t rows, int slice) {
+constexpr int kSliceSlots = sizeof(T) == 4 ? 1 : 2;
+
+struct Slices {
+    int64_t rows;
+    int count;    // rows of a cluster, one after another
+    int vectors;  // of a slice
+};
+
+// What a block has to know of a row before it can work on it.
+struct Given {
+    int target;  // -1: the row is left out
+    float w;
+
+    __device__ __forceinline__ Given(const Logits& a, int64_t row, bool in) : target(-1), w(0.0f) {
+        int64_t y;
+        if (in && row_live(a, row, &y, &w)) target = static_cast<int>(y);
+    }
+    __device__ __forceinline__ bool live() const { return target >= 0; }
+};
+
+template <typename T, int HELD>
+__global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slice_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, const __grid_constant__ Slices c) {
     extern __shared__ __align__(128) uint8_t dynamic[];
-    __shared__ Stat shared[kSliceThreads / 32], joined[8];
-    __shared__ uint64_t arrived[kParts];
+    constexpr int THREADS = kSliceThreads, kSlots = kSliceSlots<T>, kPer = Row<T>::kPer, kVectors = HELD / kPer;
+    __shared__ Stat shared[2][THREADS / 32];  // two sets: a warp may be a row ahead of one that still reads
+    __shared__ float4 joined[2][8];           // of the cluster's blocks: m, s, the target's logit
+    __shared__ uint64_t arrived[kSlots], told[2];
     __shared__ int abort;
-    uint4* const held = reinterpret_cast<uint4*>(dynamic);
     uint32_t rank, size;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
-    const int64_t row = blockIdx.x / size;
-    const int t = threadIdx.x;
-    const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
-    const Row<T> dz(static_cast<T*>(a.dz) + row * a.dz_stride, a.vocab);
-    const int64_t first = static_cast<int64_t>(rank) * slice;
-    int64_t target;
-    float w;
-    if (!row_live(a, row, &target, &w)) {  // for every block of the cluster
-        const int64_t most = dz.vectors > z.vectors ? dz.vectors : z.vectors;
-        zero_of(dz, first + t, min(rank + 1 == size ? most : first + slice, dz.vectors), kSliceThreads);
-        if (rank == 0 && t == 0) store_term(a, p, rows, row, 0.0f, PolicyTerm{0.0f, 0.0f, 0.0f, 0.0f});
-        return;
-    }
-    // every block of the cluster must have begun before another writes to its memory
-    if (size > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    const int n = static_cast<int>(max(min(z.vectors - first, static_cast<int64_t>(slice)), static_cast<int64_t>(0)));
-    const int part = (n + kParts - 1) / kParts;
+    const uint32_t t = threadIdx.x;
+    const int64_t row0 = blockIdx.x / size * static_cast<int64_t>(c.count);
+    const int count = static_cast<int>(min(static_cast<int64_t>(c.count), c.rows - row0));
+    const uint32_t begin = rank * c.vectors, stop = begin + c.vectors;  // this block's vectors of a row
+    const float k = a.c * kLog2e;
+    const T* const z0 = static_cast<const T*>(a.z);
+
     if (t == 0) {
-        for (int i = 0; i < kParts; ++i) mbar_init(smem_addr(&arrived[i]), 1);
+        for (int i = 0; i < kSlots; ++i) mbar_init(smem_addr(&arrived[i]), 1);
+        mbar_init(smem_addr(&told[0]), 1);
+        mbar_init(smem_addr(&told[1]), 1);
         abort = 0;
         mbar_init_visible();
-        // whole vectors by bulk copies; the first and the last of the row, if they are not, below
-        const int lo = n > 0 && !z.whole(first) ? 1 : 0, hi = n > 0 && !z.whole(first + n - 1) ? n - 1 : n;
-        for (int i = 0; i < kParts; ++i) {
-            const int from = max(i * part, lo), to = min((i + 1) * part, hi);
-            const uint32_t bytes = to > from ? (to - from) * 16 : 0;
-            mbar_expect(smem_addr(&arrived[i]), bytes);
-            if (bytes > 0) bulk_load(smem_addr(held + from), z.vector(first + from), smem_addr(&arrived[i]), bytes);
-        }
     }
-    if (t == 32 && n > 0) {
-        Vec<T> x;
-        if (!z.whole(first)) x.load(z, first), held[0] = x.v;
-        if (!z.whole(first + n - 1)) x.load(z, first + n - 1), held[n - 1] = x.v;
+    auto slot_of = [&](int i) { return reinterpret_cast<uint4*>(dynamic) + (kSlots == 2 ? i & 1 : 0) * c.vectors; };
+    auto fetch = [&](int i) {  // by one thread: the whole vectors of the slice
+        const Row<T> z(z0 + (row0 + i) * a.z_stride, a.vocab);
+        const uint32_t from = max(begin, z.lo), to = min(stop, z.hi), bytes = to > from ? (to - from) * 16 : 0;
+        const uint32_t bar = smem_addr(&arrived[kSlots == 2 ? i & 1 : 0]);
+        mbar_expect(bar, bytes);
+        if (bytes > 0) bulk_load(smem_addr(slot_of(i) + (from - begin)), z.vector(from), bar, bytes);
+    };
+
+    Given now(a, row0, true), next(a, row0 + 1, count > 1);
+    if (t == 0) {
+        if (now.live()) fetch(0);
+        if (kSlots == 2 && next.live()) fetch(1);
     }
-    const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(target + z.head));
     __syncthreads();
-    Stat s{-INFINITY, 0.0f};
+    // every block of the cluster must have begun, and its barriers be ready, before another writes to its memory
+    // (the barriers' initialisation has a fence of its own)
+    if (size > 1) asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    uint32_t slot_parity = 0, live_rows = 0;  // slot_parity: a bit for each slot
     bool ok = true;
-    for (int i = 0; i < kParts; ++i) {
-        ok = mbar_wait(smem_addr(&arrived[i]), 0, &abort) && ok;
-        for (int j = i * part + t; j < min((i + 1) * part, n); j += kSliceThreads) {
-            Vec<T> x;
-            x.v = held[j];
-            add_vector(s, x, k);
+    for (int i = 0; i < count; ++i) {
+        const int64_t row = row0 + i;
+        const Row<T> z(z0 + row * a.z_stride, a.vocab);
+        const Row<T> dz(static_cast<T*>(a.dz) + row * a.dz_stride, a.vocab);
+        const Given later(a, row + 2, i + 2 < count);
+        const bool fetch_next = kSlots == 2 ? later.live() : next.live();
+        if (!now.live()) {  // for every block of the cluster
+            zero_of(dz, begin, rank + 1 == size ? 0xFFFFFFFFu : stop, t, THREADS);
+            if (rank == 0 && t == 0) store_term(a, p, c.rows, row, 0.0f, PolicyTerm{0.0f, 0.0f, 0.0f, 0.0f});
+            if (fetch_next && t == 0) fetch(i + kSlots);
+        } else {
+            const int slot = kSlots == 2 ? i & 1 : 0, set = live_rows & 1;
+            const PolicyRow given(p, row);
+            const uint32_t target = now.target + z.head, target_vector = target / kPer;
+            const bool has_target = target_vector >= begin && target_vector < stop;
+            float picked = has_target ? Elem<T>::load(z.element(target)) : 0.0f;
+            if (size > 1 && t == 0) mbar_expect(smem_addr(&told[set]), size * 16);
+
+            // this thread's vectors of the row are begin + t + u * THREADS; whole ones are below `whole`
+            const uint4* const held = slot_of(i) + t;
+            const uint32_t whole = min(stop, z.hi) > begin + t ? min(stop, z.hi) - begin - t : 0;
+            const bool odd_first = z.first && begin == 0 && t == 0;
+            const bool odd_last = z.last && z.hi >= begin && z.hi < stop && (z.hi - begin) % THREADS == t;
+            ok = mbar_wait(smem_addr(&arrived[slot]), (slot_parity >> slot) & 1, &abort) && ok;
+            slot_parity ^= 1u << slot;
+            Vec<T> x[kVectors];
+#pragma unroll
+            for (int u = 0; u < kVectors; ++u) {
+                if (u * THREADS < whole) x[u].v = held[u * THREADS];
+                else x[u].none();
+            }
+            if (odd_first) x[0].load_partial(z, 0);
+            if (odd_last) {
+#pragma unroll
+                for (int u = 0; u < kVectors; ++u)
+                    if (begin + t + u * THREADS == z.hi) x[u].load_partial(z, z.hi);
+            }
+            const float top = top_of(x), minus = top == -INFINITY ? 0.0f : -top;
+            float e[HELD], sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int u = 0; u < kVectors; ++u)
+#pragma unroll
+                for (int v = 0; v < kPer; v += 2) {
+                    const float2 d = sub_mul2(x[u].get(v), x[u].get(v + 1), minus, k);
+                    sum[0] += e[u * kPer + v] = exp2_fast(d.x);
+                    sum[1] += e[u * kPer + v + 1] = exp2_fast(d.y);
+                }
+            Stat s{top, sum[0] + sum[1]};
+            if (!ok) s.s = __uint_as_float(0x7FC00000u);  // a copy that did not arrive shows
+            s = row_join<THREADS>(s, shared[set], k);
+            // the block is past a barrier: its slot has been read
+            if (fetch_next && t == 0) fetch(i + kSlots);
+            if (size > 1) {
+                if (t < size) tell(smem_addr(&joined[set][rank]), smem_addr(&told[set]), t, make_float4(s.m, s.s, picked, 0.0f));
+                ok = mbar_wait(smem_addr(&told[set]), (live_rows >> 1) & 1, &abort) && ok;
+                const uint32_t lane = t & 31;
+                const float4 o = lane < size ? joined[set][lane] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+                s = warp_join<8>(Stat{o.x, o.y}, k);
+                float logit = o.z;  // 0 but for the block that has the target
+#pragma unroll
+                for (int d = 4; d > 0; d >>= 1) logit += __shfl_xor_sync(0xFFFFFFFFu, logit, d);
+                picked = __shfl_sync(0xFFFFFFFFu, logit, 0);
+                if (!ok) s.s = __uint_as_float(0x7FC00000u);
+            }
+            ++live_rows;
+            const float logp = (picked - s.m) * a.c - logf(s.s);
+            const PolicyTerm term = policy_term(p, given, logp, now.w);
+            if (rank == 0 && t == 0) store_term(a, p, c.rows, row, logp, term);
+            const float coef = term.slope * scale_of(a), all = -coef / s.s, f = all * exp2_fast((top - s.m) * k);
+            auto grad = [&](int u) {
+                float g[kPer];
+#pragma unroll
+                for (int v = 0; v < kPer; v += 2) {
+                    const float2 r = mul2(e[u * kPer + v], e[u * kPer + v + 1], f);
+                    g[v] = r.x, g[v + 1] = r.y;
+                }
+                Vec<T> v;
+                v.set(g);
+                return v;
+            };
+            if (z.head == dz.head) {
+                uint4* const q = dz.vector(begin + t);
+#pragma unroll
+                for (int u = 0; u < kVectors; ++u)
+                    if (u * THREADS < whole && !(u == 0 && odd_first)) __stcs(q + u * THREADS, grad(u).v);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kVectors; ++u)
+                    if (u * THREADS < whole && !(u == 0 && odd_first)) grad(u).store_partial(z, dz, begin + t + u * THREADS);
+            }
+            if (odd_first) grad(0).store_partial(z, dz, 0);
+            if (odd_last) {
+#pragma unroll
+                for (int u = 0; u < kVectors; ++u)
+                    if (begin + t + u * THREADS == z.hi) grad(u).store_partial(z, dz, z.hi);
+            }
+            // once more, by the thread that wrote it
+            if (has_target && (target_vector - begin) % THREADS == t)
+                Elem<T>::store(dz.element(now.target + dz.head), fmaf(all, exp2_fast((picked - s.m) * k), coef));
         }
-    }
-    if (!ok) s.s = __uint_as_float(0x7FC00000u);  // a copy that did not arrive shows
-    s = row_join<kSliceThreads>(s, shared, k);
-    if (size > 1) {
-        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        if (t < static_cast<int>(size)) {
-            uint32_t at;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(&joined[rank])), "r"(t));
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(s.m), "f"(s.s) : "memory");
-        }
-        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-        s = joined[0];
-        for (uint32_t i = 1; i < size; ++i) s = join(s, joined[i], k);
-    }
-    const float logp = (picked - s.m) * a.c - logf(s.s);
-    const PolicyTerm term = policy_term(p, row, logp, w);
-    if (rank == 0 && t == 0) store_term(a, p, rows, row, logp, term);
-    const float coef = term.slope * scale_of(a), f = -coef / s.s;
-    for (int j = t; j < n; j += kSliceThreads) {
-        Vec<T> x;
-        x.v = held[j];
-        store_vector(grad_vector(x, first + j, target + z.head, s.m, k, f, coef), z, dz, first + j);
+        now = next;
+        next = later;
     }
 }
 
@@ -445,8 +600,8 @@ __global__ void __launch_bounds__(block_of<THREADS>()) row_stat_kernel(const __g
     float logp = 0.0f;
     if (row_live(a, row, &target, &w)) {
         const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
-        const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(target + z.head));
-        s = row_join<THREADS>(stat_of(z, t, z.vectors, THREADS, k), shared, k);
+        const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(static_cast<uint32_t>(target) + z.head));
+        s = row_join<THREADS>(stat_of<T, THREADS>(z, t, k), shared, k);
         logp = (picked - s.m) * a.c - logf(s.s);
     }
     if (t == 0) {
@@ -522,15 +677,18 @@ __global__ void __launch_bounds__(block_of<THREADS>()) row_grad_kernel(const __g
     const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
     const Row<T> dz(static_cast<T*>(a.dz) + row * a.dz_stride, a.vocab);
     const float coef = r.coef[row];
-    if (coef == 0.0f) zero_of(dz, t, dz.vectors, THREADS);
-    else grad_of(z, dz, t, z.vectors, THREADS, a.targets[row], r.stat[row], a.c * kLog2e, coef);
+    if (coef == 0.0f) {
+        zero_of(dz, 0, dz.vectors(), t, THREADS);
+    } else {
+        const uint32_t target = static_cast<uint32_t>(a.targets[row]);
+        grad_of<T, THREADS>(z, dz, t, target, Elem<T>::load(z.element(target + z.head)), r.stat[row], a.c * kLog2e, coef);
+    }
 }
 
 // ---- choices of a launch ------------------------------------------------------------------------------
 constexpr int64_t kWarpRowBytes = 8192;     // rows up to this size: a warp each
 constexpr int kFewRows = 296;               // fewer rows than two for each SM: a large block each
-constexpr int64_t kSliceBytes = 72 * 1024;  // three such blocks on an SM
-constexpr int64_t kMostSliceBytes = 208 * 1024;
+constexpr int kMostCount = 8;               // rows of a cluster
 
 template <typename F>
 void pick_threads(int64_t rows, int64_t vocab, ss_dtype dt, F&& launch) {
@@ -548,32 +706,45 @@ unsigned rows_grid(int64_t rows) {
     return static_cast<unsigned>((rows + per - 1) / per);
 }
 
-// Blocks that share a row in policy_slice_kernel, 0 if it does not fit (or is small): the fewest with which
-// three blocks fit on an SM, more where there are not enough rows for all SMs.
-int cluster_of(int64_t rows, int64_t vocab, size_t eb) {
-    const int64_t bytes = vocab * static_cast<int64_t>(eb) + 16;
-    if (bytes <= kWarpRowBytes || bytes > 8 * kMostSliceBytes) return 0;
+// Blocks that share a row in policy_slice_kernel, 0 if even 8 do not hold it: the fewest that do, more where there are
+// not enough rows for all SMs.
+template <typename T, int HELD>
+int cluster_of(int64_t rows, int64_t vectors, int sms) {
+    if (vectors > 8 * kSliceVectors<T, HELD>) return 0;
     int size = 1;
-    while (size < 8 && (bytes > size * kSliceBytes || (rows * size < 148 && bytes > size * 8192))) size *= 2;
+    while (size < 8 && (vectors > size * kSliceVectors<T, HELD> || (rows * size * 2 <= sms && vectors > size * kSliceThreads))) size *= 2;
     return size;
 }
 
-template <typename T>
-cudaError_t launch_slices(const Logits& a, const Policy& p, int64_t rows, int size, cudaStream_t st) {
-    const int64_t vectors = (a.vocab * static_cast<int64_t>(sizeof(T)) + 15 + 15) / 16;  // wherever the row starts
-    const int slice = static_cast<int>((vectors + size - 1) / size);
+template <typename T, int HELD>
+cudaError_t launch_slices(const Logits& a, const Policy& p, int64_t rows, int64_t vectors, int size, int sms, cudaStream_t st) {
+    Slices c{rows, 1, static_cast<int>((vectors + size - 1) / size)};
+    // as many rows to a cluster as leave three rounds of blocks for every SM
+    const int64_t count = rows * size / (3 * kSliceBlocks<HELD> * sms);
+    c.count = static_cast<int>(count < 1 ? 1 : (count > kMostCount ? kMostCount : count));
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(rows * size));
+    cfg.gridDim = dim3(static_cast<unsigned>((rows + c.count - 1) / c.count * size));
     cfg.blockDim = dim3(kSliceThreads);
-    cfg.dynamicSmemBytes = static_cast<size_t>(slice) * 16;
+    cfg.dynamicSmemBytes = static_cast<size_t>(c.vectors) * 16 * kSliceSlots<T>;
     cfg.stream = st;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = size, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaFuncSetAttribute(policy_slice_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(cfg.dynamicSmemBytes));
-    return e != cudaSuccess ? e : cudaLaunchKernelEx(&cfg, policy_slice_kernel<T>, a, p, rows, slice);
+    const cudaError_t e = cudaFuncSetAttribute(policy_slice_kernel<T, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(cfg.dynamicSmemBytes));
+    return e != cudaSuccess ? e : cudaLaunchKernelEx(&cfg, policy_slice_kernel<T, HELD>, a, p, c);
+}
+
+// Whether the rows were given to policy_slice_kernel.
+template <typename T>
+bool try_slices(const Logits& a, const Policy& p, const Mat& z, int sms, cudaStream_t st, cudaError_t* e) {
+    const int64_t bytes = z.cols * static_cast<int64_t>(sizeof(T)), vectors = z.row_aligned(16) ? (bytes + 15) / 16 : (bytes + 30) / 16;
+    if (bytes <= kWarpRowBytes) return false;
+    if (const int size = cluster_of<T, 64>(z.rows, vectors, sms)) *e = launch_slices<T, 64>(a, p, z.rows, vectors, size, sms, st);
+    else if (const int size = cluster_of<T, 128>(z.rows, vectors, sms)) *e = launch_slices<T, 128>(a, p, z.rows, vectors, size, sms, st);
+    else return false;
+    return true;
 }
 
 // ---- checks shared by the two losses ------------------------------------------------------------------
@@ -650,9 +821,10 @@ int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64
     const Logits a{logits, dlogits, z.stride, dz.stride, vocab, targets, weights, grad_scale, inv_temperature, logp};
     const Policy p{old_logp, ref_logp, advantages, 1.0f - clip_low, 1.0f + clip_high, kl_coef, static_cast<float*>(workspace)};
     if (rows > 0) {
-        const int size = dlogits == nullptr ? 0 : cluster_of(rows, vocab, dtype_bytes(dt));
-        if (size > 0 && rows * size <= kMaxSide) {
-            const cudaError_t e = dt == SS_F32 ? launch_slices<uint32_t>(a, p, rows, size, st) : launch_slices<uint16_t>(a, p, rows, size, st);
+        cudaError_t e;
+        const int sms = device_sm_count(&e);
+        if (e != cudaSuccess) return cuda_status_public(e);
+        if (dlogits != nullptr && (dt == SS_F32 ? try_slices<uint32_t>(a, p, z, sms, st, &e) : try_slices<uint16_t>(a, p, z, sms, st, &e))) {
             if (e != cudaSuccess) return cuda_status_public(e);
         } else {
             pick_threads(rows, vocab, dt, [&](auto t, auto threads) {
