@@ -19,19 +19,24 @@
 namespace ss {
 namespace {
 
-constexpr int kTileN = 128, kTileK = 256;  // of dW: n from dY, k from x^
+// Two blocks on neighbouring SMs share a 256 x 256 tile: each copies and keeps 128 of its columns
+// of dY and its sums, and decodes 128 of its columns of x^ for both. Against one block for a 128 x
+// 256 tile that halves the decoding and takes a third off the shared memory's traffic.
+constexpr int kTileN = 256, kTileK = 256;  // of dW: n from dY, k from x^
+constexpr int kBlockN = kTileN / 2, kBlockK = kTileK / 2;
 constexpr int kRows = 64;                  // rows of a stage
-constexpr int kStages = 4;
+constexpr int kStages = 6;
 constexpr int kChunk = 8;                  // stages summed in the matrix unit
 constexpr int kWorkers = 512;              // threads that decode and add
-constexpr int kThreads = kWorkers + 128;   // and a warp each for the copies and the matrix unit (two more idle)
-// A worker holds 64 sums and its share of a stage's codes. The block is launched with 96 registers
-// a thread (what 640 threads leave of an SM's 65536); the other warps give some of theirs up:
-// 512 * 112 + 128 * 32 = 640 * 96 = 61440.
+constexpr int kThreads = kWorkers + 128;   // and a warp for the copies, one for the matrix unit, two for the word between the blocks
+// A worker holds 64 sums and its share of the next stages' codes. The block is launched with 96
+// registers a thread (what 640 threads leave of an SM's 65536); the other warps give most of
+// theirs up: 512 * 112 + 128 * 32 = 640 * 96 = 61440.
 constexpr int kWorkerRegs = 112, kOtherRegs = 32;
 constexpr int kSums = kTileK / (kWorkers / 128);  // columns of a worker
+constexpr int kAhead = 4;                  // stages of codes on their way
 constexpr uint32_t kPanel = kRows * 128;   // bytes of 64 columns of a stage
-constexpr uint32_t kBytesA = kTileN / 64 * kPanel, kBytesB = kTileK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
+constexpr uint32_t kBytesA = kBlockN / 64 * kPanel, kBytesB = kBlockK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
 constexpr uint32_t kSquareBytes = 32 * 16 * 4;  // a worker warp's way out
 constexpr size_t kSmem = 1024 + kStages * kStageBytes + kWorkers / 32 * kSquareBytes;
 
@@ -39,7 +44,7 @@ struct Plan {
     int tiles_n, tiles_k;   // tiles of dW; tile i: n index i % tiles_n
     int planes;             // bf16 terms of dY: 1, or 3 for fp32
     int stages_per_plane;   // stages of one plane
-    int whole;              // tiles formed by one block from all rows
+    int whole;              // tiles formed by one pair of blocks from all rows
     int parts;              // parts that each of the other tiles' rows are split in
     int part_stages;
     int units;              // whole + others * parts
@@ -68,68 +73,61 @@ __device__ __forceinline__ Unit unit_of(const Plan& p, int u) {
 
 struct Shared {
     uint64_t full_a[kStages], full_b[kStages], empty[kStages], summed[2], last;
+    uint64_t decoded[kStages];  // by this block's workers; full_b of the first block: by both blocks
     uint32_t tmem;
     int abort;
 };
 
-// The worker's share of a stage of codes: 16 columns of two rows, 32 rows apart.
+// The worker's share of a stage of codes: 16 columns of a row. Four lanes take 64 columns of a row,
+// the next four the row after it, then come the other 64 columns, then the other rows: a warp
+// loads four rows of 128 bytes, and eight lanes of a store cover all banks (see store_codes).
 struct Codes {
-    uint4 q[2];
-    uint32_t e[2];
+    uint4 q;
+    uint32_t e;
 };
 
-// Where they are: of the row t, in steps of a stage.
+__device__ __forceinline__ int share_row(int tid) { return ((tid >> 2) & 1) + 2 * ((tid >> 4) & 1) + 4 * (tid >> 5); }
+__device__ __forceinline__ int share_panel(int tid) { return (tid >> 3) & 1; }
+__device__ __forceinline__ int share_piece(int tid) { return tid & 3; }
+
+// The codes of all stages of all units of this pair, in order. Rows and columns that do not exist
+// are read as ones that do: dY has zeros for such rows, and such columns of dW are not stored. (A
+// marked group may stand in for a row: its column is NaN anyhow.)
 struct Walk {
-    const uint8_t *values, *exps;
-    int t, left;  // rows from t to the plane's end; negative: columns that do not exist
+    int unit, at, left;  // next stage to load, of its plane; stages left of the unit
+    uint32_t k;          // column of the values
 
-    __device__ __forceinline__ void start(const WeightGrad& a, int stage, int k0, int tid) {
-        const int64_t k = static_cast<int64_t>(k0) + 16 * (tid & 15);
-        t = stage * kRows + (tid >> 4);
-        left = k < a.x.groups * SS_ACT8_GROUP ? static_cast<int>(a.rows) : 0;
-        values = a.x.values + t * a.x.groups * SS_ACT8_GROUP + k;
-        exps = a.x.exps + t * a.x.groups + (k >> 5);
+    __device__ __forceinline__ void start(const WeightGrad& a, int first_unit, uint32_t rank, int tid) {
+        unit = first_unit, left = 0;
+        if (unit >= a.plan.units) return;
+        const Unit u = unit_of(a.plan, unit);
+        at = u.first % a.plan.stages_per_plane, left = u.stages;
+        k = u.tile / a.plan.tiles_n * kTileK + rank * kBlockK + 64 * share_panel(tid) + 16 * share_piece(tid);
+        if (k >= a.x.groups * SS_ACT8_GROUP) k = 0;
     }
-    __device__ __forceinline__ void next(const WeightGrad& a) {
-        t += kRows;
-        values += a.x.groups * (SS_ACT8_GROUP * kRows);
-        exps += a.x.groups * kRows;
-    }
-    __device__ __forceinline__ void load(const WeightGrad& a, Codes* c) const {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            c->q[i] = make_uint4(0u, 0u, 0u, 0u);
-            c->e[i] = 1u;
-            if (t + 32 * i < left) {
-                c->q[i] = *reinterpret_cast<const uint4*>(values + i * 32 * a.x.groups * SS_ACT8_GROUP);
-                c->e[i] = exps[i * 32 * a.x.groups];
-            }
-        }
+    __device__ __forceinline__ void load(const WeightGrad& a, int step, uint32_t rank, int tid, Codes* c) {
+        if (left == 0) return;
+        const int64_t g = min(at * kRows + share_row(tid), static_cast<int>(a.rows) - 1) * a.x.groups;
+        c->q = *reinterpret_cast<const uint4*>(a.x.values + g * SS_ACT8_GROUP + k);
+        c->e = a.x.exps[g + (k >> 5)];
+        if (++at == a.plan.stages_per_plane) at = 0;  // the next plane goes over the same codes again
+        if (--left == 0) start(a, unit + step, rank, tid);
     }
 };
 
-// Decodes them into the stage's operand: column chunk c (8 columns, 16 bytes) of row t sits at
-// chunk c ^ (t & 7) of the row. Lanes 8 apart in a row address the same banks in another panel;
-// half of them store their second chunk first, so that eight lanes always cover all banks.
+// Decodes them into the stage's operand: column chunk c (8 columns, 16 bytes) of row t of a panel
+// sits at chunk c ^ (t & 7). Eight lanes write chunks 0, 2, 4, 6 (or 1, 3, 5, 7) of an even row and
+// of the odd one after it, which the exclusive or places on all eight.
 __device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const Codes& c) {
-    const int piece = tid & 15, t0 = tid >> 4;
-    const uint32_t panel = stage_b + (piece >> 2) * kPanel;
-    const uint32_t chunk = 2 * (piece & 3), swap = (piece >> 2) & 1;
+    const int t = share_row(tid);
+    const uint32_t at = stage_b + share_panel(tid) * kPanel + t * 128, chunk = 2 * share_piece(tid);
+    const uint32_t e2 = act8_exponent_pair(c.e);
+    const uint32_t w[4] = {c.q.x, c.q.y, c.q.z, c.q.w};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int t = t0 + 32 * i;
-        const uint32_t e2 = act8_exponent_pair(c.e[i]);
-        const uint32_t w[4] = {c.q[i].x, c.q[i].y, c.q[i].z, c.q[i].w};
-        uint32_t d[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[2 * j] = act8_value_pair<0>(w[j], e2), d[2 * j + 1] = act8_value_pair<1>(w[j], e2);
-        const uint32_t row = panel + t * 128;
-        const uint32_t first = row + (((chunk + swap) ^ (t & 7)) << 4), second = row + (((chunk + 1 - swap) ^ (t & 7)) << 4);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(first), "r"(swap ? d[4] : d[0]), "r"(swap ? d[5] : d[1]),
-                     "r"(swap ? d[6] : d[2]), "r"(swap ? d[7] : d[3]) : "memory");
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(second), "r"(swap ? d[0] : d[4]), "r"(swap ? d[1] : d[5]),
-                     "r"(swap ? d[2] : d[6]), "r"(swap ? d[3] : d[7]) : "memory");
-    }
+    for (int h = 0; h < 2; ++h)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + h) ^ (t & 7)) << 4)),
+                     "r"(act8_value_pair<0>(w[2 * h], e2)), "r"(act8_value_pair<1>(w[2 * h], e2)),
+                     "r"(act8_value_pair<0>(w[2 * h + 1], e2)), "r"(act8_value_pair<1>(w[2 * h + 1], e2)) : "memory");
 }
 
 // Where 32 rows of a tile go: dW, or the part's own tile.
@@ -190,9 +188,9 @@ __device__ __forceinline__ void store_square(uint32_t buf, int lane, const Dest&
     }
 }
 
-// A wait ran out: nothing of this block's tiles can be trusted, and that shows.
-__device__ __noinline__ void spoil(const WeightGrad& a, int tid) {
-    for (int unit = blockIdx.x; unit < a.plan.units; unit += gridDim.x) {
+// A wait ran out: nothing of this pair's tiles can be trusted, and that shows.
+__device__ __noinline__ void spoil(const WeightGrad& a, int pair, int pairs, int tid) {
+    for (int unit = pair; unit < a.plan.units; unit += pairs) {
         const int tile = unit_of(a.plan, unit).tile;
         const int64_t n0 = static_cast<int64_t>(tile % a.plan.tiles_n) * kTileN, k0 = static_cast<int64_t>(tile / a.plan.tiles_n) * kTileK;
         for (int i = tid; i < kTileN * kTileK; i += kWorkers) {
@@ -210,13 +208,17 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
     __shared__ Shared sh;
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const Plan& p = a.plan;
     volatile int* abort = &sh.abort;
+    uint32_t rank;  // in the pair; the first block issues the matrix instructions and waits for both blocks' operands
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_addr(&sh.full_a[s]), 1);
-            mbar_init(smem_addr(&sh.full_b[s]), kWorkers / 32);
+            mbar_init(smem_addr(&sh.full_b[s]), 2);
+            mbar_init(smem_addr(&sh.decoded[s]), kWorkers / 32);
             mbar_init(smem_addr(&sh.empty[s]), 1);
         }
         mbar_init(smem_addr(&sh.summed[0]), 1);
@@ -225,39 +227,36 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
         sh.abort = 0;
         mbar_init_visible();
     }
-    if (warp == 0) tmem_alloc(smem_addr(&sh.tmem), 512);
+    if (warp == 0) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
     tc_fence_before();
     __syncthreads();
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
     if (warp < kWorkers / 32) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWorkerRegs));
         // ---- decoding, and sums of the chunks. A chunk is added while the next one is decoded, after
-        // its first four stages: the last of them goes to the slot of the chunk's last stage, so the
-        // matrix unit has finished the chunk by then, and has four stages ready to work on meanwhile.
-        const int lane = tid & 31, n_local = (warp & 3) * 32, k_local = (warp >> 2) * kSums;
+        // its first six stages: the last of them goes to the slot of the chunk's last stage, so the
+        // matrix unit has finished the chunk by then, and has six stages ready to work on meanwhile.
+        const int lane = tid & 31, n_local = rank * kBlockN + (warp & 3) * 32, k_local = (warp >> 2) * kSums;
         const uint32_t out = stages + kStages * kStageBytes + warp * kSquareBytes;
-        const uint32_t tmem_at = tmem + (static_cast<uint32_t>(n_local) << 16) + k_local;
+        const uint32_t tmem_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + k_local;
         float acc[kSums];
 #pragma unroll
         for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
-        int it = 0, added = 0;                   // stages decoded, chunks added
-        int unit = blockIdx.x, at = 0, left = 0; // where the next chunk begins: its first stage, stages left of the unit
-        int prev_unit = -1;                      // the chunk to add: its unit, and whether it ends it
-        bool prev_ends = false;
-        int k0 = 0;
-        Walk walk{};
-        Codes codes{};
-        bool ok = true;
+        int it = 0, added = 0;          // stages decoded, chunks added
+        int slot = 0, unit = pair, left = 0;  // of the next stage; stages left of the unit
+        uint32_t parity = 1;
+        int prev_unit = -1;             // the chunk to add: its unit, and whether it ends it
+        bool prev_ends = false, ok = true;
+        Walk walk;
+        Codes codes[kAhead];
+        walk.start(a, pair, rank, tid);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) walk.load(a, pairs, rank, tid, &codes[i]);
         while (ok) {
-            if (left == 0 && unit < p.units) {
-                const Unit u = unit_of(p, unit);
-                at = u.first % p.stages_per_plane, left = u.stages;
-                k0 = u.tile / p.tiles_n * kTileK;
-                walk.start(a, at, k0, tid);
-                walk.load(a, &codes);
-            }
+            if (left == 0 && unit < p.units) left = unit_of(p, unit).stages;
             const int len = min(kChunk, left);
 #pragma unroll 1
             for (int s = 0;; ++s) {
@@ -291,98 +290,127 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
                     prev_unit = -1;
                 }
                 if (s >= len) break;
-                const int slot = it % kStages;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.empty[slot]), ((it / kStages) & 1) ^ 1, abort));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.empty[slot]), parity, abort));
                 if (!ok) break;
-                store_codes(stages + slot * kStageBytes + kBytesA, tid, codes);
+                auto decode = [&](Codes* c) {
+                    store_codes(stages + slot * kStageBytes + kBytesA, tid, *c);
+                    walk.load(a, pairs, rank, tid, c);
+                };
+                switch (it & (kAhead - 1)) {
+                    case 0: decode(&codes[0]); break;
+                    case 1: decode(&codes[1]); break;
+                    case 2: decode(&codes[2]); break;
+                    default: decode(&codes[3]); break;
+                }
                 smem_to_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.full_b[slot]));
+                if (lane == 0) mbar_arrive(smem_addr(&sh.decoded[slot]));
                 ++it;
-                if (++at == p.stages_per_plane) {  // the next plane goes over the same codes again
-                    at = 0;
-                    walk.start(a, 0, k0, tid);
-                } else {
-                    walk.next(a);
-                }
-                if (s + 1 < left) walk.load(a, &codes);  // on their way while the slot is waited for
+                if (++slot == kStages) slot = 0, parity ^= 1;
             }
             if (!ok || len == 0) break;
             prev_unit = unit;
             left -= len;
             prev_ends = left == 0;
-            if (prev_ends) unit += gridDim.x;
+            if (prev_ends) unit += pairs;
         }
-        if (!ok) spoil(a, tid);
+        if (!ok) spoil(a, pair, pairs, tid);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == kWorkers / 32) {
-            // ---- copies of dY
+            // ---- copies of dY: this block's half, counted by the first block's barrier
             if ((tid & 31) == 0) {
-                int it = 0;
+                const uint32_t full_a = cluster_addr(smem_addr(&sh.full_a[0]), 0);
+                int it = 0, slot = 0;
+                uint32_t parity = 1;
                 bool ok = true;
-                for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+                for (int unit = pair; ok && unit < p.units; unit += pairs) {
                     const Unit u = unit_of(p, unit);
-                    const int n0 = (u.tile % p.tiles_n) * kTileN;
+                    const int n0 = (u.tile % p.tiles_n) * kTileN + rank * kBlockN;
+                    int plane = u.first / p.stages_per_plane, at = u.first - plane * p.stages_per_plane;
 #pragma unroll 1
                     for (int s = 0; s < u.stages; ++s, ++it) {
-                        const int slot = it % kStages;
-                        ok = mbar_wait(smem_addr(&sh.empty[slot]), ((it / kStages) & 1) ^ 1, abort);
+                        ok = mbar_wait(smem_addr(&sh.empty[slot]), parity, abort);
                         if (!ok) break;
-                        const uint32_t bar = smem_addr(&sh.full_a[slot]), dst = stages + slot * kStageBytes;
-                        const int at = u.first + s, plane = at / p.stages_per_plane, t0 = (at - plane * p.stages_per_plane) * kRows;
-                        mbar_expect(bar, kBytesA);
-                        tma_load_3d(dst, &dy_map, bar, n0, t0, plane);
-                        tma_load_3d(dst + kPanel, &dy_map, bar, n0 + 64, t0, plane);
+                        if (rank == 0) mbar_expect(smem_addr(&sh.full_a[slot]), 2 * kBytesA);
+                        const uint32_t bar = full_a + slot * 8, dst = stages + slot * kStageBytes;
+                        tma_load_3d_pair(dst, &dy_map, bar, n0, at * kRows, plane);
+                        tma_load_3d_pair(dst + kPanel, &dy_map, bar, n0 + 64, at * kRows, plane);
+                        if (++at == p.stages_per_plane) at = 0, ++plane;
+                        if (++slot == kStages) slot = 0, parity ^= 1;
                     }
                 }
-                if (!ok) {  // the copies under way end in this block's memory: not before they have
+                for (int i = it > kStages ? it - kStages : 0; ok && i < it; ++i)  // the last signals arrive in this block's memory
+                    ok = mbar_wait(smem_addr(&sh.empty[i % kStages]), (i / kStages) & 1, abort);
+                if (!ok && rank == 0) {  // the copies under way end in the pair's memory: not before they have
                     int own = 0;
                     for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
                         mbar_wait(smem_addr(&sh.full_a[i % kStages]), (i / kStages) & 1, &own);
                 }
             }
-        } else if (warp == kWorkers / 32 + 1) {
+        } else if (warp >= kWorkers / 32 + 2) {
+            // ---- word of decoded stages to the first block, by two warps in turn. A release to the
+            // cluster waits for the loads that its thread has under way: the workers have four
+            // stages of codes on their way and would wait for all of them at each stage.
+            if ((tid & 31) == 0) {
+                const uint32_t full_b = cluster_addr(smem_addr(&sh.full_b[0]), 0);
+                int slot = 0, it = 0;
+                uint32_t parity = 0;
+                bool ok = true;
+                for (int unit = pair; ok && unit < p.units; unit += pairs) {
+                    const int n = unit_of(p, unit).stages;
+#pragma unroll 1
+                    for (int s = 0; s < n; ++s, ++it) {
+                        if ((it & 1) == (warp & 1)) {
+                            ok = mbar_wait(smem_addr(&sh.decoded[slot]), parity, abort);
+                            if (!ok) break;
+                            mbar_arrive_cluster(full_b + slot * 8);
+                        }
+                        if (++slot == kStages) slot = 0, parity ^= 1;
+                    }
+                }
+            }
+        } else if (warp == kWorkers / 32 + 1 && rank == 0) {
             // ---- matrix unit
             if ((tid & 31) == 0) {
                 constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK);
-                int it = 0, chunk = 0;
+                int it = 0, chunk = 0, slot = 0;
+                uint32_t parity = 0;
                 bool ok = true;
-                for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
-                    const Unit u = unit_of(p, unit);
+                for (int unit = pair; ok && unit < p.units; unit += pairs) {
+                    const int n = unit_of(p, unit).stages;
 #pragma unroll 1
-                    for (int s = 0; s < u.stages; ++s, ++it) {
-                        const int slot = it % kStages;
-                        ok = mbar_wait(smem_addr(&sh.full_a[slot]), (it / kStages) & 1, abort) &&
-                             mbar_wait(smem_addr(&sh.full_b[slot]), (it / kStages) & 1, abort);
+                    for (int s = 0; s < n; ++s, ++it) {
+                        ok = mbar_wait(smem_addr(&sh.full_a[slot]), parity, abort) && mbar_wait(smem_addr(&sh.full_b[slot]), parity, abort);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t at = stages + slot * kStageBytes, d = tmem + (chunk & 1) * kTileK;
 #pragma unroll
                         for (int k = 0; k < kRows / 16; ++k)
-                            tc_mma_bf16(d, tc_desc_rows(at + k * 2048, kPanel), tc_desc_rows(at + kBytesA + k * 2048, kPanel), idesc,
-                                        (s % kChunk) != 0 || k != 0);
-                        tc_commit(smem_addr(&sh.empty[slot]));
-                        if (s % kChunk == kChunk - 1 || s + 1 == u.stages) {
-                            tc_commit(smem_addr(&sh.summed[chunk & 1]));
+                            tc_mma_bf16_pair(d, tc_desc_rows(at + k * 2048, kPanel), tc_desc_rows(at + kBytesA + k * 2048, kPanel), idesc,
+                                             (s % kChunk) != 0 || k != 0);
+                        tc_commit_pair(smem_addr(&sh.empty[slot]));
+                        if (s % kChunk == kChunk - 1 || s + 1 == n) {
+                            tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
                             ++chunk;
                         }
+                        if (++slot == kStages) slot = 0, parity ^= 1;
                     }
                 }
                 if (!ok) {  // nothing may still be running when the tensor memory is given back
                     int own = 0;
-                    tc_commit(smem_addr(&sh.last));
+                    tc_commit_pair(smem_addr(&sh.last));
                     mbar_wait(smem_addr(&sh.last), 0, &own);
                 }
-                for (int i = it > kStages ? it - kStages : 0; ok && i < it; ++i)  // its signals arrive in this block's memory
-                    ok = mbar_wait(smem_addr(&sh.empty[i % kStages]), (i / kStages) & 1, abort);
             }
         }
     }
+    // neither block leaves while the other may still signal to it or use its operands
     tc_fence_before();
     __syncthreads();
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
     tc_fence_after();
-    if (warp == 0) tmem_free(tmem, 512);
+    if (warp == 0) tmem_free_pair(tmem, 512);
 }
 
 // dW of the tiles whose rows were split: the parts added in their order.
@@ -436,9 +464,9 @@ __global__ void __launch_bounds__(256) stage_dy_kernel(const T* dy, int64_t stri
 
 constexpr int64_t kMaxUnits = 1 << 24;  // tiles, and stages: rows and their products with kRows stay in 32 bits
 
-// How dY reaches the matrix unit, and how the work is cut. The blocks take whole tiles as long as
-// every SM gets one; the tiles that are left over (all, if there are fewer than SMs) have their
-// rows split so that they too keep most SMs busy.
+// How dY reaches the matrix unit, and how the work is cut. The pairs of blocks take whole tiles as
+// long as every pair gets one; the tiles that are left over (all, if there are fewer than pairs)
+// have their rows split so that they too keep most SMs busy.
 struct Layout {
     bool staged;
     int64_t stride, planes;  // of the staged copy
@@ -457,12 +485,12 @@ int layout_of(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int6
     Plan& p = out->plan;
     p.tiles_n = static_cast<int>(tn), p.tiles_k = static_cast<int>(tk);
     p.planes = static_cast<int>(out->planes), p.stages_per_plane = static_cast<int>(per);
-    const int tiles = static_cast<int>(tn * tk), all = p.planes * p.stages_per_plane, others = tiles % sms;
+    const int pairs = sms / 2, tiles = static_cast<int>(tn * tk), all = p.planes * p.stages_per_plane, others = tiles % pairs;
     p.whole = tiles - others;
     p.parts = 1;
     p.part_stages = all;
     if (others > 0) {
-        int parts = sms / others;
+        int parts = pairs / others;
         if (parts > all / kChunk) parts = all / kChunk;  // a part is at least one chunk
         if (parts > 1) {
             const int chunks = (all + kChunk - 1) / kChunk;
@@ -572,7 +600,18 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     }
     float* partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.staged_bytes);
     const WeightGrad a{ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, n_in), dw, partial, mw.stride, rows, n_out, n_in, accumulate, l.plan};
-    weight_grad8_kernel<<<static_cast<unsigned>(l.plan.units < sms ? l.plan.units : sms), kThreads, kSmem, st>>>(map, a);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * (l.plan.units < sms / 2 ? l.plan.units : sms / 2)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, weight_grad8_kernel, map, a);
+    if (e != cudaSuccess) return cuda_status_public(e);
     if (l.plan.parts > 1) {
         const unsigned others = static_cast<unsigned>(l.plan.tiles_n * l.plan.tiles_k - l.plan.whole);
         join_parts_kernel<<<dim3(others, 16), 256, 0, st>>>(a);
