@@ -24,12 +24,16 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {  // an address from cluster_addr
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// An arrival at a barrier of either block of a pair (an address from cluster_addr). It releases to
+// this block only, which is all that operands in shared memory need: their stores are complete, and
+// visible to the matrix unit, once the fence of smem_to_async has passed. A release to the cluster
+// would wait for every load that the thread has under way.
+__device__ __forceinline__ void mbar_arrive_pair(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -46,6 +50,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
     *abort = 1;
     return false;
+}
+
+// The same for a role of one thread, whose few instructions are fetched anew each time between those of
+// the other warps: only the first try stands in its way.
+static __device__ __noinline__ bool mbar_wait_more(uint32_t bar, uint32_t parity, volatile int* abort) { return mbar_wait(bar, parity, abort); }
+__device__ __forceinline__ bool mbar_wait_lean(uint32_t bar, uint32_t parity, volatile int* abort) {
+    return mbar_try(bar, parity) || mbar_wait_more(bar, parity, abort);
 }
 
 __device__ __forceinline__ void mbar_init_visible() {  // to the copies and the matrix unit too

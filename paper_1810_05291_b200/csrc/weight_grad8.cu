@@ -28,13 +28,12 @@ constexpr int kRows = 64;                  // rows of a stage
 constexpr int kStages = 6;
 constexpr int kChunk = 8;                  // stages summed in the matrix unit
 constexpr int kWorkers = 512;              // threads that decode and add
-constexpr int kThreads = kWorkers + 128;   // and a warp for the copies, one for the matrix unit, two for the word between the blocks
-// A worker holds 64 sums and its share of the next stages' codes. The block is launched with 96
+constexpr int kThreads = kWorkers + 128;   // and a warp each for the copies and the matrix unit (two more idle)
+// A worker holds 64 sums and its share of a stage's codes. The block is launched with 96
 // registers a thread (what 640 threads leave of an SM's 65536); the other warps give most of
 // theirs up: 512 * 112 + 128 * 32 = 640 * 96 = 61440.
 constexpr int kWorkerRegs = 112, kOtherRegs = 32;
 constexpr int kSums = kTileK / (kWorkers / 128);  // columns of a worker
-constexpr int kAhead = 4;                  // stages of codes on their way
 constexpr uint32_t kPanel = kRows * 128;   // bytes of 64 columns of a stage
 constexpr uint32_t kBytesA = kBlockN / 64 * kPanel, kBytesB = kBlockK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
 constexpr uint32_t kSquareBytes = 32 * 16 * 4;  // a worker warp's way out
@@ -72,46 +71,68 @@ __device__ __forceinline__ Unit unit_of(const Plan& p, int u) {
 }
 
 struct Shared {
-    uint64_t full_a[kStages], full_b[kStages], empty[kStages], summed[2], last;
-    uint64_t decoded[kStages];  // by this block's workers; full_b of the first block: by both blocks
+    uint64_t full[kStages], added[2];  // of the first block: by both blocks
+    uint64_t empty[kStages], summed[2], last;
     uint32_t tmem;
     int abort;
 };
 
-// The worker's share of a stage of codes: 16 columns of a row. Four lanes take 64 columns of a row,
-// the next four the row after it, then come the other 64 columns, then the other rows: a warp
-// loads four rows of 128 bytes, and eight lanes of a store cover all banks (see store_codes).
+// A stage is decoded by one group of four warps, the next stage by the next group: a group has four
+// stages' time from the wait for its slot to its last store. Of a stage a thread takes 16 columns of
+// four rows. Four lanes take 64 columns of a row, the next four the row after it, then come the other
+// 64 columns, then the other rows: a warp loads four rows of 128 bytes at a time, and eight lanes
+// of a store cover all banks (see store_codes).
+constexpr int kGroups = kWorkers / 128;
+
 struct Codes {
-    uint4 q;
-    uint32_t e;
+    uint4 q[4];
+    uint32_t e[4];
 };
 
-__device__ __forceinline__ int share_row(int tid) { return ((tid >> 2) & 1) + 2 * ((tid >> 4) & 1) + 4 * (tid >> 5); }
+__device__ __forceinline__ int share_row(int tid) { return ((tid >> 2) & 1) + 2 * ((tid >> 4) & 1) + 4 * ((tid >> 5) & 3); }
 __device__ __forceinline__ int share_panel(int tid) { return (tid >> 3) & 1; }
 __device__ __forceinline__ int share_piece(int tid) { return tid & 3; }
 
-// The codes of all stages of all units of this pair, in order. Rows and columns that do not exist
-// are read as ones that do: dY has zeros for such rows, and such columns of dW are not stored. (A
-// marked group may stand in for a row: its column is NaN anyhow.)
+// The codes of a group's stages, of all units of this pair, in order. Rows and columns that do not
+// exist are read as ones that do: dY has zeros for such rows, and such columns of dW are not
+// stored. (A marked group may stand in for a row: its column is NaN anyhow.)
 struct Walk {
-    int unit, at, left;  // next stage to load, of its plane; stages left of the unit
-    uint32_t k;          // column of the values
+    int unit, s, n;  // the next stage is the s-th of the unit's n
+    int at;          // stage of its plane
+    uint32_t k;      // column of the values
 
-    __device__ __forceinline__ void start(const WeightGrad& a, int first_unit, uint32_t rank, int tid) {
-        unit = first_unit, left = 0;
+    __device__ __forceinline__ void enter(const WeightGrad& a, uint32_t rank, int tid) {
         if (unit >= a.plan.units) return;
         const Unit u = unit_of(a.plan, unit);
-        at = u.first % a.plan.stages_per_plane, left = u.stages;
+        n = u.stages;
+        at = (u.first + s) % a.plan.stages_per_plane;
         k = u.tile / a.plan.tiles_n * kTileK + rank * kBlockK + 64 * share_panel(tid) + 16 * share_piece(tid);
         if (k >= a.x.groups * SS_ACT8_GROUP) k = 0;
     }
+    __device__ __forceinline__ void skip_units(const WeightGrad& a, int step, uint32_t rank, int tid) {
+        while (unit < a.plan.units && s >= n) {
+            s -= n;
+            unit += step;
+            enter(a, rank, tid);
+        }
+    }
+    __device__ __forceinline__ void start(const WeightGrad& a, int first_unit, int step, uint32_t rank, int tid) {
+        unit = first_unit, s = tid >> 7, n = 0;
+        enter(a, rank, tid);
+        skip_units(a, step, rank, tid);
+    }
     __device__ __forceinline__ void load(const WeightGrad& a, int step, uint32_t rank, int tid, Codes* c) {
-        if (left == 0) return;
-        const int64_t g = min(at * kRows + share_row(tid), static_cast<int>(a.rows) - 1) * a.x.groups;
-        c->q = *reinterpret_cast<const uint4*>(a.x.values + g * SS_ACT8_GROUP + k);
-        c->e = a.x.exps[g + (k >> 5)];
-        if (++at == a.plan.stages_per_plane) at = 0;  // the next plane goes over the same codes again
-        if (--left == 0) start(a, unit + step, rank, tid);
+        if (unit >= a.plan.units) return;
+        const int last = static_cast<int>(a.rows) - 1, t = at * kRows + share_row(tid);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t g = min(t + 16 * i, last) * a.x.groups;
+            c->q[i] = *reinterpret_cast<const uint4*>(a.x.values + g * SS_ACT8_GROUP + k);
+            c->e[i] = a.x.exps[g + (k >> 5)];
+        }
+        s += kGroups;
+        for (at += kGroups; at >= a.plan.stages_per_plane;) at -= a.plan.stages_per_plane;  // the next plane goes over the same codes again
+        skip_units(a, step, rank, tid);
     }
 };
 
@@ -119,15 +140,19 @@ struct Walk {
 // sits at chunk c ^ (t & 7). Eight lanes write chunks 0, 2, 4, 6 (or 1, 3, 5, 7) of an even row and
 // of the odd one after it, which the exclusive or places on all eight.
 __device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const Codes& c) {
-    const int t = share_row(tid);
+    const int t = share_row(tid);  // 16 rows on t & 7 is the same
     const uint32_t at = stage_b + share_panel(tid) * kPanel + t * 128, chunk = 2 * share_piece(tid);
-    const uint32_t e2 = act8_exponent_pair(c.e);
-    const uint32_t w[4] = {c.q.x, c.q.y, c.q.z, c.q.w};
+    const uint32_t to[2] = {at + ((chunk ^ (t & 7)) << 4), at + (((chunk + 1) ^ (t & 7)) << 4)};
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + h) ^ (t & 7)) << 4)),
-                     "r"(act8_value_pair<0>(w[2 * h], e2)), "r"(act8_value_pair<1>(w[2 * h], e2)),
-                     "r"(act8_value_pair<0>(w[2 * h + 1], e2)), "r"(act8_value_pair<1>(w[2 * h + 1], e2)) : "memory");
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t e2 = act8_exponent_pair(c.e[i]);
+        const uint32_t w[4] = {c.q[i].x, c.q[i].y, c.q[i].z, c.q[i].w};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to[h] + i * 16 * 128),
+                         "r"(act8_value_pair<0>(w[2 * h], e2)), "r"(act8_value_pair<1>(w[2 * h], e2)),
+                         "r"(act8_value_pair<0>(w[2 * h + 1], e2)), "r"(act8_value_pair<1>(w[2 * h + 1], e2)) : "memory");
+    }
 }
 
 // Where 32 rows of a tile go: dW, or the part's own tile.
@@ -216,13 +241,13 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&sh.full_a[s]), 1);
-            mbar_init(smem_addr(&sh.full_b[s]), 2);
-            mbar_init(smem_addr(&sh.decoded[s]), kWorkers / 32);
+            mbar_init(smem_addr(&sh.full[s]), 1 + 2 * kWorkers / 32 / kGroups);
             mbar_init(smem_addr(&sh.empty[s]), 1);
         }
-        mbar_init(smem_addr(&sh.summed[0]), 1);
-        mbar_init(smem_addr(&sh.summed[1]), 1);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_addr(&sh.summed[b]), 1);
+            mbar_init(smem_addr(&sh.added[b]), 2 * kWorkers / 32);
+        }
         mbar_init(smem_addr(&sh.last), 1);
         sh.abort = 0;
         mbar_init_visible();
@@ -236,77 +261,72 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
 
     if (warp < kWorkers / 32) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWorkerRegs));
-        // ---- decoding, and sums of the chunks. A chunk is added while the next one is decoded, after
-        // its first six stages: the last of them goes to the slot of the chunk's last stage, so the
-        // matrix unit has finished the chunk by then, and has six stages ready to work on meanwhile.
+        // ---- decoding, and sums of the chunks. A group adds a chunk (its 64 columns) once it has
+        // decoded its stages of the next one: the last of those goes to a slot that the matrix unit
+        // gave back at the end of the chunk or later, and has six stages to work on meanwhile.
         const int lane = tid & 31, n_local = rank * kBlockN + (warp & 3) * 32, k_local = (warp >> 2) * kSums;
         const uint32_t out = stages + kStages * kStageBytes + warp * kSquareBytes;
         const uint32_t tmem_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + k_local;
         float acc[kSums];
 #pragma unroll
         for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
-        int it = 0, added = 0;          // stages decoded, chunks added
-        int slot = 0, unit = pair, left = 0;  // of the next stage; stages left of the unit
-        uint32_t parity = 1;
+        const int group = warp >> 2;
+        const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0);  // and after them `added`
+        int it = 0, added = 0;          // stages of the chunks so far, chunks added
+        int unit = pair, left = 0;      // of the next chunk; stages left of the unit
         int prev_unit = -1;             // the chunk to add: its unit, and whether it ends it
         bool prev_ends = false, ok = true;
+        int next = group, slot = group; // the group's next stage
+        uint32_t parity = 1;
         Walk walk;
-        Codes codes[kAhead];
-        walk.start(a, pair, rank, tid);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) walk.load(a, pairs, rank, tid, &codes[i]);
+        Codes codes;
+        walk.start(a, pair, pairs, rank, tid);
+        walk.load(a, pairs, rank, tid, &codes);
         while (ok) {
             if (left == 0 && unit < p.units) left = unit_of(p, unit).stages;
             const int len = min(kChunk, left);
-#pragma unroll 1
-            for (int s = 0;; ++s) {
-                if (s == min(kStages, len) && prev_unit >= 0) {
-                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[added & 1]), (added >> 1) & 1, abort));
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t src = tmem_at + (added & 1) * kTileK;
-#pragma unroll
-                    for (int j = 0; j < kSums; j += 16) {
-                        uint32_t r[16];
-                        tmem_load16(src + j, r);
-                        tmem_load_wait();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[j + i] += __uint_as_float(r[i]);
-                    }
-                    tc_fence_before();
-                    ++added;
-                    if (prev_ends) {
-                        const Dest d = dest_of(a, prev_unit, n_local, k_local);
-#pragma unroll
-                        for (int j = 0; j < kSums; j += 16) {
-                            stage_square(out, lane, acc + j);
-                            __syncwarp();
-                            store_square(out, lane, d, j);
-                            __syncwarp();
-                        }
-#pragma unroll
-                        for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
-                    }
-                    prev_unit = -1;
-                }
-                if (s >= len) break;
+            it += len;
+            while (next < it) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.empty[slot]), parity, abort));
                 if (!ok) break;
-                auto decode = [&](Codes* c) {
-                    store_codes(stages + slot * kStageBytes + kBytesA, tid, *c);
-                    walk.load(a, pairs, rank, tid, c);
-                };
-                switch (it & (kAhead - 1)) {
-                    case 0: decode(&codes[0]); break;
-                    case 1: decode(&codes[1]); break;
-                    case 2: decode(&codes[2]); break;
-                    default: decode(&codes[3]); break;
-                }
+                store_codes(stages + slot * kStageBytes + kBytesA, tid, codes);
                 smem_to_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.decoded[slot]));
-                ++it;
-                if (++slot == kStages) slot = 0, parity ^= 1;
+                if (lane == 0) mbar_arrive_pair(full + slot * 8);
+                walk.load(a, pairs, rank, tid, &codes);
+                next += kGroups;
+                slot += kGroups;
+                if (slot >= kStages) slot -= kStages, parity ^= 1;
+            }
+            if (ok && prev_unit >= 0) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[added & 1]), (added >> 1) & 1, abort));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t src = tmem_at + (added & 1) * kTileK;
+#pragma unroll
+                for (int j = 0; j < kSums; j += 16) {
+                    uint32_t r[16];
+                    tmem_load16(src + j, r);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[j + i] += __uint_as_float(r[i]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_pair(full + kStages * 8 + (added & 1) * 8);
+                ++added;
+                if (prev_ends) {
+                    const Dest d = dest_of(a, prev_unit, n_local, k_local);
+#pragma unroll
+                    for (int j = 0; j < kSums; j += 16) {
+                        stage_square(out, lane, acc + j);
+                        __syncwarp();
+                        store_square(out, lane, d, j);
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
+                }
             }
             if (!ok || len == 0) break;
             prev_unit = unit;
@@ -317,26 +337,32 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
         if (!ok) spoil(a, pair, pairs, tid);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        // Roles of one thread each. What bounds them is the fetching of their instructions, between
+        // those of the workers: with separate barriers for copies and codes, descriptors formed at each stage and
+        // waits in line, the matrix unit's thread took 1150 cycles a stage, the unit itself 512.
         if (warp == kWorkers / 32) {
             // ---- copies of dY: this block's half, counted by the first block's barrier
             if ((tid & 31) == 0) {
-                const uint32_t full_a = cluster_addr(smem_addr(&sh.full_a[0]), 0);
+                const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
                 int it = 0, slot = 0;
                 uint32_t parity = 1;
                 bool ok = true;
                 for (int unit = pair; ok && unit < p.units; unit += pairs) {
                     const Unit u = unit_of(p, unit);
                     const int n0 = (u.tile % p.tiles_n) * kTileN + rank * kBlockN;
-                    int plane = u.first / p.stages_per_plane, at = u.first - plane * p.stages_per_plane;
+                    int plane = u.first / p.stages_per_plane, t0 = (u.first - plane * p.stages_per_plane) * kRows;
+                    const int end = p.stages_per_plane * kRows;
 #pragma unroll 1
-                    for (int s = 0; s < u.stages; ++s, ++it) {
-                        ok = mbar_wait(smem_addr(&sh.empty[slot]), parity, abort);
+                    for (int s = 0; s < u.stages; ++s) {
+                        ok = mbar_wait_lean(empty + slot * 8, parity, abort);
                         if (!ok) break;
-                        if (rank == 0) mbar_expect(smem_addr(&sh.full_a[slot]), 2 * kBytesA);
-                        const uint32_t bar = full_a + slot * 8, dst = stages + slot * kStageBytes;
-                        tma_load_3d_pair(dst, &dy_map, bar, n0, at * kRows, plane);
-                        tma_load_3d_pair(dst + kPanel, &dy_map, bar, n0 + 64, at * kRows, plane);
-                        if (++at == p.stages_per_plane) at = 0, ++plane;
+                        const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
+                        if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, 2 * kBytesA);
+                        tma_load_3d_pair(dst, &dy_map, bar, n0, t0, plane);
+                        tma_load_3d_pair(dst + kPanel, &dy_map, bar, n0 + 64, t0, plane);
+                        ++it;
+                        t0 += kRows;
+                        if (t0 == end) t0 = 0, ++plane;
                         if (++slot == kStages) slot = 0, parity ^= 1;
                     }
                 }
@@ -345,56 +371,35 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
                 if (!ok && rank == 0) {  // the copies under way end in the pair's memory: not before they have
                     int own = 0;
                     for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
-                        mbar_wait(smem_addr(&sh.full_a[i % kStages]), (i / kStages) & 1, &own);
-                }
-            }
-        } else if (warp >= kWorkers / 32 + 2) {
-            // ---- word of decoded stages to the first block, by two warps in turn. A release to the
-            // cluster waits for the loads that its thread has under way: the workers have four
-            // stages of codes on their way and would wait for all of them at each stage.
-            if ((tid & 31) == 0) {
-                const uint32_t full_b = cluster_addr(smem_addr(&sh.full_b[0]), 0);
-                int slot = 0, it = 0;
-                uint32_t parity = 0;
-                bool ok = true;
-                for (int unit = pair; ok && unit < p.units; unit += pairs) {
-                    const int n = unit_of(p, unit).stages;
-#pragma unroll 1
-                    for (int s = 0; s < n; ++s, ++it) {
-                        if ((it & 1) == (warp & 1)) {
-                            ok = mbar_wait(smem_addr(&sh.decoded[slot]), parity, abort);
-                            if (!ok) break;
-                            mbar_arrive_cluster(full_b + slot * 8);
-                        }
-                        if (++slot == kStages) slot = 0, parity ^= 1;
-                    }
+                        mbar_wait(smem_addr(&sh.full[i % kStages]), (i / kStages) & 1, &own);
                 }
             }
         } else if (warp == kWorkers / 32 + 1 && rank == 0) {
             // ---- matrix unit
             if ((tid & 31) == 0) {
-                constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK);
-                int it = 0, chunk = 0, slot = 0;
-                uint32_t parity = 0;
+                constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK), kStep = kStageBytes >> 4;
+                const uint64_t desc_a = tc_desc_rows(stages, kPanel), desc_b = tc_desc_rows(stages + kBytesA, kPanel);
+                const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
+                uint32_t slot = 0, parity = 0, chunk = 0;
                 bool ok = true;
                 for (int unit = pair; ok && unit < p.units; unit += pairs) {
-                    const int n = unit_of(p, unit).stages;
+                    for (int left = unit_of(p, unit).stages; ok && left > 0; left -= kChunk, ++chunk) {
+                        const int n = min(left, kChunk);
+                        const uint32_t d = tmem + (chunk & 1) * kTileK;
+                        // the half of the tensor memory is free once the chunk before the last has been added
+                        if (chunk >= 2 && !(ok = mbar_wait_lean(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, abort))) break;
 #pragma unroll 1
-                    for (int s = 0; s < n; ++s, ++it) {
-                        ok = mbar_wait(smem_addr(&sh.full_a[slot]), parity, abort) && mbar_wait(smem_addr(&sh.full_b[slot]), parity, abort);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t at = stages + slot * kStageBytes, d = tmem + (chunk & 1) * kTileK;
+                        for (int s = 0; s < n; ++s) {
+                            ok = mbar_wait_lean(full + slot * 8, parity, abort);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
 #pragma unroll
-                        for (int k = 0; k < kRows / 16; ++k)
-                            tc_mma_bf16_pair(d, tc_desc_rows(at + k * 2048, kPanel), tc_desc_rows(at + kBytesA + k * 2048, kPanel), idesc,
-                                             (s % kChunk) != 0 || k != 0);
-                        tc_commit_pair(smem_addr(&sh.empty[slot]));
-                        if (s % kChunk == kChunk - 1 || s + 1 == n) {
-                            tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
-                            ++chunk;
+                            for (int k = 0; k < kRows / 16; ++k) tc_mma_bf16_pair(d, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, s != 0 || k != 0);
+                            tc_commit_pair(empty + slot * 8);
+                            if (++slot == kStages) slot = 0, parity ^= 1;
                         }
-                        if (++slot == kStages) slot = 0, parity ^= 1;
+                        if (ok) tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
                     }
                 }
                 if (!ok) {  // nothing may still be running when the tensor memory is given back
