@@ -52,11 +52,25 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return false;
 }
 
-// The same for a role of one thread, whose few instructions are fetched anew each time between those of
-// the other warps: only the first try stands in its way.
-static __device__ __noinline__ bool mbar_wait_more(uint32_t bar, uint32_t parity, volatile int* abort) { return mbar_wait(bar, parity, abort); }
-__device__ __forceinline__ bool mbar_wait_lean(uint32_t bar, uint32_t parity, volatile int* abort) {
-    return mbar_try(bar, parity) || mbar_wait_more(bar, parity, abort);
+// The same for a warp whose control flow has to stay uniform: gives no answer. When it gave up, or
+// *abort was up before, its caller goes on; further waits of the block end at once.
+__device__ __forceinline__ void mbar_wait_uniform(uint32_t bar, uint32_t parity, const int* abort) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .u32 n, f;\n\tmov.u32 n, 0;\n"
+        "TRY:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%0], %1;\n\t@p bra DONE;\n\t"
+        "ld.volatile.shared.u32 f, [%2];\n\tsetp.ne.u32 p, f, 0;\n\t@p bra DONE;\n\t"
+        "add.u32 n, n, 1;\n\tsetp.lt.u32 p, n, %3;\n\t@p bra TRY;\n\t"
+        "st.volatile.shared.u32 [%2], 1;\n"
+        "DONE:\n\t}"
+        ::"r"(bar), "r"(parity), "r"(smem_addr(abort)), "n"(kMaxTries) : "memory");
+}
+
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 
 __device__ __forceinline__ void mbar_init_visible() {  // to the copies and the matrix unit too
@@ -72,6 +86,12 @@ __device__ __forceinline__ void smem_to_async() { asm volatile("fence.proxy.asyn
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const void* map, uint32_t bar, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+
+// A box of a matrix to this block's shared memory.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* map, uint32_t bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
 
 // Untiled copy: addresses and size in multiples of 16 bytes.

@@ -25,19 +25,21 @@ namespace {
 constexpr int kTileN = 256, kTileK = 256;  // of dW: n from dY, k from x^
 constexpr int kBlockN = kTileN / 2, kBlockK = kTileK / 2;
 constexpr int kRows = 64;                  // rows of a stage
-constexpr int kStages = 6;
+constexpr int kStages = 5;
+constexpr int kCodeSlots = 6;               // stages of codes, ahead of the decoding
 constexpr int kChunk = 8;                  // stages summed in the matrix unit
-constexpr int kWorkers = 512;              // threads that decode and add
-constexpr int kThreads = kWorkers + 128;   // and a warp each for the copies and the matrix unit (two more idle)
-// A worker holds 64 sums and its share of a stage's codes. The block is launched with 96
-// registers a thread (what 640 threads leave of an SM's 65536); the other warps give most of
-// theirs up: 512 * 112 + 128 * 32 = 640 * 96 = 61440.
-constexpr int kWorkerRegs = 112, kOtherRegs = 32;
-constexpr int kSums = kTileK / (kWorkers / 128);  // columns of a worker
+// Warps 0-7 add, 8-15 decode, 16 and 18 copy, 17 issues the matrix instructions (19 is idle). The
+// block is launched with 96 registers a thread (what 640 threads leave of an SM's 65536) and shares
+// them out again: 256 * 160 + 256 * 64 + 128 * 32 = 640 * 96 = 61440.
+constexpr int kAdders = 256, kDecoders = 256, kThreads = kAdders + kDecoders + 128;
+constexpr int kAdderRegs = 160, kDecoderRegs = 64, kOtherRegs = 32;
+constexpr int kGroups = kDecoders / 128;   // a stage is decoded by four warps
+constexpr int kSums = kTileK / (kAdders / 128);  // columns of an adder
 constexpr uint32_t kPanel = kRows * 128;   // bytes of 64 columns of a stage
 constexpr uint32_t kBytesA = kBlockN / 64 * kPanel, kBytesB = kBlockK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
-constexpr uint32_t kSquareBytes = 32 * 16 * 4;  // a worker warp's way out
-constexpr size_t kSmem = 1024 + kStages * kStageBytes + kWorkers / 32 * kSquareBytes;
+constexpr uint32_t kCodeBytes = kRows * kBlockK;
+constexpr uint32_t kSquareBytes = 32 * 16 * 4;  // an adding warp's way out
+constexpr size_t kSmem = 1024 + kStages * kStageBytes + kCodeSlots * kCodeBytes + kAdders / 32 * kSquareBytes;
 
 struct Plan {
     int tiles_n, tiles_k;   // tiles of dW; tile i: n index i % tiles_n
@@ -73,41 +75,43 @@ __device__ __forceinline__ Unit unit_of(const Plan& p, int u) {
 struct Shared {
     uint64_t full[kStages], added[2];  // of the first block: by both blocks
     uint64_t empty[kStages], summed[2], last;
+    uint64_t codes[kCodeSlots], taken[kCodeSlots];
     uint32_t tmem;
     int abort;
 };
 
-// A stage is decoded by one group of four warps, the next stage by the next group: a group has four
-// stages' time from the wait for its slot to its last store. Of a stage a thread takes 16 columns of
-// four rows. Four lanes take 64 columns of a row, the next four the row after it, then come the other
-// 64 columns, then the other rows: a warp loads four rows of 128 bytes at a time, and eight lanes
-// of a store cover all banks (see store_codes).
-constexpr int kGroups = kWorkers / 128;
-
-struct Codes {
-    uint4 q[4];
-    uint32_t e[4];
-};
-
-__device__ __forceinline__ int share_row(int tid) { return ((tid >> 2) & 1) + 2 * ((tid >> 4) & 1) + 4 * ((tid >> 5) & 3); }
+// A stage is decoded by one group of four warps, the next stage by the other. Its codes come by a
+// copy into a ring of their own, in rows of 128 bytes whose 16-byte chunks are swizzled like the
+// operand's. (Loads to registers a stage ahead, which is all that fits, came too late: a stage took
+// 1300 cycles to decode, twice what its products take.) A thread takes 16 columns of four rows
+// 16 apart. Four lanes take 64 columns of a row t, the next four those of row t ^ 5: so eight lanes
+// of a load (four neighbouring chunks c at c ^ (t & 7)) and of a store (every second chunk) cover all banks.
+__device__ __forceinline__ int share_row(int tid) {
+    const int t = 2 * ((tid >> 4) & 7);
+    return (tid & 4) ? t ^ 5 : t;
+}
 __device__ __forceinline__ int share_panel(int tid) { return (tid >> 3) & 1; }
 __device__ __forceinline__ int share_piece(int tid) { return tid & 3; }
 
-// The codes of a group's stages, of all units of this pair, in order. Rows and columns that do not
-// exist are read as ones that do: dY has zeros for such rows, and such columns of dW are not
-// stored. (A marked group may stand in for a row: its column is NaN anyhow.)
+// The exponents of a group's stages, of all units of this pair, in order. For rows and columns that
+// do not exist others stand in: dY has zeros for such rows, and such columns of dW are not stored.
+// (A marked group may stand in for a row: its column is NaN anyhow.)
+struct Exponents {
+    uint32_t e[4];
+};
+
 struct Walk {
     int unit, s, n;  // the next stage is the s-th of the unit's n
     int at;          // stage of its plane
-    uint32_t k;      // column of the values
+    uint32_t group;  // of columns
 
     __device__ __forceinline__ void enter(const WeightGrad& a, uint32_t rank, int tid) {
         if (unit >= a.plan.units) return;
         const Unit u = unit_of(a.plan, unit);
         n = u.stages;
         at = (u.first + s) % a.plan.stages_per_plane;
-        k = u.tile / a.plan.tiles_n * kTileK + rank * kBlockK + 64 * share_panel(tid) + 16 * share_piece(tid);
-        if (k >= a.x.groups * SS_ACT8_GROUP) k = 0;
+        group = (u.tile / a.plan.tiles_n * kTileK + rank * kBlockK + 64 * share_panel(tid) + 16 * share_piece(tid)) >> 5;
+        if (group >= a.x.groups) group = 0;
     }
     __device__ __forceinline__ void skip_units(const WeightGrad& a, int step, uint32_t rank, int tid) {
         while (unit < a.plan.units && s >= n) {
@@ -116,37 +120,39 @@ struct Walk {
             enter(a, rank, tid);
         }
     }
-    __device__ __forceinline__ void start(const WeightGrad& a, int first_unit, int step, uint32_t rank, int tid) {
-        unit = first_unit, s = tid >> 7, n = 0;
+    __device__ __forceinline__ void start(const WeightGrad& a, int first_unit, int first, int step, uint32_t rank, int tid) {
+        unit = first_unit, s = first, n = 0;
         enter(a, rank, tid);
         skip_units(a, step, rank, tid);
     }
-    __device__ __forceinline__ void load(const WeightGrad& a, int step, uint32_t rank, int tid, Codes* c) {
+    __device__ __forceinline__ void load(const WeightGrad& a, int step, uint32_t rank, int tid, Exponents* x) {
         if (unit >= a.plan.units) return;
         const int last = static_cast<int>(a.rows) - 1, t = at * kRows + share_row(tid);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t g = min(t + 16 * i, last) * a.x.groups;
-            c->q[i] = *reinterpret_cast<const uint4*>(a.x.values + g * SS_ACT8_GROUP + k);
-            c->e[i] = a.x.exps[g + (k >> 5)];
-        }
+        for (int i = 0; i < 4; ++i) x->e[i] = a.x.exps[min(t + 16 * i, last) * a.x.groups + group];
         s += kGroups;
         for (at += kGroups; at >= a.plan.stages_per_plane;) at -= a.plan.stages_per_plane;  // the next plane goes over the same codes again
         skip_units(a, step, rank, tid);
     }
 };
 
-// Decodes them into the stage's operand: column chunk c (8 columns, 16 bytes) of row t of a panel
-// sits at chunk c ^ (t & 7). Eight lanes write chunks 0, 2, 4, 6 (or 1, 3, 5, 7) of an even row and
-// of the odd one after it, which the exclusive or places on all eight.
-__device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const Codes& c) {
-    const int t = share_row(tid);  // 16 rows on t & 7 is the same
+__device__ __forceinline__ void load_codes(uint32_t codes, int tid, uint4 (&q)[4]) {
+    const int t = share_row(tid);
+    const uint32_t at = codes + t * 128 + (((4 * share_panel(tid) + share_piece(tid)) ^ (t & 7)) << 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[i].x), "=r"(q[i].y), "=r"(q[i].z), "=r"(q[i].w) : "r"(at + i * 16 * 128) : "memory");
+}
+
+// To the stage's operand: column chunk c (8 columns, 16 bytes) of row t of a panel sits at chunk c ^ (t & 7).
+__device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const uint4 (&q)[4], const Exponents& x) {
+    const int t = share_row(tid);
     const uint32_t at = stage_b + share_panel(tid) * kPanel + t * 128, chunk = 2 * share_piece(tid);
     const uint32_t to[2] = {at + ((chunk ^ (t & 7)) << 4), at + (((chunk + 1) ^ (t & 7)) << 4)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t e2 = act8_exponent_pair(c.e[i]);
-        const uint32_t w[4] = {c.q[i].x, c.q[i].y, c.q[i].z, c.q[i].w};
+        const uint32_t e2 = act8_exponent_pair(x.e[i]);
+        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to[h] + i * 16 * 128),
@@ -218,7 +224,7 @@ __device__ __noinline__ void spoil(const WeightGrad& a, int pair, int pairs, int
     for (int unit = pair; unit < a.plan.units; unit += pairs) {
         const int tile = unit_of(a.plan, unit).tile;
         const int64_t n0 = static_cast<int64_t>(tile % a.plan.tiles_n) * kTileN, k0 = static_cast<int64_t>(tile / a.plan.tiles_n) * kTileK;
-        for (int i = tid; i < kTileN * kTileK; i += kWorkers) {
+        for (int i = tid; i < kTileN * kTileK; i += kAdders) {
             const int64_t n = n0 + i / kTileK, k = k0 + i % kTileK;
             if (n < a.n_out && k < a.n_in) a.dw[n * a.dw_stride + k] = __uint_as_float(0x7FC00000u);
             if (unit >= a.plan.whole && a.plan.parts > 1)
@@ -228,7 +234,7 @@ __device__ __noinline__ void spoil(const WeightGrad& a, int pair, int pairs, int
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
-weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ WeightGrad a) {
+weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ WeightGrad a) {
     extern __shared__ uint8_t dynamic[];
     __shared__ Shared sh;
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
@@ -241,12 +247,16 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&sh.full[s]), 1 + 2 * kWorkers / 32 / kGroups);
+            mbar_init(smem_addr(&sh.full[s]), 1 + 2 * 4);
             mbar_init(smem_addr(&sh.empty[s]), 1);
+        }
+        for (int c = 0; c < kCodeSlots; ++c) {
+            mbar_init(smem_addr(&sh.codes[c]), 1);
+            mbar_init(smem_addr(&sh.taken[c]), 4);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_addr(&sh.summed[b]), 1);
-            mbar_init(smem_addr(&sh.added[b]), 2 * kWorkers / 32);
+            mbar_init(smem_addr(&sh.added[b]), 2 * kAdders / 32);
         }
         mbar_init(smem_addr(&sh.last), 1);
         sh.abort = 0;
@@ -259,50 +269,25 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
-    if (warp < kWorkers / 32) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWorkerRegs));
-        // ---- decoding, and sums of the chunks. A group adds a chunk (its 64 columns) once it has
-        // decoded its stages of the next one: the last of those goes to a slot that the matrix unit
-        // gave back at the end of the chunk or later, and has six stages to work on meanwhile.
+    if (warp < kAdders / 32) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kAdderRegs));
+        // ---- sums of the chunks: 32 rows of the tile and 128 columns to a warp
         const int lane = tid & 31, n_local = rank * kBlockN + (warp & 3) * 32, k_local = (warp >> 2) * kSums;
-        const uint32_t out = stages + kStages * kStageBytes + warp * kSquareBytes;
+        const uint32_t out = stages + kStages * kStageBytes + kCodeSlots * kCodeBytes + warp * kSquareBytes;
         const uint32_t tmem_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + k_local;
-        float acc[kSums];
+        const uint32_t added = cluster_addr(smem_addr(&sh.added[0]), 0);
+        uint32_t chunk = 0;
+        bool ok = true;
+        for (int unit = pair; ok && unit < p.units; unit += pairs) {
+            float acc[kSums];
 #pragma unroll
-        for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
-        const int group = warp >> 2;
-        const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0);  // and after them `added`
-        int it = 0, added = 0;          // stages of the chunks so far, chunks added
-        int unit = pair, left = 0;      // of the next chunk; stages left of the unit
-        int prev_unit = -1;             // the chunk to add: its unit, and whether it ends it
-        bool prev_ends = false, ok = true;
-        int next = group, slot = group; // the group's next stage
-        uint32_t parity = 1;
-        Walk walk;
-        Codes codes;
-        walk.start(a, pair, pairs, rank, tid);
-        walk.load(a, pairs, rank, tid, &codes);
-        while (ok) {
-            if (left == 0 && unit < p.units) left = unit_of(p, unit).stages;
-            const int len = min(kChunk, left);
-            it += len;
-            while (next < it) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.empty[slot]), parity, abort));
-                if (!ok) break;
-                store_codes(stages + slot * kStageBytes + kBytesA, tid, codes);
-                smem_to_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_pair(full + slot * 8);
-                walk.load(a, pairs, rank, tid, &codes);
-                next += kGroups;
-                slot += kGroups;
-                if (slot >= kStages) slot -= kStages, parity ^= 1;
-            }
-            if (ok && prev_unit >= 0) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[added & 1]), (added >> 1) & 1, abort));
+            for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
+#pragma unroll 1
+            for (int left = unit_of(p, unit).stages; left > 0; left -= kChunk, ++chunk) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t src = tmem_at + (added & 1) * kTileK;
+                const uint32_t src = tmem_at + (chunk & 1) * kTileK;
 #pragma unroll
                 for (int j = 0; j < kSums; j += 16) {
                     uint32_t r[16];
@@ -313,101 +298,159 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_pair(full + kStages * 8 + (added & 1) * 8);
-                ++added;
-                if (prev_ends) {
-                    const Dest d = dest_of(a, prev_unit, n_local, k_local);
-#pragma unroll
-                    for (int j = 0; j < kSums; j += 16) {
-                        stage_square(out, lane, acc + j);
-                        __syncwarp();
-                        store_square(out, lane, d, j);
-                        __syncwarp();
-                    }
-#pragma unroll
-                    for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
-                }
+                if (lane == 0) mbar_arrive_pair(added + (chunk & 1) * 8);
             }
-            if (!ok || len == 0) break;
-            prev_unit = unit;
-            left -= len;
-            prev_ends = left == 0;
-            if (prev_ends) unit += pairs;
+            if (!ok) break;
+            const Dest d = dest_of(a, unit, n_local, k_local);
+#pragma unroll
+            for (int j = 0; j < kSums; j += 16) {
+                stage_square(out, lane, acc + j);
+                __syncwarp();
+                store_square(out, lane, d, j);
+                __syncwarp();
+            }
         }
         if (!ok) spoil(a, pair, pairs, tid);
+    } else if (warp < (kAdders + kDecoders) / 32) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecoderRegs));
+        // ---- decoding: a group's stages, the exponents of the next two on their way
+        const int lane = tid & 31, group = (tid - kAdders) >> 7;
+        const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
+        const uint32_t arrived = smem_addr(&sh.codes[0]), taken = smem_addr(&sh.taken[0]);
+        int total = 0, slot = group, code_slot = group;
+        uint32_t parity = 1, code_parity = 0;
+        for (int unit = pair; unit < p.units; unit += pairs) total += unit_of(p, unit).stages;
+        Walk walk;
+        Exponents exps[2];
+        walk.start(a, pair, group, pairs, rank, tid);
+        walk.load(a, pairs, rank, tid, &exps[0]);
+        walk.load(a, pairs, rank, tid, &exps[1]);
+        bool ok = true;
+        auto decode = [&](Exponents* x) {
+            uint4 q[4];
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(arrived + code_slot * 8, code_parity, abort));
+            if (!ok) return;
+            load_codes(stages + kStages * kStageBytes + code_slot * kCodeBytes, tid, q);
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty + slot * 8, parity, abort));
+            if (!ok) return;
+            store_codes(stages + slot * kStageBytes + kBytesA, tid, q, *x);
+            smem_to_async();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive_pair(full + slot * 8);
+                mbar_arrive(taken + code_slot * 8);
+            }
+            walk.load(a, pairs, rank, tid, x);
+            slot += kGroups;
+            if (slot >= kStages) slot -= kStages, parity ^= 1;
+            code_slot += kGroups;
+            if (code_slot >= kCodeSlots) code_slot -= kCodeSlots, code_parity ^= 1;
+        };
+#pragma unroll 1
+        for (int i = group; ok && i < total; i += 2 * kGroups) {
+            decode(&exps[0]);
+            if (ok && i + kGroups < total) decode(&exps[1]);
+        }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        // Roles of one thread each. What bounds them is the fetching of their instructions, between
-        // those of the workers: with separate barriers for copies and codes, descriptors formed at each stage and
-        // waits in line, the matrix unit's thread took 1150 cycles a stage, the unit itself 512.
-        if (warp == kWorkers / 32) {
+        // Roles of one lane each, but the whole warp walks through them: so addresses and descriptors are formed in
+        // uniform registers, from which the copies and the matrix instructions take them. (A lane that walked alone
+        // took 700 cycles for a stage whose products take 512.)
+        if (warp == (kAdders + kDecoders) / 32) {
             // ---- copies of dY: this block's half, counted by the first block's barrier
-            if ((tid & 31) == 0) {
-                const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
-                int it = 0, slot = 0;
-                uint32_t parity = 1;
-                bool ok = true;
-                for (int unit = pair; ok && unit < p.units; unit += pairs) {
-                    const Unit u = unit_of(p, unit);
-                    const int n0 = (u.tile % p.tiles_n) * kTileN + rank * kBlockN;
-                    int plane = u.first / p.stages_per_plane, t0 = (u.first - plane * p.stages_per_plane) * kRows;
-                    const int end = p.stages_per_plane * kRows;
+            const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
+            const bool leader = elect_one();
+            int it = 0, slot = 0;
+            uint32_t parity = 1;
+            for (int unit = pair; unit < p.units; unit += pairs) {
+                const Unit u = unit_of(p, unit);
+                const int n0 = (u.tile % p.tiles_n) * kTileN + rank * kBlockN;
+                int plane = u.first / p.stages_per_plane, t0 = (u.first - plane * p.stages_per_plane) * kRows;
+                const int end = p.stages_per_plane * kRows;
 #pragma unroll 1
-                    for (int s = 0; s < u.stages; ++s) {
-                        ok = mbar_wait_lean(empty + slot * 8, parity, abort);
-                        if (!ok) break;
-                        const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
+                for (int s = 0; s < u.stages; ++s) {
+                    mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
+                    const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
+                    if (leader) {
                         if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, 2 * kBytesA);
                         tma_load_3d_pair(dst, &dy_map, bar, n0, t0, plane);
                         tma_load_3d_pair(dst + kPanel, &dy_map, bar, n0 + 64, t0, plane);
-                        ++it;
-                        t0 += kRows;
-                        if (t0 == end) t0 = 0, ++plane;
-                        if (++slot == kStages) slot = 0, parity ^= 1;
                     }
-                }
-                for (int i = it > kStages ? it - kStages : 0; ok && i < it; ++i)  // the last signals arrive in this block's memory
-                    ok = mbar_wait(smem_addr(&sh.empty[i % kStages]), (i / kStages) & 1, abort);
-                if (!ok && rank == 0) {  // the copies under way end in the pair's memory: not before they have
-                    int own = 0;
-                    for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
-                        mbar_wait(smem_addr(&sh.full[i % kStages]), (i / kStages) & 1, &own);
+                    ++it;
+                    t0 += kRows;
+                    if (t0 == end) t0 = 0, ++plane;
+                    if (++slot == kStages) slot = 0, parity ^= 1;
                 }
             }
-        } else if (warp == kWorkers / 32 + 1 && rank == 0) {
-            // ---- matrix unit
-            if ((tid & 31) == 0) {
-                constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK), kStep = kStageBytes >> 4;
-                const uint64_t desc_a = tc_desc_rows(stages, kPanel), desc_b = tc_desc_rows(stages + kBytesA, kPanel);
-                const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
-                uint32_t slot = 0, parity = 0, chunk = 0;
-                bool ok = true;
-                for (int unit = pair; ok && unit < p.units; unit += pairs) {
-                    for (int left = unit_of(p, unit).stages; ok && left > 0; left -= kChunk, ++chunk) {
-                        const int n = min(left, kChunk);
-                        const uint32_t d = tmem + (chunk & 1) * kTileK;
-                        // the half of the tensor memory is free once the chunk before the last has been added
-                        if (chunk >= 2 && !(ok = mbar_wait_lean(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, abort))) break;
+            // the last signals, and copies, arrive in this block's memory: not before that
+            const int from = it > kStages ? it - kStages : 0;
+            for (int i = from; i < it; ++i) mbar_wait_uniform(empty + i % kStages * 8, (i / kStages) & 1, &sh.abort);
+            if (*abort != 0 && rank == 0) {
+                int own = 0;
+                for (int i = from; i < it; ++i) mbar_wait(smem_addr(&sh.full[i % kStages]), (i / kStages) & 1, &own);
+            }
+        } else if (warp == (kAdders + kDecoders) / 32 + 2) {
+            // ---- copies of the codes: this block's half
+            const uint32_t arrived = smem_addr(&sh.codes[0]), taken = smem_addr(&sh.taken[0]);
+            const bool leader = elect_one();
+            int it = 0, slot = 0;
+            uint32_t parity = 1;
+            for (int unit = pair; unit < p.units; unit += pairs) {
+                const Unit u = unit_of(p, unit);
+                const int k0 = u.tile / p.tiles_n * kTileK + rank * kBlockK, end = p.stages_per_plane * kRows;
+                int t0 = u.first % p.stages_per_plane * kRows;
 #pragma unroll 1
-                        for (int s = 0; s < n; ++s) {
-                            ok = mbar_wait_lean(full + slot * 8, parity, abort);
-                            if (!ok) break;
-                            tc_fence_after();
-                            const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
+                for (int s = 0; s < u.stages; ++s) {
+                    mbar_wait_uniform(taken + slot * 8, parity, &sh.abort);
+                    if (leader) {
+                        mbar_expect(arrived + slot * 8, kCodeBytes);
+                        tma_load_2d(stages + kStages * kStageBytes + slot * kCodeBytes, &x_map, arrived + slot * 8, k0, t0);
+                    }
+                    ++it;
+                    t0 += kRows;
+                    if (t0 == end) t0 = 0;
+                    if (++slot == kCodeSlots) slot = 0, parity ^= 1;
+                }
+            }
+            if (*abort != 0) {
+                int own = 0;
+                for (int i = it > kCodeSlots ? it - kCodeSlots : 0; i < it; ++i)
+                    mbar_wait(smem_addr(&sh.codes[i % kCodeSlots]), (i / kCodeSlots) & 1, &own);
+            }
+        } else if (warp == (kAdders + kDecoders) / 32 + 1 && rank == 0) {
+            // ---- matrix unit
+            constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK), kStep = kStageBytes >> 4;
+            const uint64_t desc_a = tc_desc_rows(stages, kPanel), desc_b = tc_desc_rows(stages + kBytesA, kPanel);
+            const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
+            const bool leader = elect_one();
+            uint32_t slot = 0, parity = 0, chunk = 0;
+            for (int unit = pair; unit < p.units; unit += pairs) {
+                for (int left = unit_of(p, unit).stages; left > 0; left -= kChunk, ++chunk) {
+                    const int n = min(left, kChunk);
+                    const uint32_t d = tmem + (chunk & 1) * kTileK;
+                    // the half of the tensor memory is free once the chunk before the last has been added
+                    if (chunk >= 2) mbar_wait_uniform(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, &sh.abort);
+#pragma unroll 1
+                    for (int s = 0; s < n; ++s) {
+                        mbar_wait_uniform(full + slot * 8, parity, &sh.abort);
+                        tc_fence_after();
+                        const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
+                        if (leader) {
 #pragma unroll
                             for (int k = 0; k < kRows / 16; ++k) tc_mma_bf16_pair(d, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, s != 0 || k != 0);
                             tc_commit_pair(empty + slot * 8);
-                            if (++slot == kStages) slot = 0, parity ^= 1;
                         }
-                        if (ok) tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
+                        __syncwarp();
+                        if (++slot == kStages) slot = 0, parity ^= 1;
                     }
-                }
-                if (!ok) {  // nothing may still be running when the tensor memory is given back
-                    int own = 0;
-                    tc_commit_pair(smem_addr(&sh.last));
-                    mbar_wait(smem_addr(&sh.last), 0, &own);
+                    if (leader) tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
+                    __syncwarp();
                 }
             }
+            // nothing may still be running when the tensor memory is given back
+            int own = 0;
+            if (leader) tc_commit_pair(smem_addr(&sh.last));
+            mbar_wait(smem_addr(&sh.last), 0, &own);
         }
     }
     // neither block leaves while the other may still signal to it or use its operands
@@ -594,6 +637,13 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, src, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return SS_ERR_UNSUPPORTED;
+    CUtensorMap x_map;
+    const cuuint64_t pitch = static_cast<cuuint64_t>(act8_groups(n_in)) * SS_ACT8_GROUP;
+    const cuuint64_t x_dims[2] = {pitch, static_cast<cuuint64_t>(rows)};
+    const cuuint32_t x_box[2] = {kBlockK, kRows};
+    if (encode(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(ckpt_x), x_dims, &pitch, x_box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return SS_ERR_UNSUPPORTED;
     e = cudaFuncSetAttribute(weight_grad8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
     if (e != cudaSuccess) return cuda_status_public(e);
 
@@ -615,7 +665,7 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     at.val.clusterDim.x = 2, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, weight_grad8_kernel, map, a);
+    e = cudaLaunchKernelEx(&cfg, weight_grad8_kernel, map, x_map, a);
     if (e != cudaSuccess) return cuda_status_public(e);
     if (l.plan.parts > 1) {
         const unsigned others = static_cast<unsigned>(l.plan.tiles_n * l.plan.tiles_k - l.plan.whole);
