@@ -5,10 +5,10 @@
 // decoded by eight warps from the 8-bit codes straight into the swizzled operand layout. A decoded
 // value has 7 significant bits and is exact in bf16; no operand is rounded.
 //
-// Sums. The matrix unit adds into fp32 with truncation: measured with inputs of mean 0, its sums
-// come out low by 1e-9 of their size for each row (1.9e-5 for 16384 rows). So a tile is summed
-// there over 512 rows at a time, in one half of the tensor memory, and the eight warps add that
-// to fp32 registers, rounding to nearest, while the matrix unit fills the other half: 5e-7.
+// Sums. The matrix unit adds into fp32 with truncation: of a product with inputs of mean 0 over 16384
+// rows that it sums alone, 1.9e-5 is lost. So a tile is summed there over 2048 rows at a time, in
+// one half of the tensor memory, and added to dW, rounded to nearest, while the matrix unit fills the other half:
+// 4.5e-7 (512 rows: 1.3e-7, 1024: 2.1e-7; an fp32 product of the same: 5.1e-7).
 #include <cuda.h>
 
 #include <atomic>
@@ -27,18 +27,16 @@ constexpr int kBlockN = kTileN / 2, kBlockK = kTileK / 2;
 constexpr int kRows = 64;                  // rows of a stage
 constexpr int kStages = 5;
 constexpr int kCodeSlots = 6;               // stages of codes, ahead of the decoding
-constexpr int kChunk = 8;                  // stages summed in the matrix unit
-// Warps 0-7 add, 8-15 decode, 16 and 18 copy, 17 issues the matrix instructions (19 is idle). The
-// block is launched with 96 registers a thread (what 640 threads leave of an SM's 65536) and shares
-// them out again: 256 * 160 + 256 * 64 + 128 * 32 = 640 * 96 = 61440.
-constexpr int kAdders = 256, kDecoders = 256, kThreads = kAdders + kDecoders + 128;
-constexpr int kAdderRegs = 160, kDecoderRegs = 64, kOtherRegs = 32;
+static_assert(kCodeSlots > kStages, "see the waits of the decoding warps");
+constexpr int kChunk = 32;                 // stages summed in the matrix unit
+constexpr int kLeastPart = 8;              // stages of a part
+// Warps 0-3 bring the sums out, 4-19 decode, 20 and 22 copy, 21 issues the matrix instructions (23 is idle).
+constexpr int kAdders = 128, kDecoders = 512, kThreads = kAdders + kDecoders + 128;
 constexpr int kGroups = kDecoders / 128;   // a stage is decoded by four warps
-constexpr int kSums = kTileK / (kAdders / 128);  // columns of an adder
 constexpr uint32_t kPanel = kRows * 128;   // bytes of 64 columns of a stage
 constexpr uint32_t kBytesA = kBlockN / 64 * kPanel, kBytesB = kBlockK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
 constexpr uint32_t kCodeBytes = kRows * kBlockK;
-constexpr uint32_t kSquareBytes = 32 * 16 * 4;  // an adding warp's way out
+constexpr uint32_t kSquareBytes = 32 * 32 * 4;  // an adding warp's way out
 constexpr size_t kSmem = 1024 + kStages * kStageBytes + kCodeSlots * kCodeBytes + kAdders / 32 * kSquareBytes;
 
 struct Plan {
@@ -80,7 +78,7 @@ struct Shared {
     int abort;
 };
 
-// A stage is decoded by one group of four warps, the next stage by the other. Its codes come by a
+// A stage is decoded by one group of four warps, the next stage by the next of four groups. Its codes come by a
 // copy into a ring of their own, in rows of 128 bytes whose 16-byte chunks are swizzled like the
 // operand's. (Loads to registers a stage ahead, which is all that fits, came too late: a stage took
 // 1300 cycles to decode, twice what its products take.) A thread takes 16 columns of four rows
@@ -181,40 +179,39 @@ __device__ __forceinline__ Dest dest_of(const WeightGrad& a, int unit, int n_loc
                 static_cast<int>(min(a.n_in - k, static_cast<int64_t>(kTileK))), a.accumulate != 0};
 }
 
-// 32 x 16 sums, a row a lane, through the warp's own shared memory so that each row is written by
-// neighbouring lanes. 16-byte chunk c of row r is kept at chunk c ^ (r / 2 mod 4).
-__device__ __forceinline__ void stage_square(uint32_t buf, int lane, const float* v) {
+// 32 x 32 sums, a row a lane, through the warp's own shared memory so that each row is written by
+// neighbouring lanes. 16-byte chunk c of row r is kept at chunk c ^ (r & 7).
+__device__ __forceinline__ void stage_square(uint32_t buf, int lane, const uint32_t* v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)), "f"(v[4 * i]),
-                     "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
+    for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]),
+                     "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
 }
 
-__device__ __forceinline__ void store_square(uint32_t buf, int lane, const Dest& d, int col) {
-    if (col + 16 <= d.cols && (reinterpret_cast<uintptr_t>(d.p) & 15) == 0 && (d.stride & 3) == 0) {
-        const int chunk = lane & 3;
-#pragma unroll 2
-        for (int r = lane >> 2; r < 32; r += 8) {
-            if (r >= d.rows) break;
+// Written, or (`add`) added by the memory itself: nothing is read back, and as the same lane writes an
+// element of the tile each time, its sums come in their order.
+__device__ __forceinline__ void store_square(uint32_t buf, int lane, const Dest& d, int col, bool add) {
+    if (col + 32 <= d.cols && (reinterpret_cast<uintptr_t>(d.p) & 15) == 0 && (d.stride & 3) == 0) {
+        const int chunk = lane & 7;
+#pragma unroll 4
+        for (int i = 0; i < 8; ++i) {
+            const int r = (lane >> 3) + 4 * i;
             float4 v;
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                         : "r"(buf + r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4)) : "memory");
-            float4* p = reinterpret_cast<float4*>(d.p + r * d.stride + col + 4 * chunk);
-            if (d.add) {
-                const float4 o = *p;
-                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-            }
-            *p = v;
+                         : "r"(buf + r * 128 + ((chunk ^ (r & 7)) << 4)) : "memory");
+            if (r >= d.rows) continue;
+            float* p = d.p + r * d.stride + col + 4 * chunk;
+            if (add) asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(__cvta_generic_to_global(p)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+            else *reinterpret_cast<float4*>(p) = v;
         }
-    } else {
-        const int c = lane & 15;
-        if (col + c >= d.cols) return;
+    } else if (col + lane < d.cols) {
 #pragma unroll 2
-        for (int r = lane >> 4; r < min(32, d.rows); r += 2) {
+        for (int r = 0; r < min(32, d.rows); ++r) {
             float v;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(buf + r * 64 + (((c >> 2) ^ ((r >> 1) & 3)) << 4) + (c & 3) * 4) : "memory");
-            float* p = d.p + r * d.stride + col + c;
-            *p = d.add ? *p + v : v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+            float* p = d.p + r * d.stride + col + lane;
+            if (add) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(__cvta_generic_to_global(p)), "f"(v) : "memory");
+            else *p = v;
         }
     }
 }
@@ -270,49 +267,39 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
     const uint32_t tmem = sh.tmem;
 
     if (warp < kAdders / 32) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kAdderRegs));
-        // ---- sums of the chunks: 32 rows of the tile and 128 columns to a warp
-        const int lane = tid & 31, n_local = rank * kBlockN + (warp & 3) * 32, k_local = (warp >> 2) * kSums;
+        // ---- sums of the chunks, to dW: 32 rows of the tile to a warp
+        const int lane = tid & 31, n_local = rank * kBlockN + warp * 32;
         const uint32_t out = stages + kStages * kStageBytes + kCodeSlots * kCodeBytes + warp * kSquareBytes;
-        const uint32_t tmem_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + k_local;
+        const uint32_t tmem_at = tmem + (static_cast<uint32_t>(warp * 32) << 16);
         const uint32_t added = cluster_addr(smem_addr(&sh.added[0]), 0);
         uint32_t chunk = 0;
         bool ok = true;
         for (int unit = pair; ok && unit < p.units; unit += pairs) {
-            float acc[kSums];
-#pragma unroll
-            for (int j = 0; j < kSums; ++j) acc[j] = 0.0f;
-#pragma unroll 1
+            const Dest d = dest_of(a, unit, n_local, 0);
+            bool add = d.add;
             for (int left = unit_of(p, unit).stages; left > 0; left -= kChunk, ++chunk) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t src = tmem_at + (chunk & 1) * kTileK;
-#pragma unroll
-                for (int j = 0; j < kSums; j += 16) {
-                    uint32_t r[16];
-                    tmem_load16(src + j, r);
+#pragma unroll 1
+                for (int j = 0; j < kTileK; j += 32) {
+                    uint32_t r[32];
+                    tmem_load32(src + j, r);
                     tmem_load_wait();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[j + i] += __uint_as_float(r[i]);
+                    stage_square(out, lane, r);
+                    __syncwarp();
+                    store_square(out, lane, d, j, add);
+                    __syncwarp();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_pair(added + (chunk & 1) * 8);
-            }
-            if (!ok) break;
-            const Dest d = dest_of(a, unit, n_local, k_local);
-#pragma unroll
-            for (int j = 0; j < kSums; j += 16) {
-                stage_square(out, lane, acc + j);
-                __syncwarp();
-                store_square(out, lane, d, j);
-                __syncwarp();
+                add = true;
             }
         }
         if (!ok) spoil(a, pair, pairs, tid);
     } else if (warp < (kAdders + kDecoders) / 32) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecoderRegs));
         // ---- decoding: a group's stages, the exponents of the next two on their way
         const int lane = tid & 31, group = (tid - kAdders) >> 7;
         const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
@@ -328,11 +315,13 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
         bool ok = true;
         auto decode = [&](Exponents* x) {
             uint4 q[4];
+            // In this order: the slot is free once the stage five before has been used, so the codes of the stage six before have
+            // come, and the wait for this stage's cannot take their arrival for one it has not seen yet.
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty + slot * 8, parity, abort));
+            if (!ok) return;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(arrived + code_slot * 8, code_parity, abort));
             if (!ok) return;
             load_codes(stages + kStages * kStageBytes + code_slot * kCodeBytes, tid, q);
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty + slot * 8, parity, abort));
-            if (!ok) return;
             store_codes(stages + slot * kStageBytes + kBytesA, tid, q, *x);
             smem_to_async();
             __syncwarp();
@@ -352,7 +341,6 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
             if (ok && i + kGroups < total) decode(&exps[1]);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         // Roles of one lane each, but the whole warp walks through them: so addresses and descriptors are formed in
         // uniform registers, from which the copies and the matrix instructions take them. (A lane that walked alone
         // took 700 cycles for a stage whose products take 512.)
@@ -539,10 +527,9 @@ int layout_of(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int6
     p.part_stages = all;
     if (others > 0) {
         int parts = pairs / others;
-        if (parts > all / kChunk) parts = all / kChunk;  // a part is at least one chunk
+        if (parts > all / kLeastPart) parts = all / kLeastPart;
         if (parts > 1) {
-            const int chunks = (all + kChunk - 1) / kChunk;
-            p.part_stages = (chunks + parts - 1) / parts * kChunk;
+            p.part_stages = (all + parts - 1) / parts;
             p.parts = (all + p.part_stages - 1) / p.part_stages;
         }
     }
