@@ -182,25 +182,27 @@ __device__ __forceinline__ Dest dest_of(const WeightGrad& a, int unit, int n_loc
 // 32 x 32 sums, a row a lane, through the warp's own shared memory so that each row is written by
 // neighbouring lanes. 16-byte chunk c of row r is kept at chunk c ^ (r & 7).
 __device__ __forceinline__ void stage_square(uint32_t buf, int lane, const uint32_t* v) {
+    const uint32_t at = buf + lane * 128 + ((lane & 7) << 4);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]),
-                     "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at ^ (i << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
 }
 
-// Written, or (`add`) added by the memory itself: nothing is read back, and as the same lane writes an
-// element of the tile each time, its sums come in their order.
-__device__ __forceinline__ void store_square(uint32_t buf, int lane, const Dest& d, int col, bool add) {
-    if (col + 32 <= d.cols && (reinterpret_cast<uintptr_t>(d.p) & 15) == 0 && (d.stride & 3) == 0) {
-        const int chunk = lane & 7;
-#pragma unroll 4
-        for (int i = 0; i < 8; ++i) {
-            const int r = (lane >> 3) + 4 * i;
+// Written, or (`add`) added by the memory itself: nothing is read back, and as the same lane writes
+// an element of the tile each time, its sums come in their order. `row`: the lane's first row of the
+// fast form, at its chunk; `step`: bytes of four rows.
+__device__ __forceinline__ void store_square(uint32_t buf, int lane, const Dest& d, int col, bool add, bool vectors, char* row, int64_t step) {
+    if (vectors && col + 32 <= d.cols) {
+        const int first = lane >> 3;
+        const uint32_t at = buf + first * 128 + (((lane & 7) ^ first) << 4);
+        char* p = row + col * 4;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, p += step) {
             float4 v;
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                         : "r"(buf + r * 128 + ((chunk ^ (r & 7)) << 4)) : "memory");
-            if (r >= d.rows) continue;
-            float* p = d.p + r * d.stride + col + 4 * chunk;
+                         : "r"((at ^ ((i & 1) << 6)) + i * 512) : "memory");
+            if (first + 4 * i >= d.rows) continue;
             if (add) asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(__cvta_generic_to_global(p)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
             else *reinterpret_cast<float4*>(p) = v;
         }
@@ -276,6 +278,8 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
         bool ok = true;
         for (int unit = pair; ok && unit < p.units; unit += pairs) {
             const Dest d = dest_of(a, unit, n_local, 0);
+            const bool vectors = (reinterpret_cast<uintptr_t>(d.p) & 15) == 0 && (d.stride & 3) == 0;
+            char* const row = reinterpret_cast<char*>(d.p + (lane >> 3) * d.stride + 4 * (lane & 7));
             bool add = d.add;
             for (int left = unit_of(p, unit).stages; left > 0; left -= kChunk, ++chunk) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
@@ -289,7 +293,7 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
                     tmem_load_wait();
                     stage_square(out, lane, r);
                     __syncwarp();
-                    store_square(out, lane, d, j, add);
+                    store_square(out, lane, d, j, add, vectors, row, d.stride * 16);
                     __syncwarp();
                 }
                 tc_fence_before();
