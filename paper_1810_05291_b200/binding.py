@@ -13,6 +13,7 @@ signs and votes ``int32`` (bit pattern of the uint32 words), ``ceil(d/32)`` of t
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -173,9 +174,9 @@ def _ptr_array(ptrs: Sequence[int]):
     return (ctypes.c_void_p * len(ptrs))(*ptrs)
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+def _stream(stream):
+    if stream is None:  # the handle alone: a Stream object costs as much as a launch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -503,9 +504,9 @@ def _mat(t: torch.Tensor, dtype, name: str, shape=None):
 
 
 def _vec(t: torch.Tensor, dtype, name: str, n: int) -> int:
-    if t.dtype != dtype or not t.is_cuda or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise (TypeError if t.dtype != dtype else ValueError)("%s must be a contiguous CUDA tensor of %d %s" % (name, n, dtype))
-    return t.data_ptr()
+    if t.dtype is dtype and t.is_cuda and t.dim() == 1 and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    raise (ValueError if t.dtype is dtype else TypeError)("%s must be a contiguous CUDA tensor of %d %s" % (name, n, dtype))
 
 
 def _opt_vec(t: Optional[torch.Tensor], dtype, name: str, n: int) -> Optional[int]:
@@ -513,12 +514,16 @@ def _opt_vec(t: Optional[torch.Tensor], dtype, name: str, n: int) -> Optional[in
 
 
 def _scratch(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor):
-    """The caller's workspace, or one of the size asked for from PyTorch's allocator."""
+    """(address, bytes) of the caller's workspace, or of one of the size asked for from PyTorch's
+    allocator, and the tensor to keep until the call returns (its memory is safe after that: it is
+    given out again in the order of the stream)."""
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        if need <= 0:
+            return None, 0, None
+        workspace = like.new_empty(need, dtype=torch.uint8)
     elif not workspace.is_cuda or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA uint8 tensor")
-    return workspace
+    return workspace.data_ptr(), workspace.numel(), workspace
 
 
 def ss_act8_bytes(rows: int, cols: int) -> int:
@@ -589,14 +594,13 @@ def ss_weight_grad8(dy: torch.Tensor, ckpt_x: torch.Tensor, dw: torch.Tensor, ac
         raise ValueError("dw must have one row for each of dy's %d columns" % n_out)
     n_in = dw.shape[1]
     L = lib()
-    if workspace is None:
-        need = L.ss_weight_grad8_workspace(dy_ptr, dy_stride, code, rows, n_out, n_in)
-        workspace = _scratch(None, max(need, 0), dy) if need else None
-    w_ptr, w_bytes = (None, 0) if workspace is None else (_scratch(workspace, 0, dy).data_ptr(), workspace.numel())
+    need = 0 if workspace is not None else L.ss_weight_grad8_workspace(dy_ptr, dy_stride, code, rows, n_out, n_in)
+    w_ptr, w_bytes, workspace = _scratch(workspace, need, dy)
     _check(L.ss_weight_grad8(dy_ptr, dy_stride, code, _ckpt(ckpt_x, rows, n_in, "ckpt_x"), rows, n_out, n_in, dw_ptr,
                              dw_stride, int(bool(accumulate)), w_ptr, w_bytes, _stream(stream)), "ss_weight_grad8")
 
 
+@functools.lru_cache(maxsize=256)
 def ss_loss_workspace(rows: int, n_pairs: int = 0) -> int:
     return int(lib().ss_loss_workspace(int(rows), int(n_pairs)))
 
@@ -612,13 +616,13 @@ def ss_policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.
     rows, vocab = logits.shape
     d_ptr, d_stride = (None, 0) if dlogits is None else _mat(dlogits, logits.dtype, "dlogits", logits.shape)
     L = lib()
-    ws = _scratch(workspace, 0 if workspace is not None else L.ss_loss_workspace(rows, 0), logits)
+    w_ptr, w_bytes, workspace = _scratch(workspace, ss_loss_workspace(rows, 0), logits)
     _check(L.ss_policy_loss(z_ptr, z_stride, code, rows, vocab, _vec(targets, torch.int64, "targets", rows),
                             _vec(old_logp, f32, "old_logp", rows), _opt_vec(ref_logp, f32, "ref_logp", rows),
                             _vec(advantages, f32, "advantages", rows), _vec(weights, f32, "weights", rows),
                             inv_temperature, clip_low, clip_high, kl_coef, _opt_vec(grad_scale, f32, "grad_scale", 1),
                             _vec(totals, f32, "totals", 3), _vec(logp, f32, "logp", rows), d_ptr, d_stride,
-                            ws.data_ptr(), ws.numel(), _stream(stream)), "ss_policy_loss")
+                            w_ptr, w_bytes, _stream(stream)), "ss_policy_loss")
 
 
 def ss_preference_loss(logits: torch.Tensor, targets: torch.Tensor, weights: torch.Tensor, seq_begin: torch.Tensor,
@@ -633,11 +637,11 @@ def ss_preference_loss(logits: torch.Tensor, targets: torch.Tensor, weights: tor
     pairs = margins.shape[0]
     d_ptr, d_stride = (None, 0) if dlogits is None else _mat(dlogits, logits.dtype, "dlogits", logits.shape)
     L = lib()
-    ws = _scratch(workspace, 0 if workspace is not None else L.ss_loss_workspace(rows, pairs), logits)
+    w_ptr, w_bytes, workspace = _scratch(workspace, ss_loss_workspace(rows, pairs), logits)
     _check(L.ss_preference_loss(z_ptr, z_stride, code, rows, vocab, _vec(targets, i64, "targets", rows),
                                 _vec(weights, f32, "weights", rows), _vec(seq_begin, i64, "seq_begin", 2 * pairs + 1),
                                 pairs, _vec(ref_seq_logp, f32, "ref_seq_logp", 2 * pairs), inv_temperature, kind, beta,
                                 label_smoothing, scale, _opt_vec(grad_scale, f32, "grad_scale", 1),
                                 _vec(loss, f32, "loss", 1), _vec(margins, f32, "margins", pairs),
                                 _vec(seq_logp, f32, "seq_logp", 2 * pairs), _vec(logp, f32, "logp", rows), d_ptr,
-                                d_stride, ws.data_ptr(), ws.numel(), _stream(stream)), "ss_preference_loss")
+                                d_stride, w_ptr, w_bytes, _stream(stream)), "ss_preference_loss")

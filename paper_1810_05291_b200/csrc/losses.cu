@@ -573,13 +573,13 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
     return v;
 }
 
-__global__ void __launch_bounds__(kSumThreads) totals_kernel(const float* terms, int64_t n, double scale, float* out) {
+__global__ void __launch_bounds__(kSumThreads) totals_kernel(const float* terms, int64_t n, float* out) {
     __shared__ double shared[32];
     const float* x = terms + blockIdx.x * n;
     double v = 0.0;
     for (int64_t i = threadIdx.x; i < n; i += kSumThreads) v += x[i];
     v = block_sum(v, shared);
-    if (threadIdx.x == 0) out[blockIdx.x] = static_cast<float>(scale * v);
+    if (threadIdx.x == 0) out[blockIdx.x] = static_cast<float>(v);
 }
 
 // ---- preference loss: statistics of every row, then every pair's coefficient, then the gradient -----
@@ -668,9 +668,29 @@ __global__ void __launch_bounds__(kSumThreads) pair_kernel(const __grid_constant
         }
 }
 
+// Loss from the pairs' losses, by one warp in a fixed order.
+struct Total {
+    const float* pair_loss;
+    int64_t pairs;
+    double scale;
+    float* loss;
+
+    __device__ __forceinline__ void write() const {
+        double v = 0.0;
+        for (int64_t i = threadIdx.x & 31; i < pairs; i += 32) v += pair_loss[i];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        if ((threadIdx.x & 31) == 0) *loss = static_cast<float>(scale * v);
+    }
+};
+
+__global__ void __launch_bounds__(32) total_kernel(const __grid_constant__ Total total) { total.write(); }
+
 // In the order opposite to the statistics', so that it begins with the rows that the caches still hold.
+// The first warp of the last block also writes the loss.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(block_of<THREADS>()) row_grad_kernel(const __grid_constant__ Logits a, Rows r, int64_t rows) {
+__global__ void __launch_bounds__(block_of<THREADS>()) row_grad_kernel(const __grid_constant__ Logits a, Rows r, int64_t rows, const __grid_constant__ Total total) {
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x < 32) total.write();
     const int64_t row = rows - 1 - (static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS);
     const int t = threadIdx.x % THREADS;
     if (row < 0) return;
@@ -717,7 +737,11 @@ int cluster_of(int64_t rows, int64_t vectors, int sms) {
 }
 
 template <typename T, int HELD>
+struct SliceKernel {};
+
+template <typename T, int HELD>
 cudaError_t launch_slices(const Logits& a, const Policy& p, int64_t rows, int64_t vectors, int size, int sms, cudaStream_t st) {
+    constexpr int kSliceSmem = kSliceVectors<T, HELD> * 16 * kSliceSlots<T>;
     Slices c{rows, 1, static_cast<int>((vectors + size - 1) / size)};
     // as many rows to a cluster as leave three rounds of blocks for every SM
     const int64_t count = rows * size / (3 * kSliceBlocks<HELD> * sms);
@@ -732,7 +756,7 @@ cudaError_t launch_slices(const Logits& a, const Policy& p, int64_t rows, int64_
     at.val.clusterDim.x = size, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaFuncSetAttribute(policy_slice_kernel<T, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(cfg.dynamicSmemBytes));
+    const cudaError_t e = allow_shared<SliceKernel<T, HELD>>(reinterpret_cast<const void*>(policy_slice_kernel<T, HELD>), kSliceSmem);
     return e != cudaSuccess ? e : cudaLaunchKernelEx(&cfg, policy_slice_kernel<T, HELD>, a, p, c);
 }
 
@@ -832,7 +856,7 @@ int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64
             });
         }
     }
-    totals_kernel<<<3, kSumThreads, 0, st>>>(p.terms, rows, 1.0, totals);
+    totals_kernel<<<3, kSumThreads, 0, st>>>(p.terms, rows, totals);
     return cuda_status_public(cudaGetLastError());
 }
 
@@ -872,10 +896,12 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
         });
     }
     if (n_pairs > 0) pair_kernel<<<static_cast<unsigned>(n_pairs), kSumThreads, 0, st>>>(a, p, r);
-    totals_kernel<<<1, kSumThreads, 0, st>>>(pair_loss, n_pairs, scale, loss);
-    if (rows > 0 && dlogits != nullptr) {
+    const Total total{pair_loss, n_pairs, scale, loss};
+    if (rows == 0 || dlogits == nullptr) {
+        total_kernel<<<1, 32, 0, st>>>(total);
+    } else {
         pick_threads(rows, vocab, dt, [&](auto t, auto threads) {
-            row_grad_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, r, rows);
+            row_grad_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, r, rows, total);
         });
     }
     return cuda_status_public(cudaGetLastError());

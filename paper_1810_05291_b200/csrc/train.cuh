@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/signsgd_train.h"
 #include "common.cuh"
 
@@ -65,6 +67,21 @@ inline bool mat_overlaps(const Mat& a, const void* p, size_t n) { return bytes_o
 // An output that is an input in place: the same elements at the same places.
 inline bool same_mat(const Mat& a, const Mat& b) {
     return a.p == b.p && a.rows == b.rows && a.cols == b.cols && a.stride == b.stride && a.eb == b.eb;
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory on the current device: asked of the runtime once
+// for each kernel (KEY: a type of its own) and device, and again only for more.
+template <typename KEY>
+cudaError_t allow_shared(const void* kernel, int bytes) {
+    static std::atomic<int> allowed[64];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const bool known = device < 64;
+    if (known && allowed[device].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && known) allowed[device].store(bytes, std::memory_order_relaxed);
+    return e;
 }
 
 // ---- the two element types -------------------------------------------------------------------------

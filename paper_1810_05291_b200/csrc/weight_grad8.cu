@@ -651,7 +651,7 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     if (encode(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(ckpt_x), x_dims, &pitch, x_box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return SS_ERR_UNSUPPORTED;
-    e = cudaFuncSetAttribute(weight_grad8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+    e = allow_shared<WeightGrad>(reinterpret_cast<const void*>(weight_grad8_kernel), static_cast<int>(kSmem));
     if (e != cudaSuccess) return cuda_status_public(e);
 
     if (l.staged) {

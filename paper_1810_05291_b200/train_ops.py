@@ -1,0 +1,169 @@
+"""The training operators as autograd functions: linear layers and activations that keep their
+inputs in 8 bits for the backward pass, and losses over logits.
+
+They make the gradients that ``optim.SignumVote`` compresses: a linear layer's weight gradient is
+added straight into the parameter's ``grad``, which under ``SignumVote`` is a view of the flat
+buffer that the vote reads. Matrix products with the weights are PyTorch's; everything else of the
+two passes is in the kernels of ``binding`` (``include/signsgd_train.h`` has the formulas).
+"""
+
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding as B
+
+ACTIVATIONS = {"gelu": B.SS_ACT_GELU, "silu": B.SS_ACT_SILU}
+PREFERENCES = {"sigmoid": B.SS_PREF_SIGMOID, "hinge": B.SS_PREF_HINGE, "squared": B.SS_PREF_SQUARED}
+
+
+def _rows(x: torch.Tensor) -> torch.Tensor:
+    """[..., cols] as a matrix with unit column stride (a view where that is possible)."""
+    m = x.reshape(-1, x.shape[-1])
+    return m if m.stride(1) == 1 or m.shape[1] < 2 else m.contiguous()
+
+
+def _grad_buffer(weight: torch.Tensor) -> Optional[torch.Tensor]:
+    g = weight.grad
+    return g if g is not None and g.dtype == torch.float32 and g.dim() == 2 and (g.stride(1) == 1 or g.shape[1] < 2) else None
+
+
+class _Linear8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, kept, into_grad):
+        m = _rows(x)
+        if kept is None:
+            kept = B.act8_checkpoint(m.shape[0], m.shape[1], m.device)
+            B.ss_act8_pack(m, kept)
+        w = weight.to(x.dtype)
+        ctx.kept, ctx.weight, ctx.shape, ctx.into_grad = kept, weight, x.shape, into_grad
+        ctx.save_for_backward(w)
+        return (m @ w.t()).view(*x.shape[:-1], weight.shape[0])
+
+    @staticmethod
+    def backward(ctx, dy):
+        weight, d = ctx.weight, _rows(dy)
+        dx = (d @ ctx.saved_tensors[0]).view(ctx.shape) if ctx.needs_input_grad[0] else None
+        dw = None
+        if ctx.needs_input_grad[1]:
+            into = _grad_buffer(weight) if ctx.into_grad else None
+            if into is not None:                  # no second buffer, no addition afterwards
+                B.ss_weight_grad8(d, ctx.kept, into, accumulate=True)
+            else:
+                dw = torch.empty(weight.shape, dtype=torch.float32, device=weight.device)
+                B.ss_weight_grad8(d, ctx.kept, dw)
+        return dx, dw, None, None
+
+
+class _Act8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, up, act, keep_output):
+        m, u = _rows(x), None if up is None else _rows(up)
+        new = lambda: B.act8_checkpoint(m.shape[0], m.shape[1], m.device)  # noqa: E731
+        y = torch.empty(m.shape, dtype=m.dtype, device=m.device)
+        ctx.act, ctx.shape = act, x.shape
+        ctx.kept, ctx.kept_up = new(), None if u is None else new()
+        kept_y = new() if keep_output else None
+        B.ss_act8_forward(m, u, act, y, ctx.kept, ctx.kept_up, kept_y)
+        if kept_y is not None:
+            ctx.mark_non_differentiable(kept_y)
+        return y.view(x.shape), kept_y
+
+    @staticmethod
+    def backward(ctx, dy, _):
+        d = _rows(dy)
+        dx = torch.empty(d.shape, dtype=d.dtype, device=d.device)
+        dup = None if ctx.kept_up is None else torch.empty_like(dx)
+        B.ss_act8_backward(d, ctx.kept, ctx.kept_up, ctx.act, dx, dup)
+        return dx.view(ctx.shape), None if dup is None else dup.view(ctx.shape), None, None
+
+
+def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] = None,
+            into_grad: bool = True) -> torch.Tensor:
+    """``x @ weight.T`` whose input is kept in 8 bits (33 bytes for 32 values) for the weight
+    gradient. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
+    ``x``'s type. Where ``weight.grad`` is a float32 matrix already, the gradient is added to it
+    during the backward pass, and nothing is handed on to autograd (``into_grad=False``: always handed
+    on, as ``torch.autograd.grad`` and hooks on the weight need it). ``kept``: the checkpoint of ``x``,
+    if it is at hand (``act8`` makes its output's)."""
+    return _Linear8.apply(x, weight, kept, into_grad)
+
+
+def act8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: str = "silu",
+         keep_output: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """``f(x)`` or ``f(x) * up`` whose inputs are kept in 8 bits. Returns the result and, with
+    ``keep_output``, its checkpoint for the ``linear8`` that follows (else None)."""
+    return _Act8.apply(x, up, ACTIVATIONS[act], keep_output)
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, old_logp, ref_logp, advantages, weights, inv_temperature, clip_low, clip_high, kl_coef):
+        z = _rows(logits)
+        args = (z, targets, old_logp, ref_logp, advantages, weights)
+        ctx.save_for_backward(*args)
+        ctx.options = dict(inv_temperature=inv_temperature, clip_low=clip_low, clip_high=clip_high, kl_coef=kl_coef)
+        ctx.shape = logits.shape
+        totals, logp = torch.empty(3, device=z.device), torch.empty(z.shape[0], device=z.device)
+        B.ss_policy_loss(*args, totals, logp, None, **ctx.options)
+        loss, rest = totals[0].clone(), totals[1:]
+        ctx.mark_non_differentiable(rest, logp)
+        return loss, rest, logp
+
+    @staticmethod
+    def backward(ctx, g, *_):
+        z = ctx.saved_tensors[0]
+        dz, totals, logp = torch.empty_like(z), torch.empty(3, device=z.device), torch.empty(z.shape[0], device=z.device)
+        B.ss_policy_loss(*ctx.saved_tensors, totals, logp, dz, grad_scale=g.reshape(1).float(), **ctx.options)
+        return (dz.view(ctx.shape),) + (None,) * 9
+
+
+def _preference_outputs(args):
+    z, ref = args[0], args[4]
+    new = lambda n: torch.empty(n, device=z.device)  # noqa: E731
+    return new(1), new(ref.shape[0] // 2), new(ref.shape[0]), new(z.shape[0])
+
+
+class _PreferenceLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, weights, seq_begin, ref_seq_logp, options):
+        z = _rows(logits)
+        args = (z, targets, weights, seq_begin, ref_seq_logp)
+        ctx.save_for_backward(*args)
+        ctx.options, ctx.shape = options, logits.shape
+        outs = _preference_outputs(args)
+        B.ss_preference_loss(*args, *outs, None, **options)
+        loss = outs[0].reshape(())
+        ctx.mark_non_differentiable(*outs[1:])
+        return (loss,) + outs[1:]
+
+    @staticmethod
+    def backward(ctx, g, *_):
+        args = ctx.saved_tensors
+        dz = torch.empty_like(args[0])
+        B.ss_preference_loss(*args, *_preference_outputs(args), dz, grad_scale=g.reshape(1).float(), **ctx.options)
+        return dz.view(ctx.shape), None, None, None, None, None
+
+
+def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, kl_coef: float = 0.0,
+                clip_low: float = 0.2, clip_high: float = 0.2, inv_temperature: float = 1.0):
+    """Clipped policy loss with a KL term over ``logits`` [rows, vocab]. Returns the loss, two
+    figures (the weighted sum of the KL terms, the weight of the clipped positions) and the log
+    probabilities. The forward pass forms no gradient; a loop of its own that wants loss and
+    gradient in one pass over the logits calls ``binding.ss_policy_loss`` with ``dlogits``."""
+    return _PolicyLoss.apply(logits, targets, old_logp, ref_logp, advantages, weights, inv_temperature, clip_low, clip_high, kl_coef)
+
+
+def preference_loss(logits, targets, weights, seq_begin, ref_seq_logp, kind: str = "sigmoid", beta: float = 0.1,
+                    label_smoothing: float = 0.0, scale: Optional[float] = None, inv_temperature: float = 1.0):
+    """Preference loss over pairs of packed sequences: sequence ``s`` covers rows
+    ``seq_begin[s] : seq_begin[s + 1]``, ``2 p`` is the preferred one of pair ``p``. ``scale``
+    defaults to the mean over the pairs. Returns the loss, the margins, the sequences' log
+    probabilities and the positions' log probabilities."""
+    pairs = ref_seq_logp.shape[0] // 2
+    return _PreferenceLoss.apply(logits, targets, weights, seq_begin, ref_seq_logp,
+                                 dict(kind=PREFERENCES[kind], beta=beta, label_smoothing=label_smoothing,
+                                      scale=1.0 / max(pairs, 1) if scale is None else scale,
+                                      inv_temperature=inv_temperature))
