@@ -585,6 +585,7 @@ __global__ void __launch_bounds__(kSumThreads) totals_kernel(const float* terms,
 // ---- preference loss: statistics of every row, then every pair's coefficient, then the gradient -----
 struct Rows {
     Stat* stat;
+    float* weight;  // what counts of weights[t]: 0 for rows left out
     float* coef;
 };
 
@@ -598,7 +599,8 @@ __global__ void __launch_bounds__(block_of<THREADS>()) row_stat_kernel(const __g
     float w;
     Stat s{0.0f, 1.0f};
     float logp = 0.0f;
-    if (row_live(a, row, &target, &w)) {
+    const bool live = row_live(a, row, &target, &w);
+    if (live) {
         const Row<T> z(static_cast<const T*>(a.z) + row * a.z_stride, a.vocab);
         const float k = a.c * kLog2e, picked = Elem<T>::load(z.element(static_cast<uint32_t>(target) + z.head));
         s = row_join<THREADS>(stat_of<T, THREADS>(z, t, k), shared, k);
@@ -607,6 +609,7 @@ __global__ void __launch_bounds__(block_of<THREADS>()) row_stat_kernel(const __g
     if (t == 0) {
         a.logp[row] = logp;
         r.stat[row] = s;
+        r.weight[row] = live ? w : 0.0f;
         r.coef[row] = 0.0f;  // of rows that belong to no sequence
     }
 }
@@ -621,22 +624,32 @@ struct Preference {
 };
 
 __global__ void __launch_bounds__(kSumThreads) pair_kernel(const __grid_constant__ Logits a, const __grid_constant__ Preference p, Rows r) {
-    __shared__ double shared[32];
+    __shared__ double shared[2][32];
     const int64_t pair = blockIdx.x;
     int64_t at[3];
     for (int i = 0; i < 3; ++i) {
         const int64_t b = p.begin[2 * pair + i];
         at[i] = b < 0 ? 0 : (b > p.rows ? p.rows : b);
     }
-    double sum[2];
-    for (int i = 0; i < 2; ++i) {
-        double v = 0.0;
+    // both sequences at once, each position to its own sum; the sums in a fixed order
+    double sum[2] = {0.0, 0.0};
+    for (int i = 0; i < 2; ++i)
         for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kSumThreads) {
-            int64_t target;
-            float w;
-            if (row_live(a, t, &target, &w)) v += static_cast<double>(w) * a.logp[t];
+            const float w = r.weight[t];
+            if (w != 0.0f) sum[i] += static_cast<double>(w) * a.logp[t];
         }
-        sum[i] = block_sum(v, shared);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        sum[0] += __shfl_xor_sync(0xFFFFFFFFu, sum[0], o);
+        sum[1] += __shfl_xor_sync(0xFFFFFFFFu, sum[1], o);
+    }
+    if ((threadIdx.x & 31) == 0) shared[0][threadIdx.x >> 5] = sum[0], shared[1][threadIdx.x >> 5] = sum[1];
+    __syncthreads();
+    sum[0] = shared[0][threadIdx.x & 31], sum[1] = shared[1][threadIdx.x & 31];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        sum[0] += __shfl_xor_sync(0xFFFFFFFFu, sum[0], o);
+        sum[1] += __shfl_xor_sync(0xFFFFFFFFu, sum[1], o);
     }
     const double h = (sum[0] - p.ref[2 * pair]) - (sum[1] - p.ref[2 * pair + 1]);
     const float m = static_cast<float>(p.beta * h);
@@ -662,9 +675,8 @@ __global__ void __launch_bounds__(kSumThreads) pair_kernel(const __grid_constant
     slope *= p.scale * (a.grad_scale == nullptr ? 1.0f : *a.grad_scale);
     for (int i = 0; i < 2; ++i)
         for (int64_t t = at[i] + threadIdx.x; t < at[i + 1]; t += kSumThreads) {
-            int64_t target;
-            float w;
-            if (row_live(a, t, &target, &w)) r.coef[t] = (i == 0 ? slope : -slope) * w * a.c;
+            const float w = r.weight[t];
+            if (w != 0.0f) r.coef[t] = (i == 0 ? slope : -slope) * w * a.c;
         }
 }
 
@@ -816,7 +828,7 @@ extern "C" {
 
 int64_t ss_loss_workspace(int64_t rows, int64_t n_pairs) {
     if (rows < 0 || rows > kMaxSide || n_pairs < 0 || n_pairs > kMaxSide) return -1;
-    return round_up(rows * 12, 256) + round_up(n_pairs * 4, 256);
+    return round_up(rows * 16, 256) + round_up(n_pairs * 4, 256);
 }
 
 int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64_t rows, int64_t vocab,
@@ -887,8 +899,8 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
     if (s != SS_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const Logits a{logits, dlogits, z.stride, dz.stride, vocab, targets, weights, grad_scale, inv_temperature, logp};
-    const Rows r{static_cast<Stat*>(workspace), static_cast<float*>(workspace) + 2 * rows};
-    float* pair_loss = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up(rows * 12, 256));
+    const Rows r{static_cast<Stat*>(workspace), static_cast<float*>(workspace) + 2 * rows, static_cast<float*>(workspace) + 3 * rows};
+    float* pair_loss = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up(rows * 16, 256));
     const Preference p{seq_begin, ref_seq_logp, n_pairs, rows, kind, beta, label_smoothing, scale, margins, seq_logp, pair_loss};
     if (rows > 0) {
         pick_threads(rows, vocab, dt, [&](auto t, auto threads) {

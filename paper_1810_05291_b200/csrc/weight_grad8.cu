@@ -494,26 +494,43 @@ __global__ void __launch_bounds__(256) zero_kernel(float* dw, int64_t stride, in
 // dY as the copies want it: bf16, rows at multiples of 16 bytes. An fp32 value is the sum of three
 // bf16: its leading 8 bits, the next 8 and the last 8, cut off, so that the sum is exact and
 // nothing overflows; an infinity or NaN is carried by the first alone.
+// A thread takes four columns.
 template <typename T>
 __global__ void __launch_bounds__(256) stage_dy_kernel(const T* dy, int64_t stride, int64_t rows, int64_t n_out, uint16_t* out, int64_t out_stride) {
-    const int64_t total = rows * out_stride, plane = total;
+    const int64_t fours = out_stride / 4, total = rows * fours, plane = rows * out_stride;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t t = i / out_stride, n = i - t * out_stride;
-        if constexpr (sizeof(T) == 2) {
-            out[i] = n < n_out ? dy[t * stride + n] : uint16_t(0);
+        const int64_t t = total <= 0xFFFFFFFFll ? static_cast<int64_t>(static_cast<uint32_t>(i) / static_cast<uint32_t>(fours)) : i / fours;
+        const int64_t n = (i - t * fours) * 4;
+        const T* const src = dy + t * stride + n;
+        T v[4];
+        if (sizeof(T) == 4 && n + 4 <= n_out && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+            const uint4 x = *reinterpret_cast<const uint4*>(src);
+            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
         } else {
-            const float v = n < n_out ? dy[t * stride + n] : 0.0f;
-            uint32_t hi = __float_as_uint(v) & 0xFFFF0000u, mid = 0, lo = 0;
-            if ((hi & 0x7F800000u) == 0x7F800000u) {
-                if (v != v) hi = 0x7FC00000u;
-            } else {
-                const float rest = v - __uint_as_float(hi);
-                mid = __float_as_uint(rest) & 0xFFFF0000u;
-                lo = __float_as_uint(rest - __uint_as_float(mid));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = n + j < n_out ? src[j] : T(0);
+        }
+        uint16_t* const dst = out + t * out_stride + n;
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint2*>(dst) = make_uint2(v[0] | (static_cast<uint32_t>(v[1]) << 16), v[2] | (static_cast<uint32_t>(v[3]) << 16));
+        } else {
+            uint32_t part[3][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float f = __uint_as_float(v[j]);
+                uint32_t hi = v[j] & 0xFFFF0000u, mid = 0, lo = 0;
+                if ((hi & 0x7F800000u) == 0x7F800000u) {
+                    if (f != f) hi = 0x7FC00000u;
+                } else {
+                    const float rest = f - __uint_as_float(hi);
+                    mid = __float_as_uint(rest) & 0xFFFF0000u;
+                    lo = __float_as_uint(rest - __uint_as_float(mid));
+                }
+                part[0][j] = hi, part[1][j] = mid, part[2][j] = lo;
             }
-            out[i] = static_cast<uint16_t>(hi >> 16);
-            out[plane + i] = static_cast<uint16_t>(mid >> 16);
-            out[2 * plane + i] = static_cast<uint16_t>(lo >> 16);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                *reinterpret_cast<uint2*>(dst + k * plane) = make_uint2(__byte_perm(part[k][0], part[k][1], 0x7632), __byte_perm(part[k][2], part[k][3], 0x7632));
         }
     }
 }
@@ -655,9 +672,9 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     if (e != cudaSuccess) return cuda_status_public(e);
 
     if (l.staged) {
-        const int64_t want = (rows * l.stride + 255) / 256, most = static_cast<int64_t>(sms) * 16;
+        const int64_t want = (rows * l.stride / 4 + 255) / 256, most = static_cast<int64_t>(sms) * 16;
         const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-        if (dt == SS_F32) stage_dy_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
+        if (dt == SS_F32) stage_dy_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
         else stage_dy_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
     }
     float* partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.staged_bytes);
