@@ -586,6 +586,25 @@ def test_preference_loss(rows, vocab, pairs, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
+@pytest.mark.parametrize("begin", [[3, 100, 190, 190, 190, 400, 650, 651, 652, 680, 690], [0, 0, 0, 350, 700, 700, 700], [0, 1, 2] + [700] * 6,
+                                   [10] * 7, list(range(0, 701, 25))], ids=["rows of none", "empty", "short", "all empty", "even"])
+def test_preference_loss_over_many_logits(begin, dtype):
+    """Logits too large for the L2 cache: statistics and gradients by turns in one kernel. In place too, and the same bits again."""
+    rows, vocab = 700, 50001
+    pairs = (len(begin) - 1) // 2
+    z, y, w, _, _, _ = loss_inputs(rows, vocab, dtype, pad=2)
+    begin = torch.tensor(begin, device=DEV)
+    now = ref.preference(z, y, w, begin, torch.zeros(2 * pairs, device=DEV), 1.0, 0, 0.1, 0.0, 1.0)[2]
+    rlp = (now + 3 * torch.randn(2 * pairs, generator=gen(rows), device=DEV)).float()
+    for kind in (0, 2):
+        check_preference(z, y, w, begin, rlp, kind=kind, scale=1.0 / pairs)
+    like = lambda: torch.empty_strided(z.shape, z.stride(), dtype=dtype, device=DEV)  # noqa: E731
+    zs, dz, over = like().copy_(z), like(), like().copy_(z)
+    first, second = run_preference(zs, y, w, begin, rlp, dz), run_preference(over, y, w, begin, rlp, over)
+    assert torch.equal(dz, over) and all(torch.equal(p, q) for p, q in zip(first, second))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 @pytest.mark.parametrize("pad,off,out_pad,out_off", [(1, 0, 1, 0), (0, 1, 0, 0), (3, 2, 5, 1), (7, 1, 7, 1)])
 def test_preference_loss_strides_and_alignment(pad, off, out_pad, out_off, dtype):
     for vocab in (5, 1001, 4096):
