@@ -346,6 +346,7 @@ constexpr int block_of() { return THREADS > 256 ? THREADS : 256; }
 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(block_of<THREADS>()) policy_stream_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, int64_t rows) {
+    next_may_begin();
     __shared__ Stat shared[THREADS / 32];
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS;
     const int t = threadIdx.x % THREADS;
@@ -410,6 +411,7 @@ struct Given {
 
 template <typename T, int HELD>
 __global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slice_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, const __grid_constant__ Slices c) {
+    next_may_begin();
     extern __shared__ __align__(128) uint8_t dynamic[];
     constexpr int THREADS = kSliceThreads, kSlots = kSliceSlots<T>, kPer = Row<T>::kPer, kVectors = HELD / kPer;
     __shared__ Stat shared[2][THREADS / 32];  // two sets: a warp may be a row ahead of one that still reads
@@ -574,6 +576,7 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
 }
 
 __global__ void __launch_bounds__(kSumThreads) totals_kernel(const float* terms, int64_t n, float* out) {
+    after_previous();
     __shared__ double shared[32];
     const float* x = terms + blockIdx.x * n;
     double v = 0.0;
@@ -591,6 +594,7 @@ struct Rows {
 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(block_of<THREADS>()) row_stat_kernel(const __grid_constant__ Logits a, Rows r, int64_t rows) {
+    next_may_begin();
     __shared__ Stat shared[THREADS / 32];
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS;
     const int t = threadIdx.x % THREADS;
@@ -624,6 +628,8 @@ struct Preference {
 };
 
 __global__ void __launch_bounds__(kSumThreads) pair_kernel(const __grid_constant__ Logits a, const __grid_constant__ Preference p, Rows r) {
+    next_may_begin();
+    after_previous();
     __shared__ double shared[2][32];
     const int64_t pair = blockIdx.x;
     int64_t at[3];
@@ -696,12 +702,16 @@ struct Total {
     }
 };
 
-__global__ void __launch_bounds__(32) total_kernel(const __grid_constant__ Total total) { total.write(); }
+__global__ void __launch_bounds__(32) total_kernel(const __grid_constant__ Total total) {
+    after_previous();
+    total.write();
+}
 
 // In the order opposite to the statistics', so that it begins with the rows that the caches still hold.
 // The first warp of the last block also writes the loss.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(block_of<THREADS>()) row_grad_kernel(const __grid_constant__ Logits a, Rows r, int64_t rows, const __grid_constant__ Total total) {
+    after_previous();
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x < 32) total.write();
     const int64_t row = rows - 1 - (static_cast<int64_t>(blockIdx.x) * (blockDim.x / THREADS) + threadIdx.x / THREADS);
     const int t = threadIdx.x % THREADS;
@@ -868,8 +878,9 @@ int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64
             });
         }
     }
-    totals_kernel<<<3, kSumThreads, 0, st>>>(p.terms, rows, totals);
-    return cuda_status_public(cudaGetLastError());
+    const cudaError_t first = cudaGetLastError();
+    if (first != cudaSuccess) return cuda_status_public(first);
+    return cuda_status_public(launch_next(rows > 0, totals_kernel, 3, kSumThreads, st, p.terms, rows, totals));
 }
 
 int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64_t rows, int64_t vocab,
@@ -907,16 +918,18 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
             row_stat_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, r, rows);
         });
     }
-    if (n_pairs > 0) pair_kernel<<<static_cast<unsigned>(n_pairs), kSumThreads, 0, st>>>(a, p, r);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess && n_pairs > 0) e = launch_next(rows > 0, pair_kernel, static_cast<unsigned>(n_pairs), kSumThreads, st, a, p, r);
+    if (e != cudaSuccess) return cuda_status_public(e);
     const Total total{pair_loss, n_pairs, scale, loss};
     if (rows == 0 || dlogits == nullptr) {
-        total_kernel<<<1, 32, 0, st>>>(total);
+        e = launch_next(rows > 0 || n_pairs > 0, total_kernel, 1, 32, st, total);
     } else {
         pick_threads(rows, vocab, dt, [&](auto t, auto threads) {
-            row_grad_kernel<decltype(t), threads.value><<<rows_grid<threads.value>(rows), block_of<threads.value>(), 0, st>>>(a, r, rows, total);
+            e = launch_next(true, row_grad_kernel<decltype(t), threads.value>, rows_grid<threads.value>(rows), block_of<threads.value>(), st, a, r, rows, total);
         });
     }
-    return cuda_status_public(cudaGetLastError());
+    return cuda_status_public(e);
 }
 
 #pragma GCC visibility pop

@@ -84,6 +84,26 @@ cudaError_t allow_shared(const void* kernel, int bytes) {
     return e;
 }
 
+// ---- kernels of one call that follow one another ---------------------------------------------------
+// A kernel that another of the same call follows says so at its start; the other is launched with
+// launch_next and begins with after_previous(), before it touches any memory. So its blocks are set up
+// while the first kernel's last ones run, but it neither reads nor writes before the first has ended
+// and its stores are seen. (`follows` is false where the call has launched nothing yet: such a kernel
+// begins when all that the stream held before has ended, like any other.)
+__device__ __forceinline__ void next_may_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_next(bool follows, void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t st, const A&... args) {
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid, cfg.blockDim = block, cfg.stream = st;
+    cfg.attrs = &at, cfg.numAttrs = follows ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // ---- the two element types -------------------------------------------------------------------------
 template <typename T>
 struct Elem;  // T: float, or uint16_t for the bits of a bf16

@@ -54,7 +54,7 @@ struct WeightGrad {
     float* dw;
     float* partial;  // one tile for each part
     int64_t dw_stride, rows, n_out, n_in;
-    int accumulate;
+    int accumulate, follows;  // follows: stage_dy_kernel goes before
     Plan plan;
 };
 
@@ -264,6 +264,8 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
     if (warp == 0) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
     tc_fence_before();
     __syncthreads();
+    next_may_begin();
+    if (a.follows) after_previous();
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
@@ -456,6 +458,7 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
 // dW of the tiles whose rows were split: the parts added in their order, four columns to a thread and
 // four parts under way at a time.
 __global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ WeightGrad a) {
+    after_previous();
     const Plan& p = a.plan;
     const int other = blockIdx.x, tile = p.whole + other, i = (blockIdx.y * 256 + threadIdx.x) * 4;
     const int64_t n = static_cast<int64_t>(tile % p.tiles_n) * kTileN + i / kTileK, k = static_cast<int64_t>(tile / p.tiles_n) * kTileK + i % kTileK;
@@ -497,6 +500,7 @@ __global__ void __launch_bounds__(256) zero_kernel(float* dw, int64_t stride, in
 // A thread takes four columns.
 template <typename T>
 __global__ void __launch_bounds__(256) stage_dy_kernel(const T* dy, int64_t stride, int64_t rows, int64_t n_out, uint16_t* out, int64_t out_stride) {
+    next_may_begin();
     const int64_t fours = out_stride / 4, total = rows * fours, plane = rows * out_stride;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
         const int64_t t = total <= 0xFFFFFFFFll ? static_cast<int64_t>(static_cast<uint32_t>(i) / static_cast<uint32_t>(fours)) : i / fours;
@@ -676,26 +680,30 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
         const unsigned grid = static_cast<unsigned>(want < most ? want : most);
         if (dt == SS_F32) stage_dy_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
         else stage_dy_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(dy), my.stride, rows, n_out, static_cast<uint16_t*>(workspace), l.stride);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return cuda_status_public(e);
     }
     float* partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.staged_bytes);
-    const WeightGrad a{ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, n_in), dw, partial, mw.stride, rows, n_out, n_in, accumulate, l.plan};
+    const WeightGrad a{ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, n_in), dw, partial, mw.stride, rows, n_out, n_in, accumulate, l.staged, l.plan};
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(2 * (l.plan.units < sms / 2 ? l.plan.units : sms / 2)));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = 2, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = l.staged ? 2 : 1;
     e = cudaLaunchKernelEx(&cfg, weight_grad8_kernel, map, x_map, a);
     if (e != cudaSuccess) return cuda_status_public(e);
     if (l.plan.parts > 1) {
         const unsigned others = static_cast<unsigned>(l.plan.tiles_n * l.plan.tiles_k - l.plan.whole);
-        join_parts_kernel<<<dim3(others, kTileN * kTileK / 1024), 256, 0, st>>>(a);
+        e = launch_next(true, join_parts_kernel, dim3(others, kTileN * kTileK / 1024), 256, st, a);
     }
-    return cuda_status_public(cudaGetLastError());
+    return cuda_status_public(e);
 }
 
 #pragma GCC visibility pop
