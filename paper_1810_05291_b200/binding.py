@@ -513,14 +513,19 @@ def _opt_vec(t: Optional[torch.Tensor], dtype, name: str, n: int) -> Optional[in
     return None if t is None else _vec(t, dtype, name, n)
 
 
-def _scratch(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor):
+def _scratch(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, stream):
     """(address, bytes) of the caller's workspace, or of one of the size asked for from PyTorch's
-    allocator, and the tensor to keep until the call returns (its memory is safe after that: it is
-    given out again in the order of the stream)."""
+    allocator, and the tensor to keep until the call returns (its memory is safe after that: it
+    belongs to the call's stream, and is given out again in the order of that stream)."""
     if workspace is None:
         if need <= 0:
             return None, 0, None
-        workspace = like.new_empty(need, dtype=torch.uint8)
+        if stream is None:
+            workspace = like.new_empty(need, dtype=torch.uint8)
+        else:
+            own = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), like.device)
+            with torch.cuda.stream(own):
+                workspace = like.new_empty(need, dtype=torch.uint8)
     elif not workspace.is_cuda or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA uint8 tensor")
     return workspace.data_ptr(), workspace.numel(), workspace
@@ -595,7 +600,7 @@ def ss_weight_grad8(dy: torch.Tensor, ckpt_x: torch.Tensor, dw: torch.Tensor, ac
     n_in = dw.shape[1]
     L = lib()
     need = 0 if workspace is not None else L.ss_weight_grad8_workspace(dy_ptr, dy_stride, code, rows, n_out, n_in)
-    w_ptr, w_bytes, workspace = _scratch(workspace, need, dy)
+    w_ptr, w_bytes, workspace = _scratch(workspace, need, dy, stream)
     _check(L.ss_weight_grad8(dy_ptr, dy_stride, code, _ckpt(ckpt_x, rows, n_in, "ckpt_x"), rows, n_out, n_in, dw_ptr,
                              dw_stride, int(bool(accumulate)), w_ptr, w_bytes, _stream(stream)), "ss_weight_grad8")
 
@@ -616,7 +621,7 @@ def ss_policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.
     rows, vocab = logits.shape
     d_ptr, d_stride = (None, 0) if dlogits is None else _mat(dlogits, logits.dtype, "dlogits", logits.shape)
     L = lib()
-    w_ptr, w_bytes, workspace = _scratch(workspace, ss_loss_workspace(rows, 0), logits)
+    w_ptr, w_bytes, workspace = _scratch(workspace, ss_loss_workspace(rows, 0), logits, stream)
     _check(L.ss_policy_loss(z_ptr, z_stride, code, rows, vocab, _vec(targets, torch.int64, "targets", rows),
                             _vec(old_logp, f32, "old_logp", rows), _opt_vec(ref_logp, f32, "ref_logp", rows),
                             _vec(advantages, f32, "advantages", rows), _vec(weights, f32, "weights", rows),
@@ -637,7 +642,7 @@ def ss_preference_loss(logits: torch.Tensor, targets: torch.Tensor, weights: tor
     pairs = margins.shape[0]
     d_ptr, d_stride = (None, 0) if dlogits is None else _mat(dlogits, logits.dtype, "dlogits", logits.shape)
     L = lib()
-    w_ptr, w_bytes, workspace = _scratch(workspace, ss_loss_workspace(rows, pairs), logits)
+    w_ptr, w_bytes, workspace = _scratch(workspace, ss_loss_workspace(rows, pairs), logits, stream)
     _check(L.ss_preference_loss(z_ptr, z_stride, code, rows, vocab, _vec(targets, i64, "targets", rows),
                                 _vec(weights, f32, "weights", rows), _vec(seq_begin, i64, "seq_begin", 2 * pairs + 1),
                                 pairs, _vec(ref_seq_logp, f32, "ref_seq_logp", 2 * pairs), inv_temperature, kind, beta,

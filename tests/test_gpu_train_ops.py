@@ -589,7 +589,7 @@ def test_preference_loss(rows, vocab, pairs, kind, dtype):
 @pytest.mark.parametrize("begin", [[3, 100, 190, 190, 190, 400, 650, 651, 652, 680, 690], [0, 0, 0, 350, 700, 700, 700], [0, 1, 2] + [700] * 6,
                                    [10] * 7, list(range(0, 701, 25))], ids=["rows of none", "empty", "short", "all empty", "even"])
 def test_preference_loss_over_many_logits(begin, dtype):
-    """Logits too large for the L2 cache: statistics and gradients by turns in one kernel. In place too, and the same bits again."""
+    """Logits too large for the L2 cache, sequences cut in every way. In place too, and the same bits again."""
     rows, vocab = 700, 50001
     pairs = (len(begin) - 1) // 2
     z, y, w, _, _, _ = loss_inputs(rows, vocab, dtype, pad=2)
@@ -692,3 +692,40 @@ def test_another_stream_and_the_same_bits_every_time():
         for s, t in zip(p, q):
             assert torch.equal(s, t)
     assert torch.equal(back.double(), ref.act8(x)[2])
+
+
+@pytest.mark.parametrize("as_handle", [False, True], ids=["stream", "handle"])
+def test_scratch_memory_belongs_to_the_call_s_stream(as_handle):
+    """A call that is given a stream other than the current one, and no workspace, while that stream is busy:
+    what the current stream allocates and fills in the meantime must not be the call's workspace."""
+    rows, vocab = 40, 9001
+    z, y, w, old, rlp, adv = loss_inputs(rows, vocab, torch.bfloat16)
+    dy, x = torch.randn(700, 130, device=DEV), torch.randn(700, 96, device=DEV)
+    ck = B.act8_checkpoint(700, 96, DEV)
+    B.ss_act8_pack(x, ck)
+    begin, seq_ref = cuts(rows, 2, 4), torch.zeros(4, device=DEV)
+
+    def outputs():
+        return {"totals": torch.empty(3, device=DEV), "logp": torch.empty(rows, device=DEV), "dlogits": torch.empty_like(z)}
+
+    def calls(stream):
+        a, b = outputs(), outputs()
+        loss, margins, seq = torch.empty(1, device=DEV), torch.empty(2, device=DEV), torch.empty(4, device=DEV)
+        dw = torch.empty(130, 96, device=DEV)
+        torch.cuda.synchronize()
+        if stream is not None:
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(20_000_000)  # cycles: about 10 ms
+        B.ss_policy_loss(z, y, old, rlp, adv, w, a["totals"], a["logp"], a["dlogits"], kl_coef=0.05, stream=stream)
+        B.ss_preference_loss(z, y, w, begin, seq_ref, loss, margins, seq, b["logp"], b["dlogits"], stream=stream)
+        B.ss_weight_grad8(dy, ck, dw, stream=stream)
+        sizes = (B.ss_loss_workspace(rows, 0), B.ss_loss_workspace(rows, 2), B.ss_weight_grad8_workspace(dy, 96))
+        kept = [torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(bool((k == 0xFF).all()) for k in kept)
+        return [a["totals"], a["logp"], a["dlogits"], loss, margins, seq, b["logp"], b["dlogits"], dw]
+
+    want = calls(None)
+    side = torch.cuda.Stream()
+    for got, expected in zip(calls(side.cuda_stream if as_handle else side), want):
+        assert torch.equal(got, expected)
