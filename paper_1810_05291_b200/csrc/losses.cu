@@ -240,9 +240,13 @@ __device__ __forceinline__ Stat stat_of(const Row<T>& r, uint32_t t, float k) {
         for (int u = 0; u < kAhead; ++u) x[u].v = p[u * THREADS];
         add_vectors(v, x, k);
     }
-    for (; j < n; j += THREADS, p += THREADS) {
-        Vec<T> x[1];
-        x[0].v = *p;
+    if (j < n) {  // the rest of them at once too
+        Vec<T> x[kAhead - 1];
+#pragma unroll
+        for (int u = 0; u < kAhead - 1; ++u) {
+            if (j + u * THREADS < n) x[u].v = p[u * THREADS];
+            else x[u].none();
+        }
         add_vectors(v, x, k);
     }
     if ((r.first && t == 0) || (r.last && t == THREADS - 1)) {
@@ -271,11 +275,13 @@ __device__ __forceinline__ void grad_of(const Row<T>& z, const Row<T>& dz, uint3
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) __stcs(q + u * THREADS, grad_vector(x[u], s.m, k, f).v);
         }
-        for (; j < n; j += THREADS, p += THREADS, q += THREADS) {
-            Vec<T> x;
-            x.v = *p;
-            __stcs(q, grad_vector(x, s.m, k, f).v);
-        }
+        Vec<T> x[kAhead - 1];
+#pragma unroll
+        for (int u = 0; u < kAhead - 1; ++u)
+            if (j + u * THREADS < n) x[u].v = p[u * THREADS];
+#pragma unroll
+        for (int u = 0; u < kAhead - 1; ++u)
+            if (j + u * THREADS < n) __stcs(q + u * THREADS, grad_vector(x[u], s.m, k, f).v);
     } else {  // rows of dz lie otherwise against 16 bytes: element by element
         for (; j < n; j += THREADS, p += THREADS) {
             Vec<T> x;
