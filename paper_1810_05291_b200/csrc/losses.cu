@@ -348,7 +348,7 @@ __device__ __forceinline__ float scale_of(const Logits& a) { return a.c * (a.gra
 // ---- rows read straight from memory, THREADS threads (a warp or a block) to a row. With a
 // gradient the row is read twice, the second time from the caches. ------------------------------------
 template <int THREADS>
-constexpr int block_of() { return THREADS > 256 ? THREADS : 256; }
+constexpr int block_of() { return THREADS > 32 ? THREADS : 256; }
 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(block_of<THREADS>()) policy_stream_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, int64_t rows) {
@@ -384,11 +384,19 @@ __device__ __forceinline__ void tell(uint32_t at, uint32_t bar, int to, const fl
 }
 
 // ---- rows read once: one block to a row, or a cluster of up to 8 whose blocks take a slice each. Slices
-// come by bulk copies, a row or two ahead; a thread turns its 32 logits of a row into exponentials
+// come by bulk copies, a row or two ahead; a thread turns its 64 (or 128) logits of a row into exponentials
 // relative to its own maximum, which stay in registers while the block, and the cluster, join their
 // statistics. So the gradient needs one more factor and no second exponential: with two of them for
 // each bf16 logit the exponential unit alone would take as long as the memory (8192 x 131072: 986 us).
+//
+// Bound by memory: a logit is read once and its gradient written once. 8192 x 131072 bf16 720 us
+// (6.0 TB/s), 16384 x 32768 344 us (6.2), 30000 x 8000 165 us (5.8), 4096 x 131072 fp32 658 us (6.5). A row
+// to a block of 512 threads with the row in shared memory: 986 us for the first, streaming it twice 957.
+// Few rows are bound by the launches: 16 x 32768 takes 6.2 us with the totals.
 constexpr int kSliceThreads = 128;
+// Logits of a thread: 64, and where 8 blocks of that do not hold the row 128, at the price of two blocks fewer on an SM.
+// (128 always: 2053 x 32001 fp32 112 us instead of 91, 4100 x 32001 bf16 136 instead of 112, 16384 x 32768 342
+// instead of 344. Four blocks instead of five at 64: 820 us instead of 714 at 8192 x 131072, six the same.)
 template <int HELD>
 constexpr int kSliceBlocks = HELD == 64 ? 5 : 3;  // on an SM
 
@@ -592,6 +600,12 @@ __global__ void __launch_bounds__(kSumThreads) totals_kernel(const float* terms,
 }
 
 // ---- preference loss: statistics of every row, then every pair's coefficient, then the gradient -----
+// A row's gradient has a factor that depends on every row of its pair, so the logits are read twice: three
+// passes over memory with the write, and bound by it: 16384 rows of 65536 bf16, a quarter of them left out,
+// 831 us (6.4 TB/s over the three; two passes alone would take 574). One kernel that forms the statistics of a pair while the
+// pair before, still in the L2 cache, gets its gradient took 1045 us: the gradients that are written
+// push the logits out, and what is under way at once is too little. Small calls wait for the three
+// kernels to follow one another: 96 x 32768 fp32 in one pair 16.4 us.
 struct Rows {
     Stat* stat;
     float* weight;  // what counts of weights[t]: 0 for rows left out
@@ -734,15 +748,27 @@ __global__ void __launch_bounds__(block_of<THREADS>()) row_grad_kernel(const __g
 }
 
 // ---- choices of a launch ------------------------------------------------------------------------------
-constexpr int64_t kWarpRowBytes = 8192;     // rows up to this size: a warp each
-constexpr int kFewRows = 296;               // fewer rows than two for each SM: a large block each
-constexpr int kMostCount = 8;               // rows of a cluster
+// A warp to a row of up to 8 KB: both losses at 40000 x 3000 bf16 (6 KB) take 106 and 157 us, against 164
+// (policy_slice_kernel) and 322 (256 threads); at 12 KB and 200 rows the warp takes 11.2 and 17.0 us,
+// against 7.5 and 14.4.
+constexpr int64_t kWarpRowBytes = 8192;
+// Longer rows, fewer than two for each SM: 1024 threads each, so that there is enough under way (preference
+// loss, 16 and 250 rows of 131072 bf16: 20.6 and 43 us, with 256 threads 27.7 and 55; 500 rows of 32768: 29.6
+// against 22.3).
+constexpr int kFewRows = 296;
+// Else 128 threads up to 48 KB, so that a thread has a few rounds of vectors to a row, and 256 beyond
+// (preference loss, 40000 x 8000 and x 20000 bf16: 373 and 779 us with 128, 471 and 838 with 256; 4000 x 32001:
+// 147 against 140, 4000 x 65536: 271 against 258).
+constexpr int64_t kSmallBlockRowBytes = 49152;
+// Rows of a cluster in policy_slice_kernel, one after another (8192 x 131072 bf16, us: 1 row 738, 8 rows 714, 32 rows 749).
+constexpr int kMostCount = 8;
 
 template <typename F>
 void pick_threads(int64_t rows, int64_t vocab, ss_dtype dt, F&& launch) {
     auto by_type = [&](auto t) {
         if (vocab * static_cast<int64_t>(sizeof(t)) <= kWarpRowBytes) launch(t, std::integral_constant<int, 32>{});
         else if (rows < kFewRows) launch(t, std::integral_constant<int, 1024>{});
+        else if (vocab * static_cast<int64_t>(sizeof(t)) <= kSmallBlockRowBytes) launch(t, std::integral_constant<int, 128>{});
         else launch(t, std::integral_constant<int, 256>{});
     };
     if (dt == SS_F32) by_type(uint32_t{}); else by_type(uint16_t{});
@@ -754,13 +780,12 @@ unsigned rows_grid(int64_t rows) {
     return static_cast<unsigned>((rows + per - 1) / per);
 }
 
-// Blocks that share a row in policy_slice_kernel, 0 if even 8 do not hold it: the fewest that do, more where there are
-// not enough rows for all SMs.
+// Blocks that share a row in policy_slice_kernel: the fewest that hold it, 0 if even 8 do not.
 template <typename T, int HELD>
-int cluster_of(int64_t rows, int64_t vectors, int sms) {
+int cluster_of(int64_t vectors) {
     if (vectors > 8 * kSliceVectors<T, HELD>) return 0;
     int size = 1;
-    while (size < 8 && (vectors > size * kSliceVectors<T, HELD> || (rows * size * 2 <= sms && vectors > size * kSliceThreads))) size *= 2;
+    while (vectors > size * kSliceVectors<T, HELD>) size *= 2;
     return size;
 }
 
@@ -771,7 +796,8 @@ template <typename T, int HELD>
 cudaError_t launch_slices(const Logits& a, const Policy& p, int64_t rows, int64_t vectors, int size, int sms, cudaStream_t st) {
     constexpr int kSliceSmem = kSliceVectors<T, HELD> * 16 * kSliceSlots<T>;
     Slices c{rows, 1, static_cast<int>((vectors + size - 1) / size)};
-    // as many rows to a cluster as leave three rounds of blocks for every SM
+    // As many rows to a cluster as leave three rounds of blocks for every SM (for one round, and for eight: 2053 x
+    // 32001 fp32 100 and 92.5 us instead of 91, 4100 x 32001 bf16 108 and 113 instead of 112).
     const int64_t count = rows * size / (3 * kSliceBlocks<HELD> * sms);
     c.count = static_cast<int>(count < 1 ? 1 : (count > kMostCount ? kMostCount : count));
     cudaLaunchConfig_t cfg{};
@@ -793,8 +819,8 @@ template <typename T>
 bool try_slices(const Logits& a, const Policy& p, const Mat& z, int sms, cudaStream_t st, cudaError_t* e) {
     const int64_t bytes = z.cols * static_cast<int64_t>(sizeof(T)), vectors = z.row_aligned(16) ? (bytes + 15) / 16 : (bytes + 30) / 16;
     if (bytes <= kWarpRowBytes) return false;
-    if (const int size = cluster_of<T, 64>(z.rows, vectors, sms)) *e = launch_slices<T, 64>(a, p, z.rows, vectors, size, sms, st);
-    else if (const int size = cluster_of<T, 128>(z.rows, vectors, sms)) *e = launch_slices<T, 128>(a, p, z.rows, vectors, size, sms, st);
+    if (const int size = cluster_of<T, 64>(vectors)) *e = launch_slices<T, 64>(a, p, z.rows, vectors, size, sms, st);
+    else if (const int size = cluster_of<T, 128>(vectors)) *e = launch_slices<T, 128>(a, p, z.rows, vectors, size, sms, st);
     else return false;
     return true;
 }
