@@ -101,7 +101,8 @@ int ss_act8_backward(const void* dy, int64_t dy_stride, const uint8_t* ckpt_x, c
  *                      accumulate (a parameter's slice of a flat gradient buffer, say)
  *   workspace  scratch workspace_bytes >= ss_weight_grad8_workspace of the same arguments
  * rows == 0 leaves dW as it is with accumulate and zeroes it without. Too small a workspace is
- * SS_ERR_INVALID_ARG.
+ * SS_ERR_INVALID_ARG. Sums are added to dW by the memory, which may flush a subnormal sum to zero. A
+ * wait inside the kernel that ran out (it is bounded) shows as NaN in the tiles concerned.
  */
 int64_t ss_weight_grad8_workspace(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int64_t n_out,
                                   int64_t n_in);

@@ -69,6 +69,12 @@ __device__ __forceinline__ void act_value_slope(float x, float* f, float* slope)
 // A thread takes 8 columns of a row, four neighbouring lanes a group of 32. Pieces are numbered in
 // the checkpoint's order, so its values and exponents are read and written in one run; row and
 // column follow by a division.
+//
+// Bound by memory where rows start on 16 bytes: 16384 x 8192 bf16, gated silu, forward 176 and backward 176
+// us (6.1 TB/s; DRAM at 67-69 % of its nominal rate, instructions issued in 72 % of the cycles); gated gelu 203 and 199, the
+// instructions' share; pack 74 us (5.5 TB/s), unpack 68. Rows at odd places cost
+// the shifting of vectors: 4099 x 2731 gated silu 27.4 and 27.7 us (3.3 TB/s), the integer pipe 70 % busy; a column
+// to a thread, element by element, took 149 us for both passes.
 constexpr int kPiece = 8;
 constexpr int kBlock = 256;
 

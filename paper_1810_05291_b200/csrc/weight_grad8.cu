@@ -2,13 +2,21 @@
 //
 // The contraction runs over the rows t, so both operands lie in memory with the contraction index
 // slow, and go to the matrix unit that way, without a transpose: tiles of dY by TMA, tiles of x^
-// decoded by eight warps from the 8-bit codes straight into the swizzled operand layout. A decoded
-// value has 7 significant bits and is exact in bf16; no operand is rounded.
+// decoded by sixteen warps from the 8-bit codes straight into the swizzled operand layout. A decoded
+// value has 7 significant bits and is exact in bf16; no operand is rounded. An fp32 dY goes as three
+// bf16 terms whose sum it is exactly; the codes of a stage are decoded once for all three.
 //
 // Sums. The matrix unit adds into fp32 with truncation: of a product with inputs of mean 0 over 16384
-// rows that it sums alone, 1.9e-5 is lost. So a tile is summed there over 2048 rows at a time, in
-// one half of the tensor memory, and added to dW, rounded to nearest, while the matrix unit fills the other half:
-// 4.5e-7 (512 rows: 1.3e-7, 1024: 2.1e-7; an fp32 product of the same: 5.1e-7).
+// rows that it sums alone, 1.9e-5 is lost. So a tile is summed there over 2048 rows (672 for three terms)
+// at a time, in one half of the tensor memory, and added to dW, rounded to nearest, while the matrix unit fills the
+// other half: 4.5e-7 (512 rows: 1.3e-7, 1024: 2.1e-7; an fp32 product of the same: 5.1e-7).
+//
+// What bounds it. 16384 x 4096 x 4096 bf16 takes 407 us (1350 TFLOP/s; a library product of the same sizes
+// whose operands are both bf16 in memory 330 us), 16384 x 2048 x 9472 444 us (1430). Shared memory is busy 87 % of the time
+// and the matrix unit 76 %: for 64 rows a block copies in 24 KB, reads 8 KB of codes, writes 16 KB of operand and
+// feeds 32 to 48 KB to the matrix unit, 640 to 750 cycles at 128 bytes, where the products take 512 and a stage 725.
+// With three terms a stage of 32 rows takes 900 cycles and its products 768 (4099 x 1000 x 2050 fp32: 66 us, of them 7 to split
+// dY and 5 to join the parts; with each term decoded by itself 73).
 #include <cuda.h>
 
 #include <atomic>
@@ -24,10 +32,12 @@ namespace {
 // 256 tile that halves the decoding and takes a third off the shared memory's traffic.
 constexpr int kTileN = 256, kTileK = 256;  // of dW: n from dY, k from x^
 constexpr int kBlockN = kTileN / 2, kBlockK = kTileK / 2;
-constexpr int kStages = 5;
+constexpr int kStages = 5;                  // what shared memory has room for
 constexpr int kCodeSlots = 6;               // stages of codes, ahead of the decoding
 static_assert(kCodeSlots > kStages, "see the waits of the decoding warps");
-constexpr int kLeastPart = 8;              // stages of a part
+// Stages of a part, at least: fewer do not pay for their start and for joining them. (1200 x 256 x 256 and 2048 x 512 x 512
+// bf16, 1000 x 512 x 512 fp32: 14.4, 14.4 and 16.5 us with 8; with 16 of them 16.4, 16.5 and 20.5; with 4 the same.)
+constexpr int kLeastPart = 8;
 // Warps 0-3 bring the sums out, 4-19 decode, 20 and 22 copy, 21 issues the matrix instructions (23 is idle).
 constexpr int kAdders = 128, kDecoders = 512, kThreads = kAdders + kDecoders + 128;
 constexpr int kGroups = kDecoders / 128;   // a stage is decoded by four warps
@@ -82,11 +92,12 @@ struct Shared {
     int abort;
 };
 
-// A stage is decoded by one group of four warps, the next stage by the next of four groups. Its codes come by a
+// A stage is decoded by one group of four warps, the next stage by the next of four groups, so that a group has four
+// stages' time (it takes 1600 cycles; with eight decoding warps beside eight adding ones the product took 446 us instead of 411). Its codes come by a
 // copy into a ring of their own, in rows of 128 bytes whose 16-byte chunks are swizzled like the
 // operand's. (Loads to registers a stage ahead, which is all that fits, came too late: a stage took
-// 1300 cycles to decode, twice what its products take.) A thread takes 16 columns of four rows
-// 16 apart. Four lanes take 64 columns of a row t, the next four those of row t ^ 5: so eight lanes
+// 1300 cycles to decode, twice what its products take.) A thread takes 16 columns of rows
+// 16 apart (four, or two). Four lanes take 64 columns of a row t, the next four those of row t ^ 5: so eight lanes
 // of a load (four neighbouring chunks c at c ^ (t & 7)) and of a store (every second chunk) cover all banks.
 __device__ __forceinline__ int share_row(int tid) {
     const int t = 2 * ((tid >> 4) & 7);
@@ -462,7 +473,9 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
 }
 
 // dW of the tiles whose rows were split: the parts added in their order, four columns to a thread and
-// four parts under way at a time.
+// four parts under way at a time (1024 x 1024 in four parts: 5.5 us; one column and one part at a time 22 us). It reads what
+// the L2 cache still holds. weight_grad8_kernel does not say early that it may begin: its few blocks
+// would all sit on the SMs that are free first (65536 x 256 x 256: 52 us instead of 33.5).
 __global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ WeightGrad a) {
     after_previous();
     const Plan& p = a.plan;
@@ -503,7 +516,8 @@ __global__ void __launch_bounds__(256) zero_kernel(float* dw, int64_t stride, in
 // dY as the copies want it: bf16, rows at multiples of 16 bytes. An fp32 value is the sum of three
 // bf16: its leading 8 bits, the next 8 and the last 8, cut off, so that the sum is exact and
 // nothing overflows; an infinity or NaN is carried by the first alone.
-// A thread takes four columns.
+// A thread takes four columns (4099 x 1000 fp32: 8 us; one column a thread 18). The copy is written and read once; it is small next to
+// the product that follows, whose copies want rows at multiples of 16 bytes.
 template <typename T>
 __global__ void __launch_bounds__(256) stage_dy_kernel(const T* dy, int64_t stride, int64_t rows, int64_t n_out, uint16_t* out, int64_t out_stride) {
     next_may_begin();
