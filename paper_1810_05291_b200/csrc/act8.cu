@@ -73,10 +73,20 @@ __device__ __forceinline__ void act_value_slope(float x, float* f, float* slope)
 // Bound by memory where rows start on 16 bytes: 16384 x 8192 bf16, gated silu, forward 176 and backward 176
 // us (6.1 TB/s; DRAM at 67-69 % of its nominal rate, instructions issued in 72 % of the cycles); gated gelu 203 and 199, the
 // instructions' share; pack 74 us (5.5 TB/s), unpack 68. Rows at odd places cost
-// the shifting of vectors: 4099 x 2731 gated silu 27.4 and 27.7 us (3.3 TB/s), the integer pipe 70 % busy; a column
+// the shifting of vectors: 4099 x 2731 gated silu 29.1 and 26.7 us in a row of calls (3.2 TB/s), the integer pipe 70 % busy; a column
 // to a thread, element by element, took 149 us for both passes.
 constexpr int kPiece = 8;
 constexpr int kBlock = 256;
+
+// Where rows do not start on 16 bytes: threads over which stored vectors are put together. A block's
+// for bf16 (gated silu 16384 x 8191, forward and backward: 280 and 246 us; a warp's 284 and 281), a warp's for
+// fp32 (8192 x 8191: 188 and 166 us; a block's 195 and 174).
+template <typename T>
+constexpr int kRun = sizeof(T) == 2 ? kBlock : 32;
+// Blocks that an SM holds at least. (Without the bound on registers the same took 309 and 268 us in bf16, 211 and 182 in
+// fp32; with one more block 268 and 266, and 190 and 168.)
+template <typename T>
+constexpr int kBlocks = sizeof(T) == 2 ? 5 : 4;
 
 struct Pieces {
     int64_t groups;      // of one row
@@ -191,10 +201,16 @@ struct Eight {
     }
 
     // Where rows do not start on 16 bytes, the aligned vectors that begin in the previous piece
-    // are put together from the lane before, so that all but a run's ends are whole vectors.
-    // Every lane of the warp calls it; `joined`: the lane before holds the piece before, whole.
+    // are put together from the thread before, so that all but the ends of a row, or of a run of
+    // kRun threads, are whole vectors. `joined`: the thread before holds the piece before, whole; `follows`:
+    // so does this one for the next. hand_on() comes before, and between the two every thread of the block
+    // waits for the others; a place in `ends` is used once.
     template <bool ALIGNED>
-    __device__ __forceinline__ void store(T* p, int n, bool joined) const {
+    __device__ __forceinline__ void hand_on(uint4* ends) const {
+        if (!ALIGNED && kRun<T> > 32 && (threadIdx.x & 31) == 31) ends[threadIdx.x >> 5] = make_uint4(w[kWords - 4], w[kWords - 3], w[kWords - 2], w[kWords - 1]);
+    }
+    template <bool ALIGNED>
+    __device__ __forceinline__ void store(T* p, int n, bool joined, bool follows, const uint4* ends) const {
         if (ALIGNED) {
             if (n == kPiece) {
 #pragma unroll
@@ -210,9 +226,12 @@ struct Eight {
         for (int i = 0; i < 4; ++i) x[i] = __shfl_up_sync(0xFFFFFFFFu, w[kWords - 4 + i], 1);
 #pragma unroll
         for (int i = 0; i < kWords; ++i) x[4 + i] = w[i];
+        if (kRun<T> > 32 && (threadIdx.x & 31) == 0 && joined) {
+            const uint4 v = ends[(threadIdx.x >> 5) - 1];
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        }
         const uint32_t m = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u;
-        const bool vector = joined && n == kPiece;                                   // writes from its aligned address on
-        const bool follows = __shfl_down_sync(0xFFFFFFFFu, vector, 1) && (threadIdx.x & 31) != 31;  // the next lane writes this one's end
+        const bool vector = joined && n == kPiece;  // writes from its aligned address on
         const int end = follows ? kPiece - static_cast<int>(m / sizeof(T)) : n;
         if (vector) {
             const uint32_t o = 16u - m;  // of the run, from where the vectors are taken
@@ -225,7 +244,7 @@ struct Eight {
             uint4* q = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) & ~static_cast<uintptr_t>(15));
 #pragma unroll
             for (int i = 0; i < kWords; i += 4) q[i / 4] = make_uint4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-            store_some(p, kPiece - static_cast<int>(m / sizeof(T)), follows ? 0 : kPiece);
+            if (!follows) store_some(p, kPiece - static_cast<int>(m / sizeof(T)), kPiece);
         } else {
             store_some(p, 0, end);
         }
@@ -296,10 +315,11 @@ struct Kept {
 };
 
 // Where a thread's piece lies.
+template <typename T>
 struct At {
     int64_t i, row, col;
     int n;  // columns that exist; 0 beyond the last piece
-    bool in, joined;
+    bool in, joined, follows;
 
     __device__ __forceinline__ At(const Pieces& p, int u) {
         i = (static_cast<int64_t>(blockIdx.x) * 2 + u) * kBlock + threadIdx.x;
@@ -310,9 +330,9 @@ struct At {
         col = piece * kPiece;
         const int64_t left = p.cols - col;
         n = !in || left <= 0 ? 0 : (left >= kPiece ? kPiece : static_cast<int>(left));
-        joined = in && piece > 0 && (threadIdx.x & 31) != 0;
+        joined = in && piece > 0 && threadIdx.x % kRun<T> != 0;
+        follows = in && left >= 2 * kPiece && threadIdx.x % kRun<T> != kRun<T> - 1;
     }
-    template <typename T>
     __device__ __forceinline__ T* of(const Side& m) const {
         return static_cast<T*>(m.p) + row * m.stride + col;
     }
@@ -321,17 +341,18 @@ struct At {
 // A block takes 2 * 256 pieces, both loads of a thread under way before the first is used.
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kBlock) act8_pack_kernel(const __grid_constant__ Pieces p, const __grid_constant__ Side x, const __grid_constant__ Ckpt c) {
-    const At at[2] = {At(p, 0), At(p, 1)};
+    const At<T> at[2] = {At<T>(p, 0), At<T>(p, 1)};
     Eight<T> v[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) v[u].template load<ALIGNED>(x, at[u].of<T>(x), at[u].n);
+    for (int u = 0; u < 2; ++u) v[u].template load<ALIGNED>(x, at[u].of(x), at[u].n);
 #pragma unroll
     for (int u = 0; u < 2; ++u) keep(c, at[u].i, at[u].in, v[u]);
 }
 
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kBlock) act8_unpack_kernel(const __grid_constant__ Pieces p, const __grid_constant__ Ckpt c, const __grid_constant__ Side out) {
-    const At at[2] = {At(p, 0), At(p, 1)};
+    const At<T> at[2] = {At<T>(p, 0), At<T>(p, 1)};
+    __shared__ uint4 ends[ALIGNED ? 1 : 2][kBlock / 32];
     Kept k[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -346,7 +367,10 @@ __global__ void __launch_bounds__(kBlock) act8_unpack_kernel(const __grid_consta
 #pragma unroll
             for (int j = 0; j < kPiece; ++j) v.w[j] = __float_as_uint(kept.get(j));
         }
-        v.template store<ALIGNED>(at[u].of<T>(out), at[u].n, at[u].joined);
+        uint4* const end = ends[ALIGNED ? 0 : u];
+        v.template hand_on<ALIGNED>(end);
+        if constexpr (!ALIGNED && kRun<T> > 32) __syncthreads();
+        v.template store<ALIGNED>(at[u].of(out), at[u].n, at[u].joined, at[u].follows, end);
     }
 }
 
@@ -357,13 +381,14 @@ struct Forward {
 };
 
 template <typename T, int ACT, bool GATED, bool ALIGNED>
-__global__ void __launch_bounds__(kBlock) act8_forward_kernel(const __grid_constant__ Forward a) {
-    const At at[2] = {At(a.p, 0), At(a.p, 1)};
+__global__ void __launch_bounds__(kBlock, kBlocks<T>) act8_forward_kernel(const __grid_constant__ Forward a) {
+    const At<T> at[2] = {At<T>(a.p, 0), At<T>(a.p, 1)};
+    __shared__ uint4 ends[ALIGNED ? 1 : 2][kBlock / 32];
     Eight<T> x[2], up[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        x[u].template load<ALIGNED>(a.x, at[u].of<T>(a.x), at[u].n);
-        if constexpr (GATED) up[u].template load<ALIGNED>(a.up, at[u].of<T>(a.up), at[u].n);
+        x[u].template load<ALIGNED>(a.x, at[u].of(a.x), at[u].n);
+        if constexpr (GATED) up[u].template load<ALIGNED>(a.up, at[u].of(a.up), at[u].n);
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -375,10 +400,13 @@ __global__ void __launch_bounds__(kBlock) act8_forward_kernel(const __grid_const
         }
         Eight<T> y;  // columns that do not exist: f(0) = 0
         y.set(f);
+        uint4* const end = ends[ALIGNED ? 0 : u];
+        y.template hand_on<ALIGNED>(end);
         keep(a.cx, at[u].i, at[u].in, x[u]);
         if constexpr (GATED) keep(a.cu, at[u].i, at[u].in, up[u]);
         if (a.cy.values != nullptr) keep(a.cy, at[u].i, at[u].in, y);  // of what the next layer reads
-        y.template store<ALIGNED>(at[u].of<T>(a.y), at[u].n, at[u].joined);
+        if constexpr (!ALIGNED && kRun<T> > 32) __syncthreads();  // (in place too: every thread has its inputs)
+        y.template store<ALIGNED>(at[u].of(a.y), at[u].n, at[u].joined, at[u].follows, end);
     }
 }
 
@@ -389,13 +417,14 @@ struct Backward {
 };
 
 template <typename T, int ACT, bool GATED, bool ALIGNED>
-__global__ void __launch_bounds__(kBlock) act8_backward_kernel(const __grid_constant__ Backward a) {
-    const At at[2] = {At(a.p, 0), At(a.p, 1)};
+__global__ void __launch_bounds__(kBlock, kBlocks<T>) act8_backward_kernel(const __grid_constant__ Backward a) {
+    const At<T> at[2] = {At<T>(a.p, 0), At<T>(a.p, 1)};
+    __shared__ uint4 ends[ALIGNED ? 1 : 4][kBlock / 32];
     Eight<T> dy[2];
     Kept kx[2], ku[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        dy[u].template load<ALIGNED>(a.dy, at[u].of<T>(a.dy), at[u].n);
+        dy[u].template load<ALIGNED>(a.dy, at[u].of(a.dy), at[u].n);
         if (at[u].in) {
             kx[u].load(a.cx, at[u].i);
             if constexpr (GATED) ku[u].load(a.cu, at[u].i);
@@ -417,13 +446,17 @@ __global__ void __launch_bounds__(kBlock) act8_backward_kernel(const __grid_cons
                 dx[j] = d * slope;
             }
         }
-        Eight<T> v;
-        v.set(dx);
-        v.template store<ALIGNED>(at[u].of<T>(a.dx), at[u].n, at[u].joined);
+        Eight<T> vx, vu;
+        vx.set(dx);
+        uint4 *const end_x = ends[ALIGNED ? 0 : 2 * u], *const end_u = ends[ALIGNED ? 0 : 2 * u + 1];
+        vx.template hand_on<ALIGNED>(end_x);
         if constexpr (GATED) {
-            v.set(dup);
-            v.template store<ALIGNED>(at[u].of<T>(a.dup), at[u].n, at[u].joined);
+            vu.set(dup);
+            vu.template hand_on<ALIGNED>(end_u);
         }
+        if constexpr (!ALIGNED && kRun<T> > 32) __syncthreads();  // (in place too: every thread has its inputs)
+        vx.template store<ALIGNED>(at[u].of(a.dx), at[u].n, at[u].joined, at[u].follows, end_x);
+        if constexpr (GATED) vu.template store<ALIGNED>(at[u].of(a.dup), at[u].n, at[u].joined, at[u].follows, end_u);
     }
 }
 
