@@ -4,10 +4,10 @@
 // slow, and go to the matrix unit that way, without a transpose: tiles of dY by TMA, tiles of x^
 // decoded by sixteen warps from the 8-bit codes straight into the swizzled operand layout. A decoded
 // value has 7 significant bits and is exact in bf16; no operand is rounded. An fp32 dY goes as three
-// bf16 terms whose sum it is exactly; the codes of a stage are decoded once for all three.
+// bf16 terms whose sum it is exactly, one after another over all rows.
 //
 // Sums. The matrix unit adds into fp32 with truncation: of a product with inputs of mean 0 over 16384
-// rows that it sums alone, 1.9e-5 is lost. So a tile is summed there over 2048 rows (672 for three terms)
+// rows that it sums alone, 1.9e-5 is lost. So a tile is summed there over 2048 rows
 // at a time, in one half of the tensor memory, and added to dW, rounded to nearest, while the matrix unit fills the
 // other half: 4.5e-7 (512 rows: 1.3e-7, 1024: 2.1e-7; an fp32 product of the same: 5.1e-7).
 //
@@ -15,8 +15,9 @@
 // whose operands are both bf16 in memory 330 us), 16384 x 2048 x 9472 444 us (1430). Shared memory is busy 87 % of the time
 // and the matrix unit 76 %: for 64 rows a block copies in 24 KB, reads 8 KB of codes, writes 16 KB of operand and
 // feeds 32 to 48 KB to the matrix unit, 640 to 750 cycles at 128 bytes, where the products take 512 and a stage 725.
-// With three terms a stage of 32 rows takes 900 cycles and its products 768 (4099 x 1000 x 2050 fp32: 66 us, of them 7 to split
-// dY and 5 to join the parts; with each term decoded by itself 73).
+// 4099 x 1000 x 2050 fp32 takes 73 us, of them 7 to split dY and 5 to join the parts. The three terms of 32 rows in
+// one stage, decoded once, took 66 us, but the small terms, added to the large one's sums, each cost a truncation:
+// 2.0e-6 instead of 5e-7, and at 352 rows a chunk, where it is 1.1e-6 like the plain form's, 73 us again.
 #include <cuda.h>
 
 #include <atomic>
@@ -32,32 +33,27 @@ namespace {
 // 256 tile that halves the decoding and takes a third off the shared memory's traffic.
 constexpr int kTileN = 256, kTileK = 256;  // of dW: n from dY, k from x^
 constexpr int kBlockN = kTileN / 2, kBlockK = kTileK / 2;
-constexpr int kStages = 5;                  // what shared memory has room for
-constexpr int kCodeSlots = 6;               // stages of codes, ahead of the decoding
+constexpr int kRows = 64;                  // rows of a stage
+constexpr int kStages = 5;                 // what shared memory has room for
+constexpr int kCodeSlots = 6;              // stages of codes, ahead of the decoding
 static_assert(kCodeSlots > kStages, "see the waits of the decoding warps");
+constexpr int kChunk = 32;                 // stages summed in the matrix unit
 // Stages of a part, at least: fewer do not pay for their start and for joining them. (1200 x 256 x 256 and 2048 x 512 x 512
-// bf16, 1000 x 512 x 512 fp32: 14.4, 14.4 and 16.5 us with 8; with 16 of them 16.4, 16.5 and 20.5; with 4 the same.)
+// bf16: 14.4 us with 8; with 16 of them 16.4 and 16.5; with 4 the same.)
 constexpr int kLeastPart = 8;
 // Warps 0-3 bring the sums out, 4-19 decode, 20 and 22 copy, 21 issues the matrix instructions (23 is idle).
 constexpr int kAdders = 128, kDecoders = 512, kThreads = kAdders + kDecoders + 128;
 constexpr int kGroups = kDecoders / 128;   // a stage is decoded by four warps
+constexpr uint32_t kPanel = kRows * 128;   // bytes of 64 columns of a stage
+constexpr uint32_t kBytesA = kBlockN / 64 * kPanel, kBytesB = kBlockK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
+constexpr uint32_t kCodeBytes = kRows * kBlockK;
 constexpr uint32_t kSquareBytes = 32 * 32 * 4;  // an adding warp's way out
-
-// What depends on the number of bf16 terms that dY comes in: one, or three for fp32.
-template <int TERMS>
-struct Shape {
-    static constexpr int kRows = TERMS == 1 ? 64 : 32;     // rows of a stage
-    static constexpr int kChunk = TERMS == 1 ? 32 : 21;    // stages summed in the matrix unit
-    static constexpr uint32_t kPanel = kRows * 128;        // bytes of 64 columns of a stage
-    static constexpr uint32_t kTerm = kBlockN / 64 * kPanel, kBytesA = TERMS * kTerm, kBytesB = kBlockK / 64 * kPanel, kStageBytes = kBytesA + kBytesB;
-    static constexpr uint32_t kCodeBytes = kRows * kBlockK;
-    static constexpr uint32_t kCodesAt = kStages * kStageBytes, kSquaresAt = kCodesAt + kCodeSlots * kCodeBytes;
-    static constexpr size_t kSmem = 1024 + kSquaresAt + kAdders / 32 * kSquareBytes;
-};
+constexpr size_t kSmem = 1024 + kStages * kStageBytes + kCodeSlots * kCodeBytes + kAdders / 32 * kSquareBytes;
 
 struct Plan {
     int tiles_n, tiles_k;   // tiles of dW; tile i: n index i % tiles_n
-    int stages;             // of all rows
+    int planes;             // bf16 terms of dY: 1, or 3 for fp32
+    int stages_per_plane;   // stages of one plane
     int whole;              // tiles formed by one pair of blocks from all rows
     int parts;              // parts that each of the other tiles' rows are split in
     int part_stages;
@@ -79,9 +75,10 @@ struct Unit {
 };
 
 __device__ __forceinline__ Unit unit_of(const Plan& p, int u) {
-    if (u < p.whole) return Unit{u, 0, p.stages, true};
-    const int v = u - p.whole, first = v % p.parts * p.part_stages;
-    return Unit{p.whole + v / p.parts, first, min(p.part_stages, p.stages - first), p.parts == 1};
+    if (u < p.whole) return Unit{u, 0, p.planes * p.stages_per_plane, true};
+    const int v = u - p.whole, part = v % p.parts, all = p.planes * p.stages_per_plane;
+    const int first = part * p.part_stages;
+    return Unit{p.whole + v / p.parts, first, min(p.part_stages, all - first), p.parts == 1};
 }
 
 struct Shared {
@@ -109,62 +106,61 @@ __device__ __forceinline__ int share_piece(int tid) { return tid & 3; }
 // The exponents of a group's stages, of all units of this pair, in order. For rows and columns that
 // do not exist others stand in: dY has zeros for such rows, and such columns of dW are not stored.
 // (A marked group may stand in for a row: its column is NaN anyhow.)
-template <int N>
 struct Exponents {
-    uint32_t e[N];
+    uint32_t e[4];
 };
 
 struct Walk {
-    int unit, at, end;  // the next stage, of those of its unit
-    uint32_t group;     // of columns
+    int unit, s, n;  // the next stage is the s-th of the unit's n
+    int at;          // stage of its plane
+    uint32_t group;  // of columns
 
-    __device__ __forceinline__ void enter(const WeightGrad& a, int over, uint32_t rank, int tid) {
+    __device__ __forceinline__ void enter(const WeightGrad& a, uint32_t rank, int tid) {
         if (unit >= a.plan.units) return;
         const Unit u = unit_of(a.plan, unit);
-        at = u.first + over;
-        end = u.first + u.stages;
+        n = u.stages;
+        at = (u.first + s) % a.plan.stages_per_plane;
         group = (u.tile / a.plan.tiles_n * kTileK + rank * kBlockK + 64 * share_panel(tid) + 16 * share_piece(tid)) >> 5;
         if (group >= a.x.groups) group = 0;
     }
     __device__ __forceinline__ void skip_units(const WeightGrad& a, int step, uint32_t rank, int tid) {
-        while (unit < a.plan.units && at >= end) {
+        while (unit < a.plan.units && s >= n) {
+            s -= n;
             unit += step;
-            enter(a, at - end, rank, tid);
+            enter(a, rank, tid);
         }
     }
     __device__ __forceinline__ void start(const WeightGrad& a, int first_unit, int first, int step, uint32_t rank, int tid) {
-        unit = first_unit, at = 0, end = 0;
-        enter(a, first, rank, tid);
+        unit = first_unit, s = first, n = 0;
+        enter(a, rank, tid);
         skip_units(a, step, rank, tid);
     }
-    template <int N>
-    __device__ __forceinline__ void load(const WeightGrad& a, int step, uint32_t rank, int tid, Exponents<N>* x) {
+    __device__ __forceinline__ void load(const WeightGrad& a, int step, uint32_t rank, int tid, Exponents* x) {
         if (unit >= a.plan.units) return;
-        const int last = static_cast<int>(a.rows) - 1, t = at * (16 * N) + share_row(tid);
+        const int last = static_cast<int>(a.rows) - 1, t = at * kRows + share_row(tid);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x->e[i] = a.x.exps[min(t + 16 * i, last) * a.x.groups + group];
-        at += kGroups;
+        for (int i = 0; i < 4; ++i) x->e[i] = a.x.exps[min(t + 16 * i, last) * a.x.groups + group];
+        s += kGroups;
+        for (at += kGroups; at >= a.plan.stages_per_plane;) at -= a.plan.stages_per_plane;  // the next plane goes over the same codes again
         skip_units(a, step, rank, tid);
     }
 };
 
-template <int N>
-__device__ __forceinline__ void load_codes(uint32_t codes, int tid, uint4 (&q)[N]) {
+__device__ __forceinline__ void load_codes(uint32_t codes, int tid, uint4 (&q)[4]) {
     const int t = share_row(tid);
     const uint32_t at = codes + t * 128 + (((4 * share_panel(tid) + share_piece(tid)) ^ (t & 7)) << 4);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < 4; ++i)
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[i].x), "=r"(q[i].y), "=r"(q[i].z), "=r"(q[i].w) : "r"(at + i * 16 * 128) : "memory");
 }
 
 // To the stage's operand: column chunk c (8 columns, 16 bytes) of row t of a panel sits at chunk c ^ (t & 7).
-template <int N>
-__device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const uint4 (&q)[N], const Exponents<N>& x) {
+__device__ __forceinline__ void store_codes(uint32_t stage_b, int tid, const uint4 (&q)[4], const Exponents& x) {
     const int t = share_row(tid);
-    const uint32_t at = stage_b + share_panel(tid) * (16 * N * 128) + t * 128, chunk = 2 * share_piece(tid);
+    const uint32_t at = stage_b + share_panel(tid) * kPanel + t * 128, chunk = 2 * share_piece(tid);
     const uint32_t to[2] = {at + ((chunk ^ (t & 7)) << 4), at + (((chunk + 1) ^ (t & 7)) << 4)};
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const uint32_t e2 = act8_exponent_pair(x.e[i]);
         const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
 #pragma unroll
@@ -248,10 +244,8 @@ __device__ __noinline__ void spoil(const WeightGrad& a, int pair, int pairs, int
     }
 }
 
-template <int TERMS>
 __global__ void __launch_bounds__(kThreads, 1)
 weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ WeightGrad a) {
-    using S = Shape<TERMS>;
     extern __shared__ uint8_t dynamic[];
     __shared__ Shared sh;
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
@@ -290,7 +284,7 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
     if (warp < kAdders / 32) {
         // ---- sums of the chunks, to dW: 32 rows of the tile to a warp
         const int lane = tid & 31, n_local = rank * kBlockN + warp * 32;
-        const uint32_t out = stages + S::kSquaresAt + warp * kSquareBytes;
+        const uint32_t out = stages + kStages * kStageBytes + kCodeSlots * kCodeBytes + warp * kSquareBytes;
         const uint32_t tmem_at = tmem + (static_cast<uint32_t>(warp * 32) << 16);
         const uint32_t added = cluster_addr(smem_addr(&sh.added[0]), 0);
         uint32_t chunk = 0;
@@ -300,7 +294,7 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
             const bool vectors = (reinterpret_cast<uintptr_t>(d.p) & 15) == 0 && (d.stride & 3) == 0;
             char* const row = reinterpret_cast<char*>(d.p + (lane >> 3) * d.stride + 4 * (lane & 7));
             bool add = d.add;
-            for (int left = unit_of(p, unit).stages; left > 0; left -= S::kChunk, ++chunk) {
+            for (int left = unit_of(p, unit).stages; left > 0; left -= kChunk, ++chunk) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
@@ -331,22 +325,21 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
         uint32_t parity = 1, code_parity = 0;
         for (int unit = pair; unit < p.units; unit += pairs) total += unit_of(p, unit).stages;
         Walk walk;
-        constexpr int N = S::kRows / 16;
-        Exponents<N> exps[2];
+        Exponents exps[2];
         walk.start(a, pair, group, pairs, rank, tid);
         walk.load(a, pairs, rank, tid, &exps[0]);
         walk.load(a, pairs, rank, tid, &exps[1]);
         bool ok = true;
-        auto decode = [&](Exponents<N>* x) {
-            uint4 q[N];
+        auto decode = [&](Exponents* x) {
+            uint4 q[4];
             // In this order: the slot is free once the stage five before has been used, so the codes of the stage six before have
             // come, and the wait for this stage's cannot take their arrival for one it has not seen yet.
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty + slot * 8, parity, abort));
             if (!ok) return;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(arrived + code_slot * 8, code_parity, abort));
             if (!ok) return;
-            load_codes(stages + S::kCodesAt + code_slot * S::kCodeBytes, tid, q);
-            store_codes(stages + slot * S::kStageBytes + S::kBytesA, tid, q, *x);
+            load_codes(stages + kStages * kStageBytes + code_slot * kCodeBytes, tid, q);
+            store_codes(stages + slot * kStageBytes + kBytesA, tid, q, *x);
             smem_to_async();
             __syncwarp();
             if (lane == 0) {
@@ -377,19 +370,20 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
             for (int unit = pair; unit < p.units; unit += pairs) {
                 const Unit u = unit_of(p, unit);
                 const int n0 = (u.tile % p.tiles_n) * kTileN + rank * kBlockN;
-                int t0 = u.first * S::kRows;
+                int plane = u.first / p.stages_per_plane, t0 = (u.first - plane * p.stages_per_plane) * kRows;
+                const int end = p.stages_per_plane * kRows;
 #pragma unroll 1
-                for (int s = 0; s < u.stages; ++s, ++it, t0 += S::kRows) {
+                for (int s = 0; s < u.stages; ++s) {
                     mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
-                    const uint32_t bar = full + slot * 8, dst = stages + slot * S::kStageBytes;
+                    const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
                     if (leader) {
-                        if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, 2 * S::kBytesA);
-#pragma unroll
-                        for (int term = 0; term < TERMS; ++term) {
-                            tma_load_3d_pair(dst + term * S::kTerm, &dy_map, bar, n0, t0, term);
-                            tma_load_3d_pair(dst + term * S::kTerm + S::kPanel, &dy_map, bar, n0 + 64, t0, term);
-                        }
+                        if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, 2 * kBytesA);
+                        tma_load_3d_pair(dst, &dy_map, bar, n0, t0, plane);
+                        tma_load_3d_pair(dst + kPanel, &dy_map, bar, n0 + 64, t0, plane);
                     }
+                    ++it;
+                    t0 += kRows;
+                    if (t0 == end) t0 = 0, ++plane;
                     if (++slot == kStages) slot = 0, parity ^= 1;
                 }
             }
@@ -408,15 +402,18 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
             uint32_t parity = 1;
             for (int unit = pair; unit < p.units; unit += pairs) {
                 const Unit u = unit_of(p, unit);
-                const int k0 = u.tile / p.tiles_n * kTileK + rank * kBlockK;
-                int t0 = u.first * S::kRows;
+                const int k0 = u.tile / p.tiles_n * kTileK + rank * kBlockK, end = p.stages_per_plane * kRows;
+                int t0 = u.first % p.stages_per_plane * kRows;
 #pragma unroll 1
-                for (int s = 0; s < u.stages; ++s, ++it, t0 += S::kRows) {
+                for (int s = 0; s < u.stages; ++s) {
                     mbar_wait_uniform(taken + slot * 8, parity, &sh.abort);
                     if (leader) {
-                        mbar_expect(arrived + slot * 8, S::kCodeBytes);
-                        tma_load_2d(stages + S::kCodesAt + slot * S::kCodeBytes, &x_map, arrived + slot * 8, k0, t0);
+                        mbar_expect(arrived + slot * 8, kCodeBytes);
+                        tma_load_2d(stages + kStages * kStageBytes + slot * kCodeBytes, &x_map, arrived + slot * 8, k0, t0);
                     }
+                    ++it;
+                    t0 += kRows;
+                    if (t0 == end) t0 = 0;
                     if (++slot == kCodeSlots) slot = 0, parity ^= 1;
                 }
             }
@@ -427,14 +424,14 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
             }
         } else if (warp == (kAdders + kDecoders) / 32 + 1 && rank == 0) {
             // ---- matrix unit
-            constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK), kStep = S::kStageBytes >> 4;
-            const uint64_t desc_a = tc_desc_rows(stages, S::kPanel), desc_b = tc_desc_rows(stages + S::kBytesA, S::kPanel);
+            constexpr uint32_t idesc = tc_idesc_bf16_rows(kTileN, kTileK), kStep = kStageBytes >> 4;
+            const uint64_t desc_a = tc_desc_rows(stages, kPanel), desc_b = tc_desc_rows(stages + kBytesA, kPanel);
             const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
             const bool leader = elect_one();
             uint32_t slot = 0, parity = 0, chunk = 0;
             for (int unit = pair; unit < p.units; unit += pairs) {
-                for (int left = unit_of(p, unit).stages; left > 0; left -= S::kChunk, ++chunk) {
-                    const int n = min(left, S::kChunk);
+                for (int left = unit_of(p, unit).stages; left > 0; left -= kChunk, ++chunk) {
+                    const int n = min(left, kChunk);
                     const uint32_t d = tmem + (chunk & 1) * kTileK;
                     // the half of the tensor memory is free once the chunk before the last has been added
                     if (chunk >= 2) mbar_wait_uniform(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, &sh.abort);
@@ -445,10 +442,7 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
                         const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
                         if (leader) {
 #pragma unroll
-                            for (int k = 0; k < S::kRows / 16; ++k)
-#pragma unroll
-                                for (int term = 0; term < TERMS; ++term)
-                                    tc_mma_bf16_pair(d, da + term * (S::kTerm >> 4) + k * (2048 >> 4), db + k * (2048 >> 4), idesc, s != 0 || k != 0 || term != 0);
+                            for (int k = 0; k < kRows / 16; ++k) tc_mma_bf16_pair(d, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, s != 0 || k != 0);
                             tc_commit_pair(empty + slot * 8);
                         }
                         __syncwarp();
@@ -559,7 +553,7 @@ __global__ void __launch_bounds__(256) stage_dy_kernel(const T* dy, int64_t stri
     }
 }
 
-constexpr int64_t kMaxUnits = 1 << 24;  // tiles, and stages: rows of all stages stay in 32 bits
+constexpr int64_t kMaxUnits = 1 << 24;  // tiles, and stages: rows and their products with kRows stay in 32 bits
 
 // How dY reaches the matrix unit, and how the work is cut. The pairs of blocks take whole tiles as
 // long as every pair gets one; the tiles that are left over (all, if there are fewer than pairs)
@@ -577,13 +571,12 @@ int layout_of(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int6
     out->planes = dt == SS_F32 ? 3 : 1;
     out->stride = out->staged ? (n_out + 7) / 8 * 8 : m.stride;
     out->staged_bytes = out->staged ? (out->planes * rows * out->stride * 2 + 255) / 256 * 256 : 0;
-    const int64_t tn = (n_out + kTileN - 1) / kTileN, tk = (n_in + kTileK - 1) / kTileK;
-    const int64_t stage_rows = dt == SS_F32 ? Shape<3>::kRows : Shape<1>::kRows, stages = (rows + stage_rows - 1) / stage_rows;
-    if (tn * tk > kMaxUnits || stages > kMaxUnits) return SS_ERR_UNSUPPORTED;
+    const int64_t tn = (n_out + kTileN - 1) / kTileN, tk = (n_in + kTileK - 1) / kTileK, per = (rows + kRows - 1) / kRows;
+    if (tn * tk > kMaxUnits || per * out->planes > kMaxUnits) return SS_ERR_UNSUPPORTED;
     Plan& p = out->plan;
     p.tiles_n = static_cast<int>(tn), p.tiles_k = static_cast<int>(tk);
-    const int pairs = sms / 2, tiles = static_cast<int>(tn * tk), all = static_cast<int>(stages), others = tiles % pairs;
-    p.stages = all;
+    p.planes = static_cast<int>(out->planes), p.stages_per_plane = static_cast<int>(per);
+    const int pairs = sms / 2, tiles = static_cast<int>(tn * tk), all = p.planes * p.stages_per_plane, others = tiles % pairs;
     p.whole = tiles - others;
     p.parts = 1;
     p.part_stages = all;
@@ -616,29 +609,6 @@ EncodeTiled encode_tiled(cudaError_t* err) {
         known.store(f, std::memory_order_relaxed);
     }
     return reinterpret_cast<EncodeTiled>(f);
-}
-
-template <int TERMS>
-struct TermsKernel {};
-
-template <int TERMS>
-cudaError_t launch_terms(const CUtensorMap& map, const CUtensorMap& x_map, const WeightGrad& a, int sms, cudaStream_t st) {
-    constexpr size_t kSmem = Shape<TERMS>::kSmem;
-    const cudaError_t e = allow_shared<TermsKernel<TERMS>>(reinterpret_cast<const void*>(weight_grad8_kernel<TERMS>), static_cast<int>(kSmem));
-    if (e != cudaSuccess) return e;
-    cudaLaunchAttribute at[2] = {};
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(2 * (a.plan.units < sms / 2 ? a.plan.units : sms / 2)));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmem;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = a.follows ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, weight_grad8_kernel<TERMS>, map, x_map, a);
 }
 
 // SMs that the plan is made for. Without a device (sizes asked for on a host without one) the B200's.
@@ -701,11 +671,10 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     if (e != cudaSuccess) return cuda_status_public(e);
 
     CUtensorMap map;
-    const cuuint32_t stage_rows = dt == SS_F32 ? Shape<3>::kRows : Shape<1>::kRows;
     const cuuint64_t row_bytes = static_cast<cuuint64_t>(l.stride) * 2;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(n_out), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(l.planes)};
     const cuuint64_t strides[2] = {row_bytes, l.planes > 1 ? row_bytes * rows : row_bytes};
-    const cuuint32_t box[3] = {64, stage_rows, 1}, ones[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, kRows, 1}, ones[3] = {1, 1, 1};
     void* src = l.staged ? workspace : const_cast<void*>(dy);
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, src, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
@@ -713,10 +682,13 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     CUtensorMap x_map;
     const cuuint64_t pitch = static_cast<cuuint64_t>(act8_groups(n_in)) * SS_ACT8_GROUP;
     const cuuint64_t x_dims[2] = {pitch, static_cast<cuuint64_t>(rows)};
-    const cuuint32_t x_box[2] = {kBlockK, stage_rows};
+    const cuuint32_t x_box[2] = {kBlockK, kRows};
     if (encode(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(ckpt_x), x_dims, &pitch, x_box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return SS_ERR_UNSUPPORTED;
+    e = allow_shared<WeightGrad>(reinterpret_cast<const void*>(weight_grad8_kernel), static_cast<int>(kSmem));
+    if (e != cudaSuccess) return cuda_status_public(e);
+
     if (l.staged) {
         const int64_t want = (rows * l.stride / 4 + 255) / 256, most = static_cast<int64_t>(sms) * 16;
         const unsigned grid = static_cast<unsigned>(want < most ? want : most);
@@ -727,7 +699,19 @@ int ss_weight_grad8(const void* dy, int64_t dy_stride, ss_dtype dt, const uint8_
     }
     float* partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.staged_bytes);
     const WeightGrad a{ckpt_of(const_cast<uint8_t*>(ckpt_x), rows, n_in), dw, partial, mw.stride, rows, n_out, n_in, accumulate, l.staged, l.plan};
-    e = dt == SS_F32 ? launch_terms<3>(map, x_map, a, sms, st) : launch_terms<1>(map, x_map, a, sms, st);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * (l.plan.units < sms / 2 ? l.plan.units : sms / 2)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = l.staged ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, weight_grad8_kernel, map, x_map, a);
     if (e != cudaSuccess) return cuda_status_public(e);
     if (l.plan.parts > 1) {
         const unsigned others = static_cast<unsigned>(l.plan.tiles_n * l.plan.tiles_k - l.plan.whole);
