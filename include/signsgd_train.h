@@ -100,6 +100,7 @@ int ss_act8_backward(const void* dy, int64_t dy_stride, const uint8_t* ckpt_x, c
  *   dw         out     [n_out, n_in] fp32, unit column stride, row stride dw_stride; in/out with
  *                      accumulate (a parameter's slice of a flat gradient buffer, say)
  *   workspace  scratch workspace_bytes >= ss_weight_grad8_workspace of the same arguments
+ * At most 2^30 rows (a third of that for fp32) and 2^24 tiles of 256 x 256; more is SS_ERR_UNSUPPORTED.
  * rows == 0 leaves dW as it is with accumulate and zeroes it without. Too small a workspace is
  * SS_ERR_INVALID_ARG. Sums are added to dW by the memory, which may flush a subnormal sum to zero. A
  * wait inside the kernel that ran out (it is bounded) shows as NaN in the tiles concerned.

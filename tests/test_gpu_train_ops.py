@@ -9,7 +9,7 @@ Tolerances, derived from the arithmetic:
   are exact in fp32. Sums in the matrix unit truncate: at most 2^-23 of the partial sum for each
   of the 32 steps of 16 rows between two promotions, and 2^-23 of the largest term in the
   alignment of each step, so 64 * 2^-23 of sum |dy x^| bounds an element. (Written when a promotion
-  came every 32 steps. It comes every 128 or 126 now; the tolerance is kept, though the worst case
+  came every 32 steps. It comes every 128 now; the tolerance is kept, though the worst case
   is four times as large: terms of both signs come nowhere near it.)
 * log probabilities: a difference of numbers of the size of the row's largest |c z| and of
   log(vocab), each rounded to 2^-24 a few times: 1e-6 * (max |c z| + log(vocab) + 1).
