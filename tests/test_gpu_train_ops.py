@@ -731,3 +731,39 @@ def test_scratch_memory_belongs_to_the_call_s_stream(as_handle):
     side = torch.cuda.Stream()
     for got, expected in zip(calls(side.cuda_stream if as_handle else side), want):
         assert torch.equal(got, expected)
+
+
+def test_calls_in_a_cuda_graph():
+    """Captured once, replayed on new contents of the same buffers: the bits of plain calls."""
+    rows, vocab = 40, 9001
+    z, y, w, old, rlp, adv = loss_inputs(rows, vocab, torch.bfloat16)
+    dy, x = torch.randn(700, 130, device=DEV), torch.randn(700, 96, device=DEV)
+    ck = B.act8_checkpoint(700, 96, DEV)
+    begin, seq_ref = cuts(rows, 2, 4), torch.zeros(4, device=DEV)
+    ws = torch.empty(max(B.ss_loss_workspace(rows, 2), B.ss_weight_grad8_workspace(dy, 96)), dtype=torch.uint8, device=DEV)
+    new = lambda n: torch.empty(n, device=DEV)  # noqa: E731
+    totals, logp, loss, margins, seq, dw = new(3), new(rows), new(1), new(2), new(4), new((130, 96))
+    dz, dp = torch.empty_like(z), torch.empty_like(z)
+    outs = [totals, logp, loss, margins, seq, dw, dz, dp]
+
+    def calls():
+        B.ss_policy_loss(z, y, old, rlp, adv, w, totals, logp, dz, kl_coef=0.05, workspace=ws)
+        B.ss_preference_loss(z, y, w, begin, seq_ref, loss, margins, seq, logp, dp, workspace=ws)
+        B.ss_act8_pack(x, ck)
+        B.ss_weight_grad8(dy, ck, dw, workspace=ws)
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for scale in (1.0, 0.5):
+        z.mul_(scale), x.mul_(scale)
+        for t in outs:
+            t.fill_(-7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outs))
