@@ -31,9 +31,9 @@ class Block(torch.nn.Module):
     def forward(self, x):
         kept = T.B.act8_checkpoint(x.shape[0], x.shape[1], x.device)  # one checkpoint for both projections
         T.B.ss_act8_pack(x.detach(), kept)
-        gate, up = T.linear8(x, self.gate, kept), T.linear8(x, self.up, kept)
+        gate, up = T.linear8(x, self.gate, kept, into_grad=True), T.linear8(x, self.up, kept, into_grad=True)
         h, kept_h = T.act8(gate, up, "silu", keep_output=True)
-        return x + T.linear8(h, self.down, kept_h)
+        return x + T.linear8(h, self.down, kept_h, into_grad=True)
 
 
 class Model(torch.nn.Module):
@@ -50,7 +50,7 @@ class Model(torch.nn.Module):
         x = (self.now[tokens] + self.before[previous]).bfloat16()
         for block in self.blocks:
             x = block(x)
-        return T.linear8(x, self.head)
+        return T.linear8(x, self.head, into_grad=True)
 
 
 def pairs_of(vocab, n, gen, device):

@@ -1,9 +1,9 @@
 """The training operators as autograd functions: linear layers and activations that keep their
 inputs in 8 bits for the backward pass, and losses over logits.
 
-They make the gradients that ``optim.SignumVote`` compresses: a linear layer's weight gradient is
-added straight into the parameter's ``grad``, which under ``SignumVote`` is a view of the flat
-buffer that the vote reads. Matrix products with the weights are PyTorch's; everything else of the
+They make the gradients that ``optim.SignumVote`` compresses: a linear layer's weight gradient goes
+to the parameter's ``grad``, which under ``SignumVote`` is a view of the flat buffer that the vote
+reads, through autograd or, where the layer is asked to, straight. Matrix products with the weights are PyTorch's; everything else of the
 two passes is in the kernels of ``binding`` (``include/signsgd_train.h`` has the formulas).
 """
 
@@ -20,14 +20,23 @@ PREFERENCES = {"sigmoid": B.SS_PREF_SIGMOID, "hinge": B.SS_PREF_HINGE, "squared"
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
-    """[..., cols] as a matrix with unit column stride (a view where that is possible)."""
-    m = x.reshape(-1, x.shape[-1])
+    """[..., cols] as a matrix with unit column stride (``x`` itself or a view where that is possible)."""
+    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
     return m if m.stride(1) == 1 or m.shape[1] < 2 else m.contiguous()
 
 
-def _grad_buffer(weight: torch.Tensor) -> Optional[torch.Tensor]:
+def _grad_buffer(ctx, weight: torch.Tensor) -> Optional[torch.Tensor]:
+    """``weight.grad``, if the kernel may add to it in autograd's place: a matrix that it takes, of a
+    weight that this backward pass accumulates into, and whose gradient nothing looks at on its way."""
+    if not weight.is_leaf or weight._backward_hooks or weight._post_accumulate_grad_hooks:
+        return None
     g = weight.grad
-    return g if g is not None and g.dtype == torch.float32 and g.dim() == 2 and (g.stride(1) == 1 or g.shape[1] < 2) else None
+    if g is None or g.dtype != torch.float32 or g.dim() != 2 or g.requires_grad or _rows(g) is not g:
+        return None
+    try:  # whether autograd will run the node that accumulates: not for autograd.grad, nor for other inputs alone
+        return g if torch._C._will_engine_execute_node(ctx.next_functions[1][0]) else None
+    except RuntimeError:  # autograd.grad with respect to the weight: the gradient is to be returned
+        return None
 
 
 class _Linear8(torch.autograd.Function):
@@ -48,7 +57,7 @@ class _Linear8(torch.autograd.Function):
         dx = (d @ ctx.saved_tensors[0]).view(ctx.shape) if ctx.needs_input_grad[0] else None
         dw = None
         if ctx.needs_input_grad[1]:
-            into = _grad_buffer(weight) if ctx.into_grad else None
+            into = _grad_buffer(ctx, weight) if ctx.into_grad else None
             if into is not None:                  # no second buffer, no addition afterwards
                 B.ss_weight_grad8(d, ctx.kept, into, accumulate=True)
             else:
@@ -81,13 +90,16 @@ class _Act8(torch.autograd.Function):
 
 
 def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] = None,
-            into_grad: bool = True) -> torch.Tensor:
+            into_grad: bool = False) -> torch.Tensor:
     """``x @ weight.T`` whose input is kept in 8 bits (33 bytes for 32 values) for the weight
     gradient. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
-    ``x``'s type. Where ``weight.grad`` is a float32 matrix already, the gradient is added to it
-    during the backward pass, and nothing is handed on to autograd (``into_grad=False``: always handed
-    on, as ``torch.autograd.grad`` and hooks on the weight need it). ``kept``: the checkpoint of ``x``,
-    if it is at hand (``act8`` makes its output's)."""
+    ``x``'s type. ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's).
+
+    The weight's gradient is handed on to autograd. With ``into_grad`` the kernel adds it to
+    ``weight.grad`` itself, without a buffer in between, in a backward pass that accumulates there
+    anyway; where there is no float32 ``weight.grad`` yet, or the weight has hooks, or the pass was
+    asked for other gradients, it is handed on as well. (Hooks on the node that accumulates, which
+    autograd does not show, are called without a gradient.)"""
     return _Linear8.apply(x, weight, kept, into_grad)
 
 

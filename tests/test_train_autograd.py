@@ -1,0 +1,86 @@
+"""The autograd side of the training operators on the CPU, with stand-ins for the kernels: what a backward pass
+changes, and what it refuses."""
+import pytest
+import torch
+
+from paper_1810_05291_b200 import train_ops as T
+from tests import train_ref as ref
+from tests import train_stand_ins
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    return train_stand_ins.install(monkeypatch)
+
+
+def rand(*shape, seed=0, dtype=torch.float32):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def layer(seed=0, rows=6, n_in=40, n_out=8):
+    x, w, dy = rand(rows, n_in, seed=seed), rand(n_out, n_in, seed=seed + 1), rand(rows, n_out, seed=seed + 2)
+    want = (dy.double().t() @ ref.act8(x)[2]).float()
+    return x.requires_grad_(), w.requires_grad_(), dy, want
+
+
+# ---- whose gradient a backward pass changes ---------------------------------------------------------
+# A stand-in's product is rounded once and so is its sum with what is there: 2^-23 of the terms.
+
+@pytest.mark.parametrize("options", [{}, {"into_grad": True}], ids=["default", "into_grad"])
+def test_a_gradient_of_the_input_alone_leaves_the_weight_s_as_it_is(calls, options):
+    x, w, dy, _ = layer()
+    w.grad = rand(8, 40, seed=9)
+    before = w.grad.clone()
+    torch.autograd.grad(T.linear8(x, w, **options), [x], dy)
+    assert torch.equal(w.grad, before)
+    T.linear8(x, w, **options).backward(dy, inputs=[x])
+    assert torch.equal(w.grad, before) and x.grad is not None
+
+
+@pytest.mark.parametrize("options", [{}, {"into_grad": True}], ids=["default", "into_grad"])
+def test_a_gradient_of_the_weight_is_returned_and_not_added(calls, options):
+    x, w, dy, want = layer()
+    w.grad = rand(8, 40, seed=9)
+    before = w.grad.clone()
+    got = torch.autograd.grad(T.linear8(x, w, **options), [x, w], dy)[1]
+    assert torch.equal(got, want) and torch.equal(w.grad, before)
+
+
+@pytest.mark.parametrize("options", [{}, {"into_grad": True}], ids=["default", "into_grad"])
+@pytest.mark.parametrize("where", ["before", "after"])
+def test_a_hook_on_the_weight_acts(calls, options, where):
+    x, w, dy, want = layer()
+    w.grad = torch.zeros_like(w)
+    at, seen = w.grad.data_ptr(), []
+    if where == "before":
+        w.register_hook(lambda g: 0.5 * g)
+        want = 0.5 * want
+    else:
+        w.register_post_accumulate_grad_hook(lambda p: seen.append(p.grad.clone()))
+    T.linear8(x, w, **options).backward(dy)
+    assert torch.equal(w.grad, want) and w.grad.data_ptr() == at
+    assert where == "before" or (len(seen) == 1 and torch.equal(seen[0], want))
+
+
+@pytest.mark.parametrize("options", [{}, {"into_grad": True}], ids=["default", "into_grad"])
+def test_the_weight_s_gradient_is_added_in_place(calls, options):
+    x, w, dy, want = layer()
+    start = rand(8, 40, seed=9)
+    w.grad = start.clone()
+    at = w.grad.data_ptr()
+    T.linear8(x, w, **options).backward(dy)
+    T.linear8(x, w, **options).backward(dy, inputs=[w])
+    assert torch.equal(w.grad, (start + want) + want) and w.grad.data_ptr() == at
+    w.grad = None
+    T.linear8(x, w, **options).backward(dy)
+    assert torch.equal(w.grad, want)
+
+
+def test_into_grad_forms_no_second_buffer(calls, monkeypatch):
+    x, w, dy, want = layer()
+    w.grad = torch.zeros_like(w)
+    y, made = T.linear8(x, w, into_grad=True), []
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: made.append(a))
+    y.backward(dy)
+    monkeypatch.undo()
+    assert made == [] and torch.equal(w.grad, want)
