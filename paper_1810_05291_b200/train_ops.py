@@ -4,7 +4,8 @@ inputs in 8 bits for the backward pass, and losses over logits.
 They make the gradients that ``optim.SignumVote`` compresses: a linear layer's weight gradient goes
 to the parameter's ``grad``, which under ``SignumVote`` is a view of the flat buffer that the vote
 reads, through autograd or, where the layer is asked to, straight. Matrix products with the weights are PyTorch's; everything else of the
-two passes is in the kernels of ``binding`` (``include/signsgd_train.h`` has the formulas).
+two passes is in the kernels of ``binding`` (``include/signsgd_train.h`` has the formulas). The
+kernels have no second derivatives; a backward pass through the backward pass raises.
 """
 
 from __future__ import annotations
@@ -12,6 +13,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -52,6 +54,7 @@ class _Linear8(torch.autograd.Function):
         return (m @ w.t()).view(*x.shape[:-1], weight.shape[0])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         weight, d = ctx.weight, _rows(dy)
         dx = (d @ ctx.saved_tensors[0]).view(ctx.shape) if ctx.needs_input_grad[0] else None
@@ -81,6 +84,7 @@ class _Act8(torch.autograd.Function):
         return y.view(x.shape), kept_y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, _):
         d = _rows(dy)
         dx = torch.empty(d.shape, dtype=d.dtype, device=d.device)
@@ -125,6 +129,7 @@ class _PolicyLoss(torch.autograd.Function):
         return loss, rest, logp
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g, *_):
         z = ctx.saved_tensors[0]
         dz, totals, logp = torch.empty_like(z), torch.empty(3, device=z.device), torch.empty(z.shape[0], device=z.device)
@@ -152,6 +157,7 @@ class _PreferenceLoss(torch.autograd.Function):
         return (loss,) + outs[1:]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g, *_):
         args = ctx.saved_tensors
         dz = torch.empty_like(args[0])

@@ -84,3 +84,24 @@ def test_into_grad_forms_no_second_buffer(calls, monkeypatch):
     y.backward(dy)
     monkeypatch.undo()
     assert made == [] and torch.equal(w.grad, want)
+
+
+# ---- second derivatives -------------------------------------------------------------------------------
+
+def losses(z):
+    rows = z.shape[0]
+    y, w, zero = torch.arange(rows) % z.shape[1], torch.ones(rows), torch.zeros(rows)
+    begin = torch.tensor([0, rows // 2, rows])
+    return {"policy": lambda: T.policy_loss(z, y, zero - 2, torch.ones(rows), w)[0],
+            "preference": lambda: T.preference_loss(z, y, w, begin, torch.zeros(2))[0]}
+
+
+@pytest.mark.parametrize("what", ["linear8", "act8", "gated act8", "policy", "preference"])
+def test_a_second_derivative_is_refused(calls, what):
+    """The kernels have none. A first derivative that passed for a constant would leave terms out of the second."""
+    x, w = rand(6, 40).requires_grad_(), rand(8, 40, seed=1).requires_grad_()
+    out = {"linear8": lambda: T.linear8(x, w).square().sum(), "act8": lambda: T.act8(x)[0].square().sum(),
+           "gated act8": lambda: T.act8(x, w[:6] * 2)[0].square().sum(), **losses(x)}[what]()
+    g, = torch.autograd.grad(out, [x], create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (g.square().sum() + x.square().sum()).backward()
