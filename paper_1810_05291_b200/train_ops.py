@@ -3,17 +3,18 @@ inputs in 8 bits for the backward pass, and losses over logits.
 
 They make the gradients that ``optim.SignumVote`` compresses: a linear layer's weight gradient goes
 to the parameter's ``grad``, which under ``SignumVote`` is a view of the flat buffer that the vote
-reads, through autograd or, where the layer is asked to, straight. Matrix products with the weights are PyTorch's; everything else of the
-two passes is in the kernels of ``binding`` (``include/signsgd_train.h`` has the formulas). The
-kernels have no second derivatives; a backward pass through the backward pass raises.
+reads, through autograd or, where the layer is asked to, straight. Matrix products with
+the weights are PyTorch's; everything else of the two passes is in the kernels of ``binding``
+(``include/signsgd_train.h`` has the formulas). The kernels have no second derivatives: a backward
+pass through the backward pass raises.
 """
 
 from __future__ import annotations
 
+import functools
 from typing import Optional, Tuple
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -41,6 +42,30 @@ def _grad_buffer(ctx, weight: torch.Tensor) -> Optional[torch.Tensor]:
         return None
 
 
+class _NoSecond(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, g):
+        return g.view_as(g)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the training operators have no second derivatives")
+
+
+def _first_derivative(backward):
+    """A backward pass whose results are not constants, though they carry no graph: under ``create_graph`` a
+    backward pass that reaches them raises. (``once_differentiable`` lets them pass for constants where the
+    gradient that arrives is one, as that of a sum is.)"""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        return tuple(None if g is None else _NoSecond.apply(g.requires_grad_()) for g in out)
+    return run
+
+
 class _Linear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, kept, into_grad):
@@ -54,7 +79,7 @@ class _Linear8(torch.autograd.Function):
         return (m @ w.t()).view(*x.shape[:-1], weight.shape[0])
 
     @staticmethod
-    @once_differentiable
+    @_first_derivative
     def backward(ctx, dy):
         weight, d = ctx.weight, _rows(dy)
         dx = (d @ ctx.saved_tensors[0]).view(ctx.shape) if ctx.needs_input_grad[0] else None
@@ -84,7 +109,7 @@ class _Act8(torch.autograd.Function):
         return y.view(x.shape), kept_y
 
     @staticmethod
-    @once_differentiable
+    @_first_derivative
     def backward(ctx, dy, _):
         d = _rows(dy)
         dx = torch.empty(d.shape, dtype=d.dtype, device=d.device)
@@ -129,7 +154,7 @@ class _PolicyLoss(torch.autograd.Function):
         return loss, rest, logp
 
     @staticmethod
-    @once_differentiable
+    @_first_derivative
     def backward(ctx, g, *_):
         z = ctx.saved_tensors[0]
         dz, totals, logp = torch.empty_like(z), torch.empty(3, device=z.device), torch.empty(z.shape[0], device=z.device)
@@ -157,7 +182,7 @@ class _PreferenceLoss(torch.autograd.Function):
         return (loss,) + outs[1:]
 
     @staticmethod
-    @once_differentiable
+    @_first_derivative
     def backward(ctx, g, *_):
         args = ctx.saved_tensors
         dz = torch.empty_like(args[0])

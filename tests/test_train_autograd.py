@@ -96,12 +96,22 @@ def losses(z):
             "preference": lambda: T.preference_loss(z, y, w, begin, torch.zeros(2))[0]}
 
 
-@pytest.mark.parametrize("what", ["linear8", "act8", "gated act8", "policy", "preference"])
+@pytest.mark.parametrize("what", ["linear8", "act8", "gated act8", "sum of act8", "policy", "preference"])
 def test_a_second_derivative_is_refused(calls, what):
     """The kernels have none. A first derivative that passed for a constant would leave terms out of the second."""
     x, w = rand(6, 40).requires_grad_(), rand(8, 40, seed=1).requires_grad_()
     out = {"linear8": lambda: T.linear8(x, w).square().sum(), "act8": lambda: T.act8(x)[0].square().sum(),
-           "gated act8": lambda: T.act8(x, w[:6] * 2)[0].square().sum(), **losses(x)}[what]()
+           "gated act8": lambda: T.act8(x, w[:6] * 2)[0].square().sum(), "sum of act8": lambda: T.act8(x)[0].sum(),
+           **losses(x)}[what]()
     g, = torch.autograd.grad(out, [x], create_graph=True)
-    with pytest.raises(RuntimeError, match="once_differentiable"):
+    with pytest.raises(RuntimeError, match="second derivative"):
         (g.square().sum() + x.square().sum()).backward()
+
+
+def test_create_graph_alone_is_no_error(calls):
+    x, w, dy, want = layer()
+    gx, gw = torch.autograd.grad(T.linear8(x, w), [x, w], dy, create_graph=True)
+    assert torch.equal(gw, want) and torch.equal(gx, dy @ w.detach())
+    T.linear8(x, w).backward(dy, create_graph=True)
+    assert torch.equal(w.grad, want)
+    (x * 2).sum().backward()                         # and what else the graph holds goes on
