@@ -30,8 +30,8 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
 
 def _grad_buffer(ctx, weight: torch.Tensor) -> Optional[torch.Tensor]:
     """``weight.grad``, if the kernel may add to it in autograd's place: a matrix that it takes, of a
-    weight that this backward pass accumulates into, and whose gradient nothing looks at on its way."""
-    if not weight.is_leaf or weight._backward_hooks or weight._post_accumulate_grad_hooks:
+    weight that this backward pass accumulates into, and whose gradient nothing looks at on its way or later."""
+    if ctx.create_graph or not weight.is_leaf or weight._backward_hooks or weight._post_accumulate_grad_hooks:
         return None
     g = weight.grad
     if g is None or g.dtype != torch.float32 or g.dim() != 2 or g.requires_grad or _rows(g) is not g:
@@ -58,9 +58,10 @@ def _first_derivative(backward):
     gradient that arrives is one, as that of a sum is.)"""
     @functools.wraps(backward)
     def run(ctx, *grads):
+        ctx.create_graph = torch.is_grad_enabled()
         with torch.no_grad():
             out = backward(ctx, *grads)
-        if not torch.is_grad_enabled():
+        if not ctx.create_graph:
             return out
         return tuple(None if g is None else _NoSecond.apply(g.requires_grad_()) for g in out)
     return run

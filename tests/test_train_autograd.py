@@ -115,3 +115,12 @@ def test_create_graph_alone_is_no_error(calls):
     T.linear8(x, w).backward(dy, create_graph=True)
     assert torch.equal(w.grad, want)
     (x * 2).sum().backward()                         # and what else the graph holds goes on
+
+
+def test_a_second_derivative_through_the_weight_s_grad_is_refused(calls):
+    x, w, dy, want = layer()
+    w.grad = torch.zeros_like(w)
+    T.linear8(x, w, into_grad=True).backward(dy, create_graph=True)
+    assert torch.equal(w.grad, want)
+    with pytest.raises(RuntimeError, match="second derivative"):
+        w.grad.square().sum().backward()
