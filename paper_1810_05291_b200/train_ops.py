@@ -11,6 +11,7 @@ pass through the backward pass raises.
 
 from __future__ import annotations
 
+import contextlib
 import functools
 from typing import Optional, Tuple
 
@@ -40,6 +41,25 @@ def _grad_buffer(ctx, weight: torch.Tensor) -> Optional[torch.Tensor]:
         return g if torch._C._will_engine_execute_node(ctx.next_functions[1][0]) else None
     except RuntimeError:  # autograd.grad with respect to the weight: the gradient is to be returned
         return None
+
+
+@contextlib.contextmanager
+def _in_order(node, g: torch.Tensor):
+    """Around a kernel that adds to ``g`` in the place of ``node``, autograd's node that accumulates there. Autograd
+    orders streams for the gradients that it hands on only. So the kernel comes after others that did the same on
+    another stream in this pass, and the node's stream, which the caller's waits for, comes after all of them."""
+    stream, pending = torch.cuda.current_stream(g.device), node.metadata
+    before = pending.get(_in_order)
+    if before is not None:
+        stream.wait_event(before)
+    yield
+    g.record_stream(stream)
+    pending[_in_order] = stream.record_event()
+    if before is None:
+        def wait(_):
+            torch.cuda.current_stream(g.device).wait_event(pending.pop(_in_order))
+            handle.remove()
+        handle = node.register_prehook(wait)
 
 
 class _NoSecond(torch.autograd.Function):
@@ -88,7 +108,8 @@ class _Linear8(torch.autograd.Function):
         if ctx.needs_input_grad[1]:
             into = _grad_buffer(ctx, weight) if ctx.into_grad else None
             if into is not None:                  # no second buffer, no addition afterwards
-                B.ss_weight_grad8(d, ctx.kept, into, accumulate=True)
+                with _in_order(ctx.next_functions[1][0], into):
+                    B.ss_weight_grad8(d, ctx.kept, into, accumulate=True)
             else:
                 dw = torch.empty(weight.shape, dtype=torch.float32, device=weight.device)
                 B.ss_weight_grad8(d, ctx.kept, dw)
