@@ -87,6 +87,17 @@ def _first_derivative(backward):
     return run
 
 
+def _brought(kept: torch.Tensor, m: torch.Tensor) -> torch.Tensor:
+    """A caller's checkpoint of ``m``, checked while the caller is there to see it."""
+    if kept.dtype != torch.uint8:
+        raise TypeError("kept must be uint8, got %s" % kept.dtype)
+    size = B.ss_act8_bytes(*m.shape)
+    if kept.shape != (size,) or not kept.is_contiguous() or kept.device != m.device or kept.data_ptr() % 16:
+        raise ValueError("kept must be a contiguous, 16-byte aligned tensor of %d bytes on %s, the checkpoint of [%d, %d]"
+                         % (size, m.device, *m.shape))
+    return kept
+
+
 class _Linear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, kept, into_grad):
@@ -94,25 +105,28 @@ class _Linear8(torch.autograd.Function):
         if kept is None:
             kept = B.act8_checkpoint(m.shape[0], m.shape[1], m.device)
             B.ss_act8_pack(m, kept)
+        else:
+            kept = _brought(kept, m)
         w = weight.to(x.dtype)
-        ctx.kept, ctx.weight, ctx.shape, ctx.into_grad = kept, weight, x.shape, into_grad
-        ctx.save_for_backward(w)
+        ctx.weight, ctx.shape, ctx.into_grad = weight, x.shape, into_grad
+        ctx.save_for_backward(w, kept)  # with their versions: what is written again in between is refused
         return (m @ w.t()).view(*x.shape[:-1], weight.shape[0])
 
     @staticmethod
     @_first_derivative
     def backward(ctx, dy):
         weight, d = ctx.weight, _rows(dy)
-        dx = (d @ ctx.saved_tensors[0]).view(ctx.shape) if ctx.needs_input_grad[0] else None
+        w, kept = ctx.saved_tensors
+        dx = (d @ w).view(ctx.shape) if ctx.needs_input_grad[0] else None
         dw = None
         if ctx.needs_input_grad[1]:
             into = _grad_buffer(ctx, weight) if ctx.into_grad else None
             if into is not None:                  # no second buffer, no addition afterwards
                 with _in_order(ctx.next_functions[1][0], into):
-                    B.ss_weight_grad8(d, ctx.kept, into, accumulate=True)
+                    B.ss_weight_grad8(d, kept, into, accumulate=True)
             else:
                 dw = torch.empty(weight.shape, dtype=torch.float32, device=weight.device)
-                B.ss_weight_grad8(d, ctx.kept, dw)
+                B.ss_weight_grad8(d, kept, dw)
         return dx, dw, None, None
 
 
@@ -123,9 +137,10 @@ class _Act8(torch.autograd.Function):
         new = lambda: B.act8_checkpoint(m.shape[0], m.shape[1], m.device)  # noqa: E731
         y = torch.empty(m.shape, dtype=m.dtype, device=m.device)
         ctx.act, ctx.shape = act, x.shape
-        ctx.kept, ctx.kept_up = new(), None if u is None else new()
+        kept, kept_up = new(), None if u is None else new()
         kept_y = new() if keep_output else None
-        B.ss_act8_forward(m, u, act, y, ctx.kept, ctx.kept_up, kept_y)
+        B.ss_act8_forward(m, u, act, y, kept, kept_up, kept_y)
+        ctx.save_for_backward(kept, kept_up)
         if kept_y is not None:
             ctx.mark_non_differentiable(kept_y)
         return y.view(x.shape), kept_y
@@ -135,8 +150,9 @@ class _Act8(torch.autograd.Function):
     def backward(ctx, dy, _):
         d = _rows(dy)
         dx = torch.empty(d.shape, dtype=d.dtype, device=d.device)
-        dup = None if ctx.kept_up is None else torch.empty_like(dx)
-        B.ss_act8_backward(d, ctx.kept, ctx.kept_up, ctx.act, dx, dup)
+        kept, kept_up = ctx.saved_tensors
+        dup = None if kept_up is None else torch.empty_like(dx)
+        B.ss_act8_backward(d, kept, kept_up, ctx.act, dx, dup)
         return dx.view(ctx.shape), None if dup is None else dup.view(ctx.shape), None, None
 
 
@@ -144,7 +160,8 @@ def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] 
             into_grad: bool = False) -> torch.Tensor:
     """``x @ weight.T`` whose input is kept in 8 bits (33 bytes for 32 values) for the weight
     gradient. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
-    ``x``'s type. ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's).
+    ``x``'s type. ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's);
+    its contents are needed until the backward pass, which refuses one that was written again.
 
     The weight's gradient is handed on to autograd. With ``into_grad`` the kernel adds it to
     ``weight.grad`` itself, without a buffer in between, in a backward pass that accumulates there

@@ -124,3 +124,29 @@ def test_a_second_derivative_through_the_weight_s_grad_is_refused(calls):
     assert torch.equal(w.grad, want)
     with pytest.raises(RuntimeError, match="second derivative"):
         w.grad.square().sum().backward()
+
+
+# ---- checkpoints that a caller brings -------------------------------------------------------------------
+
+def test_a_checkpoint_of_other_sizes_is_refused_at_once(calls):
+    x, w, _, _ = layer()
+    for rows, cols in ((6, 64 + 1), (5, 40), (7, 40)):
+        with pytest.raises(ValueError):
+            T.linear8(x, w, torch.empty(rows * 33 * -(-cols // 32), dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        T.linear8(x, w, torch.empty(6 * 66, dtype=torch.int8))
+    with pytest.raises(ValueError):
+        T.linear8(x, w, torch.empty(12 * 66, dtype=torch.uint8)[::2])
+
+
+def test_a_checkpoint_written_again_in_between_is_refused(calls):
+    x, w, dy, want = layer()
+    kept = torch.empty(6 * 66, dtype=torch.uint8)
+    T.B.ss_act8_pack(x.detach(), kept)
+    y = T.linear8(x, w, kept)
+    y.backward(dy)
+    assert torch.equal(w.grad, want)
+    y = T.linear8(x, w, kept)
+    kept.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward(dy)
