@@ -150,3 +150,48 @@ def test_a_checkpoint_written_again_in_between_is_refused(calls):
     kept.zero_()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward(dy)
+
+
+# ---- strides --------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("shape,over", [((6, 40), 0), ((2, 3, 40), (0, 1)), ((1, 6, 40), 1)], ids=["rows", "both", "batch of one"])
+def test_the_gradient_of_a_sum_over_rows(calls, shape, over):
+    """It arrives with a row stride of 0."""
+    x, w = rand(*shape).requires_grad_(), rand(8, 40, seed=1).requires_grad_()
+    v = rand(8, seed=2)
+    (T.linear8(x, w).sum(over) * v).sum().backward()
+    flat = x.detach().reshape(6, 40)
+    assert torch.equal(w.grad, (v.expand(6, 8).double().t() @ ref.act8(flat)[2]).float())
+    assert torch.equal(x.grad.reshape(6, 40), (v.expand(6, 8) @ w.detach()))
+    up, u = rand(*shape, seed=3).requires_grad_(), rand(40, seed=4)
+    x.grad = None
+    (T.act8(x, up)[0].sum(over) * u).sum().backward()
+    f, slope = ref.act("silu", ref.act8(flat)[2])
+    assert torch.equal(x.grad.reshape(6, 40), (u.double() * ref.act8(up.detach().reshape(6, 40))[2] * slope).float())
+    assert torch.equal(up.grad.reshape(6, 40), (u.double() * f).float())
+
+
+def test_expanded_and_overlapping_inputs(calls):
+    w, dy = rand(8, 40, seed=1).requires_grad_(), rand(6, 8, seed=2)
+    base = rand(1, 40).requires_grad_()
+    T.linear8(base.expand(6, 40), w).backward(dy)
+    want = dy.double().t() @ ref.act8(base.detach())[2].expand(6, 40)
+    assert torch.equal(w.grad, want.float())
+    assert torch.allclose(base.grad, (dy @ w.detach()).sum(0, keepdim=True), rtol=1e-5, atol=1e-5)
+    window = rand(64).as_strided((6, 40), (4, 1))           # rows overlap
+    assert torch.equal(T.act8(window)[0], ref.act("silu", window.double())[0].float())
+    gate, up = rand(6, 40, seed=5).requires_grad_(), rand(1, 40, seed=6).requires_grad_()
+    T.act8(gate, up.expand(6, 40))[0].sum().backward()
+    f = ref.act("silu", ref.act8(gate.detach())[2])[0]
+    assert torch.allclose(up.grad.double(), f.sum(0, keepdim=True), rtol=1e-5, atol=1e-6)
+    column = rand(6, 1).requires_grad_()
+    T.act8(column)[0].sum().backward()
+    assert column.grad.shape == (6, 1)
+
+
+def test_losses_of_expanded_logits(calls):
+    z = rand(1, 40).requires_grad_()
+    for loss in losses(z.expand(6, 40)).values():
+        z.grad = None
+        loss().backward()
+        assert bool(torch.isfinite(z.grad).all()) and bool(z.grad.any())

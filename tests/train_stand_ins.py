@@ -19,11 +19,15 @@ def _library_takes(*mats):
 
 
 def _pack(x, ckpt):
+    if x.numel() == 0:
+        return
     codes, exps, _, _ = ref.act8(x)
     ckpt.copy_(torch.cat([codes.reshape(-1), exps.reshape(-1)]))
 
 
 def decoded(ckpt, rows, cols):
+    if rows * cols == 0:
+        return torch.zeros(rows, cols, dtype=torch.float64)
     groups = -(-cols // ref.GROUP)
     codes, exps = ckpt[:rows * groups * ref.GROUP].long(), ckpt[rows * groups * ref.GROUP:].long()
     q = (codes & 127) * (1 - 2 * (codes >> 7))
