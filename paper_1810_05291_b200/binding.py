@@ -490,7 +490,7 @@ def ss_vote_apply_guarded_segments(packed: Sequence[torch.Tensor], param: torch.
 # ---- training operators (include/signsgd_train.h) -----------------------------------------------
 
 def _mat(t: torch.Tensor, dtype, name: str, shape=None):
-    """(address, row stride) of a 2-D CUDA tensor with unit column stride."""
+    """(address, row stride) of a 2-D CUDA tensor with unit column stride (one without elements has none)."""
     if not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor" % name)
     if t.dtype != dtype:
@@ -498,7 +498,7 @@ def _mat(t: torch.Tensor, dtype, name: str, shape=None):
     if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError("%s must have shape %s, has %s" % (name, "[rows, cols]" if shape is None else list(shape), list(t.shape)))
     stride, unit = t.stride()
-    if unit != 1 and t.shape[1] > 1:
+    if unit != 1 and t.shape[1] > 1 and t.shape[0] > 0:
         raise ValueError("%s must have unit column stride" % name)
     return t.data_ptr(), stride
 

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import contextlib
 import functools
+import math
 from typing import Optional, Tuple
 
 import torch
@@ -26,7 +27,7 @@ PREFERENCES = {"sigmoid": B.SS_PREF_SIGMOID, "hinge": B.SS_PREF_HINGE, "squared"
 def _rows(x: torch.Tensor) -> torch.Tensor:
     """[..., cols] as a matrix that the library takes: unit column stride, rows that do not overlap (``x``
     itself or a view where that is possible, not for the broadcast gradient of a sum over rows, say)."""
-    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    m = x if x.dim() == 2 else x.reshape(math.prod(x.shape[:-1]), x.shape[-1])
     fits = (m.stride(1) == 1 or m.shape[1] < 2) and (m.stride(0) >= m.shape[1] or m.shape[0] < 2)
     return m if fits else m.contiguous()
 

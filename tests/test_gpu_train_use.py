@@ -43,3 +43,32 @@ def test_checkpoints_under_inference_mode():
         y, kept = T.act8(x, keep_output=True)
         T.linear8(y, rand((8, 64), 2), kept)
     assert torch.equal(back.double(), ref.act8(x)[2])
+
+
+@pytest.mark.parametrize("shape", [(0, 40), (2, 0, 40), (3, 0), (2, 3, 0)])
+def test_empty_inputs(shape):
+    """The gradient of a sum of nothing has column stride 0."""
+    x, w = rand(shape, 1).requires_grad_(), rand((8, shape[-1]), 2).requires_grad_()
+    T.linear8(x, w).sum().backward()
+    assert w.grad.shape == w.shape and not bool(w.grad.any()) and x.grad.shape == shape
+    x.grad = None
+    T.act8(x, torch.ones(shape, device=DEV))[0].sum().backward()
+    assert x.grad.shape == shape
+    z, none = rand((0, 40), 3).requires_grad_(), torch.empty(0, device=DEV)
+    loss = T.policy_loss(z, none.long(), none, none, none)[0]
+    loss.backward()
+    assert float(loss.detach()) == 0 and z.grad.shape == z.shape
+
+
+@pytest.mark.parametrize("shape,over", [((70, 96), 0), ((2, 35, 96), (0, 1)), ((1, 70, 96), 1)], ids=["rows", "both", "batch of one"])
+def test_the_gradient_of_a_sum_over_rows(shape, over):
+    x, w, v = rand(shape, 1).requires_grad_(), rand((24, 96), 2).requires_grad_(), rand((24,), 3)
+    (T.linear8(x, w).sum(over) * v).sum().backward()
+    flat = x.detach().reshape(70, 96)
+    near(w.grad, v.expand(70, 24).double().t() @ ref.act8(flat)[2])
+    u, up = rand((96,), 4), rand((96,), 5).requires_grad_()
+    x.grad = None
+    (T.act8(x, up.expand(shape))[0].sum(over) * u).sum().backward()
+    f, slope = ref.act("silu", ref.act8(flat)[2])
+    near(x.grad.reshape(70, 96), u.double() * ref.act8(up.detach().expand(70, 96))[2] * slope)
+    near(up.grad, (u.double() * f).sum(0))

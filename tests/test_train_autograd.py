@@ -195,3 +195,15 @@ def test_losses_of_expanded_logits(calls):
         z.grad = None
         loss().backward()
         assert bool(torch.isfinite(z.grad).all()) and bool(z.grad.any())
+
+
+@pytest.mark.parametrize("shape", [(0, 40), (2, 0, 40), (3, 0), (2, 3, 0)])
+def test_empty_inputs(calls, shape):
+    x, w = rand(*shape).requires_grad_(), rand(8, shape[-1], seed=1).requires_grad_()
+    y = T.linear8(x, w)
+    assert y.shape == shape[:-1] + (8,) and not bool(y.any())
+    y.sum().backward()
+    assert w.grad.shape == w.shape and not bool(w.grad.any()) and x.grad.shape == shape
+    x.grad = None
+    T.act8(x, torch.ones(shape))[0].sum().backward()
+    assert x.grad.shape == shape

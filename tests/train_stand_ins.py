@@ -14,7 +14,7 @@ def _library_takes(*mats):
         rows, cols = m.shape
         if m.dtype not in (torch.float32, torch.bfloat16):
             raise TypeError("element type")
-        if (cols > 1 and m.stride(1) != 1) or (rows > 1 and m.stride(0) < cols):
+        if (cols > 1 and m.stride(1) != 1 and rows > 0) or (rows > 1 and m.stride(0) < cols):
             raise B.SignSGDError(B.SS_ERR_INVALID_ARG, "stand-in")
 
 
