@@ -120,7 +120,10 @@ class _Linear8(torch.autograd.Function):
     def backward(ctx, dy):
         weight, d = ctx.weight, _rows(dy)
         w, kept = ctx.saved_tensors
-        dx = (d @ w).view(ctx.shape) if ctx.needs_input_grad[0] else None
+        dx = None
+        if ctx.needs_input_grad[0]:
+            with torch.autocast(d.device.type, enabled=False):  # in the types of the forward pass
+                dx = (d @ w).view(ctx.shape)
         dw = None
         if ctx.needs_input_grad[1]:
             into = _grad_buffer(ctx, weight) if ctx.into_grad else None
@@ -163,7 +166,7 @@ def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] 
             into_grad: bool = False) -> torch.Tensor:
     """``x @ weight.T`` whose input is kept in 8 bits (33 bytes for 32 values) for the weight
     gradient. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
-    ``x``'s type. ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's);
+    ``x``'s type (under autocast, in that of the region, as other linear layers are). ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's);
     its contents are needed until the backward pass, which refuses one that was written again.
 
     The weight's gradient is handed on to autograd. With ``into_grad`` the kernel adds it to
@@ -171,6 +174,8 @@ def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] 
     anyway; where there is no float32 ``weight.grad`` yet, or the weight has hooks, or the pass was
     asked for other gradients, it is handed on as well. (Hooks on the node that accumulates, which
     autograd does not show, are called without a gradient.)"""
+    if torch.is_autocast_enabled(x.device.type) and x.dtype != torch.float64:
+        x = x.to(torch.get_autocast_dtype(x.device.type))
     return _Linear8.apply(x, weight, kept, into_grad)
 
 

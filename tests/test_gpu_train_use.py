@@ -72,3 +72,19 @@ def test_the_gradient_of_a_sum_over_rows(shape, over):
     f, slope = ref.act("silu", ref.act8(flat)[2])
     near(x.grad.reshape(70, 96), u.double() * ref.act8(up.detach().expand(70, 96))[2] * slope)
     near(up.grad, (u.double() * f).sum(0))
+
+
+def test_layers_under_autocast():
+    """An fp32 input is taken in the region's type, as other linear layers take it; gradients come back in fp32."""
+    x, w, dy = rand((70, 96), 1).requires_grad_(), rand((24, 96), 2).requires_grad_(), rand((70, 24), 3, torch.bfloat16)
+    low = x.detach().bfloat16()
+    with torch.autocast("cuda", torch.bfloat16):
+        y = T.linear8(x, w)
+        h, _ = T.act8(T.linear8(x, w), act="gelu")
+        loss = T.policy_loss(h, torch.zeros(70, dtype=torch.int64, device=DEV), *[torch.ones(70, device=DEV) for _ in range(3)])[0]
+    assert y.dtype == h.dtype == torch.bfloat16 and torch.equal(y, low @ w.detach().bfloat16().t())
+    y.backward(dy)
+    assert x.grad.dtype == torch.float32 and torch.equal(x.grad, (dy @ w.detach().bfloat16()).float())
+    near(w.grad, dy.double().t() @ ref.act8(low)[2])
+    loss.backward()
+    assert bool(torch.isfinite(w.grad).all())

@@ -207,3 +207,29 @@ def test_empty_inputs(calls, shape):
     x.grad = None
     T.act8(x, torch.ones(shape))[0].sum().backward()
     assert x.grad.shape == shape
+
+
+# ---- autocast -------------------------------------------------------------------------------------------
+
+def test_linear8_under_autocast_is_a_bf16_layer(calls):
+    x, w, dy, _ = layer()
+    start = rand(8, 40, seed=9)
+    low = x.detach().bfloat16()
+    want = dy.bfloat16().double().t() @ ref.act8(low)[2]
+    for options in ({}, {"into_grad": True}):
+        x.grad, w.grad = None, start.clone()
+        with torch.autocast("cpu", torch.bfloat16):
+            y = T.linear8(x, w, **options)
+        assert y.dtype == torch.bfloat16 and torch.equal(y, low @ w.detach().bfloat16().t())
+        y.backward(dy.bfloat16())
+        assert torch.equal(w.grad, start + want.float())
+        assert x.grad.dtype == torch.float32 and torch.equal(x.grad, (dy.bfloat16() @ w.detach().bfloat16()).float())
+
+
+def test_linear8_backward_under_autocast(calls):
+    """A backward pass inside the region computes in the types of its forward pass, as one outside does."""
+    x, w, dy, want = layer()
+    y = T.linear8(x, w)
+    with torch.autocast("cpu", torch.bfloat16):
+        y.backward(dy)
+    assert torch.equal(x.grad, dy @ w.detach()) and torch.equal(w.grad, want)
