@@ -324,15 +324,34 @@ struct PolicyRow {
         : adv(p.advantages[row]), old_logp(p.old_logp[row]), ref_logp(p.ref_logp == nullptr ? 0.0f : p.ref_logp[row]) {}
 };
 
+// exp(x) - 1 and exp(x) - 1 - x. Near 0, where a policy still is its reference, the second is x^2 / 2 and next to
+// nothing would be left of it after two differences; up to 1/2 it is its series, cut off below 2^-24 of it (x^7 / 9! of x^2).
+__device__ __forceinline__ float2 exp_less_one(float x) {
+    if (fabsf(x) < 0.5f) {
+        float q = 1.0f / 40320.0f;
+        q = fmaf(q, x, 1.0f / 5040.0f);
+        q = fmaf(q, x, 1.0f / 720.0f);
+        q = fmaf(q, x, 1.0f / 120.0f);
+        q = fmaf(q, x, 1.0f / 24.0f);
+        q = fmaf(q, x, 1.0f / 6.0f);
+        q = fmaf(q, x, 0.5f);
+        const float r = q * x * x;
+        return make_float2(x + r, r);
+    }
+    const float e = expf(x) - 1.0f;
+    return make_float2(e, e - x);
+}
+
 __device__ __forceinline__ PolicyTerm policy_term(const Policy& p, const PolicyRow& g, float logp, float w) {
     const float adv = g.adv, r = expf(logp - g.old_logp);
     const float gain = r * adv, held = fminf(fmaxf(r, p.lo), p.hi) * adv;
     const bool clipped = gain > held;
     float kl = 0.0f, dkl = 0.0f;
     if (p.ref_logp != nullptr) {
-        const float back = g.ref_logp - logp, u = expf(back);
-        kl = u - back - 1.0f;
-        dkl = 1.0f - u;
+        const float back = g.ref_logp - logp;
+        const float2 e = exp_less_one(back);
+        kl = e.y;
+        dkl = -e.x;
     }
     return PolicyTerm{w * (p.beta * kl - (clipped ? held : gain)), w * kl, clipped ? w : 0.0f,
                       w * ((clipped ? 0.0f : -gain) + p.beta * dkl)};
