@@ -142,7 +142,7 @@ int64_t ss_loss_workspace(int64_t rows, int64_t n_pairs);
  *   old_logp, advantages  in   rows fp32
  *   ref_logp              in   rows fp32, or NULL (then kl_coef must be 0 and kl_t is 0)
  *   totals                out  3 fp32: loss, sum_t weights_t kl_t, sum_t weights_t [clipped]
- * 0 <= clip_low <= 1, 0 <= clip_high, kl_coef finite.
+ * 0 <= clip_low <= 1, 0 <= clip_high, kl_coef finite; 0 leaves the KL term out of loss and gradient, be it infinite.
  */
 int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64_t rows, int64_t vocab,
                    const int64_t* targets, const float* old_logp, const float* ref_logp, const float* advantages,
@@ -166,7 +166,7 @@ int ss_policy_loss(const void* logits, int64_t logits_stride, ss_dtype dt, int64
  *   loss          out  1 fp32
  *   margins       out  n_pairs fp32: m_p
  *   seq_logp      out  2 n_pairs fp32: S_s
- * beta > 0, 0 <= label_smoothing <= 1/2 (0 unless SS_PREF_SIGMOID).
+ * beta > 0, 0 <= label_smoothing <= 1/2 (0 unless SS_PREF_SIGMOID; 0 leaves the second term out, be it infinite).
  */
 typedef enum { SS_PREF_SIGMOID = 0, SS_PREF_HINGE = 1, SS_PREF_SQUARED = 2 } ss_pref;
 

@@ -353,8 +353,9 @@ __device__ __forceinline__ PolicyTerm policy_term(const Policy& p, const PolicyR
         kl = e.y;
         dkl = -e.x;
     }
-    return PolicyTerm{w * (p.beta * kl - (clipped ? held : gain)), w * kl, clipped ? w : 0.0f,
-                      w * ((clipped ? 0.0f : -gain) + p.beta * dkl)};
+    const bool penalty = p.beta != 0.0f;  // a coefficient of 0 leaves the term out, an infinite one too
+    return PolicyTerm{w * ((penalty ? p.beta * kl : 0.0f) - (clipped ? held : gain)), w * kl, clipped ? w : 0.0f,
+                      w * ((clipped ? 0.0f : -gain) + (penalty ? p.beta * dkl : 0.0f))};
 }
 
 __device__ __forceinline__ void store_term(const Logits& a, const Policy& p, int64_t rows, int64_t row, float logp, const PolicyTerm& t) {
@@ -702,7 +703,7 @@ __global__ void __launch_bounds__(kSumThreads) pair_kernel(const __grid_constant
     if (p.kind == SS_PREF_SIGMOID) {
         const float lost = log1pf(expf(-fabsf(m)));  // -log sigma(|m|)
         const float plus = lost + fmaxf(-m, 0.0f), minus = lost + fmaxf(m, 0.0f);
-        loss = (1.0f - p.smoothing) * plus + p.smoothing * minus;
+        loss = (1.0f - p.smoothing) * plus + (p.smoothing != 0.0f ? p.smoothing * minus : 0.0f);  // minus may be infinite
         slope = p.beta * (p.smoothing / (1.0f + expf(-m)) - (1.0f - p.smoothing) / (1.0f + expf(m)));
     } else if (p.kind == SS_PREF_HINGE) {
         loss = 1.0f - m > 0.0f ? 1.0f - m : (m >= 1.0f ? 0.0f : m);

@@ -54,3 +54,33 @@ def test_the_kl_term_near_its_zero(size, vocab):
         w[k] = 1.0
         alone = policy(z, y, logp, rlp, zero, w, None, kl_coef=1.0)[0]
         assert float(alone[1]) >= 0.0
+
+
+def test_a_kl_coefficient_of_zero_leaves_the_term_out():
+    """A reference given for the figure alone: where the KL term is infinite, loss and gradient are those without it."""
+    z, y = confident(6, 300, 7)
+    z[2, y[2]] = float("-inf")                       # a token that this policy cannot take: logp is -inf, the term has no end
+    one = torch.ones(6, device=DEV)
+    old, rlp, adv = -one, -one, torch.tensor([1.0, -1.0] * 3, device=DEV)
+    rlp[4] = 200.0                                   # the term overflows
+    dz, plain = torch.empty_like(z), torch.empty_like(z)
+    totals, logp = policy(z, y, old, rlp, adv, one, dz, kl_coef=0.0)
+    want, _ = policy(z, y, old, None, adv, one, plain)
+    assert torch.equal(totals[[0, 2]], want[[0, 2]]) and torch.equal(dz, plain) and bool(torch.isfinite(dz).all())
+    assert not bool(torch.isfinite(totals[1]))       # the figure says what it is
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.25])
+def test_a_label_smoothing_of_zero_leaves_the_term_out(smoothing):
+    """A rejected answer with a token that cannot be taken: the margin is +inf, -log sigma of it is 0."""
+    z, y = confident(8, 300, 8)
+    z[5, y[5]] = float("-inf")
+    begin, w = torch.tensor([0, 4, 8], device=DEV), torch.ones(8, device=DEV)
+    loss, margins, seq, logp = torch.empty(1, device=DEV), torch.empty(1, device=DEV), torch.empty(2, device=DEV), torch.empty(8, device=DEV)
+    dz = torch.empty_like(z)
+    B.ss_preference_loss(z, y, w, begin, torch.zeros(2, device=DEV), loss, margins, seq, logp, dz, label_smoothing=smoothing)
+    assert float(margins) == float("inf") and float(seq[1]) == float("-inf")
+    if smoothing == 0.0:
+        assert float(loss) == 0.0 and not bool(dz.any())
+    else:
+        assert float(loss) == float("inf")
