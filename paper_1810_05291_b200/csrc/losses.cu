@@ -443,6 +443,21 @@ struct Given {
     __device__ __forceinline__ bool live() const { return target >= 0; }
 };
 
+// The end of a block in which a wait of thread 0 ran out, by that thread. (Where they were all met, every copy and message to the
+// block has arrived.) Waits, with limits, for the copies that are still under way, and for the messages after every other
+// block of the cluster has sent its own or has ended.
+__device__ __noinline__ void drain(uint64_t* arrived, int slots, uint64_t* told, uint32_t size, uint32_t live_rows) {
+    int own = 0;
+    for (int i = 0; i < slots; ++i) {  // the phase that has not completed is the copy's, if there is one
+        const uint32_t bar = smem_addr(&arrived[i]), parity = mbar_try(bar, 0) ? 1 : 0;
+        mbar_wait(bar, parity, &own, kMaxTries >> 6);
+    }
+    if (size < 2) return;
+    asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    for (uint32_t i = 0; i < 2; ++i)
+        if (const uint32_t rounds = (live_rows + 1 - i) >> 1) mbar_wait(smem_addr(&told[i]), (rounds - 1) & 1, &own);
+}
+
 template <typename T, int HELD>
 __global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slice_kernel(const __grid_constant__ Logits a, const __grid_constant__ Policy p, const __grid_constant__ Slices c) {
     next_may_begin();
@@ -470,7 +485,7 @@ __global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slic
         mbar_init_visible();
     }
     auto slot_of = [&](int i) { return reinterpret_cast<uint4*>(dynamic) + (kSlots == 2 ? i & 1 : 0) * c.vectors; };
-    auto fetch = [&](int i) {  // by one thread: the whole vectors of the slice
+    auto fetch = [&](int i) {  // by thread 0: the whole vectors of the slice
         const Row<T> z(z0 + (row0 + i) * a.z_stride, a.vocab);
         const uint32_t from = max(begin, z.lo), to = min(stop, z.hi), bytes = to > from ? (to - from) * 16 : 0;
         const uint32_t bar = smem_addr(&arrived[kSlots == 2 ? i & 1 : 0]);
@@ -498,7 +513,7 @@ __global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slic
         if (!now.live()) {  // for every block of the cluster
             zero_of(dz, begin, rank + 1 == size ? 0xFFFFFFFFu : stop, t, THREADS);
             if (rank == 0 && t == 0) store_term(a, p, c.rows, row, 0.0f, PolicyTerm{0.0f, 0.0f, 0.0f, 0.0f});
-            if (fetch_next && t == 0) fetch(i + kSlots);
+            if (fetch_next && t == 0 && ok) fetch(i + kSlots);  // once a wait ran out, nothing more is begun
         } else {
             const int slot = kSlots == 2 ? i & 1 : 0, set = live_rows & 1;
             const PolicyRow given(p, row);
@@ -540,7 +555,7 @@ __global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slic
             if (!ok) s.s = __uint_as_float(0x7FC00000u);  // a copy that did not arrive shows
             s = row_join<THREADS>(s, shared[set], k);
             // the block is past a barrier: its slot has been read
-            if (fetch_next && t == 0) fetch(i + kSlots);
+            if (fetch_next && t == 0 && ok) fetch(i + kSlots);  // once a wait ran out, nothing more is begun
             if (size > 1) {
                 if (t < size) tell(smem_addr(&joined[set][rank]), smem_addr(&told[set]), t, make_float4(s.m, s.s, picked, 0.0f));
                 ok = mbar_wait(smem_addr(&told[set]), (live_rows >> 1) & 1, &abort) && ok;
@@ -592,6 +607,7 @@ __global__ void __launch_bounds__(kSliceThreads, kSliceBlocks<HELD>) policy_slic
         now = next;
         next = later;
     }
+    if (t == 0 && !ok) drain(arrived, kSlots, told, size, live_rows);
 }
 
 constexpr int kSumThreads = 1024;

@@ -42,9 +42,9 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 // after a number of tries that no working launch comes near (a try suspends for a while by
 // itself), or when another thread of the block has given up.
 constexpr int kMaxTries = 1 << 20;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort, int tries = kMaxTries) {
 #pragma unroll 1
-    for (int i = 0; i < kMaxTries; ++i) {
+    for (int i = 0; i < tries; ++i) {
         if (mbar_try(bar, parity)) return true;
         if ((i & 63) == 63 && *abort != 0) return false;
     }
