@@ -78,9 +78,12 @@ class _NoSecond(torch.autograd.Function):
 def _first_derivative(backward):
     """A backward pass whose results are not constants, though they carry no graph: under ``create_graph`` a
     backward pass that reaches them raises. (``once_differentiable`` lets them pass for constants where the
-    gradient that arrives is one, as that of a sum is.)"""
+    gradient that arrives is one, as that of a sum is.) It is called with a gradient of its first result; the
+    others have none, and no zeros are made for them (the forward pass says so)."""
     @functools.wraps(backward)
     def run(ctx, *grads):
+        if grads[0] is None:
+            return (None,) * len(ctx.needs_input_grad)
         ctx.create_graph = torch.is_grad_enabled()
         with torch.no_grad():
             out = backward(ctx, *grads)
@@ -104,6 +107,7 @@ def _brought(kept: torch.Tensor, m: torch.Tensor) -> torch.Tensor:
 class _Linear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, kept, into_grad):
+        ctx.set_materialize_grads(False)
         m = _rows(x)
         if kept is None:
             kept = B.act8_checkpoint(m.shape[0], m.shape[1], m.device)
@@ -139,6 +143,7 @@ class _Linear8(torch.autograd.Function):
 class _Act8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, up, act, keep_output):
+        ctx.set_materialize_grads(False)
         m, u = _rows(x), None if up is None else _rows(up)
         new = lambda: B.act8_checkpoint(m.shape[0], m.shape[1], m.device)  # noqa: E731
         y = torch.empty(m.shape, dtype=m.dtype, device=m.device)
@@ -189,6 +194,7 @@ def act8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: str = "silu",
 class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, old_logp, ref_logp, advantages, weights, inv_temperature, clip_low, clip_high, kl_coef):
+        ctx.set_materialize_grads(False)
         z = _rows(logits)
         args = (z, targets, old_logp, ref_logp, advantages, weights)
         ctx.save_for_backward(*args)
@@ -218,6 +224,7 @@ def _preference_outputs(args):
 class _PreferenceLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, weights, seq_begin, ref_seq_logp, options):
+        ctx.set_materialize_grads(False)
         z = _rows(logits)
         args = (z, targets, weights, seq_begin, ref_seq_logp)
         ctx.save_for_backward(*args)

@@ -88,3 +88,16 @@ def test_layers_under_autocast():
     near(w.grad, dy.double().t() @ ref.act8(low)[2])
     loss.backward()
     assert bool(torch.isfinite(w.grad).all())
+
+
+def test_the_backward_pass_of_an_activation_makes_no_buffer_for_the_checkpoint():
+    """At its peak it holds its two gradients beside what was there; a gradient of kept_y would be 1056 bytes a row more."""
+    rows, cols = 4096, 1024
+    x, up = (rand((rows, cols), k, torch.bfloat16).requires_grad_() for k in (1, 2))
+    dy = rand((rows, cols), 3, torch.bfloat16)
+    y, kept = T.act8(x, up, keep_output=True)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    y.backward(dy)
+    assert torch.cuda.max_memory_allocated() - before <= 2 * rows * cols * 2 + 4096

@@ -233,3 +233,43 @@ def test_linear8_backward_under_autocast(calls):
     with torch.autocast("cpu", torch.bfloat16):
         y.backward(dy)
     assert torch.equal(x.grad, dy @ w.detach()) and torch.equal(w.grad, want)
+
+
+# ---- work that nobody asked for -------------------------------------------------------------------------
+
+def test_the_checkpoint_of_the_result_gets_no_gradient(calls, monkeypatch):
+    """PyTorch fills one with zeros unless it is told not to."""
+    made = []
+    for name, f in (("act8", T._Act8), ("linear8", T._Linear8), ("policy", T._PolicyLoss), ("preference", T._PreferenceLoss)):
+        def watch(ctx, *grads, _run=f.backward, _name=name):
+            made.append((_name, [g is None for g in grads]))
+            return _run(ctx, *grads)
+        monkeypatch.setattr(f, "backward", staticmethod(watch))
+    x, up, w = rand(6, 40).requires_grad_(), rand(6, 40, seed=1).requires_grad_(), rand(8, 40, seed=2).requires_grad_()
+    y, kept = T.act8(x, up, keep_output=True)
+    z = T.linear8(y, w, kept)
+    (losses(z)["policy"]() + losses(z)["preference"]()).backward()
+    assert sorted(made) == [("act8", [False, True]), ("linear8", [False]), ("policy", [False, True, True]),
+                            ("preference", [False, True, True, True])]
+
+
+def test_a_result_without_a_gradient(calls):
+    """A Function whose result is left out of the loss, beside one that is not."""
+    class Both(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, a, b):
+            ctx.set_materialize_grads(False)
+            return a * 2, b * 2
+
+        @staticmethod
+        def backward(ctx, da, db):
+            return None, db * 2
+
+    x, w = rand(6, 40).requires_grad_(), rand(8, 40, seed=2).requires_grad_()
+    y, other = T.act8(T.linear8(x, w))[0], rand(6, 8, seed=3).requires_grad_()
+    Both.apply(y, other)[1].sum().backward()
+    assert x.grad is None and w.grad is None and torch.equal(other.grad, torch.full((6, 8), 2.0))
+    z = rand(6, 40, seed=4).requires_grad_()
+    for loss in losses(z).values():
+        Both.apply(loss(), other.sum())[1].backward()
+        assert z.grad is None
