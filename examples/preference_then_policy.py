@@ -29,10 +29,12 @@ class Block(torch.nn.Module):
         self.gate, self.up, self.down = new(hidden, width), new(hidden, width), new(width, hidden)
 
     def forward(self, x):
-        kept = T.B.act8_checkpoint(x.shape[0], x.shape[1], x.device)  # one checkpoint for both projections
-        T.B.ss_act8_pack(x.detach(), kept)
+        kept = None
+        if torch.is_grad_enabled():  # one checkpoint for both projections
+            kept = T.B.act8_checkpoint(x.shape[0], x.shape[1], x.device)
+            T.B.ss_act8_pack(x.detach(), kept)
         gate, up = T.linear8(x, self.gate, kept, into_grad=True), T.linear8(x, self.up, kept, into_grad=True)
-        h, kept_h = T.act8(gate, up, "silu", keep_output=True)
+        h, kept_h = T.act8(gate, up, "silu", keep_output=torch.is_grad_enabled())
         return x + T.linear8(h, self.down, kept_h, into_grad=True)
 
 

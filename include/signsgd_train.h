@@ -72,8 +72,8 @@ int ss_act8_unpack(const uint8_t* ckpt, int64_t rows, int64_t cols, void* out, i
  * computed from the unrounded x and up.
  *   x, up    in   [rows, cols] of dt; up may be NULL
  *   y        out  [rows, cols] of dt; may be x or up in place
- *   ckpt_x   out  checkpoint of x
- *   ckpt_up  out  checkpoint of up; required if and only if up is given
+ *   ckpt_x   out  checkpoint of x; or NULL: nothing is kept of the inputs (no backward pass follows)
+ *   ckpt_up  out  checkpoint of up; required if and only if up and ckpt_x are given
  *   ckpt_y   out  checkpoint of y as stored (after its rounding to dt), the input of the layer
  *                 that follows; or NULL
  */

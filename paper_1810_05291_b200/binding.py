@@ -566,8 +566,8 @@ def ss_act8_unpack(ckpt: torch.Tensor, out: torch.Tensor, stream=None) -> None:
            "ss_act8_unpack")
 
 
-def ss_act8_forward(x: torch.Tensor, up: Optional[torch.Tensor], act: int, y: torch.Tensor, ckpt_x: torch.Tensor,
-                    ckpt_up: Optional[torch.Tensor] = None, ckpt_y: Optional[torch.Tensor] = None,
+def ss_act8_forward(x: torch.Tensor, up: Optional[torch.Tensor], act: int, y: torch.Tensor,
+                    ckpt_x: Optional[torch.Tensor] = None, ckpt_up: Optional[torch.Tensor] = None, ckpt_y: Optional[torch.Tensor] = None,
                     stream=None) -> None:
     code, dt, shape = _dtype_code(x), x.dtype, x.shape
     x_ptr, x_stride = _mat(x, dt, "x")
@@ -575,7 +575,7 @@ def ss_act8_forward(x: torch.Tensor, up: Optional[torch.Tensor], act: int, y: to
     u_ptr, u_stride = (None, 0) if up is None else _mat(up, dt, "up", shape)
     y_ptr, y_stride = _mat(y, dt, "y", shape)
     _check(lib().ss_act8_forward(x_ptr, x_stride, u_ptr, u_stride, code, act, rows, cols, y_ptr, y_stride,
-                                 _ckpt(ckpt_x, rows, cols, "ckpt_x"),
+                                 None if ckpt_x is None else _ckpt(ckpt_x, rows, cols, "ckpt_x"),
                                  None if ckpt_up is None else _ckpt(ckpt_up, rows, cols, "ckpt_up"),
                                  None if ckpt_y is None else _ckpt(ckpt_y, rows, cols, "ckpt_y"), _stream(stream)),
            "ss_act8_forward")

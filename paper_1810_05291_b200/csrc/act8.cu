@@ -380,7 +380,9 @@ struct Forward {
     Ckpt cx, cu, cy;
 };
 
-template <typename T, int ACT, bool GATED, bool ALIGNED>
+// KEEP: the inputs' checkpoints are written. (A test of the pointer in the kernel instead: gated silu 4099 x 2736 bf16 20.5 us
+// instead of 19.7, 16384 x 8192 172.6 instead of 170.3.)
+template <typename T, int ACT, bool GATED, bool ALIGNED, bool KEEP>
 __global__ void __launch_bounds__(kBlock, kBlocks<T>) act8_forward_kernel(const __grid_constant__ Forward a) {
     const At<T> at[2] = {At<T>(a.p, 0), At<T>(a.p, 1)};
     __shared__ uint4 ends[ALIGNED ? 1 : 2][kBlock / 32];
@@ -402,8 +404,10 @@ __global__ void __launch_bounds__(kBlock, kBlocks<T>) act8_forward_kernel(const 
         y.set(f);
         uint4* const end = ends[ALIGNED ? 0 : u];
         y.template hand_on<ALIGNED>(end);
-        keep(a.cx, at[u].i, at[u].in, x[u]);
-        if constexpr (GATED) keep(a.cu, at[u].i, at[u].in, up[u]);
+        if constexpr (KEEP) {
+            keep(a.cx, at[u].i, at[u].in, x[u]);
+            if constexpr (GATED) keep(a.cu, at[u].i, at[u].in, up[u]);
+        }
         if (a.cy.values != nullptr) keep(a.cy, at[u].i, at[u].in, y);  // of what the next layer reads
         if constexpr (!ALIGNED && kRun<T> > 32) __syncthreads();  // (in place too: every thread has its inputs)
         y.template store<ALIGNED>(at[u].of(a.y), at[u].n, at[u].joined, at[u].follows, end);
@@ -554,15 +558,16 @@ int ss_act8_forward(const void* x, int64_t x_stride, const void* up, int64_t up_
                     uint8_t* ckpt_y, void* cuda_stream) {
     if (!dtype_known(dt) || (act != SS_ACT_GELU && act != SS_ACT_SILU) || !sides_ok(rows, cols)) return SS_ERR_INVALID_ARG;
     if (!stride_ok(rows, cols, x_stride) || !stride_ok(rows, cols, y_stride)) return SS_ERR_INVALID_ARG;
-    if ((up != nullptr) != (ckpt_up != nullptr) || (up != nullptr && !stride_ok(rows, cols, up_stride))) return SS_ERR_INVALID_ARG;
+    if ((up == nullptr && ckpt_up != nullptr) || (up != nullptr && !stride_ok(rows, cols, up_stride))) return SS_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return SS_OK;
+    if (up != nullptr && (ckpt_x != nullptr) != (ckpt_up != nullptr)) return SS_ERR_INVALID_ARG;
     const size_t eb = dtype_bytes(dt), kept = ss_act8_bytes(rows, cols);
     const Mat mx = mat(x, rows, cols, x_stride, eb), my = mat(y, rows, cols, y_stride, eb);
     const Mat mu = mat(up, rows, cols, up_stride, eb);
     SS_TRY(mat_check(mx, x_stride));
     SS_TRY(mat_check(my, y_stride));
     if (up != nullptr) SS_TRY(mat_check(mu, up_stride));
-    SS_TRY(ckpt_check(ckpt_x));
+    if (ckpt_x != nullptr) SS_TRY(ckpt_check(ckpt_x));
     if (ckpt_up != nullptr) SS_TRY(ckpt_check(ckpt_up));
     if (ckpt_y != nullptr) SS_TRY(ckpt_check(ckpt_y));
     if (mats_overlap(my, mx) && !same_mat(my, mx)) return SS_ERR_INVALID_ARG;
@@ -579,8 +584,9 @@ int ss_act8_forward(const void* x, int64_t x_stride, const void* up, int64_t up_
                     ckpt_of(ckpt_up, rows, cols), ckpt_of(ckpt_y, rows, cols)};
     const bool aligned = mx.row_aligned(16) && my.row_aligned(16) && (up == nullptr || mu.row_aligned(16));
     pick(dt, aligned, act, up != nullptr, [&](auto t, auto al, auto f, auto gated) {
-        act8_forward_kernel<decltype(t), f.value, gated.value, al.value>
-            <<<piece_grid(a.p), kBlock, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
+        const auto kernel = ckpt_x != nullptr ? act8_forward_kernel<decltype(t), f.value, gated.value, al.value, true>
+                                              : act8_forward_kernel<decltype(t), f.value, gated.value, al.value, false>;
+        kernel<<<piece_grid(a.p), kBlock, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
     });
     return cuda_status_public(cudaGetLastError());
 }

@@ -106,14 +106,14 @@ def _brought(kept: torch.Tensor, m: torch.Tensor) -> torch.Tensor:
 
 class _Linear8(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, kept, into_grad):
+    def forward(ctx, x, weight, kept, into_grad, wanted):
         ctx.set_materialize_grads(False)
         m = _rows(x)
-        if kept is None:
+        if kept is not None:
+            kept = _brought(kept, m)
+        elif wanted:
             kept = B.act8_checkpoint(m.shape[0], m.shape[1], m.device)
             B.ss_act8_pack(m, kept)
-        else:
-            kept = _brought(kept, m)
         w = weight.to(x.dtype)
         ctx.weight, ctx.shape, ctx.into_grad = weight, x.shape, into_grad
         ctx.save_for_backward(w, kept)  # with their versions: what is written again in between is refused
@@ -137,18 +137,18 @@ class _Linear8(torch.autograd.Function):
             else:
                 dw = torch.empty(weight.shape, dtype=torch.float32, device=weight.device)
                 B.ss_weight_grad8(d, kept, dw)
-        return dx, dw, None, None
+        return dx, dw, None, None, None
 
 
 class _Act8(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, up, act, keep_output):
+    def forward(ctx, x, up, act, keep_output, wanted):
         ctx.set_materialize_grads(False)
         m, u = _rows(x), None if up is None else _rows(up)
         new = lambda: B.act8_checkpoint(m.shape[0], m.shape[1], m.device)  # noqa: E731
         y = torch.empty(m.shape, dtype=m.dtype, device=m.device)
         ctx.act, ctx.shape = act, x.shape
-        kept, kept_up = new(), None if u is None else new()
+        kept, kept_up = new() if wanted else None, new() if wanted and u is not None else None
         kept_y = new() if keep_output else None
         B.ss_act8_forward(m, u, act, y, kept, kept_up, kept_y)
         ctx.save_for_backward(kept, kept_up)
@@ -164,13 +164,13 @@ class _Act8(torch.autograd.Function):
         kept, kept_up = ctx.saved_tensors
         dup = None if kept_up is None else torch.empty_like(dx)
         B.ss_act8_backward(d, kept, kept_up, ctx.act, dx, dup)
-        return dx.view(ctx.shape), None if dup is None else dup.view(ctx.shape), None, None
+        return dx.view(ctx.shape), None if dup is None else dup.view(ctx.shape), None, None, None
 
 
 def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] = None,
             into_grad: bool = False) -> torch.Tensor:
     """``x @ weight.T`` whose input is kept in 8 bits (33 bytes for 32 values) for the weight
-    gradient. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
+    gradient, if one can be asked for. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
     ``x``'s type (under autocast, in that of the region, as other linear layers are). ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's);
     its contents are needed until the backward pass, which refuses one that was written again.
 
@@ -181,14 +181,15 @@ def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] 
     autograd does not show, are called without a gradient.)"""
     if torch.is_autocast_enabled(x.device.type) and x.dtype != torch.float64:
         x = x.to(torch.get_autocast_dtype(x.device.type))
-    return _Linear8.apply(x, weight, kept, into_grad)
+    return _Linear8.apply(x, weight, kept, into_grad, torch.is_grad_enabled() and weight.requires_grad)
 
 
 def act8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: str = "silu",
          keep_output: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
-    """``f(x)`` or ``f(x) * up`` whose inputs are kept in 8 bits. Returns the result and, with
+    """``f(x)`` or ``f(x) * up`` whose inputs are kept in 8 bits, if a gradient can be asked for. Returns the result and, with
     ``keep_output``, its checkpoint for the ``linear8`` that follows (else None)."""
-    return _Act8.apply(x, up, ACTIVATIONS[act], keep_output)
+    wanted = torch.is_grad_enabled() and (x.requires_grad or (up is not None and up.requires_grad))
+    return _Act8.apply(x, up, ACTIVATIONS[act], keep_output, wanted)
 
 
 class _PolicyLoss(torch.autograd.Function):

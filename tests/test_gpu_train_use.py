@@ -101,3 +101,25 @@ def test_the_backward_pass_of_an_activation_makes_no_buffer_for_the_checkpoint()
     before = torch.cuda.memory_allocated()
     y.backward(dy)
     assert torch.cuda.max_memory_allocated() - before <= 2 * rows * cols * 2 + 4096
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("shape", [(1, 1), (37, 130), (64, 256)])
+def test_an_activation_that_keeps_nothing(shape, gated, dtype):
+    """The bits of the one that does, and, where asked for, the same checkpoint of the result."""
+    x, up = rand(shape, 1, dtype), rand(shape, 2, dtype) if gated else None
+    new = lambda: B.act8_checkpoint(*shape, DEV)  # noqa: E731
+    y, ck = torch.empty_like(x), new()
+    B.ss_act8_forward(x, up, B.SS_ACT_GELU, y, new(), new() if gated else None, ck)
+    alone, only = torch.empty_like(x), new()
+    B.ss_act8_forward(x, up, B.SS_ACT_GELU, alone)
+    assert torch.equal(alone, y)
+    B.ss_act8_forward(x, up, B.SS_ACT_GELU, alone.zero_(), None, None, only)
+    assert torch.equal(alone, y) and torch.equal(only, ck)
+    with torch.no_grad():
+        assert torch.equal(T.act8(x, up, "gelu")[0], y)
+    if gated:
+        for kept in ((new(), None), (None, new())):
+            with pytest.raises(B.SignSGDError):
+                B.ss_act8_forward(x, up, B.SS_ACT_GELU, alone, *kept)

@@ -273,3 +273,31 @@ def test_a_result_without_a_gradient(calls):
     for loss in losses(z).values():
         Both.apply(loss(), other.sum())[1].backward()
         assert z.grad is None
+
+
+def test_no_gradients_no_checkpoints(calls):
+    x, up, w = rand(6, 40).requires_grad_(), rand(6, 40, seed=1).requires_grad_(), rand(8, 40, seed=2).requires_grad_()
+    with torch.no_grad():
+        y, kept = T.act8(x, up)
+        T.linear8(y, w)
+    assert kept is None and calls == ["forward"]
+    del calls[:]
+    T.act8(x.detach(), up.detach())
+    T.linear8(x, w.detach()).sum().backward()        # a frozen weight: the input's gradient alone
+    assert calls == ["forward"] and x.grad is not None
+    with torch.no_grad():                            # asked for: made
+        y, kept = T.act8(x, keep_output=True)
+    assert calls == ["forward", "forward", "kept"]
+    w.grad = None
+    T.linear8(y, w, kept).sum().backward()
+    assert torch.equal(w.grad, (torch.ones(6, 8).double().t() @ ref.act8(y)[2]).float())
+
+
+def test_a_gradient_of_one_input_alone(calls):
+    x, up, dy = rand(6, 40), rand(6, 40, seed=1), rand(6, 40, seed=2)
+    f, slope = ref.act("silu", ref.act8(x)[2])
+    a, b = x.clone().requires_grad_(), up.clone().requires_grad_()
+    T.act8(a, up)[0].backward(dy)
+    assert torch.equal(a.grad, (dy.double() * ref.act8(up)[2] * slope).float())
+    T.act8(x, b)[0].backward(dy)
+    assert torch.equal(b.grad, (dy.double() * f).float())

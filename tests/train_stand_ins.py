@@ -49,7 +49,7 @@ def install(monkeypatch):
         out = (dy.double().t() @ decoded(ckpt_x, dy.shape[0], dw.shape[1])).float()
         dw.detach().copy_(dw.detach() + out if accumulate else out)
 
-    def ss_act8_forward(x, up, act, y, ckpt_x, ckpt_up=None, ckpt_y=None, stream=None):
+    def ss_act8_forward(x, up, act, y, ckpt_x=None, ckpt_up=None, ckpt_y=None, stream=None):
         calls.append("forward")
         _library_takes(*[m for m in (x, up, y) if m is not None])
         f = ref.act("gelu" if act == B.SS_ACT_GELU else "silu", x.double())[0]
