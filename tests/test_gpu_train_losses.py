@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_1810_05291_b200 import binding as B
+from tests.test_gpu_train_ops import Guarded, check_policy, loss_inputs
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -84,3 +85,43 @@ def test_a_label_smoothing_of_zero_leaves_the_term_out(smoothing):
         assert float(loss) == 0.0 and not bool(dz.any())
     else:
         assert float(loss) == float("inf")
+
+
+# ---- rows of a cluster one after another ----------------------------------------------------------------
+# For 148 SMs. A cluster takes more than one row where rows times blocks of a row come to 4440 or more (2664 for the rows
+# whose threads hold 128 logits): the comments give the blocks and rows of a cluster for bf16.
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,pad,off", [
+    (9000, 5001, 0, 0),       # 1 block, 4 rows
+    (13001, 4104, 0, 0),      # 1 block, 5 rows, aligned rows in bf16
+    (5000, 9001, 3, 1),       # 2 blocks, 4 rows
+    (2300, 32001, 0, 0),      # 4 blocks, 4 rows
+    (2500, 50001, 7, 0),      # 8 blocks, 8 rows (fp32: 128 logits to a thread)
+    (500, 100001, 0, 3),      # 8 blocks, 128 logits to a thread, 3 rows
+    (340, 131072, 0, 0),      # the longest row there is room for
+])
+def test_policy_rows_one_after_another(rows, vocab, pad, off, dtype):
+    z, y, w, old, rlp, adv = loss_inputs(rows, vocab, dtype, pad, off)
+    w[5:9], w[20:37], w[-3:] = 0.0, 0.0, 0.0                     # runs of rows left out, longer than a cluster's share
+    y[41], y[43], y[44] = -100, vocab, -1
+    w[50:70] = 0.0
+    w[60] = 1.0
+    z[21:25] = float("nan")
+    check_policy(z, y, old, rlp, adv, w)
+    out = Guarded(rows, vocab, dtype, vocab + 5, 1)              # gradients that lie otherwise against 16 bytes
+    check_policy(z, y, old, None, adv, w, beta=0.0, out=out, scale=0.5)
+    out.check()
+    like = lambda: torch.empty_strided(z.shape, z.stride(), dtype=dtype, device=DEV)  # noqa: E731
+    apart, over = like().copy_(z), like().copy_(z)               # in place: the same bits
+    dz = like()
+    first = policy(apart, y, old, rlp, adv, w, dz, kl_coef=0.05)
+    second = policy(over, y, old, rlp, adv, w, over, kl_coef=0.05)
+    assert torch.equal(over, dz) and all(torch.equal(a, b) for a, b in zip(first, second))
+
+
+def test_policy_rows_all_left_out():
+    for rows, vocab in ((9000, 5001), (2300, 32001)):
+        z, y, w, old, rlp, adv = loss_inputs(rows, vocab, torch.bfloat16)
+        z.fill_(float("nan"))
+        check_policy(z, y, old, rlp, adv, torch.zeros_like(w))
