@@ -1,7 +1,10 @@
 """The training operators on several streams: a backward pass, and what reads its results on the stream that called it."""
+import threading
+
 import pytest
 import torch
 
+from paper_1810_05291_b200 import binding as B
 from paper_1810_05291_b200 import train_ops as T
 from tests import train_ref as ref
 
@@ -69,3 +72,47 @@ def test_a_weight_used_on_two_streams(options, late):
     got = w.grad.clone()
     torch.cuda.synchronize()
     near(got, want)
+
+
+def test_calls_from_two_threads():
+    """Every operator from two host threads at once, each on its own stream and buffers: the bits of one thread's calls."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    rows, vocab = 300, 20001
+    sets = []
+    for _ in range(2):
+        z = torch.randn(rows, vocab, generator=g, device=DEV, dtype=torch.bfloat16)
+        x, dy = torch.randn(rows, 200, generator=g, device=DEV), torch.randn(rows, 136, generator=g, device=DEV)
+        sets.append((z, x, dy))
+    y, one = torch.arange(rows, device=DEV), torch.ones(rows, device=DEV)
+    begin, zero = torch.tensor([0, 100, 300], device=DEV), torch.zeros(2, device=DEV)
+
+    def calls(z, x, dy):
+        new = lambda *n: torch.empty(*n, device=DEV)  # noqa: E731
+        totals, logp, dz, loss, margins, seq, dp = new(3), new(rows), torch.empty_like(z), new(1), new(1), new(2), torch.empty_like(z)
+        ck, ck_y, out, dx, dw = B.act8_checkpoint(rows, 200, DEV), B.act8_checkpoint(rows, 200, DEV), torch.empty_like(x), torch.empty_like(x), new(136, 200)
+        B.ss_policy_loss(z, y, one, None, one, one, totals, logp, dz)
+        B.ss_preference_loss(z, y, one, begin, zero, loss, margins, seq, logp, dp)
+        B.ss_act8_forward(x, None, B.SS_ACT_GELU, out, ck, None, ck_y)
+        B.ss_act8_backward(out, ck, None, B.SS_ACT_GELU, dx)
+        B.ss_weight_grad8(dy, ck_y, dw)
+        return totals, logp, dz, loss, margins, seq, dp, out, dx, dw, ck, ck_y
+
+    want = [calls(*s) for s in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got[k].append(calls(*sets[k]))
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for k in (0, 1):
+        assert len(got[k]) == 20
+        for outs in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(outs, want[k]))
