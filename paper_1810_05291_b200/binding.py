@@ -544,11 +544,13 @@ def _ckpt(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
     return _vec(t, torch.uint8, name, rows * (SS_ACT8_GROUP + 1) * -(-cols // SS_ACT8_GROUP))
 
 
-def _written(t: torch.Tensor) -> None:
-    """Tells autograd that a kernel wrote to ``t``, so that a checkpoint which a backward pass has yet to read
-    is not written again without a word."""
-    if not t.is_inference():
-        torch.autograd.graph.increment_version(t)
+def _written(tensors) -> None:
+    """Tells autograd that a kernel wrote to these, so that a checkpoint which a backward pass has yet to read is not
+    written again without a word."""
+    try:
+        torch._C._increment_version(tensors)
+    except RuntimeError:  # inference tensors, which no backward pass reads, have no version
+        torch._C._increment_version([t for t in tensors if not t.is_inference()])
 
 
 def ss_act8_pack(x: torch.Tensor, ckpt: torch.Tensor, stream=None) -> None:
@@ -556,7 +558,7 @@ def ss_act8_pack(x: torch.Tensor, ckpt: torch.Tensor, stream=None) -> None:
     rows, cols = x.shape
     _check(lib().ss_act8_pack(ptr, stride, code, rows, cols, _ckpt(ckpt, rows, cols, "ckpt"), _stream(stream)),
            "ss_act8_pack")
-    _written(ckpt)
+    _written((ckpt,))
 
 
 def ss_act8_unpack(ckpt: torch.Tensor, out: torch.Tensor, stream=None) -> None:
@@ -579,9 +581,7 @@ def ss_act8_forward(x: torch.Tensor, up: Optional[torch.Tensor], act: int, y: to
                                  None if ckpt_up is None else _ckpt(ckpt_up, rows, cols, "ckpt_up"),
                                  None if ckpt_y is None else _ckpt(ckpt_y, rows, cols, "ckpt_y"), _stream(stream)),
            "ss_act8_forward")
-    for ckpt in (ckpt_x, ckpt_up, ckpt_y):
-        if ckpt is not None:
-            _written(ckpt)
+    _written([c for c in (ckpt_x, ckpt_up, ckpt_y) if c is not None])
 
 
 def ss_act8_backward(dy: torch.Tensor, ckpt_x: torch.Tensor, ckpt_up: Optional[torch.Tensor], act: int,
