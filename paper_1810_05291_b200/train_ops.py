@@ -116,7 +116,8 @@ class _Linear8(torch.autograd.Function):
             B.ss_act8_pack(m, kept)
         w = weight.to(x.dtype)
         ctx.weight, ctx.shape, ctx.into_grad = weight, x.shape, into_grad
-        ctx.save_for_backward(w, kept)  # with their versions: what is written again in between is refused
+        # with their versions: what is written again in between is refused
+        ctx.save_for_backward(w if ctx.needs_input_grad[0] else None, kept if wanted else None)
         return (m @ w.t()).view(*x.shape[:-1], weight.shape[0])
 
     @staticmethod

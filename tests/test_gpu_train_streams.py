@@ -30,6 +30,7 @@ def near(got, want):
     assert float((got.double() - want).norm() / want.norm()) < 1.5e-6
 
 
+@pytest.mark.filterwarnings("ignore:The AccumulateGrad node's stream does not match")
 @pytest.mark.parametrize("options", [{}, {"into_grad": True}], ids=["default", "into_grad"])
 @pytest.mark.parametrize("forward,older,caller", [("side", "main", "main"), ("main", "side", "side"), ("side", "other", "main"), ("side", "side", "main")])
 def test_the_caller_s_stream_waits_for_the_weight_s_gradient(options, forward, older, caller):

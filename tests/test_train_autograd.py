@@ -301,3 +301,14 @@ def test_a_gradient_of_one_input_alone(calls):
     assert torch.equal(a.grad, (dy.double() * ref.act8(up)[2] * slope).float())
     T.act8(x, b)[0].backward(dy)
     assert torch.equal(b.grad, (dy.double() * f).float())
+
+
+def test_what_a_layer_holds_until_its_backward_pass(calls):
+    """The weight in the input's type for the input's gradient, the checkpoint for the weight's: no more than is needed."""
+    x, w = rand(6, 40, dtype=torch.bfloat16), rand(8, 40, seed=1)
+    kept = torch.empty(6 * 66, dtype=torch.uint8)
+    T.B.ss_act8_pack(x, kept)
+    held = lambda y: [t is not None for t in y.grad_fn.saved_tensors]  # noqa: E731
+    assert held(T.linear8(x, w.requires_grad_(), kept)) == [False, True]
+    assert held(T.linear8(x.requires_grad_(), w.detach(), kept)) == [True, False]
+    assert held(T.linear8(x, w)) == [True, True]
