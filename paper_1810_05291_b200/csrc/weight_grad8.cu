@@ -11,9 +11,10 @@
 // at a time, in one half of the tensor memory, and added to dW, rounded to nearest, while the matrix unit fills the
 // other half: 4.5e-7 (512 rows: 1.3e-7, 1024: 2.1e-7; an fp32 product of the same: 5.1e-7).
 //
-// What bounds it. 16384 x 4096 x 4096 bf16 takes 407 us (1350 TFLOP/s; a library product of the same sizes
-// whose operands are both bf16 in memory 330 us), 16384 x 2048 x 9472 444 us (1430). Shared memory is busy 87 % of the time
-// and the matrix unit 76 %: for 64 rows a block copies in 24 KB, reads 8 KB of codes, writes 16 KB of operand and
+// What bounds it. A launch of 16384 x 4096 x 4096 bf16 alone takes 407 to 423 us (1300 to 1350 TFLOP/s; a library product of the same
+// sizes whose operands are both bf16 in memory 330 to 353), of 16384 x 2048 x 9472 444 to 463 us (1370 to 1430). In a row of calls the
+// power limit lowers the clock: 465 us after 160 of them and 510 after 800 (1080 TFLOP/s; the library product 363 and 402). Shared
+// memory is busy 87 % of the time and the matrix unit 76 %: for 64 rows a block copies in 24 KB, reads 8 KB of codes, writes 16 KB of operand and
 // feeds 32 to 48 KB to the matrix unit, 640 to 750 cycles at 128 bytes, where the products take 512 and a stage 725.
 // 4099 x 1000 x 2050 fp32 takes 73 us, of them 7 to split dY and 5 to join the parts. The three terms of 32 rows in
 // one stage, decoded once, took 66 us, but the small terms, added to the large one's sums, each cost a truncation:

@@ -171,9 +171,10 @@ class _Act8(torch.autograd.Function):
 def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] = None,
             into_grad: bool = False) -> torch.Tensor:
     """``x @ weight.T`` whose input is kept in 8 bits (33 bytes for 32 values) for the weight
-    gradient, if one can be asked for. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in] float32, used in
-    ``x``'s type (under autocast, in that of the region, as other linear layers are). ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's);
-    its contents are needed until the backward pass, which refuses one that was written again.
+    gradient, if one can be asked for. ``x``: [..., n_in] bfloat16 or float32; ``weight``: [n_out, n_in]
+    float32, used in ``x``'s type (under autocast both are used in the region's, as in other linear
+    layers). ``kept``: the checkpoint of ``x``, if it is at hand (``act8`` makes its output's); its
+    contents are needed until the backward pass, which refuses one that was written again.
 
     The weight's gradient is handed on to autograd. With ``into_grad`` the kernel adds it to
     ``weight.grad`` itself, without a buffer in between, in a backward pass that accumulates there
@@ -187,8 +188,9 @@ def linear8(x: torch.Tensor, weight: torch.Tensor, kept: Optional[torch.Tensor] 
 
 def act8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: str = "silu",
          keep_output: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
-    """``f(x)`` or ``f(x) * up`` whose inputs are kept in 8 bits, if a gradient can be asked for. Returns the result and, with
-    ``keep_output``, its checkpoint for the ``linear8`` that follows (else None)."""
+    """``f(x)`` or ``f(x) * up`` whose inputs are kept in 8 bits, if a gradient can be asked for.
+    Returns the result and, with ``keep_output``, its checkpoint for the ``linear8`` that follows
+    (else None)."""
     wanted = torch.is_grad_enabled() and (x.requires_grad or (up is not None and up.requires_grad))
     return _Act8.apply(x, up, ACTIVATIONS[act], keep_output, wanted)
 
