@@ -177,6 +177,39 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
                        float* seq_logp, float* logp, void* dlogits, int64_t dlogits_stride, void* workspace,
                        int64_t workspace_bytes, void* cuda_stream);
 
+/*
+ * Softmax cross entropy at the head of a language model, from the hidden states and the head's weight:
+ * the logits z = x w^T are formed in pieces and never kept as a whole. With lse_t = log sum_v exp(c z_t[v]):
+ *   logp_t = c z_t[targets[t]] - lse_t
+ *   loss = sum_t weights_t (-logp_t + z_coef lse_t^2)
+ *   P_t[v] = d loss / d z_t[v] = c weights_t ((1 + 2 z_coef lse_t) exp(c z_t[v] - lse_t) - [v = targets[t]])
+ *   dx = P w,  dw = P^T x,  both times *grad_scale
+ * Positions are left out as in the losses over logits: their x is not read, their logp and dx are 0. A row of x, or a
+ * w, that holds an infinity or a NaN gives what the formulas give, NaN for the most part.
+ *   x        in      [rows, width] of dt
+ *   w        in      [vocab, width] of dt
+ *   totals   out     2 fp32: loss, sum_t weights_t lse_t^2
+ *   logp     out     rows fp32
+ *   dx       out     [rows, width] of dt, or NULL; may be x in place
+ *   dw       out     [vocab, width] of dw_dt, or NULL; fp32, or for bf16 inputs bf16 as well. With accumulate
+ *                    (fp32 only) it is added to
+ *   workspace        scratch of ss_linear_cross_entropy_workspace of the same arguments: about 1 GiB at the
+ *                    most for the pieces, the rows that count, and where w is fp32 or its rows do not start on 16 bytes a
+ *                    copy of it; a bf16 dw that more than one GiB's rows add to has its sums there too
+ * targets, weights, inv_temperature, grad_scale as above. z_coef finite; 0 leaves its term out.
+ * width, vocab >= 1 where there are rows. No rows: totals 0, dw 0 unless accumulate. More than 2^24 rows or 2^24
+ * tiles of 256 x 256 are SS_ERR_UNSUPPORTED.
+ * bf16: products of bf16 with fp32 sums; P is rounded to bf16. fp32: products of three bf16 terms, as precise as fp32
+ * sums. Sums that are added by the memory may flush a subnormal to zero. A wait inside a kernel that ran out (it is bounded) shows as NaN.
+ */
+int64_t ss_linear_cross_entropy_workspace(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_t width,
+                                          int64_t vocab, int want_dx, int want_dw, ss_dtype dw_dt);
+int ss_linear_cross_entropy(const void* x, int64_t x_stride, const void* w, int64_t w_stride, ss_dtype dt, int64_t rows,
+                            int64_t width, int64_t vocab, const int64_t* targets, const float* weights,
+                            float inv_temperature, float z_coef, const float* grad_scale, float* totals, float* logp,
+                            void* dx, int64_t dx_stride, void* dw, int64_t dw_stride, ss_dtype dw_dt, int accumulate,
+                            void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

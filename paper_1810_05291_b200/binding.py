@@ -1,7 +1,7 @@
 """Python names for the C ABI of libsignsgd.so -- argument marshalling only.
 
 Each function below has the name and the argument order of its C entry point (see
-``include/signsgd.h`` and ``include/signsgd_train.h``) and does nothing but check tensor types, take ``data_ptr()`` and the
+``include/signsgd.h``, ``include/signsgd_train.h`` and ``include/signsgd_ortho.h``) and does nothing but check tensor types, take ``data_ptr()`` and the
 current CUDA stream, call into the library and raise on a non-zero status. All arithmetic
 of Algorithm 1 happens in the CUDA kernels. There is no CPU fallback: if the library has
 not been built (``python -m paper_1810_05291_b200.build``), the first call raises.
@@ -31,6 +31,8 @@ SS_FLAGS_MAX_TIMEOUT_NS = 2_000_000_000
 SS_ACT8_GROUP = 32
 SS_ACT_GELU, SS_ACT_SILU = 0, 1
 SS_PREF_SIGMOID, SS_PREF_HINGE, SS_PREF_SQUARED = 0, 1, 2
+SS_ORTHO_MAX_MATRICES, SS_ORTHO_MAX_STEPS = 64, 32
+ORTHO_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
 
 SS_OK = 0
 SS_ERR_INVALID_ARG = -1
@@ -47,7 +49,8 @@ EXPORTS = ("ss_packed_words", "ss_status_string", "ss_last_cuda_error", "ss_sign
            "ss_vote_apply_guarded_segments",
            "ss_act8_bytes", "ss_act8_pack", "ss_act8_unpack", "ss_act8_forward", "ss_act8_backward",
            "ss_weight_grad8", "ss_weight_grad8_workspace", "ss_loss_workspace", "ss_policy_loss",
-           "ss_preference_loss")
+           "ss_preference_loss", "ss_linear_cross_entropy", "ss_linear_cross_entropy_workspace",
+           "ss_orthogonal_workspace", "ss_orthogonalise", "ss_orthogonal_update")
 
 
 class ss_segment(ctypes.Structure):
@@ -124,6 +127,17 @@ def lib() -> ctypes.CDLL:
                                  vp, i64, vp]
     L.ss_preference_loss.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, i64, vp, f32, i32, f32, f32, f32, vp, vp, vp,
                                      vp, vp, vp, i64, vp, i64, vp]
+    L.ss_linear_cross_entropy_workspace.argtypes = [vp, i64, i32, i64, i64, i64, i32, i32, i32]
+    L.ss_linear_cross_entropy.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, vp, f32, f32, vp, vp, vp, vp, i64, vp,
+                                          i64, i32, i32, vp, i64, vp]
+    L.ss_orthogonal_workspace.argtypes = [i32, i64, i64]
+    L.ss_orthogonalise.argtypes = [vp, i64, i32, vp, i64, i32, i32, i64, i64, vp, i32, vp, i64, vp]
+    L.ss_orthogonal_update.argtypes = [vp, i64, i32, vp, vp, i64, vp, vp, i64, i32, i64, i64, f32, i32, vp, i32, f32, f32,
+                                       f32, vp, i64, vp]
+    for name in ("ss_linear_cross_entropy_workspace", "ss_orthogonal_workspace"):
+        getattr(L, name).restype = i64
+    for name in ("ss_linear_cross_entropy", "ss_orthogonalise", "ss_orthogonal_update"):
+        getattr(L, name).restype = i32
     for name in ("ss_act8_bytes", "ss_weight_grad8_workspace", "ss_loss_workspace"):
         getattr(L, name).restype = i64
     for name in ("ss_act8_pack", "ss_act8_unpack", "ss_act8_forward", "ss_act8_backward", "ss_weight_grad8",
@@ -661,3 +675,143 @@ def ss_preference_loss(logits: torch.Tensor, targets: torch.Tensor, weights: tor
                                 _vec(loss, f32, "loss", 1), _vec(margins, f32, "margins", pairs),
                                 _vec(seq_logp, f32, "seq_logp", 2 * pairs), _vec(logp, f32, "logp", rows), d_ptr,
                                 d_stride, w_ptr, w_bytes, _stream(stream)), "ss_preference_loss")
+
+
+def _one_device(tensors) -> int:
+    """The GPU that all of them are on."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError("all tensors of a call must be on one device")
+    return device
+
+
+def _on_its_device(call):
+    """A call whose tensors are on another GPU than the current one is made there (its workspace, its stream)."""
+    @functools.wraps(call)
+    def made(*args, **kwargs):
+        first = args[0][0] if isinstance(args[0], (list, tuple)) and len(args[0]) else args[0]
+        device = first.get_device() if isinstance(first, torch.Tensor) else -1
+        if device < 0 or device == torch.cuda.current_device():
+            return call(*args, **kwargs)
+        with torch.cuda.device(device):
+            return call(*args, **kwargs)
+    return made
+
+
+def ss_linear_cross_entropy_workspace(weight: torch.Tensor, rows: int, dx: bool = True, dw: Optional[torch.dtype] = None) -> int:
+    """Scratch bytes of ``ss_linear_cross_entropy`` for that many rows; ``dw``: the type of its gradient, if it is formed."""
+    ptr, stride = _mat(weight, weight.dtype, "weight")
+    vocab, width = weight.shape
+    return int(lib().ss_linear_cross_entropy_workspace(ptr, stride, _dtype_code(weight), int(rows), width, vocab, int(dx), int(dw is not None),
+                                                       SS_BF16 if dw is torch.bfloat16 else SS_F32))
+
+
+@_on_its_device
+def ss_linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, weights: torch.Tensor,
+                            totals: torch.Tensor, logp: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                            dw: Optional[torch.Tensor] = None, accumulate: bool = False, inv_temperature: float = 1.0,
+                            z_coef: float = 0.0, grad_scale: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    f32, dt, code = torch.float32, x.dtype, _dtype_code(x)
+    x_ptr, x_stride = _mat(x, dt, "x")
+    rows, width = x.shape
+    w_ptr, w_stride = _mat(weight, dt, "weight")
+    vocab = weight.shape[0]
+    if weight.shape[1] != width:
+        raise ValueError("weight must have one column for each of x's %d, has %d" % (width, weight.shape[1]))
+    _one_device([t for t in (x, weight, targets, weights, totals, logp, dx, dw, grad_scale, workspace) if t is not None])
+    dx_ptr, dx_stride = (None, 0) if dx is None else _mat(dx, dt, "dx", x.shape)
+    dw_code = SS_F32 if dw is None else _dtype_code(dw)
+    dw_ptr, dw_stride = (None, 0) if dw is None else _mat(dw, dw.dtype, "dw", weight.shape)
+    L = lib()
+    need = 0 if workspace is not None else L.ss_linear_cross_entropy_workspace(w_ptr, w_stride, code, rows, width, vocab, int(dx is not None),
+                                                                              int(dw is not None), dw_code)
+    ws_ptr, ws_bytes, workspace = _scratch(workspace, need, x, stream)
+    _check(L.ss_linear_cross_entropy(x_ptr, x_stride, w_ptr, w_stride, code, rows, width, vocab,
+                                     _vec(targets, torch.int64, "targets", rows), _vec(weights, f32, "weights", rows),
+                                     inv_temperature, z_coef, _opt_vec(grad_scale, f32, "grad_scale", 1),
+                                     _vec(totals, f32, "totals", 2), _vec(logp, f32, "logp", rows), dx_ptr, dx_stride,
+                                     dw_ptr, dw_stride, dw_code, int(bool(accumulate)), ws_ptr, ws_bytes, _stream(stream)),
+           "ss_linear_cross_entropy")
+
+
+# ---- orthogonal update (include/signsgd_ortho.h) -------------------------------------------------
+
+def _mats(tensors: Sequence[torch.Tensor], dtype, name: str, shape):
+    """(addresses, row stride) of matrices of one shape and stride."""
+    stride = None
+    ptrs = []
+    for i, t in enumerate(tensors):
+        ptr, s = _mat(t, dtype, "%s[%d]" % (name, i), shape)
+        if stride is None:
+            stride = s
+        elif s != stride and shape[0] > 1:
+            raise ValueError("%s must have one row stride, has %d and %d" % (name, stride, s))
+        ptrs.append(ptr)
+    return _ptr_array(ptrs), 0 if stride is None else stride
+
+
+@functools.lru_cache(maxsize=64)
+def _coefficients(rows):
+    flat = [float(v) for step in rows for v in step]
+    if any(len(step) != 3 for step in rows):
+        raise ValueError("coefficients must be (a, b, c) for each step")
+    return (ctypes.c_float * len(flat))(*flat), len(rows)
+
+
+@functools.lru_cache(maxsize=256)
+def ss_orthogonal_workspace(count: int, rows: int, cols: int) -> int:
+    return int(lib().ss_orthogonal_workspace(int(count), int(rows), int(cols)))
+
+
+def _same_count(count: int, **lists) -> None:
+    for name, tensors in lists.items():
+        if len(tensors) != count:
+            raise ValueError("%s must hold %d matrices, holds %d" % (name, count, len(tensors)))
+
+
+@_on_its_device
+def ss_orthogonalise(inputs: Sequence[torch.Tensor], outputs: Sequence[torch.Tensor], coefficients=ORTHO_COEFFICIENTS,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``inputs`` and ``outputs``: up to 64 matrices of one shape, of one type and row stride each."""
+    count = len(inputs)
+    _same_count(count, outputs=outputs)
+    if count == 0:
+        return
+    _one_device([*inputs, *outputs] if workspace is None else [*inputs, *outputs, workspace])
+    shape, in_code, out_code = inputs[0].shape, _dtype_code(inputs[0]), _dtype_code(outputs[0])
+    a, a_stride = _mats(inputs, inputs[0].dtype, "inputs", shape)
+    b, b_stride = _mats(outputs, outputs[0].dtype, "outputs", shape)
+    rows, cols = shape
+    table, steps = _coefficients(tuple(map(tuple, coefficients)))
+    need = 0 if workspace is not None else ss_orthogonal_workspace(count, rows, cols)
+    w_ptr, w_bytes, workspace = _scratch(workspace, need, inputs[0], stream)
+    _check(lib().ss_orthogonalise(a, a_stride, in_code, b, b_stride, out_code, count, rows, cols, table, steps, w_ptr, w_bytes,
+                                  _stream(stream)), "ss_orthogonalise")
+
+
+@_on_its_device
+def ss_orthogonal_update(grads: Sequence[torch.Tensor], momenta: Sequence[torch.Tensor], momenta_out: Sequence[torch.Tensor],
+                         params: Sequence[torch.Tensor], params_out: Sequence[torch.Tensor], beta: float, nesterov: bool = True,
+                         coefficients=ORTHO_COEFFICIENTS, lr: float = 1e-3, scale: float = 1.0, weight_decay: float = 0.0,
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Up to 64 matrices of one shape; ``momenta_out`` may be ``momenta``, ``params_out`` ``params``."""
+    count = len(grads)
+    _same_count(count, momenta=momenta, momenta_out=momenta_out, params=params, params_out=params_out)
+    if count == 0:
+        return
+    every = [*grads, *momenta, *momenta_out, *params, *params_out]
+    _one_device(every if workspace is None else every + [workspace])
+    f32, shape, code = torch.float32, grads[0].shape, _dtype_code(grads[0])
+    g, g_stride = _mats(grads, grads[0].dtype, "grads", shape)
+    v, v_stride = _mats([*momenta, *momenta_out], f32, "momenta and momenta_out", shape)
+    p, p_stride = _mats([*params, *params_out], f32, "params and params_out", shape)
+    half = count * ctypes.sizeof(ctypes.c_void_p)
+    rows, cols = shape
+    table, steps = _coefficients(tuple(map(tuple, coefficients)))
+    need = 0 if workspace is not None else ss_orthogonal_workspace(count, rows, cols)
+    w_ptr, w_bytes, workspace = _scratch(workspace, need, grads[0], stream)
+    _check(lib().ss_orthogonal_update(g, g_stride, code, v, ctypes.byref(v, half), v_stride, p, ctypes.byref(p, half), p_stride, count,
+                                      rows, cols, beta, int(bool(nesterov)), table, steps, lr, scale, weight_decay, w_ptr,
+                                      w_bytes, _stream(stream)), "ss_orthogonal_update")

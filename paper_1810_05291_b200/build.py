@@ -22,16 +22,17 @@ LIB = os.path.join(HERE, "libsignsgd.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "signsgd")
 
 SOURCES = ["abi.cu", "step_f32.cu", "step_bf16.cu", "vote_apply.cu", "noalloc.cu", "ternary.cu", "exchange_flags.cu",
-           "act8.cu", "weight_grad8.cu", "losses.cu"]
-HEADERS = ["bitslice.cuh", "common.cuh", "step_kernel.cuh", "step_oct_kernel.cuh", "exchange.cuh", "train.cuh", "act8.cuh", "tcgen05.cuh",
-           os.path.join("..", "..", "include", "signsgd.h"), os.path.join("..", "..", "include", "signsgd_train.h")]
+           "act8.cu", "weight_grad8.cu", "losses.cu", "head_loss.cu", "ortho.cu"]
+HEADERS = ["bitslice.cuh", "common.cuh", "step_kernel.cuh", "step_oct_kernel.cuh", "exchange.cuh", "train.cuh", "act8.cuh", "tcgen05.cuh", "product.cuh",
+           os.path.join("..", "..", "include", "signsgd.h"), os.path.join("..", "..", "include", "signsgd_train.h"),
+           os.path.join("..", "..", "include", "signsgd_ortho.h")]
 
 # -fmad=false: no multiply-add contraction anywhere (the arithmetic also uses explicitly
 # rounded intrinsics); no -use_fast_math, denormals kept. The training operators are compared with
 # a tolerance, not bit for bit, and may contract.
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
-CONTRACTED = ("act8.cu", "weight_grad8.cu", "losses.cu")
+CONTRACTED = ("act8.cu", "weight_grad8.cu", "losses.cu", "head_loss.cu", "ortho.cu")
 
 
 def _nvcc() -> str:

@@ -1,0 +1,550 @@
+// The orthogonal update: X <- a X + (b S + c S S) X with S = X X^T over the smaller side, some steps.
+//
+// A step is three products: S (symmetric: tiles on and above the diagonal, each stored twice), Q = b S + c S S
+// (symmetric as well) and Y = a X + Q X, the sums of each brought from the tensor memory straight into what the
+// next one reads. A tall matrix has S = X^T X and X Q instead; the operands' maps differ, nothing is transposed.
+//
+// Rounding. The operands X, S and Q are fp16: with bf16 (8 bits) the result is 1 to 3 % off, with fp16 0.2 %. The
+// term a X takes X with 22 bits, as the sum of two fp16 of which the first is the operand: it alone carries the
+// directions whose singular values are small, which each step enlarges 3.4 times; with 11 bits there a momentum
+// of few strong directions comes out 0.35 % off instead of 0.03 %.
+#include "../../include/signsgd_ortho.h"
+#include "product.cuh"
+
+#include <cuda_fp16.h>
+
+#include <cmath>
+
+namespace ss {
+namespace {
+
+constexpr int kMostMatrices = SS_ORTHO_MAX_MATRICES;
+
+struct Table {
+    const void* p[kMostMatrices];
+};
+
+__device__ __forceinline__ uint2 half4(float4 v) {
+    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+__device__ __forceinline__ float4 float4_of(uint2 h) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&h.y));
+    return make_float4(a.x, a.y, b.x, b.y);
+}
+// The two fp16 whose sum v is, to 22 bits.
+__device__ __forceinline__ void split4(float4 v, uint2* hi, uint2* lo) {
+    *hi = half4(v);
+    const float4 h = float4_of(*hi);
+    *lo = half4(make_float4(v.x - h.x, v.y - h.y, v.z - h.z, v.w - h.w));
+}
+
+// ---- ends of the products --------------------------------------------------------------------------
+
+// out = c sums (+ b lin), symmetric: a square above the diagonal's tiles is stored a second time, mirrored.
+struct Symmetric {
+    static constexpr bool kWhole = false;
+    struct Fetched {
+        uint2 lin[8];
+    };
+    uint16_t* out;
+    const uint16_t* lin;  // NULL: none
+    int64_t plane;
+    int ld;
+    float b, c;
+
+    __device__ __forceinline__ int64_t at(const ProdUnit& u, int row, int col) const { return u.batch * plane + static_cast<int64_t>(row) * ld + col; }
+
+    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const {
+        if (lin == nullptr) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row + (lane >> 3) + 4 * i;
+            f.lin[i] = r < m ? *reinterpret_cast<const uint2*>(lin + at(u, r, col + 4 * (lane & 7))) : make_uint2(0, 0);
+        }
+    }
+    __device__ __forceinline__ void square(const ProdUnit& u, int m, int row, int col, int lane, uint32_t buf, const Fetched& f, bool) const {
+        const bool mirror = u.m0 != u.n0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = (lane >> 3) + 4 * i;
+            const uint4 w = square_get(buf, r, lane & 7);
+            float4 v = make_float4(c * __uint_as_float(w.x), c * __uint_as_float(w.y), c * __uint_as_float(w.z), c * __uint_as_float(w.w));
+            if (lin != nullptr) {
+                const float4 l = float4_of(f.lin[i]);
+                v.x += b * l.x, v.y += b * l.y, v.z += b * l.z, v.w += b * l.w;
+            }
+            if (row + r < m) *reinterpret_cast<uint2*>(out + at(u, row + r, col + 4 * (lane & 7))) = half4(v);
+            if (mirror) square_set(buf, r, lane & 7, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+        }
+        if (!mirror) return;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int cc = (lane >> 3) + 4 * i, r = 4 * (lane & 7);
+            const float4 v = make_float4(square_word(buf, r, cc), square_word(buf, r + 1, cc), square_word(buf, r + 2, cc), square_word(buf, r + 3, cc));
+            if (col + cc < m) *reinterpret_cast<uint2*>(out + at(u, col + cc, row + r)) = half4(v);
+        }
+    }
+};
+
+// X carried as hi + lo, scaled by a power of two: the next one is a (hi + lo) + sums.
+struct Carried {
+    const uint16_t* hi;
+    uint16_t* lo;
+    int64_t plane;
+    int ld;
+    float a;
+
+    struct Fetched {
+        uint2 hi[8], lo[8];
+    };
+    __device__ __forceinline__ int64_t at(const ProdUnit& u, int row, int col) const { return u.batch * plane + static_cast<int64_t>(row) * ld + col; }
+    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row + (lane >> 3) + 4 * i;
+            const int64_t k = at(u, r, col + 4 * (lane & 7));
+            f.hi[i] = r < m ? *reinterpret_cast<const uint2*>(hi + k) : make_uint2(0, 0);
+            f.lo[i] = r < m ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
+        }
+    }
+    __device__ __forceinline__ float4 next(uint32_t buf, int lane, int i, const Fetched& f) const {
+        const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+        const float4 h = float4_of(f.hi[i]), l = float4_of(f.lo[i]);
+        return make_float4(a * (h.x + l.x) + __uint_as_float(w.x), a * (h.y + l.y) + __uint_as_float(w.y),
+                           a * (h.z + l.z) + __uint_as_float(w.z), a * (h.w + l.w) + __uint_as_float(w.w));
+    }
+};
+
+struct Next {
+    static constexpr bool kWhole = false;
+    using Fetched = Carried::Fetched;
+    Carried x;
+    uint16_t* hi_out;
+
+    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const { x.fetch(u, m, row, col, lane, f); }
+    __device__ __forceinline__ void square(const ProdUnit& u, int m, int row, int col, int lane, uint32_t buf, const Fetched& f, bool) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row + (lane >> 3) + 4 * i;
+            uint2 hi, lo;
+            split4(x.next(buf, lane, i, f), &hi, &lo);
+            if (r >= m) continue;
+            const int64_t k = x.at(u, r, col + 4 * (lane & 7));
+            *reinterpret_cast<uint2*>(hi_out + k) = hi;
+            *reinterpret_cast<uint2*>(x.lo + k) = lo;  // nothing but this place of this tile reads it
+        }
+    }
+};
+
+// The last step's result, to the caller: O, or the parameter moved by it.
+struct Result {
+    static constexpr bool kWhole = false;
+    using Fetched = Carried::Fetched;
+    Carried x;
+    float unscale;  // of the power of two
+    int64_t stride;
+    int cols, dt;   // of out
+    int vectors;    // four neighbouring elements of every matrix start on their size
+    int update;
+    float lr, scale, decay;
+    Table out, param;
+
+    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const { x.fetch(u, m, row, col, lane, f); }
+    __device__ __forceinline__ float moved(float p, float o) const { return p - lr * (scale * o + decay * p); }
+    __device__ __forceinline__ void square(const ProdUnit& u, int m, int row, int col, int lane, uint32_t buf, const Fetched& f, bool) const {
+        void* const to = const_cast<void*>(out.p[u.batch]);
+        const float* const from = static_cast<const float*>(param.p[u.batch]);
+        const int c = col + 4 * (lane & 7);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row + (lane >> 3) + 4 * i;
+            const float4 n = x.next(buf, lane, i, f);
+            if (r >= m || c >= cols) continue;
+            float4 o = make_float4(n.x * unscale, n.y * unscale, n.z * unscale, n.w * unscale);
+            const int64_t k = r * stride + c;
+            if (vectors && c + 4 <= cols) {
+                if (update) {
+                    const float4 p = *reinterpret_cast<const float4*>(from + k);
+                    o = make_float4(moved(p.x, o.x), moved(p.y, o.y), moved(p.z, o.z), moved(p.w, o.w));
+                }
+                if (dt == SS_F32) *reinterpret_cast<float4*>(static_cast<float*>(to) + k) = o;
+                else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(to) + k) = make_uint2(bf16_pair(o.x, o.y), bf16_pair(o.z, o.w));
+            } else {
+                const float v[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c + j >= cols) break;
+                    const float e = update ? moved(from[k + j], v[j]) : v[j];
+                    if (dt == SS_F32) static_cast<float*>(to)[k + j] = e;
+                    else Elem<uint16_t>::store(static_cast<uint16_t*>(to) + k + j, e);
+                }
+            }
+        }
+    }
+};
+
+// ---- the start: momentum, norm, first operand ------------------------------------------------------
+
+struct Start {
+    Table in, momentum, momentum_out;  // momentum: unused without update
+    int64_t in_stride, momentum_stride, plane, rows;
+    int cols, ld, update, nesterov, vectors, blocks;
+    float beta, rest;  // rest = 1 - beta
+    double scale;      // the power of two
+    double* partial;   // [count][blocks]
+    uint16_t *hi, *lo;
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load_four(const T* p, int n, bool vectors) {
+    if (vectors && n >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            return *reinterpret_cast<const float4*>(p);
+        } else {
+            const uint2 r = *reinterpret_cast<const uint2*>(p);
+            return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xFFFF0000u));
+        }
+    }
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = j < n ? Elem<T>::load(p + j) : 0.0f;
+    return make_float4(v[0], v[1], v[2], v[3]);
+}
+
+__device__ __forceinline__ float4 mix(float4 g, float4 v, float rest, float beta) {
+    return make_float4(rest * g.x + beta * v.x, rest * g.y + beta * v.y, rest * g.z + beta * v.z, rest * g.w + beta * v.w);
+}
+
+// Sum over the block, the same in every thread; the order is fixed.
+__device__ __forceinline__ double block_sum(double s) {
+    __shared__ double part[8];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = part[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += part[i];
+    return s;
+}
+
+// Four columns of a row at a time, over all of the matrix.
+template <typename F>
+__device__ __forceinline__ void over_fours(const Start& a, F f) {
+    const uint32_t fours = (a.cols + 3) / 4;
+    const int64_t total = a.rows * fours;
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(a.blocks) * 256) {
+        const int64_t r = total <= 0xFFFFFFFFll ? static_cast<int64_t>(static_cast<uint32_t>(i) / fours) : i / fours;
+        const int c = static_cast<int>(i - r * fours) * 4;
+        f(r, c, min(4, a.cols - c));
+    }
+}
+
+// The momentum's update, and partial sums of u's squares, in fp64: the square of a large gradient has no place in fp32, and a
+// fp64 product for each element costs nothing next to its bytes.
+template <typename T>
+__global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__ Start a) {
+    next_may_begin();
+    const T* const in = static_cast<const T*>(a.in.p[blockIdx.y]);
+    const float* const mom = static_cast<const float*>(a.momentum.p[blockIdx.y]);
+    float* const mom_out = static_cast<float*>(const_cast<void*>(a.momentum_out.p[blockIdx.y]));
+    double sum = 0.0;
+    over_fours(a, [&](int64_t r, int c, int n) {
+        float4 u = load_four(in + r * a.in_stride + c, n, a.vectors);
+        if (a.update) {
+            const int64_t k = r * a.momentum_stride + c;
+            const float4 g = u, v = mix(g, load_four(mom + k, n, a.vectors), a.rest, a.beta);
+            if (a.vectors && n >= 4) {
+                *reinterpret_cast<float4*>(mom_out + k) = v;
+            } else {
+                const float e[4] = {v.x, v.y, v.z, v.w};
+                for (int j = 0; j < n; ++j) mom_out[k + j] = e[j];
+            }
+            u = a.nesterov ? mix(g, v, a.rest, a.beta) : v;
+        }
+        const double x = u.x, y = u.y, z = u.z, w = u.w;
+        sum += x * x + y * y + (n == 4 ? z * z + w * w : (n == 3 ? z * z : 0.0));
+    });
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) a.partial[static_cast<int64_t>(blockIdx.y) * a.blocks + blockIdx.x] = sum;
+}
+
+// X_0 = u / |u|, scaled, as hi + lo.
+template <typename T>
+__global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant__ Start a) {
+    next_may_begin();
+    after_previous();
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.blocks; i += 256) sum += a.partial[static_cast<int64_t>(blockIdx.y) * a.blocks + i];
+    sum = block_sum(sum);
+    // nothing but zeros stays that; an infinity or a NaN anywhere is NaN everywhere
+    const double factor = sum == 0.0 ? 0.0 : (sum < INFINITY ? a.scale / sqrt(sum) : NAN);
+    const T* const in = static_cast<const T*>(a.in.p[blockIdx.y]);
+    const float* const mom = static_cast<const float*>(a.momentum_out.p[blockIdx.y]);
+    over_fours(a, [&](int64_t r, int c, int n) {
+        float4 u;
+        if (a.update) {
+            u = load_four(mom + r * a.momentum_stride + c, n, a.vectors);
+            if (a.nesterov) u = mix(load_four(in + r * a.in_stride + c, n, a.vectors), u, a.rest, a.beta);
+        } else {
+            u = load_four(in + r * a.in_stride + c, n, a.vectors);
+        }
+        u = make_float4(static_cast<float>(u.x * factor), static_cast<float>(u.y * factor), static_cast<float>(u.z * factor), static_cast<float>(u.w * factor));
+        uint2 hi, lo;
+        split4(u, &hi, &lo);
+        const int64_t k = blockIdx.y * a.plane + r * a.ld + c;
+        *reinterpret_cast<uint2*>(a.hi + k) = hi;
+        *reinterpret_cast<uint2*>(a.lo + k) = lo;
+    });
+}
+
+// ---- host side -------------------------------------------------------------------------------------
+
+constexpr int64_t kMostSide = int64_t(1) << 20, kMostTiles = int64_t(1) << 24;
+constexpr int kMostBlocks = 592;  // of the start's kernels: four to an SM
+
+struct Layout {
+    int64_t side, ld, side_ld;   // the smaller side; row strides of X and of S and Q
+    int64_t plane, side_plane;   // elements of a matrix
+    int blocks;                  // of the start, for each matrix
+    int64_t hi[2], lo, s, q, partial, bytes;  // places in the workspace
+};
+
+inline int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+
+bool sizes_ok(int count, int64_t rows, int64_t cols) { return count >= 0 && count <= kMostMatrices && sides_ok(rows, cols); }
+
+int layout_of(int count, int64_t rows, int64_t cols, Layout* l) {
+    if (rows > kMostSide || cols > kMostSide) return SS_ERR_UNSUPPORTED;
+    if (((rows + 255) / 256) * ((cols + 255) / 256) * count > kMostTiles) return SS_ERR_UNSUPPORTED;
+    l->side = rows < cols ? rows : cols;
+    l->ld = up_to(cols, 64), l->side_ld = up_to(l->side, 64);
+    l->plane = rows * l->ld, l->side_plane = l->side * l->side_ld;
+    const int64_t want = (rows * ((cols + 3) / 4) + 1023) / 1024, most = kMostBlocks / count > 1 ? kMostBlocks / count : 1;
+    l->blocks = static_cast<int>(want < most ? want : most);
+    int64_t at = 0;
+    auto place = [&](int64_t bytes) {
+        const int64_t p = at;
+        at += up_to(bytes, 256);
+        return p;
+    };
+    l->hi[0] = place(count * l->plane * 2), l->hi[1] = place(count * l->plane * 2), l->lo = place(count * l->plane * 2);
+    l->s = place(count * l->side_plane * 2), l->q = place(count * l->side_plane * 2);
+    l->partial = place(static_cast<int64_t>(count) * l->blocks * 8);
+    l->bytes = at;
+    return SS_OK;
+}
+
+struct Call {
+    Start start;
+    Result result;
+    ss_dtype in_dt;
+    int count;
+    int64_t rows, cols;
+    const float* coefficients;
+    int steps;
+};
+
+int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
+    const int64_t big = c.rows > c.cols ? c.rows : c.cols;
+    int power = 0;  // 2^power: about the root of the larger side, so that X ends with values about 1
+    while ((int64_t(1) << (2 * (power + 1))) <= big) ++power;
+    const float scale = std::ldexp(1.0f, power), unscale = std::ldexp(1.0f, -power);
+    uint16_t* hi[2] = {reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.hi[1])};
+    uint16_t* const lo = reinterpret_cast<uint16_t*>(ws + l.lo);
+    uint16_t *const s = reinterpret_cast<uint16_t*>(ws + l.s), *const q = reinterpret_cast<uint16_t*>(ws + l.q);
+    Start& a = c.start;
+    a.plane = l.plane, a.rows = c.rows, a.cols = static_cast<int>(c.cols), a.ld = static_cast<int>(l.ld), a.blocks = l.blocks;
+    a.scale = scale, a.partial = reinterpret_cast<double*>(ws + l.partial), a.hi = hi[0], a.lo = lo;
+    const dim3 grid(static_cast<unsigned>(l.blocks), static_cast<unsigned>(c.count));
+    cudaError_t e;
+    if (c.in_dt == SS_F32) e = launch_next(false, ortho_norm_kernel<float>, grid, 256, st, a);
+    else e = launch_next(false, ortho_norm_kernel<uint16_t>, grid, 256, st, a);
+    if (e != cudaSuccess) return cuda_status_public(e);
+    if (c.in_dt == SS_F32) e = launch_next(true, ortho_start_kernel<float>, grid, 256, st, a);
+    else e = launch_next(true, ortho_start_kernel<uint16_t>, grid, 256, st, a);
+    if (e != cudaSuccess) return cuda_status_public(e);
+
+    const bool tall = c.rows > c.cols;
+    const int64_t row_bytes = l.ld * 2, plane_bytes = l.plane * 2, side_row = l.side_ld * 2, side_bytes = l.side_plane * 2;
+    CUtensorMap x_sum[2], x_prod[2], s_map, q_map;  // X as an operand of S and of Q X
+    int status = SS_OK;
+    auto map = [&](CUtensorMap* m, const void* p, int64_t fast, int64_t slow, int64_t rb, int64_t pb, bool mn) {
+        if (status == SS_OK) status = map_operand(m, p, false, fast, slow, rb, c.count, pb, mn);
+    };
+    for (int i = 0; i < 2; ++i) {
+        map(&x_sum[i], hi[i], c.cols, c.rows, row_bytes, plane_bytes, tall);
+        map(&x_prod[i], hi[i], c.cols, c.rows, row_bytes, plane_bytes, !tall);
+    }
+    map(&s_map, s, l.side, l.side, side_row, side_bytes, false);
+    map(&q_map, q, l.side, l.side, side_row, side_bytes, false);
+    if (status != SS_OK) return status;
+
+    Product ps = product_of(l.side, l.side, big, false), pq = product_of(l.side, l.side, l.side, false);
+    Product px = product_of(c.rows, c.cols, l.side, false);
+    for (Product* p : {&ps, &pq, &px}) p->batches = c.count, p->bf16 = 0, p->follows = 1, p->m_fast = 1;
+    ps.upper = pq.upper = 1;
+    for (int k = 0; k < c.steps; ++k) {
+        const float *const co = c.coefficients + 3 * k;
+        const int from = k & 1;
+        const Symmetric es{s, nullptr, l.side_plane, static_cast<int>(l.side_ld), 0.0f, unscale * unscale};
+        const Symmetric eq{q, s, l.side_plane, static_cast<int>(l.side_ld), co[1], co[2]};
+        const Carried x{hi[from], lo, l.plane, static_cast<int>(l.ld), co[0]};
+        status = tall ? launch_product<Symmetric, true, true>(x_sum[from], x_sum[from], ps, es, st)
+                      : launch_product<Symmetric, false, false>(x_sum[from], x_sum[from], ps, es, st);
+        if (status == SS_OK) status = launch_product<Symmetric, false, false>(s_map, s_map, pq, eq, st);
+        if (status != SS_OK) return status;
+        if (k + 1 < c.steps) {
+            const Next en{x, hi[from ^ 1]};
+            status = tall ? launch_product<Next, false, false>(x_prod[from], q_map, px, en, st)
+                          : launch_product<Next, false, true>(q_map, x_prod[from], px, en, st);
+        } else {
+            Result& r = c.result;
+            r.x = x, r.unscale = unscale, r.cols = static_cast<int>(c.cols);
+            status = tall ? launch_product<Result, false, false>(x_prod[from], q_map, px, r, st)
+                          : launch_product<Result, false, true>(q_map, x_prod[from], px, r, st);
+        }
+        if (status != SS_OK) return status;
+    }
+    return SS_OK;
+}
+
+// The matrices of an argument, checked; a NULL array or pointer is refused.
+struct Mats {
+    Mat m[kMostMatrices];
+    int status;
+    bool vectors;  // every row starts on four elements
+
+    Mats(const void* const* p, int count, int64_t rows, int64_t cols, int64_t stride, size_t eb) : status(SS_OK), vectors(true) {
+        if (p == nullptr || !stride_ok(rows, cols, stride)) {
+            status = SS_ERR_INVALID_ARG;
+            return;
+        }
+        for (int i = 0; i < count; ++i) {
+            if (p[i] == nullptr) status = SS_ERR_INVALID_ARG;
+            m[i] = mat(p[i], rows, cols, stride, eb);
+            if (status == SS_OK && !addr_aligned(p[i], eb)) status = SS_ERR_MISALIGNED;
+            vectors = vectors && m[i].row_aligned(4 * eb);
+        }
+    }
+};
+
+// Whether matrix i of `out` shares an element with any of `in`, but for in[i] in place where that is allowed.
+bool overlaps(const Mats& out, const Mats& in, int count, bool in_place) {
+    for (int i = 0; i < count; ++i)
+        for (int j = 0; j < count; ++j)
+            if (mats_overlap(out.m[i], in.m[j]) && !(in_place && i == j && same_mat(out.m[i], in.m[j]))) return true;
+    return false;
+}
+
+bool overlaps_itself(const Mats& out, int count) {
+    for (int i = 0; i < count; ++i)
+        for (int j = 0; j < i; ++j)
+            if (mats_overlap(out.m[i], out.m[j])) return true;
+    return false;
+}
+
+bool overlaps_scratch(const Mats& a, int count, const void* p, size_t n) {
+    for (int i = 0; i < count; ++i)
+        if (mat_overlaps(a.m[i], p, n)) return true;
+    return false;
+}
+
+int check_coefficients(const float* c, int steps) {
+    if (steps < 1 || steps > SS_ORTHO_MAX_STEPS || c == nullptr) return SS_ERR_INVALID_ARG;
+    for (int i = 0; i < 3 * steps; ++i)
+        if (!std::isfinite(c[i])) return SS_ERR_INVALID_ARG;
+    return SS_OK;
+}
+
+int check_workspace(const Layout& l, const void* workspace, int64_t bytes) {
+    if (workspace == nullptr || bytes < l.bytes) return SS_ERR_INVALID_ARG;
+    return addr_aligned(workspace, 256) ? SS_OK : SS_ERR_MISALIGNED;
+}
+
+void fill(Table* t, const Mats& m, int count) {
+    for (int i = 0; i < count; ++i) t->p[i] = m.m[i].p;
+}
+
+}  // namespace
+}  // namespace ss
+
+using namespace ss;
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+int64_t ss_orthogonal_workspace(int count, int64_t rows, int64_t cols) {
+    if (!sizes_ok(count, rows, cols)) return -1;
+    if (count == 0 || rows == 0 || cols == 0) return 0;
+    Layout l;
+    return layout_of(count, rows, cols, &l) == SS_OK ? l.bytes : -1;
+}
+
+int ss_orthogonalise(const void* const* in, int64_t in_stride, ss_dtype in_dt, void* const* out, int64_t out_stride,
+                     ss_dtype out_dt, int count, int64_t rows, int64_t cols, const float* coefficients, int steps,
+                     void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+    if (!dtype_known(in_dt) || !dtype_known(out_dt) || !sizes_ok(count, rows, cols)) return SS_ERR_INVALID_ARG;
+    int status = check_coefficients(coefficients, steps);
+    if (status != SS_OK) return status;
+    if (count == 0 || rows == 0 || cols == 0) return SS_OK;
+    const Mats a(in, count, rows, cols, in_stride, dtype_bytes(in_dt)), b(out, count, rows, cols, out_stride, dtype_bytes(out_dt));
+    for (const Mats* m : {&a, &b})
+        if (m->status != SS_OK) return m->status;
+    if (overlaps(b, a, count, true) || overlaps_itself(b, count)) return SS_ERR_INVALID_ARG;
+    Layout l;
+    status = layout_of(count, rows, cols, &l);
+    if (status == SS_OK) status = check_workspace(l, workspace, workspace_bytes);
+    if (status != SS_OK) return status;
+    if (overlaps_scratch(a, count, workspace, l.bytes) || overlaps_scratch(b, count, workspace, l.bytes)) return SS_ERR_INVALID_ARG;
+    Call c{};
+    fill(&c.start.in, a, count);
+    c.start.in_stride = a.m[0].stride, c.start.vectors = a.vectors;
+    fill(&c.result.out, b, count);
+    c.result.stride = b.m[0].stride, c.result.dt = out_dt, c.result.vectors = b.vectors;
+    c.in_dt = in_dt, c.count = count, c.rows = rows, c.cols = cols, c.coefficients = coefficients, c.steps = steps;
+    return run(c, l, static_cast<uint8_t*>(workspace), static_cast<cudaStream_t>(cuda_stream));
+}
+
+int ss_orthogonal_update(const void* const* grads, int64_t grad_stride, ss_dtype dt, const float* const* momenta,
+                         float* const* momenta_out, int64_t momentum_stride, const float* const* params,
+                         float* const* params_out, int64_t param_stride, int count, int64_t rows, int64_t cols,
+                         float beta, int nesterov, const float* coefficients, int steps, float lr, float scale,
+                         float weight_decay, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+    if (!dtype_known(dt) || !sizes_ok(count, rows, cols)) return SS_ERR_INVALID_ARG;
+    if (!(beta >= 0.0f && beta < 1.0f) || !std::isfinite(lr) || !std::isfinite(scale) || !std::isfinite(weight_decay)) return SS_ERR_INVALID_ARG;
+    int status = check_coefficients(coefficients, steps);
+    if (status != SS_OK) return status;
+    if (count == 0 || rows == 0 || cols == 0) return SS_OK;
+    using P = const void* const*;
+    const Mats g(grads, count, rows, cols, grad_stride, dtype_bytes(dt));
+    const Mats v(reinterpret_cast<P>(momenta), count, rows, cols, momentum_stride, 4), vo(reinterpret_cast<P>(momenta_out), count, rows, cols, momentum_stride, 4);
+    const Mats p(reinterpret_cast<P>(params), count, rows, cols, param_stride, 4), po(reinterpret_cast<P>(params_out), count, rows, cols, param_stride, 4);
+    for (const Mats* m : {&g, &v, &vo, &p, &po})
+        if (m->status != SS_OK) return m->status;
+    if (overlaps_itself(vo, count) || overlaps_itself(po, count) || overlaps(vo, po, count, false)) return SS_ERR_INVALID_ARG;
+    if (overlaps(vo, v, count, true) || overlaps(vo, g, count, false) || overlaps(vo, p, count, false)) return SS_ERR_INVALID_ARG;
+    if (overlaps(po, p, count, true) || overlaps(po, g, count, false) || overlaps(po, v, count, false)) return SS_ERR_INVALID_ARG;
+    Layout l;
+    status = layout_of(count, rows, cols, &l);
+    if (status == SS_OK) status = check_workspace(l, workspace, workspace_bytes);
+    if (status != SS_OK) return status;
+    for (const Mats* m : {&g, &v, &vo, &p, &po})
+        if (overlaps_scratch(*m, count, workspace, l.bytes)) return SS_ERR_INVALID_ARG;
+    Call c{};
+    Start& s = c.start;
+    fill(&s.in, g, count), fill(&s.momentum, v, count), fill(&s.momentum_out, vo, count);
+    s.in_stride = g.m[0].stride, s.momentum_stride = v.m[0].stride, s.vectors = g.vectors && v.vectors && vo.vectors;
+    s.update = 1, s.nesterov = nesterov != 0, s.beta = beta, s.rest = 1.0f - beta;
+    Result& r = c.result;
+    fill(&r.param, p, count), fill(&r.out, po, count);
+    r.stride = p.m[0].stride, r.dt = SS_F32, r.vectors = p.vectors && po.vectors;
+    r.update = 1, r.lr = lr, r.scale = scale, r.decay = weight_decay;
+    c.in_dt = dt, c.count = count, c.rows = rows, c.cols = cols, c.coefficients = coefficients, c.steps = steps;
+    return run(c, l, static_cast<uint8_t*>(workspace), static_cast<cudaStream_t>(cuda_stream));
+}
+
+#pragma GCC visibility pop
+}  // extern "C"

@@ -1,0 +1,377 @@
+// Products of matrices on the matrix unit, C = A B^T and its transposed forms, with something at the end
+// of each tile: the core that the loss at the head and the orthogonal update share.
+//
+// Two blocks on neighbouring SMs form a 256 x 256 tile: each copies and keeps 128 of its rows of A, 128
+// of its rows of B, and the sums of its 128 rows. One warp copies stages of 64 contraction indices by TMA, one
+// issues the matrix instructions, eight bring the sums out of the tensor memory, whose other half the matrix
+// unit fills meanwhile. An operand may lie in memory with its contraction index fast or slow (XMN); the
+// tiles are swizzled by the copies either way, and nothing is transposed.
+//
+// Operands have 16 bits (bf16 or fp16), sums 32. An fp32 operand goes as three bf16 terms whose sum it is
+// exactly ("planes" of a 3-D tensor map), and a product of two such as six passes, from the
+// smallest terms to the largest; the three that are left out are below 2^-24 of the largest.
+#pragma once
+
+#include <cuda.h>
+
+#include "tcgen05.cuh"
+#include "train.cuh"
+
+namespace ss {
+
+constexpr int kProdTile = 256, kProdHalf = kProdTile / 2;  // of C, in both directions; a block's share
+constexpr int kProdK = 64, kProdStages = 6;                // contraction indices of a stage; stages that shared memory has room for
+constexpr uint32_t kProdOperand = kProdHalf * kProdK * 2, kProdStageBytes = 2 * kProdOperand;
+constexpr uint32_t kProdPanel = kProdK * 128;              // 64 elements of an operand whose contraction index is slow
+constexpr int kProdOut = 256, kProdThreads = kProdOut + 64;  // warps 0-7 bring out, 8 copies, 9 issues
+constexpr uint32_t kProdSquare = 32 * 32 * 4;              // an outgoing warp's own shared memory
+constexpr size_t kProdSmem = 1024 + kProdStages * kProdStageBytes + kProdOut / 32 * kProdSquare;
+
+constexpr int kTerms = 3, kMostPasses = 6;
+
+struct Product {
+    int m, n, k;      // C is m x n, summed over k
+    int batches;      // matrices one after another (the maps' third coordinate), where passes is 1
+    int passes;       // pairs of planes: (plane_a[i], plane_b[i])
+    int8_t plane_a[kMostPasses], plane_b[kMostPasses];
+    int chunk;        // stages that are summed in tensor memory before they are brought out
+    int m_fast;       // the order of tiles: neighbours share columns of C, or rows
+    int upper;        // m == n: only tiles on the diagonal and above
+    int bf16;         // operands: bf16 or fp16
+    int follows;      // another kernel of the call goes before
+    const int* live;  // rows that there are (all of the call's), or NULL
+    int live_from;    // the first of them that is meant here
+    int live_side;    // 1: they are m; 2: they are k (at the call's start one stage at least, whose rows are zeros)
+};
+
+inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms) {
+    Product p{};
+    p.m = static_cast<int>(m), p.n = static_cast<int>(n), p.k = static_cast<int>(k);
+    p.batches = 1, p.passes = 1, p.chunk = 1 << 30, p.bf16 = 1;
+    if (terms) {
+        const int8_t a[kMostPasses] = {0, 2, 1, 0, 1, 0}, b[kMostPasses] = {2, 0, 1, 1, 0, 0};
+        p.passes = kMostPasses;
+        for (int i = 0; i < kMostPasses; ++i) p.plane_a[i] = a[i], p.plane_b[i] = b[i];
+    }
+    return p;
+}
+
+struct Schedule {
+    int m, tiles_m, tiles_n, per_batch, units;
+    int pass_stages, stages;  // of one pass; of all
+};
+
+__device__ __forceinline__ Schedule schedule_of(const Product& p) {
+    Schedule s;
+    int m = p.m, k = p.k;
+    bool any = true;
+    if (p.live != nullptr) {
+        const int live = max(*p.live - p.live_from, 0);
+        any = live > 0 || p.live_from == 0;
+        if (p.live_side == 1) m = min(m, live);
+        else k = max(min(k, live), 1);
+    }
+    s.m = m;
+    s.tiles_m = (m + kProdTile - 1) / kProdTile;
+    s.tiles_n = (p.n + kProdTile - 1) / kProdTile;
+    s.per_batch = p.upper ? s.tiles_m * (s.tiles_m + 1) / 2 : s.tiles_m * s.tiles_n;
+    s.units = any ? s.per_batch * p.batches : 0;
+    s.pass_stages = (k + kProdK - 1) / kProdK;
+    s.stages = s.pass_stages * p.passes;
+    return s;
+}
+
+struct ProdUnit {
+    int batch, m0, n0;
+};
+
+__device__ __forceinline__ ProdUnit prod_unit(const Product& p, const Schedule& s, int u) {
+    ProdUnit r;
+    r.batch = u / s.per_batch;
+    int t = u - r.batch * s.per_batch, i, j;
+    if (p.upper) {
+        for (i = 0; t >= s.tiles_m - i; ++i) t -= s.tiles_m - i;
+        j = i + t;
+    } else if (p.m_fast) {
+        j = t / s.tiles_m, i = t - j * s.tiles_m;
+    } else {
+        i = t / s.tiles_n, j = t - i * s.tiles_n;
+    }
+    r.m0 = i * kProdTile, r.n0 = j * kProdTile;
+    return r;
+}
+
+struct ProdShared {
+    uint64_t full[kProdStages], added[2];  // of the first block: by both blocks
+    uint64_t empty[kProdStages], summed[2], last;
+    uint32_t tmem;
+    int abort;
+};
+
+// 32 x 32 words, a row a lane, to the warp's own shared memory: 16-byte chunk c of row r at chunk c ^ (r & 7).
+__device__ __forceinline__ void square_put(uint32_t buf, int lane, const uint32_t* v) {
+    const uint32_t at = buf + lane * 128 + ((lane & 7) << 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at ^ (i << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+}
+// Words 4 chunk .. 4 chunk + 3 of row `row`.
+__device__ __forceinline__ uint32_t square_at(uint32_t buf, int row, int chunk) { return buf + row * 128 + ((chunk ^ (row & 7)) << 4); }
+__device__ __forceinline__ uint4 square_get(uint32_t buf, int row, int chunk) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(square_at(buf, row, chunk)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void square_set(uint32_t buf, int row, int chunk, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(square_at(buf, row, chunk)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float square_word(uint32_t buf, int row, int col) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(square_at(buf, row, col >> 2) + (col & 3) * 4) : "memory");
+    return v;
+}
+
+constexpr uint32_t kNanBits = 0x7FC00000u;
+
+// EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
+// registers, and gets them at once: EPI(args).whole(unit, m, row, col, lane, buf, sums). Otherwise it gets each chunk in
+// squares of 32 x 32 in the warp's shared memory: fetch(...) before they have come, square(..., first chunk?).
+// A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
+template <class EPI, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kProdThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ Product p,
+               const __grid_constant__ EPI epi) {
+    extern __shared__ uint8_t dynamic[];
+    __shared__ ProdShared sh;
+    const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    volatile int* abort = &sh.abort;
+    uint32_t rank;  // in the pair; the first block issues the matrix instructions and waits for both blocks' operands
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+
+    next_may_begin();
+    if (tid == 0) {
+        for (int s = 0; s < kProdStages; ++s) {
+            mbar_init(smem_addr(&sh.full[s]), 1);
+            mbar_init(smem_addr(&sh.empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_addr(&sh.summed[b]), 1);
+            mbar_init(smem_addr(&sh.added[b]), 2 * kProdOut / 32);
+        }
+        mbar_init(smem_addr(&sh.last), 1);
+        sh.abort = 0;
+        mbar_init_visible();
+    }
+    if (warp == 0) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    if (p.follows) after_previous();
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    const Schedule sc = schedule_of(p);
+
+    if (warp < kProdOut / 32) {
+        // ---- sums out: 32 rows and half of the columns to a warp
+        const int row_local = rank * kProdHalf + (warp & 3) * 32, col_local = (warp >> 2) * kProdHalf;
+        const uint32_t buf = stages + kProdStages * kProdStageBytes + warp * kProdSquare;
+        const uint32_t tmem_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + col_local;
+        const uint32_t added = cluster_addr(smem_addr(&sh.added[0]), 0);
+        uint32_t chunk = 0;
+        bool ok = true;
+        for (int unit = pair; unit < sc.units; unit += pairs) {
+            const ProdUnit u = prod_unit(p, sc, unit);
+            const int row = u.m0 + row_local, col = u.n0 + col_local;
+            if constexpr (EPI::kWhole) {
+                float sums[kProdHalf];
+#pragma unroll
+                for (int i = 0; i < kProdHalf; ++i) sums[i] = 0.0f;
+                for (int left = sc.stages; left > 0; left -= p.chunk, ++chunk) {
+                    if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
+                    tc_fence_after();
+                    const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
+#pragma unroll
+                    for (int j = 0; j < kProdHalf; j += 16) {
+                        uint32_t r[16];
+                        tmem_load16(src + j, r);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sums[j + i] += __uint_as_float(r[i]);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_pair(added + (chunk & 1) * 8);
+                }
+                if (!ok) {
+#pragma unroll
+                    for (int i = 0; i < kProdHalf; ++i) sums[i] = __uint_as_float(kNanBits);
+                }
+                epi.whole(u, sc.m, row, col, lane, buf, sums);
+            } else {
+                bool first = true;
+                for (int left = sc.stages; left > 0; left -= p.chunk, ++chunk) {
+                    if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
+                    tc_fence_after();
+                    const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
+#pragma unroll 1
+                    for (int j = 0; j < kProdHalf; j += 32) {
+                        if (row >= sc.m || col + j >= p.n) continue;
+                        typename EPI::Fetched f;
+                        epi.fetch(u, sc.m, row, col + j, lane, f);
+                        uint32_t r[32];
+                        tmem_load32(src + j, r);
+                        tmem_load_wait();
+                        if (!ok) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) r[i] = kNanBits;
+                        }
+                        square_put(buf, lane, r);
+                        __syncwarp();
+                        epi.square(u, sc.m, row, col + j, lane, buf, f, first);
+                        __syncwarp();
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_pair(added + (chunk & 1) * 8);
+                    first = false;
+                }
+            }
+        }
+    } else if (warp == kProdOut / 32) {
+        // Roles of one lane each, but the whole warp walks through them, so that addresses and descriptors are formed
+        // in uniform registers.
+        // ---- copies: this block's halves, counted by the first block's barrier
+        const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
+        const bool leader = elect_one();
+        int it = 0, slot = 0;
+        uint32_t parity = 1;
+        for (int unit = pair; unit < sc.units; unit += pairs) {
+            const ProdUnit u = prod_unit(p, sc, unit);
+            const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + rank * kProdHalf;
+            int pass = 0, k0 = 0;
+            const int end = sc.pass_stages * kProdK;
+#pragma unroll 1
+            for (int s = 0; s < sc.stages; ++s) {
+                mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
+                const uint32_t bar = full + slot * 8, dst = stages + slot * kProdStageBytes;
+                const int za = p.passes > 1 ? p.plane_a[pass] : u.batch, zb = p.passes > 1 ? p.plane_b[pass] : u.batch;
+                if (leader) {
+                    if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, 2 * kProdStageBytes);
+                    if constexpr (A_MN) {
+                        tma_load_3d_pair(dst, &a_map, bar, m0, k0, za);
+                        tma_load_3d_pair(dst + kProdPanel, &a_map, bar, m0 + 64, k0, za);
+                    } else {
+                        tma_load_3d_pair(dst, &a_map, bar, k0, m0, za);
+                    }
+                    if constexpr (B_MN) {
+                        tma_load_3d_pair(dst + kProdOperand, &b_map, bar, n0, k0, zb);
+                        tma_load_3d_pair(dst + kProdOperand + kProdPanel, &b_map, bar, n0 + 64, k0, zb);
+                    } else {
+                        tma_load_3d_pair(dst + kProdOperand, &b_map, bar, k0, n0, zb);
+                    }
+                }
+                ++it;
+                k0 += kProdK;
+                if (k0 == end) k0 = 0, ++pass;
+                if (++slot == kProdStages) slot = 0, parity ^= 1;
+            }
+        }
+        // the last signals, and copies, arrive in this block's memory: not before that
+        const int from = it > kProdStages ? it - kProdStages : 0;
+        for (int i = from; i < it; ++i) mbar_wait_uniform(empty + i % kProdStages * 8, (i / kProdStages) & 1, &sh.abort);
+        if (*abort != 0 && rank == 0) {
+            int own = 0;
+            for (int i = from; i < it; ++i) mbar_wait(smem_addr(&sh.full[i % kProdStages]), (i / kProdStages) & 1, &own);
+        }
+    } else if (rank == 0) {
+        // ---- matrix unit
+        const uint32_t idesc = tc_idesc(kProdTile, kProdTile, p.bf16 != 0, A_MN, B_MN);
+        constexpr uint32_t kStep = kProdStageBytes >> 4, kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
+        const uint64_t desc_a = A_MN ? tc_desc_rows(stages, kProdPanel) : tc_desc_cols(stages);
+        const uint64_t desc_b = B_MN ? tc_desc_rows(stages + kProdOperand, kProdPanel) : tc_desc_cols(stages + kProdOperand);
+        const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
+        const bool leader = elect_one();
+        uint32_t slot = 0, parity = 0, chunk = 0;
+        for (int unit = pair; unit < sc.units; unit += pairs) {
+            for (int left = sc.stages; left > 0; left -= p.chunk, ++chunk) {
+                const int n = min(left, p.chunk);
+                const uint32_t d = tmem + (chunk & 1) * kProdTile;
+                // the half of the tensor memory is free once the chunk before the last has been brought out
+                if (chunk >= 2) mbar_wait_uniform(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, &sh.abort);
+                tc_fence_after();
+#pragma unroll 1
+                for (int s = 0; s < n; ++s) {
+                    mbar_wait_uniform(full + slot * 8, parity, &sh.abort);
+                    tc_fence_after();
+                    const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < kProdK / 16; ++k) tc_mma_f16_pair(d, da + k * kStepA, db + k * kStepB, idesc, s != 0 || k != 0);
+                        tc_commit_pair(empty + slot * 8);
+                    }
+                    __syncwarp();
+                    if (++slot == kProdStages) slot = 0, parity ^= 1;
+                }
+                if (leader) tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
+                __syncwarp();
+            }
+        }
+        // nothing may still be running when the tensor memory is given back
+        int own = 0;
+        if (leader) tc_commit_pair(smem_addr(&sh.last));
+        mbar_wait(smem_addr(&sh.last), 0, &own);
+    }
+    // neither block leaves while the other may still signal to it or use its operands
+    tc_fence_before();
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    tc_fence_after();
+    if (warp == 0) tmem_free_pair(tmem, 512);
+}
+
+// ---- host side -------------------------------------------------------------------------------------
+
+// An operand's map: `fast` elements of unit stride, `slow` rows `row_bytes` apart, `planes` of them. mn: the contraction index is the slow one.
+inline int map_operand(CUtensorMap* map, const void* p, bool bf16, int64_t fast, int64_t slow, int64_t row_bytes, int64_t planes, int64_t plane_bytes, bool mn) {
+    cudaError_t e;
+    const EncodeTiled encode = encode_tiled(&e);
+    if (encode == nullptr) return cuda_status_public(e);
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(fast), static_cast<cuuint64_t>(slow), static_cast<cuuint64_t>(planes)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_bytes), static_cast<cuuint64_t>(planes > 1 ? plane_bytes : row_bytes)};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(mn ? kProdK : kProdHalf), 1}, ones[3] = {1, 1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims, strides, box, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? SS_OK : SS_ERR_UNSUPPORTED;
+}
+
+template <class EPI, bool A_MN, bool B_MN>
+int launch_product(const CUtensorMap& a, const CUtensorMap& b, const Product& p, const EPI& epi, cudaStream_t st) {
+    cudaError_t e = cudaSuccess;
+    const int sms = device_sm_count(&e);
+    if (e != cudaSuccess) return cuda_status_public(e);
+    const auto kernel = product_kernel<EPI, A_MN, B_MN>;
+    struct Key {};
+    e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kProdSmem));
+    if (e != cudaSuccess) return cuda_status_public(e);
+    const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile;
+    int64_t units = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
+    if (units > sms / 2) units = sms / 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * units));
+    cfg.blockDim = dim3(kProdThreads);
+    cfg.dynamicSmemBytes = kProdSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = p.follows ? 2 : 1;
+    return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, a, b, p, epi));
+}
+
+}  // namespace ss

@@ -2,8 +2,11 @@
 // waits on shared-memory barriers.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <atomic>
 
 namespace ss {
 
@@ -111,9 +114,9 @@ __device__ __forceinline__ void tmem_free_pair(uint32_t addr, uint32_t columns) 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// D[tmem] (+)= A B over a pair of blocks, both operands bf16 in shared memory: each block holds
+// D[tmem] (+)= A B over a pair of blocks, both operands bf16 or both fp16 in shared memory: each block holds
 // half of A's rows (and of D's) and half of B's columns. Issued by one thread of the first block.
-__device__ __forceinline__ void tc_mma_bf16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void tc_mma_f16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
 }
@@ -135,6 +138,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
 }
+// 16 columns.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory operand whose contraction index is the slow one: panels of 64 elements (128
@@ -145,9 +156,36 @@ __device__ __forceinline__ uint64_t tc_desc_rows(uint32_t addr, uint32_t panel) 
            (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
+// The same whose contraction index is the fast one: rows of 64 elements of it (128 bytes, swizzled), 1024 bytes from 8 rows to the next 8.
+__device__ __forceinline__ uint64_t tc_desc_cols(uint32_t addr) {
+    return static_cast<uint64_t>((addr >> 4) & 0x3FFF) | (1ull << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// fp32 sums of bf16 or fp16 products; an operand's contraction index is slow (rows) or fast.
+__device__ __forceinline__ constexpr uint32_t tc_idesc(uint32_t m, uint32_t n, bool bf16, bool a_rows, bool b_rows) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_rows ? 1u << 15 : 0u) | (b_rows ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
 // fp32 sums of bf16 products, both operands with the contraction index slow.
-__device__ __forceinline__ constexpr uint32_t tc_idesc_bf16_rows(uint32_t m, uint32_t n) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
+__device__ __forceinline__ constexpr uint32_t tc_idesc_bf16_rows(uint32_t m, uint32_t n) { return tc_idesc(m, n, true, true, true); }
+
+// ---- host side: the driver's function that describes a tensor to the copies
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiled encode_tiled(cudaError_t* err) {
+    static std::atomic<void*> known{nullptr};
+    void* f = known.load(std::memory_order_relaxed);
+    *err = cudaSuccess;
+    if (f == nullptr) {
+        cudaDriverEntryPointQueryResult found;
+        *err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+        if (*err == cudaSuccess && (found != cudaDriverEntryPointSuccess || f == nullptr)) *err = cudaErrorSymbolNotFound;
+        if (*err != cudaSuccess) return nullptr;
+        known.store(f, std::memory_order_relaxed);
+    }
+    return reinterpret_cast<EncodeTiled>(f);
 }
 
 }  // namespace ss

@@ -19,10 +19,6 @@
 // 4099 x 1000 x 2050 fp32 takes 73 us, of them 7 to split dY and 5 to join the parts. The three terms of 32 rows in
 // one stage, decoded once, took 66 us, but the small terms, added to the large one's sums, each cost a truncation:
 // 2.0e-6 instead of 5e-7, and at 352 rows a chunk, where it is 1.1e-6 like the plain form's, 73 us again.
-#include <cuda.h>
-
-#include <atomic>
-
 #include "act8.cuh"
 #include "tcgen05.cuh"
 
@@ -443,7 +439,7 @@ weight_grad8_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_con
                         const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
                         if (leader) {
 #pragma unroll
-                            for (int k = 0; k < kRows / 16; ++k) tc_mma_bf16_pair(d, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, s != 0 || k != 0);
+                            for (int k = 0; k < kRows / 16; ++k) tc_mma_f16_pair(d, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, s != 0 || k != 0);
                             tc_commit_pair(empty + slot * 8);
                         }
                         __syncwarp();
@@ -592,24 +588,6 @@ int layout_of(const void* dy, int64_t dy_stride, ss_dtype dt, int64_t rows, int6
     p.units = p.whole + others * p.parts;
     out->partial_bytes = p.parts > 1 ? static_cast<int64_t>(others) * p.parts * kTileN * kTileK * 4 : 0;
     return SS_OK;
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled(cudaError_t* err) {
-    static std::atomic<void*> known{nullptr};
-    void* f = known.load(std::memory_order_relaxed);
-    *err = cudaSuccess;
-    if (f == nullptr) {
-        cudaDriverEntryPointQueryResult found;
-        *err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
-        if (*err == cudaSuccess && (found != cudaDriverEntryPointSuccess || f == nullptr)) *err = cudaErrorSymbolNotFound;
-        if (*err != cudaSuccess) return nullptr;
-        known.store(f, std::memory_order_relaxed);
-    }
-    return reinterpret_cast<EncodeTiled>(f);
 }
 
 // SMs that the plan is made for. Without a device (sizes asked for on a host without one) the B200's.
