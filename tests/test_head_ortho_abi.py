@@ -54,7 +54,7 @@ def test_head_refusals(L):
         assert head(L, scratch=other) == BAD
     far = dict(x=1 << 44, w=2 << 44, y=3 << 44, k=4 << 44, logp=5 << 44, dx=6 << 44, dw=7 << 44)
     assert head(L, rows=(1 << 24) + 1, **far) == UNS
-    assert head(L, vocab=(1 << 31) - 1, width=1 << 10, ws=1 << 10, dws=1 << 10, xs=1 << 10, dxs=1 << 10, **far) == UNS
+    assert head(L, vocab=(1 << 31) - 1, rows=1024, **far) == UNS
 
 
 @pytest.mark.parametrize("dt", [0, 1])
