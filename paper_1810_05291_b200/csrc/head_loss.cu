@@ -23,7 +23,7 @@ namespace ss {
 namespace {
 
 constexpr int kPartCols = kProdHalf;              // logits of a thread
-constexpr int kLogitChunk = 4;                    // stages that the matrix unit sums of a logit
+constexpr int kLogitChunk = 16;                    // stages that the matrix unit sums of a logit
 // Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16; 2048 lose 5e-7.
 constexpr int kGradChunk = 256, kGradChunkF32 = 32;
 constexpr int64_t kChunkBytes = int64_t(1) << 30; // of e and P
@@ -51,7 +51,7 @@ struct Head {
     uint16_t *gathered, *staged_w;
     float2* parts;                  // [chunk rows][n_parts]: maximum, sum
     uint16_t *e16, *p16;            // e, P of bf16 inputs (the same place); planes of P of fp32 ones
-    float *e32, *acc;
+    float *e32, *acc, *partial;
     int64_t width_ld, e_ld, row_cap, chunk_rows;
     int n_parts, first;             // first row of the chunk
 };
@@ -61,30 +61,43 @@ __device__ __forceinline__ bool counts(const Head& a, int64_t t) {
     return a.weights[t] != 0.0f && y >= 0 && y < a.vocab;
 }
 
-// Which rows count, in their order.
+// Which rows count, in their order. One block; four rows of a thread under way at a time.
 __global__ void __launch_bounds__(1024) head_rows_kernel(const __grid_constant__ Head a) {
     next_may_begin();
-    __shared__ int sums[32];
+    __shared__ int sums[4][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int base = 0;
-    for (int64_t t0 = 0; t0 < a.rows; t0 += 1024) {
-        const int64_t t = t0 + threadIdx.x;
-        const bool in = t < a.rows && counts(a, t);
-        const uint32_t votes = __ballot_sync(0xFFFFFFFFu, in);
-        if (lane == 0) sums[warp] = __popc(votes);
+    for (int64_t t0 = 0; t0 < a.rows; t0 += 4096) {
+        int64_t y[4];
+        float w[4];
+        uint32_t votes[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t t = t0 + 1024 * i + threadIdx.x;
+            y[i] = t < a.rows ? a.targets[t] : -1, w[i] = t < a.rows ? a.weights[t] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            votes[i] = __ballot_sync(0xFFFFFFFFu, w[i] != 0.0f && y[i] >= 0 && y[i] < a.vocab);
+            if (lane == 0) sums[i][warp] = __popc(votes[i]);
+        }
         __syncthreads();
-        int before = 0, all = 0;
-        for (int i = 0; i < 32; ++i) {
-            const int n = sums[i];
-            if (i < warp) before += n;
-            all += n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            int before = sums[i][lane];  // of the warps up to that of this lane's number
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int n = __shfl_up_sync(0xFFFFFFFFu, before, d);
+                if (lane >= d) before += n;
+            }
+            const int all = __shfl_sync(0xFFFFFFFFu, before, 31), mine = __shfl_sync(0xFFFFFFFFu, before, (warp + 31) & 31);
+            if (votes[i] >> lane & 1) {
+                const int s = base + (warp > 0 ? mine : 0) + __popc(votes[i] & ((1u << lane) - 1u));
+                a.index[s] = static_cast<int>(t0 + 1024 * i + threadIdx.x);
+                a.target[s] = static_cast<int>(y[i]);
+            }
+            base += all;
         }
-        if (in) {
-            const int s = base + before + __popc(votes & ((1u << lane) - 1u));
-            a.index[s] = static_cast<int>(t);
-            a.target[s] = static_cast<int>(a.targets[t]);
-        }
-        base += all;
         __syncthreads();
     }
     if (threadIdx.x == 0) *a.live = base;
@@ -298,101 +311,223 @@ __global__ void __launch_bounds__(256) head_statistics_kernel(const __grid_const
     }
 }
 
-// e -> P: eight columns to a thread. Rows behind the last up to a whole stage become zeros.
+// e -> P: four times eight columns to a thread, all loads before the first store. Rows behind the last up to a whole stage
+// become zeros.
+constexpr int kGradientPieces = 4;
+
 template <bool F32>
 __global__ void __launch_bounds__(256) head_gradient_kernel(const __grid_constant__ Head a) {
     next_may_begin();
     after_previous();
-    const int64_t r = blockIdx.y + static_cast<int64_t>(blockIdx.z) * 65535, here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
+    const int64_t r = blockIdx.y, here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
     const int64_t upto = max((here + kProdK - 1) / kProdK * kProdK, static_cast<int64_t>(a.first == 0 ? kProdK : 0));
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (r >= min(upto, a.chunk_rows) || c >= a.e_ld) return;
-    float v[8];
+    const int c0 = blockIdx.x * (256 * 8 * kGradientPieces) + threadIdx.x * 8, end = static_cast<int>(a.e_ld);
+    if (r >= min(upto, a.chunk_rows)) return;
+    uint16_t* const out = a.p16 + r * a.e_ld;
+    const int64_t plane = a.chunk_rows * a.e_ld;  // of fp32's terms
     if (r >= here) {
+        for (int c = c0, i = 0; i < kGradientPieces && c < end; c += 256 * 8, ++i)
+            for (int q = 0; q < (F32 ? kTerms : 1); ++q) *reinterpret_cast<uint4*>(out + q * plane + c) = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    uint4 x[kGradientPieces][F32 ? 2 : 1];
+    float top[kGradientPieces];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    } else {
-        const float2 part = a.parts[r * a.n_parts + c / kPartCols];
-        // an empty part, or one of -inf alone, has m = -inf and zeros for e
-        const float f = a.factor[r] * (part.x == -INFINITY ? 0.0f : ex2((part.x - a.top[r]) * a.k));
+    for (int i = 0; i < kGradientPieces; ++i) {
+        const int c = c0 + i * 256 * 8;
+        if (c >= end) continue;
         if constexpr (F32) {
-            const float4* const src = reinterpret_cast<const float4*>(a.e32 + r * a.e_ld + c);
-            const float4 x = src[0], y = src[1];
-            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+            const uint4* const src = reinterpret_cast<const uint4*>(a.e32 + r * a.e_ld + c);
+            x[i][0] = __ldcs(src), x[i][1] = __ldcs(src + 1);
         } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(a.e16 + r * a.e_ld + c);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            x[i][0] = __ldcs(reinterpret_cast<const uint4*>(a.e16 + r * a.e_ld + c));
+        }
+        top[i] = a.parts[r * a.n_parts + c / kPartCols].x;
+    }
+    const float factor = a.factor[r], row_top = a.top[r], target_grad = a.target_grad[r];
+    const int target = a.target[a.first + r];
+#pragma unroll
+    for (int i = 0; i < kGradientPieces; ++i) {
+        const int c = c0 + i * 256 * 8;
+        if (c >= end) continue;
+        // an empty part, or one of -inf alone, has -inf for its maximum and zeros for e
+        const float f = factor * (top[i] == -INFINITY ? 0.0f : ex2((top[i] - row_top) * a.k));
+        float v[8];
+        if constexpr (F32) {
+            const uint4 y = x[i][0], z = x[i][1];
+            const uint32_t w[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+        } else {
+            const uint32_t w[4] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
                 v[2 * j] = p.x, v[2 * j + 1] = p.y;
             }
         }
-        const int y = a.target[a.first + r] - c;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j == y ? a.target_grad[r] : v[j] * f;
-    }
-    if constexpr (F32) {
-        const int64_t plane = a.chunk_rows * a.e_ld;
-        const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-        store_terms(a.p16 + r * a.e_ld + c, plane, lo);
-        store_terms(a.p16 + r * a.e_ld + c + 4, plane, hi);
-    } else {
-        *reinterpret_cast<uint4*>(a.p16 + r * a.e_ld + c) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+        for (int j = 0; j < 8; ++j) v[j] *= f;
+        const int y = target - c;
+        if (y >= 0 && y < 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j == y ? target_grad : v[j];
+        }
+        if constexpr (F32) {
+            const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+            store_terms(out + c, plane, lo);
+            store_terms(out + c + 4, plane, hi);
+        } else {
+            *reinterpret_cast<uint4*>(out + c) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+        }
     }
 }
 
 // ---- the end of the gradients' products: written, or added by the memory itself (the same lane adds to an element each
-// time, so its sums come in their order).
-struct Gradient {
-    static constexpr bool kWhole = false;
-    struct Fetched {};
-    float* dst;
-    uint16_t* dst16;  // bf16 instead; every chunk but the first would be lost, so there is one
-    int64_t stride;
+// time, so its sums come in their order). A part of a tile goes to a place of its own.
+__device__ __forceinline__ void add_global(float* p, float4 v) {
+    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(__cvta_generic_to_global(p)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void add_global(float* p, float v) {
+    asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(__cvta_generic_to_global(p)), "f"(v) : "memory");
+}
+
+constexpr int kTileFloats = kProdTile * kProdTile;
+
+// Where a gradient goes: fp32, or bf16 that takes the sums of earlier rows (fp32) into its rounding.
+struct Dest {
+    float* f32;
+    uint16_t* bf16;
+    const float* before;  // with bf16: those sums, or NULL
+    int64_t stride, before_stride;
     int cols, vectors, add;
 
-    __device__ __forceinline__ void fetch(const ProdUnit&, int, int, int, int, Fetched&) const {}
-    __device__ __forceinline__ void square(const ProdUnit&, int m, int row, int col, int lane, uint32_t buf, const Fetched&, bool first) const {
-        const int c = col + 4 * (lane & 7);
-        if (c >= cols) return;
-        const bool adds = add || !first;
+    __device__ __forceinline__ void put(int64_t row, int c, float4 v, float4 b, bool adds) const {
+        const int64_t at = row * stride + c;
+        v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
+        if (vectors && c + 4 <= cols) {
+            if (bf16 != nullptr) *reinterpret_cast<uint2*>(bf16 + at) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+            else if (adds) add_global(f32 + at, v);
+            else *reinterpret_cast<float4*>(f32 + at) = v;
+        } else {
+            const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int q = (lane >> 3) + 4 * i;
-            const uint4 w = square_get(buf, q, lane & 7);
-            if (row + q >= m) continue;
-            const int64_t at = (row + q) * stride + c;
-            const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
-            if (vectors && c + 4 <= cols) {
-                if (dst16 != nullptr) *reinterpret_cast<uint2*>(dst16 + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-                else if (adds) asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(__cvta_generic_to_global(dst + at)), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
-                else *reinterpret_cast<float4*>(dst + at) = make_float4(v[0], v[1], v[2], v[3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c + j >= cols) break;
-                    if (dst16 != nullptr) Elem<uint16_t>::store(dst16 + at + j, v[j]);
-                    else if (adds) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(__cvta_generic_to_global(dst + at + j)), "f"(v[j]) : "memory");
-                    else dst[at + j] = v[j];
-                }
+            for (int j = 0; j < 4; ++j) {
+                if (c + j >= cols) break;
+                if (bf16 != nullptr) Elem<uint16_t>::store(bf16 + at + j, e[j]);
+                else if (adds) add_global(f32 + at + j, e[j]);
+                else f32[at + j] = e[j];
             }
         }
     }
+    __device__ __forceinline__ float4 earlier(int64_t row, int c) const {
+        return before == nullptr ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : *reinterpret_cast<const float4*>(before + row * before_stride + c);
+    }
 };
+
+// OUT16: to.bf16, else to.f32. BEFORE: with to.before.
+template <bool OUT16, bool BEFORE>
+struct Gradient {
+    static constexpr bool kWhole = false;
+    struct Fetched {
+        float4 before[BEFORE ? 8 : 1];
+    };
+    Dest to;
+    float* partial;
+
+    struct Tile {
+        char* p;       // this lane's first row, at its first column
+        int64_t step;  // bytes from its row to the next
+        const float* before;
+        int row, col, rows, cols;  // rows and columns: that exist from there on
+        int part;
+        bool add;
+
+        __device__ __forceinline__ Tile(const Gradient& e, const ProdUnit& u, int m, int row0, int col0, int lane) {
+            row = row0 + (lane >> 3), col = col0 + 4 * (lane & 7), part = u.part, add = e.to.add;
+            rows = m - row, cols = e.to.cols - col;
+            if (part >= 0) {
+                p = reinterpret_cast<char*>(e.partial + static_cast<int64_t>(part) * kTileFloats + (row - u.m0) * kProdTile + (col - u.n0));
+                step = 4 * kProdTile * 4;
+                add = false;
+            } else {
+                const int64_t at = row * e.to.stride + col;
+                p = OUT16 ? reinterpret_cast<char*>(e.to.bf16 + at) : reinterpret_cast<char*>(e.to.f32 + at);
+                step = 4 * e.to.stride * (OUT16 ? 2 : 4);
+            }
+            before = BEFORE ? e.to.before + row * e.to.before_stride + col : nullptr;
+        }
+        __device__ __forceinline__ void fetch(const Gradient& e, int j, Fetched& f) const {
+            if constexpr (BEFORE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    f.before[i] = part < 0 && 4 * i < rows && j < cols ? *reinterpret_cast<const float4*>(before + j + 4 * i * e.to.before_stride) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+        }
+        __device__ __forceinline__ void square(const Gradient& e, int j, int lane, uint32_t buf, const Fetched& f, bool first) const {
+            const bool adds = add || !first;
+            char* q = p + j * (OUT16 && part < 0 ? 2 : 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i, q += step) {
+                const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+                float4 v = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+                if (4 * i >= rows || j >= cols) continue;
+                if (part >= 0 || (e.to.vectors && j + 4 <= cols)) {
+                    if constexpr (BEFORE) v.x += f.before[i].x, v.y += f.before[i].y, v.z += f.before[i].z, v.w += f.before[i].w;
+                    if (OUT16 && part < 0) *reinterpret_cast<uint2*>(q) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+                    else if (adds) add_global(reinterpret_cast<float*>(q), v);
+                    else *reinterpret_cast<float4*>(q) = v;
+                } else {
+                    e.to.put(row + 4 * i, col + j, v, BEFORE ? f.before[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f), adds);
+                }
+            }
+        }
+    };
+};
+
+// Four columns of a tile that came in parts, the parts in their order, four under way at a time.
+__device__ __forceinline__ float4 joined(const float* partial, const Schedule& sc, int other, int r, int c) {
+    const float* const p = partial + static_cast<int64_t>(other) * sc.parts * kTileFloats + r * kProdTile + c;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s = 0; s < sc.parts; s += 4) {
+        float4 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            x[u] = s + u < sc.parts ? __ldcs(reinterpret_cast<const float4*>(p + static_cast<int64_t>(s + u) * kTileFloats)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v.x += x[u].x, v.y += x[u].y, v.z += x[u].z, v.w += x[u].w;
+    }
+    return v;
+}
+
+// dW of the tiles that came in parts.
+__global__ void __launch_bounds__(256) head_join_kernel(const __grid_constant__ Product p, const __grid_constant__ Dest to, const float* partial) {
+    next_may_begin();
+    after_previous();
+    const Schedule sc = schedule_of(p);
+    const int others = sc.parts > 1 ? sc.per_batch - sc.whole : 0, i = (blockIdx.y * 256 + threadIdx.x) * 4;
+    for (int other = blockIdx.x; other < others; other += gridDim.x) {
+        const ProdUnit u = prod_unit(p, sc, sc.whole + other * sc.parts);
+        const int r = u.m0 + i / kProdTile, c = u.n0 + i % kProdTile;
+        if (r < sc.m && c < p.n) to.put(r, c, joined(partial, sc, other, i / kProdTile, i % kProdTile), to.earlier(r, c), to.add);
+    }
+}
 
 // dx of the chunk's rows, from their sums to their places.
 template <typename T>
-__global__ void __launch_bounds__(256) head_dx_kernel(const __grid_constant__ Head a) {
+__global__ void __launch_bounds__(256) head_dx_kernel(const __grid_constant__ Head a, const __grid_constant__ Product p) {
     next_may_begin();
     after_previous();
     const int lane = threadIdx.x & 31;
+    const Schedule sc = schedule_of(p);
     const int64_t here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
     for (int64_t r = blockIdx.x * 8 + (threadIdx.x >> 5); r < here; r += gridDim.x * 8) {
         const float* const src = a.acc + r * a.width_ld;
         T* const dst = static_cast<T*>(a.dx) + a.index[a.first + r] * a.dx_stride;
         for (int c = 4 * lane; c < a.width; c += 128) {
-            const float4 v = *reinterpret_cast<const float4*>(src + c);
+            const int tile = c / kProdTile * sc.tiles_m + static_cast<int>(r / kProdTile);
+            const float4 v = tile < sc.whole ? *reinterpret_cast<const float4*>(src + c)
+                                             : joined(a.partial, sc, tile - sc.whole, static_cast<int>(r % kProdTile), c % kProdTile);
             if (a.dx_vectors && c + 4 <= a.width) {
                 if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst + c) = v;
                 else *reinterpret_cast<uint2*>(dst + c) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
@@ -404,14 +539,6 @@ __global__ void __launch_bounds__(256) head_dx_kernel(const __grid_constant__ He
             }
         }
     }
-}
-
-// Sums in fp32 to a dW of bf16, where they came in several chunks.
-__global__ void __launch_bounds__(256) head_round_kernel(const float* src, int64_t src_stride, uint16_t* dst, int64_t stride, int64_t rows, int width) {
-    next_may_begin();
-    after_previous();
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < width; c += 256) Elem<uint16_t>::store(dst + r * stride + c, src[r * src_stride + c]);
 }
 
 __global__ void __launch_bounds__(256) head_zero_kernel(void* dst, int64_t row_bytes, int64_t stride_bytes, int64_t rows) {
@@ -446,12 +573,19 @@ __global__ void __launch_bounds__(1024) head_totals_kernel(const __grid_constant
 
 constexpr int64_t kMostRows = int64_t(1) << 24, kMostTilesHead = int64_t(1) << 24;
 
+// SMs that the workspace is made for. Without a device (sizes asked for on a host without one) the B200's.
+int plan_sms() {
+    cudaError_t err = cudaSuccess;
+    const int sms = device_sm_count(&err);
+    return err == cudaSuccess && sms > 0 ? sms : 148;
+}
+
 inline int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 struct Layout {
     bool f32, dx, dw, stage_w, sums_w;  // sums_w: dW of bf16 from several chunks
     int64_t planes, width_ld, e_ld, n_parts, chunks, chunk_rows, row_cap;
-    int64_t index, target, live, rows_f32, gathered, staged_w, parts, e, p, acc, w32, bytes;
+    int64_t index, target, live, rows_f32, gathered, staged_w, parts, e, p, acc, w32, partial, bytes;
 };
 
 int layout_of(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_t width, int64_t vocab, bool dx, bool dw, ss_dtype dw_dt, Layout* l) {
@@ -484,6 +618,7 @@ int layout_of(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_
     l->p = l->f32 && (dx || dw) ? place(kTerms * l->chunk_rows * l->e_ld * 2) : l->e;
     l->acc = place(dx ? l->chunk_rows * l->width_ld * 4 : 0);
     l->w32 = place(l->sums_w ? vocab * l->width_ld * 4 : 0);
+    l->partial = place(dx || dw ? static_cast<int64_t>(plan_sms() / 2) * kTileFloats * 4 : 0);
     l->bytes = at;
     return SS_OK;
 }
@@ -497,6 +632,13 @@ unsigned blocks_for(int64_t warps, int sms) {
     return static_cast<unsigned>(want < 1 ? 1 : (want < most ? want : most));
 }
 
+// Whether a product over as many rows as the call has may come in parts (it does not with the rows that count where those are too few).
+bool may_split(const Product& p) {
+    const int64_t tiles = static_cast<int64_t>((p.m + kProdTile - 1) / kProdTile) * ((p.n + kProdTile - 1) / kProdTile), others = tiles % p.pairs;
+    const int64_t stages = static_cast<int64_t>((p.k + kProdK - 1) / kProdK) * p.passes;
+    return others > 0 && p.pairs / others > 1 && stages / kLeastPart > 1;
+}
+
 int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_dtype dw_dt, bool dw_vectors, int accumulate, cudaStream_t st) {
     cudaError_t e = cudaSuccess;
     const int sms = device_sm_count(&e);
@@ -508,7 +650,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
     a.gathered = reinterpret_cast<uint16_t*>(ws + l.gathered), a.staged_w = reinterpret_cast<uint16_t*>(ws + l.staged_w);
     a.parts = reinterpret_cast<float2*>(ws + l.parts);
     a.e16 = reinterpret_cast<uint16_t*>(ws + l.e), a.e32 = reinterpret_cast<float*>(ws + l.e), a.p16 = reinterpret_cast<uint16_t*>(ws + l.p);
-    a.acc = reinterpret_cast<float*>(ws + l.acc);
+    a.acc = reinterpret_cast<float*>(ws + l.acc), a.partial = reinterpret_cast<float*>(ws + l.partial);
     a.width_ld = l.width_ld, a.e_ld = l.e_ld, a.row_cap = l.row_cap, a.chunk_rows = l.chunk_rows, a.n_parts = static_cast<int>(l.n_parts);
     const bool grads = l.dx || l.dw;
     const int64_t rows = a.rows, width = a.width, vocab = a.vocab;
@@ -539,7 +681,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         if (status == SS_OK && l.dw) status = map_operand(&p_rows, a.p16, true, vocab, l.chunk_rows, p_row, l.planes, p_plane, true);
         if (status != SS_OK) return status;
 
-        Product pz = product_of(l.chunk_rows, vocab, width, l.f32);
+        Product pz = product_of(l.chunk_rows, vocab, width, l.f32, sms);
         pz.chunk = kLogitChunk, pz.m_fast = 1, pz.follows = 1, pz.live = a.live, pz.live_from = a.first, pz.live_side = 1;
         const Logits ez{a.target + first, a.target_logit, a.parts, grads && !l.f32 ? a.e16 : nullptr, grads && l.f32 ? a.e32 : nullptr,
                         l.e_ld, a.n_parts, a.vocab, a.k};
@@ -548,41 +690,45 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         e = launch_next(true, head_statistics_kernel, blocks_for(l.chunk_rows, sms), 256, st, a);
         if (e != cudaSuccess) return cuda_status_public(e);
         if (!grads) continue;
-        const dim3 grid(static_cast<unsigned>((l.e_ld / 8 + 255) / 256), static_cast<unsigned>(l.chunk_rows));
+        const int64_t wide = 256 * 8 * kGradientPieces;
+        const dim3 grid(static_cast<unsigned>((l.e_ld + wide - 1) / wide), static_cast<unsigned>(l.chunk_rows));
         e = l.f32 ? launch_next(true, head_gradient_kernel<true>, grid, 256, st, a) : launch_next(true, head_gradient_kernel<false>, grid, 256, st, a);
         if (e != cudaSuccess) return cuda_status_public(e);
         if (l.dx) {
-            Product px = product_of(l.chunk_rows, width, vocab, l.f32);
+            Product px = product_of(l.chunk_rows, width, vocab, l.f32, sms);
             px.chunk = l.f32 ? kGradChunkF32 : kGradChunk, px.m_fast = 1, px.follows = 1, px.live = a.live, px.live_from = a.first, px.live_side = 1;
-            const Gradient ex{a.acc, nullptr, l.width_ld, a.width, 1, 0};
-            status = launch_product<Gradient, false, true>(p_cols, w_rows, px, ex, st);
+            px.split = 1;
+            const Gradient<false, false> ex{{a.acc, nullptr, nullptr, l.width_ld, 0, a.width, 1, 0}, a.partial};
+            status = launch_product<Gradient<false, false>, false, true>(p_cols, w_rows, px, ex, st);
             if (status != SS_OK) return status;
-            e = l.f32 ? launch_next(true, head_dx_kernel<float>, blocks_for(l.chunk_rows, sms), 256, st, a)
-                      : launch_next(true, head_dx_kernel<uint16_t>, blocks_for(l.chunk_rows, sms), 256, st, a);
+            e = l.f32 ? launch_next(true, head_dx_kernel<float>, blocks_for(l.chunk_rows, sms), 256, st, a, px)
+                      : launch_next(true, head_dx_kernel<uint16_t>, blocks_for(l.chunk_rows, sms), 256, st, a, px);
             if (e != cudaSuccess) return cuda_status_public(e);
         }
         if (l.dw) {
-            Product pw = product_of(vocab, width, l.chunk_rows, l.f32);
-            pw.follows = 1, pw.live = a.live, pw.live_from = a.first, pw.live_side = 2;
-            Gradient ew{};
-            ew.cols = a.width, ew.add = accumulate || i > 0;
-            if (l.sums_w) {
-                ew.dst = reinterpret_cast<float*>(ws + l.w32), ew.stride = l.width_ld, ew.vectors = 1, ew.add = i > 0;
+            Product pw = product_of(vocab, width, l.chunk_rows, l.f32, sms);
+            pw.follows = 1, pw.live = a.live, pw.live_from = a.first, pw.live_side = 2, pw.split = 1;
+            Dest to{};
+            to.cols = a.width, to.add = accumulate || i > 0, to.stride = dw_stride, to.vectors = dw_vectors;
+            float* const sums = l.sums_w ? reinterpret_cast<float*>(ws + l.w32) : nullptr;
+            if (l.sums_w && i + 1 < l.chunks) {
+                to.f32 = sums, to.stride = l.width_ld, to.vectors = 1;
             } else if (dw_dt == SS_BF16) {
-                ew.dst16 = static_cast<uint16_t*>(dw), ew.stride = dw_stride, ew.vectors = dw_vectors;
+                to.bf16 = static_cast<uint16_t*>(dw), to.before = sums, to.before_stride = l.width_ld;
             } else {
-                ew.dst = static_cast<float*>(dw), ew.stride = dw_stride, ew.vectors = dw_vectors;
+                to.f32 = static_cast<float*>(dw);
             }
-            if (ew.dst16 == nullptr) pw.chunk = l.f32 ? kGradChunkF32 : kGradChunk;
-            status = launch_product<Gradient, true, true>(p_rows, x_rows, pw, ew, st);
+            // a bf16 result is written once: its rows, at most kMostChunkRows, are one chunk
+            pw.chunk = l.f32 ? kGradChunkF32 : kGradChunk;
+            if (to.bf16 == nullptr) status = launch_product<Gradient<false, false>, true, true>(p_rows, x_rows, pw, Gradient<false, false>{to, a.partial}, st);
+            else if (to.before == nullptr) status = launch_product<Gradient<true, false>, true, true>(p_rows, x_rows, pw, Gradient<true, false>{to, a.partial}, st);
+            else status = launch_product<Gradient<true, true>, true, true>(p_rows, x_rows, pw, Gradient<true, true>{to, a.partial}, st);
             if (status != SS_OK) return status;
+            if (may_split(pw)) {
+                e = launch_next(true, head_join_kernel, dim3(static_cast<unsigned>(sms / 2), kTileFloats / 1024), 256, st, pw, to, static_cast<const float*>(a.partial));
+                if (e != cudaSuccess) return cuda_status_public(e);
+            }
         }
-    }
-    if (l.sums_w) {
-        const int64_t most = static_cast<int64_t>(sms) * 16;
-        e = launch_next(true, head_round_kernel, static_cast<unsigned>(vocab < most ? vocab : most), 256, st, reinterpret_cast<const float*>(ws + l.w32), l.width_ld,
-                        static_cast<uint16_t*>(dw), dw_stride, vocab, a.width);
-        if (e != cudaSuccess) return cuda_status_public(e);
     }
     return cuda_status_public(launch_next(true, head_totals_kernel, 1, 1024, st, a, 0));
 }

@@ -41,51 +41,70 @@ __device__ __forceinline__ void split4(float4 v, uint2* hi, uint2* lo) {
 
 // ---- ends of the products --------------------------------------------------------------------------
 
-// out = c sums (+ b lin), symmetric: a square above the diagonal's tiles is stored a second time, mirrored.
+// A lane has four neighbouring columns of every fourth row of a square: row lane / 8 + 4 i, columns 4 (lane % 8) on.
+__device__ __forceinline__ float4 sums_of(uint32_t buf, int lane, int i) {
+    const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+    return make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+}
+
+// out = c sums (+ b lin), symmetric: a square of a tile above the diagonal is stored a second time, mirrored.
+template <bool LIN>
 struct Symmetric {
     static constexpr bool kWhole = false;
     struct Fetched {
-        uint2 lin[8];
+        uint2 lin[LIN ? 8 : 1];
     };
     uint16_t* out;
-    const uint16_t* lin;  // NULL: none
+    const uint16_t* lin;
     int64_t plane;
     int ld;
     float b, c;
 
-    __device__ __forceinline__ int64_t at(const ProdUnit& u, int row, int col) const { return u.batch * plane + static_cast<int64_t>(row) * ld + col; }
+    struct Tile {
+        uint16_t *to, *mirrored;
+        const uint16_t* from;
+        int rows, cols;  // that exist from this lane's first row on, and from its first column's mirrored row on
+        bool mirror;
 
-    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const {
-        if (lin == nullptr) return;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = row + (lane >> 3) + 4 * i;
-            f.lin[i] = r < m ? *reinterpret_cast<const uint2*>(lin + at(u, r, col + 4 * (lane & 7))) : make_uint2(0, 0);
+        __device__ __forceinline__ Tile(const Symmetric& e, const ProdUnit& u, int m, int row, int col, int lane) {
+            const int64_t r = row + (lane >> 3), c = col + (lane >> 3);
+            const int64_t at = u.batch * e.plane + r * e.ld + col + 4 * (lane & 7);
+            to = e.out + at, from = LIN ? e.lin + at : nullptr;
+            mirrored = e.out + u.batch * e.plane + c * e.ld + row + 4 * (lane & 7);
+            rows = m - static_cast<int>(r), cols = m - static_cast<int>(c);
+            mirror = u.m0 != u.n0;
         }
-    }
-    __device__ __forceinline__ void square(const ProdUnit& u, int m, int row, int col, int lane, uint32_t buf, const Fetched& f, bool) const {
-        const bool mirror = u.m0 != u.n0;
+        __device__ __forceinline__ void fetch(const Symmetric& e, int j, Fetched& f) const {
+            if constexpr (LIN) {
+                const uint16_t* p = from + j;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = (lane >> 3) + 4 * i;
-            const uint4 w = square_get(buf, r, lane & 7);
-            float4 v = make_float4(c * __uint_as_float(w.x), c * __uint_as_float(w.y), c * __uint_as_float(w.z), c * __uint_as_float(w.w));
-            if (lin != nullptr) {
-                const float4 l = float4_of(f.lin[i]);
-                v.x += b * l.x, v.y += b * l.y, v.z += b * l.z, v.w += b * l.w;
+                for (int i = 0; i < 8; ++i, p += 4 * e.ld) f.lin[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
             }
-            if (row + r < m) *reinterpret_cast<uint2*>(out + at(u, row + r, col + 4 * (lane & 7))) = half4(v);
-            if (mirror) square_set(buf, r, lane & 7, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
         }
-        if (!mirror) return;
-        __syncwarp();
+        __device__ __forceinline__ void square(const Symmetric& e, int j, int lane, uint32_t buf, const Fetched& f, bool) const {
+            uint16_t* p = to + j;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int cc = (lane >> 3) + 4 * i, r = 4 * (lane & 7);
-            const float4 v = make_float4(square_word(buf, r, cc), square_word(buf, r + 1, cc), square_word(buf, r + 2, cc), square_word(buf, r + 3, cc));
-            if (col + cc < m) *reinterpret_cast<uint2*>(out + at(u, col + cc, row + r)) = half4(v);
+            for (int i = 0; i < 8; ++i, p += 4 * e.ld) {
+                float4 v = sums_of(buf, lane, i);
+                v = make_float4(e.c * v.x, e.c * v.y, e.c * v.z, e.c * v.w);
+                if constexpr (LIN) {
+                    const float4 l = float4_of(f.lin[i]);
+                    v.x += e.b * l.x, v.y += e.b * l.y, v.z += e.b * l.z, v.w += e.b * l.w;
+                }
+                if (4 * i < rows) *reinterpret_cast<uint2*>(p) = half4(v);
+                if (mirror) square_set(buf, (lane >> 3) + 4 * i, lane & 7, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+            }
+            if (!mirror) return;
+            __syncwarp();
+            p = mirrored + static_cast<int64_t>(j) * e.ld;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, p += 4 * e.ld) {
+                const int c = (lane >> 3) + 4 * i, r = 4 * (lane & 7);
+                const float4 v = make_float4(square_word(buf, r, c), square_word(buf, r + 1, c), square_word(buf, r + 2, c), square_word(buf, r + 3, c));
+                if (j + 4 * i < cols) *reinterpret_cast<uint2*>(p) = half4(v);
+            }
         }
-    }
+    };
 };
 
 // X carried as hi + lo, scaled by a power of two: the next one is a (hi + lo) + sums.
@@ -95,94 +114,122 @@ struct Carried {
     int64_t plane;
     int ld;
     float a;
-
-    struct Fetched {
-        uint2 hi[8], lo[8];
-    };
-    __device__ __forceinline__ int64_t at(const ProdUnit& u, int row, int col) const { return u.batch * plane + static_cast<int64_t>(row) * ld + col; }
-    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = row + (lane >> 3) + 4 * i;
-            const int64_t k = at(u, r, col + 4 * (lane & 7));
-            f.hi[i] = r < m ? *reinterpret_cast<const uint2*>(hi + k) : make_uint2(0, 0);
-            f.lo[i] = r < m ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
-        }
-    }
-    __device__ __forceinline__ float4 next(uint32_t buf, int lane, int i, const Fetched& f) const {
-        const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
-        const float4 h = float4_of(f.hi[i]), l = float4_of(f.lo[i]);
-        return make_float4(a * (h.x + l.x) + __uint_as_float(w.x), a * (h.y + l.y) + __uint_as_float(w.y),
-                           a * (h.z + l.z) + __uint_as_float(w.z), a * (h.w + l.w) + __uint_as_float(w.w));
-    }
 };
+
+__device__ __forceinline__ float4 next_of(float a, float4 sums, uint2 hi, uint2 lo) {
+    const float4 h = float4_of(hi), l = float4_of(lo);
+    return make_float4(a * (h.x + l.x) + sums.x, a * (h.y + l.y) + sums.y, a * (h.z + l.z) + sums.z, a * (h.w + l.w) + sums.w);
+}
 
 struct Next {
     static constexpr bool kWhole = false;
-    using Fetched = Carried::Fetched;
+    struct Fetched {
+        uint2 hi[8], lo[8];
+    };
     Carried x;
     uint16_t* hi_out;
 
-    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const { x.fetch(u, m, row, col, lane, f); }
-    __device__ __forceinline__ void square(const ProdUnit& u, int m, int row, int col, int lane, uint32_t buf, const Fetched& f, bool) const {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = row + (lane >> 3) + 4 * i;
-            uint2 hi, lo;
-            split4(x.next(buf, lane, i, f), &hi, &lo);
-            if (r >= m) continue;
-            const int64_t k = x.at(u, r, col + 4 * (lane & 7));
-            *reinterpret_cast<uint2*>(hi_out + k) = hi;
-            *reinterpret_cast<uint2*>(x.lo + k) = lo;  // nothing but this place of this tile reads it
+    struct Tile {
+        const uint16_t* hi;
+        uint16_t *lo, *hi_out;
+        int rows;
+
+        __device__ __forceinline__ Tile(const Next& e, const ProdUnit& u, int m, int row, int col, int lane) {
+            const int64_t r = row + (lane >> 3), at = u.batch * e.x.plane + r * e.x.ld + col + 4 * (lane & 7);
+            hi = e.x.hi + at, lo = e.x.lo + at, hi_out = e.hi_out + at;
+            rows = m - static_cast<int>(r);
         }
-    }
+        __device__ __forceinline__ void fetch(const Next& e, int j, Fetched& f) const {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
+                f.hi[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(hi + k) : make_uint2(0, 0);
+                f.lo[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
+            }
+        }
+        __device__ __forceinline__ void square(const Next& e, int j, int lane, uint32_t buf, const Fetched& f, bool) const {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
+                uint2 h, l;
+                split4(next_of(e.x.a, sums_of(buf, lane, i), f.hi[i], f.lo[i]), &h, &l);
+                if (4 * i >= rows) continue;
+                *reinterpret_cast<uint2*>(hi_out + k) = h;
+                *reinterpret_cast<uint2*>(lo + k) = l;  // nothing but this place of this tile reads it
+            }
+        }
+    };
 };
 
+enum { kToF32, kToBf16, kToParam };
+
 // The last step's result, to the caller: O, or the parameter moved by it.
+template <int TO>
 struct Result {
     static constexpr bool kWhole = false;
-    using Fetched = Carried::Fetched;
+    struct Fetched {
+        uint2 hi[8], lo[8];
+        float4 p[TO == kToParam ? 8 : 1];
+    };
     Carried x;
     float unscale;  // of the power of two
     int64_t stride;
-    int cols, dt;   // of out
+    int cols;       // of out
     int vectors;    // four neighbouring elements of every matrix start on their size
-    int update;
     float lr, scale, decay;
     Table out, param;
 
-    __device__ __forceinline__ void fetch(const ProdUnit& u, int m, int row, int col, int lane, Fetched& f) const { x.fetch(u, m, row, col, lane, f); }
     __device__ __forceinline__ float moved(float p, float o) const { return p - lr * (scale * o + decay * p); }
-    __device__ __forceinline__ void square(const ProdUnit& u, int m, int row, int col, int lane, uint32_t buf, const Fetched& f, bool) const {
-        void* const to = const_cast<void*>(out.p[u.batch]);
-        const float* const from = static_cast<const float*>(param.p[u.batch]);
-        const int c = col + 4 * (lane & 7);
+
+    struct Tile {
+        const uint16_t *hi, *lo;
+        char* to;
+        const float* from;
+        int rows, cols;  // that exist from this lane's first ones on
+
+        __device__ __forceinline__ Tile(const Result& e, const ProdUnit& u, int m, int row, int col, int lane) {
+            const int64_t r = row + (lane >> 3), c = col + 4 * (lane & 7), at = u.batch * e.x.plane + r * e.x.ld + c;
+            hi = e.x.hi + at, lo = e.x.lo + at;
+            to = static_cast<char*>(const_cast<void*>(e.out.p[u.batch])) + (r * e.stride + c) * (TO == kToBf16 ? 2 : 4);
+            from = TO == kToParam ? static_cast<const float*>(e.param.p[u.batch]) + r * e.stride + c : nullptr;
+            rows = m - static_cast<int>(r), cols = e.cols - static_cast<int>(c);
+        }
+        __device__ __forceinline__ void fetch(const Result& e, int j, Fetched& f) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = row + (lane >> 3) + 4 * i;
-            const float4 n = x.next(buf, lane, i, f);
-            if (r >= m || c >= cols) continue;
-            float4 o = make_float4(n.x * unscale, n.y * unscale, n.z * unscale, n.w * unscale);
-            const int64_t k = r * stride + c;
-            if (vectors && c + 4 <= cols) {
-                if (update) {
-                    const float4 p = *reinterpret_cast<const float4*>(from + k);
-                    o = make_float4(moved(p.x, o.x), moved(p.y, o.y), moved(p.z, o.z), moved(p.w, o.w));
-                }
-                if (dt == SS_F32) *reinterpret_cast<float4*>(static_cast<float*>(to) + k) = o;
-                else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(to) + k) = make_uint2(bf16_pair(o.x, o.y), bf16_pair(o.z, o.w));
-            } else {
-                const float v[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c + j >= cols) break;
-                    const float e = update ? moved(from[k + j], v[j]) : v[j];
-                    if (dt == SS_F32) static_cast<float*>(to)[k + j] = e;
-                    else Elem<uint16_t>::store(static_cast<uint16_t*>(to) + k + j, e);
+            for (int i = 0; i < 8; ++i) {
+                const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
+                f.hi[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(hi + k) : make_uint2(0, 0);
+                f.lo[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
+                if constexpr (TO == kToParam) {
+                    if (e.vectors && 4 * i < rows && j + 4 <= cols) f.p[i] = *reinterpret_cast<const float4*>(from + j + 4 * i * e.stride);
                 }
             }
         }
-    }
+        __device__ __forceinline__ void square(const Result& e, int j, int lane, uint32_t buf, const Fetched& f, bool) const {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 n = next_of(e.x.a, sums_of(buf, lane, i), f.hi[i], f.lo[i]);
+                if (4 * i >= rows || j >= cols) continue;
+                float4 o = make_float4(n.x * e.unscale, n.y * e.unscale, n.z * e.unscale, n.w * e.unscale);
+                char* const p = to + (j + 4 * i * e.stride) * (TO == kToBf16 ? 2 : 4);
+                if (e.vectors && j + 4 <= cols) {
+                    if constexpr (TO == kToParam) o = make_float4(e.moved(f.p[i].x, o.x), e.moved(f.p[i].y, o.y), e.moved(f.p[i].z, o.z), e.moved(f.p[i].w, o.w));
+                    if constexpr (TO == kToBf16) *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(o.x, o.y), bf16_pair(o.z, o.w));
+                    else *reinterpret_cast<float4*>(p) = o;
+                } else {
+                    const float v[4] = {o.x, o.y, o.z, o.w};
+                    const float* const q = from + j + 4 * i * e.stride;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        if (j + d >= cols) break;
+                        if constexpr (TO == kToBf16) Elem<uint16_t>::store(reinterpret_cast<uint16_t*>(p) + d, v[d]);
+                        else if constexpr (TO == kToParam) reinterpret_cast<float*>(p)[d] = e.moved(q[d], v[d]);
+                        else reinterpret_cast<float*>(p)[d] = v[d];
+                    }
+                }
+            }
+        }
+    };
 };
 
 // ---- the start: momentum, norm, first operand ------------------------------------------------------
@@ -339,7 +386,8 @@ int layout_of(int count, int64_t rows, int64_t cols, Layout* l) {
 
 struct Call {
     Start start;
-    Result result;
+    Result<kToF32> result;
+    int to;
     ss_dtype in_dt;
     int count;
     int64_t rows, cols;
@@ -382,29 +430,35 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     map(&q_map, q, l.side, l.side, side_row, side_bytes, false);
     if (status != SS_OK) return status;
 
-    Product ps = product_of(l.side, l.side, big, false), pq = product_of(l.side, l.side, l.side, false);
-    Product px = product_of(c.rows, c.cols, l.side, false);
+    const int sms = device_sm_count(&e);
+    if (e != cudaSuccess) return cuda_status_public(e);
+    Product ps = product_of(l.side, l.side, big, false, sms), pq = product_of(l.side, l.side, l.side, false, sms);
+    Product px = product_of(c.rows, c.cols, l.side, false, sms);
     for (Product* p : {&ps, &pq, &px}) p->batches = c.count, p->bf16 = 0, p->follows = 1, p->m_fast = 1;
     ps.upper = pq.upper = 1;
     for (int k = 0; k < c.steps; ++k) {
         const float *const co = c.coefficients + 3 * k;
         const int from = k & 1;
-        const Symmetric es{s, nullptr, l.side_plane, static_cast<int>(l.side_ld), 0.0f, unscale * unscale};
-        const Symmetric eq{q, s, l.side_plane, static_cast<int>(l.side_ld), co[1], co[2]};
+        const Symmetric<false> es{s, nullptr, l.side_plane, static_cast<int>(l.side_ld), 0.0f, unscale * unscale};
+        const Symmetric<true> eq{q, s, l.side_plane, static_cast<int>(l.side_ld), co[1], co[2]};
         const Carried x{hi[from], lo, l.plane, static_cast<int>(l.ld), co[0]};
-        status = tall ? launch_product<Symmetric, true, true>(x_sum[from], x_sum[from], ps, es, st)
-                      : launch_product<Symmetric, false, false>(x_sum[from], x_sum[from], ps, es, st);
-        if (status == SS_OK) status = launch_product<Symmetric, false, false>(s_map, s_map, pq, eq, st);
+        status = tall ? launch_product<Symmetric<false>, true, true>(x_sum[from], x_sum[from], ps, es, st)
+                      : launch_product<Symmetric<false>, false, false>(x_sum[from], x_sum[from], ps, es, st);
+        if (status == SS_OK) status = launch_product<Symmetric<true>, false, false>(s_map, s_map, pq, eq, st);
         if (status != SS_OK) return status;
         if (k + 1 < c.steps) {
             const Next en{x, hi[from ^ 1]};
             status = tall ? launch_product<Next, false, false>(x_prod[from], q_map, px, en, st)
                           : launch_product<Next, false, true>(q_map, x_prod[from], px, en, st);
         } else {
-            Result& r = c.result;
-            r.x = x, r.unscale = unscale, r.cols = static_cast<int>(c.cols);
-            status = tall ? launch_product<Result, false, false>(x_prod[from], q_map, px, r, st)
-                          : launch_product<Result, false, true>(q_map, x_prod[from], px, r, st);
+            auto last = [&](auto r) {
+                using R = decltype(r);
+                r.x = x, r.unscale = unscale, r.cols = static_cast<int>(c.cols);
+                r.stride = c.result.stride, r.vectors = c.result.vectors, r.lr = c.result.lr, r.scale = c.result.scale, r.decay = c.result.decay;
+                r.out = c.result.out, r.param = c.result.param;
+                return tall ? launch_product<R, false, false>(x_prod[from], q_map, px, r, st) : launch_product<R, false, true>(q_map, x_prod[from], px, r, st);
+            };
+            status = c.to == kToParam ? last(Result<kToParam>{}) : (c.to == kToBf16 ? last(Result<kToBf16>{}) : last(Result<kToF32>{}));
         }
         if (status != SS_OK) return status;
     }
@@ -503,7 +557,7 @@ int ss_orthogonalise(const void* const* in, int64_t in_stride, ss_dtype in_dt, v
     fill(&c.start.in, a, count);
     c.start.in_stride = a.m[0].stride, c.start.vectors = a.vectors;
     fill(&c.result.out, b, count);
-    c.result.stride = b.m[0].stride, c.result.dt = out_dt, c.result.vectors = b.vectors;
+    c.result.stride = b.m[0].stride, c.result.vectors = b.vectors, c.to = out_dt == SS_BF16 ? kToBf16 : kToF32;
     c.in_dt = in_dt, c.count = count, c.rows = rows, c.cols = cols, c.coefficients = coefficients, c.steps = steps;
     return run(c, l, static_cast<uint8_t*>(workspace), static_cast<cudaStream_t>(cuda_stream));
 }
@@ -538,10 +592,11 @@ int ss_orthogonal_update(const void* const* grads, int64_t grad_stride, ss_dtype
     fill(&s.in, g, count), fill(&s.momentum, v, count), fill(&s.momentum_out, vo, count);
     s.in_stride = g.m[0].stride, s.momentum_stride = v.m[0].stride, s.vectors = g.vectors && v.vectors && vo.vectors;
     s.update = 1, s.nesterov = nesterov != 0, s.beta = beta, s.rest = 1.0f - beta;
-    Result& r = c.result;
+    Result<kToF32>& r = c.result;
+    c.to = kToParam;
     fill(&r.param, p, count), fill(&r.out, po, count);
-    r.stride = p.m[0].stride, r.dt = SS_F32, r.vectors = p.vectors && po.vectors;
-    r.update = 1, r.lr = lr, r.scale = scale, r.decay = weight_decay;
+    r.stride = p.m[0].stride, r.vectors = p.vectors && po.vectors;
+    r.lr = lr, r.scale = scale, r.decay = weight_decay;
     c.in_dt = dt, c.count = count, c.rows = rows, c.cols = cols, c.coefficients = coefficients, c.steps = steps;
     return run(c, l, static_cast<uint8_t*>(workspace), static_cast<cudaStream_t>(cuda_stream));
 }

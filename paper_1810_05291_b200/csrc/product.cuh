@@ -35,6 +35,8 @@ struct Product {
     int passes;       // pairs of planes: (plane_a[i], plane_b[i])
     int8_t plane_a[kMostPasses], plane_b[kMostPasses];
     int chunk;        // stages that are summed in tensor memory before they are brought out
+    int pairs;        // of blocks
+    int split;        // whether the contraction of tiles that do not fill a round of pairs may be cut into parts
     int m_fast;       // the order of tiles: neighbours share columns of C, or rows
     int upper;        // m == n: only tiles on the diagonal and above
     int bf16;         // operands: bf16 or fp16
@@ -44,8 +46,9 @@ struct Product {
     int live_side;    // 1: they are m; 2: they are k (at the call's start one stage at least, whose rows are zeros)
 };
 
-inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms) {
+inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms, int sms) {
     Product p{};
+    p.pairs = sms / 2;
     p.m = static_cast<int>(m), p.n = static_cast<int>(n), p.k = static_cast<int>(k);
     p.batches = 1, p.passes = 1, p.chunk = 1 << 30, p.bf16 = 1;
     if (terms) {
@@ -56,10 +59,14 @@ inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms) {
     return p;
 }
 
+// The pairs of blocks take whole tiles as long as every pair gets one; the contraction of the tiles that are left over (all, if
+// there are fewer than pairs) is cut into parts, so that they too keep most pairs busy. Parts are joined afterwards, in their order.
 struct Schedule {
-    int m, tiles_m, tiles_n, per_batch, units;
-    int pass_stages, stages;  // of one pass; of all
+    int m, tiles_m, tiles_n, per_batch;
+    int pass_stages, stages;          // of one pass; of all
+    int whole, parts, part_stages, units;
 };
+constexpr int kLeastPart = 8;         // stages: fewer do not pay for their start and for joining them
 
 __device__ __forceinline__ Schedule schedule_of(const Product& p) {
     Schedule s;
@@ -75,18 +82,38 @@ __device__ __forceinline__ Schedule schedule_of(const Product& p) {
     s.tiles_m = (m + kProdTile - 1) / kProdTile;
     s.tiles_n = (p.n + kProdTile - 1) / kProdTile;
     s.per_batch = p.upper ? s.tiles_m * (s.tiles_m + 1) / 2 : s.tiles_m * s.tiles_n;
-    s.units = any ? s.per_batch * p.batches : 0;
     s.pass_stages = (k + kProdK - 1) / kProdK;
     s.stages = s.pass_stages * p.passes;
+    const int tiles = any ? s.per_batch * p.batches : 0, others = tiles % p.pairs;
+    s.whole = tiles, s.parts = 1, s.part_stages = s.stages;
+    if (p.split && others > 0) {
+        const int parts = min(p.pairs / others, s.stages / kLeastPart);
+        if (parts > 1) {
+            s.whole = tiles - others;
+            s.part_stages = (s.stages + parts - 1) / parts;
+            s.parts = (s.stages + s.part_stages - 1) / s.part_stages;
+        }
+    }
+    s.units = s.whole + (tiles - s.whole) * s.parts;
     return s;
 }
 
 struct ProdUnit {
     int batch, m0, n0;
+    int part;           // of all parts, or -1: a whole tile
+    int first, stages;
 };
 
 __device__ __forceinline__ ProdUnit prod_unit(const Product& p, const Schedule& s, int u) {
     ProdUnit r;
+    r.part = -1, r.first = 0, r.stages = s.stages;
+    if (u >= s.whole) {
+        r.part = u - s.whole;
+        const int other = r.part / s.parts;
+        r.first = (r.part - other * s.parts) * s.part_stages;
+        r.stages = min(s.part_stages, s.stages - r.first);
+        u = s.whole + other;
+    }
     r.batch = u / s.per_batch;
     int t = u - r.batch * s.per_batch, i, j;
     if (p.upper) {
@@ -135,8 +162,9 @@ __device__ __forceinline__ float square_word(uint32_t buf, int row, int col) {
 constexpr uint32_t kNanBits = 0x7FC00000u;
 
 // EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
-// registers, and gets them at once: EPI(args).whole(unit, m, row, col, lane, buf, sums). Otherwise it gets each chunk in
-// squares of 32 x 32 in the warp's shared memory: fetch(...) before they have come, square(..., first chunk?).
+// registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
+// columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
+// square(column, ..., first chunk?).
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
 template <class EPI, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kProdThreads, 1)
@@ -146,7 +174,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
     __shared__ ProdShared sh;
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int pair = blockIdx.x >> 1, pairs = p.pairs;
     volatile int* abort = &sh.abort;
     uint32_t rank;  // in the pair; the first block issues the matrix instructions and waits for both blocks' operands
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -189,7 +217,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                 float sums[kProdHalf];
 #pragma unroll
                 for (int i = 0; i < kProdHalf; ++i) sums[i] = 0.0f;
-                for (int left = sc.stages; left > 0; left -= p.chunk, ++chunk) {
+                for (int left = u.stages; left > 0; left -= p.chunk, ++chunk) {
                     if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                     tc_fence_after();
                     const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
@@ -212,15 +240,17 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                 epi.whole(u, sc.m, row, col, lane, buf, sums);
             } else {
                 bool first = true;
-                for (int left = sc.stages; left > 0; left -= p.chunk, ++chunk) {
+                const bool any = row < sc.m && col < p.n;
+                typename EPI::Tile tile(epi, u, sc.m, row, col, lane);
+                typename EPI::Fetched f;
+                for (int left = u.stages; left > 0; left -= p.chunk, ++chunk) {
+                    if (any) tile.fetch(epi, 0, f);
                     if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                     tc_fence_after();
                     const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
 #pragma unroll 1
-                    for (int j = 0; j < kProdHalf; j += 32) {
-                        if (row >= sc.m || col + j >= p.n) continue;
-                        typename EPI::Fetched f;
-                        epi.fetch(u, sc.m, row, col + j, lane, f);
+                    for (int j = 0; any && j < kProdHalf && col + j < p.n; j += 32) {
+                        if (j > 0) tile.fetch(epi, j, f);
                         uint32_t r[32];
                         tmem_load32(src + j, r);
                         tmem_load_wait();
@@ -230,7 +260,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                         }
                         square_put(buf, lane, r);
                         __syncwarp();
-                        epi.square(u, sc.m, row, col + j, lane, buf, f, first);
+                        tile.square(epi, j, lane, buf, f, first);
                         __syncwarp();
                     }
                     tc_fence_before();
@@ -251,10 +281,10 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         for (int unit = pair; unit < sc.units; unit += pairs) {
             const ProdUnit u = prod_unit(p, sc, unit);
             const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + rank * kProdHalf;
-            int pass = 0, k0 = 0;
+            int pass = u.first / sc.pass_stages, k0 = (u.first - pass * sc.pass_stages) * kProdK;
             const int end = sc.pass_stages * kProdK;
 #pragma unroll 1
-            for (int s = 0; s < sc.stages; ++s) {
+            for (int s = 0; s < u.stages; ++s) {
                 mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
                 const uint32_t bar = full + slot * 8, dst = stages + slot * kProdStageBytes;
                 const int za = p.passes > 1 ? p.plane_a[pass] : u.batch, zb = p.passes > 1 ? p.plane_b[pass] : u.batch;
@@ -296,7 +326,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         const bool leader = elect_one();
         uint32_t slot = 0, parity = 0, chunk = 0;
         for (int unit = pair; unit < sc.units; unit += pairs) {
-            for (int left = sc.stages; left > 0; left -= p.chunk, ++chunk) {
+            for (int left = prod_unit(p, sc, unit).stages; left > 0; left -= p.chunk, ++chunk) {
                 const int n = min(left, p.chunk);
                 const uint32_t d = tmem + (chunk & 1) * kProdTile;
                 // the half of the tensor memory is free once the chunk before the last has been brought out
@@ -350,15 +380,13 @@ inline int map_operand(CUtensorMap* map, const void* p, bool bf16, int64_t fast,
 template <class EPI, bool A_MN, bool B_MN>
 int launch_product(const CUtensorMap& a, const CUtensorMap& b, const Product& p, const EPI& epi, cudaStream_t st) {
     cudaError_t e = cudaSuccess;
-    const int sms = device_sm_count(&e);
-    if (e != cudaSuccess) return cuda_status_public(e);
     const auto kernel = product_kernel<EPI, A_MN, B_MN>;
     struct Key {};
     e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kProdSmem));
     if (e != cudaSuccess) return cuda_status_public(e);
     const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile;
     int64_t units = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
-    if (units > sms / 2) units = sms / 2;
+    if (units > p.pairs || p.split) units = p.pairs;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(2 * units));
     cfg.blockDim = dim3(kProdThreads);
