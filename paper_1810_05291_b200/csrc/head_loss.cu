@@ -205,7 +205,7 @@ __device__ __forceinline__ uint4 half8(const float* v) {
 
 // ---- the end of the logits' product
 struct Logits {
-    static constexpr bool kWhole = true;
+    static constexpr bool kWhole = true, kSmall = false;
     const int* target;  // of the chunk's rows
     float* target_logit;
     float2* parts;
@@ -428,7 +428,7 @@ struct Dest {
 // OUT16: to.bf16, else to.f32. BEFORE: with to.before.
 template <bool OUT16, bool BEFORE>
 struct Gradient {
-    static constexpr bool kWhole = false;
+    static constexpr bool kWhole = false, kSmall = false;
     struct Fetched {
         float4 before[BEFORE ? 8 : 1];
     };

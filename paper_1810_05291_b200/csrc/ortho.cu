@@ -50,7 +50,7 @@ __device__ __forceinline__ float4 sums_of(uint32_t buf, int lane, int i) {
 // out = c sums (+ b lin), symmetric: a square of a tile above the diagonal is stored a second time, mirrored.
 template <bool LIN>
 struct Symmetric {
-    static constexpr bool kWhole = false;
+    static constexpr bool kWhole = false, kSmall = true;
     struct Fetched {
         uint2 lin[LIN ? 8 : 1];
     };
@@ -122,7 +122,7 @@ __device__ __forceinline__ float4 next_of(float a, float4 sums, uint2 hi, uint2 
 }
 
 struct Next {
-    static constexpr bool kWhole = false;
+    static constexpr bool kWhole = false, kSmall = true;
     struct Fetched {
         uint2 hi[8], lo[8];
     };
@@ -166,7 +166,7 @@ enum { kToF32, kToBf16, kToParam };
 // The last step's result, to the caller: O, or the parameter moved by it.
 template <int TO>
 struct Result {
-    static constexpr bool kWhole = false;
+    static constexpr bool kWhole = false, kSmall = true;
     struct Fetched {
         uint2 hi[8], lo[8];
         float4 p[TO == kToParam ? 8 : 1];
@@ -436,6 +436,7 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     Product px = product_of(c.rows, c.cols, l.side, false, sms);
     for (Product* p : {&ps, &pq, &px}) p->batches = c.count, p->bf16 = 0, p->follows = 1, p->m_fast = 1;
     ps.upper = pq.upper = 1;
+    for (Product* p : {&ps, &pq, &px}) p->small = small_blocks(*p, sms);
     for (int k = 0; k < c.steps; ++k) {
         const float *const co = c.coefficients + 3 * k;
         const int from = k & 1;

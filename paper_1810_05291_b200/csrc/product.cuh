@@ -39,6 +39,7 @@ struct Product {
     int split;        // whether the contraction of tiles that do not fill a round of pairs may be cut into parts
     int m_fast;       // the order of tiles: neighbours share columns of C, or rows
     int upper;        // m == n: only tiles on the diagonal and above
+    int small;        // blocks that share a 128 x 128 tile (1, 2, 4, 8), or 0: pairs on 256 x 256 tiles
     int bf16;         // operands: bf16 or fp16
     int follows;      // another kernel of the call goes before
     const int* live;  // rows that there are (all of the call's), or NULL
@@ -164,7 +165,7 @@ constexpr uint32_t kNanBits = 0x7FC00000u;
 // EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
 // registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
-// square(column, ..., first chunk?).
+// square(column, ..., first chunk?). EPI::kSmall: it also ends the small products below.
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
 template <class EPI, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kProdThreads, 1)
@@ -362,6 +363,184 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
     if (warp == 0) tmem_free_pair(tmem, 512);
 }
 
+// ---- small products --------------------------------------------------------------------------------
+// Products that are too small to fill the machine with pairs: one 128 x 128 tile to a cluster of 1, 2, 4 or 8 blocks that
+// share the contraction. Each forms its part of the sums, keeps it in shared memory, and adds up its share of
+// the tile's squares from all of them, in the order of their ranks, before it brings it out. A block needs little enough
+// that two fit on an SM: those of the kernel that follows are set up while this one runs.
+constexpr int kSmallTile = 128, kSmallStages = 3, kSmallOut = 128, kSmallThreads = kSmallOut + 64;  // warps 0-3 bring out, 4 copies, 5 issues
+constexpr size_t kSmallSmem = 1024 + kSmallStages * kProdStageBytes;
+static_assert(kSmallTile * kSmallTile * 4 <= kSmallStages * kProdStageBytes, "the sums take the place of the operands");
+
+struct SmallShared {
+    uint64_t full[kSmallStages], empty[kSmallStages], summed;
+    uint32_t tmem;
+    int abort;
+};
+
+template <class EPI, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kSmallThreads, 2)
+small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ Product p,
+                     const __grid_constant__ EPI epi) {
+    extern __shared__ uint8_t dynamic[];
+    __shared__ SmallShared sh;
+    const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int blocks = p.small, rank = blockIdx.x % blocks;
+
+    next_may_begin();
+    ProdUnit u;
+    {
+        const int tiles_m = (p.m + kSmallTile - 1) / kSmallTile, tiles_n = (p.n + kSmallTile - 1) / kSmallTile;
+        const int per_batch = p.upper ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n, unit = blockIdx.x / blocks;
+        u.part = -1, u.batch = unit / per_batch;
+        int t = unit - u.batch * per_batch, i, j;
+        if (p.upper) {
+            for (i = 0; t >= tiles_m - i; ++i) t -= tiles_m - i;
+            j = i + t;
+        } else {
+            j = t / tiles_m, i = t - j * tiles_m;
+        }
+        u.m0 = i * kSmallTile, u.n0 = j * kSmallTile;
+        const int all = (p.k + kProdK - 1) / kProdK;
+        u.first = all * rank / blocks, u.stages = all * (rank + 1) / blocks - u.first;
+    }
+    if (tid == 0) {
+        for (int s = 0; s < kSmallStages; ++s) {
+            mbar_init(smem_addr(&sh.full[s]), 1);
+            mbar_init(smem_addr(&sh.empty[s]), 1);
+        }
+        mbar_init(smem_addr(&sh.summed), 1);
+        sh.abort = 0;
+        mbar_init_visible();
+    }
+    if (warp == 0) tmem_alloc(smem_addr(&sh.tmem), kSmallTile);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (p.follows) after_previous();
+    const uint32_t tmem = sh.tmem;
+
+    if (warp < kSmallOut / 32) {
+        const int row = u.m0 + warp * 32;
+        const bool any = row < p.m;
+        typename EPI::Tile tile(epi, u, p.m, row, u.n0, lane);
+        typename EPI::Fetched f;
+        auto mine = [&](int j) { return ((4 * j + warp) * blocks >> 4) == rank && any && u.n0 + 32 * j < p.n; };
+        auto square = [&](int j) { return stages + (4 * warp + j) * kProdSquare; };
+        int fetched = -1;
+#pragma unroll 1
+        for (int j = 0; j < 4 && fetched < 0; ++j)
+            if (mine(j)) fetched = j;
+        if (fetched >= 0) tile.fetch(epi, 32 * fetched, f);
+        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed), 0, &sh.abort));
+        tc_fence_after();
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            if (blocks == 1 && !mine(j)) continue;
+            uint32_t r[32];
+            tmem_load32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + 32 * j, r);
+            tmem_load_wait();
+            if (!ok) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) r[i] = kNanBits;
+            }
+            square_put(square(j), lane, r);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (blocks > 1) cluster_sync();
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            if (!mine(j)) continue;
+            if (j != fetched) tile.fetch(epi, 32 * j, f);
+            if (blocks > 1) {
+#pragma unroll 2
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t at = square_at(square(j), (lane >> 3) + 4 * i, lane & 7);
+                    float4 v = cluster_load4(cluster_addr(at, 0));
+                    for (int q = 1; q < blocks; ++q) {
+                        const float4 x = cluster_load4(cluster_addr(at, q));
+                        v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+                    }
+                    __syncwarp();
+                    square_set(square(j), (lane >> 3) + 4 * i, lane & 7, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+                }
+                __syncwarp();
+            }
+            tile.square(epi, 32 * j, lane, square(j), f, true);
+            __syncwarp();
+        }
+    } else {
+        if (warp == kSmallOut / 32) {
+            // ---- copies
+            const bool leader = elect_one();
+            int slot = 0, k0 = u.first * kProdK;
+            uint32_t parity = 1;
+#pragma unroll 1
+            for (int s = 0; s < u.stages; ++s, k0 += kProdK) {
+                mbar_wait_uniform(smem_addr(&sh.empty[0]) + slot * 8, parity, &sh.abort);
+                const uint32_t bar = smem_addr(&sh.full[0]) + slot * 8, dst = stages + slot * kProdStageBytes;
+                if (leader) {
+                    mbar_expect(bar, kProdStageBytes);
+                    if constexpr (A_MN) {
+                        tma_load_3d(dst, &a_map, bar, u.m0, k0, u.batch);
+                        tma_load_3d(dst + kProdPanel, &a_map, bar, u.m0 + 64, k0, u.batch);
+                    } else {
+                        tma_load_3d(dst, &a_map, bar, k0, u.m0, u.batch);
+                    }
+                    if constexpr (B_MN) {
+                        tma_load_3d(dst + kProdOperand, &b_map, bar, u.n0, k0, u.batch);
+                        tma_load_3d(dst + kProdOperand + kProdPanel, &b_map, bar, u.n0 + 64, k0, u.batch);
+                    } else {
+                        tma_load_3d(dst + kProdOperand, &b_map, bar, k0, u.n0, u.batch);
+                    }
+                }
+                __syncwarp();
+                if (++slot == kSmallStages) slot = 0, parity ^= 1;
+            }
+            // A copy may still be under way only if a wait ran out: it has to arrive before the block ends.
+            if (*static_cast<volatile int*>(&sh.abort) != 0) {
+                int own = 0;
+                for (int i = u.stages > kSmallStages ? u.stages - kSmallStages : 0; i < u.stages; ++i)
+                    mbar_wait(smem_addr(&sh.full[i % kSmallStages]), (i / kSmallStages) & 1, &own);
+            }
+        } else {
+            // ---- matrix unit
+            const uint32_t idesc = tc_idesc(kSmallTile, kSmallTile, p.bf16 != 0, A_MN, B_MN);
+            constexpr uint32_t kStep = kProdStageBytes >> 4, kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
+            const uint64_t desc_a = A_MN ? tc_desc_rows(stages, kProdPanel) : tc_desc_cols(stages);
+            const uint64_t desc_b = B_MN ? tc_desc_rows(stages + kProdOperand, kProdPanel) : tc_desc_cols(stages + kProdOperand);
+            const bool leader = elect_one();
+            uint32_t slot = 0, parity = 0;
+#pragma unroll 1
+            for (int s = 0; s < u.stages; ++s) {
+                mbar_wait_uniform(smem_addr(&sh.full[0]) + slot * 8, parity, &sh.abort);
+                tc_fence_after();
+                const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
+                if (leader) {
+#pragma unroll
+                    for (int k = 0; k < kProdK / 16; ++k) tc_mma_f16(tmem, da + k * kStepA, db + k * kStepB, idesc, s != 0 || k != 0);
+                    tc_commit(smem_addr(&sh.empty[0]) + slot * 8);
+                }
+                __syncwarp();
+                if (++slot == kSmallStages) slot = 0, parity ^= 1;
+            }
+            // nothing may still be running when its results are read, the operands' place is taken and the tensor memory given back
+            if (leader) tc_commit(smem_addr(&sh.summed));
+            int own = 0;
+            mbar_wait(smem_addr(&sh.summed), 0, &own);
+        }
+        __syncwarp();
+        if (blocks > 1) cluster_sync();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (blocks > 1) cluster_sync();  // the others may still be reading this block's sums
+    tc_fence_after();
+    if (warp == 0) tmem_free(tmem, kSmallTile);
+}
+
 // ---- host side -------------------------------------------------------------------------------------
 
 // An operand's map: `fast` elements of unit stride, `slow` rows `row_bytes` apart, `planes` of them. mn: the contraction index is the slow one.
@@ -377,21 +556,29 @@ inline int map_operand(CUtensorMap* map, const void* p, bool bf16, int64_t fast,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? SS_OK : SS_ERR_UNSUPPORTED;
 }
 
+inline int64_t small_tiles(const Product& p) {
+    const int64_t tm = (p.m + kSmallTile - 1) / kSmallTile, tn = (p.n + kSmallTile - 1) / kSmallTile;
+    return (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
+}
+
+// How many blocks share a 128 x 128 tile, or 0 for pairs on 256 x 256 tiles: the least of an estimate in cycles. A pair takes 700
+// for a stage, a small block 600 (it copies as much for half the products), 900 with another on its SM; with what a tile costs besides.
+inline int small_blocks(const Product& p, int sms) {
+    const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile, stages = (p.k + kProdK - 1) / kProdK;
+    const int64_t tiles = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches, small = small_tiles(p);
+    int64_t best = (tiles + p.pairs - 1) / p.pairs * stages * 700 + (tiles > p.pairs ? 9000 : 8000);
+    int blocks = 0;
+    for (int c = 1; c <= 8 && c <= stages; c *= 2) {
+        const int64_t all = small * c, rounds = (all + 2 * sms - 1) / (2 * sms);
+        const int64_t t = rounds * ((stages + c - 1) / c * (all <= sms ? 600 : 900) + 5000) + (c > 1 ? 1000 : 0);
+        if (t < best) best = t, blocks = c;
+    }
+    return blocks;
+}
+
 template <class EPI, bool A_MN, bool B_MN>
 int launch_product(const CUtensorMap& a, const CUtensorMap& b, const Product& p, const EPI& epi, cudaStream_t st) {
-    cudaError_t e = cudaSuccess;
-    const auto kernel = product_kernel<EPI, A_MN, B_MN>;
-    struct Key {};
-    e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kProdSmem));
-    if (e != cudaSuccess) return cuda_status_public(e);
-    const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile;
-    int64_t units = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
-    if (units > p.pairs || p.split) units = p.pairs;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(2 * units));
-    cfg.blockDim = dim3(kProdThreads);
-    cfg.dynamicSmemBytes = kProdSmem;
-    cfg.stream = st;
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
@@ -399,6 +586,31 @@ int launch_product(const CUtensorMap& a, const CUtensorMap& b, const Product& p,
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = p.follows ? 2 : 1;
+    cfg.stream = st;
+    cudaError_t e = cudaSuccess;
+    if constexpr (EPI::kSmall) {
+        if (p.small > 0) {
+            const auto kernel = small_product_kernel<EPI, A_MN, B_MN>;
+            struct Key {};
+            e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kSmallSmem));
+            if (e != cudaSuccess) return cuda_status_public(e);
+            cfg.gridDim = dim3(static_cast<unsigned>(small_tiles(p) * p.small));
+            cfg.blockDim = dim3(kSmallThreads);
+            cfg.dynamicSmemBytes = kSmallSmem;
+            at[0].val.clusterDim.x = p.small;
+            return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, a, b, p, epi));
+        }
+    }
+    const auto kernel = product_kernel<EPI, A_MN, B_MN>;
+    struct Key {};
+    e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kProdSmem));
+    if (e != cudaSuccess) return cuda_status_public(e);
+    const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile;
+    int64_t units = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
+    if (units > p.pairs || p.split) units = p.pairs;
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * units));
+    cfg.blockDim = dim3(kProdThreads);
+    cfg.dynamicSmemBytes = kProdSmem;
     return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, a, b, p, epi));
 }
 
