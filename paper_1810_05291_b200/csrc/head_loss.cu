@@ -464,13 +464,12 @@ struct Gradient {
                     f.before[i] = part < 0 && 4 * i < rows && j < cols ? *reinterpret_cast<const float4*>(before + j + 4 * i * e.to.before_stride) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
         }
-        __device__ __forceinline__ void square(const Gradient& e, int j, int lane, uint32_t buf, const Fetched& f, bool first) const {
+        __device__ __forceinline__ void square(const Gradient& e, int j, int, uint32_t, float4 (&sums)[8], const Fetched& f, bool first) const {
             const bool adds = add || !first;
             char* q = p + j * (OUT16 && part < 0 ? 2 : 4);
 #pragma unroll
             for (int i = 0; i < 8; ++i, q += step) {
-                const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
-                float4 v = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+                float4 v = sums[i];
                 if (4 * i >= rows || j >= cols) continue;
                 if (part >= 0 || (e.to.vectors && j + 4 <= cols)) {
                     if constexpr (BEFORE) v.x += f.before[i].x, v.y += f.before[i].y, v.z += f.before[i].z, v.w += f.before[i].w;

@@ -41,16 +41,11 @@ __device__ __forceinline__ void split4(float4 v, uint2* hi, uint2* lo) {
 
 // ---- ends of the products --------------------------------------------------------------------------
 
-// A lane has four neighbouring columns of every fourth row of a square: row lane / 8 + 4 i, columns 4 (lane % 8) on.
-__device__ __forceinline__ float4 sums_of(uint32_t buf, int lane, int i) {
-    const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
-    return make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
-}
-
 // out = c sums (+ b lin), symmetric: a square of a tile above the diagonal is stored a second time, mirrored.
 template <bool LIN>
 struct Symmetric {
     static constexpr bool kWhole = false, kSmall = true;
+    static constexpr int kSmallBlocks = 2;
     struct Fetched {
         uint2 lin[LIN ? 8 : 1];
     };
@@ -81,12 +76,11 @@ struct Symmetric {
                 for (int i = 0; i < 8; ++i, p += 4 * e.ld) f.lin[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
             }
         }
-        __device__ __forceinline__ void square(const Symmetric& e, int j, int lane, uint32_t buf, const Fetched& f, bool) const {
+        __device__ __forceinline__ void square(const Symmetric& e, int j, int lane, uint32_t buf, float4 (&sums)[8], const Fetched& f, bool) const {
             uint16_t* p = to + j;
 #pragma unroll
             for (int i = 0; i < 8; ++i, p += 4 * e.ld) {
-                float4 v = sums_of(buf, lane, i);
-                v = make_float4(e.c * v.x, e.c * v.y, e.c * v.z, e.c * v.w);
+                float4 v = make_float4(e.c * sums[i].x, e.c * sums[i].y, e.c * sums[i].z, e.c * sums[i].w);
                 if constexpr (LIN) {
                     const float4 l = float4_of(f.lin[i]);
                     v.x += e.b * l.x, v.y += e.b * l.y, v.z += e.b * l.z, v.w += e.b * l.w;
@@ -123,6 +117,7 @@ __device__ __forceinline__ float4 next_of(float a, float4 sums, uint2 hi, uint2 
 
 struct Next {
     static constexpr bool kWhole = false, kSmall = true;
+    static constexpr int kSmallBlocks = 2;
     struct Fetched {
         uint2 hi[8], lo[8];
     };
@@ -147,12 +142,12 @@ struct Next {
                 f.lo[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
             }
         }
-        __device__ __forceinline__ void square(const Next& e, int j, int lane, uint32_t buf, const Fetched& f, bool) const {
+        __device__ __forceinline__ void square(const Next& e, int j, int lane, uint32_t buf, float4 (&sums)[8], const Fetched& f, bool) const {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
                 uint2 h, l;
-                split4(next_of(e.x.a, sums_of(buf, lane, i), f.hi[i], f.lo[i]), &h, &l);
+                split4(next_of(e.x.a, sums[i], f.hi[i], f.lo[i]), &h, &l);
                 if (4 * i >= rows) continue;
                 *reinterpret_cast<uint2*>(hi_out + k) = h;
                 *reinterpret_cast<uint2*>(lo + k) = l;  // nothing but this place of this tile reads it
@@ -167,6 +162,7 @@ enum { kToF32, kToBf16, kToParam };
 template <int TO>
 struct Result {
     static constexpr bool kWhole = false, kSmall = true;
+    static constexpr int kSmallBlocks = TO == kToParam ? 1 : 2;
     struct Fetched {
         uint2 hi[8], lo[8];
         float4 p[TO == kToParam ? 8 : 1];
@@ -175,7 +171,7 @@ struct Result {
     float unscale;  // of the power of two
     int64_t stride;
     int cols;       // of out
-    int vectors;    // four neighbouring elements of every matrix start on their size
+    int vectors;    // every row of every matrix starts on 16 bytes
     float lr, scale, decay;
     Table out, param;
 
@@ -205,10 +201,10 @@ struct Result {
                 }
             }
         }
-        __device__ __forceinline__ void square(const Result& e, int j, int lane, uint32_t buf, const Fetched& f, bool) const {
+        __device__ __forceinline__ void square(const Result& e, int j, int lane, uint32_t buf, float4 (&sums)[8], const Fetched& f, bool) const {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float4 n = next_of(e.x.a, sums_of(buf, lane, i), f.hi[i], f.lo[i]);
+                const float4 n = next_of(e.x.a, sums[i], f.hi[i], f.lo[i]);
                 if (4 * i >= rows || j >= cols) continue;
                 float4 o = make_float4(n.x * e.unscale, n.y * e.unscale, n.z * e.unscale, n.w * e.unscale);
                 char* const p = to + (j + 4 * i * e.stride) * (TO == kToBf16 ? 2 : 4);
@@ -237,31 +233,43 @@ struct Result {
 struct Start {
     Table in, momentum, momentum_out;  // momentum: unused without update
     int64_t in_stride, momentum_stride, plane, rows;
-    int cols, ld, update, nesterov, vectors, blocks;
+    int cols, ld, update, nesterov, vectors, blocks, row_threads;
     float beta, rest;  // rest = 1 - beta
     double scale;      // the power of two
     double* partial;   // [count][blocks]
     uint16_t *hi, *lo;
 };
 
+// Eight neighbouring columns; those that do not exist are 0.
+struct Eight {
+    float v[8];
+};
+
 template <typename T>
-__device__ __forceinline__ float4 load_four(const T* p, int n, bool vectors) {
-    if (vectors && n >= 4) {
+__device__ __forceinline__ Eight load_eight(const T* p, int n, bool vectors) {
+    Eight e;
+    if (vectors && n >= 8) {
         if constexpr (sizeof(T) == 4) {
-            return *reinterpret_cast<const float4*>(p);
+            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+            e = Eight{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
         } else {
-            const uint2 r = *reinterpret_cast<const uint2*>(p);
-            return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xFFFF0000u));
-        }
-    }
-    float v[4];
+            const uint4 r = *reinterpret_cast<const uint4*>(p);
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = j < n ? Elem<T>::load(p + j) : 0.0f;
-    return make_float4(v[0], v[1], v[2], v[3]);
+            for (int j = 0; j < 4; ++j) e.v[2 * j] = __uint_as_float(w[j] << 16), e.v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e.v[j] = j < n ? Elem<T>::load(p + j) : 0.0f;
+    }
+    return e;
 }
 
-__device__ __forceinline__ float4 mix(float4 g, float4 v, float rest, float beta) {
-    return make_float4(rest * g.x + beta * v.x, rest * g.y + beta * v.y, rest * g.z + beta * v.z, rest * g.w + beta * v.w);
+__device__ __forceinline__ Eight mix(const Eight& g, const Eight& v, float rest, float beta) {
+    Eight u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u.v[j] = rest * g.v[j] + beta * v.v[j];
+    return u;
 }
 
 // Sum over the block, the same in every thread; the order is fixed.
@@ -269,6 +277,7 @@ __device__ __forceinline__ double block_sum(double s) {
     __shared__ double part[8];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    __syncthreads();
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
     __syncthreads();
     s = part[0];
@@ -277,44 +286,59 @@ __device__ __forceinline__ double block_sum(double s) {
     return s;
 }
 
-// Four columns of a row at a time, over all of the matrix.
+// Eight columns of a row at a time, over all of the matrix. A row is taken by row_threads (a power of two) neighbouring threads: no
+// divisions. (Four columns at a running index, divided for its row, and everything in fp64: 150 instructions for four elements, and 24
+// + 25 us for 4096 x 4096 bf16.)
 template <typename F>
-__device__ __forceinline__ void over_fours(const Start& a, F f) {
-    const uint32_t fours = (a.cols + 3) / 4;
-    const int64_t total = a.rows * fours;
-    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(a.blocks) * 256) {
-        const int64_t r = total <= 0xFFFFFFFFll ? static_cast<int64_t>(static_cast<uint32_t>(i) / fours) : i / fours;
-        const int c = static_cast<int>(i - r * fours) * 4;
-        f(r, c, min(4, a.cols - c));
-    }
+__device__ __forceinline__ void over_eights(const Start& a, F f) {
+    const int tc = threadIdx.x & (a.row_threads - 1), tr = threadIdx.x / a.row_threads, rows = 256 / a.row_threads;
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * rows + tr; r < a.rows; r += static_cast<int64_t>(a.blocks) * rows)
+        for (int c = tc * 8; c < a.cols; c += a.row_threads * 8) f(r, c, a.cols - c);
 }
 
-// The momentum's update, and partial sums of u's squares, in fp64: the square of a large gradient has no place in fp32, and a
-// fp64 product for each element costs nothing next to its bytes.
+// The momentum's update, and partial sums of u's squares. A thread's squares are summed in fp32, threads in fp64. A block whose
+// squares leave fp32's range, or come near its lower end, forms them in fp64 again.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__ Start a) {
     next_may_begin();
     const T* const in = static_cast<const T*>(a.in.p[blockIdx.y]);
     const float* const mom = static_cast<const float*>(a.momentum.p[blockIdx.y]);
     float* const mom_out = static_cast<float*>(const_cast<void*>(a.momentum_out.p[blockIdx.y]));
-    double sum = 0.0;
-    over_fours(a, [&](int64_t r, int c, int n) {
-        float4 u = load_four(in + r * a.in_stride + c, n, a.vectors);
+    float squares = 0.0f;
+    over_eights(a, [&](int64_t r, int c, int n) {
+        Eight u = load_eight(in + r * a.in_stride + c, n, a.vectors);
         if (a.update) {
             const int64_t k = r * a.momentum_stride + c;
-            const float4 g = u, v = mix(g, load_four(mom + k, n, a.vectors), a.rest, a.beta);
-            if (a.vectors && n >= 4) {
-                *reinterpret_cast<float4*>(mom_out + k) = v;
+            const Eight g = u, v = mix(g, load_eight(mom + k, n, a.vectors), a.rest, a.beta);
+            if (a.vectors && n >= 8) {
+                reinterpret_cast<float4*>(mom_out + k)[0] = make_float4(v.v[0], v.v[1], v.v[2], v.v[3]);
+                reinterpret_cast<float4*>(mom_out + k)[1] = make_float4(v.v[4], v.v[5], v.v[6], v.v[7]);
             } else {
-                const float e[4] = {v.x, v.y, v.z, v.w};
-                for (int j = 0; j < n; ++j) mom_out[k + j] = e[j];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < n) mom_out[k + j] = v.v[j];
             }
             u = a.nesterov ? mix(g, v, a.rest, a.beta) : v;
         }
-        const double x = u.x, y = u.y, z = u.z, w = u.w;
-        sum += x * x + y * y + (n == 4 ? z * z + w * w : (n == 3 ? z * z : 0.0));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) squares += u.v[j] * u.v[j];
     });
-    sum = block_sum(sum);
+    double sum = block_sum(squares);
+    if (!(sum > 1e-20 && sum < INFINITY)) {
+        double again = 0.0;
+        over_eights(a, [&](int64_t r, int c, int n) {
+            Eight u;
+            if (a.update) {
+                u = load_eight(mom_out + r * a.momentum_stride + c, n, a.vectors);
+                if (a.nesterov) u = mix(load_eight(in + r * a.in_stride + c, n, a.vectors), u, a.rest, a.beta);
+            } else {
+                u = load_eight(in + r * a.in_stride + c, n, a.vectors);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) again += static_cast<double>(u.v[j]) * u.v[j];
+        });
+        sum = block_sum(again);
+    }
     if (threadIdx.x == 0) a.partial[static_cast<int64_t>(blockIdx.y) * a.blocks + blockIdx.x] = sum;
 }
 
@@ -328,34 +352,38 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
     sum = block_sum(sum);
     // nothing but zeros stays that; an infinity or a NaN anywhere is NaN everywhere
     const double factor = sum == 0.0 ? 0.0 : (sum < INFINITY ? a.scale / sqrt(sum) : NAN);
+    const float factor32 = static_cast<float>(factor);
+    const bool wide = !(factor32 > 1e-30f && factor32 < 1e30f);  // a factor, or what it is applied to, outside fp32's safe range
     const T* const in = static_cast<const T*>(a.in.p[blockIdx.y]);
     const float* const mom = static_cast<const float*>(a.momentum_out.p[blockIdx.y]);
-    over_fours(a, [&](int64_t r, int c, int n) {
-        float4 u;
+    over_eights(a, [&](int64_t r, int c, int n) {
+        Eight u;
         if (a.update) {
-            u = load_four(mom + r * a.momentum_stride + c, n, a.vectors);
-            if (a.nesterov) u = mix(load_four(in + r * a.in_stride + c, n, a.vectors), u, a.rest, a.beta);
+            u = load_eight(mom + r * a.momentum_stride + c, n, a.vectors);
+            if (a.nesterov) u = mix(load_eight(in + r * a.in_stride + c, n, a.vectors), u, a.rest, a.beta);
         } else {
-            u = load_four(in + r * a.in_stride + c, n, a.vectors);
+            u = load_eight(in + r * a.in_stride + c, n, a.vectors);
         }
-        u = make_float4(static_cast<float>(u.x * factor), static_cast<float>(u.y * factor), static_cast<float>(u.z * factor), static_cast<float>(u.w * factor));
-        uint2 hi, lo;
-        split4(u, &hi, &lo);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u.v[j] = wide ? static_cast<float>(u.v[j] * factor) : u.v[j] * factor32;
+        uint2 hi[2], lo[2];
+        split4(make_float4(u.v[0], u.v[1], u.v[2], u.v[3]), &hi[0], &lo[0]);
+        split4(make_float4(u.v[4], u.v[5], u.v[6], u.v[7]), &hi[1], &lo[1]);
         const int64_t k = blockIdx.y * a.plane + r * a.ld + c;
-        *reinterpret_cast<uint2*>(a.hi + k) = hi;
-        *reinterpret_cast<uint2*>(a.lo + k) = lo;
+        *reinterpret_cast<uint4*>(a.hi + k) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
+        *reinterpret_cast<uint4*>(a.lo + k) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
     });
 }
 
 // ---- host side -------------------------------------------------------------------------------------
 
 constexpr int64_t kMostSide = int64_t(1) << 20, kMostTiles = int64_t(1) << 24;
-constexpr int kMostBlocks = 592;  // of the start's kernels: four to an SM
+constexpr int kMostBlocks = 1184;  // of the start's kernels: eight to an SM
 
 struct Layout {
     int64_t side, ld, side_ld;   // the smaller side; row strides of X and of S and Q
     int64_t plane, side_plane;   // elements of a matrix
-    int blocks;                  // of the start, for each matrix
+    int blocks, row_threads;     // of the start, for each matrix; for each row
     int64_t hi[2], lo, s, q, partial, bytes;  // places in the workspace
 };
 
@@ -369,7 +397,9 @@ int layout_of(int count, int64_t rows, int64_t cols, Layout* l) {
     l->side = rows < cols ? rows : cols;
     l->ld = up_to(cols, 64), l->side_ld = up_to(l->side, 64);
     l->plane = rows * l->ld, l->side_plane = l->side * l->side_ld;
-    const int64_t want = (rows * ((cols + 3) / 4) + 1023) / 1024, most = kMostBlocks / count > 1 ? kMostBlocks / count : 1;
+    l->row_threads = 1;
+    while (l->row_threads < 256 && l->row_threads * 8 < cols) l->row_threads *= 2;
+    const int64_t want = (rows + 256 / l->row_threads - 1) / (256 / l->row_threads), most = kMostBlocks / count > 1 ? kMostBlocks / count : 1;
     l->blocks = static_cast<int>(want < most ? want : most);
     int64_t at = 0;
     auto place = [&](int64_t bytes) {
@@ -404,7 +434,7 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     uint16_t* const lo = reinterpret_cast<uint16_t*>(ws + l.lo);
     uint16_t *const s = reinterpret_cast<uint16_t*>(ws + l.s), *const q = reinterpret_cast<uint16_t*>(ws + l.q);
     Start& a = c.start;
-    a.plane = l.plane, a.rows = c.rows, a.cols = static_cast<int>(c.cols), a.ld = static_cast<int>(l.ld), a.blocks = l.blocks;
+    a.plane = l.plane, a.rows = c.rows, a.cols = static_cast<int>(c.cols), a.ld = static_cast<int>(l.ld), a.blocks = l.blocks, a.row_threads = l.row_threads;
     a.scale = scale, a.partial = reinterpret_cast<double*>(ws + l.partial), a.hi = hi[0], a.lo = lo;
     const dim3 grid(static_cast<unsigned>(l.blocks), static_cast<unsigned>(c.count));
     cudaError_t e;
@@ -470,7 +500,7 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
 struct Mats {
     Mat m[kMostMatrices];
     int status;
-    bool vectors;  // every row starts on four elements
+    bool vectors;  // every row starts on 16 bytes
 
     Mats(const void* const* p, int count, int64_t rows, int64_t cols, int64_t stride, size_t eb) : status(SS_OK), vectors(true) {
         if (p == nullptr || !stride_ok(rows, cols, stride)) {
@@ -481,7 +511,7 @@ struct Mats {
             if (p[i] == nullptr) status = SS_ERR_INVALID_ARG;
             m[i] = mat(p[i], rows, cols, stride, eb);
             if (status == SS_OK && !addr_aligned(p[i], eb)) status = SS_ERR_MISALIGNED;
-            vectors = vectors && m[i].row_aligned(4 * eb);
+            vectors = vectors && m[i].row_aligned(16);
         }
     }
 };

@@ -39,7 +39,7 @@ struct Product {
     int split;        // whether the contraction of tiles that do not fill a round of pairs may be cut into parts
     int m_fast;       // the order of tiles: neighbours share columns of C, or rows
     int upper;        // m == n: only tiles on the diagonal and above
-    int small;        // blocks that share a 128 x 128 tile (1, 2, 4, 8), or 0: pairs on 256 x 256 tiles
+    int small;        // blocks that share a 128 x 128 tile (1, 2, 4), or 0: pairs on 256 x 256 tiles
     int bf16;         // operands: bf16 or fp16
     int follows;      // another kernel of the call goes before
     const int* live;  // rows that there are (all of the call's), or NULL
@@ -160,12 +160,21 @@ __device__ __forceinline__ float square_word(uint32_t buf, int row, int col) {
     return v;
 }
 
+// A lane takes four neighbouring columns of every fourth row of a square: row lane / 8 + 4 i, columns 4 (lane % 8) on.
+__device__ __forceinline__ void square_sums(uint32_t buf, int lane, float4 (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint4 w = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+        v[i] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+    }
+}
+
 constexpr uint32_t kNanBits = 0x7FC00000u;
 
 // EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
 // registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
-// square(column, ..., first chunk?). EPI::kSmall: it also ends the small products below.
+// square(column, ..., its sums, first chunk?). EPI::kSmall: it also ends the small products below.
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
 template <class EPI, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kProdThreads, 1)
@@ -261,7 +270,9 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                         }
                         square_put(buf, lane, r);
                         __syncwarp();
-                        tile.square(epi, j, lane, buf, f, first);
+                        float4 v[8];
+                        square_sums(buf, lane, v);
+                        tile.square(epi, j, lane, buf, v, f, first);
                         __syncwarp();
                     }
                     tc_fence_before();
@@ -364,11 +375,11 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
 }
 
 // ---- small products --------------------------------------------------------------------------------
-// Products that are too small to fill the machine with pairs: one 128 x 128 tile to a cluster of 1, 2, 4 or 8 blocks that
+// Products that are too small to fill the machine with pairs: one 128 x 128 tile to a cluster of 1, 2 or 4 blocks that
 // share the contraction. Each forms its part of the sums, keeps it in shared memory, and adds up its share of
 // the tile's squares from all of them, in the order of their ranks, before it brings it out. A block needs little enough
 // that two fit on an SM: those of the kernel that follows are set up while this one runs.
-constexpr int kSmallTile = 128, kSmallStages = 3, kSmallOut = 128, kSmallThreads = kSmallOut + 64;  // warps 0-3 bring out, 4 copies, 5 issues
+constexpr int kSmallTile = 128, kSmallStages = 3, kSmallOut = 256, kSmallThreads = kSmallOut + 64;  // warps 0-7 bring out, 8 copies, 9 issues
 constexpr size_t kSmallSmem = 1024 + kSmallStages * kProdStageBytes;
 static_assert(kSmallTile * kSmallTile * 4 <= kSmallStages * kProdStageBytes, "the sums take the place of the operands");
 
@@ -379,7 +390,7 @@ struct SmallShared {
 };
 
 template <class EPI, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(kSmallThreads, 2)
+__global__ void __launch_bounds__(kSmallThreads, EPI::kSmallBlocks)
 small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ Product p,
                      const __grid_constant__ EPI epi) {
     extern __shared__ uint8_t dynamic[];
@@ -422,24 +433,21 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
     const uint32_t tmem = sh.tmem;
 
     if (warp < kSmallOut / 32) {
-        const int row = u.m0 + warp * 32;
-        const bool any = row < p.m;
+        // a warp has 32 rows and two squares of them; with two blocks each takes one of the two, with four each takes its own of all four
+        const int quarter = warp & 3, j0 = (warp >> 2) * 2, row = u.m0 + quarter * 32;
         typename EPI::Tile tile(epi, u, p.m, row, u.n0, lane);
         typename EPI::Fetched f;
-        auto mine = [&](int j) { return ((4 * j + warp) * blocks >> 4) == rank && any && u.n0 + 32 * j < p.n; };
-        auto square = [&](int j) { return stages + (4 * warp + j) * kProdSquare; };
-        int fetched = -1;
-#pragma unroll 1
-        for (int j = 0; j < 4 && fetched < 0; ++j)
-            if (mine(j)) fetched = j;
+        auto mine = [&](int j) { return (blocks == 1 || (j & (blocks - 1)) == rank) && row < p.m && u.n0 + 32 * j < p.n; };
+        auto square = [&](int j) { return stages + (4 * quarter + j) * kProdSquare; };
+        const int fetched = mine(j0) ? j0 : (mine(j0 + 1) ? j0 + 1 : -1);
         if (fetched >= 0) tile.fetch(epi, 32 * fetched, f);
         const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed), 0, &sh.abort));
         tc_fence_after();
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {
+        for (int j = j0; j < j0 + 2; ++j) {
             if (blocks == 1 && !mine(j)) continue;
             uint32_t r[32];
-            tmem_load32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + 32 * j, r);
+            tmem_load32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + 32 * j, r);
             tmem_load_wait();
             if (!ok) {
 #pragma unroll
@@ -451,24 +459,26 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
         __syncwarp();
         if (blocks > 1) cluster_sync();
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {
+        for (int j = j0; j < j0 + 2; ++j) {
             if (!mine(j)) continue;
             if (j != fetched) tile.fetch(epi, 32 * j, f);
-            if (blocks > 1) {
-#pragma unroll 2
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t at = square_at(square(j), (lane >> 3) + 4 * i, lane & 7);
-                    float4 v = cluster_load4(cluster_addr(at, 0));
-                    for (int q = 1; q < blocks; ++q) {
-                        const float4 x = cluster_load4(cluster_addr(at, q));
-                        v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-                    }
-                    __syncwarp();
-                    square_set(square(j), (lane >> 3) + 4 * i, lane & 7, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+            float4 v[8];
+            if (blocks == 1) {
+                square_sums(square(j), lane, v);
+            } else {  // eight loads of a block under way at a time
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+                for (int q = 0; q < blocks; ++q) {
+                    float4 x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = cluster_load4(cluster_addr(square_at(square(j), (lane >> 3) + 4 * i, lane & 7), q));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i].x += x[i].x, v[i].y += x[i].y, v[i].z += x[i].z, v[i].w += x[i].w;
                 }
                 __syncwarp();
             }
-            tile.square(epi, 32 * j, lane, square(j), f, true);
+            tile.square(epi, 32 * j, lane, square(j), v, f, true);
             __syncwarp();
         }
     } else {
@@ -561,16 +571,19 @@ inline int64_t small_tiles(const Product& p) {
     return (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
 }
 
-// How many blocks share a 128 x 128 tile, or 0 for pairs on 256 x 256 tiles: the least of an estimate in cycles. A pair takes 700
-// for a stage, a small block 600 (it copies as much for half the products), 900 with another on its SM; with what a tile costs besides.
+// How many blocks share a 128 x 128 tile, or 0 for pairs on 256 x 256 tiles: the least of an estimate in ns, fitted to products of
+// 128 to 4096 rows and contractions of 128 to 4608 (which it meets within 2 us). Small blocks wait for the L2 cache, the more of them
+// the longer; two fit on an SM. S of 1000 x 2048: 19 us in pairs, 13.1, 12.9 and 13.2 with 1, 2 and 4 blocks; of two of 300 x 3000 19.5, 16.8, 13.9
+// and 10.3; of 4096 x 4096 52 in pairs and 90 with one block.
 inline int small_blocks(const Product& p, int sms) {
     const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile, stages = (p.k + kProdK - 1) / kProdK;
     const int64_t tiles = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches, small = small_tiles(p);
-    int64_t best = (tiles + p.pairs - 1) / p.pairs * stages * 700 + (tiles > p.pairs ? 9000 : 8000);
+    const int64_t pair_rounds = (tiles + p.pairs - 1) / p.pairs, hidden = stages * 370 < 6000 ? 6000 - stages * 370 : 0;
+    int64_t best = pair_rounds * stages * 370 + 8500 + (pair_rounds - 1) * hidden;
     int blocks = 0;
-    for (int c = 1; c <= 8 && c <= stages; c *= 2) {
-        const int64_t all = small * c, rounds = (all + 2 * sms - 1) / (2 * sms);
-        const int64_t t = rounds * ((stages + c - 1) / c * (all <= sms ? 600 : 900) + 5000) + (c > 1 ? 1000 : 0);
+    for (int c = 1; c <= 4 && c <= stages; c *= 2) {
+        const int64_t all = small * c, rounds = (all + 2 * sms - 1) / (2 * sms), at_once = all < 2 * sms ? all : 2 * sms;
+        const int64_t t = rounds * ((stages + c - 1) / c * (170 + at_once * 9 / 4)) + 5500 + (rounds - 1) * 2000 + (c == 2 ? 800 : (c == 4 ? 1000 + 20 * all : 0));
         if (t < best) best = t, blocks = c;
     }
     return blocks;
