@@ -375,6 +375,305 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
     });
 }
 
+// ---- matrices with a side of at most 128: all steps in one launch -----------------------------------
+// A cluster of up to eight blocks holds a matrix on chip: each has 256 of the longer side's indices l, as fp32 in registers (a
+// thread has 128 neighbouring elements of a row, in memory's order: rows are the shorter side's indices i, or l where the matrix is tall)
+// and as fp16 operand in shared memory. A step is three products within the block; between them S is summed over the cluster, each
+// block a share of its rows, which it hands to all. Per step one block alone takes 3 us and eight 5; 15 products of their own take 4 to 6 us each, most of it start and end.
+constexpr int kHeldSide = 128, kHeldLong = 256, kHeldThreads = 256, kMostHeldBlocks = 8;
+constexpr uint32_t kHeldX = kHeldSide * kHeldLong * 2, kHeldS = kHeldSide * kHeldSide * 2, kHeldPart = kHeldSide * kHeldSide * 4;
+constexpr size_t kHeldSmem = 1024 + kHeldX + 2 * kHeldS + kHeldPart;
+
+struct Held {
+    Start start;        // in, momentum, momentum_out, strides, rows, cols, update, nesterov, beta, rest, scale
+    Table out, param;
+    int64_t out_stride;
+    int in_vectors, out_vectors, to, steps;
+    float unscale, lr, scale, decay;
+    float coefficients[3 * SS_ORTHO_MAX_STEPS];
+};
+
+// Row r of an operand of 64 elements (128 bytes, swizzled) a row: its 16-byte chunk c.
+__device__ __forceinline__ uint32_t held_chunk(uint32_t panel, int r, int c) { return panel + r * 128 + ((c ^ (r & 7)) << 4); }
+
+template <typename T, bool TALL>
+__global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __grid_constant__ Held a) {
+    extern __shared__ uint8_t dynamic[];
+    __shared__ uint64_t bar;
+    __shared__ uint32_t tmem_address;
+    __shared__ int abort;
+    __shared__ double norm_part;
+    const uint32_t xs = (smem_addr(dynamic) + 1023u) & ~1023u, ss_ = xs + kHeldX, qs = ss_ + kHeldS, ps = qs + kHeldS;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, half = warp >> 2;
+    uint32_t rank, blocks;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
+    const int matrix = blockIdx.x / blocks;
+
+    if (tid == 0) {
+        mbar_init(smem_addr(&bar), 1);
+        abort = 0;
+        mbar_init_visible();
+    }
+    if (warp == 0) tmem_alloc(smem_addr(&tmem_address), 512);
+
+    // this thread's elements: row `row` of the matrix, columns from `col` on
+    const int i_or_l = quarter * 32 + lane;
+    const int64_t row = TALL ? static_cast<int64_t>(rank) * kHeldLong + half * 128 + i_or_l : i_or_l;
+    const int64_t col = TALL ? 0 : static_cast<int64_t>(rank) * kHeldLong + half * 128;
+    const int there = row < a.start.rows ? static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(128), a.start.cols - col))) : 0;
+    float x[128];
+    double sum = 0.0;
+    {
+        const Start& st = a.start;
+        const T* const in = static_cast<const T*>(st.in.p[matrix]) + row * st.in_stride + col;
+        const float* const mom = static_cast<const float*>(st.momentum.p[matrix]) + row * st.momentum_stride + col;
+        float* const mom_out = static_cast<float*>(const_cast<void*>(st.momentum_out.p[matrix])) + row * st.momentum_stride + col;
+#pragma unroll
+        for (int j = 0; j < 128; j += 8) {
+            Eight u;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) u.v[d] = 0.0f;
+            const int n = there - j;
+            if (n > 0) {
+                u = load_eight(in + j, n, a.in_vectors);
+                if (st.update) {
+                    const Eight g = u, v = mix(g, load_eight(mom + j, n, a.in_vectors), st.rest, st.beta);
+                    if (a.in_vectors && n >= 8) {
+                        reinterpret_cast<float4*>(mom_out + j)[0] = make_float4(v.v[0], v.v[1], v.v[2], v.v[3]);
+                        reinterpret_cast<float4*>(mom_out + j)[1] = make_float4(v.v[4], v.v[5], v.v[6], v.v[7]);
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < 8; ++d)
+                            if (d < n) mom_out[j + d] = v.v[d];
+                    }
+                    u = st.nesterov ? mix(g, v, st.rest, st.beta) : v;
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < 8; ++d) x[j + d] = u.v[d];
+        }
+    }
+    {   // fp32 holds the squares' sum unless it leaves the range: then again in fp64
+        float squares = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 128; ++j) squares += x[j] * x[j];
+        sum = block_sum(squares);
+        if (!(sum > 1e-20 && sum < INFINITY)) {
+            double again = 0.0;
+#pragma unroll
+            for (int j = 0; j < 128; ++j) again += static_cast<double>(x[j]) * x[j];
+            sum = block_sum(again);
+        }
+    }
+    if (tid == 0) norm_part = sum;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (blocks > 1) {
+        cluster_sync();
+        sum = 0.0;
+        for (uint32_t q = 0; q < blocks; ++q) sum += cluster_load_double(cluster_addr(smem_addr(&norm_part), q));
+    }
+    const double factor = sum == 0.0 ? 0.0 : (sum < INFINITY ? a.start.scale / sqrt(sum) : NAN);
+    const float factor32 = static_cast<float>(factor);
+    if (factor32 > 1e-30f && factor32 < 1e30f) {
+#pragma unroll
+        for (int j = 0; j < 128; ++j) x[j] *= factor32;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 128; ++j) x[j] = static_cast<float>(x[j] * factor);
+    }
+
+    const uint32_t tmem = tmem_address, lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const float inverse = a.unscale * a.unscale;
+    uint32_t parity = 0;
+    bool ok = true;
+    // one warp issues, all wait for the products to have ended
+    auto products = [&](auto issue) {
+        smem_to_async();
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (warp == 0) {
+            if (elect_one()) {
+                issue();
+                tc_commit(smem_addr(&bar));
+            }
+            __syncwarp();
+        }
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&bar), parity, &abort)) && ok;
+        parity ^= 1;
+        tc_fence_after();
+    };
+    constexpr uint32_t kIdescCols = tc_idesc(128, 128, false, false, false);
+    // of this block's 256 long indices, those that the matrix has, in sixteens (one at least: S is written by it)
+    const int64_t longest = (TALL ? a.start.rows : static_cast<int64_t>(a.start.cols)) - static_cast<int64_t>(rank) * kHeldLong;
+    const int long_steps = static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(kHeldLong / 16), (longest + 15) / 16)));
+
+    for (int step = 0; step < a.steps; ++step) {
+        const float ca = a.coefficients[3 * step], cb = a.coefficients[3 * step + 1], cc = a.coefficients[3 * step + 2];
+        // ---- the operand: rows of 64 elements in panels, wide: [l / 64][i][l % 64], tall: [i / 64][l][i % 64]
+        {
+            const int r = TALL ? half * 128 + i_or_l : i_or_l;
+            const uint32_t panel = TALL ? kHeldLong * 128 : kHeldSide * 128, first = xs + (TALL ? 0 : half * 2 * panel);
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+                const uint2 lo = half4(make_float4(x[8 * c], x[8 * c + 1], x[8 * c + 2], x[8 * c + 3])), hi = half4(make_float4(x[8 * c + 4], x[8 * c + 5], x[8 * c + 6], x[8 * c + 7]));
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(first + (c >> 3) * panel, r, c & 7)), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
+            }
+        }
+        // ---- S of this block's part
+        products([&] {
+            constexpr uint32_t idesc = tc_idesc(128, 128, false, TALL, TALL);
+#pragma unroll 1
+            for (int k = 0; k < long_steps; ++k) {
+                const uint64_t d = TALL ? tc_desc_rows(xs + k * 2048, kHeldLong * 128) : tc_desc_cols(xs + (k >> 2) * kHeldSide * 128 + (k & 3) * 32);
+                tc_mma_f16(tmem, d, d, idesc, k != 0);
+            }
+        });
+        // ---- S as an operand: rows of 128, in two panels of 64. This thread: row i_or_l, columns 64 half on
+        if (blocks == 1) {
+#pragma unroll
+            for (int c = 0; c < 8; c += 2) {
+                uint32_t r[16];
+                tmem_load16(tmem + lanes + half * 64 + c * 8, r);
+                tmem_load_wait();
+                uint2 w[4];
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    w[d] = half4(make_float4(inverse * __uint_as_float(r[4 * d]), inverse * __uint_as_float(r[4 * d + 1]), inverse * __uint_as_float(r[4 * d + 2]), inverse * __uint_as_float(r[4 * d + 3])));
+#pragma unroll
+                for (int d = 0; d < 2; ++d)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(ss_ + half * kHeldSide * 128, i_or_l, c + d)), "r"(w[2 * d].x), "r"(w[2 * d].y), "r"(w[2 * d + 1].x), "r"(w[2 * d + 1].y) : "memory");
+            }
+        } else {
+            // parts as rows of 512 bytes, whose 16-byte chunks are swizzled by the row
+#pragma unroll
+            for (int c = 0; c < 16; c += 4) {
+                uint32_t r[16];
+                tmem_load16(tmem + lanes + half * 64 + c * 4, r);
+                tmem_load_wait();
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ps + i_or_l * 512 + (((half * 16 + c + d) ^ (i_or_l & 7)) << 4)), "r"(r[4 * d]), "r"(r[4 * d + 1]), "r"(r[4 * d + 2]), "r"(r[4 * d + 3]) : "memory");
+            }
+            cluster_sync();
+            const int rows = kHeldSide / blocks;  // eight columns to a thread
+            for (int e = tid; e < rows * 16; e += kHeldThreads) {
+                const int r = rank * rows + (e >> 4), c = e & 15;
+                float v[8];
+#pragma unroll
+                for (int d = 0; d < 8; ++d) v[d] = 0.0f;
+                const uint32_t at = ps + r * 512, c0 = ((2 * c) ^ (r & 7)) << 4, c1 = ((2 * c + 1) ^ (r & 7)) << 4;
+#pragma unroll 4
+                for (uint32_t q = 0; q < blocks; ++q) {  // in the order of the ranks
+                    const uint32_t there_ = cluster_addr(at, q);
+                    const float4 y = cluster_load4(there_ + c0), z = cluster_load4(there_ + c1);
+                    v[0] += y.x, v[1] += y.y, v[2] += y.z, v[3] += y.w, v[4] += z.x, v[5] += z.y, v[6] += z.z, v[7] += z.w;
+                }
+                const uint2 lo = half4(make_float4(inverse * v[0], inverse * v[1], inverse * v[2], inverse * v[3])), hi = half4(make_float4(inverse * v[4], inverse * v[5], inverse * v[6], inverse * v[7]));
+                const uint32_t to = held_chunk(ss_ + (c >> 3) * kHeldSide * 128, r, c & 7);
+#pragma unroll 4
+                for (uint32_t q = 0; q < blocks; ++q) cluster_store4(cluster_addr(to, q), make_uint4(lo.x, lo.y, hi.x, hi.y));
+            }
+            cluster_sync();
+        }
+        // ---- Q = b S + c S S
+        products([&] {
+#pragma unroll
+            for (int k = 0; k < kHeldSide / 16; ++k) {
+                const uint64_t d = tc_desc_cols(ss_ + (k >> 2) * kHeldSide * 128 + (k & 3) * 32);
+                tc_mma_f16(tmem, d, d, kIdescCols, k != 0);
+            }
+        });
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) {
+            uint32_t r[16];
+            tmem_load16(tmem + lanes + half * 64 + c * 8, r);
+            tmem_load_wait();
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                uint4 s;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(s.x), "=r"(s.y), "=r"(s.z), "=r"(s.w) : "r"(held_chunk(ss_ + half * kHeldSide * 128, i_or_l, c + d)) : "memory");
+                const float4 y = float4_of(make_uint2(s.x, s.y)), z = float4_of(make_uint2(s.z, s.w));
+                const uint32_t* const p = r + 8 * d;
+                const uint2 lo = half4(make_float4(cb * y.x + cc * __uint_as_float(p[0]), cb * y.y + cc * __uint_as_float(p[1]), cb * y.z + cc * __uint_as_float(p[2]), cb * y.w + cc * __uint_as_float(p[3])));
+                const uint2 hi = half4(make_float4(cb * z.x + cc * __uint_as_float(p[4]), cb * z.y + cc * __uint_as_float(p[5]), cb * z.z + cc * __uint_as_float(p[6]), cb * z.w + cc * __uint_as_float(p[7])));
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(qs + half * kHeldSide * 128, i_or_l, c + d)), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
+            }
+        }
+        // ---- X = a X + Q X
+        products([&] {
+            if constexpr (TALL) {  // X Q, 128 rows of X at a time
+#pragma unroll 1
+                for (int h = 0; h < kHeldLong / 128; ++h)
+#pragma unroll 1
+                    for (int k = 0; k < kHeldSide / 16; ++k)
+                        tc_mma_f16(tmem + 128 + h * 128, tc_desc_cols(xs + (k >> 2) * kHeldLong * 128 + h * 128 * 128 + (k & 3) * 32),
+                                   tc_desc_cols(qs + (k >> 2) * kHeldSide * 128 + (k & 3) * 32), kIdescCols, k != 0);
+            } else {
+                constexpr uint32_t idesc = tc_idesc(128, kHeldLong, false, false, true);
+#pragma unroll 1
+                for (int k = 0; k < kHeldSide / 16; ++k)
+                    tc_mma_f16(tmem + 128, tc_desc_cols(qs + (k >> 2) * kHeldSide * 128 + (k & 3) * 32), tc_desc_rows(xs + k * 2048, kHeldSide * 128), idesc, k != 0);
+            }
+        });
+#pragma unroll
+        for (int j = 0; j < 128; j += 16) {
+            uint32_t r[16];
+            tmem_load16(tmem + lanes + 128 + half * 128 + j, r);
+            tmem_load_wait();
+#pragma unroll
+            for (int d = 0; d < 16; ++d) x[j + d] = ca * x[j + d] + __uint_as_float(r[d]);
+        }
+    }
+    if (!ok) {
+#pragma unroll
+        for (int j = 0; j < 128; ++j) x[j] = __uint_as_float(kNanBits);
+    }
+    // ---- out
+    {
+        const int64_t at = row * a.out_stride + col;
+        float* const to32 = static_cast<float*>(const_cast<void*>(a.out.p[matrix])) + at;
+        uint16_t* const to16 = static_cast<uint16_t*>(const_cast<void*>(a.out.p[matrix])) + at;
+        const float* const from = static_cast<const float*>(a.param.p[matrix]) + at;
+#pragma unroll
+        for (int j = 0; j < 128; j += 8) {
+            const int n = there - j;
+            if (n <= 0) continue;
+            Eight o;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) o.v[d] = x[j + d] * a.unscale;
+            if (a.to == kToParam) {
+                const Eight p = load_eight(from + j, n, a.out_vectors);
+#pragma unroll
+                for (int d = 0; d < 8; ++d) o.v[d] = p.v[d] - a.lr * (a.scale * o.v[d] + a.decay * p.v[d]);
+            }
+            if (a.out_vectors && n >= 8) {
+                if (a.to == kToBf16) {
+                    *reinterpret_cast<uint4*>(to16 + j) = make_uint4(bf16_pair(o.v[0], o.v[1]), bf16_pair(o.v[2], o.v[3]), bf16_pair(o.v[4], o.v[5]), bf16_pair(o.v[6], o.v[7]));
+                } else {
+                    reinterpret_cast<float4*>(to32 + j)[0] = make_float4(o.v[0], o.v[1], o.v[2], o.v[3]);
+                    reinterpret_cast<float4*>(to32 + j)[1] = make_float4(o.v[4], o.v[5], o.v[6], o.v[7]);
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < 8; ++d) {
+                    if (d >= n) continue;
+                    if (a.to == kToBf16) Elem<uint16_t>::store(to16 + j + d, o.v[d]);
+                    else to32[j + d] = o.v[d];
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (blocks > 1) cluster_sync();  // the others may still be reading this block's memory
+    tc_fence_after();
+    if (warp == 0) tmem_free(tmem, 512);
+}
+
 // ---- host side -------------------------------------------------------------------------------------
 
 constexpr int64_t kMostSide = int64_t(1) << 20, kMostTiles = int64_t(1) << 24;
@@ -425,11 +724,50 @@ struct Call {
     int steps;
 };
 
+template <typename T, bool TALL>
+int launch_held(const Held& h, int matrices, int blocks, cudaStream_t st) {
+    const auto kernel = ortho_held_kernel<T, TALL>;
+    struct Key {};
+    cudaError_t e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kHeldSmem));
+    if (e != cudaSuccess) return cuda_status_public(e);
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = blocks, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(static_cast<unsigned>(matrices * blocks)), cfg.blockDim = dim3(kHeldThreads);
+    cfg.dynamicSmemBytes = kHeldSmem, cfg.stream = st, cfg.attrs = &at, cfg.numAttrs = 1;
+    return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, h));
+}
+
+// Blocks that hold a matrix of these sides, or 0: it is held only up to kHeldSide by kMostHeldBlocks * kHeldLong.
+int held_blocks(int64_t rows, int64_t cols) {
+    const int64_t small = rows < cols ? rows : cols, big = rows < cols ? cols : rows;
+    if (small > kHeldSide || big > kMostHeldBlocks * kHeldLong) return 0;
+    int blocks = 1;
+    while (blocks * kHeldLong < big) blocks *= 2;
+    return blocks;
+}
+
+int run_held(const Call& c, int blocks, float scale, float unscale, cudaStream_t st) {
+    Held h{};
+    h.start = c.start;
+    h.start.rows = c.rows, h.start.cols = static_cast<int>(c.cols), h.start.scale = scale;
+    h.in_vectors = c.start.vectors, h.out_vectors = c.result.vectors, h.out = c.result.out, h.param = c.result.param;
+    h.out_stride = c.result.stride, h.to = c.to, h.steps = c.steps;
+    h.unscale = unscale, h.lr = c.result.lr, h.scale = c.result.scale, h.decay = c.result.decay;
+    for (int i = 0; i < 3 * c.steps; ++i) h.coefficients[i] = c.coefficients[i];
+    const bool tall = c.rows > c.cols;
+    if (c.in_dt == SS_F32) return tall ? launch_held<float, true>(h, c.count, blocks, st) : launch_held<float, false>(h, c.count, blocks, st);
+    return tall ? launch_held<uint16_t, true>(h, c.count, blocks, st) : launch_held<uint16_t, false>(h, c.count, blocks, st);
+}
+
 int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     const int64_t big = c.rows > c.cols ? c.rows : c.cols;
     int power = 0;  // 2^power: about the root of the larger side, so that X ends with values about 1
     while ((int64_t(1) << (2 * (power + 1))) <= big) ++power;
     const float scale = std::ldexp(1.0f, power), unscale = std::ldexp(1.0f, -power);
+    const int held = held_blocks(c.rows, c.cols);
+    if (held > 0) return run_held(c, held, scale, unscale, st);
     uint16_t* hi[2] = {reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.hi[1])};
     uint16_t* const lo = reinterpret_cast<uint16_t*>(ws + l.lo);
     uint16_t *const s = reinterpret_cast<uint16_t*>(ws + l.s), *const q = reinterpret_cast<uint16_t*>(ws + l.q);

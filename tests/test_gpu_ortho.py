@@ -45,7 +45,8 @@ def run(mats, out_dtype=F32, coefficients=ref.COEFFICIENTS):
     return out
 
 
-SHAPES = [(1, 1), (1, 40), (40, 1), (2, 3), (17, 33), (64, 64), (33, 17), (100, 257), (257, 100), (128, 640), (300, 300), (511, 513), (700, 260), (1000, 2048)]
+SHAPES = [(1, 1), (1, 40), (40, 1), (2, 3), (17, 33), (64, 64), (33, 17), (100, 257), (257, 100), (128, 640), (300, 300), (511, 513), (700, 260), (1000, 2048),
+          (5, 256), (256, 5), (128, 257), (257, 128), (77, 1000), (1025, 128), (128, 2048), (2048, 100), (2049, 128), (129, 129), (64, 4000)]
 
 
 @pytest.mark.parametrize("kind", ["strong", "noise"])
@@ -57,7 +58,7 @@ def test_orthogonalise(shape, kind):
             near("%s -> %s" % (dtype, out), run([u], out)[0], u)
 
 
-@pytest.mark.parametrize("shape", [(96, 200), (200, 96)])
+@pytest.mark.parametrize("shape", [(96, 200), (200, 96), (120, 900), (600, 50), (300, 150)])
 def test_several_matrices_are_each_their_own(shape):
     mats = [matrix(*shape, seed=i, size=10.0 ** (i - 3)) for i in range(7)]
     for got, u in zip(run(mats), mats):
@@ -80,9 +81,10 @@ def test_coefficients_of_each_step(steps):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("pad,offset", [(8, 0), (4, 4), (3, 1)])
-def test_slices_of_wider_matrices(dtype, pad, offset):
-    u = matrix(90, 130 + pad, seed=pad, dtype=dtype)[:, offset:offset + 130]
-    whole = torch.full((90, 130 + pad), 7.0, dtype=dtype, device=DEV)
+@pytest.mark.parametrize("rows", [90, 190])
+def test_slices_of_wider_matrices(rows, dtype, pad, offset):
+    u = matrix(rows, 130 + pad, seed=pad, dtype=dtype)[:, offset:offset + 130]
+    whole = torch.full((rows, 130 + pad), 7.0, dtype=dtype, device=DEV)
     out = whole[:, offset:offset + 130]
     B.ss_orthogonalise([u], [out])
     assert torch.equal(out, run([u.contiguous()], dtype)[0])
@@ -99,7 +101,7 @@ def test_in_place():
             assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("shape", [(48, 80), (80, 48)])
+@pytest.mark.parametrize("shape", [(48, 80), (80, 48), (100, 700), (200, 160)])
 def test_zeros_and_values_that_are_not_finite(shape):
     zero, nan, inf, fine = (matrix(*shape, seed=i) for i in range(4))
     zero.zero_()
@@ -110,8 +112,9 @@ def test_zeros_and_values_that_are_not_finite(shape):
 
 
 @pytest.mark.parametrize("size", [1e-38, 1e-25, 1e30, 3e37])
-def test_the_whole_range_of_fp32(size):
-    u = matrix(60, 70, seed=2, kind="noise", size=1.0) * size
+@pytest.mark.parametrize("shape", [(60, 70), (150, 170)])
+def test_the_whole_range_of_fp32(shape, size):
+    u = matrix(*shape, seed=2, kind="noise", size=1.0) * size
     near("size %g" % size, run([u])[0], u)
 
 
@@ -123,7 +126,7 @@ def update(g, v, p, beta=0.95, nesterov=True, lr=0.02, scale=0.7, decay=0.1, in_
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("nesterov", [False, True])
-@pytest.mark.parametrize("shape", [(1, 1), (130, 70), (65, 259), (512, 512)])
+@pytest.mark.parametrize("shape", [(1, 1), (130, 70), (65, 259), (900, 33), (512, 512), (140, 1111)])
 def test_update(shape, nesterov, dtype):
     g, v, p = ([matrix(*shape, seed=10 * k + i, size=s).to(dt) for i in range(2)] for k, s, dt in ((1, 1e-3, dtype), (2, 1e-3, F32), (3, 1e-2, F32)))
     vo, po = update(g, v, p, nesterov=nesterov)
