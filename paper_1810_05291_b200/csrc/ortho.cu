@@ -379,10 +379,12 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
 // A cluster of up to eight blocks holds a matrix on chip: each has 256 of the longer side's indices l, as fp32 in registers (a
 // thread has 128 neighbouring elements of a row, in memory's order: rows are the shorter side's indices i, or l where the matrix is tall)
 // and as fp16 operand in shared memory. A step is three products within the block; between them S is summed over the cluster, each
-// block a share of its rows, which it hands to all. Per step one block alone takes 3 us and eight 5; 15 products of their own take 4 to 6 us each, most of it start and end.
+// block a share of its rows, which it hands to all.
 constexpr int kHeldSide = 128, kHeldLong = 256, kHeldThreads = 256, kMostHeldBlocks = 8;
 constexpr uint32_t kHeldX = kHeldSide * kHeldLong * 2, kHeldS = kHeldSide * kHeldSide * 2, kHeldPart = kHeldSide * kHeldSide * 4;
-constexpr size_t kHeldSmem = 1024 + kHeldX + 2 * kHeldS + kHeldPart;
+// X; S; Q, whose place the others' shares of S take before it is formed, and 32 KB more of those; this block's part of S
+constexpr size_t kHeldSmem = 1024 + kHeldX + 3 * kHeldS + kHeldPart;
+static_assert(kHeldPart == 2 * kHeldS, "the others' shares are as many bytes as a part");
 
 struct Held {
     Start start;        // in, momentum, momentum_out, strides, rows, cols, update, nesterov, beta, rest, scale
@@ -393,17 +395,58 @@ struct Held {
     float coefficients[3 * SS_ORTHO_MAX_STEPS];
 };
 
+// Four neighbouring columns of a row.
+__device__ __forceinline__ float4 load_whole(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load_whole(const uint16_t* p) {
+    const uint2 r = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xFFFF0000u));
+}
+template <typename T>
+__device__ __forceinline__ float4 load_four(const T* p, int n, bool vectors) {
+    if (vectors && n >= 4) return load_whole(p);
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = j < n ? Elem<T>::load(p + j) : 0.0f;
+    return make_float4(v[0], v[1], v[2], v[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store_four(T* p, float4 v, int n, bool vectors) {
+    if (vectors && n >= 4) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = v;
+        else *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+    } else {
+        const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) Elem<T>::store(p + j, e[j]);
+    }
+}
+__device__ __forceinline__ float4 mix(float4 g, float4 v, float rest, float beta) {
+    return make_float4(rest * g.x + beta * v.x, rest * g.y + beta * v.y, rest * g.z + beta * v.z, rest * g.w + beta * v.w);
+}
+
+__device__ __forceinline__ float4 shared_load4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// Chunk c (16 bytes) of row r of a square of 32 rows of 512 bytes.
+__device__ __forceinline__ void turn_put(uint32_t at, int r, int c, float4 v) {
+    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + r * 512 + ((c ^ (r & 7)) << 4)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ float4 turn_get(uint32_t at, int r, int c) { return shared_load4(at + r * 512 + ((c ^ (r & 7)) << 4)); }
+
 // Row r of an operand of 64 elements (128 bytes, swizzled) a row: its 16-byte chunk c.
 __device__ __forceinline__ uint32_t held_chunk(uint32_t panel, int r, int c) { return panel + r * 128 + ((c ^ (r & 7)) << 4); }
 
 template <typename T, bool TALL>
 __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __grid_constant__ Held a) {
     extern __shared__ uint8_t dynamic[];
-    __shared__ uint64_t bar;
+    __shared__ uint64_t bar, came, handed;
     __shared__ uint32_t tmem_address;
     __shared__ int abort;
     __shared__ double norm_part;
-    const uint32_t xs = (smem_addr(dynamic) + 1023u) & ~1023u, ss_ = xs + kHeldX, qs = ss_ + kHeldS, ps = qs + kHeldS;
+    const uint32_t xs = (smem_addr(dynamic) + 1023u) & ~1023u, ss_ = xs + kHeldX, qs = ss_ + kHeldS, ps = qs + 2 * kHeldS;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, half = warp >> 2;
     uint32_t rank, blocks;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -412,46 +455,67 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
 
     if (tid == 0) {
         mbar_init(smem_addr(&bar), 1);
+        mbar_init(smem_addr(&came), 1);
+        mbar_init(smem_addr(&handed), 1);
         abort = 0;
         mbar_init_visible();
     }
     if (warp == 0) tmem_alloc(smem_addr(&tmem_address), 512);
 
-    // this thread's elements: row `row` of the matrix, columns from `col` on
+    // This thread's elements: one row of the matrix, 128 columns from `col` on. A warp has 32 rows from `row0` on; they come and
+    // go a row at a time, four columns to a lane, and are turned in shared memory. (A row a lane in global memory takes a cycle for each of a load's 32
+    // lines: 6 us for 128 x 128 instead of 2.)
     const int i_or_l = quarter * 32 + lane;
-    const int64_t row = TALL ? static_cast<int64_t>(rank) * kHeldLong + half * 128 + i_or_l : i_or_l;
+    const int64_t row0 = TALL ? static_cast<int64_t>(rank) * kHeldLong + half * 128 + quarter * 32 : quarter * 32;
     const int64_t col = TALL ? 0 : static_cast<int64_t>(rank) * kHeldLong + half * 128;
-    const int there = row < a.start.rows ? static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(128), a.start.cols - col))) : 0;
+    const int rows = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), a.start.rows - row0)));
+    const int cols = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(128), a.start.cols - col)));
+    const uint32_t turn = (warp < 4 ? xs + warp * 16384 : ps + (warp - 4) * 16384);  // 32 rows of 512 bytes
     float x[128];
     double sum = 0.0;
     {
         const Start& st = a.start;
-        const T* const in = static_cast<const T*>(st.in.p[matrix]) + row * st.in_stride + col;
-        const float* const mom = static_cast<const float*>(st.momentum.p[matrix]) + row * st.momentum_stride + col;
-        float* const mom_out = static_cast<float*>(const_cast<void*>(st.momentum_out.p[matrix])) + row * st.momentum_stride + col;
-#pragma unroll
-        for (int j = 0; j < 128; j += 8) {
-            Eight u;
-#pragma unroll
-            for (int d = 0; d < 8; ++d) u.v[d] = 0.0f;
-            const int n = there - j;
-            if (n > 0) {
-                u = load_eight(in + j, n, a.in_vectors);
-                if (st.update) {
-                    const Eight g = u, v = mix(g, load_eight(mom + j, n, a.in_vectors), st.rest, st.beta);
-                    if (a.in_vectors && n >= 8) {
-                        reinterpret_cast<float4*>(mom_out + j)[0] = make_float4(v.v[0], v.v[1], v.v[2], v.v[3]);
-                        reinterpret_cast<float4*>(mom_out + j)[1] = make_float4(v.v[4], v.v[5], v.v[6], v.v[7]);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < 8; ++d)
-                            if (d < n) mom_out[j + d] = v.v[d];
-                    }
-                    u = st.nesterov ? mix(g, v, st.rest, st.beta) : v;
-                }
+        const T* const in = static_cast<const T*>(st.in.p[matrix]) + row0 * st.in_stride + col;
+        const float* const mom = static_cast<const float*>(st.momentum.p[matrix]) + row0 * st.momentum_stride + col;
+        float* const mom_out = static_cast<float*>(const_cast<void*>(st.momentum_out.p[matrix])) + row0 * st.momentum_stride + col;
+        const int n = cols - 4 * lane;
+        const bool whole = a.in_vectors && n >= 4;  // of this lane
+        auto take = [&](int r, float4 g, float4 v) {
+            float4 u = g;
+            if (st.update) {
+                u = mix(g, v, st.rest, st.beta);
+                if (r < rows) store_four(mom_out + r * st.momentum_stride + 4 * lane, u, n, a.in_vectors);
+                if (st.nesterov) u = mix(g, u, st.rest, st.beta);
             }
+            turn_put(turn, r, lane, u);
+        };
+        if (__all_sync(0xFFFFFFFFu, whole || n <= 0)) {
+#pragma unroll 1
+            for (int r0 = 0; r0 < 32; r0 += 8) {
+                float4 g[8], v[8];
 #pragma unroll
-            for (int d = 0; d < 8; ++d) x[j + d] = u.v[d];
+                for (int r = 0; r < 8; ++r) {
+                    g[r] = v[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (r0 + r >= rows || n <= 0) continue;
+                    g[r] = load_whole(in + (r0 + r) * st.in_stride + 4 * lane);
+                    if (st.update) v[r] = load_whole(mom + (r0 + r) * st.momentum_stride + 4 * lane);
+                }
+#pragma unroll
+                for (int r = 0; r < 8; ++r) take(r0 + r, g[r], v[r]);
+            }
+        } else {
+#pragma unroll 2
+            for (int r = 0; r < 32; ++r) {
+                const int m = r < rows ? n : 0;
+                take(r, load_four(in + r * st.in_stride + 4 * lane, m, a.in_vectors),
+                     st.update ? load_four(mom + r * st.momentum_stride + 4 * lane, m, a.in_vectors) : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            const float4 u = turn_get(turn, lane, c);
+            x[4 * c] = u.x, x[4 * c + 1] = u.y, x[4 * c + 2] = u.z, x[4 * c + 3] = u.w;
         }
     }
     {   // fp32 holds the squares' sum unless it leaves the range: then again in fp64
@@ -511,6 +575,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
     const int64_t longest = (TALL ? a.start.rows : static_cast<int64_t>(a.start.cols)) - static_cast<int64_t>(rank) * kHeldLong;
     const int long_steps = static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(kHeldLong / 16), (longest + 15) / 16)));
 
+    if (blocks > 1) cluster_arrive();
     for (int step = 0; step < a.steps; ++step) {
         const float ca = a.coefficients[3 * step], cb = a.coefficients[3 * step + 1], cc = a.coefficients[3 * step + 2];
         // ---- the operand: rows of 64 elements in panels, wide: [l / 64][i][l % 64], tall: [i / 64][l][i % 64]
@@ -548,36 +613,57 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(ss_ + half * kHeldSide * 128, i_or_l, c + d)), "r"(w[2 * d].x), "r"(w[2 * d].y), "r"(w[2 * d + 1].x), "r"(w[2 * d + 1].y) : "memory");
             }
         } else {
-            // parts as rows of 512 bytes, whose 16-byte chunks are swizzled by the row
+            // Each block gets its share of S's rows from all, adds them up and hands the sum to all, by copies between the blocks' memories.
+            // (Rows of 512 bytes, chunks swizzled by the row. Loads from the others instead of copies took 7 us a step with eight blocks, stores to
+            // them 5.6.) The others have used what the copies overwrite: they arrived after their last product with it.
+            cluster_wait();
 #pragma unroll
             for (int c = 0; c < 16; c += 4) {
-                uint32_t r[16];
-                tmem_load16(tmem + lanes + half * 64 + c * 4, r);
+                uint32_t w[16];
+                tmem_load16(tmem + lanes + half * 64 + c * 4, w);
                 tmem_load_wait();
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ps + i_or_l * 512 + (((half * 16 + c + d) ^ (i_or_l & 7)) << 4)), "r"(r[4 * d]), "r"(r[4 * d + 1]), "r"(r[4 * d + 2]), "r"(r[4 * d + 3]) : "memory");
+                    turn_put(ps, i_or_l, half * 16 + c + d, make_float4(__uint_as_float(w[4 * d]), __uint_as_float(w[4 * d + 1]), __uint_as_float(w[4 * d + 2]), __uint_as_float(w[4 * d + 3])));
             }
-            cluster_sync();
-            const int rows = kHeldSide / blocks;  // eight columns to a thread
-            for (int e = tid; e < rows * 16; e += kHeldThreads) {
-                const int r = rank * rows + (e >> 4), c = e & 15;
+            const uint32_t share = kHeldSide / blocks;  // rows; a multiple of 16
+            smem_to_async();
+            __syncthreads();
+            if (tid == 0) {
+                mbar_expect(smem_addr(&came), (blocks - 1) * share * 512);
+                for (uint32_t d = 1; d < blocks; ++d) {
+                    const uint32_t q = (rank + d) % blocks;
+                    bulk_to_cluster(cluster_addr(qs + rank * share * 512, q), ps + q * share * 512, share * 512, cluster_addr(smem_addr(&came), q));
+                }
+            }
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&came), step & 1, &abort)) && ok;
+            for (uint32_t e = tid; e < share * 16; e += kHeldThreads) {  // eight columns to a thread
+                const uint32_t r = e >> 4, c = e & 15;
                 float v[8];
 #pragma unroll
                 for (int d = 0; d < 8; ++d) v[d] = 0.0f;
-                const uint32_t at = ps + r * 512, c0 = ((2 * c) ^ (r & 7)) << 4, c1 = ((2 * c + 1) ^ (r & 7)) << 4;
-#pragma unroll 4
+#pragma unroll 2
                 for (uint32_t q = 0; q < blocks; ++q) {  // in the order of the ranks
-                    const uint32_t there_ = cluster_addr(at, q);
-                    const float4 y = cluster_load4(there_ + c0), z = cluster_load4(there_ + c1);
+                    const uint32_t at = (q == rank ? ps : qs) + q * share * 512;
+                    const float4 y = turn_get(at, r, 2 * c), z = turn_get(at, r, 2 * c + 1);
                     v[0] += y.x, v[1] += y.y, v[2] += y.z, v[3] += y.w, v[4] += z.x, v[5] += z.y, v[6] += z.z, v[7] += z.w;
                 }
                 const uint2 lo = half4(make_float4(inverse * v[0], inverse * v[1], inverse * v[2], inverse * v[3])), hi = half4(make_float4(inverse * v[4], inverse * v[5], inverse * v[6], inverse * v[7]));
-                const uint32_t to = held_chunk(ss_ + (c >> 3) * kHeldSide * 128, r, c & 7);
-#pragma unroll 4
-                for (uint32_t q = 0; q < blocks; ++q) cluster_store4(cluster_addr(to, q), make_uint4(lo.x, lo.y, hi.x, hi.y));
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(ss_ + (c >> 3) * kHeldSide * 128, rank * share + r, c & 7)), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
             }
-            cluster_sync();
+            smem_to_async();
+            __syncthreads();
+            if (tid == 0) {
+                mbar_expect(smem_addr(&handed), (blocks - 1) * share * 256);
+                for (uint32_t d = 1; d < blocks; ++d) {
+                    const uint32_t q = (rank + d) % blocks;
+                    for (uint32_t panel = 0; panel < 2; ++panel) {
+                        const uint32_t at = ss_ + panel * kHeldSide * 128 + rank * share * 128;
+                        bulk_to_cluster(cluster_addr(at, q), at, share * 128, cluster_addr(smem_addr(&handed), q));
+                    }
+                }
+            }
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&handed), step & 1, &abort)) && ok;
         }
         // ---- Q = b S + c S S
         products([&] {
@@ -619,6 +705,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                     tc_mma_f16(tmem + 128, tc_desc_cols(qs + (k >> 2) * kHeldSide * 128 + (k & 3) * 32), tc_desc_rows(xs + k * 2048, kHeldSide * 128), idesc, k != 0);
             }
         });
+        if (blocks > 1 && step + 1 < a.steps) cluster_arrive();
 #pragma unroll
         for (int j = 0; j < 128; j += 16) {
             uint32_t r[16];
@@ -634,35 +721,33 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
     }
     // ---- out
     {
-        const int64_t at = row * a.out_stride + col;
+#pragma unroll
+        for (int c = 0; c < 32; ++c) turn_put(turn, lane, c, make_float4(x[4 * c] * a.unscale, x[4 * c + 1] * a.unscale, x[4 * c + 2] * a.unscale, x[4 * c + 3] * a.unscale));
+        __syncwarp();
+        const int64_t at = row0 * a.out_stride + col + 4 * lane;
         float* const to32 = static_cast<float*>(const_cast<void*>(a.out.p[matrix])) + at;
         uint16_t* const to16 = static_cast<uint16_t*>(const_cast<void*>(a.out.p[matrix])) + at;
         const float* const from = static_cast<const float*>(a.param.p[matrix]) + at;
+        const int n = cols - 4 * lane;
+        if (a.to == kToBf16) {
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r) store_four(to16 + r * a.out_stride, turn_get(turn, r, lane), n, a.out_vectors);
+        } else if (a.to == kToF32) {
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r) store_four(to32 + r * a.out_stride, turn_get(turn, r, lane), n, a.out_vectors);
+        } else {
+#pragma unroll 1
+            for (int r0 = 0; r0 < rows; r0 += 8) {
+                float4 p[8];
 #pragma unroll
-        for (int j = 0; j < 128; j += 8) {
-            const int n = there - j;
-            if (n <= 0) continue;
-            Eight o;
+                for (int r = 0; r < 8; ++r) p[r] = load_four(from + (r0 + r) * a.out_stride, r0 + r < rows ? n : 0, a.out_vectors);
 #pragma unroll
-            for (int d = 0; d < 8; ++d) o.v[d] = x[j + d] * a.unscale;
-            if (a.to == kToParam) {
-                const Eight p = load_eight(from + j, n, a.out_vectors);
-#pragma unroll
-                for (int d = 0; d < 8; ++d) o.v[d] = p.v[d] - a.lr * (a.scale * o.v[d] + a.decay * p.v[d]);
-            }
-            if (a.out_vectors && n >= 8) {
-                if (a.to == kToBf16) {
-                    *reinterpret_cast<uint4*>(to16 + j) = make_uint4(bf16_pair(o.v[0], o.v[1]), bf16_pair(o.v[2], o.v[3]), bf16_pair(o.v[4], o.v[5]), bf16_pair(o.v[6], o.v[7]));
-                } else {
-                    reinterpret_cast<float4*>(to32 + j)[0] = make_float4(o.v[0], o.v[1], o.v[2], o.v[3]);
-                    reinterpret_cast<float4*>(to32 + j)[1] = make_float4(o.v[4], o.v[5], o.v[6], o.v[7]);
-                }
-            } else {
-#pragma unroll
-                for (int d = 0; d < 8; ++d) {
-                    if (d >= n) continue;
-                    if (a.to == kToBf16) Elem<uint16_t>::store(to16 + j + d, o.v[d]);
-                    else to32[j + d] = o.v[d];
+                for (int r = 0; r < 8; ++r) {
+                    if (r0 + r >= rows) continue;
+                    const float4 o = turn_get(turn, r0 + r, lane);
+                    store_four(to32 + (r0 + r) * a.out_stride,
+                               make_float4(p[r].x - a.lr * (a.scale * o.x + a.decay * p[r].x), p[r].y - a.lr * (a.scale * o.y + a.decay * p[r].y),
+                                           p[r].z - a.lr * (a.scale * o.z + a.decay * p[r].z), p[r].w - a.lr * (a.scale * o.w + a.decay * p[r].w)), n, a.out_vectors);
                 }
             }
         }
