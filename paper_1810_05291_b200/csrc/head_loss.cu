@@ -129,6 +129,7 @@ __device__ __forceinline__ void store_terms(uint16_t* dst, int64_t plane, const 
 // A row to the layout of an operand: bf16 as it is, fp32 as three terms.
 template <typename T>
 __device__ __forceinline__ void stage_row(const T* src, uint16_t* dst, int64_t plane, int width, bool vectors, int lane) {
+#pragma unroll 4
     for (int c = 4 * lane; c < width; c += 128) {
         const int n = width - c;
         if constexpr (sizeof(T) == 2) {
@@ -156,6 +157,8 @@ __device__ __forceinline__ void stage_row(const T* src, uint16_t* dst, int64_t p
     }
 }
 
+constexpr int kGatherCols = 512;  // that a warp takes of a row
+
 // Rows that count gathered; behind them zeros up to a whole stage, since dW sums over whole stages; the results of the others.
 template <typename T>
 __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant__ Head a) {
@@ -164,21 +167,24 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant_
     const int lane = threadIdx.x & 31;
     const int64_t live = *a.live, padded = (live + kProdK - 1) / kProdK * kProdK, plane = a.row_cap * a.width_ld;
     const int64_t upto = padded > kProdK ? padded : kProdK;
-    for (int64_t i = blockIdx.x * 8 + (threadIdx.x >> 5); i < a.rows + kProdK; i += gridDim.x * 8) {
+    const int pieces = (a.width + kGatherCols - 1) / kGatherCols;
+    for (int64_t j = blockIdx.x * 8 + (threadIdx.x >> 5); j < (a.rows + kProdK) * pieces; j += gridDim.x * 8) {
+        const int64_t i = j / pieces;
+        const int first = static_cast<int>(j - i * pieces) * kGatherCols, n = min(kGatherCols, a.width - first);
         if (i < upto) {
-            uint16_t* const dst = a.gathered + i * a.width_ld;
+            uint16_t* const dst = a.gathered + i * a.width_ld + first;
             if (i < live) {
-                stage_row(static_cast<const T*>(a.x) + a.index[i] * a.x_stride, dst, plane, a.width, a.vectors, lane);
+                stage_row(static_cast<const T*>(a.x) + a.index[i] * a.x_stride + first, dst, plane, n, a.vectors, lane);
             } else {
                 for (int q = 0; q < (sizeof(T) == 4 ? kTerms : 1); ++q)
-                    for (int c = lane; c < a.width; c += 32) dst[q * plane + c] = 0;
+                    for (int c = lane; c < n; c += 32) dst[q * plane + c] = 0;
             }
         }
         if (i < a.rows && !counts(a, i)) {
             if (lane == 0) a.logp[i] = 0.0f;
             if (a.dx != nullptr) {
-                T* const dst = static_cast<T*>(a.dx) + i * a.dx_stride;
-                for (int c = lane; c < a.width; c += 32) dst[c] = T(0);
+                T* const dst = static_cast<T*>(a.dx) + i * a.dx_stride + first;
+                for (int c = lane; c < n; c += 32) dst[c] = T(0);
             }
         }
     }
@@ -205,7 +211,7 @@ __device__ __forceinline__ uint4 half8(const float* v) {
 
 // ---- the end of the logits' product
 struct Logits {
-    static constexpr bool kWhole = true, kSmall = false;
+    static constexpr bool kWhole = true, kSmall = false, kAlone = true, kPacks = false;
     const int* target;  // of the chunk's rows
     float* target_logit;
     float2* parts;
@@ -281,10 +287,12 @@ __global__ void __launch_bounds__(256) head_statistics_kernel(const __grid_const
     for (int64_t r = blockIdx.x * 8 + (threadIdx.x >> 5); r < here; r += gridDim.x * 8) {
         const float2* const p = a.parts + r * a.n_parts;
         float top = -INFINITY, sum = 0.0f;
+#pragma unroll 8
         for (int i = lane; i < a.n_parts; i += 32) top = fmaxf(top, p[i].x);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
         const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll 8
         for (int i = lane; i < a.n_parts; i += 32) {
             const float2 v = p[i];
             sum += v.y * ex2((v.x - from) * a.k);
@@ -311,14 +319,45 @@ __global__ void __launch_bounds__(256) head_statistics_kernel(const __grid_const
     }
 }
 
+// Loss and sum of weighted squares: fp64, in a fixed order, by the first 256 threads of a block.
+__device__ __forceinline__ void totals_of(const Head& a, int64_t live) {
+    __shared__ double part[2][8];
+    double loss = 0.0, square = 0.0;
+#pragma unroll 4
+    for (int64_t s = threadIdx.x; s < live; s += 256) loss += a.loss[s], square += a.square[s];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        loss += __shfl_xor_sync(0xFFFFFFFFu, loss, d);
+        square += __shfl_xor_sync(0xFFFFFFFFu, square, d);
+    }
+    if ((threadIdx.x & 31) == 0) part[0][threadIdx.x >> 5] = loss, part[1][threadIdx.x >> 5] = square;
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        double v = 0.0;
+        for (int i = 0; i < 8; ++i) v += part[threadIdx.x][i];
+        a.totals[threadIdx.x] = static_cast<float>(v);
+    }
+}
+
+// Where no gradient follows; none: no rows.
+__global__ void __launch_bounds__(256) head_totals_kernel(const __grid_constant__ Head a, int none) {
+    next_may_begin();
+    if (!none) after_previous();
+    totals_of(a, none ? 0 : *a.live);
+}
+
 // e -> P: four times eight columns to a thread, all loads before the first store. Rows behind the last up to a whole stage
-// become zeros.
+// become zeros. A row of blocks behind all rows, where the call's last chunk has it, forms the totals.
 constexpr int kGradientPieces = 4;
 
 template <bool F32>
 __global__ void __launch_bounds__(256) head_gradient_kernel(const __grid_constant__ Head a) {
     next_may_begin();
     after_previous();
+    if (blockIdx.y == a.chunk_rows) {
+        if (blockIdx.x == 0) totals_of(a, *a.live);
+        return;
+    }
     const int64_t r = blockIdx.y, here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
     const int64_t upto = max((here + kProdK - 1) / kProdK * kProdK, static_cast<int64_t>(a.first == 0 ? kProdK : 0));
     const int c0 = blockIdx.x * (256 * 8 * kGradientPieces) + threadIdx.x * 8, end = static_cast<int>(a.e_ld);
@@ -392,7 +431,7 @@ __device__ __forceinline__ void add_global(float* p, float v) {
     asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(__cvta_generic_to_global(p)), "f"(v) : "memory");
 }
 
-constexpr int kTileFloats = kProdTile * kProdTile;
+constexpr int kTileFloats = kProdTile * kProdTile;  // of a pair's part; a block's alone is half of that, and there are twice as many
 
 // Where a gradient goes: fp32, or bf16 that takes the sums of earlier rows (fp32) into its rounding.
 struct Dest {
@@ -401,6 +440,7 @@ struct Dest {
     const float* before;  // with bf16: those sums, or NULL
     int64_t stride, before_stride;
     int cols, vectors, add;
+    int wide;  // bf16: rows start on 16 bytes
 
     __device__ __forceinline__ void put(int64_t row, int c, float4 v, float4 b, bool adds) const {
         const int64_t at = row * stride + c;
@@ -428,12 +468,13 @@ struct Dest {
 // OUT16: to.bf16, else to.f32. BEFORE: with to.before.
 template <bool OUT16, bool BEFORE>
 struct Gradient {
-    static constexpr bool kWhole = false, kSmall = false;
+    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE;
     struct Fetched {
         float4 before[BEFORE ? 8 : 1];
     };
     Dest to;
     float* partial;
+    int part_floats;
 
     struct Tile {
         char* p;       // this lane's first row, at its first column
@@ -441,13 +482,19 @@ struct Gradient {
         const float* before;
         int row, col, rows, cols;  // rows and columns: that exist from there on
         int part;
-        bool add;
+        bool add, packs;
 
+        __device__ __forceinline__ static uint32_t pack(uint32_t a, uint32_t b) { return bf16_pair(__uint_as_float(a), __uint_as_float(b)); }
+        __device__ __forceinline__ void packed(int j, int lane, uint32_t buf) const {
+            char* q = p + (j + 4 * (lane & 7)) * 2;  // p is at four columns a lane, this at eight
+#pragma unroll
+            for (int i = 0; i < 8; ++i, q += step) *reinterpret_cast<uint4*>(q) = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+        }
         __device__ __forceinline__ Tile(const Gradient& e, const ProdUnit& u, int m, int row0, int col0, int lane) {
             row = row0 + (lane >> 3), col = col0 + 4 * (lane & 7), part = u.part, add = e.to.add;
             rows = m - row, cols = e.to.cols - col;
             if (part >= 0) {
-                p = reinterpret_cast<char*>(e.partial + static_cast<int64_t>(part) * kTileFloats + (row - u.m0) * kProdTile + (col - u.n0));
+                p = reinterpret_cast<char*>(e.partial + static_cast<int64_t>(part) * e.part_floats + (row - u.m0) * kProdTile + (col - u.n0));
                 step = 4 * kProdTile * 4;
                 add = false;
             } else {
@@ -455,6 +502,7 @@ struct Gradient {
                 p = OUT16 ? reinterpret_cast<char*>(e.to.bf16 + at) : reinterpret_cast<char*>(e.to.f32 + at);
                 step = 4 * e.to.stride * (OUT16 ? 2 : 4);
             }
+            packs = OUT16 && part < 0 && e.to.wide && row0 + 32 <= m && col0 + kProdHalf <= e.to.cols;
             before = BEFORE ? e.to.before + row * e.to.before_stride + col : nullptr;
         }
         __device__ __forceinline__ void fetch(const Gradient& e, int j, Fetched& f) const {
@@ -484,17 +532,17 @@ struct Gradient {
     };
 };
 
-// Four columns of a tile that came in parts, the parts in their order, four under way at a time.
-__device__ __forceinline__ float4 joined(const float* partial, const Schedule& sc, int other, int r, int c) {
-    const float* const p = partial + static_cast<int64_t>(other) * sc.parts * kTileFloats + r * kProdTile + c;
+// Four columns of a tile that came in parts, the parts in their order, eight under way at a time.
+__device__ __forceinline__ float4 joined(const float* partial, const Schedule& sc, int tile_floats, int other, int r, int c) {
+    const float* const p = partial + static_cast<int64_t>(other) * sc.parts * tile_floats + r * kProdTile + c;
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s = 0; s < sc.parts; s += 4) {
-        float4 x[4];
+    for (int s = 0; s < sc.parts; s += 8) {
+        float4 x[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            x[u] = s + u < sc.parts ? __ldcs(reinterpret_cast<const float4*>(p + static_cast<int64_t>(s + u) * kTileFloats)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int u = 0; u < 8; ++u)
+            x[u] = s + u < sc.parts ? __ldcs(reinterpret_cast<const float4*>(p + static_cast<int64_t>(s + u) * tile_floats)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v.x += x[u].x, v.y += x[u].y, v.z += x[u].z, v.w += x[u].w;
+        for (int u = 0; u < 8; ++u) v.x += x[u].x, v.y += x[u].y, v.z += x[u].z, v.w += x[u].w;
     }
     return v;
 }
@@ -508,7 +556,7 @@ __global__ void __launch_bounds__(256) head_join_kernel(const __grid_constant__ 
     for (int other = blockIdx.x; other < others; other += gridDim.x) {
         const ProdUnit u = prod_unit(p, sc, sc.whole + other * sc.parts);
         const int r = u.m0 + i / kProdTile, c = u.n0 + i % kProdTile;
-        if (r < sc.m && c < p.n) to.put(r, c, joined(partial, sc, other, i / kProdTile, i % kProdTile), to.earlier(r, c), to.add);
+        if (r < sc.m && c < p.n) to.put(r, c, joined(partial, sc, kTileFloats, other, i / kProdTile, i % kProdTile), to.earlier(r, c), to.add);
     }
 }
 
@@ -520,22 +568,23 @@ __global__ void __launch_bounds__(256) head_dx_kernel(const __grid_constant__ He
     const int lane = threadIdx.x & 31;
     const Schedule sc = schedule_of(p);
     const int64_t here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
-    for (int64_t r = blockIdx.x * 8 + (threadIdx.x >> 5); r < here; r += gridDim.x * 8) {
-        const float* const src = a.acc + r * a.width_ld;
-        T* const dst = static_cast<T*>(a.dx) + a.index[a.first + r] * a.dx_stride;
-        for (int c = 4 * lane; c < a.width; c += 128) {
-            const int tile = c / kProdTile * sc.tiles_m + static_cast<int>(r / kProdTile);
-            const float4 v = tile < sc.whole ? *reinterpret_cast<const float4*>(src + c)
-                                             : joined(a.partial, sc, tile - sc.whole, static_cast<int>(r % kProdTile), c % kProdTile);
-            if (a.dx_vectors && c + 4 <= a.width) {
-                if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst + c) = v;
-                else *reinterpret_cast<uint2*>(dst + c) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
-            } else {
-                const float e[4] = {v.x, v.y, v.z, v.w};
+    const int pieces = (a.width + 127) / 128;  // a warp takes 128 columns of a row
+    for (int64_t i = blockIdx.x * 8 + (threadIdx.x >> 5); i < here * pieces; i += gridDim.x * 8) {
+        const int64_t r = i / pieces;
+        const int c = static_cast<int>(i - r * pieces) * 128 + 4 * lane;
+        if (c >= a.width) continue;
+        T* const dst = static_cast<T*>(a.dx) + a.index[a.first + r] * a.dx_stride + c;
+        const int tile = c / kProdTile * sc.tiles_m + static_cast<int>(r / p.tile_m);
+        const float4 v = tile < sc.whole ? *reinterpret_cast<const float4*>(a.acc + r * a.width_ld + c)
+                                         : joined(a.partial, sc, p.tile_m * kProdTile, tile - sc.whole, static_cast<int>(r % p.tile_m), c % kProdTile);
+        if (a.dx_vectors && c + 4 <= a.width) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = v;
+            else *reinterpret_cast<uint2*>(dst) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+        } else {
+            const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (c + j < a.width) Elem<T>::store(dst + c + j, e[j]);
-            }
+            for (int j = 0; j < 4; ++j)
+                if (c + j < a.width) Elem<T>::store(dst + j, e[j]);
         }
     }
 }
@@ -544,28 +593,6 @@ __global__ void __launch_bounds__(256) head_zero_kernel(void* dst, int64_t row_b
     next_may_begin();
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
         for (int64_t c = threadIdx.x * 2; c < row_bytes; c += 512) *reinterpret_cast<uint16_t*>(static_cast<char*>(dst) + r * stride_bytes + c) = 0;
-}
-
-// Loss and sum of weighted squares: fp64, in a fixed order.
-__global__ void __launch_bounds__(1024) head_totals_kernel(const __grid_constant__ Head a, int none) {
-    next_may_begin();
-    if (!none) after_previous();
-    __shared__ double part[2][32];
-    const int64_t live = none ? 0 : *a.live;
-    double loss = 0.0, square = 0.0;
-    for (int64_t s = threadIdx.x; s < live; s += 1024) loss += a.loss[s], square += a.square[s];
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        loss += __shfl_xor_sync(0xFFFFFFFFu, loss, d);
-        square += __shfl_xor_sync(0xFFFFFFFFu, square, d);
-    }
-    if ((threadIdx.x & 31) == 0) part[0][threadIdx.x >> 5] = loss, part[1][threadIdx.x >> 5] = square;
-    __syncthreads();
-    if (threadIdx.x < 2) {
-        double v = 0.0;
-        for (int i = 0; i < 32; ++i) v += part[threadIdx.x][i];
-        a.totals[threadIdx.x] = static_cast<float>(v);
-    }
 }
 
 // ---- host side -------------------------------------------------------------------------------------
@@ -638,7 +665,7 @@ bool may_split(const Product& p) {
     return others > 0 && p.pairs / others > 1 && stages / kLeastPart > 1;
 }
 
-int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_dtype dw_dt, bool dw_vectors, int accumulate, cudaStream_t st) {
+int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_dtype dw_dt, bool dw_vectors, bool dw_wide, int accumulate, cudaStream_t st) {
     cudaError_t e = cudaSuccess;
     const int sms = device_sm_count(&e);
     if (e != cudaSuccess) return cuda_status_public(e);
@@ -662,8 +689,8 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
     if (status != SS_OK) return status;
 
     e = launch_next(false, head_rows_kernel, 1, 1024, st, a);
-    if (e == cudaSuccess) e = l.f32 ? launch_next(true, head_gather_kernel<float>, blocks_for(rows + kProdK, sms), 256, st, a)
-                                    : launch_next(true, head_gather_kernel<uint16_t>, blocks_for(rows + kProdK, sms), 256, st, a);
+    if (e == cudaSuccess) e = l.f32 ? launch_next(true, head_gather_kernel<float>, blocks_for((rows + kProdK) * ((width + kGatherCols - 1) / kGatherCols), sms), 256, st, a)
+                                    : launch_next(true, head_gather_kernel<uint16_t>, blocks_for((rows + kProdK) * ((width + kGatherCols - 1) / kGatherCols), sms), 256, st, a);
     if (e == cudaSuccess && l.stage_w) e = l.f32 ? launch_next(true, head_stage_w_kernel<float>, blocks_for(vocab, sms), 256, st, a)
                                                  : launch_next(true, head_stage_w_kernel<uint16_t>, blocks_for(vocab, sms), 256, st, a);
     if (e != cudaSuccess) return cuda_status_public(e);
@@ -680,8 +707,9 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         if (status == SS_OK && l.dw) status = map_operand(&p_rows, a.p16, true, vocab, l.chunk_rows, p_row, l.planes, p_plane, true);
         if (status != SS_OK) return status;
 
-        Product pz = product_of(l.chunk_rows, vocab, width, l.f32, sms);
+        Product pz = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, vocab, width, l.f32, sms);
         pz.chunk = kLogitChunk, pz.m_fast = 1, pz.follows = 1, pz.live = a.live, pz.live_from = a.first, pz.live_side = 1;
+        alone(pz, sms);
         const Logits ez{a.target + first, a.target_logit, a.parts, grads && !l.f32 ? a.e16 : nullptr, grads && l.f32 ? a.e32 : nullptr,
                         l.e_ld, a.n_parts, a.vocab, a.k};
         status = launch_product<Logits, false, false>(x_cols, w_cols, pz, ez, st);
@@ -690,25 +718,26 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         if (e != cudaSuccess) return cuda_status_public(e);
         if (!grads) continue;
         const int64_t wide = 256 * 8 * kGradientPieces;
-        const dim3 grid(static_cast<unsigned>((l.e_ld + wide - 1) / wide), static_cast<unsigned>(l.chunk_rows));
+        const dim3 grid(static_cast<unsigned>((l.e_ld + wide - 1) / wide), static_cast<unsigned>(l.chunk_rows + (i + 1 == l.chunks)));
         e = l.f32 ? launch_next(true, head_gradient_kernel<true>, grid, 256, st, a) : launch_next(true, head_gradient_kernel<false>, grid, 256, st, a);
         if (e != cudaSuccess) return cuda_status_public(e);
         if (l.dx) {
-            Product px = product_of(l.chunk_rows, width, vocab, l.f32, sms);
+            Product px = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, width, vocab, l.f32, sms);
             px.chunk = l.f32 ? kGradChunkF32 : kGradChunk, px.m_fast = 1, px.follows = 1, px.live = a.live, px.live_from = a.first, px.live_side = 1;
             px.split = 1;
-            const Gradient<false, false> ex{{a.acc, nullptr, nullptr, l.width_ld, 0, a.width, 1, 0}, a.partial};
+            alone(px, sms);
+            const Gradient<false, false> ex{{a.acc, nullptr, nullptr, l.width_ld, 0, a.width, 1, 0, 0}, a.partial, px.tile_m * kProdTile};
             status = launch_product<Gradient<false, false>, false, true>(p_cols, w_rows, px, ex, st);
             if (status != SS_OK) return status;
-            e = l.f32 ? launch_next(true, head_dx_kernel<float>, blocks_for(l.chunk_rows, sms), 256, st, a, px)
-                      : launch_next(true, head_dx_kernel<uint16_t>, blocks_for(l.chunk_rows, sms), 256, st, a, px);
+            e = l.f32 ? launch_next(true, head_dx_kernel<float>, blocks_for(px.m * ((width + 127) / 128), sms), 256, st, a, px)
+                      : launch_next(true, head_dx_kernel<uint16_t>, blocks_for(px.m * ((width + 127) / 128), sms), 256, st, a, px);
             if (e != cudaSuccess) return cuda_status_public(e);
         }
         if (l.dw) {
             Product pw = product_of(vocab, width, l.chunk_rows, l.f32, sms);
             pw.follows = 1, pw.live = a.live, pw.live_from = a.first, pw.live_side = 2, pw.split = 1;
             Dest to{};
-            to.cols = a.width, to.add = accumulate || i > 0, to.stride = dw_stride, to.vectors = dw_vectors;
+            to.cols = a.width, to.add = accumulate || i > 0, to.stride = dw_stride, to.vectors = dw_vectors, to.wide = dw_wide;
             float* const sums = l.sums_w ? reinterpret_cast<float*>(ws + l.w32) : nullptr;
             if (l.sums_w && i + 1 < l.chunks) {
                 to.f32 = sums, to.stride = l.width_ld, to.vectors = 1;
@@ -719,9 +748,9 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
             }
             // a bf16 result is written once: its rows, at most kMostChunkRows, are one chunk
             pw.chunk = l.f32 ? kGradChunkF32 : kGradChunk;
-            if (to.bf16 == nullptr) status = launch_product<Gradient<false, false>, true, true>(p_rows, x_rows, pw, Gradient<false, false>{to, a.partial}, st);
-            else if (to.before == nullptr) status = launch_product<Gradient<true, false>, true, true>(p_rows, x_rows, pw, Gradient<true, false>{to, a.partial}, st);
-            else status = launch_product<Gradient<true, true>, true, true>(p_rows, x_rows, pw, Gradient<true, true>{to, a.partial}, st);
+            if (to.bf16 == nullptr) status = launch_product<Gradient<false, false>, true, true>(p_rows, x_rows, pw, Gradient<false, false>{to, a.partial, kTileFloats}, st);
+            else if (to.before == nullptr) status = launch_product<Gradient<true, false>, true, true>(p_rows, x_rows, pw, Gradient<true, false>{to, a.partial, kTileFloats}, st);
+            else status = launch_product<Gradient<true, true>, true, true>(p_rows, x_rows, pw, Gradient<true, true>{to, a.partial, kTileFloats}, st);
             if (status != SS_OK) return status;
             if (may_split(pw)) {
                 e = launch_next(true, head_join_kernel, dim3(static_cast<unsigned>(sms / 2), kTileFloats / 1024), 256, st, pw, to, static_cast<const float*>(a.partial));
@@ -729,7 +758,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
             }
         }
     }
-    return cuda_status_public(launch_next(true, head_totals_kernel, 1, 1024, st, a, 0));
+    return grads ? SS_OK : cuda_status_public(launch_next(true, head_totals_kernel, 1, 256, st, a, 0));
 }
 
 }  // namespace
@@ -781,7 +810,7 @@ int ss_linear_cross_entropy(const void* x, int64_t x_stride, const void* w, int6
     Head a{};
     a.targets = targets, a.weights = weights, a.grad_scale = grad_scale, a.totals = totals, a.logp = logp;
     if (rows == 0) {
-        cudaError_t e = launch_next(false, head_totals_kernel, 1, 1024, st, a, 1);
+        cudaError_t e = launch_next(false, head_totals_kernel, 1, 256, st, a, 1);
         if (e == cudaSuccess && dw != nullptr && any_w && !accumulate)
             e = launch_next(false, head_zero_kernel, static_cast<unsigned>(vocab < 4096 ? vocab : 4096), 256, st, dw, static_cast<int64_t>(width * web),
                             static_cast<int64_t>(mdw.stride * web), vocab);
@@ -800,7 +829,7 @@ int ss_linear_cross_entropy(const void* x, int64_t x_stride, const void* w, int6
     a.width = static_cast<int>(width), a.vocab = static_cast<int>(vocab);
     a.vectors = mx.row_aligned(4 * eb), a.w_vectors = mw.row_aligned(4 * eb), a.dx_vectors = mdx.row_aligned(4 * eb);
     a.c = inv_temperature, a.k = inv_temperature * 1.44269504f, a.z_coef = z_coef;
-    return run(a, l, static_cast<uint8_t*>(workspace), dw, mdw.stride, dw_dt, mdw.row_aligned(4 * web), accumulate, st);
+    return run(a, l, static_cast<uint8_t*>(workspace), dw, mdw.stride, dw_dt, mdw.row_aligned(4 * web), mdw.row_aligned(16), accumulate, st);
 }
 
 #pragma GCC visibility pop

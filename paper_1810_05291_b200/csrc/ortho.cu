@@ -44,7 +44,7 @@ __device__ __forceinline__ void split4(float4 v, uint2* hi, uint2* lo) {
 // out = c sums (+ b lin), symmetric: a square of a tile above the diagonal is stored a second time, mirrored.
 template <bool LIN>
 struct Symmetric {
-    static constexpr bool kWhole = false, kSmall = true;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false;
     static constexpr int kSmallBlocks = 2;
     struct Fetched {
         uint2 lin[LIN ? 8 : 1];
@@ -116,7 +116,7 @@ __device__ __forceinline__ float4 next_of(float a, float4 sums, uint2 hi, uint2 
 }
 
 struct Next {
-    static constexpr bool kWhole = false, kSmall = true;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false;
     static constexpr int kSmallBlocks = 2;
     struct Fetched {
         uint2 hi[8], lo[8];
@@ -161,7 +161,7 @@ enum { kToF32, kToBf16, kToParam };
 // The last step's result, to the caller: O, or the parameter moved by it.
 template <int TO>
 struct Result {
-    static constexpr bool kWhole = false, kSmall = true;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false;
     static constexpr int kSmallBlocks = TO == kToParam ? 1 : 2;
     struct Fetched {
         uint2 hi[8], lo[8];
@@ -889,7 +889,7 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     Product px = product_of(c.rows, c.cols, l.side, false, sms);
     for (Product* p : {&ps, &pq, &px}) p->batches = c.count, p->bf16 = 0, p->follows = 1, p->m_fast = 1;
     ps.upper = pq.upper = 1;
-    for (Product* p : {&ps, &pq, &px}) p->small = small_blocks(*p, sms);
+    for (Product* p : {&ps, &pq, &px}) choose_small(p, sms);
     for (int k = 0; k < c.steps; ++k) {
         const float *const co = c.coefficients + 3 * k;
         const int from = k & 1;

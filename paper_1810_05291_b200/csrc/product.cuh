@@ -2,7 +2,7 @@
 // of each tile: the core that the loss at the head and the orthogonal update share.
 //
 // Two blocks on neighbouring SMs form a 256 x 256 tile: each copies and keeps 128 of its rows of A, 128
-// of its rows of B, and the sums of its 128 rows. One warp copies stages of 64 contraction indices by TMA, one
+// of its rows of B, and the sums of its 128 rows. (Where C has no more than 128 rows, blocks form 128 x 256 tiles each alone, with all rows of B.) One warp copies stages of 64 contraction indices by TMA, one
 // issues the matrix instructions, eight bring the sums out of the tensor memory, whose other half the matrix
 // unit fills meanwhile. An operand may lie in memory with its contraction index fast or slow (XMN); the
 // tiles are swizzled by the copies either way, and nothing is transposed.
@@ -25,7 +25,13 @@ constexpr uint32_t kProdOperand = kProdHalf * kProdK * 2, kProdStageBytes = 2 * 
 constexpr uint32_t kProdPanel = kProdK * 128;              // 64 elements of an operand whose contraction index is slow
 constexpr int kProdOut = 256, kProdThreads = kProdOut + 64;  // warps 0-7 bring out, 8 copies, 9 issues
 constexpr uint32_t kProdSquare = 32 * 32 * 4;              // an outgoing warp's own shared memory
-constexpr size_t kProdSmem = 1024 + kProdStages * kProdStageBytes + kProdOut / 32 * kProdSquare;
+// Of a pair's block, and of a block alone, which has all 256 rows of B: stages and their bytes.
+template <bool PAIR>
+struct Stage {
+    static constexpr int kCount = PAIR ? kProdStages : 4;
+    static constexpr uint32_t kBytes = PAIR ? 2 * kProdOperand : 3 * kProdOperand;
+    static constexpr size_t kSmem = 1024 + kCount * kBytes + kProdOut / 32 * kProdSquare;
+};
 
 constexpr int kTerms = 3, kMostPasses = 6;
 
@@ -35,11 +41,13 @@ struct Product {
     int passes;       // pairs of planes: (plane_a[i], plane_b[i])
     int8_t plane_a[kMostPasses], plane_b[kMostPasses];
     int chunk;        // stages that are summed in tensor memory before they are brought out
-    int pairs;        // of blocks
+    int tile_m;       // rows of a tile: 256 for pairs, 128 for blocks alone
+    int pairs;        // of blocks, or blocks alone
     int split;        // whether the contraction of tiles that do not fill a round of pairs may be cut into parts
     int m_fast;       // the order of tiles: neighbours share columns of C, or rows
     int upper;        // m == n: only tiles on the diagonal and above
     int small;        // blocks that share a 128 x 128 tile (1, 2, 4), or 0: pairs on 256 x 256 tiles
+    int ring;         // with small: stages under way, kSmallStages or kMostSmallStages
     int bf16;         // operands: bf16 or fp16
     int follows;      // another kernel of the call goes before
     const int* live;  // rows that there are (all of the call's), or NULL
@@ -49,7 +57,7 @@ struct Product {
 
 inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms, int sms) {
     Product p{};
-    p.pairs = sms / 2;
+    p.tile_m = kProdTile, p.pairs = sms / 2;
     p.m = static_cast<int>(m), p.n = static_cast<int>(n), p.k = static_cast<int>(k);
     p.batches = 1, p.passes = 1, p.chunk = 1 << 30, p.bf16 = 1;
     if (terms) {
@@ -62,6 +70,11 @@ inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms, int sms) 
 
 // The pairs of blocks take whole tiles as long as every pair gets one; the contraction of the tiles that are left over (all, if
 // there are fewer than pairs) is cut into parts, so that they too keep most pairs busy. Parts are joined afterwards, in their order.
+// C of at most 128 rows: blocks alone.
+inline void alone(Product& p, int sms) {
+    if (p.m <= kProdHalf) p.tile_m = kProdHalf, p.pairs = sms;
+}
+
 struct Schedule {
     int m, tiles_m, tiles_n, per_batch;
     int pass_stages, stages;          // of one pass; of all
@@ -80,7 +93,7 @@ __device__ __forceinline__ Schedule schedule_of(const Product& p) {
         else k = max(min(k, live), 1);
     }
     s.m = m;
-    s.tiles_m = (m + kProdTile - 1) / kProdTile;
+    s.tiles_m = (m + p.tile_m - 1) / p.tile_m;
     s.tiles_n = (p.n + kProdTile - 1) / kProdTile;
     s.per_batch = p.upper ? s.tiles_m * (s.tiles_m + 1) / 2 : s.tiles_m * s.tiles_n;
     s.pass_stages = (k + kProdK - 1) / kProdK;
@@ -125,7 +138,7 @@ __device__ __forceinline__ ProdUnit prod_unit(const Product& p, const Schedule& 
     } else {
         i = t / s.tiles_n, j = t - i * s.tiles_n;
     }
-    r.m0 = i * kProdTile, r.n0 = j * kProdTile;
+    r.m0 = i * p.tile_m, r.n0 = j * kProdTile;
     return r;
 }
 
@@ -171,12 +184,17 @@ __device__ __forceinline__ void square_sums(uint32_t buf, int lane, float4 (&v)[
 
 constexpr uint32_t kNanBits = 0x7FC00000u;
 
+template <class TILE>
+__device__ __forceinline__ auto packs(const TILE& t) -> decltype(t.packs) { return t.packs; }
+__device__ __forceinline__ bool packs(...) { return false; }
+
 // EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
 // registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
-// square(column, ..., its sums, first chunk?). EPI::kSmall: it also ends the small products below.
+// square(column, ..., its sums, first chunk?). With EPI::kPacks a tile may take 64 columns at a time, rounded to 16 bits:
+// packed(column, ...). EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
-template <class EPI, bool A_MN, bool B_MN>
+template <class EPI, bool A_MN, bool B_MN, bool PAIR>
 __global__ void __launch_bounds__(kProdThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ Product p,
                const __grid_constant__ EPI epi) {
@@ -184,30 +202,35 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
     __shared__ ProdShared sh;
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int pair = blockIdx.x >> 1, pairs = p.pairs;
+    constexpr int kStages = Stage<PAIR>::kCount;
+    constexpr uint32_t kStageBytes = Stage<PAIR>::kBytes;
+    const int pair = PAIR ? blockIdx.x >> 1 : blockIdx.x, pairs = p.pairs;
     volatile int* abort = &sh.abort;
-    uint32_t rank;  // in the pair; the first block issues the matrix instructions and waits for both blocks' operands
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    uint32_t rank = 0;  // in the pair; the first block issues the matrix instructions and waits for both blocks' operands
+    if constexpr (PAIR) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
 
     next_may_begin();
     if (tid == 0) {
-        for (int s = 0; s < kProdStages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_addr(&sh.full[s]), 1);
             mbar_init(smem_addr(&sh.empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_addr(&sh.summed[b]), 1);
-            mbar_init(smem_addr(&sh.added[b]), 2 * kProdOut / 32);
+            mbar_init(smem_addr(&sh.added[b]), (PAIR ? 2 : 1) * kProdOut / 32);
         }
         mbar_init(smem_addr(&sh.last), 1);
         sh.abort = 0;
         mbar_init_visible();
     }
-    if (warp == 0) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
+    if (warp == 0) {
+        if constexpr (PAIR) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
+        else tmem_alloc(smem_addr(&sh.tmem), 512);
+    }
     tc_fence_before();
     __syncthreads();
     if (p.follows) after_previous();
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    if constexpr (PAIR) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     const Schedule sc = schedule_of(p);
@@ -215,9 +238,13 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
     if (warp < kProdOut / 32) {
         // ---- sums out: 32 rows and half of the columns to a warp
         const int row_local = rank * kProdHalf + (warp & 3) * 32, col_local = (warp >> 2) * kProdHalf;
-        const uint32_t buf = stages + kProdStages * kProdStageBytes + warp * kProdSquare;
+        const uint32_t buf = stages + kStages * kStageBytes + warp * kProdSquare;
         const uint32_t tmem_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + col_local;
-        const uint32_t added = cluster_addr(smem_addr(&sh.added[0]), 0);
+        const uint32_t added = PAIR ? cluster_addr(smem_addr(&sh.added[0]), 0) : smem_addr(&sh.added[0]);
+        auto arrive = [](uint32_t bar) {
+            if constexpr (PAIR) mbar_arrive_pair(bar);
+            else mbar_arrive(bar);
+        };
         uint32_t chunk = 0;
         bool ok = true;
         for (int unit = pair; unit < sc.units; unit += pairs) {
@@ -241,7 +268,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_pair(added + (chunk & 1) * 8);
+                    if (lane == 0) arrive(added + (chunk & 1) * 8);
                 }
                 if (!ok) {
 #pragma unroll
@@ -258,8 +285,28 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                     tc_fence_after();
                     const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
+                    if constexpr (EPI::kPacks) {
+                        if (tile.packs && ok) {
 #pragma unroll 1
-                    for (int j = 0; any && j < kProdHalf && col + j < p.n; j += 32) {
+                            for (int j = 0; j < kProdHalf; j += 64) {
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    uint32_t r[32];
+                                    tmem_load32(src + j + 32 * h, r);
+                                    tmem_load_wait();
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+                                        square_set(buf, lane, 4 * h + i, make_uint4(tile.pack(r[8 * i], r[8 * i + 1]), tile.pack(r[8 * i + 2], r[8 * i + 3]),
+                                                                                    tile.pack(r[8 * i + 4], r[8 * i + 5]), tile.pack(r[8 * i + 6], r[8 * i + 7])));
+                                }
+                                __syncwarp();
+                                tile.packed(j, lane, buf);
+                                __syncwarp();
+                            }
+                        }
+                    }
+#pragma unroll 1
+                    for (int j = EPI::kPacks && packs(tile) && ok ? kProdHalf : 0; any && j < kProdHalf && col + j < p.n; j += 32) {
                         if (j > 0) tile.fetch(epi, j, f);
                         uint32_t r[32];
                         tmem_load32(src + j, r);
@@ -277,7 +324,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_pair(added + (chunk & 1) * 8);
+                    if (lane == 0) arrive(added + (chunk & 1) * 8);
                     first = false;
                 }
             }
@@ -286,56 +333,68 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         // Roles of one lane each, but the whole warp walks through them, so that addresses and descriptors are formed
         // in uniform registers.
         // ---- copies: this block's halves, counted by the first block's barrier
-        const uint32_t full = cluster_addr(smem_addr(&sh.full[0]), 0), empty = smem_addr(&sh.empty[0]);
+        const uint32_t full = PAIR ? cluster_addr(smem_addr(&sh.full[0]), 0) : smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
+        auto load = [](uint32_t dst, const void* map, uint32_t bar, int x, int y, int z) {
+            if constexpr (PAIR) tma_load_3d_pair(dst, map, bar, x, y, z);
+            else tma_load_3d(dst, map, bar, x, y, z);
+        };
         const bool leader = elect_one();
         int it = 0, slot = 0;
         uint32_t parity = 1;
         for (int unit = pair; unit < sc.units; unit += pairs) {
             const ProdUnit u = prod_unit(p, sc, unit);
-            const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + rank * kProdHalf;
+            const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + rank * kProdHalf;  // PAIR: this block's half of both
             int pass = u.first / sc.pass_stages, k0 = (u.first - pass * sc.pass_stages) * kProdK;
             const int end = sc.pass_stages * kProdK;
 #pragma unroll 1
             for (int s = 0; s < u.stages; ++s) {
                 mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
-                const uint32_t bar = full + slot * 8, dst = stages + slot * kProdStageBytes;
+                const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
                 const int za = p.passes > 1 ? p.plane_a[pass] : u.batch, zb = p.passes > 1 ? p.plane_b[pass] : u.batch;
                 if (leader) {
-                    if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, 2 * kProdStageBytes);
+                    if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, (PAIR ? 2 : 1) * kStageBytes);
                     if constexpr (A_MN) {
-                        tma_load_3d_pair(dst, &a_map, bar, m0, k0, za);
-                        tma_load_3d_pair(dst + kProdPanel, &a_map, bar, m0 + 64, k0, za);
+                        load(dst, &a_map, bar, m0, k0, za);
+                        load(dst + kProdPanel, &a_map, bar, m0 + 64, k0, za);
                     } else {
-                        tma_load_3d_pair(dst, &a_map, bar, k0, m0, za);
+                        load(dst, &a_map, bar, k0, m0, za);
                     }
-                    if constexpr (B_MN) {
-                        tma_load_3d_pair(dst + kProdOperand, &b_map, bar, n0, k0, zb);
-                        tma_load_3d_pair(dst + kProdOperand + kProdPanel, &b_map, bar, n0 + 64, k0, zb);
-                    } else {
-                        tma_load_3d_pair(dst + kProdOperand, &b_map, bar, k0, n0, zb);
+#pragma unroll
+                    for (int h = 0; h < (PAIR ? 1 : 2); ++h) {
+                        const uint32_t to = dst + (1 + h) * kProdOperand;
+                        if constexpr (B_MN) {
+                            load(to, &b_map, bar, n0 + h * kProdHalf, k0, zb);
+                            load(to + kProdPanel, &b_map, bar, n0 + h * kProdHalf + 64, k0, zb);
+                        } else {
+                            load(to, &b_map, bar, k0, n0 + h * kProdHalf, zb);
+                        }
                     }
                 }
                 ++it;
                 k0 += kProdK;
                 if (k0 == end) k0 = 0, ++pass;
-                if (++slot == kProdStages) slot = 0, parity ^= 1;
+                if (++slot == kStages) slot = 0, parity ^= 1;
             }
         }
         // the last signals, and copies, arrive in this block's memory: not before that
-        const int from = it > kProdStages ? it - kProdStages : 0;
-        for (int i = from; i < it; ++i) mbar_wait_uniform(empty + i % kProdStages * 8, (i / kProdStages) & 1, &sh.abort);
+        const int from = it > kStages ? it - kStages : 0;
+        for (int i = from; i < it; ++i) mbar_wait_uniform(empty + i % kStages * 8, (i / kStages) & 1, &sh.abort);
         if (*abort != 0 && rank == 0) {
             int own = 0;
-            for (int i = from; i < it; ++i) mbar_wait(smem_addr(&sh.full[i % kProdStages]), (i / kProdStages) & 1, &own);
+            for (int i = from; i < it; ++i) mbar_wait(smem_addr(&sh.full[i % kStages]), (i / kStages) & 1, &own);
         }
     } else if (rank == 0) {
         // ---- matrix unit
-        const uint32_t idesc = tc_idesc(kProdTile, kProdTile, p.bf16 != 0, A_MN, B_MN);
-        constexpr uint32_t kStep = kProdStageBytes >> 4, kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
+        const uint32_t idesc = tc_idesc(PAIR ? kProdTile : kProdHalf, kProdTile, p.bf16 != 0, A_MN, B_MN);
+        constexpr uint32_t kStep = kStageBytes >> 4, kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
         const uint64_t desc_a = A_MN ? tc_desc_rows(stages, kProdPanel) : tc_desc_cols(stages);
         const uint64_t desc_b = B_MN ? tc_desc_rows(stages + kProdOperand, kProdPanel) : tc_desc_cols(stages + kProdOperand);
         const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
         const bool leader = elect_one();
+        auto commit = [](uint32_t bar) {
+            if constexpr (PAIR) tc_commit_pair(bar);
+            else tc_commit(bar);
+        };
         uint32_t slot = 0, parity = 0, chunk = 0;
         for (int unit = pair; unit < sc.units; unit += pairs) {
             for (int left = prod_unit(p, sc, unit).stages; left > 0; left -= p.chunk, ++chunk) {
@@ -351,27 +410,33 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     const uint64_t da = desc_a + slot * kStep, db = desc_b + slot * kStep;
                     if (leader) {
 #pragma unroll
-                        for (int k = 0; k < kProdK / 16; ++k) tc_mma_f16_pair(d, da + k * kStepA, db + k * kStepB, idesc, s != 0 || k != 0);
-                        tc_commit_pair(empty + slot * 8);
+                        for (int k = 0; k < kProdK / 16; ++k) {
+                            if constexpr (PAIR) tc_mma_f16_pair(d, da + k * kStepA, db + k * kStepB, idesc, s != 0 || k != 0);
+                            else tc_mma_f16(d, da + k * kStepA, db + k * kStepB, idesc, s != 0 || k != 0);
+                        }
+                        commit(empty + slot * 8);
                     }
                     __syncwarp();
-                    if (++slot == kProdStages) slot = 0, parity ^= 1;
+                    if (++slot == kStages) slot = 0, parity ^= 1;
                 }
-                if (leader) tc_commit_pair(smem_addr(&sh.summed[chunk & 1]));
+                if (leader) commit(smem_addr(&sh.summed[chunk & 1]));
                 __syncwarp();
             }
         }
         // nothing may still be running when the tensor memory is given back
         int own = 0;
-        if (leader) tc_commit_pair(smem_addr(&sh.last));
+        if (leader) commit(smem_addr(&sh.last));
         mbar_wait(smem_addr(&sh.last), 0, &own);
     }
     // neither block leaves while the other may still signal to it or use its operands
     tc_fence_before();
     __syncthreads();
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    if constexpr (PAIR) cluster_sync();
     tc_fence_after();
-    if (warp == 0) tmem_free_pair(tmem, 512);
+    if (warp == 0) {
+        if constexpr (PAIR) tmem_free_pair(tmem, 512);
+        else tmem_free(tmem, 512);
+    }
 }
 
 // ---- small products --------------------------------------------------------------------------------
@@ -379,12 +444,11 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
 // share the contraction. Each forms its part of the sums, keeps it in shared memory, and adds up its share of
 // the tile's squares from all of them, in the order of their ranks, before it brings it out. A block needs little enough
 // that two fit on an SM: those of the kernel that follows are set up while this one runs.
-constexpr int kSmallTile = 128, kSmallStages = 3, kSmallOut = 256, kSmallThreads = kSmallOut + 64;  // warps 0-7 bring out, 8 copies, 9 issues
-constexpr size_t kSmallSmem = 1024 + kSmallStages * kProdStageBytes;
+constexpr int kSmallTile = 128, kSmallStages = 3, kMostSmallStages = 6, kSmallOut = 256, kSmallThreads = kSmallOut + 64;  // warps 0-7 bring out, 8 copies, 9 issues
 static_assert(kSmallTile * kSmallTile * 4 <= kSmallStages * kProdStageBytes, "the sums take the place of the operands");
 
 struct SmallShared {
-    uint64_t full[kSmallStages], empty[kSmallStages], summed;
+    uint64_t full[kMostSmallStages], empty[kMostSmallStages], summed;
     uint32_t tmem;
     int abort;
 };
@@ -397,7 +461,7 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
     __shared__ SmallShared sh;
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int blocks = p.small, rank = blockIdx.x % blocks;
+    const int ring = p.ring, blocks = p.small, rank = blockIdx.x % blocks;
 
     next_may_begin();
     ProdUnit u;
@@ -417,7 +481,7 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
         u.first = all * rank / blocks, u.stages = all * (rank + 1) / blocks - u.first;
     }
     if (tid == 0) {
-        for (int s = 0; s < kSmallStages; ++s) {
+        for (int s = 0; s < ring; ++s) {
             mbar_init(smem_addr(&sh.full[s]), 1);
             mbar_init(smem_addr(&sh.empty[s]), 1);
         }
@@ -507,13 +571,13 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
                     }
                 }
                 __syncwarp();
-                if (++slot == kSmallStages) slot = 0, parity ^= 1;
+                if (++slot == ring) slot = 0, parity ^= 1;
             }
             // A copy may still be under way only if a wait ran out: it has to arrive before the block ends.
             if (*static_cast<volatile int*>(&sh.abort) != 0) {
                 int own = 0;
-                for (int i = u.stages > kSmallStages ? u.stages - kSmallStages : 0; i < u.stages; ++i)
-                    mbar_wait(smem_addr(&sh.full[i % kSmallStages]), (i / kSmallStages) & 1, &own);
+                for (int i = u.stages > ring ? u.stages - ring : 0; i < u.stages; ++i)
+                    mbar_wait(smem_addr(&sh.full[i % ring]), (i / ring) & 1, &own);
             }
         } else {
             // ---- matrix unit
@@ -534,7 +598,7 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
                     tc_commit(smem_addr(&sh.empty[0]) + slot * 8);
                 }
                 __syncwarp();
-                if (++slot == kSmallStages) slot = 0, parity ^= 1;
+                if (++slot == ring) slot = 0, parity ^= 1;
             }
             // nothing may still be running when its results are read, the operands' place is taken and the tensor memory given back
             if (leader) tc_commit(smem_addr(&sh.summed));
@@ -571,22 +635,31 @@ inline int64_t small_tiles(const Product& p) {
     return (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
 }
 
-// How many blocks share a 128 x 128 tile, or 0 for pairs on 256 x 256 tiles: the least of an estimate in ns, fitted to products of
-// 128 to 4096 rows and contractions of 128 to 4608 (which it meets within 2 us). Small blocks wait for the L2 cache, the more of them
-// the longer; two fit on an SM. S of 1000 x 2048: 19 us in pairs, 13.1, 12.9 and 13.2 with 1, 2 and 4 blocks; of two of 300 x 3000 19.5, 16.8, 13.9
-// and 10.3; of 4096 x 4096 52 in pairs and 90 with one block.
-inline int small_blocks(const Product& p, int sms) {
-    const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile, stages = (p.k + kProdK - 1) / kProdK;
-    const int64_t tiles = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches, small = small_tiles(p);
-    const int64_t pair_rounds = (tiles + p.pairs - 1) / p.pairs, hidden = stages * 370 < 6000 ? 6000 - stages * 370 : 0;
+// How many blocks share a 128 x 128 tile, and how many stages each has under way; or pairs on 256 x 256 tiles: the least of an
+// estimate in ns, fitted to products of 128 to 4096 rows and contractions of 128 to 4608. With six stages a block has an SM to itself
+// and takes 200 ns for one; with three, two share an SM and wait for the L2 cache, the longer the more there are. (36 tiles over 32 stages: 19.1 us in pairs;
+// 13.2, 12.6 and 12.9 with 1, 2 and 4 blocks of three stages, 11.9, 9.8 and 17.7 of six, as clusters of four do not find place on all
+// SMs. 144 tiles over 16: 15.4, 13.7 with three stages, 9.3 with six. 136 tiles of 256 over 64: 52 in pairs, 90 with one block a tile.)
+inline void choose_small(Product* p, int sms) {
+    const int64_t tm = (p->m + kProdTile - 1) / kProdTile, tn = (p->n + kProdTile - 1) / kProdTile, stages = (p->k + kProdK - 1) / kProdK;
+    const int64_t tiles = (p->upper ? tm * (tm + 1) / 2 : tm * tn) * p->batches, small = small_tiles(*p);
+    const int64_t pair_rounds = (tiles + p->pairs - 1) / p->pairs, hidden = stages * 370 < 6000 ? 6000 - stages * 370 : 0;
     int64_t best = pair_rounds * stages * 370 + 8500 + (pair_rounds - 1) * hidden;
-    int blocks = 0;
+    p->small = 0, p->ring = 0;
     for (int c = 1; c <= 4 && c <= stages; c *= 2) {
-        const int64_t all = small * c, rounds = (all + 2 * sms - 1) / (2 * sms), at_once = all < 2 * sms ? all : 2 * sms;
-        const int64_t t = rounds * ((stages + c - 1) / c * (170 + at_once * 9 / 4)) + 5500 + (rounds - 1) * 2000 + (c == 2 ? 800 : (c == 4 ? 1000 + 20 * all : 0));
-        if (t < best) best = t, blocks = c;
+        const int64_t all = small * c, share = (stages + c - 1) / c;
+        const int64_t joined = 5500 + (c == 2 ? 800 : (c == 4 ? 2000 + 8 * all : 0));
+        int64_t t;
+        int ring = kMostSmallStages;
+        if (all <= (c == 4 ? sms * 6 / 7 : sms)) {
+            t = share * (200 + all / 4) + joined;
+        } else {
+            const int64_t at_once = all < 2 * sms ? all : 2 * sms, rounds = (all + 2 * sms - 1) / (2 * sms), wait = at_once * 9 / 4;
+            ring = kSmallStages;
+            t = rounds * share * (170 + (wait < 350 ? wait : 350)) + (rounds - 1) * 4000 + joined;
+        }
+        if (t < best) best = t, p->small = c, p->ring = ring;
     }
-    return blocks;
 }
 
 template <class EPI, bool A_MN, bool B_MN>
@@ -605,25 +678,39 @@ int launch_product(const CUtensorMap& a, const CUtensorMap& b, const Product& p,
         if (p.small > 0) {
             const auto kernel = small_product_kernel<EPI, A_MN, B_MN>;
             struct Key {};
-            e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kSmallSmem));
+            e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), 1024 + kMostSmallStages * static_cast<int>(kProdStageBytes));
             if (e != cudaSuccess) return cuda_status_public(e);
             cfg.gridDim = dim3(static_cast<unsigned>(small_tiles(p) * p.small));
             cfg.blockDim = dim3(kSmallThreads);
-            cfg.dynamicSmemBytes = kSmallSmem;
+            cfg.dynamicSmemBytes = 1024 + p.ring * kProdStageBytes;
             at[0].val.clusterDim.x = p.small;
             return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, a, b, p, epi));
         }
     }
-    const auto kernel = product_kernel<EPI, A_MN, B_MN>;
+    if constexpr (EPI::kAlone && !A_MN) {
+        if (p.tile_m == kProdHalf) {
+            const auto kernel = product_kernel<EPI, A_MN, B_MN, false>;
+            struct Key {};
+            e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(Stage<false>::kSmem));
+            if (e != cudaSuccess) return cuda_status_public(e);
+            const int64_t units = static_cast<int64_t>((p.m + kProdHalf - 1) / kProdHalf) * ((p.n + kProdTile - 1) / kProdTile);
+            cfg.gridDim = dim3(static_cast<unsigned>(units > p.pairs || p.split ? p.pairs : units));
+            cfg.blockDim = dim3(kProdThreads);
+            cfg.dynamicSmemBytes = Stage<false>::kSmem;
+            at[0].val.clusterDim.x = 1;
+            return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, a, b, p, epi));
+        }
+    }
+    const auto kernel = product_kernel<EPI, A_MN, B_MN, true>;
     struct Key {};
-    e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kProdSmem));
+    e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(Stage<true>::kSmem));
     if (e != cudaSuccess) return cuda_status_public(e);
     const int64_t tm = (p.m + kProdTile - 1) / kProdTile, tn = (p.n + kProdTile - 1) / kProdTile;
     int64_t units = (p.upper ? tm * (tm + 1) / 2 : tm * tn) * p.batches;
     if (units > p.pairs || p.split) units = p.pairs;
     cfg.gridDim = dim3(static_cast<unsigned>(2 * units));
     cfg.blockDim = dim3(kProdThreads);
-    cfg.dynamicSmemBytes = kProdSmem;
+    cfg.dynamicSmemBytes = Stage<true>::kSmem;
     return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, a, b, p, epi));
 }
 
