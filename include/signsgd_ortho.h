@@ -12,10 +12,10 @@
  * products are formed over the smaller side. With (3.4445, -4.7750, 2.0315) five times (the default of
  * the Python side) a singular value of X_0 from 0.01 on ends between 0.67 and 1.21.
  *
- * Numerics. |u| in fp64. The products' operands are fp16 (11 significant bits), scaled by a power of
- * two so that their values lie well inside its range, with fp32 sums; X itself is carried from step to step as the
- * sum of two fp16, 22 bits, so that directions with small singular values are not lost in the rounding of large ones. Of a result O about 2e-3 (2-norm) is
- * rounding. A matrix that holds an infinity or a NaN gives NaN throughout; so does a wait inside a kernel that ran out (each is bounded).
+ * Numerics. |u| in fp64, X in fp32. The products' operands are fp16 (11 significant bits), scaled by a power of
+ * two so that their values lie well inside its range, with fp32 sums; the term a X takes X unrounded, so that directions with
+ * small singular values are not lost in the rounding of large ones. Of a result O about 2e-3 (2-norm) is rounding. A matrix that
+ * holds an infinity or a NaN gives NaN throughout; so does a wait inside a kernel that ran out (each is bounded).
  */
 #ifndef SIGNSGD_ORTHO_H_
 #define SIGNSGD_ORTHO_H_

@@ -468,7 +468,7 @@ struct Dest {
 // OUT16: to.bf16, else to.f32. BEFORE: with to.before.
 template <bool OUT16, bool BEFORE>
 struct Gradient {
-    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE;
+    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE, kAhead = true;
     struct Fetched {
         float4 before[BEFORE ? 8 : 1];
     };

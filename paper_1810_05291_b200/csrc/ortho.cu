@@ -5,9 +5,10 @@
 // next one reads. A tall matrix has S = X^T X and X Q instead; the operands' maps differ, nothing is transposed.
 //
 // Rounding. The operands X, S and Q are fp16: with bf16 (8 bits) the result is 1 to 3 % off, with fp16 0.2 %. The
-// term a X takes X with 22 bits, as the sum of two fp16 of which the first is the operand: it alone carries the
-// directions whose singular values are small, which each step enlarges 3.4 times; with 11 bits there a momentum
-// of few strong directions comes out 0.35 % off instead of 0.03 %.
+// term a X takes X from fp32: it alone carries the directions whose singular values are small, which each step
+// enlarges 3.4 times; with 11 bits there a momentum of few strong directions comes out 0.35 % off instead of
+// 0.03 %. (As the sum of two fp16, the first of them the operand, X has two bytes less to move for each element and
+// step and 22 bits, but takes seven instructions more: the same time within 2 %.)
 #include "../../include/signsgd_ortho.h"
 #include "product.cuh"
 
@@ -32,19 +33,12 @@ __device__ __forceinline__ float4 float4_of(uint2 h) {
     const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&h.y));
     return make_float4(a.x, a.y, b.x, b.y);
 }
-// The two fp16 whose sum v is, to 22 bits.
-__device__ __forceinline__ void split4(float4 v, uint2* hi, uint2* lo) {
-    *hi = half4(v);
-    const float4 h = float4_of(*hi);
-    *lo = half4(make_float4(v.x - h.x, v.y - h.y, v.z - h.z, v.w - h.w));
-}
-
 // ---- ends of the products --------------------------------------------------------------------------
 
 // out = c sums (+ b lin), symmetric: a square of a tile above the diagonal is stored a second time, mirrored.
 template <bool LIN>
 struct Symmetric {
-    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kAhead = true;
     static constexpr int kSmallBlocks = 2;
     struct Fetched {
         uint2 lin[LIN ? 8 : 1];
@@ -101,56 +95,49 @@ struct Symmetric {
     };
 };
 
-// X carried as hi + lo, scaled by a power of two: the next one is a (hi + lo) + sums.
+// X carried in fp32, scaled by a power of two: the next one is a X + sums.
 struct Carried {
-    const uint16_t* hi;
-    uint16_t* lo;
+    float* x;
     int64_t plane;
     int ld;
     float a;
 };
 
-__device__ __forceinline__ float4 next_of(float a, float4 sums, uint2 hi, uint2 lo) {
-    const float4 h = float4_of(hi), l = float4_of(lo);
-    return make_float4(a * (h.x + l.x) + sums.x, a * (h.y + l.y) + sums.y, a * (h.z + l.z) + sums.z, a * (h.w + l.w) + sums.w);
-}
+__device__ __forceinline__ float4 next_of(float a, float4 sums, float4 x) { return make_float4(a * x.x + sums.x, a * x.y + sums.y, a * x.z + sums.z, a * x.w + sums.w); }
 
 struct Next {
-    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kAhead = true;
     static constexpr int kSmallBlocks = 2;
     struct Fetched {
-        uint2 hi[8], lo[8];
+        float4 x[8];
     };
     Carried x;
-    uint16_t* hi_out;
+    uint16_t* out;  // the next operand
 
     struct Tile {
-        const uint16_t* hi;
-        uint16_t *lo, *hi_out;
+        float* x;
+        uint16_t* out;
         int rows;
 
         __device__ __forceinline__ Tile(const Next& e, const ProdUnit& u, int m, int row, int col, int lane) {
             const int64_t r = row + (lane >> 3), at = u.batch * e.x.plane + r * e.x.ld + col + 4 * (lane & 7);
-            hi = e.x.hi + at, lo = e.x.lo + at, hi_out = e.hi_out + at;
+            x = e.x.x + at, out = e.out + at;
             rows = m - static_cast<int>(r);
         }
         __device__ __forceinline__ void fetch(const Next& e, int j, Fetched& f) const {
+            const float* p = x + j;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
-                f.hi[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(hi + k) : make_uint2(0, 0);
-                f.lo[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
-            }
+            for (int i = 0; i < 8; ++i, p += 4 * e.x.ld) f.x[i] = 4 * i < rows ? *reinterpret_cast<const float4*>(p) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
         __device__ __forceinline__ void square(const Next& e, int j, int lane, uint32_t buf, float4 (&sums)[8], const Fetched& f, bool) const {
+            float* p = x + j;
+            uint16_t* q = out + j;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
-                uint2 h, l;
-                split4(next_of(e.x.a, sums[i], f.hi[i], f.lo[i]), &h, &l);
+            for (int i = 0; i < 8; ++i, p += 4 * e.x.ld, q += 4 * e.x.ld) {
+                const float4 v = next_of(e.x.a, sums[i], f.x[i]);
                 if (4 * i >= rows) continue;
-                *reinterpret_cast<uint2*>(hi_out + k) = h;
-                *reinterpret_cast<uint2*>(lo + k) = l;  // nothing but this place of this tile reads it
+                *reinterpret_cast<float4*>(p) = v;  // nothing but this place of this tile reads it
+                *reinterpret_cast<uint2*>(q) = half4(v);
             }
         }
     };
@@ -161,11 +148,10 @@ enum { kToF32, kToBf16, kToParam };
 // The last step's result, to the caller: O, or the parameter moved by it.
 template <int TO>
 struct Result {
-    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kAhead = TO != kToParam;
     static constexpr int kSmallBlocks = TO == kToParam ? 1 : 2;
     struct Fetched {
-        uint2 hi[8], lo[8];
-        float4 p[TO == kToParam ? 8 : 1];
+        float4 x[8], p[TO == kToParam ? 8 : 1];
     };
     Carried x;
     float unscale;  // of the power of two
@@ -178,14 +164,14 @@ struct Result {
     __device__ __forceinline__ float moved(float p, float o) const { return p - lr * (scale * o + decay * p); }
 
     struct Tile {
-        const uint16_t *hi, *lo;
+        const float* x;
         char* to;
         const float* from;
         int rows, cols;  // that exist from this lane's first ones on
 
         __device__ __forceinline__ Tile(const Result& e, const ProdUnit& u, int m, int row, int col, int lane) {
             const int64_t r = row + (lane >> 3), c = col + 4 * (lane & 7), at = u.batch * e.x.plane + r * e.x.ld + c;
-            hi = e.x.hi + at, lo = e.x.lo + at;
+            x = e.x.x + at;
             to = static_cast<char*>(const_cast<void*>(e.out.p[u.batch])) + (r * e.stride + c) * (TO == kToBf16 ? 2 : 4);
             from = TO == kToParam ? static_cast<const float*>(e.param.p[u.batch]) + r * e.stride + c : nullptr;
             rows = m - static_cast<int>(r), cols = e.cols - static_cast<int>(c);
@@ -193,9 +179,7 @@ struct Result {
         __device__ __forceinline__ void fetch(const Result& e, int j, Fetched& f) const {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int64_t k = j + 4 * i * static_cast<int64_t>(e.x.ld);
-                f.hi[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(hi + k) : make_uint2(0, 0);
-                f.lo[i] = 4 * i < rows ? *reinterpret_cast<const uint2*>(lo + k) : make_uint2(0, 0);
+                f.x[i] = 4 * i < rows ? *reinterpret_cast<const float4*>(x + j + 4 * i * static_cast<int64_t>(e.x.ld)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if constexpr (TO == kToParam) {
                     if (e.vectors && 4 * i < rows && j + 4 <= cols) f.p[i] = *reinterpret_cast<const float4*>(from + j + 4 * i * e.stride);
                 }
@@ -204,7 +188,7 @@ struct Result {
         __device__ __forceinline__ void square(const Result& e, int j, int lane, uint32_t buf, float4 (&sums)[8], const Fetched& f, bool) const {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float4 n = next_of(e.x.a, sums[i], f.hi[i], f.lo[i]);
+                const float4 n = next_of(e.x.a, sums[i], f.x[i]);
                 if (4 * i >= rows || j >= cols) continue;
                 float4 o = make_float4(n.x * e.unscale, n.y * e.unscale, n.z * e.unscale, n.w * e.unscale);
                 char* const p = to + (j + 4 * i * e.stride) * (TO == kToBf16 ? 2 : 4);
@@ -237,7 +221,8 @@ struct Start {
     float beta, rest;  // rest = 1 - beta
     double scale;      // the power of two
     double* partial;   // [count][blocks]
-    uint16_t *hi, *lo;
+    float* x;
+    uint16_t* operand;
 };
 
 // Eight neighbouring columns; those that do not exist are 0.
@@ -342,7 +327,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__
     if (threadIdx.x == 0) a.partial[static_cast<int64_t>(blockIdx.y) * a.blocks + blockIdx.x] = sum;
 }
 
-// X_0 = u / |u|, scaled, as hi + lo.
+// X_0 = u / |u|, scaled, and the operand made of it.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant__ Start a) {
     next_may_begin();
@@ -366,12 +351,11 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) u.v[j] = wide ? static_cast<float>(u.v[j] * factor) : u.v[j] * factor32;
-        uint2 hi[2], lo[2];
-        split4(make_float4(u.v[0], u.v[1], u.v[2], u.v[3]), &hi[0], &lo[0]);
-        split4(make_float4(u.v[4], u.v[5], u.v[6], u.v[7]), &hi[1], &lo[1]);
+        const float4 p = make_float4(u.v[0], u.v[1], u.v[2], u.v[3]), q = make_float4(u.v[4], u.v[5], u.v[6], u.v[7]);
         const int64_t k = blockIdx.y * a.plane + r * a.ld + c;
-        *reinterpret_cast<uint4*>(a.hi + k) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
-        *reinterpret_cast<uint4*>(a.lo + k) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+        reinterpret_cast<float4*>(a.x + k)[0] = p, reinterpret_cast<float4*>(a.x + k)[1] = q;
+        const uint2 lo = half4(p), hi = half4(q);
+        *reinterpret_cast<uint4*>(a.operand + k) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     });
 }
 
@@ -768,7 +752,7 @@ struct Layout {
     int64_t side, ld, side_ld;   // the smaller side; row strides of X and of S and Q
     int64_t plane, side_plane;   // elements of a matrix
     int blocks, row_threads;     // of the start, for each matrix; for each row
-    int64_t hi[2], lo, s, q, partial, bytes;  // places in the workspace
+    int64_t x, operand[2], s, q, partial, bytes;  // places in the workspace
 };
 
 inline int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
@@ -791,7 +775,7 @@ int layout_of(int count, int64_t rows, int64_t cols, Layout* l) {
         at += up_to(bytes, 256);
         return p;
     };
-    l->hi[0] = place(count * l->plane * 2), l->hi[1] = place(count * l->plane * 2), l->lo = place(count * l->plane * 2);
+    l->x = place(count * l->plane * 4), l->operand[0] = place(count * l->plane * 2), l->operand[1] = place(count * l->plane * 2);
     l->s = place(count * l->side_plane * 2), l->q = place(count * l->side_plane * 2);
     l->partial = place(static_cast<int64_t>(count) * l->blocks * 8);
     l->bytes = at;
@@ -853,12 +837,12 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     const float scale = std::ldexp(1.0f, power), unscale = std::ldexp(1.0f, -power);
     const int held = held_blocks(c.rows, c.cols);
     if (held > 0) return run_held(c, held, scale, unscale, st);
-    uint16_t* hi[2] = {reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.hi[1])};
-    uint16_t* const lo = reinterpret_cast<uint16_t*>(ws + l.lo);
+    float* const xs = reinterpret_cast<float*>(ws + l.x);
+    uint16_t* operand[2] = {reinterpret_cast<uint16_t*>(ws + l.operand[0]), reinterpret_cast<uint16_t*>(ws + l.operand[1])};
     uint16_t *const s = reinterpret_cast<uint16_t*>(ws + l.s), *const q = reinterpret_cast<uint16_t*>(ws + l.q);
     Start& a = c.start;
     a.plane = l.plane, a.rows = c.rows, a.cols = static_cast<int>(c.cols), a.ld = static_cast<int>(l.ld), a.blocks = l.blocks, a.row_threads = l.row_threads;
-    a.scale = scale, a.partial = reinterpret_cast<double*>(ws + l.partial), a.hi = hi[0], a.lo = lo;
+    a.scale = scale, a.partial = reinterpret_cast<double*>(ws + l.partial), a.x = xs, a.operand = operand[0];
     const dim3 grid(static_cast<unsigned>(l.blocks), static_cast<unsigned>(c.count));
     cudaError_t e;
     if (c.in_dt == SS_F32) e = launch_next(false, ortho_norm_kernel<float>, grid, 256, st, a);
@@ -876,8 +860,8 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
         if (status == SS_OK) status = map_operand(m, p, false, fast, slow, rb, c.count, pb, mn);
     };
     for (int i = 0; i < 2; ++i) {
-        map(&x_sum[i], hi[i], c.cols, c.rows, row_bytes, plane_bytes, tall);
-        map(&x_prod[i], hi[i], c.cols, c.rows, row_bytes, plane_bytes, !tall);
+        map(&x_sum[i], operand[i], c.cols, c.rows, row_bytes, plane_bytes, tall);
+        map(&x_prod[i], operand[i], c.cols, c.rows, row_bytes, plane_bytes, !tall);
     }
     map(&s_map, s, l.side, l.side, side_row, side_bytes, false);
     map(&q_map, q, l.side, l.side, side_row, side_bytes, false);
@@ -895,13 +879,13 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
         const int from = k & 1;
         const Symmetric<false> es{s, nullptr, l.side_plane, static_cast<int>(l.side_ld), 0.0f, unscale * unscale};
         const Symmetric<true> eq{q, s, l.side_plane, static_cast<int>(l.side_ld), co[1], co[2]};
-        const Carried x{hi[from], lo, l.plane, static_cast<int>(l.ld), co[0]};
+        const Carried x{xs, l.plane, static_cast<int>(l.ld), co[0]};
         status = tall ? launch_product<Symmetric<false>, true, true>(x_sum[from], x_sum[from], ps, es, st)
                       : launch_product<Symmetric<false>, false, false>(x_sum[from], x_sum[from], ps, es, st);
         if (status == SS_OK) status = launch_product<Symmetric<true>, false, false>(s_map, s_map, pq, eq, st);
         if (status != SS_OK) return status;
         if (k + 1 < c.steps) {
-            const Next en{x, hi[from ^ 1]};
+            const Next en{x, operand[from ^ 1]};
             status = tall ? launch_product<Next, false, false>(x_prod[from], q_map, px, en, st)
                           : launch_product<Next, false, true>(q_map, x_prod[from], px, en, st);
         } else {

@@ -184,15 +184,11 @@ __device__ __forceinline__ void square_sums(uint32_t buf, int lane, float4 (&v)[
 
 constexpr uint32_t kNanBits = 0x7FC00000u;
 
-template <class TILE>
-__device__ __forceinline__ auto packs(const TILE& t) -> decltype(t.packs) { return t.packs; }
-__device__ __forceinline__ bool packs(...) { return false; }
-
 // EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
 // registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
 // square(column, ..., its sums, first chunk?). With EPI::kPacks a tile may take 64 columns at a time, rounded to 16 bits:
-// packed(column, ...). EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
+// packed(column, ...). EPI::kAhead: registers allow two squares' fetches. EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
 template <class EPI, bool A_MN, bool B_MN, bool PAIR>
 __global__ void __launch_bounds__(kProdThreads, 1)
@@ -279,14 +275,16 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                 bool first = true;
                 const bool any = row < sc.m && col < p.n;
                 typename EPI::Tile tile(epi, u, sc.m, row, col, lane);
-                typename EPI::Fetched f;
+                typename EPI::Fetched f, g;
                 for (int left = u.stages; left > 0; left -= p.chunk, ++chunk) {
                     if (any) tile.fetch(epi, 0, f);
                     if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
                     tc_fence_after();
                     const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
+                    bool done = !any;
                     if constexpr (EPI::kPacks) {
                         if (tile.packs && ok) {
+                            done = true;
 #pragma unroll 1
                             for (int j = 0; j < kProdHalf; j += 64) {
 #pragma unroll
@@ -305,9 +303,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                             }
                         }
                     }
-#pragma unroll 1
-                    for (int j = EPI::kPacks && packs(tile) && ok ? kProdHalf : 0; any && j < kProdHalf && col + j < p.n; j += 32) {
-                        if (j > 0) tile.fetch(epi, j, f);
+                    auto square = [&](int j, typename EPI::Fetched& of) {
                         uint32_t r[32];
                         tmem_load32(src + j, r);
                         tmem_load_wait();
@@ -319,8 +315,23 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                         __syncwarp();
                         float4 v[8];
                         square_sums(buf, lane, v);
-                        tile.square(epi, j, lane, buf, v, f, first);
+                        tile.square(epi, j, lane, buf, v, of, first);
                         __syncwarp();
+                    };
+#pragma unroll 1
+                    for (int j = 0; !done && j < kProdHalf && col + j < p.n; j += 64) {  // what the next square needs is on its way while one is worked on
+                        const bool second = col + j + 32 < p.n, third = j + 64 < kProdHalf && col + j + 64 < p.n;
+                        if (EPI::kAhead && second) tile.fetch(epi, j + 32, g);
+                        square(j, f);
+                        if (!second) break;
+                        if constexpr (EPI::kAhead) {
+                            if (third) tile.fetch(epi, j + 64, f);
+                            square(j + 32, g);
+                        } else {
+                            tile.fetch(epi, j + 32, f);
+                            square(j + 32, f);
+                            if (third) tile.fetch(epi, j + 64, f);
+                        }
                     }
                     tc_fence_before();
                     __syncwarp();

@@ -9,7 +9,7 @@ def _half(x):
 
 
 def orthogonalised(u, coefficients=COEFFICIENTS, rounded=False):
-    """With ``rounded``: operands in fp16, X carried as the sum of two fp16, scaled as the kernels scale it."""
+    """With ``rounded``: operands in fp16, scaled as the kernels scale them; X itself is not rounded."""
     u = u.double()
     norm = u.square().sum().sqrt()
     x = torch.zeros_like(u) if float(norm) == 0 else u / norm
@@ -22,8 +22,7 @@ def orthogonalised(u, coefficients=COEFFICIENTS, rounded=False):
     scale = 2.0 ** power
     for a, b, c in coefficients:
         if rounded:
-            hi = _half(x * scale)
-            x, op = (hi + _half(x * scale - hi)) / scale, hi / scale
+            op = _half(x * scale) / scale
             s = _half(op @ op.t())
             x = a * x + _half(b * s + c * (s @ s)) @ op
         else:
