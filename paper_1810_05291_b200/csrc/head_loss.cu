@@ -9,8 +9,8 @@
 // So neither the logits nor P exist as a whole, and three products do, where forming the logits again for the backward pass
 // would take four; the pass over e costs a few percent of a product.
 //
-// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 256 contraction indices and
-// are added in registers, to nearest: log p would otherwise lose 1e-4 at width 4096. e is fp16 (relative to its part's
+// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 1024 contraction indices and
+// are added in registers, to nearest. e is fp16 (relative to its part's
 // maximum, 11 bits), P is bf16 as the gradient of bf16 logits is; the entry of the target, which is a
 // difference, is formed in fp32 from log p. With fp32 inputs e is fp32 and P the sum of three bf16.
 #include "product.cuh"
@@ -18,12 +18,15 @@
 #include <cuda_fp16.h>
 
 #include <cmath>
+#include <type_traits>
 
 namespace ss {
 namespace {
 
 constexpr int kPartCols = kProdHalf;              // logits of a thread
-constexpr int kLogitChunk = 16;                    // stages that the matrix unit sums of a logit
+// Stages that the matrix unit sums of a logit. log p of 8192 x 4096 over 131072 is off by 2.6e-6 with 16 (an fp32 product: 3.1e-6), and by 6e-7 with 4,
+// whose product takes 3.95 ms instead of 3.3 (with 8: 3.5): the two halves of the tensor memory fill while a tile's exponentials are formed.
+constexpr int kLogitChunk = 16;
 // Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16; 2048 lose 5e-7.
 constexpr int kGradChunk = 256, kGradChunkF32 = 32;
 constexpr int64_t kChunkBytes = int64_t(1) << 30; // of e and P
@@ -44,6 +47,7 @@ struct Head {
     const void *x, *w;
     void* dx;
     int width, vocab, vectors, dx_vectors, w_vectors;
+    int few;                        // at most kFewRows rows: launches of their own for rows and statistics are saved
     float c, k, z_coef;  // k = c log2 e
     // workspace
     int *index, *target, *live;     // of the rows that count, one after another
@@ -160,12 +164,56 @@ __device__ __forceinline__ void stage_row(const T* src, uint16_t* dst, int64_t p
 constexpr int kGatherCols = 512;  // that a warp takes of a row
 
 // Rows that count gathered; behind them zeros up to a whole stage, since dW sums over whole stages; the results of the others.
-template <typename T>
+// FEW: at most kFewRows, which each block finds by itself; the first one writes down what follows needs.
+constexpr int kFewRows = 1024;
+
+__device__ __forceinline__ int find_rows(const Head& a, int* index) {
+    __shared__ int sums[4][8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t y[4];
+    uint32_t votes[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = 256 * i + threadIdx.x;
+        y[i] = t < a.rows && a.weights[t] != 0.0f ? a.targets[t] : -1;
+        votes[i] = __ballot_sync(0xFFFFFFFFu, y[i] >= 0 && y[i] < a.vocab);
+        if (lane == 0) sums[i][warp] = __popc(votes[i]);
+    }
+    __syncthreads();
+    int base = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        int before = base;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if (w < warp) before += sums[i][w];
+            base += sums[i][w];
+        }
+        if (votes[i] >> lane & 1) {
+            const int s = before + __popc(votes[i] & ((1u << lane) - 1u)), t = 256 * i + threadIdx.x;
+            index[s] = t;
+            if (blockIdx.x == 0) a.index[s] = t, a.target[s] = static_cast<int>(y[i]);
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.live = base;
+    __syncthreads();
+    return base;
+}
+
+template <typename T, bool FEW>
 __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant__ Head a) {
     next_may_begin();
-    after_previous();
+    __shared__ int found[FEW ? kFewRows : 1];
+    int64_t live;
+    const int* index = a.index;
+    if constexpr (FEW) {
+        live = find_rows(a, found), index = found;
+    } else {
+        after_previous();
+        live = *a.live;
+    }
     const int lane = threadIdx.x & 31;
-    const int64_t live = *a.live, padded = (live + kProdK - 1) / kProdK * kProdK, plane = a.row_cap * a.width_ld;
+    const int64_t padded = (live + kProdK - 1) / kProdK * kProdK, plane = a.row_cap * a.width_ld;
     const int64_t upto = padded > kProdK ? padded : kProdK;
     const int pieces = (a.width + kGatherCols - 1) / kGatherCols;
     for (int64_t j = blockIdx.x * 8 + (threadIdx.x >> 5); j < (a.rows + kProdK) * pieces; j += gridDim.x * 8) {
@@ -174,7 +222,7 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant_
         if (i < upto) {
             uint16_t* const dst = a.gathered + i * a.width_ld + first;
             if (i < live) {
-                stage_row(static_cast<const T*>(a.x) + a.index[i] * a.x_stride + first, dst, plane, n, a.vectors, lane);
+                stage_row(static_cast<const T*>(a.x) + index[i] * a.x_stride + first, dst, plane, n, a.vectors, lane);
             } else {
                 for (int q = 0; q < (sizeof(T) == 4 ? kTerms : 1); ++q)
                     for (int c = lane; c < n; c += 32) dst[q * plane + c] = 0;
@@ -211,7 +259,7 @@ __device__ __forceinline__ uint4 half8(const float* v) {
 
 // ---- the end of the logits' product
 struct Logits {
-    static constexpr bool kWhole = true, kSmall = false, kAlone = true, kPacks = false;
+    static constexpr bool kWhole = true, kSmall = false, kAlone = true, kPacks = false, kBefore = false;
     const int* target;  // of the chunk's rows
     float* target_logit;
     float2* parts;
@@ -277,6 +325,27 @@ struct Logits {
     }
 };
 
+struct RowGrad {
+    float factor, target;
+};
+
+// Of row r of the chunk, from its largest logit and the sum of its exponentials; the row's figures written down, if asked for.
+__device__ __forceinline__ RowGrad row_grad(const Head& a, int64_t r, float top, float sum, bool write) {
+    const int64_t s = a.first + r;
+    const int t = a.index[s];
+    const float w = a.weights[t], rest = logf(sum);
+    const float lse = a.c * top + rest, logp = a.c * (a.target_logit[r] - top) - rest;
+    const float scale = w * a.c * (a.grad_scale == nullptr ? 1.0f : *a.grad_scale);
+    float loss = -w * logp, all = 1.0f, extra = 0.0f;
+    if (a.z_coef != 0.0f) {
+        loss += a.z_coef * w * lse * lse;
+        extra = 2.0f * a.z_coef * lse;
+        all += extra;
+    }
+    if (write) a.logp[t] = logp, a.loss[s] = loss, a.square[s] = w * lse * lse;
+    return RowGrad{scale * all / sum, scale * (expm1f(logp) + extra * expf(logp))};
+}
+
 // log p, and what the row's gradient is made of: P_v = factor e_v 2^(k (m_part - top)), the target's in fp32 from log p:
 // p - 1 = exp(log p) - 1 keeps its digits near certainty. A warp to a row.
 __global__ void __launch_bounds__(256) head_statistics_kernel(const __grid_constant__ Head a) {
@@ -300,22 +369,8 @@ __global__ void __launch_bounds__(256) head_statistics_kernel(const __grid_const
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
         if (lane != 0) continue;
-        const int64_t s = a.first + r;
-        const int t = a.index[s];
-        const float w = a.weights[t], rest = logf(sum);
-        const float lse = a.c * top + rest, logp = a.c * (a.target_logit[r] - top) - rest;
-        const float scale = w * a.c * (a.grad_scale == nullptr ? 1.0f : *a.grad_scale);
-        float loss = -w * logp, all = 1.0f, extra = 0.0f;
-        if (a.z_coef != 0.0f) {
-            loss += a.z_coef * w * lse * lse;
-            extra = 2.0f * a.z_coef * lse;
-            all += extra;
-        }
-        a.logp[t] = logp;
-        a.loss[s] = loss, a.square[s] = w * lse * lse;
-        a.top[r] = top;
-        a.factor[r] = scale * all / sum;
-        a.target_grad[r] = scale * (expm1f(logp) + extra * expf(logp));
+        const RowGrad g = row_grad(a, r, top, sum, true);
+        a.top[r] = top, a.factor[r] = g.factor, a.target_grad[r] = g.target;
     }
 }
 
@@ -339,18 +394,50 @@ __device__ __forceinline__ void totals_of(const Head& a, int64_t live) {
     }
 }
 
-// Where no gradient follows; none: no rows.
+// The same of few rows, by one warp.
+__device__ __forceinline__ void few_totals(const Head& a, int live, int lane) {
+    double loss = 0.0, square = 0.0;
+#pragma unroll 8
+    for (int s = lane; s < live; s += 32) loss += a.loss[s], square += a.square[s];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        loss += __shfl_xor_sync(0xFFFFFFFFu, loss, d);
+        square += __shfl_xor_sync(0xFFFFFFFFu, square, d);
+    }
+    if (lane == 0) a.totals[0] = static_cast<float>(loss), a.totals[1] = static_cast<float>(square);
+}
+
+// Where nothing else forms them; none: no rows.
 __global__ void __launch_bounds__(256) head_totals_kernel(const __grid_constant__ Head a, int none) {
     next_may_begin();
     if (!none) after_previous();
-    totals_of(a, none ? 0 : *a.live);
+    if (!a.few) totals_of(a, none ? 0 : *a.live);
+    else if (threadIdx.x < 32) few_totals(a, *a.live, threadIdx.x);
 }
 
 // e -> P: four times eight columns to a thread, all loads before the first store. Rows behind the last up to a whole stage
-// become zeros. A row of blocks behind all rows, where the call's last chunk has it, forms the totals.
+// become zeros. A row of blocks behind all rows, where the call's last chunk has it, forms the totals. FEW: the row's
+// statistics are formed here, by each of its blocks, instead of by a launch of their own.
 constexpr int kGradientPieces = 4;
 
-template <bool F32>
+// Largest or sum over the block's 256 threads, the same in all.
+template <bool MAX>
+__device__ __forceinline__ float block_reduce(float v) {
+    __shared__ float part[8];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const float o = __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        v = MAX ? fmaxf(v, o) : v + o;
+    }
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v = MAX ? fmaxf(v, part[i]) : v + part[i];
+    return v;
+}
+
+template <bool F32, bool FEW>
 __global__ void __launch_bounds__(256) head_gradient_kernel(const __grid_constant__ Head a) {
     next_may_begin();
     after_previous();
@@ -383,7 +470,23 @@ __global__ void __launch_bounds__(256) head_gradient_kernel(const __grid_constan
         }
         top[i] = a.parts[r * a.n_parts + c / kPartCols].x;
     }
-    const float factor = a.factor[r], row_top = a.top[r], target_grad = a.target_grad[r];
+    float factor, row_top, target_grad;
+    if constexpr (FEW) {
+        const float2* const p = a.parts + r * a.n_parts;
+        float m = -INFINITY, sum = 0.0f;
+        for (int i = threadIdx.x; i < a.n_parts; i += 256) m = fmaxf(m, p[i].x);
+        row_top = block_reduce<true>(m);
+        const float from = row_top == -INFINITY ? 0.0f : row_top;
+        for (int i = threadIdx.x; i < a.n_parts; i += 256) {
+            const float2 q = p[i];
+            sum += q.y * ex2((q.x - from) * a.k);
+        }
+        sum = block_reduce<false>(sum);
+        const RowGrad g = row_grad(a, r, row_top, sum, blockIdx.x == 0 && threadIdx.x == 0);
+        factor = g.factor, target_grad = g.target;
+    } else {
+        factor = a.factor[r], row_top = a.top[r], target_grad = a.target_grad[r];
+    }
     const int target = a.target[a.first + r];
 #pragma unroll
     for (int i = 0; i < kGradientPieces; ++i) {
@@ -465,16 +568,78 @@ struct Dest {
     }
 };
 
-// OUT16: to.bf16, else to.f32. BEFORE: with to.before.
-template <bool OUT16, bool BEFORE>
+// Four columns of a tile that came in parts, the parts in their order, eight under way at a time.
+__device__ __forceinline__ float4 joined(const float* partial, const Schedule& sc, int tile_floats, int other, int r, int c) {
+    const float* const p = partial + static_cast<int64_t>(other) * sc.parts * tile_floats + r * kProdTile + c;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s = 0; s < sc.parts; s += 8) {
+        float4 x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            x[u] = s + u < sc.parts ? __ldcs(reinterpret_cast<const float4*>(p + static_cast<int64_t>(s + u) * tile_floats)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v.x += x[u].x, v.y += x[u].y, v.z += x[u].z, v.w += x[u].w;
+    }
+    return v;
+}
+
+// dx of the chunk's rows, from their sums to their places, and the totals of few rows: by `warps` warps, this the warp-th.
+template <typename T>
+__device__ __forceinline__ void finish_dx(const Head& a, const Product& p, int warp, int warps, int lane) {
+    const Schedule sc = schedule_of(p);
+    const int64_t here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
+    if (a.few && warp == 0) few_totals(a, *a.live, lane);
+    const int pieces = (a.width + 127) / 128;  // a warp takes 128 columns of a row
+    for (int64_t i = warp; i < here * pieces; i += warps) {
+        const int64_t r = i / pieces;
+        const int c = static_cast<int>(i - r * pieces) * 128 + 4 * lane;
+        if (c >= a.width) continue;
+        T* const dst = static_cast<T*>(a.dx) + a.index[a.first + r] * a.dx_stride + c;
+        const int tile = c / kProdTile * sc.tiles_m + static_cast<int>(r / p.tile_m);
+        const float4 v = tile < sc.whole ? *reinterpret_cast<const float4*>(a.acc + r * a.width_ld + c)
+                                         : joined(a.partial, sc, p.tile_m * kProdTile, tile - sc.whole, static_cast<int>(r % p.tile_m), c % kProdTile);
+        if (a.dx_vectors && c + 4 <= a.width) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = v;
+            else *reinterpret_cast<uint2*>(dst) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+        } else {
+            const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < a.width) Elem<T>::store(dst + j, e[j]);
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) head_dx_kernel(const __grid_constant__ Head a, const __grid_constant__ Product p) {
+    next_may_begin();
+    after_previous();
+    finish_dx<T>(a, p, blockIdx.x * 8 + (threadIdx.x >> 5), gridDim.x * 8, threadIdx.x & 31);
+}
+
+struct Finish {
+    Head a;
+    Product p;  // of dx
+    int f32;
+};
+
+// OUT16: to.bf16, else to.f32. BEFORE: with to.before. DX: while the first sums of dW form, dx is finished.
+template <bool OUT16, bool BEFORE, bool DX>
 struct Gradient {
-    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE, kAhead = true;
+    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE, kBefore = DX, kAhead = true;
     struct Fetched {
         float4 before[BEFORE ? 8 : 1];
     };
     Dest to;
     float* partial;
     int part_floats;
+    Finish dx;
+
+    __device__ __forceinline__ void before(int warp, int lane) const {
+        const int at = blockIdx.x * (kProdOut / 32) + warp, all = gridDim.x * (kProdOut / 32);
+        if (dx.f32) finish_dx<float>(dx.a, dx.p, at, all, lane);
+        else finish_dx<uint16_t>(dx.a, dx.p, at, all, lane);
+    }
 
     struct Tile {
         char* p;       // this lane's first row, at its first column
@@ -532,21 +697,6 @@ struct Gradient {
     };
 };
 
-// Four columns of a tile that came in parts, the parts in their order, eight under way at a time.
-__device__ __forceinline__ float4 joined(const float* partial, const Schedule& sc, int tile_floats, int other, int r, int c) {
-    const float* const p = partial + static_cast<int64_t>(other) * sc.parts * tile_floats + r * kProdTile + c;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s = 0; s < sc.parts; s += 8) {
-        float4 x[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            x[u] = s + u < sc.parts ? __ldcs(reinterpret_cast<const float4*>(p + static_cast<int64_t>(s + u) * tile_floats)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v.x += x[u].x, v.y += x[u].y, v.z += x[u].z, v.w += x[u].w;
-    }
-    return v;
-}
-
 // dW of the tiles that came in parts.
 __global__ void __launch_bounds__(256) head_join_kernel(const __grid_constant__ Product p, const __grid_constant__ Dest to, const float* partial) {
     next_may_begin();
@@ -557,35 +707,6 @@ __global__ void __launch_bounds__(256) head_join_kernel(const __grid_constant__ 
         const ProdUnit u = prod_unit(p, sc, sc.whole + other * sc.parts);
         const int r = u.m0 + i / kProdTile, c = u.n0 + i % kProdTile;
         if (r < sc.m && c < p.n) to.put(r, c, joined(partial, sc, kTileFloats, other, i / kProdTile, i % kProdTile), to.earlier(r, c), to.add);
-    }
-}
-
-// dx of the chunk's rows, from their sums to their places.
-template <typename T>
-__global__ void __launch_bounds__(256) head_dx_kernel(const __grid_constant__ Head a, const __grid_constant__ Product p) {
-    next_may_begin();
-    after_previous();
-    const int lane = threadIdx.x & 31;
-    const Schedule sc = schedule_of(p);
-    const int64_t here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
-    const int pieces = (a.width + 127) / 128;  // a warp takes 128 columns of a row
-    for (int64_t i = blockIdx.x * 8 + (threadIdx.x >> 5); i < here * pieces; i += gridDim.x * 8) {
-        const int64_t r = i / pieces;
-        const int c = static_cast<int>(i - r * pieces) * 128 + 4 * lane;
-        if (c >= a.width) continue;
-        T* const dst = static_cast<T*>(a.dx) + a.index[a.first + r] * a.dx_stride + c;
-        const int tile = c / kProdTile * sc.tiles_m + static_cast<int>(r / p.tile_m);
-        const float4 v = tile < sc.whole ? *reinterpret_cast<const float4*>(a.acc + r * a.width_ld + c)
-                                         : joined(a.partial, sc, p.tile_m * kProdTile, tile - sc.whole, static_cast<int>(r % p.tile_m), c % kProdTile);
-        if (a.dx_vectors && c + 4 <= a.width) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = v;
-            else *reinterpret_cast<uint2*>(dst) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
-        } else {
-            const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < a.width) Elem<T>::store(dst + j, e[j]);
-        }
     }
 }
 
@@ -611,7 +732,7 @@ inline int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 struct Layout {
     bool f32, dx, dw, stage_w, sums_w;  // sums_w: dW of bf16 from several chunks
     int64_t planes, width_ld, e_ld, n_parts, chunks, chunk_rows, row_cap;
-    int64_t index, target, live, rows_f32, gathered, staged_w, parts, e, p, acc, w32, partial, bytes;
+    int64_t index, target, live, rows_f32, gathered, staged_w, parts, e, p, acc, w32, partial, partial_w, bytes;
 };
 
 int layout_of(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_t width, int64_t vocab, bool dx, bool dw, ss_dtype dw_dt, Layout* l) {
@@ -644,7 +765,9 @@ int layout_of(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_
     l->p = l->f32 && (dx || dw) ? place(kTerms * l->chunk_rows * l->e_ld * 2) : l->e;
     l->acc = place(dx ? l->chunk_rows * l->width_ld * 4 : 0);
     l->w32 = place(l->sums_w ? vocab * l->width_ld * 4 : 0);
-    l->partial = place(dx || dw ? static_cast<int64_t>(plan_sms() / 2) * kTileFloats * 4 : 0);
+    // dx is finished while parts of dW are written already
+    l->partial = place(dx ? static_cast<int64_t>(plan_sms() / 2) * kTileFloats * 4 : 0);
+    l->partial_w = place(dw ? static_cast<int64_t>(plan_sms() / 2) * kTileFloats * 4 : 0);
     l->bytes = at;
     return SS_OK;
 }
@@ -688,9 +811,14 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
     if (status == SS_OK && l.dx) status = map_operand(&w_rows, w, true, width, vocab, w_row, l.planes, w_plane, true);
     if (status != SS_OK) return status;
 
-    e = launch_next(false, head_rows_kernel, 1, 1024, st, a);
-    if (e == cudaSuccess) e = l.f32 ? launch_next(true, head_gather_kernel<float>, blocks_for((rows + kProdK) * ((width + kGatherCols - 1) / kGatherCols), sms), 256, st, a)
-                                    : launch_next(true, head_gather_kernel<uint16_t>, blocks_for((rows + kProdK) * ((width + kGatherCols - 1) / kGatherCols), sms), 256, st, a);
+    a.few = rows <= kFewRows;
+    const unsigned gather = blocks_for((rows + kProdK) * ((width + kGatherCols - 1) / kGatherCols), sms);
+    if (a.few) {
+        e = l.f32 ? launch_next(false, head_gather_kernel<float, true>, gather, 256, st, a) : launch_next(false, head_gather_kernel<uint16_t, true>, gather, 256, st, a);
+    } else {
+        e = launch_next(false, head_rows_kernel, 1, 1024, st, a);
+        if (e == cudaSuccess) e = l.f32 ? launch_next(true, head_gather_kernel<float, false>, gather, 256, st, a) : launch_next(true, head_gather_kernel<uint16_t, false>, gather, 256, st, a);
+    }
     if (e == cudaSuccess && l.stage_w) e = l.f32 ? launch_next(true, head_stage_w_kernel<float>, blocks_for(vocab, sms), 256, st, a)
                                                  : launch_next(true, head_stage_w_kernel<uint16_t>, blocks_for(vocab, sms), 256, st, a);
     if (e != cudaSuccess) return cuda_status_public(e);
@@ -714,24 +842,30 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
                         l.e_ld, a.n_parts, a.vocab, a.k};
         status = launch_product<Logits, false, false>(x_cols, w_cols, pz, ez, st);
         if (status != SS_OK) return status;
-        e = launch_next(true, head_statistics_kernel, blocks_for(l.chunk_rows, sms), 256, st, a);
-        if (e != cudaSuccess) return cuda_status_public(e);
-        if (!grads) continue;
+        if (!grads || !a.few) {
+            e = launch_next(true, head_statistics_kernel, blocks_for(l.chunk_rows, sms), 256, st, a);
+            if (e != cudaSuccess) return cuda_status_public(e);
+            if (!grads) continue;
+        }
         const int64_t wide = 256 * 8 * kGradientPieces;
-        const dim3 grid(static_cast<unsigned>((l.e_ld + wide - 1) / wide), static_cast<unsigned>(l.chunk_rows + (i + 1 == l.chunks)));
-        e = l.f32 ? launch_next(true, head_gradient_kernel<true>, grid, 256, st, a) : launch_next(true, head_gradient_kernel<false>, grid, 256, st, a);
+        const dim3 grid(static_cast<unsigned>((l.e_ld + wide - 1) / wide), static_cast<unsigned>(l.chunk_rows + (i + 1 == l.chunks && !a.few)));
+        if (a.few) e = l.f32 ? launch_next(true, head_gradient_kernel<true, true>, grid, 256, st, a) : launch_next(true, head_gradient_kernel<false, true>, grid, 256, st, a);
+        else e = l.f32 ? launch_next(true, head_gradient_kernel<true, false>, grid, 256, st, a) : launch_next(true, head_gradient_kernel<false, false>, grid, 256, st, a);
         if (e != cudaSuccess) return cuda_status_public(e);
+        Product px{};
         if (l.dx) {
-            Product px = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, width, vocab, l.f32, sms);
+            px = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, width, vocab, l.f32, sms);
             px.chunk = l.f32 ? kGradChunkF32 : kGradChunk, px.m_fast = 1, px.follows = 1, px.live = a.live, px.live_from = a.first, px.live_side = 1;
             px.split = 1;
             alone(px, sms);
-            const Gradient<false, false> ex{{a.acc, nullptr, nullptr, l.width_ld, 0, a.width, 1, 0, 0}, a.partial, px.tile_m * kProdTile};
-            status = launch_product<Gradient<false, false>, false, true>(p_cols, w_rows, px, ex, st);
+            const Gradient<false, false, false> ex{{a.acc, nullptr, nullptr, l.width_ld, 0, a.width, 1, 0, 0}, a.partial, px.tile_m * kProdTile, {}};
+            status = launch_product<Gradient<false, false, false>, false, true>(p_cols, w_rows, px, ex, st);
             if (status != SS_OK) return status;
-            e = l.f32 ? launch_next(true, head_dx_kernel<float>, blocks_for(px.m * ((width + 127) / 128), sms), 256, st, a, px)
-                      : launch_next(true, head_dx_kernel<uint16_t>, blocks_for(px.m * ((width + 127) / 128), sms), 256, st, a, px);
-            if (e != cudaSuccess) return cuda_status_public(e);
+            if (!l.dw) {
+                const unsigned finish = blocks_for(px.m * ((width + 127) / 128), sms);
+                e = l.f32 ? launch_next(true, head_dx_kernel<float>, finish, 256, st, a, px) : launch_next(true, head_dx_kernel<uint16_t>, finish, 256, st, a, px);
+                if (e != cudaSuccess) return cuda_status_public(e);
+            }
         }
         if (l.dw) {
             Product pw = product_of(vocab, width, l.chunk_rows, l.f32, sms);
@@ -748,17 +882,28 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
             }
             // a bf16 result is written once: its rows, at most kMostChunkRows, are one chunk
             pw.chunk = l.f32 ? kGradChunkF32 : kGradChunk;
-            if (to.bf16 == nullptr) status = launch_product<Gradient<false, false>, true, true>(p_rows, x_rows, pw, Gradient<false, false>{to, a.partial, kTileFloats}, st);
-            else if (to.before == nullptr) status = launch_product<Gradient<true, false>, true, true>(p_rows, x_rows, pw, Gradient<true, false>{to, a.partial, kTileFloats}, st);
-            else status = launch_product<Gradient<true, true>, true, true>(p_rows, x_rows, pw, Gradient<true, true>{to, a.partial, kTileFloats}, st);
+            float* const parts = reinterpret_cast<float*>(ws + l.partial_w);
+            auto product = [&](auto g) {
+                using G = decltype(g);
+                g.to = to, g.partial = parts, g.part_floats = kTileFloats;
+                if (l.dx) g.dx = Finish{a, px, l.f32};
+                return launch_product<G, true, true>(p_rows, x_rows, pw, g, st);
+            };
+            auto of = [&](auto with) {
+                constexpr bool kDx = decltype(with)::value;
+                return to.bf16 == nullptr ? product(Gradient<false, false, kDx>{}) : (to.before == nullptr ? product(Gradient<true, false, kDx>{}) : product(Gradient<true, true, kDx>{}));
+            };
+            status = l.dx ? of(std::true_type{}) : of(std::false_type{});
             if (status != SS_OK) return status;
             if (may_split(pw)) {
-                e = launch_next(true, head_join_kernel, dim3(static_cast<unsigned>(sms / 2), kTileFloats / 1024), 256, st, pw, to, static_cast<const float*>(a.partial));
+                e = launch_next(true, head_join_kernel, dim3(static_cast<unsigned>(sms / 2), kTileFloats / 1024), 256, st, pw, to, static_cast<const float*>(parts));
                 if (e != cudaSuccess) return cuda_status_public(e);
             }
         }
     }
-    return grads ? SS_OK : cuda_status_public(launch_next(true, head_totals_kernel, 1, 256, st, a, 0));
+    // with gradients formed beside them already
+    if (grads && (!a.few || l.dx)) return SS_OK;
+    return cuda_status_public(launch_next(true, head_totals_kernel, 1, 256, st, a, 0));
 }
 
 }  // namespace

@@ -38,7 +38,7 @@ __device__ __forceinline__ float4 float4_of(uint2 h) {
 // out = c sums (+ b lin), symmetric: a square of a tile above the diagonal is stored a second time, mirrored.
 template <bool LIN>
 struct Symmetric {
-    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kAhead = true;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kBefore = false, kAhead = true;
     static constexpr int kSmallBlocks = 2;
     struct Fetched {
         uint2 lin[LIN ? 8 : 1];
@@ -106,7 +106,7 @@ struct Carried {
 __device__ __forceinline__ float4 next_of(float a, float4 sums, float4 x) { return make_float4(a * x.x + sums.x, a * x.y + sums.y, a * x.z + sums.z, a * x.w + sums.w); }
 
 struct Next {
-    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kAhead = true;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kBefore = false, kAhead = true;
     static constexpr int kSmallBlocks = 2;
     struct Fetched {
         float4 x[8];
@@ -148,7 +148,7 @@ enum { kToF32, kToBf16, kToParam };
 // The last step's result, to the caller: O, or the parameter moved by it.
 template <int TO>
 struct Result {
-    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kAhead = TO != kToParam;
+    static constexpr bool kWhole = false, kSmall = true, kAlone = false, kPacks = false, kBefore = false, kAhead = TO != kToParam;
     static constexpr int kSmallBlocks = TO == kToParam ? 1 : 2;
     struct Fetched {
         float4 x[8], p[TO == kToParam ? 8 : 1];

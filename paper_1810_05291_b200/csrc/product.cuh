@@ -188,7 +188,7 @@ constexpr uint32_t kNanBits = 0x7FC00000u;
 // registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
 // square(column, ..., its sums, first chunk?). With EPI::kPacks a tile may take 64 columns at a time, rounded to 16 bits:
-// packed(column, ...). EPI::kAhead: registers allow two squares' fetches. EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
+// packed(column, ...). EPI::kBefore: before(...) is work for the outgoing warps while the first sums form. EPI::kAhead: registers allow two squares' fetches. EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
 template <class EPI, bool A_MN, bool B_MN, bool PAIR>
 __global__ void __launch_bounds__(kProdThreads, 1)
@@ -243,6 +243,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         };
         uint32_t chunk = 0;
         bool ok = true;
+        if constexpr (EPI::kBefore) epi.before(warp, lane);
         for (int unit = pair; unit < sc.units; unit += pairs) {
             const ProdUnit u = prod_unit(p, sc, unit);
             const int row = u.m0 + row_local, col = u.n0 + col_local;

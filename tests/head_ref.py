@@ -27,7 +27,8 @@ def head_bounds(x, w, y, k, want, c, z_coef, scale, dw_half):
     ax, aw = want["x"].abs(), w.double().abs()
     rows, (vocab, width), unit = x.shape[0], w.shape, 2.0 ** -23
     size = (ax @ aw.t()).amax(1)
-    e = 4 * (16 + passes * width / 256) * unit * size
+    n = passes * width
+    e = 4 * (min(n, 1024) / 16 + n / 1024) * unit * size
     logp = 2 * c * e + 2.0 ** -15 + 2.0 ** -22 * want["lse"].abs()
     kk = want["k"].abs()
     totals = torch.stack([(kk * logp).sum() + abs(z_coef) * (kk * 2 * want["lse"].abs() * logp).sum(), (kk * 2 * want["lse"].abs() * logp).sum()])

@@ -1,8 +1,8 @@
 """Softmax cross entropy at the head on the GPU, against the formulas in 64 bits.
 
-Tolerances. With T the largest sum |x| |w| of a row's logits: the matrix unit truncates each of the 16 steps of a
-chunk of 256 contraction indices, by less than 2^-23 of what it has summed (four times that is allowed for its inner
-alignment), and a chunk is added with half a unit; so a logit is off by E = 4 (16 + n / 256) 2^-23 T, n the
+Tolerances. With T the largest sum |x| |w| of a row's logits: the matrix unit truncates each of the 64 steps of a
+chunk of 1024 contraction indices, by less than 2^-23 of what it has summed (four times that is allowed for its inner
+alignment), and a chunk is added with half a unit; so a logit is off by E = 4 (min(n, 1024) / 16 + n / 1024) 2^-23 T, n the
 contraction indices of all passes. log p adds the hardware's exponentials (2^-22 each) and sums of up to 128 of
 them, then of parts: 2^-15. An entry of P is off by 2^-11 (e in fp16) and 2^-8 (P in bf16) of itself for bf16
 inputs, and by 2^-25 of the row's factor where e is below fp16's normal range; the target's by log p's error.
