@@ -688,9 +688,13 @@ def _one_device(tensors) -> int:
 
 def _on_its_device(call):
     """A call whose tensors are on another GPU than the current one is made there (its workspace, its stream)."""
+    name = call.__code__.co_varnames[0]
+
     @functools.wraps(call)
     def made(*args, **kwargs):
-        first = args[0][0] if isinstance(args[0], (list, tuple)) and len(args[0]) else args[0]
+        first = args[0] if args else kwargs.get(name)
+        if isinstance(first, (list, tuple)) and first:
+            first = first[0]
         device = first.get_device() if isinstance(first, torch.Tensor) else -1
         if device < 0 or device == torch.cuda.current_device():
             return call(*args, **kwargs)

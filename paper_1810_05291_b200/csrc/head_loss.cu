@@ -163,7 +163,8 @@ __device__ __forceinline__ void stage_row(const T* src, uint16_t* dst, int64_t p
 
 constexpr int kGatherCols = 512;  // that a warp takes of a row
 
-// Rows that count gathered; behind them zeros up to a whole stage, since dW sums over whole stages; the results of the others.
+// Rows that count gathered; behind them zeros up to a whole stage, since dW sums over whole stages, and for a first stage of
+// each chunk; the results of the others.
 // FEW: at most kFewRows, which each block finds by itself; the first one writes down what follows needs.
 constexpr int kFewRows = 1024;
 
@@ -214,12 +215,11 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant_
     }
     const int lane = threadIdx.x & 31;
     const int64_t padded = (live + kProdK - 1) / kProdK * kProdK, plane = a.row_cap * a.width_ld;
-    const int64_t upto = padded > kProdK ? padded : kProdK;
     const int pieces = (a.width + kGatherCols - 1) / kGatherCols;
     for (int64_t j = blockIdx.x * 8 + (threadIdx.x >> 5); j < (a.rows + kProdK) * pieces; j += gridDim.x * 8) {
         const int64_t i = j / pieces;
         const int first = static_cast<int>(j - i * pieces) * kGatherCols, n = min(kGatherCols, a.width - first);
-        if (i < upto) {
+        if (i < padded || (i < a.row_cap && i % a.chunk_rows < kProdK)) {
             uint16_t* const dst = a.gathered + i * a.width_ld + first;
             if (i < live) {
                 stage_row(static_cast<const T*>(a.x) + index[i] * a.x_stride + first, dst, plane, n, a.vectors, lane);
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(256) head_totals_kernel(const __grid_constant_
 }
 
 // e -> P: four times eight columns to a thread, all loads before the first store. Rows behind the last up to a whole stage
-// become zeros. A row of blocks behind all rows, where the call's last chunk has it, forms the totals. FEW: the row's
+// (one at least) become zeros. A row of blocks behind all rows, where the call's last chunk has it, forms the totals. FEW: the row's
 // statistics are formed here, by each of its blocks, instead of by a launch of their own.
 constexpr int kGradientPieces = 4;
 
@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(256) head_gradient_kernel(const __grid_constan
         return;
     }
     const int64_t r = blockIdx.y, here = min(static_cast<int64_t>(*a.live) - a.first, a.chunk_rows);
-    const int64_t upto = max((here + kProdK - 1) / kProdK * kProdK, static_cast<int64_t>(a.first == 0 ? kProdK : 0));
+    const int64_t upto = max((here + kProdK - 1) / kProdK * kProdK, static_cast<int64_t>(kProdK));
     const int c0 = blockIdx.x * (256 * 8 * kGradientPieces) + threadIdx.x * 8, end = static_cast<int>(a.e_ld);
     if (r >= min(upto, a.chunk_rows)) return;
     uint16_t* const out = a.p16 + r * a.e_ld;
@@ -871,6 +871,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
             Product pw = product_of(vocab, width, l.chunk_rows, l.f32, sms);
             pw.follows = 1, pw.live = a.live, pw.live_from = a.first, pw.live_side = 2, pw.split = 1;
             Dest to{};
+            pw.always = l.sums_w && i + 1 == l.chunks;  // it rounds what the chunks before it summed
             to.cols = a.width, to.add = accumulate || i > 0, to.stride = dw_stride, to.vectors = dw_vectors, to.wide = dw_wide;
             float* const sums = l.sums_w ? reinterpret_cast<float*>(ws + l.w32) : nullptr;
             if (l.sums_w && i + 1 < l.chunks) {

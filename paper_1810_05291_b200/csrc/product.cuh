@@ -52,7 +52,8 @@ struct Product {
     int follows;      // another kernel of the call goes before
     const int* live;  // rows that there are (all of the call's), or NULL
     int live_from;    // the first of them that is meant here
-    int live_side;    // 1: they are m; 2: they are k (at the call's start one stage at least, whose rows are zeros)
+    int live_side;    // 1: they are m; 2: they are k
+    int always;       // C is formed where no row is live, too, from a stage of zeros, as it is for the call's first rows
 };
 
 inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms, int sms) {
@@ -88,7 +89,7 @@ __device__ __forceinline__ Schedule schedule_of(const Product& p) {
     bool any = true;
     if (p.live != nullptr) {
         const int live = max(*p.live - p.live_from, 0);
-        any = live > 0 || p.live_from == 0;
+        any = live > 0 || p.live_from == 0 || p.always;
         if (p.live_side == 1) m = min(m, live);
         else k = max(min(k, live), 1);
     }

@@ -18,6 +18,7 @@ hyper-parameter tables only; the arithmetic is in the kernels.
 
 from __future__ import annotations
 
+import math
 from typing import Optional
 
 import torch
@@ -147,3 +148,88 @@ class SignumVote(torch.optim.Optimizer):
                     mv.copy_(loaded)
                 self.state[p]["momentum_buffer"] = mv
         self._table = None                       # the groups' hyper-parameters may have changed: re-upload at the next step
+
+
+class OrthogonalMomentum(torch.optim.Optimizer):
+    """Steps of matrices along their momentum with all singular values drawn towards 1 (Newton-Schulz steps), where
+    ``SignumVote`` steps along the sign of each coordinate:
+
+        v <- (1 - beta) g + beta v,   u = v, or (1 - beta) g + beta v with ``nesterov``
+        p <- p - lr (scale O(u) + weight_decay p)
+
+    For the weights of linear layers and convolutions (a parameter of more than two dimensions is the matrix of its first
+    by all others); embeddings, heads and vectors are ``SignumVote``'s. ``scale``: ``"rms"``, 0.2 sqrt(max(rows, cols)), which
+    gives the step the size of a step of Adam (0.2 a coordinate); ``"spectral"``, sqrt(max(1, rows / cols)); or a number.
+    ``coefficients``: (a, b, c) of each Newton-Schulz step.
+
+    Parameters are float32 and stay where they are; matrices of one shape and layout go through one call. A parameter
+    without a gradient is left as it is. The gradients are taken as they are: workers of a group average theirs first.
+    ``kernels`` replaces the CUDA binding (host-side tests)."""
+
+    def __init__(self, params, lr: float = 3e-4, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                 scale="rms", coefficients=None, kernels=None):
+        if not (lr >= 0.0 and weight_decay >= 0.0 and 0.0 <= momentum < 1.0):
+            raise ValueError("need lr >= 0, weight_decay >= 0 and 0 <= momentum < 1")
+        if scale not in ("rms", "spectral") and not isinstance(scale, (int, float)):
+            raise ValueError("scale must be 'rms', 'spectral' or a number")
+        super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, scale=scale))
+        if kernels is None:
+            from . import binding as kernels
+            kernels.lib()
+        self.B = kernels
+        self.coefficients = kernels.ORTHO_COEFFICIENTS if coefficients is None else tuple(tuple(map(float, c)) for c in coefficients)
+        for g in self.param_groups:
+            for p in g["params"]:
+                if p.dtype != torch.float32 or p.dim() < 2:
+                    raise ValueError("parameters must be float32 matrices, or tensors of more dimensions")
+                if self._matrix(p.data) is None:
+                    raise ValueError("a parameter's rows must be contiguous and not overlap")
+
+    @staticmethod
+    def _matrix(t: torch.Tensor) -> Optional[torch.Tensor]:
+        """``t`` as a matrix of its first dimension by all others, in place; None where memory does not have it so."""
+        if t.dim() > 2:
+            if not t.is_contiguous():
+                return None
+            t = t.view(t.shape[0], -1)
+        fits = (t.stride(1) == 1 or t.shape[1] < 2) and (t.stride(0) >= t.shape[1] or t.shape[0] < 2)
+        return t if fits else None
+
+    @staticmethod
+    def _scale(scale, rows: int, cols: int) -> float:
+        if scale == "rms":
+            return 0.2 * math.sqrt(max(rows, cols))
+        if scale == "spectral":
+            return math.sqrt(max(1.0, rows / max(cols, 1)))
+        return float(scale)
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            alike = {}
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise RuntimeError("gradients must be dense")
+                state = self.state[p]
+                if "momentum_buffer" not in state:
+                    state["momentum_buffer"] = torch.zeros_like(p, memory_format=torch.contiguous_format)
+                m = self._matrix(p.data)
+                g, v = self._matrix(p.grad), self._matrix(state["momentum_buffer"])
+                if g is None:
+                    g = p.grad.reshape(m.shape).contiguous()
+                if v is None:
+                    raise RuntimeError("the momentum of a parameter must be laid out as a matrix")
+                key = (tuple(m.shape), m.stride(0), g.dtype, g.stride(0), v.stride(0), m.device)
+                alike.setdefault(key, []).append((g, v, m))
+            for (shape, *_), found in alike.items():
+                for at in range(0, len(found), self.B.SS_ORTHO_MAX_MATRICES):
+                    g, v, m = (list(ts) for ts in zip(*found[at:at + self.B.SS_ORTHO_MAX_MATRICES]))
+                    self.B.ss_orthogonal_update(g, v, v, m, m, group["momentum"], group["nesterov"], self.coefficients,
+                                                group["lr"], self._scale(group["scale"], *shape), group["weight_decay"])
+        return loss

@@ -1,9 +1,10 @@
 """The training operators as autograd functions: linear layers and activations that keep their
-inputs in 8 bits for the backward pass, and losses over logits.
+inputs in 8 bits for the backward pass, losses over logits, and the loss at the head that takes the
+product with the head's weight in.
 
 They make the gradients that ``optim.SignumVote`` compresses: a linear layer's weight gradient goes
 to the parameter's ``grad``, which under ``SignumVote`` is a view of the flat buffer that the vote
-reads, through autograd or, where the layer is asked to, straight. Matrix products with
+reads, through autograd or, where the layer is asked to, straight. The layers' matrix products with
 the weights are PyTorch's; everything else of the two passes is in the kernels of ``binding``
 (``include/signsgd_train.h`` has the formulas). The kernels have no second derivatives: a backward
 pass through the backward pass raises.
@@ -246,6 +247,66 @@ class _PreferenceLoss(torch.autograd.Function):
         dz = torch.empty_like(args[0])
         B.ss_preference_loss(*args, *_preference_outputs(args), dz, grad_scale=g.reshape(1).float(), **ctx.options)
         return dz.view(ctx.shape), None, None, None, None, None
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, targets, weights, inv_temperature, z_coef, into_grad, want_dx, want_dw):
+        ctx.set_materialize_grads(False)
+        m, w = _rows(x), _rows(weight.to(x.dtype))
+        totals, logp = torch.empty(2, device=m.device), torch.empty(m.shape[0], device=m.device)
+        dx = torch.empty(m.shape, dtype=m.dtype, device=m.device) if want_dx else None
+        dw = torch.empty(w.shape, dtype=weight.dtype if m.dtype is torch.bfloat16 else torch.float32, device=m.device) if want_dw else None
+        B.ss_linear_cross_entropy(m, w, targets, weights, totals, logp, dx, dw, inv_temperature=inv_temperature, z_coef=z_coef)
+        ctx.weight, ctx.shape, ctx.into_grad = weight, x.shape, into_grad
+        ctx.save_for_backward(dx, dw)
+        loss, square = totals[0].clone(), totals[1].clone()
+        ctx.mark_non_differentiable(square, logp)
+        return loss, square, logp
+
+    @staticmethod
+    @_first_derivative
+    def backward(ctx, g, *_):
+        (dx, dw), weight, g = ctx.saved_tensors, ctx.weight, g.float()
+        if dx is not None:
+            dx = _times(dx, g, dx.dtype).view(ctx.shape)
+        if dw is not None:
+            into = _grad_buffer(ctx, weight) if ctx.into_grad and dw.dtype is torch.float32 else None
+            if into is not None:
+                with _in_order(ctx.next_functions[1][0], into):
+                    into.addcmul_(dw, g)
+                dw = None
+            else:
+                dw = _times(dw, g, weight.dtype)
+        return dx, dw, None, None, None, None, None, None, None
+
+
+def _times(t: torch.Tensor, g: torch.Tensor, dtype) -> torch.Tensor:
+    """``t * g`` in 32 bits, rounded once; some rows at a time, so that no 32-bit copy of a large gradient is made. (A
+    product of a bfloat16 tensor and a scalar in device memory would round the scalar first.)"""
+    if t.dtype is torch.float32 and dtype is torch.float32:
+        return t * g
+    out = torch.empty(t.shape, dtype=dtype, device=t.device)
+    step = max(1, (1 << 26) // max(t.shape[1], 1))
+    for a, b in zip(t.split(step), out.split(step)):
+        b.copy_(a.float() * g)
+    return out
+
+
+def linear_cross_entropy(x, weight, targets, weights, inv_temperature: float = 1.0, z_coef: float = 0.0, into_grad: bool = False):
+    """Softmax cross entropy of ``x @ weight.T`` at ``targets``, each position counting ``weights``, whose logits are never
+    kept. ``x``: [..., width] bfloat16 or float32; ``weight``: [vocab, width] float32 or bfloat16, used in ``x``'s type
+    (under autocast both in the region's); ``targets``, ``weights``: one for each position. Returns the loss, the weighted
+    sum of lse^2 (``z_coef`` times it is in the loss) and the positions' log probabilities.
+
+    Where gradients can be asked for they are formed with the loss, in one go: that takes three products with the
+    head, where forming the logits again in the backward pass would take four. The backward pass multiplies them by the
+    gradient that arrives. With ``into_grad`` it adds the weight's to ``weight.grad`` itself, as in ``linear8``."""
+    if torch.is_autocast_enabled(x.device.type) and x.dtype != torch.float64:
+        x = x.to(torch.get_autocast_dtype(x.device.type))
+    on = torch.is_grad_enabled()
+    return _LinearCrossEntropy.apply(x, weight, targets.reshape(-1), weights.reshape(-1), inv_temperature, z_coef, into_grad,
+                                     on and x.requires_grad, on and weight.requires_grad)
 
 
 def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, kl_coef: float = 0.0,
