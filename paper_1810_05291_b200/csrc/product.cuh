@@ -137,11 +137,17 @@ __device__ __forceinline__ ProdUnit prod_unit(const Product& p, const Schedule& 
     } else if (p.m_fast) {
         j = t / s.tiles_m, i = t - j * s.tiles_m;
     } else {
-        i = t / s.tiles_n, j = t - i * s.tiles_n;
+        // tiles with fewer columns come last, spread over all pairs; in their places they could all fall to some
+        const int full = p.n % kProdTile == 0 || s.tiles_n == 1 ? s.tiles_n : s.tiles_n - 1;
+        if (t < s.tiles_m * full) i = t / full, j = t - i * full;
+        else i = t - s.tiles_m * full, j = full;
     }
     r.m0 = i * p.tile_m, r.n0 = j * kProdTile;
     return r;
 }
+
+// Columns that are formed of a tile: those that C has, up to a multiple of 32 (of 16 for each block of a pair).
+__device__ __forceinline__ int tile_cols(const Product& p, const ProdUnit& u) { return min(kProdTile, (p.n - u.n0 + 31) / 32 * 32); }
 
 struct ProdShared {
     uint64_t full[kProdStages], added[2];  // of the first block: by both blocks
@@ -356,7 +362,8 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         uint32_t parity = 1;
         for (int unit = pair; unit < sc.units; unit += pairs) {
             const ProdUnit u = prod_unit(p, sc, unit);
-            const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + rank * kProdHalf;  // PAIR: this block's half of both
+            const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + (PAIR ? rank * (tile_cols(p, u) / 2) : 0);  // PAIR: this block's half of both
+            const bool wide = tile_cols(p, u) > kProdHalf;                                                  // more than one panel of a half, or more than a half
             int pass = u.first / sc.pass_stages, k0 = (u.first - pass * sc.pass_stages) * kProdK;
             const int end = sc.pass_stages * kProdK;
 #pragma unroll 1
@@ -365,7 +372,8 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                 const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
                 const int za = p.passes > 1 ? p.plane_a[pass] : u.batch, zb = p.passes > 1 ? p.plane_b[pass] : u.batch;
                 if (leader) {
-                    if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, (PAIR ? 2 : 1) * kStageBytes);
+                    const uint32_t less = wide ? 0 : (PAIR ? (B_MN ? kProdPanel : 0) : kProdOperand);  // not copied
+                    if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, (PAIR ? 2 : 1) * (kStageBytes - less));
                     if constexpr (A_MN) {
                         load(dst, &a_map, bar, m0, k0, za);
                         load(dst + kProdPanel, &a_map, bar, m0 + 64, k0, za);
@@ -375,9 +383,10 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
 #pragma unroll
                     for (int h = 0; h < (PAIR ? 1 : 2); ++h) {
                         const uint32_t to = dst + (1 + h) * kProdOperand;
+                        if (h == 1 && !wide) break;
                         if constexpr (B_MN) {
                             load(to, &b_map, bar, n0 + h * kProdHalf, k0, zb);
-                            load(to + kProdPanel, &b_map, bar, n0 + h * kProdHalf + 64, k0, zb);
+                            if (!PAIR || wide) load(to + kProdPanel, &b_map, bar, n0 + h * kProdHalf + 64, k0, zb);
                         } else {
                             load(to, &b_map, bar, k0, n0 + h * kProdHalf, zb);
                         }
@@ -398,7 +407,6 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         }
     } else if (rank == 0) {
         // ---- matrix unit
-        const uint32_t idesc = tc_idesc(PAIR ? kProdTile : kProdHalf, kProdTile, p.bf16 != 0, A_MN, B_MN);
         constexpr uint32_t kStep = kStageBytes >> 4, kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
         const uint64_t desc_a = A_MN ? tc_desc_rows(stages, kProdPanel) : tc_desc_cols(stages);
         const uint64_t desc_b = B_MN ? tc_desc_rows(stages + kProdOperand, kProdPanel) : tc_desc_cols(stages + kProdOperand);
@@ -410,7 +418,9 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         };
         uint32_t slot = 0, parity = 0, chunk = 0;
         for (int unit = pair; unit < sc.units; unit += pairs) {
-            for (int left = prod_unit(p, sc, unit).stages; left > 0; left -= p.chunk, ++chunk) {
+            const ProdUnit u = prod_unit(p, sc, unit);
+            const uint32_t idesc = tc_idesc(PAIR ? kProdTile : kProdHalf, tile_cols(p, u), p.bf16 != 0, A_MN, B_MN);
+            for (int left = u.stages; left > 0; left -= p.chunk, ++chunk) {
                 const int n = min(left, p.chunk);
                 const uint32_t d = tmem + (chunk & 1) * kProdTile;
                 // the half of the tensor memory is free once the chunk before the last has been brought out
