@@ -27,7 +27,8 @@ constexpr int kPartCols = kProdHalf;              // logits of a thread
 // Stages that the matrix unit sums of a logit. log p of 8192 x 4096 over 131072 is off by 2.6e-6 with 16 (an fp32 product: 3.1e-6), and by 6e-7 with 4,
 // whose product takes 3.95 ms instead of 3.3 (with 8: 3.5): the two halves of the tensor memory fill while a tile's exponentials are formed.
 constexpr int kLogitChunk = 16;
-// Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16; 2048 lose 5e-7.
+// Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16; 2048 (of each of fp32's
+// passes) lose 5e-7.
 constexpr int kGradChunk = 256, kGradChunkF32 = 32;
 constexpr int64_t kChunkBytes = int64_t(1) << 30; // of e and P
 constexpr int64_t kMostChunkRows = 16384;
@@ -718,7 +719,7 @@ __global__ void __launch_bounds__(256) head_zero_kernel(void* dst, int64_t row_b
 
 // ---- host side -------------------------------------------------------------------------------------
 
-constexpr int64_t kMostRows = int64_t(1) << 24, kMostTilesHead = int64_t(1) << 24;
+constexpr int64_t kMostSideHead = int64_t(1) << 30, kMostRows = int64_t(1) << 24, kMostTilesHead = int64_t(1) << 24;
 
 // SMs that the workspace is made for. Without a device (sizes asked for on a host without one) the B200's.
 int plan_sms() {
@@ -737,7 +738,7 @@ struct Layout {
 
 int layout_of(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_t width, int64_t vocab, bool dx, bool dw, ss_dtype dw_dt, Layout* l) {
     const int64_t tiles_v = (vocab + kProdTile - 1) / kProdTile, tiles_d = (width + kProdTile - 1) / kProdTile;
-    if (rows > kMostRows || tiles_v * ((rows + kProdTile - 1) / kProdTile) > kMostTilesHead || tiles_v * tiles_d > kMostTilesHead) return SS_ERR_UNSUPPORTED;
+    if (rows > kMostRows || vocab > kMostSideHead || width > kMostSideHead || tiles_v * ((rows + kProdTile - 1) / kProdTile) > kMostTilesHead || tiles_v * tiles_d > kMostTilesHead) return SS_ERR_UNSUPPORTED;
     l->f32 = dt == SS_F32, l->dx = dx, l->dw = dw, l->planes = l->f32 ? kTerms : 1;
     const Mat m = mat(w, vocab, width, w_stride, dtype_bytes(dt));
     l->stage_w = l->f32 || !m.row_aligned(16) || m.stride * 2 % 16 != 0 || m.stride * 2 >= (int64_t(1) << 38);
@@ -836,7 +837,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         if (status != SS_OK) return status;
 
         Product pz = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, vocab, width, l.f32, sms);
-        pz.chunk = kLogitChunk, pz.m_fast = 1, pz.follows = 1, pz.live = a.live, pz.live_from = a.first, pz.live_side = 1;
+        pz.block = kLogitChunk, pz.chunk = pz.passes * kLogitChunk, pz.m_fast = 1, pz.follows = 1, pz.live = a.live, pz.live_from = a.first, pz.live_side = 1;
         alone(pz, sms);
         const Logits ez{a.target + first, a.target_logit, a.parts, grads && !l.f32 ? a.e16 : nullptr, grads && l.f32 ? a.e32 : nullptr,
                         l.e_ld, a.n_parts, a.vocab, a.k};
@@ -855,7 +856,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         Product px{};
         if (l.dx) {
             px = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, width, vocab, l.f32, sms);
-            px.chunk = l.f32 ? kGradChunkF32 : kGradChunk, px.m_fast = 1, px.follows = 1, px.live = a.live, px.live_from = a.first, px.live_side = 1;
+            px.block = kGradChunkF32, px.chunk = l.f32 ? px.passes * kGradChunkF32 : kGradChunk, px.m_fast = 1, px.follows = 1, px.live = a.live, px.live_from = a.first, px.live_side = 1;
             px.split = 1;
             alone(px, sms);
             const Gradient<false, false, false> ex{{a.acc, nullptr, nullptr, l.width_ld, 0, a.width, 1, 0, 0}, a.partial, px.tile_m * kProdTile, {}};
@@ -882,7 +883,7 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
                 to.f32 = static_cast<float*>(dw);
             }
             // a bf16 result is written once: its rows, at most kMostChunkRows, are one chunk
-            pw.chunk = l.f32 ? kGradChunkF32 : kGradChunk;
+            pw.block = kGradChunkF32, pw.chunk = l.f32 ? pw.passes * kGradChunkF32 : kGradChunk;
             float* const parts = reinterpret_cast<float*>(ws + l.partial_w);
             auto product = [&](auto g) {
                 using G = decltype(g);

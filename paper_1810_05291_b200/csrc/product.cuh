@@ -8,8 +8,8 @@
 // tiles are swizzled by the copies either way, and nothing is transposed.
 //
 // Operands have 16 bits (bf16 or fp16), sums 32. An fp32 operand goes as three bf16 terms whose sum it is
-// exactly ("planes" of a 3-D tensor map), and a product of two such as six passes, from the
-// smallest terms to the largest; the three that are left out are below 2^-24 of the largest.
+// exactly ("planes" of a 3-D tensor map), and a product of two such as six passes, over some stages at a time, from the
+// smallest terms to the largest, which alone the matrix unit's truncation reaches; the three that are left out are below 2^-24 of the largest.
 #pragma once
 
 #include <cuda.h>
@@ -40,6 +40,7 @@ struct Product {
     int batches;      // matrices one after another (the maps' third coordinate), where passes is 1
     int passes;       // pairs of planes: (plane_a[i], plane_b[i])
     int8_t plane_a[kMostPasses], plane_b[kMostPasses];
+    int block;        // with passes: stages that go through all of them before the next do
     int chunk;        // stages that are summed in tensor memory before they are brought out
     int tile_m;       // rows of a tile: 256 for pairs, 128 for blocks alone
     int pairs;        // of blocks, or blocks alone
@@ -60,7 +61,7 @@ inline Product product_of(int64_t m, int64_t n, int64_t k, bool terms, int sms) 
     Product p{};
     p.tile_m = kProdTile, p.pairs = sms / 2;
     p.m = static_cast<int>(m), p.n = static_cast<int>(n), p.k = static_cast<int>(k);
-    p.batches = 1, p.passes = 1, p.chunk = 1 << 30, p.bf16 = 1;
+    p.batches = 1, p.passes = 1, p.block = 1 << 30, p.chunk = 1 << 30, p.bf16 = 1;
     if (terms) {
         const int8_t a[kMostPasses] = {0, 2, 1, 0, 1, 0}, b[kMostPasses] = {2, 0, 1, 1, 0, 0};
         p.passes = kMostPasses;
@@ -106,6 +107,8 @@ __device__ __forceinline__ Schedule schedule_of(const Product& p) {
         if (parts > 1) {
             s.whole = tiles - others;
             s.part_stages = (s.stages + parts - 1) / parts;
+            const int all = p.passes > 1 ? p.passes * p.block : 1;  // a part begins with the smallest terms, unless it is shorter than a block
+            if (s.part_stages > all) s.part_stages = (s.part_stages + all - 1) / all * all;
             s.parts = (s.stages + s.part_stages - 1) / s.part_stages;
         }
     }
@@ -364,8 +367,13 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
             const ProdUnit u = prod_unit(p, sc, unit);
             const int m0 = u.m0 + rank * kProdHalf, n0 = u.n0 + (PAIR ? rank * (tile_cols(p, u) / 2) : 0);  // PAIR: this block's half of both
             const bool wide = tile_cols(p, u) > kProdHalf;                                                  // more than one panel of a half, or more than a half
-            int pass = u.first / sc.pass_stages, k0 = (u.first - pass * sc.pass_stages) * kProdK;
-            const int end = sc.pass_stages * kProdK;
+            int pass = 0, k0 = u.first * kProdK, begin = 0, end = 0x7FFFFFFF;  // of the block
+            if (p.passes > 1) {
+                const int b = u.first / (p.passes * p.block), r = u.first - b * p.passes * p.block, n = min(p.block, sc.pass_stages - b * p.block);
+                pass = r / n;
+                begin = b * p.block * kProdK, end = begin + n * kProdK;
+                k0 = begin + (r - pass * n) * kProdK;
+            }
 #pragma unroll 1
             for (int s = 0; s < u.stages; ++s) {
                 mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
@@ -394,7 +402,10 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                 }
                 ++it;
                 k0 += kProdK;
-                if (k0 == end) k0 = 0, ++pass;
+                if (k0 == end) {
+                    k0 = begin;
+                    if (++pass == p.passes) pass = 0, k0 = begin = end, end = min(begin + p.block * kProdK, sc.pass_stages * kProdK);
+                }
                 if (++slot == kStages) slot = 0, parity ^= 1;
             }
         }

@@ -218,6 +218,35 @@ def test_head_in_several_pieces():
         assert not bool(t.any())
 
 
+def test_loss_alone_in_several_pieces():
+    c = head_case(40000, 64, 500, seed=4)
+    totals, logp = head_run(*c, grads=False)
+    for a, b in ((0, 700), (700, 17000), (17000, 40000)):
+        assert torch.equal(head_run(c[0][a:b], c[1], c[2][a:b], c[3][a:b], grads=False)[1], logp[a:b])
+    assert abs(float(totals[0]) + float((c[3].double() * logp.double()).sum())) < 1e-6 * float(totals[0].abs())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width,vocab", [(1, 64, 300), (200, 160, 1111), (256, 64, 70000), (257, 130, 5003), (8000, 64, 70000)])
+def test_head_writes_nothing_behind_its_workspace(rows, width, vocab, dtype):
+    x, w, y, k = head_case(rows, width, vocab, dtype)
+    for dwt in {dtype, F32}:
+        need = B.ss_linear_cross_entropy_workspace(w, rows, True, dwt)
+        ws = torch.full((need + 8192,), 171, dtype=torch.uint8, device=DEV)
+        dx, dw = torch.empty_like(x), torch.empty(vocab, width, dtype=dwt, device=DEV)
+        B.ss_linear_cross_entropy(x, w, y, k, torch.empty(2, device=DEV), torch.empty(rows, device=DEV), dx, dw, workspace=ws)
+        assert bool((ws[need:] == 171).all())
+
+
+@pytest.mark.parametrize("shape", [(3, 5), (129, 1), (130, 130), (100, 2049), (333, 257), (2000, 1999), (4100, 140)])
+def test_ortho_writes_nothing_behind_its_workspace(shape):
+    u = [rand(shape, i) for i in range(2)]
+    need = B.ss_orthogonal_workspace(2, *shape)
+    ws = torch.full((need + 8192,), 171, dtype=torch.uint8, device=DEV)
+    B.ss_orthogonalise(u, [torch.empty_like(m) for m in u], workspace=ws)
+    assert bool((ws[need:] == 171).all())
+
+
 def test_head_beyond_2_31_elements():
     """Logits of 2.4e9 and a weight gradient behind 2^31 elements of a wider buffer: a few rows and columns against the formula."""
     rows, width, vocab = 18432, 64, 131072
