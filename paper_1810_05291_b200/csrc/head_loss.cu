@@ -39,6 +39,15 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
+// (a - m) k and (b - m) k, given -m.
+__device__ __forceinline__ float2 sub_mul2(float a, float b, float minus, float k) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, m, k;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 m, {%4, %4};\n\tmov.b64 k, {%5, %5};\n\t"
+        "add.rn.f32x2 x, x, m;\n\tmul.rn.f32x2 x, x, k;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a), "f"(b), "f"(minus), "f"(k));
+    return r;
+}
+
 // What the kernels of one chunk share.
 struct Head {
     const int64_t* targets;
@@ -270,29 +279,34 @@ struct Logits {
     int n_parts, vocab;
     float k;
 
-    __device__ __forceinline__ void whole(const ProdUnit&, int m, int row, int col, int lane, uint32_t buf, float (&z)[kPartCols]) const {
+    // What is needed of the lane's row, while the sums form: its target.
+    __device__ __forceinline__ int ahead(int m, int row, int lane) const { return row + lane < m ? target[row + lane] : -1; }
+
+    __device__ __forceinline__ void whole(const ProdUnit&, int m, int row, int col, int lane, uint32_t buf, float (&z)[kPartCols], int y) const {
         if (row >= m) return;
         const int r = row + lane, there = vocab - col;
         if (there < kPartCols) {
 #pragma unroll
             for (int i = 0; i < kPartCols; ++i) z[i] = i < there ? z[i] : -INFINITY;
         }
-        const int y = r < m ? target[r] - col : -1;
+        y -= col;
         if (y >= 0 && y < kPartCols) {
             float v = 0.0f;
 #pragma unroll
             for (int i = 0; i < kPartCols; ++i) v = i == y ? z[i] : v;
             target_logit[r] = v;
         }
-        float top = z[0], sum = 0.0f;
+        float tops[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-        for (int i = 1; i < kPartCols; ++i) top = fmaxf(top, z[i]);
-        const float from = top == -INFINITY ? 0.0f : top;
+        for (int i = 4; i < kPartCols; ++i) tops[i & 3] = fmaxf(tops[i & 3], z[i]);
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), minus = top == -INFINITY ? 0.0f : -top;
+        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < kPartCols; ++i) {
-            z[i] = ex2((z[i] - from) * k);
-            sum += z[i];
+        for (int i = 0; i < kPartCols; i += 2) {
+            const float2 t = sub_mul2(z[i], z[i + 1], minus, k);
+            sums[i & 2] += z[i] = ex2(t.x), sums[(i & 2) + 1] += z[i + 1] = ex2(t.y);
         }
+        const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
         if (r < m) parts[static_cast<int64_t>(r) * n_parts + col / kPartCols] = make_float2(top, sum);
         if (e16 != nullptr) {
 #pragma unroll
@@ -627,7 +641,7 @@ struct Finish {
 // OUT16: to.bf16, else to.f32. BEFORE: with to.before. DX: while the first sums of dW form, dx is finished.
 template <bool OUT16, bool BEFORE, bool DX>
 struct Gradient {
-    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE, kBefore = DX, kAhead = true;
+    static constexpr bool kWhole = false, kSmall = false, kAlone = !OUT16, kPacks = OUT16 && !BEFORE, kBefore = DX, kAhead = BEFORE;
     struct Fetched {
         float4 before[BEFORE ? 8 : 1];
     };

@@ -195,7 +195,7 @@ __device__ __forceinline__ void square_sums(uint32_t buf, int lane, float4 (&v)[
 constexpr uint32_t kNanBits = 0x7FC00000u;
 
 // EPI brings the sums out. With EPI::kWhole a thread holds 128 columns of a row, summed over all chunks in
-// registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums). Otherwise a warp has an EPI::Tile for its 32 rows and 128
+// registers, and gets them at once: whole(unit, m, row, col, lane, buf, sums, what ahead(m, row, lane) loaded before they had come). Otherwise a warp has an EPI::Tile for its 32 rows and 128
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
 // square(column, ..., its sums, first chunk?). With EPI::kPacks a tile may take 64 columns at a time, rounded to 16 bits:
 // packed(column, ...). EPI::kBefore: before(...) is work for the outgoing warps while the first sums form. EPI::kAhead: registers allow two squares' fetches. EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
@@ -235,9 +235,9 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    if (p.follows) after_previous();
     if constexpr (PAIR) cluster_sync();
     tc_fence_after();
+    if (p.follows) after_previous();
     const uint32_t tmem = sh.tmem;
     const Schedule sc = schedule_of(p);
 
@@ -258,6 +258,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
             const ProdUnit u = prod_unit(p, sc, unit);
             const int row = u.m0 + row_local, col = u.n0 + col_local;
             if constexpr (EPI::kWhole) {
+                const auto ahead = epi.ahead(sc.m, row, lane);
                 float sums[kProdHalf];
 #pragma unroll
                 for (int i = 0; i < kProdHalf; ++i) sums[i] = 0.0f;
@@ -281,12 +282,13 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
 #pragma unroll
                     for (int i = 0; i < kProdHalf; ++i) sums[i] = __uint_as_float(kNanBits);
                 }
-                epi.whole(u, sc.m, row, col, lane, buf, sums);
+                epi.whole(u, sc.m, row, col, lane, buf, sums, ahead);
             } else {
                 bool first = true;
                 const bool any = row < sc.m && col < p.n;
                 typename EPI::Tile tile(epi, u, sc.m, row, col, lane);
-                typename EPI::Fetched f, g;
+                typename EPI::Fetched f;
+                [[maybe_unused]] typename EPI::Fetched g;
                 for (int left = u.stages; left > 0; left -= p.chunk, ++chunk) {
                     if (any) tile.fetch(epi, 0, f);
                     if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed[chunk & 1]), (chunk >> 1) & 1, abort));
@@ -329,19 +331,21 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                         tile.square(epi, j, lane, buf, v, of, first);
                         __syncwarp();
                     };
+                    if constexpr (EPI::kAhead) {
 #pragma unroll 1
-                    for (int j = 0; !done && j < kProdHalf && col + j < p.n; j += 64) {  // what the next square needs is on its way while one is worked on
-                        const bool second = col + j + 32 < p.n, third = j + 64 < kProdHalf && col + j + 64 < p.n;
-                        if (EPI::kAhead && second) tile.fetch(epi, j + 32, g);
-                        square(j, f);
-                        if (!second) break;
-                        if constexpr (EPI::kAhead) {
+                        for (int j = 0; !done && j < kProdHalf && col + j < p.n; j += 64) {  // what the next square needs is on its way while one is worked on
+                            const bool second = col + j + 32 < p.n, third = j + 64 < kProdHalf && col + j + 64 < p.n;
+                            if (second) tile.fetch(epi, j + 32, g);
+                            square(j, f);
+                            if (!second) break;
                             if (third) tile.fetch(epi, j + 64, f);
                             square(j + 32, g);
-                        } else {
-                            tile.fetch(epi, j + 32, f);
-                            square(j + 32, f);
-                            if (third) tile.fetch(epi, j + 64, f);
+                        }
+                    } else {  // less code, all of which the first tile has to wait for
+#pragma unroll 1
+                        for (int j = 0; !done && j < kProdHalf && col + j < p.n; j += 32) {
+                            if (j > 0) tile.fetch(epi, j, f);
+                            square(j, f);
                         }
                     }
                     tc_fence_before();
