@@ -10,9 +10,14 @@
 // would take four; the pass over e costs a few percent of a product.
 //
 // Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 1024 contraction indices and
-// are added in registers, to nearest. e is fp16 (relative to its part's
-// maximum, 11 bits), P is bf16 as the gradient of bf16 logits is; the entry of the target, which is a
-// difference, is formed in fp32 from log p. With fp32 inputs e is fp32 and P the sum of three bf16.
+// are added in registers, to nearest. e is fp16 (relative to its part's maximum, 11 bits), P is bf16 as the gradient
+// of bf16 logits is; the entry of the target, which is a difference, is formed in fp32 from log p. With fp32 inputs e
+// is fp32 and P the sum of three bf16.
+//
+// What bounds it. 8192 x 4096 over 131072 bf16: 19.7 to 22.5 ms at the power limit (1340 to 1170 TFLOP/s; the library's
+// product alone, back to back, 1407), the matrix unit active 91, 93 and 84 % of the logits', dx's and dW's time, e -> P
+// 0.85 ms of it at 5.1 TB/s. 64 x 1024 over 32000 bf16: 69 us in a row of calls, W read twice and dW written in 52 of them, the rest five starts.
+// 1021 x 770 over 32001 fp32: 850 us, six passes in 1300 to 1440 TFLOP/s, 120 us to split W and P into terms.
 #include "product.cuh"
 
 #include <cuda_fp16.h>

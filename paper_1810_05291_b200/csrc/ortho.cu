@@ -9,6 +9,11 @@
 // enlarges 3.4 times; with 11 bits there a momentum of few strong directions comes out 0.35 % off instead of
 // 0.03 %. (As the sum of two fp16, the first of them the operand, X has two bytes less to move for each element and
 // step and 22 bits, but takes seven instructions more: the same time within 2 %.)
+//
+// What bounds it. 4096 x 4096 bf16: 1140 us alone, 1350 in a row of calls at the power limit; S and Q take 52 to 57 us each (136
+// tiles in two rounds of 74 pairs, the matrix unit active 75 %), X + Q X 98 to 105 (79 %), the two passes of the start 42. Twelve of 4096 x 1024
+// with momenta and parameters: 1270 us, X + Q X 125 of them each, where its products alone take 62 and its 600 MB 92.
+// 1000 x 2048: 150 us, 15 products of 8 to 10 us one after another. 128 x 128: 24 us in one launch.
 #include "../../include/signsgd_ortho.h"
 #include "product.cuh"
 
@@ -277,7 +282,7 @@ __device__ __forceinline__ double block_sum(double s) {
 template <typename F>
 __device__ __forceinline__ void over_eights(const Start& a, F f) {
     const int tc = threadIdx.x & (a.row_threads - 1), tr = threadIdx.x / a.row_threads, rows = 256 / a.row_threads;
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * rows + tr; r < a.rows; r += static_cast<int64_t>(a.blocks) * rows)
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * rows + tr; r < a.rows; r += static_cast<int64_t>(gridDim.x) * rows)
         for (int c = tc * 8; c < a.cols; c += a.row_threads * 8) f(r, c, a.cols - c);
 }
 
@@ -363,7 +368,9 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
 // A cluster of up to eight blocks holds a matrix on chip: each has 256 of the longer side's indices l, as fp32 in registers (a
 // thread has 128 neighbouring elements of a row, in memory's order: rows are the shorter side's indices i, or l where the matrix is tall)
 // and as fp16 operand in shared memory. A step is three products within the block; between them S is summed over the cluster, each
-// block a share of its rows, which it hands to all.
+// block a share of its rows, which it hands to all. A step takes one block 3 us (0.45 to write the operand, 0.5, 0.45 and 0.45 for the
+// products from start to end, 0.3, 0.45 and 0.7 to bring their sums out), eight 7; 128 x 128 24 us, 128 x 2048 46, as 15 products of their
+// own 98 and 140. Loading, the norm and storing take 6.
 constexpr int kHeldSide = 128, kHeldLong = 256, kHeldThreads = 256, kMostHeldBlocks = 8;
 constexpr uint32_t kHeldX = kHeldSide * kHeldLong * 2, kHeldS = kHeldSide * kHeldSide * 2, kHeldPart = kHeldSide * kHeldSide * 4;
 // X; S; Q, whose place the others' shares of S take before it is formed, and 32 KB more of those; this block's part of S
@@ -746,7 +753,9 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
 // ---- host side -------------------------------------------------------------------------------------
 
 constexpr int64_t kMostSide = int64_t(1) << 20, kMostTiles = int64_t(1) << 24;
-constexpr int kMostBlocks = 1184;  // of the start's kernels: eight to an SM
+// Blocks of the first pass over all matrices, eight to an SM, and of the second over each: more of them, shorter, write faster (12 of
+// 4096 x 1024 110 -> 95 us).
+constexpr int kMostBlocks = 1184, kMostStartBlocks = 2400;
 
 struct Layout {
     int64_t side, ld, side_ld;   // the smaller side; row strides of X and of S and Q
@@ -848,8 +857,10 @@ int run(Call& c, const Layout& l, uint8_t* ws, cudaStream_t st) {
     if (c.in_dt == SS_F32) e = launch_next(false, ortho_norm_kernel<float>, grid, 256, st, a);
     else e = launch_next(false, ortho_norm_kernel<uint16_t>, grid, 256, st, a);
     if (e != cudaSuccess) return cuda_status_public(e);
-    if (c.in_dt == SS_F32) e = launch_next(true, ortho_start_kernel<float>, grid, 256, st, a);
-    else e = launch_next(true, ortho_start_kernel<uint16_t>, grid, 256, st, a);
+    const int64_t want = (c.rows + 256 / l.row_threads - 1) / (256 / l.row_threads);
+    const dim3 many(static_cast<unsigned>(want < kMostStartBlocks ? want : kMostStartBlocks), static_cast<unsigned>(c.count));
+    if (c.in_dt == SS_F32) e = launch_next(true, ortho_start_kernel<float>, many, 256, st, a);
+    else e = launch_next(true, ortho_start_kernel<uint16_t>, many, 256, st, a);
     if (e != cudaSuccess) return cuda_status_public(e);
 
     const bool tall = c.rows > c.cols;

@@ -1,15 +1,21 @@
 // Products of matrices on the matrix unit, C = A B^T and its transposed forms, with something at the end
 // of each tile: the core that the loss at the head and the orthogonal update share.
 //
-// Two blocks on neighbouring SMs form a 256 x 256 tile: each copies and keeps 128 of its rows of A, 128
-// of its rows of B, and the sums of its 128 rows. (Where C has no more than 128 rows, blocks form 128 x 256 tiles each alone, with all rows of B.) One warp copies stages of 64 contraction indices by TMA, one
-// issues the matrix instructions, eight bring the sums out of the tensor memory, whose other half the matrix
-// unit fills meanwhile. An operand may lie in memory with its contraction index fast or slow (XMN); the
-// tiles are swizzled by the copies either way, and nothing is transposed.
+// Two blocks on neighbouring SMs form a 256 x 256 tile: each copies and keeps 128 of its rows of A, 128 of its rows of
+// B, and the sums of its 128 rows. (Where C has no more than 128 rows, blocks form 128 x 256 tiles alone, each with
+// all rows of B.) One warp copies stages of 64 contraction indices by TMA, one issues the matrix instructions, eight
+// bring the sums out of the tensor memory, whose other half the matrix unit fills meanwhile. An operand may lie in
+// memory with its contraction index fast or slow (XMN); the tiles are swizzled by the copies either way, and nothing is
+// transposed.
 //
-// Operands have 16 bits (bf16 or fp16), sums 32. An fp32 operand goes as three bf16 terms whose sum it is
-// exactly ("planes" of a 3-D tensor map), and a product of two such as six passes, over some stages at a time, from the
-// smallest terms to the largest, which alone the matrix unit's truncation reaches; the three that are left out are below 2^-24 of the largest.
+// Operands have 16 bits (bf16 or fp16), sums 32. An fp32 operand goes as three bf16 terms whose sum it is exactly
+// ("planes" of a 3-D tensor map), and a product of two such as six passes, over some stages at a time, from the
+// smallest terms to the largest, which alone the matrix unit's truncation reaches; the three that are left out are
+// below 2^-24 of the largest.
+//
+// What bounds it. A stage of a pair takes 512 cycles of the matrix unit, which long products keep busy 90 % of the
+// time: 4100 x 2048 over 65536 bf16 (2460 rows that count) in 440 us, 1500 TFLOP/s. Below some 50 tiles it is start and
+// end: 3 us until the first sums, 1 to 4 to bring a tile out.
 #pragma once
 
 #include <cuda.h>
@@ -480,8 +486,10 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
 // ---- small products --------------------------------------------------------------------------------
 // Products that are too small to fill the machine with pairs: one 128 x 128 tile to a cluster of 1, 2 or 4 blocks that
 // share the contraction. Each forms its part of the sums, keeps it in shared memory, and adds up its share of
-// the tile's squares from all of them, in the order of their ranks, before it brings it out. A block needs little enough
-// that two fit on an SM: those of the kernel that follows are set up while this one runs.
+// the tile's squares from all of them, in the order of their ranks, before it brings it out. With three stages under way
+// two blocks fit on an SM. What bounds them is latency: of the 9.5 us of S of 1000 x 2048 (36 tiles, two blocks each) 2 are the
+// wait for the kernel before, 0.6 the first copies, 3.5 the products, 1.2 the sums' way to the other block, 1.2 the end of the
+// tile, 0.9 the wait for the other block.
 constexpr int kSmallTile = 128, kSmallStages = 3, kMostSmallStages = 6, kSmallOut = 256, kSmallThreads = kSmallOut + 64;  // warps 0-7 bring out, 8 copies, 9 issues
 static_assert(kSmallTile * kSmallTile * 4 <= kSmallStages * kProdStageBytes, "the sums take the place of the operands");
 
