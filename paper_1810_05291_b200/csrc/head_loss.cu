@@ -59,7 +59,7 @@ struct Head {
     const float *weights, *grad_scale;
     float *totals, *logp;
     int64_t rows, x_stride, w_stride, dx_stride;
-    const void *x, *w;
+    const void *x, *w, *x_end, *w_end;
     void* dx;
     int width, vocab, vectors, dx_vectors, w_vectors;
     int few;                        // at most kFewRows rows: launches of their own for rows and statistics are saved
@@ -145,24 +145,50 @@ __device__ __forceinline__ void store_terms(uint16_t* dst, int64_t plane, const 
         *reinterpret_cast<uint2*>(dst + q * plane) = make_uint2(__byte_perm(t[0][q], t[1][q], 0x7632), __byte_perm(t[2][q], t[3][q], 0x7632));
 }
 
-// A row to the layout of an operand: bf16 as it is, fp32 as three terms.
-template <typename T>
-__device__ __forceinline__ void stage_row(const T* src, uint16_t* dst, int64_t plane, int width, bool vectors, int lane) {
-#pragma unroll 4
-    for (int c = 4 * lane; c < width; c += 128) {
-        const int n = width - c;
-        if constexpr (sizeof(T) == 2) {
-            uint2 r;
-            if (vectors && n >= 4) {
-                r = *reinterpret_cast<const uint2*>(src + c);
-            } else {
-                uint32_t v[4];
+// Eight bf16 from `src` on, which starts anywhere: out of the one or two 16-byte blocks of memory that hold them, shifted into place, if those lie
+// between `begin` and `end`, which may be read.
+__device__ __forceinline__ uint4 load_shifted(const uint16_t* src, const char* begin, const char* end, int n) {
+    const char* const block = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(src) & ~uintptr_t(15));
+    const uint32_t shift = static_cast<uint32_t>(reinterpret_cast<const char*>(src) - block);  // bytes
+    uint32_t w[9];
+    if (n >= 8 && block >= begin && block + (shift != 0 ? 32 : 16) <= end) {
+        const uint4 x = *reinterpret_cast<const uint4*>(block), y = shift != 0 ? *reinterpret_cast<const uint4*>(block + 16) : make_uint4(0, 0, 0, 0);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w, w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w, w[8] = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = j < n ? src[c + j] : 0;
-                r = make_uint2(v[0] | (v[1] << 16), v[2] | (v[3] << 16));
+        for (int step = 2; step > 0; step >>= 1)
+            if (shift & (4 * step)) {
+#pragma unroll
+                for (int i = 0; i + step < 9; ++i) w[i] = w[i + step];
             }
-            *reinterpret_cast<uint2*>(dst + c) = r;
-        } else {
+        if (shift & 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        // (a shift of 8 bytes or more moved four words' worth in two steps; of the nine the first four are meant)
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? src[2 * i] : 0u) | (2 * i + 1 < n ? static_cast<uint32_t>(src[2 * i + 1]) << 16 : 0u);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A row to the layout of an operand: bf16 as it is, fp32 as three terms. begin, end: of the matrix, for rows at odd places. It is done
+// by `lanes` lanes, this the lane-th.
+template <typename T>
+__device__ __forceinline__ void stage_row(const T* src, uint16_t* dst, int64_t plane, int width, bool vectors, const void* begin, const void* end, int lane, int lanes) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll 4
+        for (int c = 8 * lane; c < width; c += 8 * lanes) {
+            const int n = width - c;
+            uint4 r;
+            if (vectors && n >= 8) r = *reinterpret_cast<const uint4*>(src + c);
+            else r = load_shifted(src + c, static_cast<const char*>(begin), static_cast<const char*>(end), n);
+            *reinterpret_cast<uint4*>(dst + c) = r;
+        }
+    } else {
+#pragma unroll 4
+        for (int c = 4 * lane; c < width; c += 4 * lanes) {
+            const int n = width - c;
             float v[4];
             if (vectors && n >= 4) {
                 const float4 r = *reinterpret_cast<const float4*>(src + c);
@@ -237,7 +263,7 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant_
         if (i < padded || (i < a.row_cap && i % a.chunk_rows < kProdK)) {
             uint16_t* const dst = a.gathered + i * a.width_ld + first;
             if (i < live) {
-                stage_row(static_cast<const T*>(a.x) + index[i] * a.x_stride + first, dst, plane, n, a.vectors, lane);
+                stage_row(static_cast<const T*>(a.x) + index[i] * a.x_stride + first, dst, plane, n, a.vectors, a.x, a.x_end, lane, 32);
             } else {
                 for (int q = 0; q < (sizeof(T) == 4 ? kTerms : 1); ++q)
                     for (int c = lane; c < n; c += 32) dst[q * plane + c] = 0;
@@ -258,8 +284,15 @@ __global__ void __launch_bounds__(256) head_stage_w_kernel(const __grid_constant
     next_may_begin();
     after_previous();
     const int64_t plane = static_cast<int64_t>(a.vocab) * a.width_ld;
-    for (int64_t i = blockIdx.x * 8 + (threadIdx.x >> 5); i < a.vocab; i += gridDim.x * 8)
-        stage_row(static_cast<const T*>(a.w) + i * a.w_stride, a.staged_w + i * a.width_ld, plane, a.width, a.w_vectors, threadIdx.x & 31);
+    int lanes = 32;  // of a row: narrow ones share a warp
+    while (lanes > 1 && (lanes / 2) * (sizeof(T) == 2 ? 8 : 4) >= a.width) lanes /= 2;
+    const int rows = 256 / lanes, lane = threadIdx.x & (lanes - 1);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * rows + threadIdx.x / lanes; i < a.vocab; i += static_cast<int64_t>(gridDim.x) * rows) {
+        const T* const src = static_cast<const T*>(a.w) + i * a.w_stride;
+        uint16_t* const dst = a.staged_w + i * a.width_ld;
+        if (lanes == 32) stage_row(src, dst, plane, a.width, a.w_vectors, a.w, a.w_end, lane, 32);
+        else stage_row(src, dst, plane, a.width, a.w_vectors, a.w, a.w_end, lane, lanes);
+    }
 }
 
 __device__ __forceinline__ uint4 half8(const float* v) {
@@ -667,13 +700,30 @@ struct Gradient {
         const float* before;
         int row, col, rows, cols;  // rows and columns: that exist from there on
         int part;
-        bool add, packs;
+        bool add, packs, whole;
 
         __device__ __forceinline__ static uint32_t pack(uint32_t a, uint32_t b) { return bf16_pair(__uint_as_float(a), __uint_as_float(b)); }
         __device__ __forceinline__ void packed(int j, int lane, uint32_t buf) const {
-            char* q = p + (j + 4 * (lane & 7)) * 2;  // p is at four columns a lane, this at eight
+            if (whole) {
+                char* q = p + (j + 4 * (lane & 7)) * 2;  // p is at four columns a lane, this at eight
 #pragma unroll
-            for (int i = 0; i < 8; ++i, q += step) *reinterpret_cast<uint4*>(q) = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+                for (int i = 0; i < 8; ++i, q += step) *reinterpret_cast<uint4*>(q) = square_get(buf, (lane >> 3) + 4 * i, lane & 7);
+                return;
+            }
+            // rows at odd places, or not all there: a row at a time, two columns to a lane
+            const int left = cols + 4 * (lane & 7) - j - 2 * lane, there = min(32, rows + (lane >> 3));
+            if (left <= 0) return;
+            uint16_t* q = reinterpret_cast<uint16_t*>(p - (lane >> 3) * (step / 4)) - 4 * (lane & 7) + j + 2 * lane;
+#pragma unroll 8
+            for (int r = 0; r < there; ++r, q = reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(q) + step / 4)) {
+                const uint32_t w = __float_as_uint(square_word(buf, r, lane));
+                if (left > 1 && (reinterpret_cast<uintptr_t>(q) & 3) == 0) {
+                    *reinterpret_cast<uint32_t*>(q) = w;
+                } else {
+                    q[0] = static_cast<uint16_t>(w);
+                    if (left > 1) q[1] = static_cast<uint16_t>(w >> 16);
+                }
+            }
         }
         __device__ __forceinline__ Tile(const Gradient& e, const ProdUnit& u, int m, int row0, int col0, int lane) {
             row = row0 + (lane >> 3), col = col0 + 4 * (lane & 7), part = u.part, add = e.to.add;
@@ -687,7 +737,8 @@ struct Gradient {
                 p = OUT16 ? reinterpret_cast<char*>(e.to.bf16 + at) : reinterpret_cast<char*>(e.to.f32 + at);
                 step = 4 * e.to.stride * (OUT16 ? 2 : 4);
             }
-            packs = OUT16 && part < 0 && e.to.wide && row0 + 32 <= m && col0 + kProdHalf <= e.to.cols;
+            packs = OUT16 && part < 0;
+            whole = e.to.wide && row0 + 32 <= m && col0 + kProdHalf <= e.to.cols;
             before = BEFORE ? e.to.before + row * e.to.before_stride + col : nullptr;
         }
         __device__ __forceinline__ void fetch(const Gradient& e, int j, Fetched& f) const {
@@ -697,7 +748,19 @@ struct Gradient {
                     f.before[i] = part < 0 && 4 * i < rows && j < cols ? *reinterpret_cast<const float4*>(before + j + 4 * i * e.to.before_stride) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
         }
-        __device__ __forceinline__ void square(const Gradient& e, int j, int, uint32_t, float4 (&sums)[8], const Fetched& f, bool first) const {
+        __device__ __forceinline__ void square(const Gradient& e, int j, int lane, uint32_t buf, float4 (&sums)[8], const Fetched& f, bool first) const {
+            if (!OUT16 && part < 0 && !e.to.vectors) {  // rows at odd places: a row at a time, a column to a lane
+                const int there = min(32, rows + (lane >> 3));
+                if (cols + 4 * (lane & 7) - j - lane <= 0) return;
+                float* q = reinterpret_cast<float*>(p - (lane >> 3) * (step / 4)) - 4 * (lane & 7) + j + lane;
+#pragma unroll 8
+                for (int r = 0; r < there; ++r, q = reinterpret_cast<float*>(reinterpret_cast<char*>(q) + step / 4)) {
+                    const float v = square_word(buf, r, lane);
+                    if (add || !first) add_global(q, v);
+                    else *q = v;
+                }
+                return;
+            }
             const bool adds = add || !first;
             char* q = p + j * (OUT16 && part < 0 ? 2 : 4);
 #pragma unroll
@@ -992,8 +1055,9 @@ int ss_linear_cross_entropy(const void* x, int64_t x_stride, const void* w, int6
     for (int i = 0; i < 5; ++i)
         if (bytes_overlap(vecs[i], size[i], workspace, l.bytes)) return SS_ERR_INVALID_ARG;
     a.rows = rows, a.x_stride = mx.stride, a.w_stride = mw.stride, a.dx_stride = mdx.stride, a.x = x, a.w = w, a.dx = dx;
+    a.x_end = static_cast<const char*>(x) + mx.extent(), a.w_end = static_cast<const char*>(w) + mw.extent();
     a.width = static_cast<int>(width), a.vocab = static_cast<int>(vocab);
-    a.vectors = mx.row_aligned(4 * eb), a.w_vectors = mw.row_aligned(4 * eb), a.dx_vectors = mdx.row_aligned(4 * eb);
+    a.vectors = mx.row_aligned(16), a.w_vectors = mw.row_aligned(16), a.dx_vectors = mdx.row_aligned(4 * eb);
     a.c = inv_temperature, a.k = inv_temperature * 1.44269504f, a.z_coef = z_coef;
     return run(a, l, static_cast<uint8_t*>(workspace), dw, mdw.stride, dw_dt, mdw.row_aligned(4 * web), mdw.row_aligned(16), accumulate, st);
 }

@@ -302,7 +302,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     const uint32_t src = tmem_at + (chunk & 1) * kProdTile;
                     bool done = !any;
                     if constexpr (EPI::kPacks) {
-                        if (tile.packs && ok) {
+                        if (!done && tile.packs && ok) {
                             done = true;
 #pragma unroll 1
                             for (int j = 0; j < kProdHalf; j += 64) {
