@@ -19,6 +19,7 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
 #include <cmath>
 
 namespace ss {
@@ -365,13 +366,13 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
 }
 
 // ---- matrices with a side of at most 128: all steps in one launch -----------------------------------
-// A cluster of up to eight blocks holds a matrix on chip: each has 256 of the longer side's indices l, as fp32 in registers (a
+// A cluster of up to sixteen blocks (eight, where the device has no place for more) holds a matrix on chip: each has 256 of the longer side's indices l, as fp32 in registers (a
 // thread has 128 neighbouring elements of a row, in memory's order: rows are the shorter side's indices i, or l where the matrix is tall)
 // and as fp16 operand in shared memory. A step is three products within the block; between them S is summed over the cluster, each
 // block a share of its rows, which it hands to all. A step takes one block 3 us (0.45 to write the operand, 0.5, 0.45 and 0.45 for the
-// products from start to end, 0.3, 0.45 and 0.7 to bring their sums out), eight 7; 128 x 128 24 us, 128 x 2048 46, as 15 products of their
-// own 98 and 140. Loading, the norm and storing take 6.
-constexpr int kHeldSide = 128, kHeldLong = 256, kHeldThreads = 256, kMostHeldBlocks = 8;
+// products from start to end, 0.3, 0.45 and 0.7 to bring their sums out), eight 7; 128 x 128 24 us, 128 x 2048 46, 128 x 4096 52, as 15 products of
+// their own 98, 140 and 145. Loading, the norm and storing take 6.
+constexpr int kHeldSide = 128, kHeldLong = 256, kHeldThreads = 256, kMostHeldBlocks = 16, kPortableBlocks = 8;
 constexpr uint32_t kHeldX = kHeldSide * kHeldLong * 2, kHeldS = kHeldSide * kHeldSide * 2, kHeldPart = kHeldSide * kHeldSide * 4;
 // X; S; Q, whose place the others' shares of S take before it is formed, and 32 KB more of those; this block's part of S
 constexpr size_t kHeldSmem = 1024 + kHeldX + 3 * kHeldS + kHeldPart;
@@ -617,7 +618,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                 for (int d = 0; d < 4; ++d)
                     turn_put(ps, i_or_l, half * 16 + c + d, make_float4(__uint_as_float(w[4 * d]), __uint_as_float(w[4 * d + 1]), __uint_as_float(w[4 * d + 2]), __uint_as_float(w[4 * d + 3])));
             }
-            const uint32_t share = kHeldSide / blocks;  // rows; a multiple of 16
+            const uint32_t share = kHeldSide / blocks;  // rows; a multiple of 8
             smem_to_async();
             __syncthreads();
             if (tid == 0) {
@@ -753,9 +754,9 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
 // ---- host side -------------------------------------------------------------------------------------
 
 constexpr int64_t kMostSide = int64_t(1) << 20, kMostTiles = int64_t(1) << 24;
-// Blocks of the first pass over all matrices, eight to an SM, and of the second over each: more of them, shorter, write faster (12 of
-// 4096 x 1024 110 -> 95 us).
-constexpr int kMostBlocks = 1184, kMostStartBlocks = 2400;
+// Blocks of the first pass over all matrices, four to an SM, and of the second over each: more of them, shorter, write faster (12 of
+// 4096 x 1024 110 -> 94 us).
+constexpr int kMostBlocks = 592, kMostStartBlocks = 2400;
 
 struct Layout {
     int64_t side, ld, side_ld;   // the smaller side; row strides of X and of S and Q
@@ -803,18 +804,44 @@ struct Call {
 };
 
 template <typename T, bool TALL>
-int launch_held(const Held& h, int matrices, int blocks, cudaStream_t st) {
-    const auto kernel = ortho_held_kernel<T, TALL>;
+cudaError_t held_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int matrices, int blocks, cudaStream_t st) {
     struct Key {};
-    cudaError_t e = allow_shared<Key>(reinterpret_cast<const void*>(kernel), static_cast<int>(kHeldSmem));
-    if (e != cudaSuccess) return cuda_status_public(e);
+    const void* const kernel = reinterpret_cast<const void*>(ortho_held_kernel<T, TALL>);
+    cudaError_t e = allow_shared<Key>(kernel, static_cast<int>(kHeldSmem));
+    if (e == cudaSuccess && blocks > kPortableBlocks) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    at->id = cudaLaunchAttributeClusterDimension;
+    at->val.clusterDim.x = blocks, at->val.clusterDim.y = 1, at->val.clusterDim.z = 1;
+    cfg->gridDim = dim3(static_cast<unsigned>(matrices * blocks)), cfg->blockDim = dim3(kHeldThreads);
+    cfg->dynamicSmemBytes = kHeldSmem, cfg->stream = st, cfg->attrs = at, cfg->numAttrs = 1;
+    return e;
+}
+
+template <typename T, bool TALL>
+int launch_held(const Held& h, int matrices, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = blocks, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
-    cfg.gridDim = dim3(static_cast<unsigned>(matrices * blocks)), cfg.blockDim = dim3(kHeldThreads);
-    cfg.dynamicSmemBytes = kHeldSmem, cfg.stream = st, cfg.attrs = &at, cfg.numAttrs = 1;
-    return cuda_status_public(cudaLaunchKernelEx(&cfg, kernel, h));
+    cudaError_t e = held_config<T, TALL>(&cfg, &at, matrices, blocks, st);
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, ortho_held_kernel<T, TALL>, h);
+    return cuda_status_public(e);
+}
+
+// Whether the current device has place for a cluster of that many blocks, asked once for each device.
+bool fits_on_device(int blocks) {
+    if (blocks <= kPortableBlocks) return true;
+    static std::atomic<int> known[64];  // 0: not asked, 1: no, 2: yes
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device >= 64) return false;
+    int answer = known[device].load(std::memory_order_relaxed);
+    if (answer == 0) {
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute at{};
+        int clusters = 0;
+        answer = held_config<float, false>(&cfg, &at, 1, blocks, nullptr) == cudaSuccess &&
+                         cudaOccupancyMaxActiveClusters(&clusters, ortho_held_kernel<float, false>, &cfg) == cudaSuccess && clusters > 0 ? 2 : 1;
+        if (answer == 1) cudaGetLastError();
+        known[device].store(answer, std::memory_order_relaxed);
+    }
+    return answer == 2;
 }
 
 // Blocks that hold a matrix of these sides, or 0: it is held only up to kHeldSide by kMostHeldBlocks * kHeldLong.
@@ -823,7 +850,7 @@ int held_blocks(int64_t rows, int64_t cols) {
     if (small > kHeldSide || big > kMostHeldBlocks * kHeldLong) return 0;
     int blocks = 1;
     while (blocks * kHeldLong < big) blocks *= 2;
-    return blocks;
+    return fits_on_device(blocks) ? blocks : 0;
 }
 
 int run_held(const Call& c, int blocks, float scale, float unscale, cudaStream_t st) {

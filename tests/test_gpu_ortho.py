@@ -46,7 +46,7 @@ def run(mats, out_dtype=F32, coefficients=ref.COEFFICIENTS):
 
 
 SHAPES = [(1, 1), (1, 40), (40, 1), (2, 3), (17, 33), (64, 64), (33, 17), (100, 257), (257, 100), (128, 640), (300, 300), (511, 513), (700, 260), (1000, 2048),
-          (5, 256), (256, 5), (128, 257), (257, 128), (77, 1000), (1025, 128), (128, 2048), (2048, 100), (2049, 128), (129, 129), (64, 4000)]
+          (5, 256), (256, 5), (128, 257), (257, 128), (77, 1000), (1025, 128), (128, 2048), (2048, 100), (2049, 128), (129, 129), (64, 4000), (4096, 128), (128, 4097), (1, 3000)]
 
 
 @pytest.mark.parametrize("kind", ["strong", "noise"])
