@@ -677,13 +677,12 @@ def ss_preference_loss(logits: torch.Tensor, targets: torch.Tensor, weights: tor
                                 d_stride, w_ptr, w_bytes, _stream(stream)), "ss_preference_loss")
 
 
-def _one_device(tensors) -> int:
-    """The GPU that all of them are on."""
+def _one_device(*tensors) -> None:
+    """All of them, but for ``None``, are on the first one's GPU."""
     device = tensors[0].get_device()
     for t in tensors:
-        if t.get_device() != device:
+        if t is not None and t.get_device() != device:
             raise ValueError("all tensors of a call must be on one device")
-    return device
 
 
 def _on_its_device(call):
@@ -701,6 +700,12 @@ def _on_its_device(call):
         with torch.cuda.device(device):
             return call(*args, **kwargs)
     return made
+
+
+@functools.lru_cache(maxsize=256)
+def _head_workspace(place: int, *sizes: int) -> int:
+    """Of the weight's address only its place among 16 bytes counts."""
+    return int(lib().ss_linear_cross_entropy_workspace(4096 + place, *sizes))
 
 
 def ss_linear_cross_entropy_workspace(weight: torch.Tensor, rows: int, dx: bool = True, dw: Optional[torch.dtype] = None) -> int:
@@ -724,13 +729,13 @@ def ss_linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torc
     vocab = weight.shape[0]
     if weight.shape[1] != width:
         raise ValueError("weight must have one column for each of x's %d, has %d" % (width, weight.shape[1]))
-    _one_device([t for t in (x, weight, targets, weights, totals, logp, dx, dw, grad_scale, workspace) if t is not None])
+    _one_device(x, weight, targets, weights, totals, logp, dx, dw, grad_scale, workspace)
     dx_ptr, dx_stride = (None, 0) if dx is None else _mat(dx, dt, "dx", x.shape)
     dw_code = SS_F32 if dw is None else _dtype_code(dw)
     dw_ptr, dw_stride = (None, 0) if dw is None else _mat(dw, dw.dtype, "dw", weight.shape)
     L = lib()
-    need = 0 if workspace is not None else L.ss_linear_cross_entropy_workspace(w_ptr, w_stride, code, rows, width, vocab, int(dx is not None),
-                                                                              int(dw is not None), dw_code)
+    need = 0 if workspace is not None else _head_workspace(w_ptr & 15, w_stride, code, rows, width, vocab, int(dx is not None),
+                                                           int(dw is not None), dw_code)
     ws_ptr, ws_bytes, workspace = _scratch(workspace, need, x, stream)
     _check(L.ss_linear_cross_entropy(x_ptr, x_stride, w_ptr, w_stride, code, rows, width, vocab,
                                      _vec(targets, torch.int64, "targets", rows), _vec(weights, f32, "weights", rows),
@@ -783,7 +788,7 @@ def ss_orthogonalise(inputs: Sequence[torch.Tensor], outputs: Sequence[torch.Ten
     _same_count(count, outputs=outputs)
     if count == 0:
         return
-    _one_device([*inputs, *outputs] if workspace is None else [*inputs, *outputs, workspace])
+    _one_device(*inputs, *outputs, workspace)
     shape, in_code, out_code = inputs[0].shape, _dtype_code(inputs[0]), _dtype_code(outputs[0])
     a, a_stride = _mats(inputs, inputs[0].dtype, "inputs", shape)
     b, b_stride = _mats(outputs, outputs[0].dtype, "outputs", shape)
@@ -805,8 +810,7 @@ def ss_orthogonal_update(grads: Sequence[torch.Tensor], momenta: Sequence[torch.
     _same_count(count, momenta=momenta, momenta_out=momenta_out, params=params, params_out=params_out)
     if count == 0:
         return
-    every = [*grads, *momenta, *momenta_out, *params, *params_out]
-    _one_device(every if workspace is None else every + [workspace])
+    _one_device(*grads, *momenta, *momenta_out, *params, *params_out, workspace)
     f32, shape, code = torch.float32, grads[0].shape, _dtype_code(grads[0])
     g, g_stride = _mats(grads, grads[0].dtype, "grads", shape)
     v, v_stride = _mats([*momenta, *momenta_out], f32, "momenta and momenta_out", shape)
