@@ -9,8 +9,8 @@
 // So neither the logits nor P exist as a whole, and three products do, where forming the logits again for the backward pass
 // would take four; the pass over e costs a few percent of a product.
 //
-// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 1024 contraction indices and
-// are added in registers, to nearest. e is fp16 (relative to its part's maximum, 11 bits), P is bf16 as the gradient
+// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 512 or 256 contraction
+// indices and are added in registers, to nearest. e is fp16 (relative to its part's maximum, 11 bits), P is bf16 as the gradient
 // of bf16 logits is; the entry of the target, which is a difference, is formed in fp32 from log p. With fp32 inputs e
 // is fp32 and P the sum of three bf16.
 //
@@ -29,9 +29,13 @@ namespace ss {
 namespace {
 
 constexpr int kPartCols = kProdHalf;              // logits of a thread
-// Stages that the matrix unit sums of a logit. log p of 8192 x 4096 over 131072 is off by 2.6e-6 with 16 (an fp32 product: 3.1e-6), and by 6e-7 with 4,
-// whose product takes 3.95 ms instead of 3.3 (with 8: 3.5): the two halves of the tensor memory fill while a tile's exponentials are formed.
-constexpr int kLogitChunk = 16;
+// Stages that the matrix unit sums of a logit: relative error of log p and time of a call with 16, 8, 4 and 2 of them
+//   2048 x 2048 over 50257 bf16, loss alone   2.7e-6  276 us,  1.3e-6  277 us,  6e-7  296 us,  4e-7  319 us   (a plain fp32 product 2e-6)
+//   64 x 1024 over 32000 bf16                 2.5e-6   69 us,  1.1e-6   69 us,  6e-7   68 us,  3e-7   69 us
+//   1021 x 770 over 32001 fp32                2.2e-6  897 us,  1.2e-6  916 us,  7e-7  878 us,  5e-7  875 us
+// With fewer the two halves of the tensor memory fill while a tile's exponentials are formed. That costs nothing where the stages come at the
+// memory's rate (at most 128 rows) or bring six products each (fp32).
+constexpr int kLogitChunk = 8, kLogitChunkSlow = 4;
 // Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16; 2048 (of each of fp32's
 // passes) lose 5e-7.
 constexpr int kGradChunk = 256, kGradChunkF32 = 32;
@@ -919,7 +923,8 @@ int run(Head& a, const Layout& l, uint8_t* ws, void* dw, int64_t dw_stride, ss_d
         if (status != SS_OK) return status;
 
         Product pz = product_of(rows < l.chunk_rows ? rows : l.chunk_rows, vocab, width, l.f32, sms);
-        pz.block = kLogitChunk, pz.chunk = pz.passes * kLogitChunk, pz.m_fast = 1, pz.follows = 1, pz.live = a.live, pz.live_from = a.first, pz.live_side = 1;
+        const int chunk = l.f32 || rows <= kProdHalf ? kLogitChunkSlow : kLogitChunk;
+        pz.block = chunk, pz.chunk = pz.passes * chunk, pz.m_fast = 1, pz.follows = 1, pz.live = a.live, pz.live_from = a.first, pz.live_side = 1;
         alone(pz, sms);
         const Logits ez{a.target + first, a.target_logit, a.parts, grads && !l.f32 ? a.e16 : nullptr, grads && l.f32 ? a.e32 : nullptr,
                         l.e_ld, a.n_parts, a.vocab, a.k};
