@@ -9,7 +9,7 @@
 // So neither the logits nor P exist as a whole, and three products do, where forming the logits again for the backward pass
 // would take four; the pass over e costs a few percent of a product.
 //
-// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 512 or 256 contraction
+// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 512 or 128 contraction
 // indices and are added in registers, to nearest. e is fp16 (relative to its part's maximum, 11 bits), P is bf16 as the gradient
 // of bf16 logits is; the entry of the target, which is a difference, is formed in fp32 from log p. With fp32 inputs e
 // is fp32 and P the sum of three bf16.
@@ -35,10 +35,10 @@ constexpr int kPartCols = kProdHalf;              // logits of a thread
 //   1021 x 770 over 32001 fp32                2.2e-6  897 us,  1.2e-6  916 us,  7e-7  878 us,  5e-7  875 us
 // With fewer the two halves of the tensor memory fill while a tile's exponentials are formed. That costs nothing where the stages come at the
 // memory's rate (at most 128 rows) or bring six products each (fp32).
-constexpr int kLogitChunk = 8, kLogitChunkSlow = 4;
-// Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16; 2048 (of each of fp32's
-// passes) lose 5e-7.
-constexpr int kGradChunk = 256, kGradChunkF32 = 32;
+constexpr int kLogitChunk = 8, kLogitChunkSlow = 2;
+// Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16. Of each of fp32's passes 1024 indices:
+// dx and dW of 1021 x 770 over 32001 are off by 1.2e-6 (2.4e-6 with 2048, plain fp32 products 1.6e-6), in the same time.
+constexpr int kGradChunk = 256, kGradChunkF32 = 16;
 constexpr int64_t kChunkBytes = int64_t(1) << 30; // of e and P
 constexpr int64_t kMostChunkRows = 16384;
 
