@@ -9,7 +9,7 @@
 // So neither the logits nor P exist as a whole, and three products do, where forming the logits again for the backward pass
 // would take four; the pass over e costs a few percent of a product.
 //
-// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 512 or 128 contraction
+// Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 768 or 128 contraction
 // indices and are added in registers, to nearest. e is fp16 (relative to its part's maximum, 11 bits), P is bf16 as the gradient
 // of bf16 logits is; the entry of the target, which is a difference, is formed in fp32 from log p. With fp32 inputs e
 // is fp32 and P the sum of three bf16.
@@ -29,13 +29,17 @@ namespace ss {
 namespace {
 
 constexpr int kPartCols = kProdHalf;              // logits of a thread
-// Stages that the matrix unit sums of a logit: relative error of log p and time of a call with 16, 8, 4 and 2 of them
-//   2048 x 2048 over 50257 bf16, loss alone   2.7e-6  276 us,  1.3e-6  277 us,  6e-7  296 us,  4e-7  319 us   (a plain fp32 product 2e-6)
-//   64 x 1024 over 32000 bf16                 2.5e-6   69 us,  1.1e-6   69 us,  6e-7   68 us,  3e-7   69 us
-//   1021 x 770 over 32001 fp32                2.2e-6  897 us,  1.2e-6  916 us,  7e-7  878 us,  5e-7  875 us
+// Stages that the matrix unit sums of a logit. Many bf16 rows, calls in turn at the power limit, relative error of log p (a plain fp32 product: 1.9e-6):
+//                                16               12               8
+//   2048 x 2048 over 50257       320 us, 2.7e-6   324 us, 1.8e-6   320 us, 1.3e-6
+//   4100 x 2048 over 65536       1767 us          1755 us          1850 us
+//   8192 x 4096 over 131072      22.1 ms          22.3 ms          22.9 ms
 // With fewer the two halves of the tensor memory fill while a tile's exponentials are formed. That costs nothing where the stages come at the
-// memory's rate (at most 128 rows) or bring six products each (fp32).
-constexpr int kLogitChunk = 8, kLogitChunkSlow = 2;
+// memory's rate (at most 128 rows) or bring six products each (fp32):
+//                                16               4                2
+//   64 x 1024 over 32000 bf16    69 us, 2.5e-6    68 us, 6e-7      69 us, 3e-7
+//   1021 x 770 over 32001 fp32   897 us, 2.2e-6   878 us, 7e-7     875 us, 5e-7
+constexpr int kLogitChunk = 12, kLogitChunkSlow = 2;
 // Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16. Of each of fp32's passes 1024 indices:
 // dx and dW of 1021 x 770 over 32001 are off by 1.2e-6 (2.4e-6 with 2048, plain fp32 products 1.6e-6), in the same time.
 constexpr int kGradChunk = 256, kGradChunkF32 = 16;
