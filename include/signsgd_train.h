@@ -199,7 +199,8 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
  * targets, weights, inv_temperature, grad_scale as above. z_coef finite; 0 leaves its term out.
  * width, vocab >= 1 where there are rows. No rows: totals 0, dw 0 unless accumulate. More than 2^24 rows, 2^30 columns
  * or 2^24 tiles of 256 x 256 are SS_ERR_UNSUPPORTED.
- * bf16: products of bf16 with fp32 sums; P is rounded to bf16. fp32: products of three bf16 terms, as precise as fp32
+ * bf16: products of bf16 with fp32 sums; exponentials are kept with 11 bits (fewer below 2^-62 of the largest of 128 neighbouring
+ * columns), P is rounded to bf16. fp32: products of three bf16 terms, as precise as fp32
  * sums. Sums that are added by the memory may flush a subnormal to zero. A wait inside a kernel that ran out (it is bounded) shows as NaN.
  */
 int64_t ss_linear_cross_entropy_workspace(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_t width,

@@ -10,7 +10,8 @@
 // would take four; the pass over e costs a few percent of a product.
 //
 // Rounding. The sums of a logit leave the matrix unit, which truncates as it adds, every 768 or 128 contraction
-// indices and are added in registers, to nearest. e is fp16 (relative to its part's maximum, 11 bits), P is bf16 as the gradient
+// indices and are added in registers, to nearest. e, relative to its part's maximum, is kept in 16 bits of which none is a sign: six of exponent, so
+// that an entry 43 nats below the largest of its 128 still has its 11 bits (fp16 lost bits from 10 nats on and everything at 17). P is bf16 as the gradient
 // of bf16 logits is; the entry of the target, which is a difference, is formed in fp32 from log p. With fp32 inputs e
 // is fp32 and P the sum of three bf16.
 //
@@ -19,8 +20,6 @@
 // 0.85 ms of it at 5.1 TB/s. 64 x 1024 over 32000 bf16: 69 us in a row of calls, W read twice and dW written in 52 of them, the rest five starts.
 // 1021 x 770 over 32001 fp32: 850 us, six passes in 1300 to 1440 TFLOP/s, 120 us to split W and P into terms.
 #include "product.cuh"
-
-#include <cuda_fp16.h>
 
 #include <cmath>
 #include <type_traits>
@@ -303,14 +302,28 @@ __global__ void __launch_bounds__(256) head_stage_w_kernel(const __grid_constant
     }
 }
 
-__device__ __forceinline__ uint4 half8(const float* v) {
+__device__ __forceinline__ float2 mul2(float a, float b, float by) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, k;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 k, {%4, %4};\n\tmul.rn.f32x2 x, x, k;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a), "f"(b), "f"(by));
+    return r;
+}
+
+// Numbers from 0 to 1 in 16 bits without a sign: six of exponent, ten of fraction, subnormal below 2^-62. Times 2^-64 a number's upper three bits in fp32
+// (the sign, and two of the exponent) are 0, and the next sixteen, rounded to nearest, are the code; fp32's own subnormals are its. (A NaN's code means nothing: its
+// row's factor is NaN.)
+constexpr float kCodeScale = 0x1p-64f, kCodeUnscale = 0x1p64f;
+__device__ __forceinline__ uint4 code8(const float* v) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __half2 p = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&p);
+        const float2 t = mul2(v[2 * i], v[2 * i + 1], kCodeScale);
+        w[i] = __byte_perm(__float_as_uint(t.x) * 8u + 0x8000u, __float_as_uint(t.y) * 8u + 0x8000u, 0x7632);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ float2 decode2(uint32_t w) {
+    return mul2(__uint_as_float((w << 13) & 0x1FFFE000u), __uint_as_float((w >> 3) & 0x1FFFE000u), kCodeUnscale);
 }
 
 // ---- the end of the logits' product
@@ -358,7 +371,7 @@ struct Logits {
 #pragma unroll
             for (int h = 0; h < kPartCols; h += 64) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) square_set(buf, lane, i, half8(z + h + 8 * i));
+                for (int i = 0; i < 8; ++i) square_set(buf, lane, i, code8(z + h + 8 * i));
                 out_square(reinterpret_cast<char*>(e16), 2, m, row, col + h, lane, buf);
             }
         } else if (e32 != nullptr) {
@@ -565,7 +578,7 @@ __global__ void __launch_bounds__(256) head_gradient_kernel(const __grid_constan
             const uint32_t w[4] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+                const float2 p = decode2(w[j]);
                 v[2 * j] = p.x, v[2 * j + 1] = p.y;
             }
         }
