@@ -559,8 +559,8 @@ def _ckpt(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
 
 
 def _written(tensors) -> None:
-    """Tells autograd that a kernel wrote to these, so that a checkpoint which a backward pass has yet to read is not
-    written again without a word."""
+    """Tells autograd that a kernel wrote to these, so that what a backward pass has yet to read (a checkpoint, a
+    parameter) is not written again without a word."""
     try:
         torch._C._increment_version(tensors)
     except RuntimeError:  # inference tensors, which no backward pass reads, have no version
@@ -743,6 +743,7 @@ def ss_linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torc
                                      _vec(totals, f32, "totals", 2), _vec(logp, f32, "logp", rows), dx_ptr, dx_stride,
                                      dw_ptr, dw_stride, dw_code, int(bool(accumulate)), ws_ptr, ws_bytes, _stream(stream)),
            "ss_linear_cross_entropy")
+    _written([t for t in (totals, logp, dx, dw) if t is not None])
 
 
 # ---- orthogonal update (include/signsgd_ortho.h) -------------------------------------------------
@@ -798,6 +799,7 @@ def ss_orthogonalise(inputs: Sequence[torch.Tensor], outputs: Sequence[torch.Ten
     w_ptr, w_bytes, workspace = _scratch(workspace, need, inputs[0], stream)
     _check(lib().ss_orthogonalise(a, a_stride, in_code, b, b_stride, out_code, count, rows, cols, table, steps, w_ptr, w_bytes,
                                   _stream(stream)), "ss_orthogonalise")
+    _written(list(outputs))
 
 
 @_on_its_device
@@ -823,3 +825,4 @@ def ss_orthogonal_update(grads: Sequence[torch.Tensor], momenta: Sequence[torch.
     _check(lib().ss_orthogonal_update(g, g_stride, code, v, ctypes.byref(v, half), v_stride, p, ctypes.byref(p, half), p_stride, count,
                                       rows, cols, beta, int(bool(nesterov)), table, steps, lr, scale, weight_decay, w_ptr,
                                       w_bytes, _stream(stream)), "ss_orthogonal_update")
+    _written([*momenta_out, *params_out])

@@ -182,7 +182,7 @@ class OrthogonalMomentum(torch.optim.Optimizer):
             for p in g["params"]:
                 if p.dtype != torch.float32 or p.dim() < 2:
                     raise ValueError("parameters must be float32 matrices, or tensors of more dimensions")
-                if self._matrix(p.data) is None:
+                if self._matrix(p.detach()) is None:
                     raise ValueError("a parameter's rows must be contiguous and not overlap")
 
     @staticmethod
@@ -219,7 +219,7 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                 state = self.state[p]
                 if "momentum_buffer" not in state:
                     state["momentum_buffer"] = torch.zeros_like(p, memory_format=torch.contiguous_format)
-                m = self._matrix(p.data)
+                m = self._matrix(p.detach())  # of p's version, which the kernel's call raises
                 g, v = self._matrix(p.grad), self._matrix(state["momentum_buffer"])
                 if g is None:
                     g = p.grad.reshape(m.shape).contiguous()
