@@ -14,7 +14,10 @@
  *
  * Numerics. |u| in fp64, X in fp32. The products' operands are fp16 (11 significant bits), scaled by a power of
  * two so that their values lie well inside its range, with fp32 sums; the term a X takes X unrounded, so that directions with
- * small singular values are not lost in the rounding of large ones. Of a result O about 2e-3 (2-norm) is rounding. A matrix that
+ * small singular values are not lost in the rounding of large ones. Of a result O about 2e-3 (2-norm) is rounding with those coefficients; with others
+ * a step adds 2^-11 (|b| s^3 + |c| s^5) or so to a direction of singular value s. Coefficients with which the operands could leave their range are refused
+ * (SS_ERR_UNSUPPORTED), whatever the matrix: |a| at least (|b| + |c|) / 64; with m_0 = 1 and m_k+1 the largest |a s + b s^3 + c s^5| over 0 <= s <= m_k, m_k
+ * at most 32 for each step's X, 1e30 for O, and |b s^2 + c s^4| at most 32768 over the same s. A matrix that
  * holds an infinity or a NaN gives NaN throughout; so does a wait inside a kernel that ran out (each is bounded).
  */
 #ifndef SIGNSGD_ORTHO_H_
@@ -38,7 +41,7 @@ int64_t ss_orthogonal_workspace(int count, int64_t rows, int64_t cols);
  * out_i = O(in_i) for `count` matrices of one shape. Array arguments are host arrays of `count` device pointers.
  *   in    in   [rows, cols] of in_dt, each with row stride in_stride
  *   out   out  [rows, cols] of out_dt, each with row stride out_stride; out_i may be in_i in place
- *   coefficients  in  3 * steps finite fp32 in host memory
+ *   coefficients  in  3 * steps finite fp32 in host memory, in the range above
  * 1 <= steps <= SS_ORTHO_MAX_STEPS, 0 <= count <= SS_ORTHO_MAX_MATRICES.
  * Sides beyond 2^20 or more than 2^24 tiles of 256 x 256 are SS_ERR_UNSUPPORTED.
  */

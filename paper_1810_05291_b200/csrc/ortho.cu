@@ -982,11 +982,39 @@ bool overlaps_scratch(const Mats& a, int count, const void* p, size_t n) {
     return false;
 }
 
-int check_coefficients(const float* c, int steps) {
-    if (steps < 1 || steps > SS_ORTHO_MAX_STEPS || c == nullptr) return SS_ERR_INVALID_ARG;
+// What the operands' range (fp16) asks of the coefficients, whatever the matrix. X_0 has singular values up to 1; `most` bounds those of each step's X, and
+// so its elements, times 2^10 at the most (the power of two of the longest side): below 2^15 with singular values up to 32. Q's elements are below its
+// largest singular value. And the linear term, which alone is not rounded, carries the small singular values: where it is nearly nothing beside the others, S, of their
+// squares, falls below the range (two steps of (0, 1, 0) on 1000 x 2048 give nothing at all). With |a| a 64th of the others the model of the roundings is off
+// by 2e-4 at most.
+constexpr double kMostSingular = 32.0, kMostQ = 32768.0, kMostResult = 1e30, kLeastLinear = 1.0 / 64;
+
+// Largest |f| on [0, end], f's extrema among `at`.
+template <typename F>
+double largest(F f, double end, const double* at, int n) {
+    double m = std::fabs(f(end));
+    for (int i = 0; i < n; ++i)
+        if (at[i] > 0.0 && at[i] < end) m = std::fmax(m, std::fabs(f(at[i])));
+    return m;
+}
+
+int check_coefficients(const float* co, int steps) {
+    if (steps < 1 || steps > SS_ORTHO_MAX_STEPS || co == nullptr) return SS_ERR_INVALID_ARG;
     for (int i = 0; i < 3 * steps; ++i)
-        if (!std::isfinite(c[i])) return SS_ERR_INVALID_ARG;
-    return SS_OK;
+        if (!std::isfinite(co[i])) return SS_ERR_INVALID_ARG;
+    double most = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const double a = co[3 * k], b = co[3 * k + 1], c = co[3 * k + 2];
+        if (most > kMostSingular || std::fabs(a) < kLeastLinear * (std::fabs(b) + std::fabs(c))) return SS_ERR_UNSUPPORTED;
+        const double q_at[1] = {c != 0.0 ? -b / (2.0 * c) : 0.0};
+        if (largest([&](double t) { return b * t + c * t * t; }, most * most, q_at, 1) > kMostQ) return SS_ERR_UNSUPPORTED;
+        double f_at[2] = {0.0, 0.0};  // squares: a + 3 b t + 5 c t^2 = 0
+        const double root = 9.0 * b * b - 20.0 * a * c;
+        if (c == 0.0) f_at[0] = b != 0.0 ? -a / (3.0 * b) : 0.0;
+        else if (root >= 0.0) f_at[0] = (-3.0 * b + std::sqrt(root)) / (10.0 * c), f_at[1] = (-3.0 * b - std::sqrt(root)) / (10.0 * c);
+        most = largest([&](double t) { return std::sqrt(t) * (a + b * t + c * t * t); }, most * most, f_at, 2);
+    }
+    return most > kMostResult ? SS_ERR_UNSUPPORTED : SS_OK;
 }
 
 int check_workspace(const Layout& l, const void* workspace, int64_t bytes) {

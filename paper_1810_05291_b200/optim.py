@@ -160,7 +160,8 @@ class OrthogonalMomentum(torch.optim.Optimizer):
     For the weights of linear layers and convolutions (a parameter of more than two dimensions is the matrix of its first
     by all others); embeddings, heads and vectors are ``SignumVote``'s. ``scale``: ``"rms"``, 0.2 sqrt(max(rows, cols)), which
     gives the step the size of a step of Adam (0.2 a coordinate); ``"spectral"``, sqrt(max(1, rows / cols)); or a number.
-    ``coefficients``: (a, b, c) of each Newton-Schulz step.
+    ``coefficients``: (a, b, c) of each Newton-Schulz step, a s + b s^3 + c s^5 of each singular value s, which is at most 1 at
+    the start. Sets that could take it beyond 32 between steps, or whose ``a`` is below (|b| + |c|) / 64, the step refuses.
 
     Parameters are float32 and stay where they are; matrices of one shape and layout go through one call. A parameter
     without a gradient is left as it is. The gradients are taken as they are: workers of a group average theirs first.
