@@ -193,9 +193,11 @@ int ss_preference_loss(const void* logits, int64_t logits_stride, ss_dtype dt, i
  *   dx       out     [rows, width] of dt, or NULL; may be x in place
  *   dw       out     [vocab, width] of dw_dt, or NULL; fp32, or for bf16 inputs bf16 as well. With accumulate
  *                    (fp32 only) it is added to
- *   workspace        scratch of ss_linear_cross_entropy_workspace of the same arguments: about 1 GiB at the
- *                    most for the pieces, the rows that count, and where w is fp32 or its rows do not start on 16 bytes a
- *                    copy of it; a bf16 dw that more than one GiB's rows add to has its sums there too
+ *   workspace        scratch of ss_linear_cross_entropy_workspace of the same arguments. With a gradient 2 bytes a
+ *                    logit (bf16) or 10 (fp32) of a piece: all rows, up to a multiple of 64, or as many as take
+ *                    1 GiB, but 256 at least. And the rows that count; where w is fp32 or its rows do not start on 16 bytes, a
+ *                    copy of it (6 or 2 bytes an element); a bf16 dw to which more than one piece adds has its sums there, 4 bytes
+ *                    an element: 8192 x 4096 over 131072 takes 3.4 GB, more than its logits in bf16 (2.1 GB), with an fp32 dw 1.3 GB
  * targets, weights, inv_temperature, grad_scale as above. z_coef finite; 0 leaves its term out.
  * width, vocab >= 1 where there are rows. No rows: totals 0, dw 0 unless accumulate. More than 2^24 rows, 2^30 columns
  * or 2^24 tiles of 256 x 256 are SS_ERR_UNSUPPORTED.

@@ -851,7 +851,8 @@ int layout_of(const void* w, int64_t w_stride, ss_dtype dt, int64_t rows, int64_
     int64_t most = kChunkBytes / per_row / kProdTile * kProdTile;
     most = most < kProdTile ? kProdTile : (most > kMostChunkRows ? kMostChunkRows : most);
     l->chunks = rows > 0 ? (rows + most - 1) / most : 1;
-    l->chunk_rows = up_to((rows + l->chunks - 1) / l->chunks, kProdTile);
+    // whole tiles, so that only the last piece has one that is not full; of one piece the rows that there are, up to a whole stage of dW's contraction
+    l->chunk_rows = up_to((rows + l->chunks - 1) / l->chunks, l->chunks > 1 ? kProdTile : kProdK);
     l->row_cap = l->chunks * l->chunk_rows;
     l->sums_w = dw && dw_dt == SS_BF16 && l->chunks > 1;
     int64_t at = 0;
