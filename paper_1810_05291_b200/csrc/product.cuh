@@ -211,7 +211,9 @@ constexpr uint32_t kNanBits = 0x7FC00000u;
 // columns of a unit and gets each chunk in squares of 32 x 32 in its shared memory: fetch(column) before they have come,
 // square(column, ..., its sums, first chunk?). With EPI::kPacks a tile may take 64 columns at a time, rounded to 16 bits:
 // packed(column, ...). EPI::kBefore: before(...) is work for the outgoing warps while the first sums form. EPI::kAhead: registers allow two squares' fetches. EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
-// A wait that ran out (each is bounded) shows as NaN in place of all sums from there on.
+// A wait that ran out (each is bounded) shows as NaN in place of all sums from there on. The copying warp then copies nothing more, an outgoing one
+// says no more that it has brought sums out, and the issuing one, which goes on with what there is, does not say that sums have been formed: so none that are half done
+// are taken for whole ones, in this block or the pair's other one. (The answer of each wait, asked before each stage's products, cost 2 to 10 %.)
 template <class EPI, bool A_MN, bool B_MN, bool PAIR>
 __global__ void __launch_bounds__(kProdThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ Product p,
@@ -288,7 +290,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) arrive(added + (chunk & 1) * 8);
+                    if (lane == 0 && ok) arrive(added + (chunk & 1) * 8);
                 }
                 if (!ok) {
 #pragma unroll
@@ -362,7 +364,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) arrive(added + (chunk & 1) * 8);
+                    if (lane == 0 && ok) arrive(added + (chunk & 1) * 8);
                     first = false;
                 }
             }
@@ -377,7 +379,8 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
             else tma_load_3d(dst, map, bar, x, y, z);
         };
         const bool leader = elect_one();
-        int it = 0, slot = 0;
+        bool go = true;
+        int it = 0, slot = 0, issued = 0;
         uint32_t parity = 1;
         for (int unit = pair; unit < sc.units; unit += pairs) {
             const ProdUnit u = prod_unit(p, sc, unit);
@@ -391,10 +394,11 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
             }
 #pragma unroll 1
             for (int s = 0; s < u.stages; ++s) {
-                mbar_wait_uniform(empty + slot * 8, parity, &sh.abort);
+                go = __all_sync(0xFFFFFFFFu, mbar_wait_uniform(empty + slot * 8, parity, &sh.abort)) && go;
                 const uint32_t bar = full + slot * 8, dst = stages + slot * kStageBytes;
                 const int za = p.passes > 1 ? p.plane_a[pass] : u.batch, zb = p.passes > 1 ? p.plane_b[pass] : u.batch;
-                if (leader) {
+                if (go) if (leader) {
+                    issued = it + 1;
                     const uint32_t less = wide ? 0 : (PAIR ? (B_MN ? kProdPanel : 0) : kProdOperand);  // not copied
                     if (rank == 0) mbar_expect(smem_addr(&sh.full[0]) + slot * 8, (PAIR ? 2 : 1) * (kStageBytes - less));
                     if constexpr (A_MN) {
@@ -427,9 +431,9 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         // the last signals, and copies, arrive in this block's memory: not before that
         const int from = it > kStages ? it - kStages : 0;
         for (int i = from; i < it; ++i) mbar_wait_uniform(empty + i % kStages * 8, (i / kStages) & 1, &sh.abort);
-        if (*abort != 0 && rank == 0) {
+        if (leader && *abort != 0 && rank == 0) {
             int own = 0;
-            for (int i = from; i < it; ++i) mbar_wait(smem_addr(&sh.full[i % kStages]), (i / kStages) & 1, &own);
+            for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(smem_addr(&sh.full[i % kStages]), (i / kStages) & 1, &own);
         }
     } else if (rank == 0) {
         // ---- matrix unit
@@ -438,6 +442,7 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
         const uint64_t desc_b = B_MN ? tc_desc_rows(stages + kProdOperand, kProdPanel) : tc_desc_cols(stages + kProdOperand);
         const uint32_t full = smem_addr(&sh.full[0]), empty = smem_addr(&sh.empty[0]);
         const bool leader = elect_one();
+        bool go = true;
         auto commit = [](uint32_t bar) {
             if constexpr (PAIR) tc_commit_pair(bar);
             else tc_commit(bar);
@@ -450,7 +455,8 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                 const int n = min(left, p.chunk);
                 const uint32_t d = tmem + (chunk & 1) * kProdTile;
                 // the half of the tensor memory is free once the chunk before the last has been brought out
-                if (chunk >= 2) mbar_wait_uniform(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, &sh.abort);
+                if (chunk >= 2) go = __all_sync(0xFFFFFFFFu, mbar_wait_uniform(smem_addr(&sh.added[chunk & 1]), ((chunk >> 1) & 1) ^ 1, &sh.abort)) && go;
+                if (!go) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int s = 0; s < n; ++s) {
@@ -468,7 +474,8 @@ product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant_
                     __syncwarp();
                     if (++slot == kStages) slot = 0, parity ^= 1;
                 }
-                if (leader) commit(smem_addr(&sh.summed[chunk & 1]));
+                go = __all_sync(0xFFFFFFFFu, *abort == 0);
+                if (go) if (leader) commit(smem_addr(&sh.summed[chunk & 1]));
                 __syncwarp();
             }
         }
@@ -499,7 +506,7 @@ constexpr int kSmallTile = 128, kSmallStages = 3, kMostSmallStages = 6, kSmallOu
 static_assert(kSmallTile * kSmallTile * 4 <= kSmallStages * kProdStageBytes, "the sums take the place of the operands");
 
 struct SmallShared {
-    uint64_t full[kMostSmallStages], empty[kMostSmallStages], summed;
+    uint64_t full[kMostSmallStages], empty[kMostSmallStages], summed, last;
     uint32_t tmem;
     int abort;
 };
@@ -513,6 +520,7 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
     const uint32_t stages = (smem_addr(dynamic) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ring = p.ring, blocks = p.small, rank = blockIdx.x % blocks;
+    volatile int* abort = &sh.abort;
 
     next_may_begin();
     ProdUnit u;
@@ -537,6 +545,7 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
             mbar_init(smem_addr(&sh.empty[s]), 1);
         }
         mbar_init(smem_addr(&sh.summed), 1);
+        mbar_init(smem_addr(&sh.last), 1);
         sh.abort = 0;
         mbar_init_visible();
     }
@@ -556,7 +565,7 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
         auto square = [&](int j) { return stages + (4 * quarter + j) * kProdSquare; };
         const int fetched = mine(j0) ? j0 : (mine(j0 + 1) ? j0 + 1 : -1);
         if (fetched >= 0) tile.fetch(epi, 32 * fetched, f);
-        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed), 0, &sh.abort));
+        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&sh.summed), 0, abort));
         tc_fence_after();
 #pragma unroll 1
         for (int j = j0; j < j0 + 2; ++j) {
@@ -600,13 +609,15 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
         if (warp == kSmallOut / 32) {
             // ---- copies
             const bool leader = elect_one();
-            int slot = 0, k0 = u.first * kProdK;
+            bool go = true;
+            int slot = 0, k0 = u.first * kProdK, issued = 0;
             uint32_t parity = 1;
 #pragma unroll 1
             for (int s = 0; s < u.stages; ++s, k0 += kProdK) {
-                mbar_wait_uniform(smem_addr(&sh.empty[0]) + slot * 8, parity, &sh.abort);
+                go = __all_sync(0xFFFFFFFFu, mbar_wait_uniform(smem_addr(&sh.empty[0]) + slot * 8, parity, &sh.abort)) && go;
                 const uint32_t bar = smem_addr(&sh.full[0]) + slot * 8, dst = stages + slot * kProdStageBytes;
-                if (leader) {
+                if (go) if (leader) {
+                    issued = s + 1;
                     mbar_expect(bar, kProdStageBytes);
                     if constexpr (A_MN) {
                         tma_load_3d(dst, &a_map, bar, u.m0, k0, u.batch);
@@ -625,9 +636,9 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
                 if (++slot == ring) slot = 0, parity ^= 1;
             }
             // A copy may still be under way only if a wait ran out: it has to arrive before the block ends.
-            if (*static_cast<volatile int*>(&sh.abort) != 0) {
+            if (leader && *abort != 0) {
                 int own = 0;
-                for (int i = u.stages > ring ? u.stages - ring : 0; i < u.stages; ++i)
+                for (int i = issued > ring ? issued - ring : 0; i < issued; ++i)
                     mbar_wait(smem_addr(&sh.full[i % ring]), (i / ring) & 1, &own);
             }
         } else {
@@ -652,9 +663,10 @@ small_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
                 if (++slot == ring) slot = 0, parity ^= 1;
             }
             // nothing may still be running when its results are read, the operands' place is taken and the tensor memory given back
-            if (leader) tc_commit(smem_addr(&sh.summed));
+            const uint32_t end = smem_addr(__all_sync(0xFFFFFFFFu, *abort == 0) ? &sh.summed : &sh.last);
+            if (leader) tc_commit(end);
             int own = 0;
-            mbar_wait(smem_addr(&sh.summed), 0, &own);
+            mbar_wait(end, 0, &own);
         }
         __syncwarp();
         if (blocks > 1) cluster_sync();

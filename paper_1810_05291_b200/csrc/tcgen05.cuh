@@ -69,18 +69,20 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return false;
 }
 
-// The same for a warp whose control flow has to stay uniform: gives no answer. When it gave up, or
-// *abort was up before, its caller goes on; further waits of the block end at once.
-__device__ __forceinline__ void mbar_wait_uniform(uint32_t bar, uint32_t parity, const int* abort) {
+// The same for a warp whose control flow has to stay uniform: its caller goes on whatever the answer, and further waits of the
+// block that would take a while end at once.
+__device__ __forceinline__ bool mbar_wait_uniform(uint32_t bar, uint32_t parity, const int* abort) {
+    uint32_t ok;
     asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .u32 n, f;\n\tmov.u32 n, 0;\n"
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n, f;\n\tmov.u32 n, 0;\n"
         "TRY:\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%0], %1;\n\t@p bra DONE;\n\t"
-        "ld.volatile.shared.u32 f, [%2];\n\tsetp.ne.u32 p, f, 0;\n\t@p bra DONE;\n\t"
-        "add.u32 n, n, 1;\n\tsetp.lt.u32 p, n, %3;\n\t@p bra TRY;\n\t"
-        "st.volatile.shared.u32 [%2], 1;\n"
-        "DONE:\n\t}"
-        ::"r"(bar), "r"(parity), "r"(smem_addr(abort)), "n"(kMaxTries) : "memory");
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+        "ld.volatile.shared.u32 f, [%3];\n\tsetp.ne.u32 q, f, 0;\n\t@q bra DONE;\n\t"
+        "add.u32 n, n, 1;\n\tsetp.lt.u32 q, n, %4;\n\t@q bra TRY;\n\t"
+        "st.volatile.shared.u32 [%3], 1;\n"
+        "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(smem_addr(abort)), "n"(kMaxTries) : "memory");
+    return ok != 0;
 }
 
 // One lane of a converged warp.
