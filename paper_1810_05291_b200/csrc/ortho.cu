@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
     extern __shared__ uint8_t dynamic[];
     __shared__ uint64_t bar, came, handed;
     __shared__ uint32_t tmem_address;
-    __shared__ int abort;
+    __shared__ int gave_up[2];
     __shared__ double norm_part;
     const uint32_t xs = (smem_addr(dynamic) + 1023u) & ~1023u, ss_ = xs + kHeldX, qs = ss_ + kHeldS, ps = qs + 2 * kHeldS;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, half = warp >> 2;
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
         mbar_init(smem_addr(&bar), 1);
         mbar_init(smem_addr(&came), 1);
         mbar_init(smem_addr(&handed), 1);
-        abort = 0;
+        gave_up[0] = gave_up[1] = 0;
         mbar_init_visible();
     }
     if (warp == 0) tmem_alloc(smem_addr(&tmem_address), 512);
@@ -544,21 +544,29 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
     const uint32_t tmem = tmem_address, lanes = static_cast<uint32_t>(quarter * 32) << 16;
     const float inverse = a.unscale * a.unscale;
     uint32_t parity = 0;
+    // Each wait is bounded. A warp whose wait ran out writes NaN from there on, into the operands too, which take it to all others. The first
+    // warp, which issues products and copies, gives up only after a whole wait of its own, never because others did, and issues nothing more: so
+    // nothing of this block's is under way, nor anything that others sent it, when it has gone through the rest.
     bool ok = true;
+    auto wait = [&](uint64_t* barrier, uint32_t phase) {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(barrier), phase, &gave_up[warp == 0])) && ok;
+        if (!ok) gave_up[0] = 1;
+    };
+    auto unless_late = [&](float v) { return ok ? v : __uint_as_float(kNanBits); };
     // one warp issues, all wait for the products to have ended
     auto products = [&](auto issue) {
         smem_to_async();
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        if (warp == 0) {
+        if (warp == 0 && ok) {
             if (elect_one()) {
                 issue();
                 tc_commit(smem_addr(&bar));
             }
             __syncwarp();
         }
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&bar), parity, &abort)) && ok;
+        wait(&bar, parity);
         parity ^= 1;
         tc_fence_after();
     };
@@ -569,7 +577,6 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
 
     if (blocks > 1) cluster_arrive();
     for (int step = 0; step < a.steps; ++step) {
-        const float ca = a.coefficients[3 * step], cb = a.coefficients[3 * step + 1], cc = a.coefficients[3 * step + 2];
         // ---- the operand: rows of 64 elements in panels, wide: [l / 64][i][l % 64], tall: [i / 64][l][i % 64]
         {
             const int r = TALL ? half * 128 + i_or_l : i_or_l;
@@ -591,6 +598,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
         });
         // ---- S as an operand: rows of 128, in two panels of 64. This thread: row i_or_l, columns 64 half on
         if (blocks == 1) {
+            const float by = unless_late(inverse);
 #pragma unroll
             for (int c = 0; c < 8; c += 2) {
                 uint32_t r[16];
@@ -599,7 +607,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                 uint2 w[4];
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
-                    w[d] = half4(make_float4(inverse * __uint_as_float(r[4 * d]), inverse * __uint_as_float(r[4 * d + 1]), inverse * __uint_as_float(r[4 * d + 2]), inverse * __uint_as_float(r[4 * d + 3])));
+                    w[d] = half4(make_float4(by * __uint_as_float(r[4 * d]), by * __uint_as_float(r[4 * d + 1]), by * __uint_as_float(r[4 * d + 2]), by * __uint_as_float(r[4 * d + 3])));
 #pragma unroll
                 for (int d = 0; d < 2; ++d)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(ss_ + half * kHeldSide * 128, i_or_l, c + d)), "r"(w[2 * d].x), "r"(w[2 * d].y), "r"(w[2 * d + 1].x), "r"(w[2 * d + 1].y) : "memory");
@@ -614,6 +622,10 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                 uint32_t w[16];
                 tmem_load16(tmem + lanes + half * 64 + c * 4, w);
                 tmem_load_wait();
+                if (!ok) {
+#pragma unroll
+                    for (int d = 0; d < 16; ++d) w[d] = kNanBits;
+                }
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
                     turn_put(ps, i_or_l, half * 16 + c + d, make_float4(__uint_as_float(w[4 * d]), __uint_as_float(w[4 * d + 1]), __uint_as_float(w[4 * d + 2]), __uint_as_float(w[4 * d + 3])));
@@ -621,14 +633,15 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
             const uint32_t share = kHeldSide / blocks;  // rows; a multiple of 8
             smem_to_async();
             __syncthreads();
-            if (tid == 0) {
+            if (tid == 0 && ok) {
                 mbar_expect(smem_addr(&came), (blocks - 1) * share * 512);
                 for (uint32_t d = 1; d < blocks; ++d) {
                     const uint32_t q = (rank + d) % blocks;
                     bulk_to_cluster(cluster_addr(qs + rank * share * 512, q), ps + q * share * 512, share * 512, cluster_addr(smem_addr(&came), q));
                 }
             }
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&came), step & 1, &abort)) && ok;
+            wait(&came, step & 1);
+            const float by = unless_late(inverse);
             for (uint32_t e = tid; e < share * 16; e += kHeldThreads) {  // eight columns to a thread
                 const uint32_t r = e >> 4, c = e & 15;
                 float v[8];
@@ -640,12 +653,12 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                     const float4 y = turn_get(at, r, 2 * c), z = turn_get(at, r, 2 * c + 1);
                     v[0] += y.x, v[1] += y.y, v[2] += y.z, v[3] += y.w, v[4] += z.x, v[5] += z.y, v[6] += z.z, v[7] += z.w;
                 }
-                const uint2 lo = half4(make_float4(inverse * v[0], inverse * v[1], inverse * v[2], inverse * v[3])), hi = half4(make_float4(inverse * v[4], inverse * v[5], inverse * v[6], inverse * v[7]));
+                const uint2 lo = half4(make_float4(by * v[0], by * v[1], by * v[2], by * v[3])), hi = half4(make_float4(by * v[4], by * v[5], by * v[6], by * v[7]));
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(held_chunk(ss_ + (c >> 3) * kHeldSide * 128, rank * share + r, c & 7)), "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y) : "memory");
             }
             smem_to_async();
             __syncthreads();
-            if (tid == 0) {
+            if (tid == 0 && ok) {
                 mbar_expect(smem_addr(&handed), (blocks - 1) * share * 256);
                 for (uint32_t d = 1; d < blocks; ++d) {
                     const uint32_t q = (rank + d) % blocks;
@@ -655,7 +668,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                     }
                 }
             }
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_addr(&handed), step & 1, &abort)) && ok;
+            wait(&handed, step & 1);
         }
         // ---- Q = b S + c S S
         products([&] {
@@ -665,6 +678,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
                 tc_mma_f16(tmem, d, d, kIdescCols, k != 0);
             }
         });
+        const float cb = unless_late(a.coefficients[3 * step + 1]), cc = a.coefficients[3 * step + 2];
 #pragma unroll
         for (int c = 0; c < 8; c += 2) {
             uint32_t r[16];
@@ -698,6 +712,7 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
             }
         });
         if (blocks > 1 && step + 1 < a.steps) cluster_arrive();
+        const float ca = unless_late(a.coefficients[3 * step]);
 #pragma unroll
         for (int j = 0; j < 128; j += 16) {
             uint32_t r[16];
@@ -706,10 +721,6 @@ __global__ void __launch_bounds__(kHeldThreads, 1) ortho_held_kernel(const __gri
 #pragma unroll
             for (int d = 0; d < 16; ++d) x[j + d] = ca * x[j + d] + __uint_as_float(r[d]);
         }
-    }
-    if (!ok) {
-#pragma unroll
-        for (int j = 0; j < 128; ++j) x[j] = __uint_as_float(kNanBits);
     }
     // ---- out
     {
