@@ -169,22 +169,32 @@ class OrthogonalMomentum(torch.optim.Optimizer):
 
     def __init__(self, params, lr: float = 3e-4, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
                  scale="rms", coefficients=None, kernels=None):
-        if not (lr >= 0.0 and weight_decay >= 0.0 and 0.0 <= momentum < 1.0):
-            raise ValueError("need lr >= 0, weight_decay >= 0 and 0 <= momentum < 1")
-        if scale not in ("rms", "spectral") and not isinstance(scale, (int, float)):
-            raise ValueError("scale must be 'rms', 'spectral' or a number")
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, scale=scale))
         if kernels is None:
             from . import binding as kernels
             kernels.lib()
         self.B = kernels
         self.coefficients = kernels.ORTHO_COEFFICIENTS if coefficients is None else tuple(tuple(map(float, c)) for c in coefficients)
-        for g in self.param_groups:
-            for p in g["params"]:
-                if p.dtype != torch.float32 or p.dim() < 2:
-                    raise ValueError("parameters must be float32 matrices, or tensors of more dimensions")
-                if self._matrix(p.detach()) is None:
-                    raise ValueError("a parameter's rows must be contiguous and not overlap")
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        try:
+            self._check(self.param_groups[-1])
+        except ValueError:
+            self.param_groups.pop()
+            raise
+
+    @classmethod
+    def _check(cls, group) -> None:
+        if not (group["lr"] >= 0.0 and group["weight_decay"] >= 0.0 and 0.0 <= group["momentum"] < 1.0):
+            raise ValueError("need lr >= 0, weight_decay >= 0 and 0 <= momentum < 1")
+        if group["scale"] not in ("rms", "spectral") and not isinstance(group["scale"], (int, float)):
+            raise ValueError("scale must be 'rms', 'spectral' or a number")
+        for p in group["params"]:
+            if p.dtype != torch.float32 or p.dim() < 2:
+                raise ValueError("parameters must be float32 matrices, or tensors of more dimensions")
+            if cls._matrix(p.detach()) is None:
+                raise ValueError("a parameter's rows must be contiguous and not overlap")
 
     @staticmethod
     def _matrix(t: torch.Tensor) -> Optional[torch.Tensor]:
@@ -192,7 +202,7 @@ class OrthogonalMomentum(torch.optim.Optimizer):
         if t.dim() > 2:
             if not t.is_contiguous():
                 return None
-            t = t.view(t.shape[0], -1)
+            t = t.view(t.shape[0], math.prod(t.shape[1:]))
         fits = (t.stride(1) == 1 or t.shape[1] < 2) and (t.stride(0) >= t.shape[1] or t.shape[0] < 2)
         return t if fits else None
 
