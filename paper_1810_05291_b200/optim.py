@@ -164,8 +164,9 @@ class OrthogonalMomentum(torch.optim.Optimizer):
     the start. Sets that could take it beyond 32 between steps, or whose ``a`` is below (|b| + |c|) / 64, the step refuses.
 
     Parameters are float32 and stay where they are; matrices of one shape and layout go through one call. A parameter
-    without a gradient is left as it is. The gradients are taken as they are: workers of a group average theirs first.
-    ``kernels`` replaces the CUDA binding (host-side tests)."""
+    without a gradient is left as it is. The gradients are taken as they are, and nothing notices workers
+    whose gradients differ: those of a group average theirs first (``dist.all_reduce(p.grad); p.grad /= world``, or
+    ``DistributedDataParallel``), and stay one model. ``kernels`` replaces the CUDA binding (host-side tests)."""
 
     def __init__(self, params, lr: float = 3e-4, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
                  scale="rms", coefficients=None, kernels=None):
