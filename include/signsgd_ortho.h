@@ -12,7 +12,7 @@
  * products are formed over the smaller side. With (3.4445, -4.7750, 2.0315) five times (the default of
  * the Python side) a singular value of X_0 from 0.01 on ends between 0.67 and 1.21.
  *
- * Numerics. |u| in fp64, X in fp32. The products' operands are fp16 (11 significant bits), scaled by a power of
+ * Numerics. |u| from squares that each thread sums in fp32, all threads' sums in fp64 (in fp64 throughout where those leave fp32's range); X in fp32. The products' operands are fp16 (11 significant bits), scaled by a power of
  * two so that their values lie well inside its range, with fp32 sums; the term a X takes X unrounded, so that directions with
  * small singular values are not lost in the rounding of large ones. Of a result O about 2e-3 (2-norm) is rounding with those coefficients; with others
  * a step adds 2^-11 (|b| s^3 + |c| s^5) or so to a direction of singular value s. Coefficients with which the operands could leave their range are refused

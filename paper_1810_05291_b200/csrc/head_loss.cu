@@ -15,10 +15,10 @@
 // of bf16 logits is; the entry of the target, which is a difference, is formed in fp32 from log p. With fp32 inputs e
 // is fp32 and P the sum of three bf16.
 //
-// What bounds it. 8192 x 4096 over 131072 bf16: 19.7 to 22.5 ms at the power limit (1340 to 1170 TFLOP/s; the library's
+// What bounds it. 8192 x 4096 over 131072 bf16: 21.7 to 23.2 ms at the power limit (1220 to 1140 TFLOP/s; the library's
 // product alone, back to back, 1407), the matrix unit active 91, 93 and 84 % of the logits', dx's and dW's time, e -> P
-// 0.85 ms of it at 5.1 TB/s. 64 x 1024 over 32000 bf16: 69 us in a row of calls, W read twice and dW written in 52 of them, the rest five starts.
-// 1021 x 770 over 32001 fp32: 850 us, six passes in 1300 to 1440 TFLOP/s, 120 us to split W and P into terms.
+// 0.87 ms of it at 4.9 TB/s. 64 x 1024 over 32000 bf16: 69 us in a row of calls, W read twice and dW written in 55 of them, the rest five starts.
+// 1021 x 770 over 32001 fp32: 820 us alone, 946 to 1003 in a row of calls at the power limit; alone six passes in 690 us, 1310 TFLOP/s, and 125 to split W and P into terms.
 #include "product.cuh"
 
 #include <cmath>
@@ -34,7 +34,7 @@ constexpr int kPartCols = kProdHalf;              // logits of a thread
 //   4100 x 2048 over 65536       1767 us          1755 us          1850 us
 //   8192 x 4096 over 131072      22.1 ms          22.3 ms          22.9 ms
 // With fewer the two halves of the tensor memory fill while a tile's exponentials are formed. That costs nothing where the stages come at the
-// memory's rate (at most 128 rows) or bring six products each (fp32):
+// memory's rate (at most 128 rows) or bring six products each (fp32; few calls, below the power limit):
 //                                16               4                2
 //   64 x 1024 over 32000 bf16    69 us, 2.5e-6    68 us, 6e-7      69 us, 3e-7
 //   1021 x 770 over 32001 fp32   897 us, 2.2e-6   878 us, 7e-7     875 us, 5e-7
@@ -42,7 +42,7 @@ constexpr int kLogitChunk = 12, kLogitChunkSlow = 2;
 // Stages that it sums of a gradient: 16384 contraction indices lose 2e-5, nothing next to an operand of bf16. Of each of fp32's passes 1024 indices:
 // dx and dW of 1021 x 770 over 32001 are off by 1.2e-6 (2.4e-6 with 2048, plain fp32 products 1.6e-6), in the same time.
 constexpr int kGradChunk = 256, kGradChunkF32 = 16;
-constexpr int64_t kChunkBytes = int64_t(1) << 30; // of e and P
+constexpr int64_t kChunkBytes = int64_t(1) << 30; // of e and P, or kProdTile rows of them
 constexpr int64_t kMostChunkRows = 16384;
 
 __device__ __forceinline__ float ex2(float x) {

@@ -10,10 +10,10 @@
 // 0.03 %. (As the sum of two fp16, the first of them the operand, X has two bytes less to move for each element and
 // step and 22 bits, but takes seven instructions more: the same time within 2 %.)
 //
-// What bounds it. 4096 x 4096 bf16: 1140 us alone, 1350 in a row of calls at the power limit; S and Q take 52 to 57 us each (136
-// tiles in two rounds of 74 pairs, the matrix unit active 75 %), X + Q X 98 to 105 (79 %), the two passes of the start 42. Twelve of 4096 x 1024
-// with momenta and parameters: 1270 us, X + Q X 125 of them each, where its products alone take 62 and its 600 MB 92.
-// 1000 x 2048: 150 us, 15 products of 8 to 10 us one after another. 128 x 128: 24 us in one launch.
+// What bounds it. 4096 x 4096 bf16: 1140 us alone, 1330 to 1400 in a row of calls at the power limit; alone S and Q take 54 to 58 us each (136
+// tiles in two rounds of 74 pairs, the matrix unit active 75 %), X + Q X 101 to 109 (79 %), the two passes of the start 40. Twelve of 4096 x 1024
+// with momenta and parameters: 1260 us alone, 1420 to 1500 in a row; alone X + Q X takes 125 of them each, where its products alone take 62 and its 600 MB 92.
+// 1000 x 2048: 151 us, 15 products of 8 to 10 us one after another. 128 x 128: 25 us in one launch.
 #include "../../include/signsgd_ortho.h"
 #include "product.cuh"
 
@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
 // thread has 128 neighbouring elements of a row, in memory's order: rows are the shorter side's indices i, or l where the matrix is tall)
 // and as fp16 operand in shared memory. A step is three products within the block; between them S is summed over the cluster, each
 // block a share of its rows, which it hands to all. A step takes one block 3 us (0.45 to write the operand, 0.5, 0.45 and 0.45 for the
-// products from start to end, 0.3, 0.45 and 0.7 to bring their sums out), eight 7; 128 x 128 24 us, 128 x 2048 46, 128 x 4096 52, as 15 products of
-// their own 98, 140 and 145. Loading, the norm and storing take 6.
+// products from start to end, 0.3, 0.45 and 0.7 to bring their sums out), eight 7; in a row of calls 128 x 128 takes 25 us, 128 x 2048 49, 128 x 4096 54, as 15
+// products of their own 98, 140 and 145. Loading, the norm and storing take 6.
 constexpr int kHeldSide = 128, kHeldLong = 256, kHeldThreads = 256, kMostHeldBlocks = 16, kPortableBlocks = 8;
 constexpr uint32_t kHeldX = kHeldSide * kHeldLong * 2, kHeldS = kHeldSide * kHeldSide * 2, kHeldPart = kHeldSide * kHeldSide * 4;
 // X; S; Q, whose place the others' shares of S take before it is formed, and 32 KB more of those; this block's part of S

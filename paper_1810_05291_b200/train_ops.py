@@ -300,8 +300,10 @@ def linear_cross_entropy(x, weight, targets, weights, inv_temperature: float = 1
     sum of lse^2 (``z_coef`` times it is in the loss) and the positions' log probabilities.
 
     Where gradients can be asked for they are formed with the loss, in one go: that takes three products with the
-    head, where forming the logits again in the backward pass would take four. The backward pass multiplies them by the
-    gradient that arrives. With ``into_grad`` it adds the weight's to ``weight.grad`` itself, as in ``linear8``."""
+    head, where forming the logits again in the backward pass would take four. They are held until the backward pass, which
+    multiplies them by the gradient that arrives, in 32 bits; those in bfloat16 are rounded when they are formed and again there (which
+    changes nothing where that gradient is a power of two). With ``into_grad`` it adds the weight's to ``weight.grad`` itself, as in
+    ``linear8``, out of the fp32 one that it holds."""
     if torch.is_autocast_enabled(x.device.type) and x.dtype != torch.float64:
         x = x.to(torch.get_autocast_dtype(x.device.type))
     on = torch.is_grad_enabled()
