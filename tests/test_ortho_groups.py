@@ -54,3 +54,10 @@ def test_a_parameter_without_elements():
     for p in ps:
         p.grad = torch.zeros_like(p)
     opt.step()
+
+
+def test_a_group_whose_options_cannot_be_compared():
+    opt = optimiser([matrix()])
+    with pytest.raises(TypeError):
+        opt.add_param_group(dict(params=[matrix()], lr="0.1"))
+    assert len(opt.param_groups) == 1
