@@ -213,7 +213,8 @@ constexpr uint32_t kNanBits = 0x7FC00000u;
 // packed(column, ...). EPI::kBefore: before(...) is work for the outgoing warps while the first sums form. EPI::kAhead: registers allow two squares' fetches. EPI::kSmall: it also ends the small products below; EPI::kAlone: those of blocks alone.
 // A wait that ran out (each is bounded) shows as NaN in place of all sums from there on. The copying warp then copies nothing more, an outgoing one
 // says no more that it has brought sums out, and the issuing one, which goes on with what there is, does not say that sums have been formed: so none that are half done
-// are taken for whole ones, in this block or the pair's other one. (The answer of each wait, asked before each stage's products, cost 2 to 10 %.)
+// are taken for whole ones, in this block or the pair's other one. (The answer of each wait, asked before each stage's products, cost 2 to 10 %; and what is asked stands in an `if`
+// of its own before that of the elected lane, which the compiler has to recognise to keep operands in uniform registers.)
 template <class EPI, bool A_MN, bool B_MN, bool PAIR>
 __global__ void __launch_bounds__(kProdThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ Product p,
